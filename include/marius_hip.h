@@ -203,6 +203,89 @@ int mar_rank_metrics_static(const int32_t* ranks, int64_t n_ranks, const int32_t
                             double* out, void* hip_stream);
 
 /*
+ * Operators on whole tables.  They need no context: matrices are plain rows of any of the types below with any stride
+ * (in elements, at least the row's width), aligned to their type alone.
+ */
+#define MAR_DTYPE_FP32 0
+#define MAR_DTYPE_BF16 1
+#define MAR_DTYPE_FP16 2
+
+/*
+ * Dropout of rows x dim values: every value is dropped (0, also where it is not finite) with probability p or multiplied
+ * by 1 / (1 - p).  p is rounded to a multiple of 2^-16, at most 65535 / 65536, and so is 1 - p, so that the expectation
+ * is kept.  The mask depends on (seed, step, row, column) alone, not on type or strides: columns 8 g .. 8 g + 7 of row r
+ * take the eight 16-bit halves, lower half first, of the Philox4x32-10 block with key = seed and counter =
+ * (r, g, step lo, 0xC0000000 | step hi), and a value is kept where its half is at least round(65536 p).  Nothing is
+ * stored: the backward pass is the same call on the gradient.
+ *   x, out           : device, rows of dim values; out == x with equal strides works in place, other overlaps do not
+ *   rows < 2^31, dim >= 1, step < 2^62
+ */
+int mar_dropout(const void* x, int64_t x_stride, int64_t rows, int32_t dim, int32_t dtype, float p, uint64_t seed,
+                uint64_t step, void* out, int64_t out_stride, void* hip_stream);
+
+/*
+ * Softmax over ALL rows of a table: query i gives row j the score s_ij = scale * (query_i . row_j).  For the bilinear score
+ * functions a query is the edge's operand of everything but the replaced endpoint (DistMult: theta_s * theta_r; ComplEx:
+ * theta_s theta_r as [re | im] for destinations; Dot: theta_s) and the table is the node embeddings.
+ * Products of bf16 and fp16 values are exact and summed in fp32; fp32 values are taken as the sum of two scaled f16
+ * numbers (as accurate as fp32).  Scores that are not finite make the results of their query NaN or infinite.
+ */
+#define MAR_SOFTMAX_MAX_ROWS    ((int64_t)0x7fffff00)
+#define MAR_SOFTMAX_MAX_QUERIES 0x7fffff00
+#define MAR_MAX_TOP 32
+typedef struct mar_softmax {
+  int64_t num_rows;      /* rows of the table, 1 .. MAR_SOFTMAX_MAX_ROWS            */
+  int64_t row_stride;    /* elements from one row to the next, dim .. 2^30          */
+  int64_t query_stride;  /* the queries'                                            */
+  int32_t num_queries;   /* 0 .. MAR_SOFTMAX_MAX_QUERIES                            */
+  int32_t dim;           /* 1 .. MAR_MAX_DIM                                        */
+  int32_t dtype;         /* MAR_DTYPE_* of queries, table and their gradients       */
+  float   scale;         /* multiplies every score (1 / temperature): 1e-6 .. 1e6   */
+} mar_softmax;
+
+/*
+ * Log probabilities of given rows, with the entropy of every query's distribution and its most probable rows.
+ *   queries, table : device
+ *   targets        : device, [num_queries] row ids, or NULL.  An id outside the table: log probability 0 (none asked for).
+ *   allowed        : device, or NULL (all rows): bit j % 32 of word j / 32 says whether row j counts for the query
+ *                    whose words begin at allowed + i * allowed_stride (0: the same words for all queries).  Rows that do
+ *                    not count have probability 0, whatever their values.
+ *   num_top        : 0 .. MAR_MAX_TOP most probable rows
+ *   log_probs      : device, out, [num_queries], or NULL; -infinity where the target is not allowed
+ *   entropy        : device, out, [num_queries], or NULL: -sum p log p in natural units
+ *   top_ids, top_log_probs : device, out, [num_queries][num_top], by descending probability; scores are compared in
+ *                    64 bits, equal ones ordered by id.  Where fewer rows count: id -1, log probability -infinity.
+ *   workspace      : device, >= mar_log_probs_workspace_bytes of the same problem and num_top, 256-byte aligned; calls
+ *                    that may overlap in time need one each
+ * A query without an allowed row: log probability -infinity, entropy 0, no top rows.
+ */
+int mar_log_probs_workspace_bytes(const mar_softmax* problem, int32_t num_top, size_t* out_bytes);
+int mar_log_probs(const mar_softmax* problem, const void* queries, const void* table, const int32_t* targets,
+                  const uint32_t* allowed, int64_t allowed_stride, int32_t num_top, float* log_probs, float* entropy,
+                  int32_t* top_ids, float* top_log_probs, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Softmax cross entropy over all rows and its gradients: Eq. 1 without the sampling approximation and with the positive in
+ * the sum.  loss_i = u_i (log sum_j exp s_ij - s_i,target), u_i the query's weight; the gradients are of the sum of all
+ * losses:
+ *     d queries_i = scale u_i (sum_j p_ij row_j - row_target),   d table_j = scale sum_i u_i (p_ij - [target_i = j]) query_i.
+ *   targets  : device, [num_queries]; a query whose id lies outside the table has weight 0: loss and gradient are 0, and its
+ *              values, finite or not, touch nothing else
+ *   weights  : device, [num_queries] of either sign, or NULL: 1
+ *   loss, lse: device, out, [num_queries] floats, each may be NULL; lse is the log-sum-exp of every query
+ *   grad_queries, grad_table : device, out, rows like the inputs' with their own strides, each may be NULL; overwritten.
+ *              They must not overlap the inputs.
+ *   workspace: device, >= mar_softmax_loss_workspace_bytes of the same problem, 256-byte aligned; calls that may overlap in
+ *              time need one each
+ * Sums are held in fp32 and formed in an order that depends on the problem alone (bit-reproducible); weights enter the
+ * gradients' products in the operands' 16 bits (fp32: as pairs), an answer's own weight in fp32.
+ */
+int mar_softmax_loss_workspace_bytes(const mar_softmax* problem, size_t* out_bytes);
+int mar_softmax_loss(const mar_softmax* problem, const void* queries, const void* table, const int32_t* targets, const float* weights,
+                     float* loss, float* lse, void* grad_queries, int64_t grad_query_stride, void* grad_table, int64_t grad_row_stride,
+                     void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Edge-bucket ordering for out-of-memory training (Sec. 4.1).  Host-only: all pointers are HOST memory.
  *   mar_beta_buffer_sequence  : Alg. 3.  Writes the sequence of partition buffers, row r = the c partition
  *                               ids in the buffer at step r; successive rows differ by one swapped

@@ -13,6 +13,8 @@ _lib = None
 
 MODEL_DISTMULT, MODEL_COMPLEX, MODEL_TRANSE, MODEL_DOT = 0, 1, 2, 3
 PRECISION_FP32, PRECISION_SPLIT_BF16 = 0, 1
+DTYPE_FP32, DTYPE_BF16, DTYPE_FP16 = 0, 1, 2
+MAX_TOP = 32
 NUM_PHASES = 6
 PHASE_NAMES = ("index", "gather", "score_softmax_gq", "neg_grad", "chain_rule", "reduce_adagrad")
 
@@ -37,9 +39,15 @@ class MarDebugOut(ctypes.Structure):
                 ("grad_rows", ctypes.c_void_p)]
 
 
+class MarSoftmax(ctypes.Structure):
+    _fields_ = [("num_rows", ctypes.c_int64), ("row_stride", ctypes.c_int64), ("query_stride", ctypes.c_int64),
+                ("num_queries", ctypes.c_int32), ("dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 EXPORTS = ("mar_workspace_bytes", "mar_init_tables", "mar_sample_negatives", "mar_train_batch", "mar_eval_scores",
            "mar_eval_filter", "mar_rank_metrics", "mar_rank_metrics_static", "mar_beta_buffer_sequence", "mar_beta_edge_bucket_order", "mar_buffer_simulate",
-           "mar_swap_lower_bound", "mar_beta_swap_count",
+           "mar_swap_lower_bound", "mar_beta_swap_count", "mar_dropout", "mar_log_probs_workspace_bytes", "mar_log_probs",
+           "mar_softmax_loss_workspace_bytes", "mar_softmax_loss",
            "mar_pipe_workspace_bytes", "mar_pipe_create", "mar_pipe_submit", "mar_pipe_drain", "mar_pipe_destroy",
            "mar_profile_enable", "mar_profile_read", "mar_destroy", "mar_last_error")
 
@@ -67,6 +75,11 @@ def load_library():
     lib.mar_eval_filter.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.mar_rank_metrics.argtypes = [vp, vp, i64, ctypes.POINTER(i32), i32, vp, vp]
     lib.mar_rank_metrics_static.argtypes = [vp, i64, ctypes.POINTER(i32), i32, vp, vp]
+    lib.mar_dropout.argtypes = [vp, i64, i64, i32, i32, ctypes.c_float, u64, u64, vp, i64, vp]
+    lib.mar_log_probs_workspace_bytes.argtypes = [ctypes.POINTER(MarSoftmax), i32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.mar_log_probs.argtypes = [ctypes.POINTER(MarSoftmax), vp, vp, vp, vp, i64, i32, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.mar_softmax_loss_workspace_bytes.argtypes = [ctypes.POINTER(MarSoftmax), ctypes.POINTER(ctypes.c_size_t)]
+    lib.mar_softmax_loss.argtypes = [ctypes.POINTER(MarSoftmax), vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, ctypes.c_size_t, vp]
     lib.mar_beta_buffer_sequence.argtypes = [i32, i32, vp, i64, ctypes.POINTER(i64)]
     lib.mar_beta_edge_bucket_order.argtypes = [i32, i32, i32, u64, vp]
     lib.mar_buffer_simulate.argtypes = [i32, i32, vp, i64, ctypes.POINTER(i64)]
@@ -162,6 +175,37 @@ def mar_rank_metrics(ctx, ranks, n_ranks, ks, out, stream=None):
 def mar_rank_metrics_static(ranks, n_ranks, ks, out, stream=None):
     arr = (ctypes.c_int32 * max(len(ks), 1))(*ks)
     _check(load_library().mar_rank_metrics_static(_ptr(ranks), int(n_ranks), arr, len(ks), _ptr(out), _stream(stream)))
+
+
+def mar_dropout(x, x_stride, rows, dim, dtype, p, seed, step, out, out_stride, stream=None):
+    _check(load_library().mar_dropout(_ptr(x), int(x_stride), int(rows), int(dim), int(dtype), float(p), int(seed), int(step),
+                                      _ptr(out), int(out_stride), _stream(stream)))
+
+
+def mar_log_probs_workspace_bytes(problem, num_top):
+    out = ctypes.c_size_t(0)
+    _check(load_library().mar_log_probs_workspace_bytes(ctypes.byref(problem), int(num_top), ctypes.byref(out)))
+    return out.value
+
+
+def mar_log_probs(problem, queries, table, targets, allowed, allowed_stride, num_top, log_probs, entropy, top_ids, top_log_probs,
+                  workspace, workspace_bytes, stream=None):
+    _check(load_library().mar_log_probs(ctypes.byref(problem), _ptr(queries), _ptr(table), _ptr(targets), _ptr(allowed),
+                                        int(allowed_stride), int(num_top), _ptr(log_probs), _ptr(entropy), _ptr(top_ids),
+                                        _ptr(top_log_probs), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def mar_softmax_loss_workspace_bytes(problem):
+    out = ctypes.c_size_t(0)
+    _check(load_library().mar_softmax_loss_workspace_bytes(ctypes.byref(problem), ctypes.byref(out)))
+    return out.value
+
+
+def mar_softmax_loss(problem, queries, table, targets, weights, loss, lse, grad_queries, grad_query_stride, grad_table,
+                     grad_row_stride, workspace, workspace_bytes, stream=None):
+    _check(load_library().mar_softmax_loss(ctypes.byref(problem), _ptr(queries), _ptr(table), _ptr(targets), _ptr(weights),
+                                           _ptr(loss), _ptr(lse), _ptr(grad_queries), int(grad_query_stride), _ptr(grad_table),
+                                           int(grad_row_stride), _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 def mar_swap_lower_bound(p, c):

@@ -7,21 +7,8 @@
 // follow are bit-reproducible.  The reduce reads segment borders off the sorted ids; ranks of the rows among the unique
 // rows and the ascending unique list are formed only where a caller asks for them.
 #include "mar_common.h"
+#include "mar_philox.h"
 #include "mar_sort_dev.h"
-
-// ---------------------------------------------------------------- Philox4x32-10 -----
-// Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3" (SC'11).
-__device__ __forceinline__ void philox4x32_10(uint32_t& c0, uint32_t& c1, uint32_t& c2, uint32_t& c3,
-                                              uint32_t k0, uint32_t k1) {
-#pragma unroll
-  for (int r = 0; r < 10; ++r) {
-    const uint32_t hi0 = __umulhi(0xD2511F53u, c0), lo0 = 0xD2511F53u * c0;
-    const uint32_t hi1 = __umulhi(0xCD9E8D57u, c2), lo1 = 0xCD9E8D57u * c2;
-    const uint32_t n0 = hi1 ^ c1 ^ k0, n2 = hi0 ^ c3 ^ k1;
-    c0 = n0; c1 = lo1; c2 = n2; c3 = lo0;
-    k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
-  }
-}
 
 // Negative sampling (Sec. 2.1; degree-based fraction of Table 1).  One thread per pair of
 // slots: counter = (slot >> 1, 2*chunk + side, step lo, step hi), key = seed; even slot takes

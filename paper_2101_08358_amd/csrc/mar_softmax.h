@@ -1,0 +1,45 @@
+// Softmax over all rows of a table (gfx950): arguments, plan and the contraction shared by log probabilities
+// (mar_softmax.hip) and by the loss with its gradients (mar_softmax_loss.hip).
+//
+// Scores are s = scale q . w for T queries and V rows.  A pass keeps "stationary" rows in registers (32 a wave and block), streams
+// the other matrix through LDS in tiles of 32 rows and takes a tile's scores with v_mfma_f32_32x32x16: A = the streamed rows from
+// LDS, B = the stationary rows, so that a lane holds 16 scores of its one stationary row and no statistic crosses lanes.
+//   PASS 0  stationary queries, streamed table: running reference, sum of weights and entropy sum, maxima of groups of rows
+//   PASS 1  stationary queries, streamed table: the same without the entropy, and O = sum of weights times rows
+//   PASS 2  stationary table rows, streamed queries: O = sum of weights times queries, with the finished log-sum-exp
+// bf16 and fp16 values go to the matrix pipe as they are; an fp32 value v is v 2^e = hi + lo, both f16 (mar_split.h), a product
+// three of theirs, with one exponent per stationary row and per eight streamed rows.
+//
+// Lane layouts (lane = 32 h + m = 16 g + i): A lane holds streamed row m, columns 16 s + 8 h .. + 7 of step s; B lane the same
+// columns of stationary row m; D lane holds stationary row m, register r = streamed row 8 (r / 4) + 4 h + r % 4.  Second product
+// O^T[c][x] += sum_y Y[y][c] P[y][x], 16 of the tile's rows a step: B = P as it lies in the registers, so slot j of half h stands for
+// row 16 s + 8 (j / 4) + 4 h + j % 4; A = Y^T by the LDS transpose read (mar_split.hip describes it).
+#pragma once
+#include "mar_common.h"
+#include "mar_split.h"
+
+constexpr int sm_nk(int d) { return d <= 32 ? 2 : (d <= 64 ? 4 : (d <= 112 ? 7 : (d <= 128 ? 8 : (d <= 192 ? 12 : (d <= 256 ? 16 : 25))))); }
+#define SM_TY 32                  // rows of a tile
+#define SM_NO_REF -3.0e38f        // reference of a row that has met no score yet
+
+struct SmArgs {
+  const void *X, *Y;               // stationary and streamed rows
+  int64_t x_stride, y_stride;
+  int32_t n_x, n_y, dim, nstripes, units;
+  int32_t parts, tps;              // parts of the streamed tiles, tiles each
+  float c;                         // scale log2(e)
+  float4* stats;                   // [parts][n_x]: reference (log2 units), sum of 2^(t - reference), sum of that times (t - reference)
+  float* gmax;                     // [n_x][ngroups]: largest t of a group of 16 group_tiles rows
+  int64_t ngroups;
+  int32_t group_tiles;
+  const uint32_t* allowed; int64_t allowed_stride;
+  const int32_t* targets;
+  float* O; int32_t o_pitch;       // [parts][n_x][o_pitch]
+  const float* row_m; const float* row_f; const float* row_u;   // pass 2: per query, see k_loss_rows
+  void* out; int64_t out_stride;   // pass 2 in one part: the gradient itself
+};
+
+struct SmPlan { int32_t qb, stripes, parts, tps, ntiles; };
+
+const char* sm_check(const mar_softmax* p, int* code);
+SmPlan sm_plan(int dtype, int dim, int pass, int64_t n_x, int64_t n_y, int multiple);

@@ -1,0 +1,188 @@
+// Softmax cross entropy over all rows of a table, with the gradients of queries and table (gfx950): pass 1 (statistics and the
+// weighted sum of rows for every query), k_loss_rows (joins the parts: log-sum-exp, loss, the queries' gradient), pass 2 (the
+// table's gradient, scores computed again), k_loss_table (adds its parts).
+#include "mar_softmax_dev.h"
+
+struct LossArgs {
+  const void *Q, *W; int64_t q_stride, w_stride;
+  int32_t n, dim, parts, o_pitch;
+  int64_t rows;
+  float scale; double unscale;     // natural units of a reference's: scale / c
+  const int32_t* targets; const float* weights;
+  const float4* stats; const float* O;
+  float *row_m, *row_f, *row_u;
+  int32_t log_f;                   // pass 2 takes log2 |u| - log2(sum) in place of u / sum
+  float *loss, *lse;
+  void* grad; int64_t grad_stride;
+};
+
+// A wave per query.
+template <int TYPE>
+__global__ void __launch_bounds__(256)
+k_loss_rows(LossArgs a) {
+  typedef typename RowType<TYPE>::T T;
+  const int lane = threadIdx.x & 63;
+  const int64_t q = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (q >= a.n) return;
+  float m = SM_NO_REF, l = 0.f;
+  for (int p = 0; p < a.parts; ++p) m = fmaxf(m, a.stats[(size_t)p * a.n + q].x);
+  for (int p = 0; p < a.parts; ++p) { const float4 s = a.stats[(size_t)p * a.n + q]; l += s.y * __builtin_amdgcn_exp2f(s.x - m); }
+  const int t = a.targets[q];
+  const bool has = t >= 0 && t < a.rows;
+  const float u = has ? (a.weights ? a.weights[q] : 1.f) : 0.f;
+  const T* qr = (const T*)a.Q + q * a.q_stride;
+  const T* wr = (const T*)a.W + (int64_t)(has ? t : 0) * a.w_stride;
+  double dot = 0.0;
+  for (int c = lane; c < a.dim; c += 64) dot = __builtin_fma((double)(float)qr[c], (double)(float)wr[c], dot);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) dot += __shfl_xor(dot, o);
+  const double lse = (double)m * a.unscale + (double)logf(l), over = dot * (double)a.scale - lse;   // log p of the answer
+  if (lane == 0) {
+    if (a.lse) a.lse[q] = (float)lse;
+    if (a.loss) a.loss[q] = u != 0.f ? (float)(-(double)u * over) : 0.f;
+    if (a.row_m) {
+      const float us = u * a.scale;
+      a.row_m[q] = u != 0.f ? m : 0.f;
+      a.row_u[q] = us;
+      a.row_f[q] = a.log_f ? (us != 0.f ? __builtin_amdgcn_logf(fabsf(us)) - __builtin_amdgcn_logf(l) : -__builtin_inff()) : (us != 0.f ? us / l : 0.f);
+    }
+  }
+  if (!a.grad) return;
+  T* out = (T*)a.grad + q * a.grad_stride;
+  const float less = expm1f((float)over), us = u * a.scale;
+  for (int c = lane; c < a.dim; c += 64) {
+    float sum = 0.f;
+    for (int p = 0; p < a.parts; ++p) sum += a.O[((size_t)p * a.n + q) * a.o_pitch + c] * __builtin_amdgcn_exp2f(a.stats[(size_t)p * a.n + q].x - m);
+    const float v = us * __builtin_fmaf(less, (float)wr[c], sum / l);
+    out[c] = (T)(us != 0.f ? v : 0.f);
+  }
+}
+
+// Adds the parts of pass 2: a thread per four columns.
+template <int TYPE>
+__global__ void __launch_bounds__(256)
+k_loss_table(const float* __restrict__ O, int parts, int64_t rows, int dim, int o_pitch, void* grad, int64_t stride) {
+  typedef typename RowType<TYPE>::T T;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int quads = o_pitch / 4;
+  const int64_t row = at / quads;
+  if (row >= rows) return;
+  const int c = 4 * (int)(at - row * quads);
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < parts; ++p) {
+    const float4 o = *reinterpret_cast<const float4*>(O + ((size_t)p * rows + row) * o_pitch + c);
+    v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w;
+  }
+  store_cols<TYPE, 4>((T*)grad + row * stride, c, dim, v);
+}
+
+// ------------------------------------------------------------------------------------------ launches -----
+template <int TYPE, int PASS>
+static void launch_nk(const SmArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)((a.units + 7) / 8 * 8)), block(256);
+  switch (sm_nk(a.dim)) {
+    case 2: hipLaunchKernelGGL((k_softmax<TYPE, 2, PASS>), grid, block, 0, st, a); break;
+    case 4: hipLaunchKernelGGL((k_softmax<TYPE, 4, PASS>), grid, block, 0, st, a); break;
+    case 7: hipLaunchKernelGGL((k_softmax<TYPE, 7, PASS>), grid, block, 0, st, a); break;
+    case 8: hipLaunchKernelGGL((k_softmax<TYPE, 8, PASS>), grid, block, 0, st, a); break;
+    case 12: hipLaunchKernelGGL((k_softmax<TYPE, 12, PASS>), grid, block, 0, st, a); break;
+    case 16: hipLaunchKernelGGL((k_softmax<TYPE, 16, PASS>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((k_softmax<TYPE, 25, PASS>), grid, block, 0, st, a); break;
+  }
+}
+template <int PASS> static hipError_t launch_pass(int dtype, const SmArgs& a, hipStream_t st) {
+  if (dtype == MAR_DTYPE_FP32) launch_nk<0, PASS>(a, st);
+  else if (dtype == MAR_DTYPE_BF16) launch_nk<1, PASS>(a, st);
+  else launch_nk<2, PASS>(a, st);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------ entry points -----
+// Workspace: statistics, the queries' sums, what pass 2 reads per query, the parts of the table's gradient.
+struct LossLayout { size_t stats, O1, row_m, row_f, row_u, O2, bytes; SmPlan p1, p2; int32_t o_pitch; };
+
+static LossLayout loss_layout(const mar_softmax* p) {
+  LossLayout L;
+  L.p1 = sm_plan(p->dtype, p->dim, 1, p->num_queries, p->num_rows, 1);
+  L.p2 = sm_plan(p->dtype, p->dim, 2, p->num_rows, p->num_queries, 1);
+  L.o_pitch = (p->dim + 3) / 4 * 4;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
+  const size_t T = (size_t)p->num_queries;
+  L.stats = take((size_t)L.p1.parts * T * sizeof(float4));
+  L.O1 = take((size_t)L.p1.parts * T * L.o_pitch * 4);
+  L.row_m = take(T * 4); L.row_f = take(T * 4); L.row_u = take(T * 4);
+  L.O2 = take(L.p2.parts > 1 ? (size_t)L.p2.parts * p->num_rows * L.o_pitch * 4 : 0);
+  L.bytes = at > 256 ? at : 256;
+  return L;
+}
+
+extern "C" int mar_softmax_loss_workspace_bytes(const mar_softmax* p, size_t* out_bytes) {
+  int code;
+  if (const char* why = sm_check(p, &code)) { mar_set_error("%s", why); return code; }
+  if (!out_bytes) { mar_set_error("out_bytes is NULL"); return MAR_EINVAL; }
+  *out_bytes = loss_layout(p).bytes;
+  return MAR_OK;
+}
+
+extern "C" int mar_softmax_loss(const mar_softmax* p, const void* queries, const void* table, const int32_t* targets, const float* weights,
+                                float* loss, float* lse, void* grad_queries, int64_t grad_query_stride, void* grad_table,
+                                int64_t grad_row_stride, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int code;
+  if (const char* why = sm_check(p, &code)) { mar_set_error("%s", why); return code; }
+  const uintptr_t align = p->dtype == MAR_DTYPE_FP32 ? 3 : 1;
+  if (!table || (p->num_queries > 0 && (!queries || !targets))) { mar_set_error("queries, table or targets is NULL"); return MAR_EINVAL; }
+  if (((uintptr_t)queries | (uintptr_t)table | (uintptr_t)grad_queries | (uintptr_t)grad_table) & align) { mar_set_error("a matrix is not aligned to its type"); return MAR_EINVAL; }
+  if (((uintptr_t)targets | (uintptr_t)weights | (uintptr_t)loss | (uintptr_t)lse) & 3) { mar_set_error("an array is not 4-byte aligned"); return MAR_EINVAL; }
+  if ((grad_queries && grad_query_stride < p->dim) || (grad_table && grad_row_stride < p->dim)) { mar_set_error("a gradient's stride is below dim"); return MAR_EINVAL; }
+  if (!workspace || ((uintptr_t)workspace & 255)) { mar_set_error("workspace must be non-NULL and 256-byte aligned"); return MAR_EINVAL; }
+  const LossLayout L = loss_layout(p);
+  if (workspace_bytes < L.bytes) { mar_set_error("workspace has %zu bytes, %zu needed", workspace_bytes, L.bytes); return MAR_ENOMEM; }
+  const hipStream_t st = (hipStream_t)hip_stream;
+  char* const ws = (char*)workspace;
+  const float c = p->scale * 1.44269504088896341f;
+
+  SmArgs a = {};
+  a.dim = p->dim; a.c = c; a.o_pitch = L.o_pitch; a.targets = targets;
+  hipError_t e = hipSuccess;
+  if (p->num_queries > 0) {
+    a.X = queries; a.x_stride = p->query_stride; a.n_x = p->num_queries;
+    a.Y = table; a.y_stride = p->row_stride; a.n_y = (int32_t)p->num_rows;
+    a.nstripes = L.p1.stripes; a.parts = L.p1.parts; a.tps = L.p1.tps; a.units = a.nstripes * a.parts;
+    a.stats = (float4*)(ws + L.stats); a.O = (float*)(ws + L.O1);
+    e = launch_pass<1>(p->dtype, a, st);
+    if (e != hipSuccess) { mar_set_error("softmax kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
+    LossArgs r = {};
+    r.Q = queries; r.W = table; r.q_stride = p->query_stride; r.w_stride = p->row_stride;
+    r.n = p->num_queries; r.dim = p->dim; r.parts = L.p1.parts; r.o_pitch = L.o_pitch; r.rows = p->num_rows;
+    r.scale = p->scale; r.unscale = (double)p->scale / (double)c;
+    r.targets = targets; r.weights = weights; r.stats = a.stats; r.O = a.O;
+    if (grad_table) { r.row_m = (float*)(ws + L.row_m); r.row_f = (float*)(ws + L.row_f); r.row_u = (float*)(ws + L.row_u); }
+    r.log_f = p->dtype != MAR_DTYPE_BF16;
+    r.loss = loss; r.lse = lse; r.grad = grad_queries; r.grad_stride = grad_query_stride;
+    const dim3 grid((unsigned)((p->num_queries + 3) / 4)), block(256);
+    if (p->dtype == MAR_DTYPE_FP32) hipLaunchKernelGGL(k_loss_rows<0>, grid, block, 0, st, r);
+    else if (p->dtype == MAR_DTYPE_BF16) hipLaunchKernelGGL(k_loss_rows<1>, grid, block, 0, st, r);
+    else hipLaunchKernelGGL(k_loss_rows<2>, grid, block, 0, st, r);
+    e = hipGetLastError();
+    if (e != hipSuccess) { mar_set_error("loss kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
+  }
+  if (!grad_table) return MAR_OK;
+  a.X = table; a.x_stride = p->row_stride; a.n_x = (int32_t)p->num_rows;
+  a.Y = queries; a.y_stride = p->query_stride; a.n_y = p->num_queries;
+  a.nstripes = L.p2.stripes; a.parts = L.p2.parts; a.tps = L.p2.tps; a.units = a.nstripes * a.parts;
+  a.row_m = (const float*)(ws + L.row_m); a.row_f = (const float*)(ws + L.row_f); a.row_u = (const float*)(ws + L.row_u);
+  a.O = (float*)(ws + L.O2);
+  if (L.p2.parts == 1) { a.out = grad_table; a.out_stride = grad_row_stride; }
+  e = launch_pass<2>(p->dtype, a, st);
+  if (e == hipSuccess && L.p2.parts > 1) {
+    const int64_t threads = p->num_rows * (L.o_pitch / 4);
+    const dim3 grid((unsigned)((threads + 255) / 256)), block(256);
+    if (p->dtype == MAR_DTYPE_FP32) hipLaunchKernelGGL(k_loss_table<0>, grid, block, 0, st, a.O, L.p2.parts, p->num_rows, p->dim, L.o_pitch, grad_table, grad_row_stride);
+    else if (p->dtype == MAR_DTYPE_BF16) hipLaunchKernelGGL(k_loss_table<1>, grid, block, 0, st, a.O, L.p2.parts, p->num_rows, p->dim, L.o_pitch, grad_table, grad_row_stride);
+    else hipLaunchKernelGGL(k_loss_table<2>, grid, block, 0, st, a.O, L.p2.parts, p->num_rows, p->dim, L.o_pitch, grad_table, grad_row_stride);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess) { mar_set_error("table gradient kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
+  return MAR_OK;
+}

@@ -1,0 +1,109 @@
+"""GPU parity of mar_dropout with the oracle's generator (bit exact: one rounding of one product), and the operators together."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2101_08358_amd as mar
+import softmax_util as su
+from oracle import philox
+
+pytestmark = pytest.mark.gpu
+DEV = su.DEV
+
+
+def keep_mask(rows, dim, p, seed, step, first_row=0):
+    groups = (dim + 7) // 8
+    r, c = np.meshgrid(np.arange(first_row, first_row + rows), np.arange(groups), indexing="ij")
+    words = philox.philox4x32_10_np(r, c, step & 0xFFFFFFFF, 0xC0000000 | (step >> 32), seed & 0xFFFFFFFF, seed >> 32)
+    u = np.stack([half for w in words for half in (w & np.uint64(0xFFFF), w >> np.uint64(16))], axis=2).reshape(rows, groups * 8)[:, :dim]
+    return u >= math.floor(p * 65536 + 0.5)
+
+
+def dropout(x, p, seed, step, out=None):
+    out = torch.full(tuple(x.shape), 7.0, dtype=x.dtype, device=DEV) if out is None else out
+    dtype = {torch.float32: mar.DTYPE_FP32, torch.bfloat16: mar.DTYPE_BF16, torch.float16: mar.DTYPE_FP16}[x.dtype]
+    mar.mar_dropout(x, max(x.stride(0), x.shape[1]), x.shape[0], x.shape[1], dtype, p, seed, step, out, max(out.stride(0), x.shape[1]))
+    return out
+
+
+@pytest.mark.parametrize("tname", ("fp32", "bf16", "fp16"))
+@pytest.mark.parametrize("rows,dim,p,seed,step", ((1, 1, 0.5, 0, 0), (3, 7, 0.1, 5, 1), (1000, 50, 0.2, 0xDEADBEEFCAFEF00D, (1 << 40) + 7), (77, 401, 0.9, 1, (1 << 62) - 1),
+                                                  (513, 100, 0.0, 9, 3), (200, 4096, 0.3333, 12, 4), (64, 8, 65535 / 65536, 3, 3), (5, 1003, 0.5, 2, 2)))
+def test_bit_exact(rows, dim, p, seed, step, tname):
+    g = su.gen(rows + dim)
+    odd = rows % 2
+    x = su.rows(g, rows, dim, su.TYPES[tname][0], stride=dim + 3 * odd, offset=odd)
+    buf = torch.full((odd + rows * (dim + odd),), 5.0, dtype=x.dtype, device=DEV)
+    out = buf[odd:].view(rows, dim + odd)[:, :dim]
+    dropout(x, p, seed, step, out)
+    keep = torch.from_numpy(keep_mask(rows, dim, p, seed, step)).to(DEV)
+    scale = torch.tensor(65536.0 / (65536 - math.floor(p * 65536 + 0.5)), dtype=torch.float32, device=DEV)
+    want = torch.where(keep, (x.float() * scale).to(x.dtype), torch.zeros((), dtype=x.dtype, device=DEV))
+    assert torch.equal(out, want)
+    if odd:
+        assert (buf[odd:].view(rows, dim + odd)[:, dim:] == 5.0).all() and (buf[:odd] == 5.0).all()
+
+
+def test_the_mask_is_the_same_for_every_type_and_in_place():
+    x = torch.ones((300, 75), device=DEV)
+    want = dropout(x, 0.4, 17, 23) != 0
+    for dt in (torch.bfloat16, torch.float16):
+        y = x.to(dt)
+        assert torch.equal(dropout(y, 0.4, 17, 23) != 0, want)
+        dropout(y, 0.4, 17, 23, out=y)
+        assert torch.equal(y != 0, want)
+    assert not torch.equal(dropout(x, 0.4, 17, 24) != 0, want)
+    assert abs(float(want.float().mean()) - 0.6) < 5 * math.sqrt(0.24 / want.numel())
+    x[:] = float("nan")                                      # dropped values are 0 whatever they were
+    assert torch.equal(torch.isnan(dropout(x, 0.4, 17, 23)), want)
+
+
+def test_no_rows():
+    mar.mar_dropout(None, 8, 0, 8, mar.DTYPE_FP32, 0.5, 0, 0, None, 8)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("tname", ("fp32", "bf16", "fp16"))
+def test_a_training_call_with_all_operators(tname):
+    """Dropout of the queries, the loss over all rows, the gradient back through the dropout, and the answers afterwards, against
+    64 bits on the same mask; then the same captured into a graph and replayed."""
+    T, V, d, p = 300, 1500, 100, 0.2
+    g = su.gen(77)
+    dt = su.TYPES[tname][0]
+    q, w = su.rows(g, T, d, dt), su.rows(g, V, d, dt)
+    targets = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    prob = su.problem(q, w, tname)
+    ws = su.workspace(max(mar.mar_softmax_loss_workspace_bytes(prob), mar.mar_log_probs_workspace_bytes(prob, 5)))
+    x, gx, gq, gw = (torch.zeros_like(t) for t in (q, q, q, w))
+    loss, lse, lp, en = (torch.zeros(T, device=DEV) for _ in range(4))
+    ids, tp = torch.zeros((T, 5), dtype=torch.int32, device=DEV), torch.zeros((T, 5), device=DEV)
+
+    def call():
+        dropout(q, p, 99, 5, out=x)
+        mar.mar_softmax_loss(prob, x, w, targets, None, loss, lse, gx, d, gw, d, ws, ws.numel())
+        dropout(gx, p, 99, 5, out=gq)
+        mar.mar_log_probs(prob, q, w, targets, None, 0, 5, lp, en, ids, tp, ws, ws.numel())
+
+    call()
+    torch.cuda.synchronize()
+    keep = torch.from_numpy(keep_mask(T, d, p, 99, 5)).to(DEV)
+    up = 65536.0 / (65536 - round(p * 65536))
+    assert torch.equal(x, torch.where(keep, (q.float() * up).to(dt), torch.zeros((), dtype=dt, device=DEV)))
+    su.check_loss((loss, lse, gx, gw), x, w, tname, targets, None, 1.0)
+    assert torch.equal(gq, torch.where(keep, (gx.float() * up).to(dt), torch.zeros((), dtype=dt, device=DEV)))
+    s = su.scores(q, w, 1.0)
+    assert torch.equal(ids.long(), s.sort(dim=1, descending=True, stable=True).indices[:, :5])
+    ref = torch.log_softmax(s, 1)[torch.arange(T, device=DEV), targets.long()]
+    assert ((lp.double() - ref).abs() <= 2 * su.score_error(q, w, 1.0) + su.sum_error(V) + ref.abs() * 2.0 ** -23).all()
+    want = [t.clone() for t in (loss, lse, gq, gw, lp, en, ids, tp)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for _ in range(3):
+        for t in (loss, lse, gq, gw, lp, en, ids, tp, x, gx):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((loss, lse, gq, gw, lp, en, ids, tp), want))
