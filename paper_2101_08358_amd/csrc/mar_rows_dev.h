@@ -12,19 +12,22 @@ typedef unsigned row_u4 __attribute__((ext_vector_type(4)));
 typedef unsigned short row_h8 __attribute__((ext_vector_type(8)));
 
 // The 16-bit values of columns c .. c + 7 of a row of d columns, zeros from column d on, as four words.  Nothing outside the
-// row is read: a part that reaches beyond its end takes the row's last eight columns and shifts them down.
-__device__ __forceinline__ row_u4 load8_bits(const void* row, int c, int d) {
+// row is read: a part that reaches beyond its end takes the row's last eight columns (take8_bits) and shifts them down (place8_bits).
+__device__ __forceinline__ row_u4 take8_bits(const void* row, int c, int d) {
   const unsigned short* r = (const unsigned short*)row;
-  row_u4 v;
   if (d < 8) {                                             // uniform
     row_h8 h = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
     for (int e = 0; e < 7; ++e) if (c + e < d) h[e] = r[c + e];
     return __builtin_bit_cast(row_u4, h);
   }
-  const int at = c < d - 8 ? c : d - 8;
-  __builtin_memcpy(&v, r + at, 16);
-  int k = c - at;                                          // columns to shift out
+  row_u4 v;
+  __builtin_memcpy(&v, r + min(c, d - 8), 16);
+  return v;
+}
+__device__ __forceinline__ row_u4 place8_bits(row_u4 v, int c, int d) {
+  if (d < 8) return v;                                     // uniform
+  int k = max(c - (d - 8), 0);                             // columns to shift out
   if ((d & 7) == 0) {                                      // uniform: all or nothing
     if (k) v = (row_u4)(0u);
     return v;
@@ -35,24 +38,38 @@ __device__ __forceinline__ row_u4 load8_bits(const void* row, int c, int d) {
   if (k) { lo = (lo >> (16 * k)) | (hi << (64 - 16 * k)); hi >>= 16 * k; }
   return (row_u4){(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
 }
+__device__ __forceinline__ row_u4 load8_bits(const void* row, int c, int d) { return place8_bits(take8_bits(row, c, d), c, d); }
 // Columns c .. c + 3 of a row of fp32 values, likewise.
-__device__ __forceinline__ void load4_floats(const float* r, int c, int d, float (&v)[4]) {
+__device__ __forceinline__ row_u4 take4_floats(const float* r, int c, int d) {
+  row_u4 v = {0u, 0u, 0u, 0u};
   if (d < 4) {                                             // uniform
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = c + e < d ? r[c + e] : 0.f;
-    return;
+    for (int e = 0; e < 3; ++e) if (c + e < d) v[e] = __float_as_uint(r[c + e]);
+    return v;
   }
-  const int at = c < d - 4 ? c : d - 4;
-  float w[4];
-  __builtin_memcpy(w, r + at, 16);
-  const int k = c - at;
+  __builtin_memcpy(&v, r + min(c, d - 4), 16);
+  return v;
+}
+__device__ __forceinline__ row_u4 place4_floats(row_u4 w, int c, int d) {
+  if (d < 4) return w;                                     // uniform
+  const int k = max(c - (d - 4), 0);
+  if ((d & 3) == 0) {                                      // uniform
+    if (k) w = (row_u4)(0u);
+    return w;
+  }
+  row_u4 v;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    float x = 0.f;                                         // w[e + k]
+    v[e] = 0u;                                             // w[e + k]
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x = e + k == j ? w[j] : x;
-    v[e] = x;
+    for (int j = e; j < 4; ++j) v[e] = e + k == j ? w[j] : v[e];
   }
+  return v;
+}
+__device__ __forceinline__ void load4_floats(const float* r, int c, int d, float (&v)[4]) {
+  const row_u4 w = place4_floats(take4_floats(r, c, d), c, d);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(w[e]);
 }
 template <int TYPE> __device__ __forceinline__ float bits_to_float(unsigned short b) {
   if (TYPE == 1) return __uint_as_float((unsigned)b << 16);

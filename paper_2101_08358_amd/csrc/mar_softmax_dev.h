@@ -1,12 +1,22 @@
 // The contraction of mar_softmax.h on the device.
 #pragma once
+#include <type_traits>
+
 #include "mar_rows_dev.h"
 #include "mar_softmax.h"
 #include "mar_split_dev.h"
 
-// Stationary blocks of 32 rows a wave takes.
-constexpr int sm_qb(int type, int nk, int pass) { return 1; }
-constexpr int sm_waves(int type, int nk, int pass) { return nk <= 8 ? 2 : (nk <= 12 && pass == 0 ? 2 : 1); }
+// f(0), .., f(N - 1), unrolled whatever the body's size: the loops index registers.
+template <int N, typename F> __device__ __forceinline__ void unrolled(F&& f) {
+  if constexpr (N > 0) { unrolled<N - 1>(f); f(std::integral_constant<int, N - 1>{}); }
+}
+// Stationary blocks of 32 rows a wave takes, and waves per SIMD (= workgroups per CU): as registers allow.  An A fragment read from LDS
+// feeds one product a block, so two blocks halve the LDS traffic; pass 0, which keeps no sums of rows, has the registers.
+constexpr int sm_qb(int type, int nk, int pass) { return pass == 0 && type != MAR_DTYPE_FP32 && nk <= 16 ? 2 : 1; }
+constexpr int sm_waves(int type, int nk, int pass) {
+  return type == MAR_DTYPE_FP32 ? (pass == 0 ? (nk <= 8 ? 3 : (nk <= 16 ? 2 : 1)) : (nk <= 4 && pass == 1 ? 3 : (nk <= 8 ? 2 : 1)))
+                                : (pass == 0 ? (nk <= 8 ? 3 : 2) : (nk <= 4 ? 3 : (nk <= 12 ? 2 : 1)));
+}
 
 template <int TYPE> __device__ __forceinline__ v16f sm_mfma(v8s a, v8s b, v16f c) {
   if (TYPE == MAR_DTYPE_BF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8b, a), __builtin_bit_cast(v8b, b), c, 0, 0, 0);
@@ -47,67 +57,90 @@ template <int TYPE, int NK> struct SmGeom {
   static constexpr int NP = (2 * NK + 7) / 8;              // 16-byte units a thread copies of a tile: eight threads to a row
 };
 
-// A tile on its way from memory to LDS: wave w takes rows 8 w .. 8 w + 7.
+// A tile on its way from memory to LDS: wave w takes rows 8 w .. 8 w + 7, eight threads to a row, a piece of 8 columns each at a time.
+// fp32: the exponent of a wave's eight rows is known once all pieces are there; the widest rows (SLIM) are loaded twice, for
+// their pieces and the sums of a pass do not fit the registers together.
 template <int TYPE, int NK> struct SmStage {
   typedef SmGeom<TYPE, NK> G;
   typedef typename RowType<TYPE>::T T;
-  row_u4 r[G::NP][G::PLANES];
-  // use: where not NULL, rows with a 0 there are taken as zeros whatever they hold
-  __device__ __forceinline__ void load(const T* __restrict__ Y, int64_t stride, int n_y, int dim, int y0, int tid, const float* __restrict__ use = nullptr) {
-    const T* row = Y + (int64_t)min(y0 + (tid >> 3), n_y - 1) * stride;      // rows beyond the last are the last again
-#pragma unroll
-    for (int p = 0; p < G::NP; ++p) {
-      const int u = (tid & 7) + 8 * p;
-      if (TYPE == MAR_DTYPE_FP32) {
-        float v[8];
-        load8<TYPE>(row, 8 * u, dim, v);
-        r[p][0] = (row_u4){__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-        r[p][G::PLANES - 1] = (row_u4){__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
-      } else {
-        r[p][0] = load8_bits(row, 8 * u, dim);
-      }
+  static constexpr bool PAIRS = TYPE == MAR_DTYPE_FP32, SLIM = PAIRS && NK > 16;
+  static constexpr int KEEP = SLIM ? 1 : G::NP;
+  row_u4 r[KEEP][G::PLANES];
+  int big;
+  bool zero;                                               // the row is taken as zeros whatever it holds
+  const T* row;
+  __device__ __forceinline__ void begin(const T* __restrict__ Y, int64_t stride, int n_y, int y0, int tid, const float* __restrict__ use) {
+    const int y = min(y0 + (tid >> 3), n_y - 1);           // rows beyond the last are the last again
+    row = Y + (int64_t)y * stride;
+    zero = use && use[y] == 0.f;
+    big = 0;
+  }
+  __device__ __forceinline__ void fetch(int p, int dim, int tid, row_u4 (&v)[G::PLANES]) const {
+    const int u = (tid & 7) + 8 * p;
+    if constexpr (PAIRS) {
+      v[0] = take4_floats(row, 8 * u, dim);
+      v[1] = take4_floats(row, 8 * u + 4, dim);
+    } else {
+      v[0] = take8_bits(row, 8 * u, dim);
     }
-    if (use && use[min(y0 + (tid >> 3), n_y - 1)] == 0.f) {
+  }
+  // columns that a piece at the row's end holds besides its own belong to the same eight rows: they may be measured too
+  __device__ __forceinline__ void measure(const row_u4 (&v)[G::PLANES]) {
 #pragma unroll
-      for (int p = 0; p < G::NP; ++p) r[p][0] = r[p][G::PLANES - 1] = (row_u4)(0u);
+    for (int k = 0; k < G::PLANES; ++k) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) big = max(big, finite_bits(__uint_as_float(v[k][j])));
+    }
+  }
+  // piece p is asked for; SLIM: the piece before it has arrived and is looked at
+  __device__ __forceinline__ void load(int p, int dim, int tid) {
+    if constexpr (SLIM) { if (p > 0) measure(r[0]); }
+    fetch(p, dim, tid, r[SLIM ? 0 : p]);
+  }
+  __device__ __forceinline__ void put(int p, char* tile, float scale, int dim, int tid, const row_u4 (&v)[G::PLANES]) const {
+    const int u = (tid & 7) + 8 * p, y = tid >> 3;
+    char* const to = tile + y * G::PA + ((16 * u) ^ (16 * sp_swizzle(G::UNITS, y)));
+    if (u >= 2 * NK) return;
+    if constexpr (PAIRS) {
+      const row_u4 q[2] = {place4_floats(v[0], 8 * u, dim), place4_floats(v[1], 8 * u + 4, dim)};
+      float f[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = zero ? 0.f : __uint_as_float(q[j >> 2][j & 3]);
+      v8s hi, lo;
+      sm_parts8(f, scale, hi, lo);
+      *reinterpret_cast<v8s*>(to) = hi;
+      *reinterpret_cast<v8s*>(to + G::PLANE) = lo;
+    } else {
+      *reinterpret_cast<row_u4*>(to) = zero ? (row_u4)(0u) : place8_bits(v[0], 8 * u, dim);
     }
   }
   // exps: the exponents of the tile's four blocks of eight rows (fp32)
-  __device__ __forceinline__ void store(char* tile, int* exps, int tid) {
-    const int row = tid >> 3;
-    char* const at = tile + row * G::PA;
-    const int swz = 16 * sp_swizzle(G::UNITS, row);
-    if (TYPE == MAR_DTYPE_FP32) {
-      int big = 0;
+  __device__ __forceinline__ void store(char* tile, int* exps, int dim, int tid) {
+    float scale = 1.f;
+    if constexpr (PAIRS) {
+      if constexpr (SLIM) measure(r[0]);
+      else {
 #pragma unroll
-      for (int p = 0; p < G::NP; ++p) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) big = max(big, finite_bits(__uint_as_float(r[p][j >> 2 ? G::PLANES - 1 : 0][j & 3])));
+        for (int p = 0; p < G::NP; ++p) measure(r[p]);
       }
+      if (zero) big = 0;
 #pragma unroll
       for (int o = 32; o >= 1; o >>= 1) big = max(big, __shfl_xor(big, o));
       const int e = sm_exponent(big);
       if ((tid & 63) == 0) exps[tid >> 6] = e;
-      const float scale = __builtin_ldexpf(1.f, e);
+      scale = __builtin_ldexpf(1.f, e);
+    }
+    if constexpr (SLIM) {
 #pragma unroll
       for (int p = 0; p < G::NP; ++p) {
-        const int u = (tid & 7) + 8 * p;
-        float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(r[p][j >> 2 ? G::PLANES - 1 : 0][j & 3]);
-        v8s hi, lo;
-        sm_parts8(v, scale, hi, lo);
-        if (u < 2 * NK) {
-          *reinterpret_cast<v8s*>(at + ((16 * u) ^ swz)) = hi;
-          *reinterpret_cast<v8s*>(at + G::PLANE + ((16 * u) ^ swz)) = lo;
-        }
+        row_u4 v[G::PLANES];
+        fetch(p, dim, tid, v);
+        put(p, tile, scale, dim, tid, v);
+        if (p % 2) __builtin_amdgcn_sched_barrier(0);      // two pieces in flight
       }
     } else {
 #pragma unroll
-      for (int p = 0; p < G::NP; ++p) {
-        const int u = (tid & 7) + 8 * p;
-        if (u < 2 * NK) *reinterpret_cast<row_u4*>(at + ((16 * u) ^ swz)) = r[p][0];
-      }
+      for (int p = 0; p < G::NP; ++p) put(p, tile, scale, dim, tid, r[p]);
     }
   }
 };
@@ -116,9 +149,10 @@ template <int TYPE, int NK> struct SmStage {
 // and moves when one exceeds it by more than 15; what is 2^-36 of the largest weight is lost to the second product (never to the sum).
 #define SM_ABOVE 15.f
 #define SM_BELOW 12.f
+#define SM_CHAIN 16               // tiles whose weights are summed before their sum is added to the part's: chains of fp32 sums stay short
 
 template <int TYPE, int NK, int PASS>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sm_waves(TYPE, NK, PASS))))
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sm_waves(TYPE, NK, PASS), sm_waves(TYPE, NK, PASS))))
 k_softmax(SmArgs a) {
   typedef SmGeom<TYPE, NK> G;
   typedef typename RowType<TYPE>::T T;
@@ -126,11 +160,15 @@ k_softmax(SmArgs a) {
   constexpr int QB = sm_qb(TYPE, NK, PASS);
   constexpr bool SECOND = PASS != 0;
   constexpr int NO = SECOND ? (NK + 1) / 2 : 1;            // 32-column blocks of the output
-  constexpr bool REFS = PASS != 2 || TYPE != MAR_DTYPE_BF16;   // weights relative to a reference
+  constexpr bool REFS = PASS != 2 || TYPE != MAR_DTYPE_BF16 || NK > 16;   // weights relative to a reference (bf16 does without; the widest rows' registers do not)
+  constexpr int PL = G::PLANES;
+  static_assert(QB == 1 || PASS == 0, "passes with a second product take one block a wave");
   __shared__ __attribute__((aligned(1024))) char smem[2 * G::TILE];
   __shared__ int exps[2][4];
+  // pass 2, per query of a tile: f = log2(|u| / sum of its weights), m its reference (16-bit types: f - m and nothing)
   __shared__ __attribute__((aligned(16))) float rows_m[2][SM_TY], rows_f[2][SM_TY], rows_u[2][SM_TY];
   __shared__ int rows_t[2][SM_TY];
+  __shared__ unsigned rows_neg[2];                         // queries with a negative u
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5, m = lane & 31, g = lane >> 4, i = lane & 15;
@@ -147,25 +185,38 @@ k_softmax(SmArgs a) {
   for (int k = tid * 16; k < 2 * G::TILE; k += 256 * 16) *reinterpret_cast<row_u4*>(smem + k) = (row_u4)(0u);
   SmStage<TYPE, NK> stage;
   const T* Y = (const T*)a.Y;
-  // pass 2: statistics of the tile's queries, row threadIdx.x of the first 32
+  const float* use = PASS == 2 ? a.row_u : nullptr;
   float q_m = 0.f, q_f = 0.f, q_u = 0.f;
   int q_t = -1;
   auto load_rows = [&](int y0) {
     if (PASS == 2 && tid < SM_TY) {
       const int y = y0 + tid;
       const bool in = y < a.n_y;
-      q_m = in ? a.row_m[y] : -SM_NO_REF; q_f = in ? a.row_f[y] : (REFS ? -__builtin_inff() : 0.f); q_u = in ? a.row_u[y] : 0.f; q_t = in ? a.targets[y] : -1;
+      q_m = in ? a.row_m[y] : 0.f; q_f = in ? a.row_f[y] : -__builtin_inff(); q_u = in ? a.row_u[y] : 0.f; q_t = in ? a.targets[y] : -1;
     }
   };
   auto store_rows = [&](int buf) {
-    if (PASS == 2 && tid < SM_TY) { rows_m[buf][tid] = q_m; rows_f[buf][tid] = q_f; rows_u[buf][tid] = q_u; rows_t[buf][tid] = q_t; }
+    if (PASS == 2 && tid < 64) {
+      const bool neg = tid < SM_TY && q_u < 0.f;
+      const unsigned long long all = __builtin_amdgcn_ballot_w64(neg);
+      if (tid < SM_TY) {
+        rows_m[buf][tid] = q_m; rows_f[buf][tid] = PAIRS ? q_f : q_f - q_m; rows_u[buf][tid] = q_u; rows_t[buf][tid] = q_t;
+        if (tid == 0) rows_neg[buf] = (unsigned)all;
+      }
+    }
   };
-  if (t_begin < t_end) { stage.load(Y, a.y_stride, a.n_y, dim, t_begin * SM_TY, tid, PASS == 2 ? a.row_u : nullptr); load_rows(t_begin * SM_TY); }
+  if (t_begin < t_end) {
+    stage.begin(Y, a.y_stride, a.n_y, t_begin * SM_TY, tid, use);
+#pragma unroll
+    for (int p = 0; p < G::NP; ++p) stage.load(p, dim, tid);
+    load_rows(t_begin * SM_TY);
+  }
 
   // ---- stationary fragments
   v8s xh[QB][NK], xl[QB][PAIRS ? NK : 1];
   int ex[QB], tgt[QB];
   bool xv[QB];
+  const uint32_t* words[QB];
 #pragma unroll
   for (int b = 0; b < QB; ++b) {
     const int64_t x = x_first + 32 * b + m;
@@ -174,20 +225,21 @@ k_softmax(SmArgs a) {
     const T* row = (const T*)a.X + xr * a.x_stride;
     ex[b] = 0;
     tgt[b] = PASS == 1 && xv[b] ? a.targets[xr] : -1;
+    words[b] = PASS == 0 && a.allowed ? a.allowed + xr * a.allowed_stride : nullptr;
     if (PAIRS) {
       int big = 0;
-#pragma unroll
-      for (int s = 0; s < NK; ++s) {
+      unrolled<NK>([&](int s) {
         float v[8];
         load8<TYPE>(row, 16 * s + 8 * h, dim, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) big = max(big, finite_bits(v[e]));
-      }
+        if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+      });
       big = max(big, __shfl_xor(big, 32));
       ex[b] = sm_exponent(big);
     }
-#pragma unroll
-    for (int s = 0; s < NK; ++s) {
+    unrolled<NK>([&](auto step) {
+      constexpr int s = step;
       if constexpr (PAIRS) {
         float v[8];
         load8<TYPE>(row, 16 * s + 8 * h, dim, v);
@@ -195,93 +247,113 @@ k_softmax(SmArgs a) {
       } else {
         xh[b][s] = __builtin_bit_cast(v8s, load8_bits(row, 16 * s + 8 * h, dim));
       }
-    }
+      if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    });
   }
 
-  v16f oacc[QB][NO];
-  float ref[QB], lsum[QB], asum[QB], gmax[QB];
+  v16f oacc[NO];
+  float ref[QB], lsum[QB], ltot[QB], asum[QB], atot[QB], gmax[QB];
+  unsigned word_next[QB];
+#pragma unroll
+  for (int c = 0; c < NO; ++c) oacc[c] = (v16f)(0.f);
 #pragma unroll
   for (int b = 0; b < QB; ++b) {
-#pragma unroll
-    for (int c = 0; c < NO; ++c) oacc[b][c] = (v16f)(0.f);
-    ref[b] = SM_NO_REF; lsum[b] = asum[b] = 0.f; gmax[b] = -__builtin_inff();
+    ref[b] = SM_NO_REF; lsum[b] = ltot[b] = asum[b] = atot[b] = 0.f; gmax[b] = -__builtin_inff();
+    word_next[b] = PASS == 0 && a.allowed && t_begin < t_end ? words[b][t_begin] : ~0u;
   }
+  int group_left = a.group_tiles;
   float neg1 = -1.f;
   asm volatile("" : "+v"(neg1));
 
   // ---- where a lane reads in a tile: row m, unit 2 s + h; transposed: row 16 s + 4 h + i / 4 (and 8 more), columns 32 c + 16 (g % 2) + 4 (i % 4)
-  const int fswz = 16 * sp_swizzle(G::UNITS, m), fofs = m * G::PA;
-  // O^T += Y^T P.  rest: bits of the weights whose remainder after rounding to 16 bits counts too (PASS 2: of an answer's own row)
-  auto second = [&](const char* tile, int b, const float (&w)[16], bool with_rest, unsigned rest) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      float p8[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p8[e] = w[8 * s + e];
-      v8s ph, pl = {0, 0, 0, 0, 0, 0, 0, 0};
-      if constexpr (PAIRS) {
-        split8<true>(p8, neg1, ph, pl);
-      } else {
-        ph = sm_round8<TYPE>(p8);
-        if (PASS == 2 && with_rest) {
-          float r8[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) r8[e] = (rest >> (8 * s + e) & 1u) ? p8[e] - sm_rounded<TYPE>(p8[e]) : 0.f;
-          pl = sm_round8<TYPE>(r8);
-        }
-      }
-      const int ty = 16 * s + 4 * h + (i >> 2), tswz = 16 * sp_swizzle(G::UNITS, ty), tswz8 = 16 * sp_swizzle(G::UNITS, ty + 8);
-#pragma unroll
-      for (int c = 0; c < NO; ++c) {
-        const int byte = 64 * c + 32 * (g & 1) + 8 * (i & 3);
-        const char* const p0 = tile + ty * G::PA + (byte ^ tswz);
-        const char* const p1 = tile + (ty + 8) * G::PA + (byte ^ tswz8);
-        const v8s yh = join8(lds_read_tr(p0), lds_read_tr(p1));
-        oacc[b][c] = sm_mfma<TYPE>(yh, ph, oacc[b][c]);
-        if constexpr (PAIRS) {
-          const v8s yl = join8(lds_read_tr(p0 + G::PLANE), lds_read_tr(p1 + G::PLANE));
-          oacc[b][c] = sm_mfma<TYPE>(yl, ph, oacc[b][c]);
-          oacc[b][c] = sm_mfma<TYPE>(yh, pl, oacc[b][c]);
-        } else if (PASS == 2 && with_rest) {
-          oacc[b][c] = sm_mfma<TYPE>(yh, pl, oacc[b][c]);
-        }
-      }
-    }
+  // Rows start at whole groups of units, so a unit of the same group is a bit pattern away and the other groups are immediate
+  // offsets; rows y and y + 16 have the same swizzle.
+  constexpr int GU = sp_group(G::UNITS);
+  auto at = [](int base, int byte) { return (base ^ (byte % (16 * GU))) + byte / (16 * GU) * (16 * GU); };
+  const int fofs = m * G::PA + ((16 * h) ^ (16 * sp_swizzle(G::UNITS, m)));
+  const int ty = 4 * h + (i >> 2), tbyte = 32 * (g & 1) + 8 * (i & 3);
+  const int trofs = ty * G::PA + (tbyte ^ (16 * sp_swizzle(G::UNITS, ty))), trofs8 = (ty + 8) * G::PA + (tbyte ^ (16 * sp_swizzle(G::UNITS, ty + 8)));
+  // rare: a real branch, or it is executed speculatively; wide rows: one block at a time leaves the accumulation registers
+  constexpr bool WIDE = sm_waves(TYPE, NK, PASS) == 1;
+  auto rescale = [&](float f) {
+    asm volatile("" : "+v"(f));
+    unrolled<NO>([&](auto block) {
+      constexpr int c = block;
+      if (WIDE) asm volatile("" : "+a"(oacc[c]));
+      oacc[c] *= f;
+      if (WIDE) asm volatile("" : "+a"(oacc[c]));
+    });
   };
   __syncthreads();                                         // the zeros are there
-  if (t_begin < t_end) { stage.store(smem, exps[0], tid); store_rows(0); }
+  if (t_begin < t_end) { stage.store(smem, exps[0], dim, tid); store_rows(0); }
   __syncthreads();
 
   for (int t = t_begin; t < t_end; ++t) {
-    const int buf = (t - t_begin) & 1;
-    const char* const tile = smem + buf * G::TILE;
+    const int buf = (t - t_begin) & 1, bofs = buf * G::TILE;
     const int y0 = t * SM_TY;
-    const bool has_next = t + 1 < t_end;
-    if (has_next) { stage.load(Y, a.y_stride, a.n_y, dim, y0 + SM_TY, tid, PASS == 2 ? a.row_u : nullptr); load_rows(y0 + SM_TY); }
+    const bool has_next = t + 1 < t_end;                   // uniform
+    unsigned word[QB];
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+      word[b] = word_next[b];
+      if (PASS == 0 && has_next && a.allowed) word_next[b] = words[b][t + 1];
+    }
+    if (has_next) { stage.begin(Y, a.y_stride, a.n_y, y0 + SM_TY, tid, use); load_rows(y0 + SM_TY); }
 
+    // ---- scores; the streamed fragments are read PD steps ahead, the next tile's pieces are asked for between the steps
     v16f sc[QB];
 #pragma unroll
     for (int b = 0; b < QB; ++b) sc[b] = (v16f)(0.f);
+    {
+      constexpr int PD = PAIRS ? 2 : (NK < 4 ? NK : 4);
+      v8s f[PD][PL];
+      const int fb = bofs + fofs;
+      auto read = [&](int s) {
 #pragma unroll
-    for (int s = 0; s < NK; ++s) {
-      const v8s yh = *reinterpret_cast<const v8s*>(tile + fofs + ((32 * s + 16 * h) ^ fswz));
-      if constexpr (PAIRS) {
-        const v8s yl = *reinterpret_cast<const v8s*>(tile + G::PLANE + fofs + ((32 * s + 16 * h) ^ fswz));
+        for (int k = 0; k < PL; ++k) f[s % PD][k] = *reinterpret_cast<const v8s*>(smem + at(fb, 32 * s) + k * G::PLANE);
+      };
+#pragma unroll
+      for (int s = 0; s < PD; ++s) read(s);
+      unrolled<NK>([&](auto step) {
+        constexpr int s = step;
+        const v8s yh = f[s % PD][0], yl = f[s % PD][PL - 1];
+        if (s + PD < NK) read(s + PD);
 #pragma unroll
         for (int b = 0; b < QB; ++b) {
-          sc[b] = sm_mfma<TYPE>(yl, xh[b][s], sc[b]); sc[b] = sm_mfma<TYPE>(yh, xl[b][s], sc[b]); sc[b] = sm_mfma<TYPE>(yh, xh[b][s], sc[b]);
+          if constexpr (PAIRS) { sc[b] = sm_mfma<TYPE>(yl, xh[b][s], sc[b]); sc[b] = sm_mfma<TYPE>(yh, xl[b][s], sc[b]); }
+          sc[b] = sm_mfma<TYPE>(yh, xh[b][s], sc[b]);
         }
-      } else {
+        if (has_next) {
 #pragma unroll
-        for (int b = 0; b < QB; ++b) sc[b] = sm_mfma<TYPE>(yh, xh[b][s], sc[b]);
-      }
+          for (int p = s * G::NP / NK; p < (s + 1) * G::NP / NK; ++p) stage.load(p, dim, tid);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      });
     }
     int ey[4] = {0, 0, 0, 0};
     if (PAIRS) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) ey[k] = __builtin_amdgcn_readfirstlane(exps[buf][k]);
     }
+    // ---- the first transposed fragments of the second product: step s of 16 rows, block c of 32 columns
+    constexpr int NG = 2 * NO, PG = SECOND ? (PAIRS ? 2 : (NG < 4 ? NG : 4)) : 1;
+    v8s tf[PG][PL];
+    auto read_tr = [&](int n) {
+      const int s = n / NO, c = n % NO;
+#pragma unroll
+      for (int k = 0; k < PL; ++k)
+        tf[n % PG][k] = join8(lds_read_tr(smem + at(bofs + trofs, 64 * c) + 16 * s * G::PA + k * G::PLANE),
+                              lds_read_tr(smem + at(bofs + trofs8, 64 * c) + 16 * s * G::PA + k * G::PLANE));
+    };
+    constexpr bool EARLY = !PAIRS && PASS == 1;            // where registers allow
+    if constexpr (SECOND && EARLY) {
+#pragma unroll
+      for (int n = 0; n < PG; ++n) read_tr(n);
+    }
 
+    float w[16];
+    bool hit = false;                                      // PASS 2: the answer of one of the tile's queries is among the wave's rows
+    unsigned own = 0u;
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
       // ---- t = sc k[r / 4]: scores in log2 units
@@ -289,41 +361,46 @@ k_softmax(SmArgs a) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) k[j] = PAIRS ? fmaxf(__builtin_ldexpf(a.c, max(-200, min(120, -(ex[b] + ey[j])))), 0x1p-126f) : a.c;   // never 0: -inf times it stays
       const int64_t x = x_first + 32 * b + m;
-      if (PASS != 2) {
+      if constexpr (PASS != 2) {
         // rows that do not count: beyond the last, or not allowed
         const int left = a.n_y - y0;
-        unsigned word = left >= 32 ? ~0u : (1u << left) - 1u;
-        if (PASS == 0 && a.allowed) word &= a.allowed[min(x, (int64_t)a.n_x - 1) * a.allowed_stride + t];
-        const bool some = PASS == 0 && a.allowed ? true : left < 32;     // uniform
-        word >>= 4 * h;
+        if (left < 32) word[b] &= (1u << left) - 1u;
+        const bool some = (PASS == 0 && a.allowed) || left < 32;             // uniform
+        const unsigned bits = word[b] >> (4 * h);
         if (some) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sc[b][r] = pick((unsigned)((int)(word << (31 - (8 * (r >> 2) + (r & 3)))) >> 31), sc[b][r], -__builtin_inff());
+          for (int r = 0; r < 16; ++r) sc[b][r] = pick((unsigned)((int)(bits << (31 - (8 * (r >> 2) + (r & 3)))) >> 31), sc[b][r], -__builtin_inff());
         }
-        float top = -__builtin_inff(), ztop = -__builtin_inff();
+        float top, ztop;
+        if constexpr (PAIRS) {
+          top = ztop = -__builtin_inff();
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float big = fmaxf(fmaxf(sc[b][4 * j], sc[b][4 * j + 1]), fmaxf(sc[b][4 * j + 2], sc[b][4 * j + 3])) * k[j];
-          top = fmaxf(top, big);
-          ztop = fmaxf(ztop, SECOND && PAIRS ? big - (float)ey[j] : big);
+          for (int j = 0; j < 4; ++j) {
+            const float big = fmaxf(fmaxf(sc[b][4 * j], sc[b][4 * j + 1]), fmaxf(sc[b][4 * j + 2], sc[b][4 * j + 3])) * k[j];
+            top = fmaxf(top, big);
+            ztop = fmaxf(ztop, SECOND ? big - (float)ey[j] : big);
+          }
+        } else {
+          top = sc[b][0];
+#pragma unroll
+          for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[b][r]);
+          top *= k[0];
+          ztop = top;
         }
-        gmax[b] = fmaxf(gmax[b], top);
         // the reference moves
         if (__any(ztop > ref[b] + SM_ABOVE)) {
           ztop = fmaxf(ztop, __shfl_xor(ztop, 32));        // both halves' weights meet in one product
-          const float to = fmaxf(ref[b], ztop - SM_BELOW), by = ref[b] - to, f = __builtin_amdgcn_exp2f(by);
-          if (PASS == 0 && lsum[b] != 0.f) asum[b] = f * __builtin_fmaf(by, lsum[b], asum[b]);
-          lsum[b] *= f;
-          if (SECOND) {
-#pragma unroll
-            for (int c = 0; c < NO; ++c) {
-#pragma unroll
-              for (int r = 0; r < 16; ++r) oacc[b][c][r] *= f;
-            }
+          const float to = fmaxf(ref[b], ztop - SM_BELOW), by = ref[b] - to, fct = __builtin_amdgcn_exp2f(by);
+          if (PASS == 0) {
+            const float l = lsum[b] + ltot[b];
+            asum[b] = l != 0.f ? fct * __builtin_fmaf(by, l, asum[b] + atot[b]) : 0.f;
+            atot[b] = 0.f;
           }
+          lsum[b] *= fct; ltot[b] *= fct;
+          if constexpr (SECOND) rescale(fct);
           ref[b] = to;
         }
-        float w[16];
+        float l16 = 0.f, a16 = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float kg = SECOND && PAIRS ? ref[b] + (float)ey[j] : ref[b];
@@ -332,59 +409,62 @@ k_softmax(SmArgs a) {
           for (int e = 0; e < 4; ++e) {
             const int r = 4 * j + e;
             float z = __builtin_fmaf(sc[b][r], k[j], -kg);
-            if (PASS == 0 && some) z = pick((unsigned)((int)(word << (31 - (8 * j + e))) >> 31), z, -1.0e30f);
+            if (PASS == 0 && some) z = pick((unsigned)((int)(bits << (31 - (8 * j + e))) >> 31), z, -1.0e30f);
             w[r] = __builtin_amdgcn_exp2f(z);
             sum4 += w[r];
-            if (PASS == 0) asum[b] = __builtin_fmaf(w[r], z, asum[b]);
+            if (PASS == 0) a16 = __builtin_fmaf(w[r], z, a16);
           }
-          lsum[b] += SECOND && PAIRS ? __builtin_ldexpf(sum4, ey[j]) : sum4;
+          l16 += SECOND && PAIRS ? __builtin_ldexpf(sum4, ey[j]) : sum4;
+        }
+        lsum[b] += l16;
+        if (PASS == 0) asum[b] += a16;
+        if ((t & (SM_CHAIN - 1)) == SM_CHAIN - 1) {        // uniform
+          ltot[b] += lsum[b]; lsum[b] = 0.f;
+          if (PASS == 0) { atot[b] += asum[b]; asum[b] = 0.f; }
         }
         if (PASS == 0 && a.gmax) {
-          const bool last = t + 1 == t_end || (t + 1) % a.group_tiles == 0;    // uniform
-          if (last) {
+          gmax[b] = fmaxf(gmax[b], top);
+          if (group_left == 1 || !has_next) {              // uniform
             if (xv[b]) a.gmax[x * a.ngroups + 2 * (int64_t)(t / a.group_tiles) + h] = gmax[b];
             gmax[b] = -__builtin_inff();
           }
         }
         if constexpr (PASS == 1) {
           // the answer's own row is left out of the product: its weight less one may cancel, and is applied in fp32 at the end
-          const int own = tgt[b] - y0;
-          if (__any(own >= 0 && own < 32)) {
+          const int mine = tgt[b] - y0;
+          if (__any(mine >= 0 && mine < 32)) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) w[r] = own == 8 * (r >> 2) + 4 * h + (r & 3) ? 0.f : w[r];
+            for (int r = 0; r < 16; ++r) w[r] = mine == 8 * (r >> 2) + 4 * h + (r & 3) ? 0.f : w[r];
           }
-          second(tile, b, w, false, 0u);
         }
       } else {
         // ---- weights p u of the tile's queries (rows) for the lane's table row
-        float w[16];
         const int tm = rows_t[buf][m];
-        const bool hit = __any(tm >= x_first + 32 * b && tm < x_first + 32 * b + 32);   // the answer of a query is among the wave's rows
-        unsigned own = 0u;
+        hit = __any(tm >= x_first && tm < x_first + 32);
         if (hit) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) own |= (int64_t)rows_t[buf][8 * (r >> 2) + 4 * h + (r & 3)] == x ? 1u << r : 0u;
         }
-        if (!REFS) {
-          // f = u / (sum of the query's weights); an answer's own weight less u, before it is rounded
+        const unsigned neg = (unsigned)__builtin_amdgcn_readfirstlane((int)rows_neg[buf]);
+        float ztop = -__builtin_inff();
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int y = 8 * (r >> 2) + 4 * h + (r & 3);
-            w[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][r], k[0], -rows_m[buf][y])) * rows_f[buf][y];
+        for (int j = 0; j < 4; ++j) {
+          const float4 f4 = *reinterpret_cast<const float4*>(&rows_f[buf][8 * j + 4 * h]);
+          const float fr[4] = {f4.x, f4.y, f4.z, f4.w};
+          float mr[4] = {0.f, 0.f, 0.f, 0.f};
+          if (PAIRS) {
+            const float4 m4 = *reinterpret_cast<const float4*>(&rows_m[buf][8 * j + 4 * h]);
+            mr[0] = m4.x; mr[1] = m4.y; mr[2] = m4.z; mr[3] = m4.w;
           }
-          if (hit) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) if (own >> r & 1u) w[r] -= rows_u[buf][8 * (r >> 2) + 4 * h + (r & 3)];
+          for (int e = 0; e < 4; ++e) {
+            const int r = 4 * j + e;
+            w[r] = PAIRS ? __builtin_fmaf(sc[b][r], k[j], -mr[e]) + (fr[e] - (float)ey[j]) : __builtin_fmaf(sc[b][r], k[j], fr[e]);
+            if (REFS) ztop = fmaxf(ztop, w[r]);
           }
-        } else {
-          // f = log2 |u| - log2(sum); weights are |p u| relative to the row's reference
-          float ztop = -__builtin_inff();
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int y = 8 * (r >> 2) + 4 * h + (r & 3);
-            w[r] = __builtin_fmaf(sc[b][r], k[r >> 2], -rows_m[buf][y]) + rows_f[buf][y] - (float)ey[r >> 2];
-            ztop = fmaxf(ztop, w[r]);
-          }
+          if (PAIRS) __builtin_amdgcn_sched_barrier(0);    // a block's statistics at a time: registers are full
+        }
+        if constexpr (REFS) {
           if (hit) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -393,29 +473,76 @@ k_softmax(SmArgs a) {
           }
           if (__any(ztop > ref[b] + SM_ABOVE)) {
             ztop = fmaxf(ztop, __shfl_xor(ztop, 32));
-            const float to = fmaxf(ref[b], ztop - SM_BELOW), f = __builtin_amdgcn_exp2f(ref[b] - to);
-#pragma unroll
-            for (int c = 0; c < NO; ++c) {
-#pragma unroll
-              for (int r = 0; r < 16; ++r) oacc[b][c][r] *= f;
-            }
+            const float to = fmaxf(ref[b], ztop - SM_BELOW), fct = __builtin_amdgcn_exp2f(ref[b] - to);
+            rescale(fct);
             ref[b] = to;
           }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w[r] = __builtin_amdgcn_exp2f(REFS ? w[r] - ref[b] : w[r]);
+        if (neg) {                                         // uniform
+          const unsigned bits = neg >> (4 * h);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) w[r] = __uint_as_float(__float_as_uint(w[r]) ^ ((bits << (31 - (8 * (r >> 2) + (r & 3)))) & 0x80000000u));
+        }
+        if (hit) {                                         // an answer's own weight less u, before it is rounded
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const float u = rows_u[buf][8 * (r >> 2) + 4 * h + (r & 3)];
-            w[r] = __builtin_amdgcn_exp2f(w[r] - ref[b]);
-            w[r] = u < 0.f ? -w[r] : w[r];
-            if (hit && (own >> r & 1u)) {
+            if (own >> r & 1u) {
+              const float u = rows_u[buf][8 * (r >> 2) + 4 * h + (r & 3)];
               // |u| 2^-(ey + reference) in two steps: neither factor leaves the floats' range alone
-              w[r] -= __builtin_ldexpf(u * __builtin_amdgcn_exp2f(-ref[b]), -ey[r >> 2]);
+              w[r] -= REFS ? __builtin_ldexpf(u * __builtin_amdgcn_exp2f(-ref[b]), -ey[r >> 2]) : u;
             }
           }
         }
-        second(tile, b, w, hit, own);
       }
     }
-    if (has_next) { stage.store(smem + (buf ^ 1) * G::TILE, exps[buf ^ 1], tid); store_rows(buf ^ 1); }
+    if (PASS == 0) group_left = group_left == 1 ? a.group_tiles : group_left - 1;
+
+    // ---- O^T += Y^T P
+    if constexpr (SECOND) {
+      v8s ph[2], pl[2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        float p8[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p8[e] = w[8 * s + e];
+        if constexpr (PAIRS) {
+          split8<true>(p8, neg1, ph[s], pl[s]);
+        } else {
+          ph[s] = sm_round8<TYPE>(p8);
+          if (PASS == 2 && hit) {                          // what an answer's own weight loses to 16 bits counts too
+            float r8[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r8[e] = (own >> (8 * s + e) & 1u) ? p8[e] - sm_rounded<TYPE>(p8[e]) : 0.f;
+            pl[s] = sm_round8<TYPE>(r8);
+          }
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (!EARLY) {
+#pragma unroll
+        for (int n = 0; n < PG; ++n) read_tr(n);
+      }
+      if constexpr (WIDE) unrolled<NO>([&](auto block) { constexpr int c = block; v16f& o = oacc[c]; asm volatile("" : "+a"(o)); });
+      unrolled<NG>([&](auto step) {
+        constexpr int n = step, s = n / NO, c = n % NO;
+        const v8s yh = tf[n % PG][0], yl = tf[n % PG][PL - 1];
+        if (n + PG < NG) read_tr(n + PG);
+        if constexpr (PAIRS) { oacc[c] = sm_mfma<TYPE>(yl, ph[s], oacc[c]); oacc[c] = sm_mfma<TYPE>(yh, pl[s], oacc[c]); }
+        oacc[c] = sm_mfma<TYPE>(yh, ph[s], oacc[c]);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if (!PAIRS && PASS == 2 && hit) {                    // uniform, rare
+        unrolled<NG>([&](auto step) {
+          constexpr int n = step, s = n / NO, c = n % NO;
+          read_tr(n);
+          oacc[c] = sm_mfma<TYPE>(tf[n % PG][0], pl[s], oacc[c]);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+      }
+    }
+    if (has_next) { stage.store(smem + (bofs ^ G::TILE), exps[buf ^ 1], dim, tid); store_rows(buf ^ 1); }
     __syncthreads();
   }
 
@@ -424,23 +551,25 @@ k_softmax(SmArgs a) {
   for (int b = 0; b < QB; ++b) {
     const int64_t x = x_first + 32 * b + m;
     if (PASS != 2) {                                       // the halves of a tile's rows share their reference
-      const float l = lsum[b] + __shfl_xor(lsum[b], 32), s = asum[b] + __shfl_xor(asum[b], 32);
+      const float lw = lsum[b] + ltot[b], aw = asum[b] + atot[b];
+      const float l = lw + __shfl_xor(lw, 32), s = aw + __shfl_xor(aw, 32);
       if (h == 0 && xv[b]) a.stats[(size_t)part * a.n_x + x] = make_float4(ref[b], l, s, 0.f);
     }
     if constexpr (SECOND) {
       float f = 1.f;                                       // twice the square root: the power itself may leave the floats' range
       if (PASS == 2 && REFS) f = __builtin_amdgcn_exp2f(0.5f * ref[b]);
-#pragma unroll
-      for (int c = 0; c < NO; ++c) {
+      unrolled<NO>([&](auto block) {
+        constexpr int c = block;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int col = 32 * c + 8 * j + 4 * h;
-          const float v[4] = {oacc[b][c][4 * j] * f * f, oacc[b][c][4 * j + 1] * f * f, oacc[b][c][4 * j + 2] * f * f, oacc[b][c][4 * j + 3] * f * f};
+          const float v[4] = {oacc[c][4 * j] * f * f, oacc[c][4 * j + 1] * f * f, oacc[c][4 * j + 2] * f * f, oacc[c][4 * j + 3] * f * f};
           if (!xv[b] || col >= dim) continue;
           if (PASS == 2 && a.out) store_cols<TYPE, 4>((T*)a.out + x * a.out_stride, col, dim, v);
           else *reinterpret_cast<float4*>(a.O + ((size_t)part * a.n_x + x) * a.o_pitch + col) = make_float4(v[0], v[1], v[2], v[3]);
         }
-      }
+      });
     }
   }
 }

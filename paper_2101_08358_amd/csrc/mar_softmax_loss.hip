@@ -11,7 +11,6 @@ struct LossArgs {
   const int32_t* targets; const float* weights;
   const float4* stats; const float* O;
   float *row_m, *row_f, *row_u;
-  int32_t log_f;                   // pass 2 takes log2 |u| - log2(sum) in place of u / sum
   float *loss, *lse;
   void* grad; int64_t grad_stride;
 };
@@ -44,7 +43,7 @@ k_loss_rows(LossArgs a) {
       const float us = u * a.scale;
       a.row_m[q] = u != 0.f ? m : 0.f;
       a.row_u[q] = us;
-      a.row_f[q] = a.log_f ? (us != 0.f ? __builtin_amdgcn_logf(fabsf(us)) - __builtin_amdgcn_logf(l) : -__builtin_inff()) : (us != 0.f ? us / l : 0.f);
+      a.row_f[q] = us != 0.f ? log2f(fabsf(us)) - log2f(l) : -__builtin_inff();
     }
   }
   if (!a.grad) return;
@@ -158,7 +157,6 @@ extern "C" int mar_softmax_loss(const mar_softmax* p, const void* queries, const
     r.scale = p->scale; r.unscale = (double)p->scale / (double)c;
     r.targets = targets; r.weights = weights; r.stats = a.stats; r.O = a.O;
     if (grad_table) { r.row_m = (float*)(ws + L.row_m); r.row_f = (float*)(ws + L.row_f); r.row_u = (float*)(ws + L.row_u); }
-    r.log_f = p->dtype != MAR_DTYPE_BF16;
     r.loss = loss; r.lse = lse; r.grad = grad_queries; r.grad_stride = grad_query_stride;
     const dim3 grid((unsigned)((p->num_queries + 3) / 4)), block(256);
     if (p->dtype == MAR_DTYPE_FP32) hipLaunchKernelGGL(k_loss_rows<0>, grid, block, 0, st, r);
