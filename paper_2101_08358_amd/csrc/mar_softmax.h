@@ -19,11 +19,17 @@
 #include "mar_split.h"
 
 constexpr int sm_nk(int d) { return d <= 32 ? 2 : (d <= 64 ? 4 : (d <= 112 ? 7 : (d <= 128 ? 8 : (d <= 192 ? 12 : (d <= 256 ? 16 : 25))))); }
+#define MAR_SOFTMAX_MAX_PARTS 64  // of the passes with a second product: a lane of k_loss_rows each
 #define SM_TY 32                  // rows of a tile
 #define SM_NO_REF -3.0e38f        // reference of a row that has met no score yet
 
+// Tiles of rows as the passes read them ("images", [tiles][planes][32][pitch], units of a row in the order of sp_swizzle), with the
+// exponents of every eight rows: laid out once, they are copied into LDS as they lie, by every stripe.
+struct SmImage { const char* tiles; const int* exps; };
+
 struct SmArgs {
   const void *X, *Y;               // stationary and streamed rows
+  SmImage ximg, yimg;              // the same as images
   int64_t x_stride, y_stride;
   int32_t n_x, n_y, dim, nstripes, units;
   int32_t parts, tps;              // parts of the streamed tiles, tiles each
@@ -36,8 +42,21 @@ struct SmArgs {
   const int32_t* targets;
   float* O; int32_t o_pitch;       // [parts][n_x][o_pitch]
   const float* row_m; const float* row_f; const float* row_u;   // pass 2: per query, see k_loss_rows
+  const int32_t* own_top;          // pass 2, per stationary row: largest log2 |u| - e of the queries whose answer it is (own_key), or SM_NO_OWN
   void* out; int64_t out_stride;   // pass 2 in one part: the gradient itself
 };
+
+// Lays rows out as images.  skip: where not NULL, a row whose weight (ids outside 0 .. num_ids - 1: 0) is 0 becomes zeros if it
+// holds values that are not finite.
+struct SmPackArgs {
+  const void* src; int64_t stride; int32_t n, dim;
+  char* tiles; int* exps;
+  const int32_t* ids; const float* weights; int64_t num_ids;
+  int32_t* own_top;                // where not NULL: [n], set to SM_NO_OWN
+};
+size_t sm_image_bytes(int dtype, int dim, int64_t rows);   // a multiple of 256
+size_t sm_exps_bytes(int64_t rows);
+hipError_t sm_pack(int dtype, const SmPackArgs& a, hipStream_t st);
 
 struct SmPlan { int32_t qb, stripes, parts, tps, ntiles; };
 

@@ -5,6 +5,10 @@
 // maxima, whose rows are scored again: in fp32, and the best of them in 64 bits, by which they are ordered.
 #include "mar_softmax_dev.h"
 
+// Stripes of queries from which the table is laid out as images first.
+#ifndef MAR_SOFTMAX_IMAGES
+#define MAR_SOFTMAX_IMAGES 8
+#endif
 #define SM_MARGIN 4               // groups, and rows, kept beyond the number asked for: what fp32 cannot tell apart
 
 struct AnswerArgs {
@@ -220,7 +224,7 @@ SmPlan sm_plan(int dtype, int dim, int pass, int64_t n_x, int64_t n_y, int multi
   const int64_t slots = 256 * sm_waves(dtype, nk, pass);
   int64_t best = INT64_MAX;
   r.parts = 1; r.tps = r.ntiles;
-  const int most = pass == 0 ? 1024 : 64;
+  const int most = pass == 0 ? 1024 : MAR_SOFTMAX_MAX_PARTS;
   for (int k = 1; k <= most && k <= r.ntiles; ++k) {
     int64_t tps = (r.ntiles + k - 1) / k;
     tps = (tps + multiple - 1) / multiple * multiple;
@@ -240,32 +244,65 @@ static int group_tiles(const mar_softmax* p, int num_top) {
   return k;
 }
 
-struct ProbsLayout { size_t stats, gmax, bytes; SmPlan p0; int group_tiles; int64_t ngroups; };
+struct ProbsLayout { size_t stats, gmax, qtiles, qexps, wtiles, wexps, bytes; SmPlan p0; int group_tiles; int64_t ngroups; bool images; };
 static ProbsLayout probs_layout(const mar_softmax* p, int num_top) {
   ProbsLayout L;
   L.group_tiles = num_top ? group_tiles(p, num_top) : 1;
   L.p0 = sm_plan(p->dtype, p->dim, 0, p->num_queries, p->num_rows, L.group_tiles);
   L.ngroups = num_top ? 2 * (int64_t)((L.p0.ntiles + L.group_tiles - 1) / L.group_tiles) : 0;
   const size_t T = (size_t)p->num_queries;
-  L.stats = 0;
-  L.gmax = ((size_t)L.p0.parts * T * sizeof(float4) + 255) / 256 * 256;
-  L.bytes = L.gmax + (T * (size_t)L.ngroups * 4 + 255) / 256 * 256;
-  if (L.bytes < 256) L.bytes = 256;
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
+  L.stats = take((size_t)L.p0.parts * T * sizeof(float4));
+  L.gmax = take(T * (size_t)L.ngroups * 4);
+  L.images = L.p0.stripes >= MAR_SOFTMAX_IMAGES;
+  L.qtiles = L.qexps = L.wtiles = L.wexps = at;
+  if (L.images) {
+    L.qtiles = take(sm_image_bytes(p->dtype, p->dim, p->num_queries)); L.qexps = take(sm_exps_bytes(p->num_queries));
+    L.wtiles = take(sm_image_bytes(p->dtype, p->dim, p->num_rows)); L.wexps = take(sm_exps_bytes(p->num_rows));
+  }
+  L.bytes = at > 256 ? at : 256;
   return L;
 }
 
-template <int TYPE> static void launch_nk(const SmArgs& a, hipStream_t st) {
+template <int TYPE, bool IMG> static void launch_nk(const SmArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)((a.units + 7) / 8 * 8)), block(256);
   switch (sm_nk(a.dim)) {
-    case 2: hipLaunchKernelGGL((k_softmax<TYPE, 2, 0>), grid, block, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((k_softmax<TYPE, 4, 0>), grid, block, 0, st, a); break;
-    case 7: hipLaunchKernelGGL((k_softmax<TYPE, 7, 0>), grid, block, 0, st, a); break;
-    case 8: hipLaunchKernelGGL((k_softmax<TYPE, 8, 0>), grid, block, 0, st, a); break;
-    case 12: hipLaunchKernelGGL((k_softmax<TYPE, 12, 0>), grid, block, 0, st, a); break;
-    case 16: hipLaunchKernelGGL((k_softmax<TYPE, 16, 0>), grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL((k_softmax<TYPE, 25, 0>), grid, block, 0, st, a); break;
+    case 2: hipLaunchKernelGGL((k_softmax<TYPE, 2, 0, IMG>), grid, block, 0, st, a); break;
+    case 4: hipLaunchKernelGGL((k_softmax<TYPE, 4, 0, IMG>), grid, block, 0, st, a); break;
+    case 7: hipLaunchKernelGGL((k_softmax<TYPE, 7, 0, IMG>), grid, block, 0, st, a); break;
+    case 8: hipLaunchKernelGGL((k_softmax<TYPE, 8, 0, IMG>), grid, block, 0, st, a); break;
+    case 12: hipLaunchKernelGGL((k_softmax<TYPE, 12, 0, IMG>), grid, block, 0, st, a); break;
+    case 16: hipLaunchKernelGGL((k_softmax<TYPE, 16, 0, IMG>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((k_softmax<TYPE, 25, 0, IMG>), grid, block, 0, st, a); break;
   }
 }
+template <int TYPE> static void launch_pack(const SmPackArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)(((int64_t)a.n + SM_TY - 1) / SM_TY)), block(256);
+  switch (sm_nk(a.dim)) {
+    case 2: hipLaunchKernelGGL((k_softmax_pack<TYPE, 2>), grid, block, 0, st, a); break;
+    case 4: hipLaunchKernelGGL((k_softmax_pack<TYPE, 4>), grid, block, 0, st, a); break;
+    case 7: hipLaunchKernelGGL((k_softmax_pack<TYPE, 7>), grid, block, 0, st, a); break;
+    case 8: hipLaunchKernelGGL((k_softmax_pack<TYPE, 8>), grid, block, 0, st, a); break;
+    case 12: hipLaunchKernelGGL((k_softmax_pack<TYPE, 12>), grid, block, 0, st, a); break;
+    case 16: hipLaunchKernelGGL((k_softmax_pack<TYPE, 16>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((k_softmax_pack<TYPE, 25>), grid, block, 0, st, a); break;
+  }
+}
+hipError_t sm_pack(int dtype, const SmPackArgs& a, hipStream_t st) {
+  if (dtype == MAR_DTYPE_FP32) launch_pack<0>(a, st); else if (dtype == MAR_DTYPE_BF16) launch_pack<1>(a, st); else launch_pack<2>(a, st);
+  return hipGetLastError();
+}
+size_t sm_image_bytes(int dtype, int dim, int64_t rows) {
+  const int nk = sm_nk(dim);
+  return (size_t)((rows + SM_TY - 1) / SM_TY) * SM_TY * sp_pitch(nk) * (dtype == MAR_DTYPE_FP32 ? 2 : 1);
+}
+size_t sm_exps_bytes(int64_t rows) { return ((size_t)((rows + SM_TY - 1) / SM_TY) * 16 + 255) / 256 * 256; }
+template <bool IMG> static hipError_t launch_stats(int dtype, const SmArgs& a, hipStream_t st) {
+  if (dtype == MAR_DTYPE_FP32) launch_nk<0, IMG>(a, st); else if (dtype == MAR_DTYPE_BF16) launch_nk<1, IMG>(a, st); else launch_nk<2, IMG>(a, st);
+  return hipGetLastError();
+}
+
 // Few queries: a wide workgroup each; many: enough of them to fill the device at 256 threads.
 template <int TYPE> static void launch_answer(const AnswerArgs& a, hipStream_t st) {
   if (a.n >= 512) hipLaunchKernelGGL((k_answer<TYPE, 256, 2048>), dim3((unsigned)a.n), dim3(256), 0, st, a);
@@ -316,8 +353,21 @@ extern "C" int mar_log_probs(const mar_softmax* p, const void* queries, const vo
   a.gmax = num_top ? (float*)((char*)workspace + L.gmax) : nullptr;
   a.ngroups = L.ngroups; a.group_tiles = L.group_tiles;
   a.allowed = allowed; a.allowed_stride = allowed_stride;
-  if (p->dtype == MAR_DTYPE_FP32) launch_nk<0>(a, st); else if (p->dtype == MAR_DTYPE_BF16) launch_nk<1>(a, st); else launch_nk<2>(a, st);
-  hipError_t e = hipGetLastError();
+  hipError_t e;
+  if (L.images) {
+    SmPackArgs k = {};
+    k.dim = p->dim;
+    k.src = table; k.stride = p->row_stride; k.n = (int32_t)p->num_rows; k.tiles = (char*)workspace + L.wtiles; k.exps = (int*)((char*)workspace + L.wexps);
+    e = sm_pack(p->dtype, k, st);
+    k.src = queries; k.stride = p->query_stride; k.n = p->num_queries; k.tiles = (char*)workspace + L.qtiles; k.exps = (int*)((char*)workspace + L.qexps);
+    if (e == hipSuccess) e = sm_pack(p->dtype, k, st);
+    if (e != hipSuccess) { mar_set_error("image kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
+    a.ximg = {(char*)workspace + L.qtiles, (const int*)((char*)workspace + L.qexps)};
+    a.yimg = {(char*)workspace + L.wtiles, (const int*)((char*)workspace + L.wexps)};
+    e = launch_stats<true>(p->dtype, a, st);
+  } else {
+    e = launch_stats<false>(p->dtype, a, st);
+  }
   if (e != hipSuccess) { mar_set_error("softmax kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
   AnswerArgs r = {};
   r.Q = queries; r.W = table; r.q_stride = p->query_stride; r.w_stride = p->row_stride; r.rows = p->num_rows;

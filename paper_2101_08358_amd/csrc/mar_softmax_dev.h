@@ -69,10 +69,9 @@ template <int TYPE, int NK> struct SmStage {
   int big;
   bool zero;                                               // the row is taken as zeros whatever it holds
   const T* row;
-  __device__ __forceinline__ void begin(const T* __restrict__ Y, int64_t stride, int n_y, int y0, int tid, const float* __restrict__ use) {
-    const int y = min(y0 + (tid >> 3), n_y - 1);           // rows beyond the last are the last again
-    row = Y + (int64_t)y * stride;
-    zero = use && use[y] == 0.f;
+  __device__ __forceinline__ void begin(const T* __restrict__ Y, int64_t stride, int n_y, int y0, int tid) {
+    row = Y + (int64_t)min(y0 + (tid >> 3), n_y - 1) * stride;               // rows beyond the last are the last again
+    zero = false;
     big = 0;
   }
   __device__ __forceinline__ void fetch(int p, int dim, int tid, row_u4 (&v)[G::PLANES]) const {
@@ -145,13 +144,18 @@ template <int TYPE, int NK> struct SmStage {
   }
 };
 
+// Floats as integers of the same order.
+#define SM_NO_OWN INT32_MIN
+__device__ __forceinline__ int own_key(float v) { const int b = __float_as_int(v); return b < 0 ? b ^ 0x7fffffff : b; }
+__device__ __forceinline__ float own_float(int k) { return __int_as_float(k < 0 ? k ^ 0x7fffffff : k); }
 // Softmax weights in fp16 (and as pairs of f16) lie between 2^-24 and 2^16: the reference is put 12 below the largest exponent met
 // and moves when one exceeds it by more than 15; what is 2^-36 of the largest weight is lost to the second product (never to the sum).
 #define SM_ABOVE 15.f
 #define SM_BELOW 12.f
 #define SM_CHAIN 16               // tiles whose weights are summed before their sum is added to the part's: chains of fp32 sums stay short
 
-template <int TYPE, int NK, int PASS>
+// IMG: both matrices as images; else from their rows (a table that few queries meet is not worth laying out).
+template <int TYPE, int NK, int PASS, bool IMG>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sm_waves(TYPE, NK, PASS), sm_waves(TYPE, NK, PASS))))
 k_softmax(SmArgs a) {
   typedef SmGeom<TYPE, NK> G;
@@ -162,12 +166,13 @@ k_softmax(SmArgs a) {
   constexpr int NO = SECOND ? (NK + 1) / 2 : 1;            // 32-column blocks of the output
   constexpr bool REFS = PASS != 2 || TYPE != MAR_DTYPE_BF16 || NK > 16;   // weights relative to a reference (bf16 does without; the widest rows' registers do not)
   constexpr int PL = G::PLANES;
+  static_assert(IMG || PASS == 0, "passes with a second product take images");
   static_assert(QB == 1 || PASS == 0, "passes with a second product take one block a wave");
   __shared__ __attribute__((aligned(1024))) char smem[2 * G::TILE];
   __shared__ int exps[2][4];
   // pass 2, per query of a tile: f = log2(|u| / sum of its weights), m its reference (16-bit types: f - m and nothing)
   __shared__ __attribute__((aligned(16))) float rows_m[2][SM_TY], rows_f[2][SM_TY], rows_u[2][SM_TY];
-  __shared__ int rows_t[2][SM_TY];
+  __shared__ __attribute__((aligned(16))) int rows_t[2][SM_TY];
   __shared__ unsigned rows_neg[2];                         // queries with a negative u
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -182,10 +187,19 @@ k_softmax(SmArgs a) {
   const int dim = a.dim;
 
   // zeros: units beyond the columns that a tile's copies write
-  for (int k = tid * 16; k < 2 * G::TILE; k += 256 * 16) *reinterpret_cast<row_u4*>(smem + k) = (row_u4)(0u);
+  if (!IMG) for (int k = tid * 16; k < 2 * G::TILE; k += 256 * 16) *reinterpret_cast<row_u4*>(smem + k) = (row_u4)(0u);
   SmStage<TYPE, NK> stage;
   const T* Y = (const T*)a.Y;
-  const float* use = PASS == 2 ? a.row_u : nullptr;
+  // images: copied by loads that write LDS, 1 KB a wave instruction; nothing but the end of the tile waits for them
+  int token = 0;
+  constexpr int NCW = (G::TILE / 1024 + 3) / 4;            // pieces a wave
+  auto copy = [&](int t, int buf, int p) {
+    const int piece = 4 * p + wave;
+    if (piece < G::TILE / 1024)
+      buf_load4_to_lds(buf_words(a.yimg.tiles + (size_t)t * G::TILE, G::TILE), lds_address_b(smem) + buf * G::TILE + piece * 1024, lane * 16, piece * 1024, token);
+  };
+  int ye = 0;                                              // exponent of block lane % 4 of the tile on its way
+  auto ask_exps = [&](int t) { if (IMG && PAIRS) ye = a.yimg.exps[4 * (int64_t)t + (lane & 3)]; };
   float q_m = 0.f, q_f = 0.f, q_u = 0.f;
   int q_t = -1;
   auto load_rows = [&](int y0) {
@@ -206,9 +220,15 @@ k_softmax(SmArgs a) {
     }
   };
   if (t_begin < t_end) {
-    stage.begin(Y, a.y_stride, a.n_y, t_begin * SM_TY, tid, use);
+    if constexpr (IMG) {
 #pragma unroll
-    for (int p = 0; p < G::NP; ++p) stage.load(p, dim, tid);
+      for (int p = 0; p < NCW; ++p) copy(t_begin, 0, p);
+      ask_exps(t_begin);
+    } else {
+      stage.begin(Y, a.y_stride, a.n_y, t_begin * SM_TY, tid);
+#pragma unroll
+      for (int p = 0; p < G::NP; ++p) stage.load(p, dim, tid);
+    }
     load_rows(t_begin * SM_TY);
   }
 
@@ -226,7 +246,18 @@ k_softmax(SmArgs a) {
     ex[b] = 0;
     tgt[b] = PASS == 1 && xv[b] ? a.targets[xr] : -1;
     words[b] = PASS == 0 && a.allowed ? a.allowed + xr * a.allowed_stride : nullptr;
-    if (PAIRS) {
+    if constexpr (IMG) {
+      const int64_t xt = min((x_first + 32 * b) / SM_TY, (int64_t)(a.n_x - 1) / SM_TY);                // a block is a tile
+      const char* const row = a.ximg.tiles + xt * G::TILE + m * G::PA;
+      const int swz = 16 * sp_swizzle(G::UNITS, m);
+      if (PAIRS) ex[b] = a.ximg.exps[4 * xt + (m >> 3)];
+      unrolled<NK>([&](auto step) {
+        constexpr int s = step;
+        xh[b][s] = *reinterpret_cast<const v8s*>(row + ((32 * s + 16 * h) ^ swz));
+        if constexpr (PAIRS) xl[b][s] = *reinterpret_cast<const v8s*>(row + G::PLANE + ((32 * s + 16 * h) ^ swz));
+      });
+    }
+    if (PAIRS && !IMG) {
       int big = 0;
       unrolled<NK>([&](int s) {
         float v[8];
@@ -238,7 +269,7 @@ k_softmax(SmArgs a) {
       big = max(big, __shfl_xor(big, 32));
       ex[b] = sm_exponent(big);
     }
-    unrolled<NK>([&](auto step) {
+    if constexpr (!IMG) unrolled<NK>([&](auto step) {
       constexpr int s = step;
       if constexpr (PAIRS) {
         float v[8];
@@ -258,7 +289,12 @@ k_softmax(SmArgs a) {
   for (int c = 0; c < NO; ++c) oacc[c] = (v16f)(0.f);
 #pragma unroll
   for (int b = 0; b < QB; ++b) {
-    ref[b] = SM_NO_REF; lsum[b] = ltot[b] = asum[b] = atot[b] = 0.f; gmax[b] = -__builtin_inff();
+    ref[b] = SM_NO_REF;
+    if (PASS == 2 && REFS) {                               // the weights of the row's own queries stay below it
+      const int own = a.own_top[min(x_first + 32 * b + m, (int64_t)a.n_x - 1)];
+      if (own != SM_NO_OWN) ref[b] = own_float(own) - SM_BELOW;
+    }
+    lsum[b] = ltot[b] = asum[b] = atot[b] = 0.f; gmax[b] = -__builtin_inff();
     word_next[b] = PASS == 0 && a.allowed && t_begin < t_end ? words[b][t_begin] : ~0u;
   }
   int group_left = a.group_tiles;
@@ -284,8 +320,17 @@ k_softmax(SmArgs a) {
       if (WIDE) asm volatile("" : "+a"(oacc[c]));
     });
   };
-  __syncthreads();                                         // the zeros are there
-  if (t_begin < t_end) { stage.store(smem, exps[0], dim, tid); store_rows(0); }
+  auto land = [&](int buf) {                               // the tile on its way is in LDS, but for the barrier
+    if constexpr (IMG) {
+      if (PAIRS && tid < 4) exps[buf][tid] = ye;
+      store_rows(buf);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    } else {
+      stage.store(smem + buf * G::TILE, exps[buf], dim, tid);
+    }
+  };
+  if (!IMG) __syncthreads();                               // the zeros are there
+  if (t_begin < t_end) land(0);
   __syncthreads();
 
   for (int t = t_begin; t < t_end; ++t) {
@@ -298,7 +343,10 @@ k_softmax(SmArgs a) {
       word[b] = word_next[b];
       if (PASS == 0 && has_next && a.allowed) word_next[b] = words[b][t + 1];
     }
-    if (has_next) { stage.begin(Y, a.y_stride, a.n_y, y0 + SM_TY, tid, use); load_rows(y0 + SM_TY); }
+    if (has_next) {
+      if constexpr (IMG) ask_exps(t + 1); else stage.begin(Y, a.y_stride, a.n_y, y0 + SM_TY, tid);
+      load_rows(y0 + SM_TY);
+    }
 
     // ---- scores; the streamed fragments are read PD steps ahead, the next tile's pieces are asked for between the steps
     v16f sc[QB];
@@ -324,8 +372,13 @@ k_softmax(SmArgs a) {
           sc[b] = sm_mfma<TYPE>(yh, xh[b][s], sc[b]);
         }
         if (has_next) {
+          if constexpr (IMG) {
 #pragma unroll
-          for (int p = s * G::NP / NK; p < (s + 1) * G::NP / NK; ++p) stage.load(p, dim, tid);
+            for (int p = s * NCW / NK; p < (s + 1) * NCW / NK; ++p) copy(t + 1, buf ^ 1, p);
+          } else {
+#pragma unroll
+            for (int p = s * G::NP / NK; p < (s + 1) * G::NP / NK; ++p) stage.load(p, dim, tid);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
       });
@@ -353,7 +406,6 @@ k_softmax(SmArgs a) {
 
     float w[16];
     bool hit = false;                                      // PASS 2: the answer of one of the tile's queries is among the wave's rows
-    unsigned own = 0u;
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
       // ---- t = sc k[r / 4]: scores in log2 units
@@ -440,11 +492,7 @@ k_softmax(SmArgs a) {
       } else {
         // ---- weights p u of the tile's queries (rows) for the lane's table row
         const int tm = rows_t[buf][m];
-        hit = __any(tm >= x_first && tm < x_first + 32);
-        if (hit) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) own |= (int64_t)rows_t[buf][8 * (r >> 2) + 4 * h + (r & 3)] == x ? 1u << r : 0u;
-        }
+        const bool hit = __any(tm >= x_first && tm < x_first + 32);   // the answer of one of the tile's queries is among the wave's rows
         const unsigned neg = (unsigned)__builtin_amdgcn_readfirstlane((int)rows_neg[buf]);
         float ztop = -__builtin_inff();
 #pragma unroll
@@ -465,12 +513,6 @@ k_softmax(SmArgs a) {
           if (PAIRS) __builtin_amdgcn_sched_barrier(0);    // a block's statistics at a time: registers are full
         }
         if constexpr (REFS) {
-          if (hit) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              if (own >> r & 1u) ztop = fmaxf(ztop, __builtin_amdgcn_logf(fabsf(rows_u[buf][8 * (r >> 2) + 4 * h + (r & 3)])) - (float)ey[r >> 2]);
-            }
-          }
           if (__any(ztop > ref[b] + SM_ABOVE)) {
             ztop = fmaxf(ztop, __shfl_xor(ztop, 32));
             const float to = fmaxf(ref[b], ztop - SM_BELOW), fct = __builtin_amdgcn_exp2f(ref[b] - to);
@@ -487,12 +529,13 @@ k_softmax(SmArgs a) {
         }
         if (hit) {                                         // an answer's own weight less u, before it is rounded
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            if (own >> r & 1u) {
-              const float u = rows_u[buf][8 * (r >> 2) + 4 * h + (r & 3)];
-              // |u| 2^-(ey + reference) in two steps: neither factor leaves the floats' range alone
-              w[r] -= REFS ? __builtin_ldexpf(u * __builtin_amdgcn_exp2f(-ref[b]), -ey[r >> 2]) : u;
-            }
+          for (int j = 0; j < 4; ++j) {
+            const float4 u4 = *reinterpret_cast<const float4*>(&rows_u[buf][8 * j + 4 * h]);
+            const int4 t4 = *reinterpret_cast<const int4*>(&rows_t[buf][8 * j + 4 * h]);
+            const float u[4] = {u4.x, u4.y, u4.z, u4.w}, f = REFS ? __builtin_amdgcn_exp2f(-(ref[b] + (float)ey[j])) : 1.f;
+            const int id[4] = {t4.x, t4.y, t4.z, t4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[4 * j + e] -= id[e] == (int)x ? u[e] * f : 0.f;
           }
         }
       }
@@ -511,12 +554,6 @@ k_softmax(SmArgs a) {
           split8<true>(p8, neg1, ph[s], pl[s]);
         } else {
           ph[s] = sm_round8<TYPE>(p8);
-          if (PASS == 2 && hit) {                          // what an answer's own weight loses to 16 bits counts too
-            float r8[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) r8[e] = (own >> (8 * s + e) & 1u) ? p8[e] - sm_rounded<TYPE>(p8[e]) : 0.f;
-            pl[s] = sm_round8<TYPE>(r8);
-          }
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -533,16 +570,8 @@ k_softmax(SmArgs a) {
         oacc[c] = sm_mfma<TYPE>(yh, ph[s], oacc[c]);
         __builtin_amdgcn_sched_barrier(0);
       });
-      if (!PAIRS && PASS == 2 && hit) {                    // uniform, rare
-        unrolled<NG>([&](auto step) {
-          constexpr int n = step, s = n / NO, c = n % NO;
-          read_tr(n);
-          oacc[c] = sm_mfma<TYPE>(tf[n % PG][0], pl[s], oacc[c]);
-          __builtin_amdgcn_sched_barrier(0);
-        });
-      }
     }
-    if (has_next) { stage.store(smem + (bofs ^ G::TILE), exps[buf ^ 1], dim, tid); store_rows(buf ^ 1); }
+    if (has_next) land(buf ^ 1);
     __syncthreads();
   }
 
@@ -572,4 +601,37 @@ k_softmax(SmArgs a) {
       });
     }
   }
+}
+
+// Images: a workgroup a tile.
+template <int TYPE, int NK>
+__global__ void __launch_bounds__(256)
+k_softmax_pack(SmPackArgs a) {
+  typedef SmGeom<TYPE, NK> G;
+  typedef typename RowType<TYPE>::T T;
+  const int tid = threadIdx.x, t = blockIdx.x, y = min(t * SM_TY + (tid >> 3), a.n - 1);
+  char* const tile = a.tiles + (size_t)t * G::TILE;
+  SmStage<TYPE, NK> stage;
+  stage.begin((const T*)a.src, a.stride, a.n, t * SM_TY, tid);
+#pragma unroll
+  for (int p = 0; p < G::NP; ++p) stage.load(p, a.dim, tid);
+  if (a.ids) {
+    const int id = a.ids[y];
+    if (id < 0 || id >= a.num_ids || (a.weights && a.weights[y] == 0.f)) {
+      bool finite = true;
+      for (int c = tid & 7; c < a.dim; c += 8) finite = finite && fabsf((float)stage.row[c]) <= 3.4028234663852886e38f;
+      // the row's eight threads are neighbours, all of them here
+      unsigned bad = finite ? 0u : 1u;
+      bad |= __shfl_xor(bad, 1); bad |= __shfl_xor(bad, 2); bad |= __shfl_xor(bad, 4);
+      stage.zero = bad != 0u;
+    }
+  }
+  if (a.own_top && tid < SM_TY && t * SM_TY + tid < a.n) a.own_top[t * SM_TY + tid] = SM_NO_OWN;
+  // units that no piece fills: up to the pitch
+  for (int u = 2 * NK + (tid & 7); u < G::UNITS; u += 8) {
+#pragma unroll
+    for (int k = 0; k < G::PLANES; ++k)
+      *reinterpret_cast<row_u4*>(tile + k * G::PLANE + (tid >> 3) * G::PA + ((16 * u) ^ (16 * sp_swizzle(G::UNITS, tid >> 3)))) = (row_u4)(0u);
+  }
+  stage.store(tile, a.exps ? a.exps + 4 * (size_t)t : nullptr, a.dim, tid);
 }

@@ -11,24 +11,33 @@ struct LossArgs {
   const int32_t* targets; const float* weights;
   const float4* stats; const float* O;
   float *row_m, *row_f, *row_u;
+  const int* exps; int32_t* own_top;   // exponents of the queries' image (fp32)
   float *loss, *lse;
   void* grad; int64_t grad_stride;
 };
 
-// A wave per query.
-template <int TYPE>
-__global__ void __launch_bounds__(256)
+// WAVES waves per query: wave w takes parts w, w + WAVES, ..
+template <int TYPE, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES)
 k_loss_rows(LossArgs a) {
   typedef typename RowType<TYPE>::T T;
-  const int lane = threadIdx.x & 63;
-  const int64_t q = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (q >= a.n) return;
-  float m = SM_NO_REF, l = 0.f;
-  for (int p = 0; p < a.parts; ++p) m = fmaxf(m, a.stats[(size_t)p * a.n + q].x);
-  for (int p = 0; p < a.parts; ++p) { const float4 s = a.stats[(size_t)p * a.n + q]; l += s.y * __builtin_amdgcn_exp2f(s.x - m); }
+  __shared__ float fac[MAR_SOFTMAX_MAX_PARTS];
+  __shared__ float4 sums[WAVES][(MAR_MAX_DIM + 3) / 4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t q = blockIdx.x;
+  // every wave for itself: a lane a part
+  const float4 mine = lane < a.parts ? a.stats[(size_t)lane * a.n + q] : make_float4(SM_NO_REF, 0.f, 0.f, 0.f);
+  float m = mine.x;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  const float f = __builtin_amdgcn_exp2f(mine.x - m);
+  float l = mine.y * f;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) l += __shfl_xor(l, o);
+  if (wave == 0) fac[lane] = f;
   const int t = a.targets[q];
   const bool has = t >= 0 && t < a.rows;
-  const float u = has ? (a.weights ? a.weights[q] : 1.f) : 0.f;
+  const float u = has ? (a.weights ? a.weights[q] : 1.f) : 0.f, us = u * a.scale;
   const T* qr = (const T*)a.Q + q * a.q_stride;
   const T* wr = (const T*)a.W + (int64_t)(has ? t : 0) * a.w_stride;
   double dot = 0.0;
@@ -36,25 +45,50 @@ k_loss_rows(LossArgs a) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) dot += __shfl_xor(dot, o);
   const double lse = (double)m * a.unscale + (double)logf(l), over = dot * (double)a.scale - lse;   // log p of the answer
-  if (lane == 0) {
+  if (threadIdx.x == 0) {
     if (a.lse) a.lse[q] = (float)lse;
     if (a.loss) a.loss[q] = u != 0.f ? (float)(-(double)u * over) : 0.f;
     if (a.row_m) {
-      const float us = u * a.scale;
       a.row_m[q] = u != 0.f ? m : 0.f;
       a.row_u[q] = us;
-      a.row_f[q] = us != 0.f ? log2f(fabsf(us)) - log2f(l) : -__builtin_inff();
+      const float lu = log2f(fabsf(us));
+      // largest of the row's own queries: the order in which they come does not matter.  A popular row's value is mostly there
+      // already (every query's atomic instead: 10,000 queries, a third of them with one answer, 66 us; none 22)
+      if (us != 0.f) {
+        const int key = own_key(lu - (TYPE == MAR_DTYPE_FP32 ? (float)a.exps[q >> 3] : 0.f));
+        if (__hip_atomic_load(a.own_top + t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < key) atomicMax(a.own_top + t, key);
+      }
+      a.row_f[q] = us != 0.f ? lu - log2f(l) : -__builtin_inff();
     }
   }
   if (!a.grad) return;
+  __syncthreads();
+  const int quads = a.o_pitch / 4;
+  for (int c = lane; c < quads; c += 64) {
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float* O = a.O + (size_t)q * a.o_pitch + 4 * c;
+#pragma unroll 4
+    for (int p = wave; p < a.parts; p += WAVES) {
+      const float4 v = *reinterpret_cast<const float4*>(O + (size_t)p * a.n * a.o_pitch);
+      const float k = fac[p];
+      sum.x = __builtin_fmaf(v.x, k, sum.x); sum.y = __builtin_fmaf(v.y, k, sum.y); sum.z = __builtin_fmaf(v.z, k, sum.z); sum.w = __builtin_fmaf(v.w, k, sum.w);
+    }
+    sums[wave][c] = sum;
+  }
+  __syncthreads();
   T* out = (T*)a.grad + q * a.grad_stride;
-  const float less = expm1f((float)over), us = u * a.scale;
-  for (int c = lane; c < a.dim; c += 64) {
+  const float less = expm1f((float)over), inv = 1.f / l;
+  for (int c = threadIdx.x; c < a.dim; c += 64 * WAVES) {
     float sum = 0.f;
-    for (int p = 0; p < a.parts; ++p) sum += a.O[((size_t)p * a.n + q) * a.o_pitch + c] * __builtin_amdgcn_exp2f(a.stats[(size_t)p * a.n + q].x - m);
-    const float v = us * __builtin_fmaf(less, (float)wr[c], sum / l);
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) sum += reinterpret_cast<const float*>(sums[w])[c];
+    const float v = us * __builtin_fmaf(less, (float)wr[c], sum * inv);
     out[c] = (T)(us != 0.f ? v : 0.f);
   }
+}
+template <int TYPE> static void launch_rows(const LossArgs& a, hipStream_t st) {
+  if (a.parts > 4) hipLaunchKernelGGL((k_loss_rows<TYPE, 4>), dim3((unsigned)a.n), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_loss_rows<TYPE, 1>), dim3((unsigned)a.n), dim3(64), 0, st, a);
 }
 
 // Adds the parts of pass 2: a thread per four columns.
@@ -80,13 +114,13 @@ template <int TYPE, int PASS>
 static void launch_nk(const SmArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)((a.units + 7) / 8 * 8)), block(256);
   switch (sm_nk(a.dim)) {
-    case 2: hipLaunchKernelGGL((k_softmax<TYPE, 2, PASS>), grid, block, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((k_softmax<TYPE, 4, PASS>), grid, block, 0, st, a); break;
-    case 7: hipLaunchKernelGGL((k_softmax<TYPE, 7, PASS>), grid, block, 0, st, a); break;
-    case 8: hipLaunchKernelGGL((k_softmax<TYPE, 8, PASS>), grid, block, 0, st, a); break;
-    case 12: hipLaunchKernelGGL((k_softmax<TYPE, 12, PASS>), grid, block, 0, st, a); break;
-    case 16: hipLaunchKernelGGL((k_softmax<TYPE, 16, PASS>), grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL((k_softmax<TYPE, 25, PASS>), grid, block, 0, st, a); break;
+    case 2: hipLaunchKernelGGL((k_softmax<TYPE, 2, PASS, true>), grid, block, 0, st, a); break;
+    case 4: hipLaunchKernelGGL((k_softmax<TYPE, 4, PASS, true>), grid, block, 0, st, a); break;
+    case 7: hipLaunchKernelGGL((k_softmax<TYPE, 7, PASS, true>), grid, block, 0, st, a); break;
+    case 8: hipLaunchKernelGGL((k_softmax<TYPE, 8, PASS, true>), grid, block, 0, st, a); break;
+    case 12: hipLaunchKernelGGL((k_softmax<TYPE, 12, PASS, true>), grid, block, 0, st, a); break;
+    case 16: hipLaunchKernelGGL((k_softmax<TYPE, 16, PASS, true>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((k_softmax<TYPE, 25, PASS, true>), grid, block, 0, st, a); break;
   }
 }
 template <int PASS> static hipError_t launch_pass(int dtype, const SmArgs& a, hipStream_t st) {
@@ -97,8 +131,8 @@ template <int PASS> static hipError_t launch_pass(int dtype, const SmArgs& a, hi
 }
 
 // ------------------------------------------------------------------------------------------ entry points -----
-// Workspace: statistics, the queries' sums, what pass 2 reads per query, the parts of the table's gradient.
-struct LossLayout { size_t stats, O1, row_m, row_f, row_u, O2, bytes; SmPlan p1, p2; int32_t o_pitch; };
+// Workspace: images of both matrices, statistics, the queries' sums, what pass 2 reads per query, the parts of the table's gradient.
+struct LossLayout { size_t qtiles, qexps, wtiles, wexps, stats, O1, row_m, row_f, row_u, own_top, O2, bytes; SmPlan p1, p2; int32_t o_pitch; };
 
 static LossLayout loss_layout(const mar_softmax* p) {
   LossLayout L;
@@ -108,9 +142,11 @@ static LossLayout loss_layout(const mar_softmax* p) {
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
   const size_t T = (size_t)p->num_queries;
+  L.qtiles = take(sm_image_bytes(p->dtype, p->dim, p->num_queries)); L.qexps = take(sm_exps_bytes(p->num_queries));
+  L.wtiles = take(sm_image_bytes(p->dtype, p->dim, p->num_rows)); L.wexps = take(sm_exps_bytes(p->num_rows));
   L.stats = take((size_t)L.p1.parts * T * sizeof(float4));
   L.O1 = take((size_t)L.p1.parts * T * L.o_pitch * 4);
-  L.row_m = take(T * 4); L.row_f = take(T * 4); L.row_u = take(T * 4);
+  L.row_m = take(T * 4); L.row_f = take(T * 4); L.row_u = take(T * 4); L.own_top = take((size_t)p->num_rows * 4);
   L.O2 = take(L.p2.parts > 1 ? (size_t)L.p2.parts * p->num_rows * L.o_pitch * 4 : 0);
   L.bytes = at > 256 ? at : 256;
   return L;
@@ -143,10 +179,22 @@ extern "C" int mar_softmax_loss(const mar_softmax* p, const void* queries, const
 
   SmArgs a = {};
   a.dim = p->dim; a.c = c; a.o_pitch = L.o_pitch; a.targets = targets;
-  hipError_t e = hipSuccess;
+  const SmImage qimg = {ws + L.qtiles, (const int*)(ws + L.qexps)}, wimg = {ws + L.wtiles, (const int*)(ws + L.wexps)};
+  SmPackArgs k = {};
+  k.dim = p->dim;
+  k.src = table; k.stride = p->row_stride; k.n = (int32_t)p->num_rows; k.tiles = ws + L.wtiles; k.exps = (int*)(ws + L.wexps);
+  k.own_top = (int32_t*)(ws + L.own_top);
+  hipError_t e = sm_pack(p->dtype, k, st);
+  k.own_top = nullptr;
+  if (e == hipSuccess && p->num_queries > 0) {
+    k.src = queries; k.stride = p->query_stride; k.n = p->num_queries; k.tiles = ws + L.qtiles; k.exps = (int*)(ws + L.qexps);
+    k.ids = targets; k.weights = weights; k.num_ids = p->num_rows;
+    e = sm_pack(p->dtype, k, st);
+  }
+  if (e != hipSuccess) { mar_set_error("image kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
   if (p->num_queries > 0) {
-    a.X = queries; a.x_stride = p->query_stride; a.n_x = p->num_queries;
-    a.Y = table; a.y_stride = p->row_stride; a.n_y = (int32_t)p->num_rows;
+    a.ximg = qimg; a.n_x = p->num_queries;
+    a.yimg = wimg; a.n_y = (int32_t)p->num_rows;
     a.nstripes = L.p1.stripes; a.parts = L.p1.parts; a.tps = L.p1.tps; a.units = a.nstripes * a.parts;
     a.stats = (float4*)(ws + L.stats); a.O = (float*)(ws + L.O1);
     e = launch_pass<1>(p->dtype, a, st);
@@ -156,20 +204,19 @@ extern "C" int mar_softmax_loss(const mar_softmax* p, const void* queries, const
     r.n = p->num_queries; r.dim = p->dim; r.parts = L.p1.parts; r.o_pitch = L.o_pitch; r.rows = p->num_rows;
     r.scale = p->scale; r.unscale = (double)p->scale / (double)c;
     r.targets = targets; r.weights = weights; r.stats = a.stats; r.O = a.O;
+    r.exps = qimg.exps; r.own_top = (int32_t*)(ws + L.own_top);
     if (grad_table) { r.row_m = (float*)(ws + L.row_m); r.row_f = (float*)(ws + L.row_f); r.row_u = (float*)(ws + L.row_u); }
     r.loss = loss; r.lse = lse; r.grad = grad_queries; r.grad_stride = grad_query_stride;
-    const dim3 grid((unsigned)((p->num_queries + 3) / 4)), block(256);
-    if (p->dtype == MAR_DTYPE_FP32) hipLaunchKernelGGL(k_loss_rows<0>, grid, block, 0, st, r);
-    else if (p->dtype == MAR_DTYPE_BF16) hipLaunchKernelGGL(k_loss_rows<1>, grid, block, 0, st, r);
-    else hipLaunchKernelGGL(k_loss_rows<2>, grid, block, 0, st, r);
+    if (p->dtype == MAR_DTYPE_FP32) launch_rows<0>(r, st); else if (p->dtype == MAR_DTYPE_BF16) launch_rows<1>(r, st); else launch_rows<2>(r, st);
     e = hipGetLastError();
     if (e != hipSuccess) { mar_set_error("loss kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
   }
   if (!grad_table) return MAR_OK;
-  a.X = table; a.x_stride = p->row_stride; a.n_x = (int32_t)p->num_rows;
-  a.Y = queries; a.y_stride = p->query_stride; a.n_y = p->num_queries;
+  a.ximg = wimg; a.n_x = (int32_t)p->num_rows;
+  a.yimg = qimg; a.n_y = p->num_queries;
   a.nstripes = L.p2.stripes; a.parts = L.p2.parts; a.tps = L.p2.tps; a.units = a.nstripes * a.parts;
   a.row_m = (const float*)(ws + L.row_m); a.row_f = (const float*)(ws + L.row_f); a.row_u = (const float*)(ws + L.row_u);
+  a.own_top = (const int32_t*)(ws + L.own_top);
   a.O = (float*)(ws + L.O2);
   if (L.p2.parts == 1) { a.out = grad_table; a.out_stride = grad_row_stride; }
   e = launch_pass<2>(p->dtype, a, st);
