@@ -35,8 +35,8 @@ struct SmArgs {
   int32_t parts, tps;              // parts of the streamed tiles, tiles each
   float c;                         // scale log2(e)
   float4* stats;                   // [parts][n_x]: reference (log2 units), sum of 2^(t - reference), sum of that times (t - reference)
-  float* gmax;                     // [n_x][ngroups]: largest t of a group of 16 group_tiles rows
-  int64_t ngroups;
+  float* gmax;                     // [n_x][2][half]: largest t of a group: one half's rows of group_tiles tiles
+  int64_t half;                    // groups a half, rounded up to a multiple of 4
   int32_t group_tiles;
   const uint32_t* allowed; int64_t allowed_stride;
   const int32_t* targets;
@@ -61,4 +61,4 @@ hipError_t sm_pack(int dtype, const SmPackArgs& a, hipStream_t st);
 struct SmPlan { int32_t qb, stripes, parts, tps, ntiles; };
 
 const char* sm_check(const mar_softmax* p, int* code);
-SmPlan sm_plan(int dtype, int dim, int pass, int64_t n_x, int64_t n_y, int multiple);
+SmPlan sm_plan(int dtype, int dim, int pass, int mode, int qb, int64_t n_x, int64_t n_y, int multiple);

@@ -9,12 +9,16 @@
 #ifndef MAR_SOFTMAX_IMAGES
 #define MAR_SOFTMAX_IMAGES 8
 #endif
+#ifndef MAR_ANSWER_WAVE
+#define MAR_ANSWER_WAVE 1000
+#define MAR_ANSWER_256 200
+#endif
 #define SM_MARGIN 4               // groups, and rows, kept beyond the number asked for: what fp32 cannot tell apart
 
 struct AnswerArgs {
   const void *Q, *W; int64_t q_stride, w_stride, rows;
   int32_t n, dim, parts, num_top, group_tiles;
-  int64_t ngroups;                 // 0: no group maxima
+  int64_t ngroups, half;           // groups a half, and as many places as a half's have in a query's row
   float scale; double unscale;
   const int32_t* targets;
   const uint32_t* allowed; int64_t allowed_stride;
@@ -29,68 +33,153 @@ __device__ __forceinline__ uint32_t order_key(float v) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// The `want` largest of keys[0 .. n) (all different, 0: none), in descending order in best[]; returns how many there are.
-// A threshold with at least `want` and at most `CAP` keys above it is found by bisection, those keys are ranked.
-template <int NT, int CAP>
-__device__ int select_top(const unsigned long long* keys, int n, int want, unsigned long long* cand, unsigned long long* best, int* cnt) {
-  const int tid = threadIdx.x;
-  auto count = [&](unsigned long long x, int turn) {
-    int c = 0;
-    for (int e = tid; e < n; e += NT) c += keys[e] >= x ? 1 : 0;
+#define SM_CAP 96                 // candidates that are ranked by comparing all with all
+
+// The best `want` entries seen so far, in order: by descending key, then ascending id.
+struct TopList {
+  __attribute__((aligned(16))) unsigned long long cand[SM_CAP + MAR_MAX_TOP + SM_MARGIN + 8], best[MAR_MAX_TOP + SM_MARGIN];   // key << 32 | ~id
+  uint32_t group[64], threshold;
+  int cnt[2][16], num, have;
+};
+
+// Adds the entries of a chunk to the list: R a thread (n in all, thread tid holds entries tid, NT + tid, ..), key[j] (0: none) with
+// id(j).  The threshold is the want-th largest of the maxima of 64 groups of threads, which at least `want` entries reach and
+// rarely more than SM_CAP.  Else one that between `want` and SM_CAP reach is found by bisection; where equal keys straddle it, a
+// second bisection over their ids takes the lowest.  All threads of the workgroup.
+template <int NT, int R, typename F>
+__device__ __forceinline__ void add_entries(TopList& top, const uint32_t (&key)[R], F id, int n, int want) {
+  constexpr int NW = NT / 64, PER = NT / 64;               // threads to a group
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  uint32_t mine = 0u;
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) c += __shfl_xor(c, o);
-    if ((tid & 63) == 0) cnt[(turn & 1) * (NT / 64) + (tid >> 6)] = c;
-    __syncthreads();
-    c = 0;
-    for (int w = 0; w < NT / 64; ++w) c += cnt[(turn & 1) * (NT / 64) + w];
-    return c;
-  };
-  __syncthreads();                                         // the keys are written
-  unsigned long long lo = 1, hi = ~0ull;
-  int turn = 0, c = count(lo, turn++);
-  unsigned long long x = lo;
-  if (c > CAP) {
-    while (hi - lo > 1) {                                  // at least `lo`: more than CAP keys, at least `hi`: fewer than `want`
-      x = lo + (hi - lo) / 2;
-      c = count(x, turn++);
-      if (c > CAP) lo = x; else if (c < want) hi = x; else break;
-    }
-  }
+  for (int j = 0; j < R; ++j) if (R == 1 || j * NT < n) mine = max(mine, key[j]);
+#pragma unroll
+  for (int o = 1; o < PER; o <<= 1) mine = max(mine, (uint32_t)__shfl_xor((int)mine, o));
   __syncthreads();
-  if (tid == 0) cnt[0] = 0;
+  if (tid % PER == 0) top.group[tid / PER] = mine;
+  if (tid == 0) top.num = 0;
   __syncthreads();
-  for (int e = tid; e < n; e += NT) {
-    if (keys[e] >= x) { const int at = atomicAdd(&cnt[0], 1); if (at < CAP) cand[at] = keys[e]; }
-  }
-  __syncthreads();
-  const int have = min(cnt[0], CAP);
-  for (int e = tid; e < have; e += NT) {
-    const unsigned long long k = cand[e];
+  // a full list's last entry bounds what can still enter
+  const int old = top.have;
+  const uint32_t floor_key = old == want ? max((uint32_t)(top.best[want - 1] >> 32), 1u) : 1u;
+  const uint32_t v = top.group[lane];
+  if (wave == 0) {
     int rank = 0;
-    for (int j = 0; j < have; ++j) rank += cand[j] > k ? 1 : 0;
-    if (rank < want) best[rank] = k;
+#pragma unroll
+    for (int j = 0; j < 64; ++j) {
+      const uint32_t w = (uint32_t)__builtin_amdgcn_readlane((int)v, j);
+      rank += w > v || (w == v && j < lane) ? 1 : 0;
+    }
+    if (rank == want - 1) top.threshold = v;
   }
   __syncthreads();
-  return min(have, want);
+  uint32_t x = max(top.threshold, floor_key);
+  uint32_t tie = 0u, id_end = ~0u;                         // of the entries with key `tie` those with an id below id_end
+  auto collect = [&]() {
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      if (R == 1 || j * NT < n) {
+        if (key[j] >= x || (tie && key[j] == tie && id(j) < id_end)) {
+          const int at = atomicAdd(&top.num, 1);
+          if (at < SM_CAP) top.cand[at] = (unsigned long long)key[j] << 32 | (uint32_t)~id(j);
+        }
+      }
+    }
+    __syncthreads();
+  };
+  collect();
+  if (top.num > SM_CAP) {                                  // uniform
+    int turn = 0;
+    auto total = [&](int c) {                              // c: of the wave
+      if (lane == 0) top.cnt[turn & 1][wave] = c;
+      __syncthreads();
+      c = 0;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) c += top.cnt[turn & 1][w];
+      ++turn;
+      return c;
+    };
+    auto count = [&](uint32_t y) {
+      int c = 0;
+#pragma unroll
+      for (int j = 0; j < R; ++j) if (R == 1 || j * NT < n) c += __popcll(__builtin_amdgcn_ballot_w64(key[j] >= y));
+      return total(c);
+    };
+    uint32_t lo = x, hi = ~0u;                             // more than SM_CAP reach lo, fewer than `want` hi
+    while (hi - lo > 1u) {
+      x = lo + (hi - lo) / 2;
+      const int c = count(x);
+      if (c > SM_CAP) lo = x; else if (c < want) hi = x; else break;
+    }
+    if (hi - lo <= 1u) {
+      x = hi; tie = lo;
+      const int above = count(x);
+      uint32_t a = 0u, b = ~0u;                            // ids below a: too few, below b: too many
+      while (true) {
+        id_end = a + (b - a) / 2;
+        int c = 0;
+#pragma unroll
+        for (int j = 0; j < R; ++j) if (R == 1 || j * NT < n) c += __popcll(__builtin_amdgcn_ballot_w64(key[j] == tie && id(j) < id_end));
+        c = above + total(c);
+        if (c < want) a = id_end; else if (c > SM_CAP) b = id_end; else break;
+      }
+    }
+    __syncthreads();
+    if (tid == 0) top.num = 0;
+    __syncthreads();
+    collect();
+  }
+  const int fresh = min(top.num, SM_CAP), all = fresh + old;
+  if (tid < old) top.cand[fresh + tid] = top.best[tid];
+  if (tid >= old && tid < old + 8) top.cand[fresh + tid] = 0ull;
+  __syncthreads();
+  if (tid < (all + 63) / 64 * 64) {                        // whole waves
+    const unsigned long long k = tid < all ? top.cand[tid] : ~0ull;
+    int rank = 0;
+    for (int j0 = 0; j0 < all; j0 += 8) {                  // eight reads in flight; entries from `all` on are 0
+      unsigned long long w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = top.cand[j0 + j];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) rank += w[j] > k ? 1 : 0;
+    }
+    if (tid < all && rank < want) top.best[rank] = k;
+  }
+  if (tid == 0) top.have = min(all, want);
+  __syncthreads();
 }
 
-// CHUNK: keys looked at together; best ones are carried from chunk to chunk.
-template <int TYPE, int NT, int CHUNK>
+// R: keys of group maxima a thread looks at together; rows are scored again NT / 8 at a time, RR rounds together.
+template <int TYPE, int NT, int R, int RR>
 __global__ void __launch_bounds__(NT)
 k_answer(AnswerArgs a) {
   typedef typename RowType<TYPE>::T T;
-  constexpr int CAP = 128, MAXW = MAR_MAX_TOP + SM_MARGIN;
-  __shared__ float s_m[NT / 64], s_l[NT / 64], s_a[NT / 64];
-  __shared__ float qs[512];
-  __shared__ unsigned long long keys[CHUNK + MAXW], cand[CAP], best[MAXW];
+  constexpr int MAXW = MAR_MAX_TOP + SM_MARGIN, NW = NT / 64;
+  __shared__ float s_m[NW], s_l[NW], s_a[NW];
+  __shared__ __attribute__((aligned(16))) float qs[(MAR_MAX_DIM + 7) / 8 * 8];
+  __shared__ TopList top;
   __shared__ double exact[MAXW];
-  __shared__ int cnt[2 * (NT / 64)], groups[MAXW];
+  __shared__ int groups[MAXW];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t q = blockIdx.x;
   const T* qr = (const T*)a.Q + q * a.q_stride;
   const T* W = (const T*)a.W;
   const uint32_t* allowed = a.allowed ? a.allowed + q * a.allowed_stride : nullptr;
   auto is_allowed = [&](int64_t row) { return !allowed || (allowed[row >> 5] >> (row & 31) & 1u); };
+  // group maxima of a chunk: element e of the query's row [2][half] belongs to group 2 (e % half) + e / half
+  const float* gm = a.gmax + q * 2 * a.half;
+  auto load_keys = [&](int64_t g0, uint32_t (&key)[R]) {
+    float v[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      const int64_t e = g0 + j * NT + tid;
+      v[j] = e < 2 * a.half && (e < a.half ? e : e - a.half) < a.ngroups ? gm[e] : -__builtin_inff();
+    }
+#pragma unroll
+    for (int j = 0; j < R; ++j) key[j] = order_key(v[j]);
+  };
+  uint32_t key[R];
+  if (a.num_top) load_keys(0, key);
 
   // ---- statistics of all parts
   auto join = [](float& m, float& l, float& s, float m2, float l2, float s2) {
@@ -100,13 +189,16 @@ k_answer(AnswerArgs a) {
   };
   float m = SM_NO_REF, l = 0.f, s = 0.f;
   for (int p = tid; p < a.parts; p += NT) { const float4 v = a.stats[(size_t)p * a.n + q]; join(m, l, s, v.x, v.y, v.z); }
+  if (a.parts > 1) {
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) join(m, l, s, __shfl_xor(m, o), __shfl_xor(l, o), __shfl_xor(s, o));
+    for (int o = 32; o >= 1; o >>= 1) join(m, l, s, __shfl_xor(m, o), __shfl_xor(l, o), __shfl_xor(s, o));
+  }
   if (lane == 0) { s_m[wave] = m; s_l[wave] = l; s_a[wave] = s; }
-  for (int c = tid; c < 512; c += NT) qs[c] = c < a.dim ? (float)qr[c] : 0.f;
+  for (int c = tid; c < (MAR_MAX_DIM + 7) / 8 * 8; c += NT) qs[c] = c < a.dim ? (float)qr[c] : 0.f;
+  if (tid == 0) top.have = 0;
   __syncthreads();
   m = s_m[0]; l = s_l[0]; s = s_a[0];
-  for (int w = 1; w < NT / 64; ++w) join(m, l, s, s_m[w], s_l[w], s_a[w]);
+  for (int w = 1; w < NW && w * 64 < a.parts; ++w) join(m, l, s, s_m[w], s_l[w], s_a[w]);
   const double lse = (double)m * a.unscale + (double)logf(l);
 
   // ---- the answer's log probability, the entropy
@@ -127,56 +219,86 @@ k_answer(AnswerArgs a) {
 
   // ---- groups with the largest maxima; among equal ones the first
   const int want = a.num_top + SM_MARGIN;
-  const float* gm = a.gmax + q * a.ngroups;
-  int have = 0;
-  for (int64_t g0 = 0; g0 < a.ngroups; g0 += CHUNK) {
-    const int n = (int)min((int64_t)CHUNK, a.ngroups - g0);
-    for (int e = tid; e < n; e += NT) {
-      const uint32_t k = order_key(gm[g0 + e]);
-      keys[e] = k ? (unsigned long long)k << 32 | (uint32_t)~(uint32_t)(g0 + e) : 0ull;
-    }
-    for (int e = tid; e < have; e += NT) keys[n + e] = best[e];
-    have = select_top<NT, CAP>(keys, n + have, want, cand, best, cnt);
+  for (int64_t g0 = 0;;) {
+    add_entries<NT, R>(top, key, [&](int j) {
+      const int64_t e = g0 + j * NT + tid;
+      return (uint32_t)(e < a.half ? 2 * e : 2 * (e - a.half) + 1);
+    }, (int)min((int64_t)NT * R, 2 * a.half - g0), want);
+    g0 += (int64_t)NT * R;
+    if (g0 >= 2 * a.half) break;
+    load_keys(g0, key);
   }
-  for (int e = tid; e < have; e += NT) groups[e] = (int)~(uint32_t)best[e];
+  const int ngr = top.have, per = 16 * a.group_tiles;
+  if (tid < ngr) groups[tid] = (int)~(uint32_t)top.best[tid];
   __syncthreads();
-  const int ngr = have, per = 16 * a.group_tiles;
-  // ---- their rows in fp32, eight lanes to a row
-  have = 0;
-  const int64_t nrows = (int64_t)ngr * per;
-  for (int64_t r0 = 0; r0 < nrows; r0 += CHUNK) {
-    const int n = (int)min((int64_t)CHUNK, nrows - r0);
-    for (int e = tid >> 3; e < (n + NT / 8 - 1) / (NT / 8) * (NT / 8); e += NT / 8) {
-      bool in = e < n;
-      int64_t row = 0;
-      if (in) {
-        const int64_t r = r0 + e;
-        const int j = (int)(r / per), w = (int)(r - (int64_t)j * per), grp = groups[j], k = w & 15;
-        row = ((int64_t)(grp >> 1) * a.group_tiles + (w >> 4)) * SM_TY + 8 * (k >> 2) + 4 * (grp & 1) + (k & 3);
-        in = row < a.rows && is_allowed(row);
-      }
-      float sum = 0.f;
-      if (in) {
-        const T* wr = W + row * a.w_stride;
-        for (int u = tid & 7; 8 * u < a.dim; u += 8) {
-          float v[8];
-          load8<TYPE>(wr, 8 * u, a.dim, v);
+  if (tid == 0) top.have = 0;
+  // ---- their rows in fp32, eight lanes to a row, the loads of one or two rows in flight; lane k % 8 of a row's keeps round k's score
+  constexpr int RZ = TYPE == MAR_DTYPE_FP32 ? 1 : 2;
+  constexpr int NU = (MAR_MAX_DIM + 63) / 64;              // eights of columns a lane takes
+  const int nrows = ngr * per, nu = (a.dim + 63) / 64;
+  for (int r0 = 0; r0 < nrows; r0 += RR * (NT / 8)) {
+    uint32_t rk[1] = {0u};
+    uint32_t rid = 0u;
+    for (int k = 0; k < RR && r0 + k * (NT / 8) < nrows; k += RZ) {            // uniform
+      row_u4 raw[RZ][NU][TYPE == MAR_DTYPE_FP32 ? 2 : 1];
+      bool in[RZ];
+      int64_t row[RZ];
 #pragma unroll
-          for (int c = 0; c < 8; ++c) sum = __builtin_fmaf(v[c], qs[8 * u + c], sum);
+      for (int z = 0; z < RZ; ++z) {
+        const int e = r0 + (k + z) * (NT / 8) + (tid >> 3);
+        in[z] = e < nrows;
+        row[z] = 0;
+        if (in[z]) {
+          const int j = e / per, w = e - j * per, grp = groups[j], i = w & 15;
+          row[z] = ((int64_t)(grp >> 1) * a.group_tiles + (w >> 4)) * SM_TY + 8 * (i >> 2) + 4 * (grp & 1) + (i & 3);
+          in[z] = row[z] < a.rows && is_allowed(row[z]);
+        }
+        if (!in[z]) continue;
+        const T* wr = W + row[z] * a.w_stride;
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+          const int c = 8 * (8 * u + (tid & 7));
+          if (u >= nu) continue;
+          if constexpr (TYPE == MAR_DTYPE_FP32) {
+            raw[z][u][0] = take4_floats(wr, c, a.dim);
+            raw[z][u][1] = take4_floats(wr, c + 4, a.dim);
+          } else {
+            raw[z][u][0] = take8_bits(wr, c, a.dim);
+          }
         }
       }
-      sum += __shfl_xor(sum, 1); sum += __shfl_xor(sum, 2); sum += __shfl_xor(sum, 4);
-      if ((tid & 7) == 0 && e < n) {
-        const uint32_t k = in ? order_key(sum) : 0u;
-        keys[e] = k ? (unsigned long long)k << 32 | (uint32_t)~(uint32_t)row : 0ull;
+#pragma unroll
+      for (int z = 0; z < RZ; ++z) {
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+          const int c = 8 * (8 * u + (tid & 7));
+          if (u >= nu || c >= a.dim || !in[z]) continue;
+          float v[8];
+          if constexpr (TYPE == MAR_DTYPE_FP32) {
+            const row_u4 lo = place4_floats(raw[z][u][0], c, a.dim), hi = place4_floats(raw[z][u][1], c + 4, a.dim);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { v[e] = __uint_as_float(lo[e]); v[4 + e] = __uint_as_float(hi[e]); }
+          } else {
+            const row_u4 w = place8_bits(raw[z][u][0], c, a.dim);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = bits_to_float<TYPE>((unsigned short)(w[e >> 1] >> (16 * (e & 1))));
+          }
+          const float4 qa = *reinterpret_cast<const float4*>(qs + c), qb = *reinterpret_cast<const float4*>(qs + c + 4);
+          const float qv[8] = {qa.x, qa.y, qa.z, qa.w, qb.x, qb.y, qb.z, qb.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(v[e], qv[e], sum);
+        }
+        sum += __shfl_xor(sum, 1); sum += __shfl_xor(sum, 2); sum += __shfl_xor(sum, 4);
+        if ((tid & 7) == k + z) { rk[0] = in[z] ? order_key(sum) : 0u; rid = (uint32_t)row[z]; }
       }
     }
-    for (int e = tid; e < have; e += NT) keys[n + e] = best[e];
-    have = select_top<NT, CAP>(keys, n + have, want, cand, best, cnt);
+    add_entries<NT, 1>(top, rk, [&](int) { return rid; }, NT, want);
   }
   // ---- the best of them in 64 bits
-  for (int e = wave; e < have; e += NT / 64) {
-    const T* wr = W + (int64_t)(uint32_t)~(uint32_t)best[e] * a.w_stride;
+  const int have = top.have;
+  for (int e = wave; e < have; e += NW) {
+    const T* wr = W + (int64_t)(uint32_t)~(uint32_t)top.best[e] * a.w_stride;
     double dot = 0.0;
     for (int c = lane; c < a.dim; c += 64) dot = __builtin_fma((double)qs[c], (double)(float)wr[c], dot);
 #pragma unroll
@@ -184,11 +306,11 @@ k_answer(AnswerArgs a) {
     if (lane == 0) exact[e] = dot;
   }
   __syncthreads();
-  for (int e = tid; e < have; e += NT) {
-    const double v = exact[e];
-    const uint32_t row = ~(uint32_t)best[e];
+  if (tid < have) {
+    const double v = exact[tid];
+    const uint32_t row = ~(uint32_t)top.best[tid];
     int rank = 0;
-    for (int j = 0; j < have; ++j) rank += exact[j] > v || (exact[j] == v && ~(uint32_t)best[j] < row) ? 1 : 0;
+    for (int j = 0; j < have; ++j) rank += exact[j] > v || (exact[j] == v && (uint32_t)~(uint32_t)top.best[j] < row) ? 1 : 0;
     if (rank < a.num_top) {
       a.top_ids[q * a.num_top + rank] = (int32_t)row;
       a.top_log_probs[q * a.num_top + rank] = (float)(v * (double)a.scale - lse);
@@ -215,13 +337,22 @@ const char* sm_check(const mar_softmax* p, int* code) {
 
 // Parts: where the stripes do not fill the device, several workgroups share one, each streaming a part of the tiles.  Estimated by
 // the rounds of workgroups and their tiles, a workgroup costing four tiles more for its rows and its first tile.
-SmPlan sm_plan(int dtype, int dim, int pass, int64_t n_x, int64_t n_y, int multiple) {
+SmPlan sm_plan(int dtype, int dim, int pass, int mode, int qb, int64_t n_x, int64_t n_y, int multiple) {
   SmPlan r;
   const int nk = sm_nk(dim);
-  r.qb = sm_qb(dtype, nk, pass);
-  r.stripes = (int32_t)((n_x + 128 * r.qb - 1) / (128 * r.qb));
+  r.qb = qb;
   r.ntiles = (int32_t)((n_y + SM_TY - 1) / SM_TY);
-  const int64_t slots = 256 * sm_waves(dtype, nk, pass);
+  if (mode == SM_FEW) {                                    // every wave that the device holds, at least a tile each
+    const int64_t tile = (int64_t)SM_TY * sp_pitch(nk) * (dtype == MAR_DTYPE_FP32 ? 2 : 1);
+    const int64_t a_cu = 4 * sm_few_waves(dtype, nk, qb), fit = 160 * 1024 / (tile + 1024), slots = 256 * (a_cu < fit ? a_cu : fit);
+    int64_t tps = (r.ntiles + slots - 1) / slots;
+    if (tps < 1) tps = 1;
+    tps = (tps + multiple - 1) / multiple * multiple;
+    r.stripes = 1; r.tps = (int32_t)tps; r.parts = (int32_t)((r.ntiles + tps - 1) / tps);
+    return r;
+  }
+  r.stripes = (int32_t)((n_x + 128 * qb - 1) / (128 * qb));
+  const int64_t slots = 256 * sm_waves_of(dtype, nk, pass, mode, qb);
   int64_t best = INT64_MAX;
   r.parts = 1; r.tps = r.ntiles;
   const int most = pass == 0 ? 1024 : MAR_SOFTMAX_MAX_PARTS;
@@ -244,20 +375,25 @@ static int group_tiles(const mar_softmax* p, int num_top) {
   return k;
 }
 
-struct ProbsLayout { size_t stats, gmax, qtiles, qexps, wtiles, wexps, bytes; SmPlan p0; int group_tiles; int64_t ngroups; bool images; };
+struct ProbsLayout { size_t stats, gmax, qtiles, qexps, wtiles, wexps, bytes; SmPlan p0; int group_tiles; int64_t ngroups, half; int mode; };
 static ProbsLayout probs_layout(const mar_softmax* p, int num_top) {
   ProbsLayout L;
   L.group_tiles = num_top ? group_tiles(p, num_top) : 1;
-  L.p0 = sm_plan(p->dtype, p->dim, 0, p->num_queries, p->num_rows, L.group_tiles);
-  L.ngroups = num_top ? 2 * (int64_t)((L.p0.ntiles + L.group_tiles - 1) / L.group_tiles) : 0;
+  const int nk = sm_nk(p->dim), few = p->dtype == MAR_DTYPE_FP32 ? 32 : 64;
+  int qb = sm_qb(p->dtype, nk, 0);
+  L.mode = p->num_queries <= few ? SM_FEW : ((p->num_queries + 128 * qb - 1) / (128 * qb) >= MAR_SOFTMAX_IMAGES ? SM_IMAGES : SM_ROWS);
+  if (L.mode == SM_FEW) qb = p->num_queries <= 32 ? 1 : 2;
+  // group maxima are stored four groups at a time, but for few queries
+  L.p0 = sm_plan(p->dtype, p->dim, 0, L.mode, qb, p->num_queries, p->num_rows, num_top ? (L.mode == SM_FEW ? 1 : 4) * L.group_tiles : 1);
+  L.ngroups = num_top ? (L.p0.ntiles + L.group_tiles - 1) / L.group_tiles : 0;
+  L.half = (L.ngroups + 3) / 4 * 4 + 8;                    // queries' rows not a power of two apart
   const size_t T = (size_t)p->num_queries;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
   L.stats = take((size_t)L.p0.parts * T * sizeof(float4));
-  L.gmax = take(T * (size_t)L.ngroups * 4);
-  L.images = L.p0.stripes >= MAR_SOFTMAX_IMAGES;
+  L.gmax = take(num_top ? T * 2 * (size_t)L.half * 4 : 0);
   L.qtiles = L.qexps = L.wtiles = L.wexps = at;
-  if (L.images) {
+  if (L.mode == SM_IMAGES) {
     L.qtiles = take(sm_image_bytes(p->dtype, p->dim, p->num_queries)); L.qexps = take(sm_exps_bytes(p->num_queries));
     L.wtiles = take(sm_image_bytes(p->dtype, p->dim, p->num_rows)); L.wexps = take(sm_exps_bytes(p->num_rows));
   }
@@ -265,16 +401,16 @@ static ProbsLayout probs_layout(const mar_softmax* p, int num_top) {
   return L;
 }
 
-template <int TYPE, bool IMG> static void launch_nk(const SmArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)((a.units + 7) / 8 * 8)), block(256);
+template <int TYPE, int MODE, int QB> static void launch_nk(const SmArgs& a, hipStream_t st) {   // QB 0: as the width has it
+  const dim3 grid((unsigned)((a.units + 7) / 8 * 8)), block(sm_threads(MODE));
   switch (sm_nk(a.dim)) {
-    case 2: hipLaunchKernelGGL((k_softmax<TYPE, 2, 0, IMG>), grid, block, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((k_softmax<TYPE, 4, 0, IMG>), grid, block, 0, st, a); break;
-    case 7: hipLaunchKernelGGL((k_softmax<TYPE, 7, 0, IMG>), grid, block, 0, st, a); break;
-    case 8: hipLaunchKernelGGL((k_softmax<TYPE, 8, 0, IMG>), grid, block, 0, st, a); break;
-    case 12: hipLaunchKernelGGL((k_softmax<TYPE, 12, 0, IMG>), grid, block, 0, st, a); break;
-    case 16: hipLaunchKernelGGL((k_softmax<TYPE, 16, 0, IMG>), grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL((k_softmax<TYPE, 25, 0, IMG>), grid, block, 0, st, a); break;
+    case 2: hipLaunchKernelGGL((k_softmax<TYPE, 2, 0, MODE, QB ? QB : sm_qb(TYPE, 2, 0)>), grid, block, 0, st, a); break;
+    case 4: hipLaunchKernelGGL((k_softmax<TYPE, 4, 0, MODE, QB ? QB : sm_qb(TYPE, 4, 0)>), grid, block, 0, st, a); break;
+    case 7: hipLaunchKernelGGL((k_softmax<TYPE, 7, 0, MODE, QB ? QB : sm_qb(TYPE, 7, 0)>), grid, block, 0, st, a); break;
+    case 8: hipLaunchKernelGGL((k_softmax<TYPE, 8, 0, MODE, QB ? QB : sm_qb(TYPE, 8, 0)>), grid, block, 0, st, a); break;
+    case 12: hipLaunchKernelGGL((k_softmax<TYPE, 12, 0, MODE, QB ? QB : sm_qb(TYPE, 12, 0)>), grid, block, 0, st, a); break;
+    case 16: hipLaunchKernelGGL((k_softmax<TYPE, 16, 0, MODE, QB ? QB : sm_qb(TYPE, 16, 0)>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((k_softmax<TYPE, 25, 0, MODE, QB ? QB : sm_qb(TYPE, 25, 0)>), grid, block, 0, st, a); break;
   }
 }
 template <int TYPE> static void launch_pack(const SmPackArgs& a, hipStream_t st) {
@@ -298,15 +434,23 @@ size_t sm_image_bytes(int dtype, int dim, int64_t rows) {
   return (size_t)((rows + SM_TY - 1) / SM_TY) * SM_TY * sp_pitch(nk) * (dtype == MAR_DTYPE_FP32 ? 2 : 1);
 }
 size_t sm_exps_bytes(int64_t rows) { return ((size_t)((rows + SM_TY - 1) / SM_TY) * 16 + 255) / 256 * 256; }
-template <bool IMG> static hipError_t launch_stats(int dtype, const SmArgs& a, hipStream_t st) {
-  if (dtype == MAR_DTYPE_FP32) launch_nk<0, IMG>(a, st); else if (dtype == MAR_DTYPE_BF16) launch_nk<1, IMG>(a, st); else launch_nk<2, IMG>(a, st);
+template <int MODE> static hipError_t launch_stats(int dtype, int qb, const SmArgs& a, hipStream_t st) {
+  if constexpr (MODE == SM_FEW) {
+    if (dtype == MAR_DTYPE_FP32) launch_nk<0, MODE, 1>(a, st);
+    else if (dtype == MAR_DTYPE_BF16) { if (qb == 1) launch_nk<1, MODE, 1>(a, st); else launch_nk<1, MODE, 2>(a, st); }
+    else { if (qb == 1) launch_nk<2, MODE, 1>(a, st); else launch_nk<2, MODE, 2>(a, st); }
+  } else {
+    if (dtype == MAR_DTYPE_FP32) launch_nk<0, MODE, 0>(a, st); else if (dtype == MAR_DTYPE_BF16) launch_nk<1, MODE, 0>(a, st); else launch_nk<2, MODE, 0>(a, st);
+  }
   return hipGetLastError();
 }
 
-// Few queries: a wide workgroup each; many: enough of them to fill the device at 256 threads.
+// Threads per query: all that hide a query's own latency where there are few, a wave each where the device is full of them.
 template <int TYPE> static void launch_answer(const AnswerArgs& a, hipStream_t st) {
-  if (a.n >= 512) hipLaunchKernelGGL((k_answer<TYPE, 256, 2048>), dim3((unsigned)a.n), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_answer<TYPE, 1024, 8192>), dim3((unsigned)a.n), dim3(1024), 0, st, a);
+  const dim3 grid((unsigned)a.n);
+  if (a.n >= MAR_ANSWER_WAVE) hipLaunchKernelGGL((k_answer<TYPE, 64, 32, 8>), grid, dim3(64), 0, st, a);
+  else if (a.n >= MAR_ANSWER_256) hipLaunchKernelGGL((k_answer<TYPE, 256, 16, 8>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_answer<TYPE, 1024, 16, 8>), grid, dim3(1024), 0, st, a);
 }
 
 static bool top_ok(int32_t num_top) {
@@ -351,10 +495,10 @@ extern "C" int mar_log_probs(const mar_softmax* p, const void* queries, const vo
   a.nstripes = L.p0.stripes; a.parts = L.p0.parts; a.tps = L.p0.tps; a.units = a.nstripes * a.parts;
   a.stats = (float4*)((char*)workspace + L.stats);
   a.gmax = num_top ? (float*)((char*)workspace + L.gmax) : nullptr;
-  a.ngroups = L.ngroups; a.group_tiles = L.group_tiles;
+  a.half = L.half; a.group_tiles = L.group_tiles;
   a.allowed = allowed; a.allowed_stride = allowed_stride;
   hipError_t e;
-  if (L.images) {
+  if (L.mode == SM_IMAGES) {
     SmPackArgs k = {};
     k.dim = p->dim;
     k.src = table; k.stride = p->row_stride; k.n = (int32_t)p->num_rows; k.tiles = (char*)workspace + L.wtiles; k.exps = (int*)((char*)workspace + L.wexps);
@@ -364,14 +508,14 @@ extern "C" int mar_log_probs(const mar_softmax* p, const void* queries, const vo
     if (e != hipSuccess) { mar_set_error("image kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
     a.ximg = {(char*)workspace + L.qtiles, (const int*)((char*)workspace + L.qexps)};
     a.yimg = {(char*)workspace + L.wtiles, (const int*)((char*)workspace + L.wexps)};
-    e = launch_stats<true>(p->dtype, a, st);
+    e = launch_stats<SM_IMAGES>(p->dtype, L.p0.qb, a, st);
   } else {
-    e = launch_stats<false>(p->dtype, a, st);
+    e = L.mode == SM_FEW ? launch_stats<SM_FEW>(p->dtype, L.p0.qb, a, st) : launch_stats<SM_ROWS>(p->dtype, L.p0.qb, a, st);
   }
   if (e != hipSuccess) { mar_set_error("softmax kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
   AnswerArgs r = {};
   r.Q = queries; r.W = table; r.q_stride = p->query_stride; r.w_stride = p->row_stride; r.rows = p->num_rows;
-  r.n = p->num_queries; r.dim = p->dim; r.parts = L.p0.parts; r.num_top = num_top; r.group_tiles = L.group_tiles; r.ngroups = L.ngroups;
+  r.n = p->num_queries; r.dim = p->dim; r.parts = L.p0.parts; r.num_top = num_top; r.group_tiles = L.group_tiles; r.ngroups = L.ngroups; r.half = L.half;
   r.scale = p->scale; r.unscale = (double)p->scale / (double)a.c;
   r.targets = targets; r.allowed = allowed; r.allowed_stride = allowed_stride; r.stats = a.stats; r.gmax = a.gmax;
   r.log_probs = log_probs; r.entropy = entropy; r.top_ids = top_ids; r.top_log_probs = top_log_probs;

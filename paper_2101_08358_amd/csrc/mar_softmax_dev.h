@@ -154,21 +154,34 @@ __device__ __forceinline__ float own_float(int k) { return __int_as_float(k < 0 
 #define SM_BELOW 12.f
 #define SM_CHAIN 16               // tiles whose weights are summed before their sum is added to the part's: chains of fp32 sums stay short
 
-// IMG: both matrices as images; else from their rows (a table that few queries meet is not worth laying out).
-template <int TYPE, int NK, int PASS, bool IMG>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sm_waves(TYPE, NK, PASS), sm_waves(TYPE, NK, PASS))))
+// How the streamed rows come: SM_IMAGES: both matrices as images.  SM_ROWS: from the rows themselves, a tile staged by the
+// workgroup (a table that few stripes of queries meet is not worth laying out).  SM_FEW: the queries fit one wave's registers;
+// every wave is a workgroup of its own and streams tiles of its own, without a barrier, at the rate of the memory.
+#define SM_ROWS 0
+#define SM_IMAGES 1
+#define SM_FEW 2
+constexpr int sm_threads(int mode) { return mode == SM_FEW ? 64 : 256; }
+// Waves per SIMD by mode: staging takes registers of its own.
+constexpr int sm_few_waves(int type, int nk, int qb) { return type == MAR_DTYPE_FP32 ? (nk <= 4 ? 2 : 1) : (nk <= 4 || (nk <= 8 && qb == 1) ? 3 : (nk <= 8 || (nk <= 12 && qb == 1) ? 2 : 1)); }
+constexpr int sm_rows_waves(int type, int nk) { return nk <= 4 ? 3 : (nk <= 12 ? 2 : (type != MAR_DTYPE_FP32 && nk > 16 ? 2 : 1)); }
+constexpr int sm_waves_of(int type, int nk, int pass, int mode, int qb) {
+  return mode == SM_FEW ? sm_few_waves(type, nk, qb) : (mode == SM_ROWS ? sm_rows_waves(type, nk) : sm_waves(type, nk, pass));
+}
+template <int TYPE, int NK, int PASS, int MODE, int QB>
+__global__ void __launch_bounds__(sm_threads(MODE)) __attribute__((amdgpu_waves_per_eu(sm_waves_of(TYPE, NK, PASS, MODE, QB), sm_waves_of(TYPE, NK, PASS, MODE, QB))))
 k_softmax(SmArgs a) {
   typedef SmGeom<TYPE, NK> G;
   typedef typename RowType<TYPE>::T T;
   constexpr bool PAIRS = TYPE == MAR_DTYPE_FP32;
-  constexpr int QB = sm_qb(TYPE, NK, PASS);
+  constexpr bool IMG = MODE == SM_IMAGES, FEW = MODE == SM_FEW;
   constexpr bool SECOND = PASS != 0;
   constexpr int NO = SECOND ? (NK + 1) / 2 : 1;            // 32-column blocks of the output
   constexpr bool REFS = PASS != 2 || TYPE != MAR_DTYPE_BF16 || NK > 16;   // weights relative to a reference (bf16 does without; the widest rows' registers do not)
   constexpr int PL = G::PLANES;
   static_assert(IMG || PASS == 0, "passes with a second product take images");
   static_assert(QB == 1 || PASS == 0, "passes with a second product take one block a wave");
-  __shared__ __attribute__((aligned(1024))) char smem[2 * G::TILE];
+  constexpr int NB = FEW ? 1 : 2;                          // tiles in LDS
+  __shared__ __attribute__((aligned(1024))) char smem[NB * G::TILE];
   __shared__ int exps[2][4];
   // pass 2, per query of a tile: f = log2(|u| / sum of its weights), m its reference (16-bit types: f - m and nothing)
   __shared__ __attribute__((aligned(16))) float rows_m[2][SM_TY], rows_f[2][SM_TY], rows_u[2][SM_TY];
@@ -183,12 +196,13 @@ k_softmax(SmArgs a) {
   const int part = unit / a.nstripes, stripe = unit - part * a.nstripes;
   const int ntiles_all = (int)(((int64_t)a.n_y + SM_TY - 1) / SM_TY);
   const int t_begin = part * a.tps, t_end = min(ntiles_all, t_begin + a.tps);
-  const int64_t x_first = (int64_t)stripe * (128 * QB) + wave * (32 * QB);
+  const int64_t x_first = FEW ? 0 : (int64_t)stripe * (128 * QB) + wave * (32 * QB);
   const int dim = a.dim;
 
   // zeros: units beyond the columns that a tile's copies write
-  if (!IMG) for (int k = tid * 16; k < 2 * G::TILE; k += 256 * 16) *reinterpret_cast<row_u4*>(smem + k) = (row_u4)(0u);
-  SmStage<TYPE, NK> stage;
+  if (!IMG) for (int k = tid * 16; k < NB * G::TILE; k += sm_threads(MODE) * 16) *reinterpret_cast<row_u4*>(smem + k) = (row_u4)(0u);
+  constexpr int NSG = FEW ? 4 : 1;                         // blocks of eight rows a wave stages
+  SmStage<TYPE, NK> stage[NSG];
   const T* Y = (const T*)a.Y;
   // images: copied by loads that write LDS, 1 KB a wave instruction; nothing but the end of the tile waits for them
   int token = 0;
@@ -225,9 +239,9 @@ k_softmax(SmArgs a) {
       for (int p = 0; p < NCW; ++p) copy(t_begin, 0, p);
       ask_exps(t_begin);
     } else {
-      stage.begin(Y, a.y_stride, a.n_y, t_begin * SM_TY, tid);
 #pragma unroll
-      for (int p = 0; p < G::NP; ++p) stage.load(p, dim, tid);
+      for (int w = 0; w < NSG; ++w) stage[w].begin(Y, a.y_stride, a.n_y, t_begin * SM_TY, 64 * w + tid);
+      unrolled<NSG * G::NP>([&](auto k) { constexpr int w = k / G::NP, p = k % G::NP; stage[w].load(p, dim, 64 * w + tid); });
     }
     load_rows(t_begin * SM_TY);
   }
@@ -298,6 +312,10 @@ k_softmax(SmArgs a) {
     word_next[b] = PASS == 0 && a.allowed && t_begin < t_end ? words[b][t_begin] : ~0u;
   }
   int group_left = a.group_tiles;
+  int64_t group = PASS == 0 ? t_begin / max(a.group_tiles, 1) : 0;             // finished groups
+  v4f gm4[QB];
+#pragma unroll
+  for (int b = 0; b < QB; ++b) gm4[b] = (v4f)(-__builtin_inff());
   float neg1 = -1.f;
   asm volatile("" : "+v"(neg1));
 
@@ -326,7 +344,7 @@ k_softmax(SmArgs a) {
       store_rows(buf);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     } else {
-      stage.store(smem + buf * G::TILE, exps[buf], dim, tid);
+      unrolled<NSG>([&](auto k) { constexpr int w = k; stage[w].store(smem + buf * G::TILE, exps[buf], dim, 64 * w + tid); });
     }
   };
   if (!IMG) __syncthreads();                               // the zeros are there
@@ -334,7 +352,7 @@ k_softmax(SmArgs a) {
   __syncthreads();
 
   for (int t = t_begin; t < t_end; ++t) {
-    const int buf = (t - t_begin) & 1, bofs = buf * G::TILE;
+    const int buf = FEW ? 0 : (t - t_begin) & 1, bofs = buf * G::TILE;
     const int y0 = t * SM_TY;
     const bool has_next = t + 1 < t_end;                   // uniform
     unsigned word[QB];
@@ -344,7 +362,13 @@ k_softmax(SmArgs a) {
       if (PASS == 0 && has_next && a.allowed) word_next[b] = words[b][t + 1];
     }
     if (has_next) {
-      if constexpr (IMG) ask_exps(t + 1); else stage.begin(Y, a.y_stride, a.n_y, y0 + SM_TY, tid);
+      if constexpr (IMG) ask_exps(t + 1);
+      else {
+#pragma unroll
+        for (int w = 0; w < NSG; ++w) stage[w].begin(Y, a.y_stride, a.n_y, y0 + SM_TY, 64 * w + tid);
+        // a wave of its own: all that it will want next at once
+        if constexpr (FEW) unrolled<NSG * G::NP>([&](auto k) { constexpr int w = k / G::NP, p = k % G::NP; stage[w].load(p, dim, 64 * w + tid); });
+      }
       load_rows(y0 + SM_TY);
     }
 
@@ -375,9 +399,9 @@ k_softmax(SmArgs a) {
           if constexpr (IMG) {
 #pragma unroll
             for (int p = s * NCW / NK; p < (s + 1) * NCW / NK; ++p) copy(t + 1, buf ^ 1, p);
-          } else {
+          } else if constexpr (!FEW) {
 #pragma unroll
-            for (int p = s * G::NP / NK; p < (s + 1) * G::NP / NK; ++p) stage.load(p, dim, tid);
+            for (int p = s * G::NP / NK; p < (s + 1) * G::NP / NK; ++p) stage[0].load(p, dim, tid);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -477,8 +501,24 @@ k_softmax(SmArgs a) {
         if (PASS == 0 && a.gmax) {
           gmax[b] = fmaxf(gmax[b], top);
           if (group_left == 1 || !has_next) {              // uniform
-            if (xv[b]) a.gmax[x * a.ngroups + 2 * (int64_t)(t / a.group_tiles) + h] = gmax[b];
+            if constexpr (FEW) {                           // parts begin where it suits the table
+              if (xv[b]) a.gmax[(x * 2 + h) * a.half + t / a.group_tiles] = gmax[b];
+              gmax[b] = -__builtin_inff();
+            } else {
+            // four groups of a lane at a time: stores of 4 bytes a row apart cost as much as the products
+            gm4[b] = (v4f){gm4[b][1], gm4[b][2], gm4[b][3], gmax[b]};
             gmax[b] = -__builtin_inff();
+            if (b == QB - 1) ++group;
+            if (xv[b]) {
+              float* const to = a.gmax + (x * 2 + h) * a.half;
+              const int64_t n = b == QB - 1 ? group : group + 1;
+              if ((n & 3) == 0) *reinterpret_cast<v4f*>(to + n - 4) = gm4[b];
+              else if (!has_next) {                        // a part's last groups
+#pragma unroll
+                for (int j = 1; j < 4; ++j) if (j >= 4 - (int)(n & 3)) to[n - 4 + j] = gm4[b][j];
+              }
+            }
+            }
           }
         }
         if constexpr (PASS == 1) {
@@ -571,8 +611,9 @@ k_softmax(SmArgs a) {
         __builtin_amdgcn_sched_barrier(0);
       });
     }
-    if (has_next) land(buf ^ 1);
-    __syncthreads();
+    if (FEW) asm volatile("" ::: "memory");                // LDS operations of a wave complete in order
+    if (has_next) land(FEW ? 0 : buf ^ 1);
+    if (FEW) asm volatile("" ::: "memory"); else __syncthreads();
   }
 
   // ---- what the part leaves

@@ -114,13 +114,13 @@ template <int TYPE, int PASS>
 static void launch_nk(const SmArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)((a.units + 7) / 8 * 8)), block(256);
   switch (sm_nk(a.dim)) {
-    case 2: hipLaunchKernelGGL((k_softmax<TYPE, 2, PASS, true>), grid, block, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((k_softmax<TYPE, 4, PASS, true>), grid, block, 0, st, a); break;
-    case 7: hipLaunchKernelGGL((k_softmax<TYPE, 7, PASS, true>), grid, block, 0, st, a); break;
-    case 8: hipLaunchKernelGGL((k_softmax<TYPE, 8, PASS, true>), grid, block, 0, st, a); break;
-    case 12: hipLaunchKernelGGL((k_softmax<TYPE, 12, PASS, true>), grid, block, 0, st, a); break;
-    case 16: hipLaunchKernelGGL((k_softmax<TYPE, 16, PASS, true>), grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL((k_softmax<TYPE, 25, PASS, true>), grid, block, 0, st, a); break;
+    case 2: hipLaunchKernelGGL((k_softmax<TYPE, 2, PASS, SM_IMAGES, 1>), grid, block, 0, st, a); break;
+    case 4: hipLaunchKernelGGL((k_softmax<TYPE, 4, PASS, SM_IMAGES, 1>), grid, block, 0, st, a); break;
+    case 7: hipLaunchKernelGGL((k_softmax<TYPE, 7, PASS, SM_IMAGES, 1>), grid, block, 0, st, a); break;
+    case 8: hipLaunchKernelGGL((k_softmax<TYPE, 8, PASS, SM_IMAGES, 1>), grid, block, 0, st, a); break;
+    case 12: hipLaunchKernelGGL((k_softmax<TYPE, 12, PASS, SM_IMAGES, 1>), grid, block, 0, st, a); break;
+    case 16: hipLaunchKernelGGL((k_softmax<TYPE, 16, PASS, SM_IMAGES, 1>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((k_softmax<TYPE, 25, PASS, SM_IMAGES, 1>), grid, block, 0, st, a); break;
   }
 }
 template <int PASS> static hipError_t launch_pass(int dtype, const SmArgs& a, hipStream_t st) {
@@ -136,8 +136,8 @@ struct LossLayout { size_t qtiles, qexps, wtiles, wexps, stats, O1, row_m, row_f
 
 static LossLayout loss_layout(const mar_softmax* p) {
   LossLayout L;
-  L.p1 = sm_plan(p->dtype, p->dim, 1, p->num_queries, p->num_rows, 1);
-  L.p2 = sm_plan(p->dtype, p->dim, 2, p->num_rows, p->num_queries, 1);
+  L.p1 = sm_plan(p->dtype, p->dim, 1, SM_IMAGES, 1, p->num_queries, p->num_rows, 1);
+  L.p2 = sm_plan(p->dtype, p->dim, 2, SM_IMAGES, 1, p->num_rows, p->num_queries, 1);
   L.o_pitch = (p->dim + 3) / 4 * 4;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
