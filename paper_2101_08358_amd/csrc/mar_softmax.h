@@ -35,7 +35,7 @@ struct SmArgs {
   int32_t parts, tps;              // parts of the streamed tiles, tiles each
   float c;                         // scale log2(e)
   float4* stats;                   // [parts][n_x]: reference (log2 units), sum of 2^(t - reference), sum of that times (t - reference)
-  float* gmax;                     // [n_x][2][half]: largest t of a group: one half's rows of group_tiles tiles
+  float *first, *second;           // [n_x][2][half]: largest and second largest score of a group: one half's rows of group_tiles tiles
   int64_t half;                    // groups a half, rounded up to a multiple of 4
   int32_t group_tiles;
   const uint32_t* allowed; int64_t allowed_stride;

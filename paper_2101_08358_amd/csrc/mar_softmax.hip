@@ -1,8 +1,10 @@
 // Log probabilities over all rows of a table: of given answers, with the distribution's entropy and its most probable rows (gfx950).
 //
-// Pass 0 (mar_softmax_dev.h) leaves statistics per query and part of the table, and the largest score of every group of 16
-// group_tiles rows.  k_answer joins the parts, a workgroup per query; the most probable rows lie in the groups with the largest
-// maxima, whose rows are scored again: in fp32, and the best of them in 64 bits, by which they are ordered.
+// Pass 0 (mar_softmax_dev.h) leaves statistics per query and part of the table, and of every group of 16 group_tiles rows the largest
+// score, with the register it came from, and the second largest.  k_answer joins the parts, a workgroup per query.  The most
+// probable rows lie in the groups with the largest maxima.  The rows behind the maxima are scored in 64 bits; only where a
+// group's second largest score reaches the k-th best of those are its other rows looked at too.  (All rows of the best groups
+// scored again, 16 each: 4,096 queries, 131,072 rows of 400 columns, 16 best rows 367 us, for 1 GB of rows read at random.)
 #include "mar_softmax_dev.h"
 
 // Stripes of queries from which the table is laid out as images first.
@@ -13,7 +15,7 @@
 #define MAR_ANSWER_WAVE 1000
 #define MAR_ANSWER_256 200
 #endif
-#define SM_MARGIN 4               // groups, and rows, kept beyond the number asked for: what fp32 cannot tell apart
+#define SM_MARGIN 12              // groups, and rows, kept beyond the number asked for: what fp32 less four bits cannot tell apart
 
 struct AnswerArgs {
   const void *Q, *W; int64_t q_stride, w_stride, rows;
@@ -22,7 +24,8 @@ struct AnswerArgs {
   float scale; double unscale;
   const int32_t* targets;
   const uint32_t* allowed; int64_t allowed_stride;
-  const float4* stats; const float* gmax;
+  const float4* stats; const float *first, *second; int32_t pairs;
+  float c;                         // scale log2(e)
   float *log_probs, *entropy, *top_log_probs; int32_t* top_ids;
 };
 
@@ -149,17 +152,20 @@ __device__ __forceinline__ void add_entries(TopList& top, const uint32_t (&key)[
   __syncthreads();
 }
 
-// R: keys of group maxima a thread looks at together; rows are scored again NT / 8 at a time, RR rounds together.
-template <int TYPE, int NT, int R, int RR>
+// R: keys of group maxima a thread looks at together.
+template <int TYPE, int NT, int R>
 __global__ void __launch_bounds__(NT)
 k_answer(AnswerArgs a) {
   typedef typename RowType<TYPE>::T T;
-  constexpr int MAXW = MAR_MAX_TOP + SM_MARGIN, NW = NT / 64;
+  constexpr int MAXW = MAR_MAX_TOP + SM_MARGIN, NW = NT / 64, BATCH = NT / 8 < 64 ? 64 : NT / 8, EPT = (BATCH + MAXW + NT - 1) / NT;
+  constexpr int QN = (MAR_MAX_DIM + 7) / 8 * 8;
   __shared__ float s_m[NW], s_l[NW], s_a[NW];
-  __shared__ __attribute__((aligned(16))) float qs[(MAR_MAX_DIM + 7) / 8 * 8];
+  __shared__ __attribute__((aligned(16))) float qs[QN];
   __shared__ TopList top;
-  __shared__ double exact[MAXW];
-  __shared__ int groups[MAXW];
+  __shared__ double exact[BATCH + MAXW];
+  __shared__ unsigned long long reach;
+  __shared__ uint32_t exact_row[BATCH + MAXW];
+  __shared__ int groups[MAXW], again[MAXW], num_exact;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t q = blockIdx.x;
   const T* qr = (const T*)a.Q + q * a.q_stride;
@@ -167,7 +173,7 @@ k_answer(AnswerArgs a) {
   const uint32_t* allowed = a.allowed ? a.allowed + q * a.allowed_stride : nullptr;
   auto is_allowed = [&](int64_t row) { return !allowed || (allowed[row >> 5] >> (row & 31) & 1u); };
   // group maxima of a chunk: element e of the query's row [2][half] belongs to group 2 (e % half) + e / half
-  const float* gm = a.gmax + q * 2 * a.half;
+  const float* gm = a.first + q * 2 * a.half;
   auto load_keys = [&](int64_t g0, uint32_t (&key)[R]) {
     float v[R];
 #pragma unroll
@@ -176,7 +182,7 @@ k_answer(AnswerArgs a) {
       v[j] = e < 2 * a.half && (e < a.half ? e : e - a.half) < a.ngroups ? gm[e] : -__builtin_inff();
     }
 #pragma unroll
-    for (int j = 0; j < R; ++j) key[j] = order_key(v[j]);
+    for (int j = 0; j < R; ++j) key[j] = v[j] > 0.99f * SM_NO_REF ? order_key(v[j]) & ~15u : 0u;
   };
   uint32_t key[R];
   if (a.num_top) load_keys(0, key);
@@ -194,7 +200,7 @@ k_answer(AnswerArgs a) {
     for (int o = 32; o >= 1; o >>= 1) join(m, l, s, __shfl_xor(m, o), __shfl_xor(l, o), __shfl_xor(s, o));
   }
   if (lane == 0) { s_m[wave] = m; s_l[wave] = l; s_a[wave] = s; }
-  for (int c = tid; c < (MAR_MAX_DIM + 7) / 8 * 8; c += NT) qs[c] = c < a.dim ? (float)qr[c] : 0.f;
+  for (int c = tid; c < QN; c += NT) qs[c] = c < a.dim ? (float)qr[c] : 0.f;
   if (tid == 0) top.have = 0;
   __syncthreads();
   m = s_m[0]; l = s_l[0]; s = s_a[0];
@@ -228,95 +234,99 @@ k_answer(AnswerArgs a) {
     if (g0 >= 2 * a.half) break;
     load_keys(g0, key);
   }
-  const int ngr = top.have, per = 16 * a.group_tiles;
+  // ---- the rows behind their maxima in 64 bits (with more than one tile to a group, that register's row of every tile)
+  const int ngr = top.have, G = a.group_tiles;
   if (tid < ngr) groups[tid] = (int)~(uint32_t)top.best[tid];
+  if (tid == 0) { num_exact = 0; reach = 0ull; }
   __syncthreads();
-  if (tid == 0) top.have = 0;
-  // ---- their rows in fp32, eight lanes to a row, the loads of one or two rows in flight; lane k % 8 of a row's keeps round k's score
-  constexpr int RZ = TYPE == MAR_DTYPE_FP32 ? 1 : 2;
-  constexpr int NU = (MAR_MAX_DIM + 63) / 64;              // eights of columns a lane takes
-  const int nrows = ngr * per, nu = (a.dim + 63) / 64;
-  for (int r0 = 0; r0 < nrows; r0 += RR * (NT / 8)) {
-    uint32_t rk[1] = {0u};
-    uint32_t rid = 0u;
-    for (int k = 0; k < RR && r0 + k * (NT / 8) < nrows; k += RZ) {            // uniform
-      row_u4 raw[RZ][NU][TYPE == MAR_DTYPE_FP32 ? 2 : 1];
-      bool in[RZ];
-      int64_t row[RZ];
+  auto element = [&](int grp) { return (int64_t)(grp & 1) * a.half + (grp >> 1); };
+  auto row_of = [&](int grp, int tile, int r) { return ((int64_t)(grp >> 1) * G + tile) * SM_TY + 8 * (r >> 2) + 4 * (grp & 1) + (r & 3); };
+  constexpr int NU = (MAR_MAX_DIM + 63) / 64;              // eights of columns that each of a row's eight lanes takes
+  double wmax = 0.0;                                       // largest squared norm of a row (fp32 squares may leave the floats' range)
+  // Scores items [0, n): row(item) or -1, eight lanes an item.  The list is cut back to its best `want` after every BATCH items.
+  auto score_items = [&](int n, auto row) {
+    for (int b0 = 0; b0 < n; b0 += BATCH) {
+      for (int e0 = b0; e0 < min(n, b0 + BATCH); e0 += NT / 8) {
+        const int e = e0 + (tid >> 3);
+        int64_t rw = e < n ? row(e) : -1;
+        if (rw >= a.rows || (rw >= 0 && !is_allowed(rw))) rw = -1;
+        double dot = 0.0, n2 = 0.0;
+        if (rw >= 0) {
+          const T* wr = W + rw * a.w_stride;
+          for (int u0 = 0; 64 * u0 < a.dim; u0 += 4) {     // uniform; four loads in flight
+            float v[4][8];
 #pragma unroll
-      for (int z = 0; z < RZ; ++z) {
-        const int e = r0 + (k + z) * (NT / 8) + (tid >> 3);
-        in[z] = e < nrows;
-        row[z] = 0;
-        if (in[z]) {
-          const int j = e / per, w = e - j * per, grp = groups[j], i = w & 15;
-          row[z] = ((int64_t)(grp >> 1) * a.group_tiles + (w >> 4)) * SM_TY + 8 * (i >> 2) + 4 * (grp & 1) + (i & 3);
-          in[z] = row[z] < a.rows && is_allowed(row[z]);
-        }
-        if (!in[z]) continue;
-        const T* wr = W + row[z] * a.w_stride;
+            for (int u = 0; u < 4; ++u) load8<TYPE>(wr, 8 * (8 * (u0 + u) + (tid & 7)), a.dim, v[u]);
 #pragma unroll
-        for (int u = 0; u < NU; ++u) {
-          const int c = 8 * (8 * u + (tid & 7));
-          if (u >= nu) continue;
-          if constexpr (TYPE == MAR_DTYPE_FP32) {
-            raw[z][u][0] = take4_floats(wr, c, a.dim);
-            raw[z][u][1] = take4_floats(wr, c + 4, a.dim);
-          } else {
-            raw[z][u][0] = take8_bits(wr, c, a.dim);
+            for (int u = 0; u < 4; ++u) {
+              const int c = min(8 * (8 * (u0 + u) + (tid & 7)), QN - 8);     // values from dim on are zeros
+              const float4 qa = *reinterpret_cast<const float4*>(qs + c), qb = *reinterpret_cast<const float4*>(qs + c + 4);
+              const float qv[8] = {qa.x, qa.y, qa.z, qa.w, qb.x, qb.y, qb.z, qb.w};
+#pragma unroll
+              for (int j = 0; j < 8; ++j) { dot = __builtin_fma((double)qv[j], (double)v[u][j], dot); n2 = __builtin_fma((double)v[u][j], (double)v[u][j], n2); }
+            }
           }
         }
-      }
 #pragma unroll
-      for (int z = 0; z < RZ; ++z) {
-        float sum = 0.f;
-#pragma unroll
-        for (int u = 0; u < NU; ++u) {
-          const int c = 8 * (8 * u + (tid & 7));
-          if (u >= nu || c >= a.dim || !in[z]) continue;
-          float v[8];
-          if constexpr (TYPE == MAR_DTYPE_FP32) {
-            const row_u4 lo = place4_floats(raw[z][u][0], c, a.dim), hi = place4_floats(raw[z][u][1], c + 4, a.dim);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { v[e] = __uint_as_float(lo[e]); v[4 + e] = __uint_as_float(hi[e]); }
-          } else {
-            const row_u4 w = place8_bits(raw[z][u][0], c, a.dim);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = bits_to_float<TYPE>((unsigned short)(w[e >> 1] >> (16 * (e & 1))));
-          }
-          const float4 qa = *reinterpret_cast<const float4*>(qs + c), qb = *reinterpret_cast<const float4*>(qs + c + 4);
-          const float qv[8] = {qa.x, qa.y, qa.z, qa.w, qb.x, qb.y, qb.z, qb.w};
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(v[e], qv[e], sum);
+        for (int o = 1; o < 8; o <<= 1) { dot += __shfl_xor(dot, o); n2 += __shfl_xor(n2, o); }
+        wmax = fmax(wmax, n2);
+        if ((tid & 7) == 0 && rw >= 0 && dot == dot) {
+          const int at = atomicAdd(&num_exact, 1);         // below BATCH + MAXW
+          exact[at] = dot; exact_row[at] = (uint32_t)rw;
         }
-        sum += __shfl_xor(sum, 1); sum += __shfl_xor(sum, 2); sum += __shfl_xor(sum, 4);
-        if ((tid & 7) == k + z) { rk[0] = in[z] ? order_key(sum) : 0u; rid = (uint32_t)row[z]; }
       }
-    }
-    add_entries<NT, 1>(top, rk, [&](int) { return rid; }, NT, want);
-  }
-  // ---- the best of them in 64 bits
-  const int have = top.have;
-  for (int e = wave; e < have; e += NW) {
-    const T* wr = W + (int64_t)(uint32_t)~(uint32_t)top.best[e] * a.w_stride;
-    double dot = 0.0;
-    for (int c = lane; c < a.dim; c += 64) dot = __builtin_fma((double)qs[c], (double)(float)wr[c], dot);
+      __syncthreads();
+      const int have = num_exact;
+      double v[EPT];
+      uint32_t rw[EPT];
+      int rank[EPT];
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) dot += __shfl_xor(dot, o);
-    if (lane == 0) exact[e] = dot;
+      for (int i = 0; i < EPT; ++i) {
+        const int e = i * NT + tid;
+        rank[i] = want;
+        if (e < have) {
+          v[i] = exact[e]; rw[i] = exact_row[e]; rank[i] = 0;
+#pragma unroll 4
+          for (int j = 0; j < have; ++j) rank[i] += exact[j] > v[i] || (exact[j] == v[i] && exact_row[j] < rw[i]) ? 1 : 0;
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) if (rank[i] < want) { exact[rank[i]] = v[i]; exact_row[rank[i]] = rw[i]; }
+      if (tid == 0) num_exact = min(have, want);
+      __syncthreads();
+    }
+  };
+  score_items(ngr * G, [&](int e) {
+    const int grp = groups[e / G];
+    return row_of(grp, e % G, (int)(__float_as_uint(gm[element(grp)]) & 15u));
+  });
+  // ---- groups whose second largest score may reach the k-th best: within what the passes' scores are off
+  atomicMax(&reach, (unsigned long long)__double_as_longlong(wmax));           // of numbers that are not negative
+  if (tid == 0) top.num = 0;
+  __syncthreads();
+  double qn = 0.0;
+  for (int c = lane; c < a.dim; c += 64) qn = __builtin_fma((double)qs[c], (double)qs[c], qn);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) qn += __shfl_xor(qn, o);
+  const bool full = num_exact >= a.num_top;
+  const double kth = full ? exact[a.num_top - 1] * (double)a.c : 0.0;
+  const float bar = (float)(kth - (fabs(kth) * 0x1p-16 + sqrt(qn) * sqrt(__longlong_as_double((long long)reach)) * (double)a.c * 0x1p-18));
+  if (tid < ngr) {
+    const float two = a.second[q * 2 * a.half + element(groups[tid])] * (a.pairs ? 1.f : a.c);
+    if (two > 0.99f * SM_NO_REF * (a.pairs ? 1.f : a.c) && (!full || two >= bar)) again[atomicAdd(&top.num, 1)] = groups[tid];
   }
   __syncthreads();
-  if (tid < have) {
-    const double v = exact[tid];
-    const uint32_t row = ~(uint32_t)top.best[tid];
-    int rank = 0;
-    for (int j = 0; j < have; ++j) rank += exact[j] > v || (exact[j] == v && (uint32_t)~(uint32_t)top.best[j] < row) ? 1 : 0;
-    if (rank < a.num_top) {
-      a.top_ids[q * a.num_top + rank] = (int32_t)row;
-      a.top_log_probs[q * a.num_top + rank] = (float)(v * (double)a.scale - lse);
-    }
+  const int nagain = top.num;
+  score_items(nagain * G * 16, [&](int e) {
+    const int grp = again[e / (G * 16)], r = e & 15, one = (int)(__float_as_uint(gm[element(grp)]) & 15u);
+    return r == one ? (int64_t)-1 : row_of(grp, (e >> 4) % G, r);
+  });
+  const int have = min(num_exact, a.num_top);
+  for (int e = tid; e < a.num_top; e += NT) {
+    a.top_ids[q * a.num_top + e] = e < have ? (int32_t)exact_row[e] : -1;
+    a.top_log_probs[q * a.num_top + e] = e < have ? (float)(exact[e] * (double)a.scale - lse) : -__builtin_inff();
   }
-  for (int e = have + tid; e < a.num_top; e += NT) { a.top_ids[q * a.num_top + e] = -1; a.top_log_probs[q * a.num_top + e] = -__builtin_inff(); }
 }
 
 // ------------------------------------------------------------------------------------------ plan and checks -----
@@ -366,16 +376,16 @@ SmPlan sm_plan(int dtype, int dim, int pass, int mode, int qb, int64_t n_x, int6
   return r;
 }
 
-// Tiles to a group: about as many group maxima to look through as rows of the best groups to score again, in bytes.
+// Tiles to a group: as many group maxima to look through as bytes of rows behind them (a row of every tile of the best groups).
 static int group_tiles(const mar_softmax* p, int num_top) {
   const double ntiles = (double)((p->num_rows + SM_TY - 1) / SM_TY), row_bytes = p->dim * (p->dtype == MAR_DTYPE_FP32 ? 4.0 : 2.0);
-  const double g = ntiles * 8.0 / ((num_top + SM_MARGIN) * 16.0 * row_bytes);
+  const double g = ntiles * 8.0 / ((num_top + SM_MARGIN) * row_bytes);
   int k = 1;
   while ((double)k * k < g) ++k;
   return k;
 }
 
-struct ProbsLayout { size_t stats, gmax, qtiles, qexps, wtiles, wexps, bytes; SmPlan p0; int group_tiles; int64_t ngroups, half; int mode; };
+struct ProbsLayout { size_t stats, first, second, qtiles, qexps, wtiles, wexps, bytes; SmPlan p0; int group_tiles; int64_t ngroups, half; int mode; };
 static ProbsLayout probs_layout(const mar_softmax* p, int num_top) {
   ProbsLayout L;
   L.group_tiles = num_top ? group_tiles(p, num_top) : 1;
@@ -391,7 +401,8 @@ static ProbsLayout probs_layout(const mar_softmax* p, int num_top) {
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
   L.stats = take((size_t)L.p0.parts * T * sizeof(float4));
-  L.gmax = take(num_top ? T * 2 * (size_t)L.half * 4 : 0);
+  L.first = take(num_top ? T * 2 * (size_t)L.half * 4 : 0);
+  L.second = take(num_top ? T * 2 * (size_t)L.half * 4 : 0);
   L.qtiles = L.qexps = L.wtiles = L.wexps = at;
   if (L.mode == SM_IMAGES) {
     L.qtiles = take(sm_image_bytes(p->dtype, p->dim, p->num_queries)); L.qexps = take(sm_exps_bytes(p->num_queries));
@@ -448,9 +459,9 @@ template <int MODE> static hipError_t launch_stats(int dtype, int qb, const SmAr
 // Threads per query: all that hide a query's own latency where there are few, a wave each where the device is full of them.
 template <int TYPE> static void launch_answer(const AnswerArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)a.n);
-  if (a.n >= MAR_ANSWER_WAVE) hipLaunchKernelGGL((k_answer<TYPE, 64, 32, 8>), grid, dim3(64), 0, st, a);
-  else if (a.n >= MAR_ANSWER_256) hipLaunchKernelGGL((k_answer<TYPE, 256, 16, 8>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_answer<TYPE, 1024, 16, 8>), grid, dim3(1024), 0, st, a);
+  if (a.n >= MAR_ANSWER_WAVE) hipLaunchKernelGGL((k_answer<TYPE, 64, 32>), grid, dim3(64), 0, st, a);
+  else if (a.n >= MAR_ANSWER_256) hipLaunchKernelGGL((k_answer<TYPE, 256, 16>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_answer<TYPE, 1024, 16>), grid, dim3(1024), 0, st, a);
 }
 
 static bool top_ok(int32_t num_top) {
@@ -494,7 +505,8 @@ extern "C" int mar_log_probs(const mar_softmax* p, const void* queries, const vo
   a.dim = p->dim; a.c = p->scale * 1.44269504088896341f;
   a.nstripes = L.p0.stripes; a.parts = L.p0.parts; a.tps = L.p0.tps; a.units = a.nstripes * a.parts;
   a.stats = (float4*)((char*)workspace + L.stats);
-  a.gmax = num_top ? (float*)((char*)workspace + L.gmax) : nullptr;
+  a.first = num_top ? (float*)((char*)workspace + L.first) : nullptr;
+  a.second = num_top ? (float*)((char*)workspace + L.second) : nullptr;
   a.half = L.half; a.group_tiles = L.group_tiles;
   a.allowed = allowed; a.allowed_stride = allowed_stride;
   hipError_t e;
@@ -517,7 +529,7 @@ extern "C" int mar_log_probs(const mar_softmax* p, const void* queries, const vo
   r.Q = queries; r.W = table; r.q_stride = p->query_stride; r.w_stride = p->row_stride; r.rows = p->num_rows;
   r.n = p->num_queries; r.dim = p->dim; r.parts = L.p0.parts; r.num_top = num_top; r.group_tiles = L.group_tiles; r.ngroups = L.ngroups; r.half = L.half;
   r.scale = p->scale; r.unscale = (double)p->scale / (double)a.c;
-  r.targets = targets; r.allowed = allowed; r.allowed_stride = allowed_stride; r.stats = a.stats; r.gmax = a.gmax;
+  r.targets = targets; r.allowed = allowed; r.allowed_stride = allowed_stride; r.stats = a.stats; r.first = a.first; r.second = a.second; r.pairs = p->dtype == MAR_DTYPE_FP32; r.c = a.c;
   r.log_probs = log_probs; r.entropy = entropy; r.top_ids = top_ids; r.top_log_probs = top_log_probs;
   if (p->dtype == MAR_DTYPE_FP32) launch_answer<0>(r, st); else if (p->dtype == MAR_DTYPE_BF16) launch_answer<1>(r, st); else launch_answer<2>(r, st);
   e = hipGetLastError();

@@ -297,7 +297,7 @@ k_softmax(SmArgs a) {
   }
 
   v16f oacc[NO];
-  float ref[QB], lsum[QB], ltot[QB], asum[QB], atot[QB], gmax[QB];
+  float ref[QB], lsum[QB], ltot[QB], asum[QB], atot[QB];
   unsigned word_next[QB];
 #pragma unroll
   for (int c = 0; c < NO; ++c) oacc[c] = (v16f)(0.f);
@@ -308,14 +308,15 @@ k_softmax(SmArgs a) {
       const int own = a.own_top[min(x_first + 32 * b + m, (int64_t)a.n_x - 1)];
       if (own != SM_NO_OWN) ref[b] = own_float(own) - SM_BELOW;
     }
-    lsum[b] = ltot[b] = asum[b] = atot[b] = 0.f; gmax[b] = -__builtin_inff();
+    lsum[b] = ltot[b] = asum[b] = atot[b] = 0.f;
     word_next[b] = PASS == 0 && a.allowed && t_begin < t_end ? words[b][t_begin] : ~0u;
   }
   int group_left = a.group_tiles;
   int64_t group = PASS == 0 ? t_begin / max(a.group_tiles, 1) : 0;             // finished groups
-  v4f gm4[QB];
+  float first_max[QB], second_max[QB];                     // of the group so far (scores of 16-bit types before their factor k)
+  v4f first4[QB], second4[QB];
 #pragma unroll
-  for (int b = 0; b < QB; ++b) gm4[b] = (v4f)(-__builtin_inff());
+  for (int b = 0; b < QB; ++b) { first_max[b] = second_max[b] = SM_NO_REF; first4[b] = second4[b] = (v4f)(SM_NO_REF); }
   float neg1 = -1.f;
   asm volatile("" : "+v"(neg1));
 
@@ -447,22 +448,36 @@ k_softmax(SmArgs a) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) sc[b][r] = pick((unsigned)((int)(bits << (31 - (8 * (r >> 2) + (r & 3)))) >> 31), sc[b][r], -__builtin_inff());
         }
-        float top, ztop;
-        if constexpr (PAIRS) {
-          top = ztop = -__builtin_inff();
+        float ztop;
+        if (PASS == 0 && a.first) {                        // uniform
+          // The largest and the second largest score of the lane's 16, the register's number in their lowest four bits (a score is
+          // as good as known without them): the rows behind them need not be looked for.
+          float v[16];
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            v[r] = __uint_as_float((__float_as_uint(PAIRS ? sc[b][r] * k[r >> 2] : sc[b][r]) & ~15u) | r);
+            if (some) v[r] = pick((unsigned)((int)(bits << (31 - (8 * (r >> 2) + (r & 3)))) >> 31), v[r], SM_NO_REF);   // -inf would become a NaN
+          }
+          float one = fmaxf(v[0], v[1]), two = fminf(v[0], v[1]);
+#pragma unroll
+          for (int r = 2; r < 16; ++r) { two = __builtin_amdgcn_fmed3f(one, two, v[r]); one = fmaxf(one, v[r]); }
+          ztop = one;
+          second_max[b] = fmaxf(fmaxf(fminf(first_max[b], one), second_max[b]), two);
+          first_max[b] = fmaxf(first_max[b], one);
+        } else if constexpr (PAIRS) {
+          ztop = -__builtin_inff();
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const float big = fmaxf(fmaxf(sc[b][4 * j], sc[b][4 * j + 1]), fmaxf(sc[b][4 * j + 2], sc[b][4 * j + 3])) * k[j];
-            top = fmaxf(top, big);
             ztop = fmaxf(ztop, SECOND ? big - (float)ey[j] : big);
           }
         } else {
-          top = sc[b][0];
+          ztop = sc[b][0];
 #pragma unroll
-          for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[b][r]);
-          top *= k[0];
-          ztop = top;
+          for (int r = 1; r < 16; ++r) ztop = fmaxf(ztop, sc[b][r]);
         }
+        if (PASS == 0) ztop = __uint_as_float(__float_as_uint(ztop) & ~15u);   // the same reference with and without the numbers
+        if (!PAIRS) ztop *= k[0];
         // the reference moves
         if (__any(ztop > ref[b] + SM_ABOVE)) {
           ztop = fmaxf(ztop, __shfl_xor(ztop, 32));        // both halves' weights meet in one product
@@ -498,27 +513,27 @@ k_softmax(SmArgs a) {
           ltot[b] += lsum[b]; lsum[b] = 0.f;
           if (PASS == 0) { atot[b] += asum[b]; asum[b] = 0.f; }
         }
-        if (PASS == 0 && a.gmax) {
-          gmax[b] = fmaxf(gmax[b], top);
+        if (PASS == 0 && a.first) {
           if (group_left == 1 || !has_next) {              // uniform
-            if constexpr (FEW) {                           // parts begin where it suits the table
-              if (xv[b]) a.gmax[(x * 2 + h) * a.half + t / a.group_tiles] = gmax[b];
-              gmax[b] = -__builtin_inff();
-            } else {
-            // four groups of a lane at a time: stores of 4 bytes a row apart cost as much as the products
-            gm4[b] = (v4f){gm4[b][1], gm4[b][2], gm4[b][3], gmax[b]};
-            gmax[b] = -__builtin_inff();
             if (b == QB - 1) ++group;
-            if (xv[b]) {
-              float* const to = a.gmax + (x * 2 + h) * a.half;
-              const int64_t n = b == QB - 1 ? group : group + 1;
-              if ((n & 3) == 0) *reinterpret_cast<v4f*>(to + n - 4) = gm4[b];
-              else if (!has_next) {                        // a part's last groups
+            const int64_t n = b == QB - 1 ? group : group + 1, row = (x * 2 + h) * a.half;     // n: groups finished
+            if constexpr (FEW) {                           // parts begin where it suits the table
+              if (xv[b]) { a.first[row + n - 1] = first_max[b]; a.second[row + n - 1] = second_max[b]; }
+            } else {
+              // four groups of a lane at a time: stores of 4 bytes a row apart cost as much as the products
+              first4[b] = (v4f){first4[b][1], first4[b][2], first4[b][3], first_max[b]};
+              second4[b] = (v4f){second4[b][1], second4[b][2], second4[b][3], second_max[b]};
+              if (xv[b]) {
+                if ((n & 3) == 0) {
+                  *reinterpret_cast<v4f*>(a.first + row + n - 4) = first4[b];
+                  *reinterpret_cast<v4f*>(a.second + row + n - 4) = second4[b];
+                } else if (!has_next) {                    // a part's last groups
 #pragma unroll
-                for (int j = 1; j < 4; ++j) if (j >= 4 - (int)(n & 3)) to[n - 4 + j] = gm4[b][j];
+                  for (int j = 1; j < 4; ++j) if (j >= 4 - (int)(n & 3)) { a.first[row + n - 4 + j] = first4[b][j]; a.second[row + n - 4 + j] = second4[b][j]; }
+                }
               }
             }
-            }
+            first_max[b] = second_max[b] = SM_NO_REF;
           }
         }
         if constexpr (PASS == 1) {
