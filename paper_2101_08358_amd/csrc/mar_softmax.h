@@ -42,7 +42,6 @@ struct SmArgs {
   const int32_t* targets;
   float* O; int32_t o_pitch;       // [parts][n_x][o_pitch]
   const float* row_m; const float* row_f; const float* row_u;   // pass 2: per query, see k_loss_rows
-  const int32_t* own_top;          // pass 2, per stationary row: largest log2 |u| - e of the queries whose answer it is (own_key), or SM_NO_OWN
   void* out; int64_t out_stride;   // pass 2 in one part: the gradient itself
 };
 
@@ -52,13 +51,12 @@ struct SmPackArgs {
   const void* src; int64_t stride; int32_t n, dim;
   char* tiles; int* exps;
   const int32_t* ids; const float* weights; int64_t num_ids;
-  int32_t* own_top;                // where not NULL: [n], set to SM_NO_OWN
 };
 size_t sm_image_bytes(int dtype, int dim, int64_t rows);   // a multiple of 256
 size_t sm_exps_bytes(int64_t rows);
 hipError_t sm_pack(int dtype, const SmPackArgs& a, hipStream_t st);
 
-struct SmPlan { int32_t qb, stripes, parts, tps, ntiles; };
+struct SmPlan { int32_t stripes, parts, tps, ntiles; };
 
 const char* sm_check(const mar_softmax* p, int* code);
-SmPlan sm_plan(int dtype, int dim, int pass, int mode, int qb, int64_t n_x, int64_t n_y, int multiple);
+SmPlan sm_plan(int dtype, int dim, int pass, int mode, int64_t n_x, int64_t n_y, int multiple);

@@ -7,14 +7,10 @@
 // scored again, 16 each: 4,096 queries, 131,072 rows of 400 columns, 16 best rows 367 us, for 1 GB of rows read at random.)
 #include "mar_softmax_dev.h"
 
-// Stripes of queries from which the table is laid out as images first.
-#ifndef MAR_SOFTMAX_IMAGES
-#define MAR_SOFTMAX_IMAGES 8
-#endif
-#ifndef MAR_ANSWER_WAVE
-#define MAR_ANSWER_WAVE 1000
-#define MAR_ANSWER_256 200
-#endif
+// Queries above which the matrices are laid out as images first, us rows / images: fp32, 120,000 rows of 100 columns, 128 queries 63 /
+// 70, 256: 89 / 83, 400: 137 / 109; 1,000,000 rows 284 / 417, 486 / 487, 845 / 671; bf16, 1,000,000 rows 241 / 257, 260 / 278,
+// 423 / 384; 100,000 rows of 400 columns 57 / 74, 78 / 91, 115 / 117.
+#define MAR_SOFTMAX_ROWS_MAX 256
 #define SM_MARGIN 12              // groups, and rows, kept beyond the number asked for: what fp32 less four bits cannot tell apart
 
 struct AnswerArgs {
@@ -65,8 +61,8 @@ __device__ __forceinline__ void add_entries(TopList& top, const uint32_t (&key)[
   // a full list's last entry bounds what can still enter
   const int old = top.have;
   const uint32_t floor_key = old == want ? max((uint32_t)(top.best[want - 1] >> 32), 1u) : 1u;
-  const uint32_t v = top.group[lane];
-  if (wave == 0) {
+  if (old < want && wave == 0) {
+    const uint32_t v = top.group[lane];
     int rank = 0;
 #pragma unroll
     for (int j = 0; j < 64; ++j) {
@@ -76,7 +72,7 @@ __device__ __forceinline__ void add_entries(TopList& top, const uint32_t (&key)[
     if (rank == want - 1) top.threshold = v;
   }
   __syncthreads();
-  uint32_t x = max(top.threshold, floor_key);
+  uint32_t x = old == want ? floor_key : max(top.threshold, 1u);
   uint32_t tie = 0u, id_end = ~0u;                         // of the entries with key `tie` those with an id below id_end
   auto collect = [&]() {
 #pragma unroll
@@ -157,7 +153,7 @@ template <int TYPE, int NT, int R>
 __global__ void __launch_bounds__(NT)
 k_answer(AnswerArgs a) {
   typedef typename RowType<TYPE>::T T;
-  constexpr int MAXW = MAR_MAX_TOP + SM_MARGIN, NW = NT / 64, BATCH = NT / 8 < 64 ? 64 : NT / 8, EPT = (BATCH + MAXW + NT - 1) / NT;
+  constexpr int MAXW = MAR_MAX_TOP + SM_MARGIN, NW = NT / 64, BATCH = NT / 8 < 64 ? 64 : NT / 8, SL = NT / BATCH, EPT = (BATCH + MAXW + BATCH - 1) / BATCH;
   constexpr int QN = (MAR_MAX_DIM + 7) / 8 * 8;
   __shared__ float s_m[NW], s_l[NW], s_a[NW];
   __shared__ __attribute__((aligned(16))) float qs[QN];
@@ -277,22 +273,26 @@ k_answer(AnswerArgs a) {
       }
       __syncthreads();
       const int have = num_exact;
+      // an entry's rank: SL threads each compare it with a part of the others
       double v[EPT];
       uint32_t rw[EPT];
       int rank[EPT];
 #pragma unroll
       for (int i = 0; i < EPT; ++i) {
-        const int e = i * NT + tid;
+        const int e = i * BATCH + tid / SL;
         rank[i] = want;
-        if (e < have) {
-          v[i] = exact[e]; rw[i] = exact_row[e]; rank[i] = 0;
+        if (i * BATCH < have) {                            // uniform
+          v[i] = exact[min(e, have - 1)]; rw[i] = exact_row[min(e, have - 1)]; rank[i] = 0;
 #pragma unroll 4
-          for (int j = 0; j < have; ++j) rank[i] += exact[j] > v[i] || (exact[j] == v[i] && exact_row[j] < rw[i]) ? 1 : 0;
+          for (int j = tid % SL; j < have; j += SL) rank[i] += exact[j] > v[i] || (exact[j] == v[i] && exact_row[j] < rw[i]) ? 1 : 0;
+#pragma unroll
+          for (int o = 1; o < SL; o <<= 1) rank[i] += __shfl_xor(rank[i], o);
+          if (e >= have) rank[i] = want;
         }
       }
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) if (rank[i] < want) { exact[rank[i]] = v[i]; exact_row[rank[i]] = rw[i]; }
+      for (int i = 0; i < EPT; ++i) if (rank[i] < want && tid % SL == 0) { exact[rank[i]] = v[i]; exact_row[rank[i]] = rw[i]; }
       if (tid == 0) num_exact = min(have, want);
       __syncthreads();
     }
@@ -302,7 +302,9 @@ k_answer(AnswerArgs a) {
     return row_of(grp, e % G, (int)(__float_as_uint(gm[element(grp)]) & 15u));
   });
   // ---- groups whose second largest score may reach the k-th best: within what the passes' scores are off
-  atomicMax(&reach, (unsigned long long)__double_as_longlong(wmax));           // of numbers that are not negative
+#pragma unroll
+  for (int o = 8; o < 64; o <<= 1) wmax = fmax(wmax, __shfl_xor(wmax, o));
+  if (lane == 0) atomicMax(&reach, (unsigned long long)__double_as_longlong(wmax));                // of numbers that are not negative
   if (tid == 0) top.num = 0;
   __syncthreads();
   double qn = 0.0;
@@ -347,22 +349,21 @@ const char* sm_check(const mar_softmax* p, int* code) {
 
 // Parts: where the stripes do not fill the device, several workgroups share one, each streaming a part of the tiles.  Estimated by
 // the rounds of workgroups and their tiles, a workgroup costing four tiles more for its rows and its first tile.
-SmPlan sm_plan(int dtype, int dim, int pass, int mode, int qb, int64_t n_x, int64_t n_y, int multiple) {
+SmPlan sm_plan(int dtype, int dim, int pass, int mode, int64_t n_x, int64_t n_y, int multiple) {
   SmPlan r;
   const int nk = sm_nk(dim);
-  r.qb = qb;
   r.ntiles = (int32_t)((n_y + SM_TY - 1) / SM_TY);
   if (mode == SM_FEW) {                                    // every wave that the device holds, at least a tile each
     const int64_t tile = (int64_t)SM_TY * sp_pitch(nk) * (dtype == MAR_DTYPE_FP32 ? 2 : 1);
-    const int64_t a_cu = 4 * sm_few_waves(dtype, nk, qb), fit = 160 * 1024 / (tile + 1024), slots = 256 * (a_cu < fit ? a_cu : fit);
+    const int64_t a_cu = 4 * sm_waves_of(dtype, nk, 0, SM_FEW), fit = 160 * 1024 / (tile + 1024), slots = 256 * (a_cu < fit ? a_cu : fit);
     int64_t tps = (r.ntiles + slots - 1) / slots;
     if (tps < 1) tps = 1;
     tps = (tps + multiple - 1) / multiple * multiple;
     r.stripes = 1; r.tps = (int32_t)tps; r.parts = (int32_t)((r.ntiles + tps - 1) / tps);
     return r;
   }
-  r.stripes = (int32_t)((n_x + 128 * qb - 1) / (128 * qb));
-  const int64_t slots = 256 * sm_waves_of(dtype, nk, pass, mode, qb);
+  r.stripes = (int32_t)((n_x + 127) / 128);
+  const int64_t slots = 256 * sm_waves_of(dtype, nk, pass, mode);
   int64_t best = INT64_MAX;
   r.parts = 1; r.tps = r.ntiles;
   const int most = pass == 0 ? 1024 : MAR_SOFTMAX_MAX_PARTS;
@@ -376,25 +377,21 @@ SmPlan sm_plan(int dtype, int dim, int pass, int mode, int qb, int64_t n_x, int6
   return r;
 }
 
-// Tiles to a group: as many group maxima to look through as bytes of rows behind them (a row of every tile of the best groups).
+// Tiles to a group: one while a query has no more than 4,096 groups, then as many as leave the rows behind the best groups' maxima to
+// one round of a workgroup of 1,024 (128 rows; a round costs as much as looking through 40,000 maxima).
 static int group_tiles(const mar_softmax* p, int num_top) {
-  const double ntiles = (double)((p->num_rows + SM_TY - 1) / SM_TY), row_bytes = p->dim * (p->dtype == MAR_DTYPE_FP32 ? 4.0 : 2.0);
-  const double g = ntiles * 8.0 / ((num_top + SM_MARGIN) * row_bytes);
-  int k = 1;
-  while ((double)k * k < g) ++k;
-  return k;
+  const int64_t ntiles = (p->num_rows + SM_TY - 1) / SM_TY, most = 128 / (num_top + SM_MARGIN);
+  const int64_t g = (ntiles + 2047) / 2048;
+  return (int)(g < most ? g : most);
 }
 
 struct ProbsLayout { size_t stats, first, second, qtiles, qexps, wtiles, wexps, bytes; SmPlan p0; int group_tiles; int64_t ngroups, half; int mode; };
 static ProbsLayout probs_layout(const mar_softmax* p, int num_top) {
   ProbsLayout L;
   L.group_tiles = num_top ? group_tiles(p, num_top) : 1;
-  const int nk = sm_nk(p->dim), few = p->dtype == MAR_DTYPE_FP32 ? 32 : 64;
-  int qb = sm_qb(p->dtype, nk, 0);
-  L.mode = p->num_queries <= few ? SM_FEW : ((p->num_queries + 128 * qb - 1) / (128 * qb) >= MAR_SOFTMAX_IMAGES ? SM_IMAGES : SM_ROWS);
-  if (L.mode == SM_FEW) qb = p->num_queries <= 32 ? 1 : 2;
+  L.mode = p->num_queries <= 32 && sm_nk(p->dim) <= 16 ? SM_FEW : (p->num_queries > MAR_SOFTMAX_ROWS_MAX ? SM_IMAGES : SM_ROWS);
   // group maxima are stored four groups at a time, but for few queries
-  L.p0 = sm_plan(p->dtype, p->dim, 0, L.mode, qb, p->num_queries, p->num_rows, num_top ? (L.mode == SM_FEW ? 1 : 4) * L.group_tiles : 1);
+  L.p0 = sm_plan(p->dtype, p->dim, 0, L.mode, p->num_queries, p->num_rows, num_top ? (L.mode == SM_FEW ? 1 : 4) * L.group_tiles : 1);
   L.ngroups = num_top ? (L.p0.ntiles + L.group_tiles - 1) / L.group_tiles : 0;
   L.half = (L.ngroups + 3) / 4 * 4 + 8;                    // queries' rows not a power of two apart
   const size_t T = (size_t)p->num_queries;
@@ -412,16 +409,16 @@ static ProbsLayout probs_layout(const mar_softmax* p, int num_top) {
   return L;
 }
 
-template <int TYPE, int MODE, int QB> static void launch_nk(const SmArgs& a, hipStream_t st) {   // QB 0: as the width has it
+template <int TYPE, int MODE> static void launch_nk(const SmArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)((a.units + 7) / 8 * 8)), block(sm_threads(MODE));
   switch (sm_nk(a.dim)) {
-    case 2: hipLaunchKernelGGL((k_softmax<TYPE, 2, 0, MODE, QB ? QB : sm_qb(TYPE, 2, 0)>), grid, block, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((k_softmax<TYPE, 4, 0, MODE, QB ? QB : sm_qb(TYPE, 4, 0)>), grid, block, 0, st, a); break;
-    case 7: hipLaunchKernelGGL((k_softmax<TYPE, 7, 0, MODE, QB ? QB : sm_qb(TYPE, 7, 0)>), grid, block, 0, st, a); break;
-    case 8: hipLaunchKernelGGL((k_softmax<TYPE, 8, 0, MODE, QB ? QB : sm_qb(TYPE, 8, 0)>), grid, block, 0, st, a); break;
-    case 12: hipLaunchKernelGGL((k_softmax<TYPE, 12, 0, MODE, QB ? QB : sm_qb(TYPE, 12, 0)>), grid, block, 0, st, a); break;
-    case 16: hipLaunchKernelGGL((k_softmax<TYPE, 16, 0, MODE, QB ? QB : sm_qb(TYPE, 16, 0)>), grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL((k_softmax<TYPE, 25, 0, MODE, QB ? QB : sm_qb(TYPE, 25, 0)>), grid, block, 0, st, a); break;
+    case 2: hipLaunchKernelGGL((k_softmax<TYPE, 2, 0, MODE>), grid, block, 0, st, a); break;
+    case 4: hipLaunchKernelGGL((k_softmax<TYPE, 4, 0, MODE>), grid, block, 0, st, a); break;
+    case 7: hipLaunchKernelGGL((k_softmax<TYPE, 7, 0, MODE>), grid, block, 0, st, a); break;
+    case 8: hipLaunchKernelGGL((k_softmax<TYPE, 8, 0, MODE>), grid, block, 0, st, a); break;
+    case 12: hipLaunchKernelGGL((k_softmax<TYPE, 12, 0, MODE>), grid, block, 0, st, a); break;
+    case 16: hipLaunchKernelGGL((k_softmax<TYPE, 16, 0, MODE>), grid, block, 0, st, a); break;
+    default: if constexpr (MODE != SM_FEW) hipLaunchKernelGGL((k_softmax<TYPE, 25, 0, MODE>), grid, block, 0, st, a); break;
   }
 }
 template <int TYPE> static void launch_pack(const SmPackArgs& a, hipStream_t st) {
@@ -445,22 +442,18 @@ size_t sm_image_bytes(int dtype, int dim, int64_t rows) {
   return (size_t)((rows + SM_TY - 1) / SM_TY) * SM_TY * sp_pitch(nk) * (dtype == MAR_DTYPE_FP32 ? 2 : 1);
 }
 size_t sm_exps_bytes(int64_t rows) { return ((size_t)((rows + SM_TY - 1) / SM_TY) * 16 + 255) / 256 * 256; }
-template <int MODE> static hipError_t launch_stats(int dtype, int qb, const SmArgs& a, hipStream_t st) {
-  if constexpr (MODE == SM_FEW) {
-    if (dtype == MAR_DTYPE_FP32) launch_nk<0, MODE, 1>(a, st);
-    else if (dtype == MAR_DTYPE_BF16) { if (qb == 1) launch_nk<1, MODE, 1>(a, st); else launch_nk<1, MODE, 2>(a, st); }
-    else { if (qb == 1) launch_nk<2, MODE, 1>(a, st); else launch_nk<2, MODE, 2>(a, st); }
-  } else {
-    if (dtype == MAR_DTYPE_FP32) launch_nk<0, MODE, 0>(a, st); else if (dtype == MAR_DTYPE_BF16) launch_nk<1, MODE, 0>(a, st); else launch_nk<2, MODE, 0>(a, st);
-  }
+template <int MODE> static hipError_t launch_stats(int dtype, const SmArgs& a, hipStream_t st) {
+  if (dtype == MAR_DTYPE_FP32) launch_nk<0, MODE>(a, st); else if (dtype == MAR_DTYPE_BF16) launch_nk<1, MODE>(a, st); else launch_nk<2, MODE>(a, st);
   return hipGetLastError();
 }
 
 // Threads per query: all that hide a query's own latency where there are few, a wave each where the device is full of them.
+// us a call, 64 / 256 / 1,024 threads: bf16, 120,000 rows of 100 columns, 128 queries 73 / 41 / 38, 512: 103 / 74 / 83, 1,000: 135 /
+// 115 / 142, 4,000: 356 / 351 / 469; 15,000 rows, 1,000 queries 56 / 55 / 82, 2,000: 66 / 80 / 139, 4,000: 125 / 157 / 283.
 template <int TYPE> static void launch_answer(const AnswerArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)a.n);
-  if (a.n >= MAR_ANSWER_WAVE) hipLaunchKernelGGL((k_answer<TYPE, 64, 32>), grid, dim3(64), 0, st, a);
-  else if (a.n >= MAR_ANSWER_256) hipLaunchKernelGGL((k_answer<TYPE, 256, 16>), grid, dim3(256), 0, st, a);
+  if (a.n >= 2000) hipLaunchKernelGGL((k_answer<TYPE, 64, 32>), grid, dim3(64), 0, st, a);
+  else if (a.n > 256) hipLaunchKernelGGL((k_answer<TYPE, 256, 16>), grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((k_answer<TYPE, 1024, 16>), grid, dim3(1024), 0, st, a);
 }
 
@@ -520,9 +513,9 @@ extern "C" int mar_log_probs(const mar_softmax* p, const void* queries, const vo
     if (e != hipSuccess) { mar_set_error("image kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
     a.ximg = {(char*)workspace + L.qtiles, (const int*)((char*)workspace + L.qexps)};
     a.yimg = {(char*)workspace + L.wtiles, (const int*)((char*)workspace + L.wexps)};
-    e = launch_stats<SM_IMAGES>(p->dtype, L.p0.qb, a, st);
+    e = launch_stats<SM_IMAGES>(p->dtype, a, st);
   } else {
-    e = L.mode == SM_FEW ? launch_stats<SM_FEW>(p->dtype, L.p0.qb, a, st) : launch_stats<SM_ROWS>(p->dtype, L.p0.qb, a, st);
+    e = L.mode == SM_FEW ? launch_stats<SM_FEW>(p->dtype, a, st) : launch_stats<SM_ROWS>(p->dtype, a, st);
   }
   if (e != hipSuccess) { mar_set_error("softmax kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
   AnswerArgs r = {};

@@ -10,12 +10,12 @@
 template <int N, typename F> __device__ __forceinline__ void unrolled(F&& f) {
   if constexpr (N > 0) { unrolled<N - 1>(f); f(std::integral_constant<int, N - 1>{}); }
 }
-// Stationary blocks of 32 rows a wave takes, and waves per SIMD (= workgroups per CU): as registers allow.  An A fragment read from LDS
-// feeds one product a block, so two blocks halve the LDS traffic; pass 0, which keeps no sums of rows, has the registers.
-constexpr int sm_qb(int type, int nk, int pass) { return pass == 0 && type != MAR_DTYPE_FP32 && nk <= 16 ? 2 : 1; }
+// Waves per SIMD (= workgroups per CU), as registers allow.  A wave takes 32 stationary rows; 64, which halves what is read of LDS,
+// left pass 0 fewer waves to hide a tile's latency (bf16, 15,000 rows of 100 columns, 256 queries 35 us, now 28; 100,000 rows of
+// 256 columns, 1,000 queries 184 and 161).
 constexpr int sm_waves(int type, int nk, int pass) {
   return type == MAR_DTYPE_FP32 ? (pass == 0 ? (nk <= 8 ? 3 : (nk <= 16 ? 2 : 1)) : (nk <= 4 && pass == 1 ? 3 : (nk <= 8 ? 2 : 1)))
-                                : (pass == 0 ? (nk <= 8 ? 3 : 2) : (nk <= 4 ? 3 : (nk <= 12 ? 2 : 1)));
+                                : (pass == 0 ? (nk <= 8 ? 4 : (nk <= 12 ? 3 : 2)) : (nk <= 4 ? 3 : (nk <= 12 ? 2 : 1)));
 }
 
 template <int TYPE> __device__ __forceinline__ v16f sm_mfma(v8s a, v8s b, v16f c) {
@@ -162,13 +162,14 @@ __device__ __forceinline__ float own_float(int k) { return __int_as_float(k < 0 
 #define SM_FEW 2
 constexpr int sm_threads(int mode) { return mode == SM_FEW ? 64 : 256; }
 // Waves per SIMD by mode: staging takes registers of its own.
-constexpr int sm_few_waves(int type, int nk, int qb) { return type == MAR_DTYPE_FP32 ? (nk <= 4 ? 2 : 1) : (nk <= 4 || (nk <= 8 && qb == 1) ? 3 : (nk <= 8 || (nk <= 12 && qb == 1) ? 2 : 1)); }
-constexpr int sm_rows_waves(int type, int nk) { return nk <= 4 ? 3 : (nk <= 12 ? 2 : (type != MAR_DTYPE_FP32 && nk > 16 ? 2 : 1)); }
-constexpr int sm_waves_of(int type, int nk, int pass, int mode, int qb) {
-  return mode == SM_FEW ? sm_few_waves(type, nk, qb) : (mode == SM_ROWS ? sm_rows_waves(type, nk) : sm_waves(type, nk, pass));
+constexpr int sm_waves_of(int type, int nk, int pass, int mode) {
+  const bool wide = type == MAR_DTYPE_FP32;
+  return mode == SM_IMAGES ? sm_waves(type, nk, pass)
+         : mode == SM_FEW  ? (wide ? (nk <= 4 ? 2 : 1) : (nk <= 8 ? 3 : (nk <= 12 ? 2 : 1)))
+                           : (wide ? (nk <= 4 ? 3 : (nk <= 12 ? 2 : 1)) : (nk <= 8 ? 4 : 2));
 }
-template <int TYPE, int NK, int PASS, int MODE, int QB>
-__global__ void __launch_bounds__(sm_threads(MODE)) __attribute__((amdgpu_waves_per_eu(sm_waves_of(TYPE, NK, PASS, MODE, QB), sm_waves_of(TYPE, NK, PASS, MODE, QB))))
+template <int TYPE, int NK, int PASS, int MODE>
+__global__ void __launch_bounds__(sm_threads(MODE)) __attribute__((amdgpu_waves_per_eu(sm_waves_of(TYPE, NK, PASS, MODE), sm_waves_of(TYPE, NK, PASS, MODE))))
 k_softmax(SmArgs a) {
   typedef SmGeom<TYPE, NK> G;
   typedef typename RowType<TYPE>::T T;
@@ -179,7 +180,6 @@ k_softmax(SmArgs a) {
   constexpr bool REFS = PASS != 2 || TYPE != MAR_DTYPE_BF16 || NK > 16;   // weights relative to a reference (bf16 does without; the widest rows' registers do not)
   constexpr int PL = G::PLANES;
   static_assert(IMG || PASS == 0, "passes with a second product take images");
-  static_assert(QB == 1 || PASS == 0, "passes with a second product take one block a wave");
   constexpr int NB = FEW ? 1 : 2;                          // tiles in LDS
   __shared__ __attribute__((aligned(1024))) char smem[NB * G::TILE];
   __shared__ int exps[2][4];
@@ -187,6 +187,7 @@ k_softmax(SmArgs a) {
   __shared__ __attribute__((aligned(16))) float rows_m[2][SM_TY], rows_f[2][SM_TY], rows_u[2][SM_TY];
   __shared__ __attribute__((aligned(16))) int rows_t[2][SM_TY];
   __shared__ unsigned rows_neg[2];                         // queries with a negative u
+  __shared__ int own[PASS == 2 && REFS ? 128 : 1];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5, m = lane & 31, g = lane >> 4, i = lane & 15;
@@ -196,7 +197,7 @@ k_softmax(SmArgs a) {
   const int part = unit / a.nstripes, stripe = unit - part * a.nstripes;
   const int ntiles_all = (int)(((int64_t)a.n_y + SM_TY - 1) / SM_TY);
   const int t_begin = part * a.tps, t_end = min(ntiles_all, t_begin + a.tps);
-  const int64_t x_first = FEW ? 0 : (int64_t)stripe * (128 * QB) + wave * (32 * QB);
+  const int64_t x_first = FEW ? 0 : (int64_t)stripe * 128 + wave * 32;
   const int dim = a.dim;
 
   // zeros: units beyond the columns that a tile's copies write
@@ -246,77 +247,84 @@ k_softmax(SmArgs a) {
     load_rows(t_begin * SM_TY);
   }
 
-  // ---- stationary fragments
-  v8s xh[QB][NK], xl[QB][PAIRS ? NK : 1];
-  int ex[QB], tgt[QB];
-  bool xv[QB];
-  const uint32_t* words[QB];
+  // Pass 2: largest log2 |u| - e of the part's queries whose answer is one of the workgroup's rows.  (One array for all rows, which
+  // k_loss_rows raised by atomics, held 8,192 queries with popular answers up 40 us.)
+  if constexpr (PASS == 2 && REFS) {
+    for (int k = tid; k < 128; k += 256) own[k] = SM_NO_OWN;
+    __syncthreads();
+    const int64_t first = (int64_t)stripe * 128, y_end = min((int64_t)a.n_y, (int64_t)t_end * SM_TY);
+    for (int64_t y0 = (int64_t)t_begin * SM_TY; y0 < y_end; y0 += 4 * 256) {
+      int id[4];
 #pragma unroll
-  for (int b = 0; b < QB; ++b) {
-    const int64_t x = x_first + 32 * b + m;
-    xv[b] = x < a.n_x;
-    const int64_t xr = xv[b] ? x : a.n_x - 1;
-    const T* row = (const T*)a.X + xr * a.x_stride;
-    ex[b] = 0;
-    tgt[b] = PASS == 1 && xv[b] ? a.targets[xr] : -1;
-    words[b] = PASS == 0 && a.allowed ? a.allowed + xr * a.allowed_stride : nullptr;
-    if constexpr (IMG) {
-      const int64_t xt = min((x_first + 32 * b) / SM_TY, (int64_t)(a.n_x - 1) / SM_TY);                // a block is a tile
-      const char* const row = a.ximg.tiles + xt * G::TILE + m * G::PA;
-      const int swz = 16 * sp_swizzle(G::UNITS, m);
-      if (PAIRS) ex[b] = a.ximg.exps[4 * xt + (m >> 3)];
-      unrolled<NK>([&](auto step) {
-        constexpr int s = step;
-        xh[b][s] = *reinterpret_cast<const v8s*>(row + ((32 * s + 16 * h) ^ swz));
-        if constexpr (PAIRS) xl[b][s] = *reinterpret_cast<const v8s*>(row + G::PLANE + ((32 * s + 16 * h) ^ swz));
-      });
-    }
-    if (PAIRS && !IMG) {
-      int big = 0;
-      unrolled<NK>([&](int s) {
-        float v[8];
-        load8<TYPE>(row, 16 * s + 8 * h, dim, v);
+      for (int k = 0; k < 4; ++k) { const int64_t y = y0 + 256 * k + tid; id[k] = y < y_end ? a.targets[y] : -1; }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) big = max(big, finite_bits(v[e]));
-        if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-      });
-      big = max(big, __shfl_xor(big, 32));
-      ex[b] = sm_exponent(big);
-    }
-    if constexpr (!IMG) unrolled<NK>([&](auto step) {
-      constexpr int s = step;
-      if constexpr (PAIRS) {
-        float v[8];
-        load8<TYPE>(row, 16 * s + 8 * h, dim, v);
-        sm_parts8(v, __builtin_ldexpf(1.f, ex[b]), xh[b][s], xl[b][s]);
-      } else {
-        xh[b][s] = __builtin_bit_cast(v8s, load8_bits(row, 16 * s + 8 * h, dim));
+      for (int k = 0; k < 4; ++k) {
+        if (id[k] < first || id[k] >= first + 128) continue;
+        const int64_t y = y0 + 256 * k + tid;
+        const float u = a.row_u[y];
+        if (u != 0.f) atomicMax(&own[id[k] - (int)first], own_key(__builtin_amdgcn_logf(fabsf(u)) - (PAIRS ? (float)a.yimg.exps[y >> 3] : 0.f)));
       }
-      if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-    });
+    }
+    __syncthreads();
   }
 
+  // ---- stationary fragments
+  v8s xh[NK], xl[PAIRS ? NK : 1];
+  const int64_t x = x_first + m;
+  const bool xv = x < a.n_x;
+  const int64_t xr = xv ? x : a.n_x - 1;
+  const T* xrow = (const T*)a.X + xr * a.x_stride;         // not for images
+  int ex = 0;
+  const int tgt = PASS == 1 && xv ? a.targets[xr] : -1;
+  const uint32_t* words = PASS == 0 && a.allowed ? a.allowed + xr * a.allowed_stride : nullptr;
+  if constexpr (IMG) {
+    const int64_t xt = min(x_first / SM_TY, (int64_t)(a.n_x - 1) / SM_TY);         // the wave's rows are a tile
+    const char* const row = a.ximg.tiles + xt * G::TILE + m * G::PA;
+    const int swz = 16 * sp_swizzle(G::UNITS, m);
+    if (PAIRS) ex = a.ximg.exps[4 * xt + (m >> 3)];
+    unrolled<NK>([&](auto step) {
+      constexpr int s = step;
+      xh[s] = *reinterpret_cast<const v8s*>(row + ((32 * s + 16 * h) ^ swz));
+      if constexpr (PAIRS) xl[s] = *reinterpret_cast<const v8s*>(row + G::PLANE + ((32 * s + 16 * h) ^ swz));
+    });
+  }
+  if (PAIRS && !IMG) {
+    int big = 0;
+    unrolled<NK>([&](int s) {
+      float v[8];
+      load8<TYPE>(xrow, 16 * s + 8 * h, dim, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) big = max(big, finite_bits(v[e]));
+      if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    });
+    big = max(big, __shfl_xor(big, 32));
+    ex = sm_exponent(big);
+  }
+  if constexpr (!IMG) unrolled<NK>([&](auto step) {
+    constexpr int s = step;
+    if constexpr (PAIRS) {
+      float v[8];
+      load8<TYPE>(xrow, 16 * s + 8 * h, dim, v);
+      sm_parts8(v, __builtin_ldexpf(1.f, ex), xh[s], xl[s]);
+    } else {
+      xh[s] = __builtin_bit_cast(v8s, load8_bits(xrow, 16 * s + 8 * h, dim));
+    }
+    if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+  });
+
   v16f oacc[NO];
-  float ref[QB], lsum[QB], ltot[QB], asum[QB], atot[QB];
-  unsigned word_next[QB];
 #pragma unroll
   for (int c = 0; c < NO; ++c) oacc[c] = (v16f)(0.f);
-#pragma unroll
-  for (int b = 0; b < QB; ++b) {
-    ref[b] = SM_NO_REF;
-    if (PASS == 2 && REFS) {                               // the weights of the row's own queries stay below it
-      const int own = a.own_top[min(x_first + 32 * b + m, (int64_t)a.n_x - 1)];
-      if (own != SM_NO_OWN) ref[b] = own_float(own) - SM_BELOW;
-    }
-    lsum[b] = ltot[b] = asum[b] = atot[b] = 0.f;
-    word_next[b] = PASS == 0 && a.allowed && t_begin < t_end ? words[b][t_begin] : ~0u;
+  float ref = SM_NO_REF, lsum = 0.f, ltot = 0.f, asum = 0.f, atot = 0.f;
+  if (PASS == 2 && REFS) {                                 // the weights of the row's own queries stay below it
+    const int top = own[wave * 32 + m];
+    if (top != SM_NO_OWN) ref = own_float(top) - SM_BELOW;
   }
+  unsigned word_next = PASS == 0 && a.allowed && t_begin < t_end ? words[t_begin] : ~0u;
   int group_left = a.group_tiles;
   int64_t group = PASS == 0 ? t_begin / max(a.group_tiles, 1) : 0;             // finished groups
-  float first_max[QB], second_max[QB];                     // of the group so far (scores of 16-bit types before their factor k)
-  v4f first4[QB], second4[QB];
-#pragma unroll
-  for (int b = 0; b < QB; ++b) { first_max[b] = second_max[b] = SM_NO_REF; first4[b] = second4[b] = (v4f)(SM_NO_REF); }
+  float first_max = SM_NO_REF, second_max = SM_NO_REF;     // of the group so far (scores of 16-bit types before their factor k)
+  v4f first4 = (v4f)(SM_NO_REF), second4 = first4;
   float neg1 = -1.f;
   asm volatile("" : "+v"(neg1));
 
@@ -356,12 +364,8 @@ k_softmax(SmArgs a) {
     const int buf = FEW ? 0 : (t - t_begin) & 1, bofs = buf * G::TILE;
     const int y0 = t * SM_TY;
     const bool has_next = t + 1 < t_end;                   // uniform
-    unsigned word[QB];
-#pragma unroll
-    for (int b = 0; b < QB; ++b) {
-      word[b] = word_next[b];
-      if (PASS == 0 && has_next && a.allowed) word_next[b] = words[b][t + 1];
-    }
+    unsigned word = word_next;
+    if (PASS == 0 && has_next && a.allowed) word_next = words[t + 1];
     if (has_next) {
       if constexpr (IMG) ask_exps(t + 1);
       else {
@@ -374,9 +378,7 @@ k_softmax(SmArgs a) {
     }
 
     // ---- scores; the streamed fragments are read PD steps ahead, the next tile's pieces are asked for between the steps
-    v16f sc[QB];
-#pragma unroll
-    for (int b = 0; b < QB; ++b) sc[b] = (v16f)(0.f);
+    v16f sc = (v16f)(0.f);
     {
       constexpr int PD = PAIRS ? 2 : (NK < 4 ? NK : 4);
       v8s f[PD][PL];
@@ -391,11 +393,8 @@ k_softmax(SmArgs a) {
         constexpr int s = step;
         const v8s yh = f[s % PD][0], yl = f[s % PD][PL - 1];
         if (s + PD < NK) read(s + PD);
-#pragma unroll
-        for (int b = 0; b < QB; ++b) {
-          if constexpr (PAIRS) { sc[b] = sm_mfma<TYPE>(yl, xh[b][s], sc[b]); sc[b] = sm_mfma<TYPE>(yh, xl[b][s], sc[b]); }
-          sc[b] = sm_mfma<TYPE>(yh, xh[b][s], sc[b]);
-        }
+        if constexpr (PAIRS) { sc = sm_mfma<TYPE>(yl, xh[s], sc); sc = sm_mfma<TYPE>(yh, xl[s], sc); }
+        sc = sm_mfma<TYPE>(yh, xh[s], sc);
         if (has_next) {
           if constexpr (IMG) {
 #pragma unroll
@@ -430,168 +429,162 @@ k_softmax(SmArgs a) {
     }
 
     float w[16];
-    bool hit = false;                                      // PASS 2: the answer of one of the tile's queries is among the wave's rows
+    // ---- t = sc k[r / 4]: scores in log2 units
+    float k[4];
 #pragma unroll
-    for (int b = 0; b < QB; ++b) {
-      // ---- t = sc k[r / 4]: scores in log2 units
-      float k[4];
+    for (int j = 0; j < 4; ++j) k[j] = PAIRS ? fmaxf(__builtin_ldexpf(a.c, max(-200, min(120, -(ex + ey[j])))), 0x1p-126f) : a.c;   // never 0: -inf times it stays
+    if constexpr (PASS != 2) {
+      // rows that do not count: beyond the last, or not allowed
+      const int left = a.n_y - y0;
+      if (left < 32) word &= (1u << left) - 1u;
+      const bool some = (PASS == 0 && a.allowed) || left < 32;             // uniform
+      const unsigned bits = word >> (4 * h);
+      if (some) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) k[j] = PAIRS ? fmaxf(__builtin_ldexpf(a.c, max(-200, min(120, -(ex[b] + ey[j])))), 0x1p-126f) : a.c;   // never 0: -inf times it stays
-      const int64_t x = x_first + 32 * b + m;
-      if constexpr (PASS != 2) {
-        // rows that do not count: beyond the last, or not allowed
-        const int left = a.n_y - y0;
-        if (left < 32) word[b] &= (1u << left) - 1u;
-        const bool some = (PASS == 0 && a.allowed) || left < 32;             // uniform
-        const unsigned bits = word[b] >> (4 * h);
-        if (some) {
+        for (int r = 0; r < 16; ++r) sc[r] = pick((unsigned)((int)(bits << (31 - (8 * (r >> 2) + (r & 3)))) >> 31), sc[r], -__builtin_inff());
+      }
+      float ztop;
+      if (PASS == 0 && a.first) {                        // uniform
+        // The largest and the second largest score of the lane's 16, the register's number in their lowest four bits (a score is
+        // as good as known without them): the rows behind them need not be looked for.
+        float v[16];
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sc[b][r] = pick((unsigned)((int)(bits << (31 - (8 * (r >> 2) + (r & 3)))) >> 31), sc[b][r], -__builtin_inff());
+        for (int r = 0; r < 16; ++r) {
+          v[r] = __uint_as_float((__float_as_uint(PAIRS ? sc[r] * k[r >> 2] : sc[r]) & ~15u) | r);
+          if (some) v[r] = pick((unsigned)((int)(bits << (31 - (8 * (r >> 2) + (r & 3)))) >> 31), v[r], SM_NO_REF);   // -inf would become a NaN
         }
-        float ztop;
-        if (PASS == 0 && a.first) {                        // uniform
-          // The largest and the second largest score of the lane's 16, the register's number in their lowest four bits (a score is
-          // as good as known without them): the rows behind them need not be looked for.
-          float v[16];
+        float one = fmaxf(v[0], v[1]), two = fminf(v[0], v[1]);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            v[r] = __uint_as_float((__float_as_uint(PAIRS ? sc[b][r] * k[r >> 2] : sc[b][r]) & ~15u) | r);
-            if (some) v[r] = pick((unsigned)((int)(bits << (31 - (8 * (r >> 2) + (r & 3)))) >> 31), v[r], SM_NO_REF);   // -inf would become a NaN
-          }
-          float one = fmaxf(v[0], v[1]), two = fminf(v[0], v[1]);
-#pragma unroll
-          for (int r = 2; r < 16; ++r) { two = __builtin_amdgcn_fmed3f(one, two, v[r]); one = fmaxf(one, v[r]); }
-          ztop = one;
-          second_max[b] = fmaxf(fmaxf(fminf(first_max[b], one), second_max[b]), two);
-          first_max[b] = fmaxf(first_max[b], one);
-        } else if constexpr (PAIRS) {
-          ztop = -__builtin_inff();
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float big = fmaxf(fmaxf(sc[b][4 * j], sc[b][4 * j + 1]), fmaxf(sc[b][4 * j + 2], sc[b][4 * j + 3])) * k[j];
-            ztop = fmaxf(ztop, SECOND ? big - (float)ey[j] : big);
-          }
-        } else {
-          ztop = sc[b][0];
-#pragma unroll
-          for (int r = 1; r < 16; ++r) ztop = fmaxf(ztop, sc[b][r]);
-        }
-        if (PASS == 0) ztop = __uint_as_float(__float_as_uint(ztop) & ~15u);   // the same reference with and without the numbers
-        if (!PAIRS) ztop *= k[0];
-        // the reference moves
-        if (__any(ztop > ref[b] + SM_ABOVE)) {
-          ztop = fmaxf(ztop, __shfl_xor(ztop, 32));        // both halves' weights meet in one product
-          const float to = fmaxf(ref[b], ztop - SM_BELOW), by = ref[b] - to, fct = __builtin_amdgcn_exp2f(by);
-          if (PASS == 0) {
-            const float l = lsum[b] + ltot[b];
-            asum[b] = l != 0.f ? fct * __builtin_fmaf(by, l, asum[b] + atot[b]) : 0.f;
-            atot[b] = 0.f;
-          }
-          lsum[b] *= fct; ltot[b] *= fct;
-          if constexpr (SECOND) rescale(fct);
-          ref[b] = to;
-        }
-        float l16 = 0.f, a16 = 0.f;
+        for (int r = 2; r < 16; ++r) { two = __builtin_amdgcn_fmed3f(one, two, v[r]); one = fmaxf(one, v[r]); }
+        ztop = one;
+        second_max = fmaxf(fmaxf(fminf(first_max, one), second_max), two);
+        first_max = fmaxf(first_max, one);
+      } else if constexpr (PAIRS) {
+        ztop = -__builtin_inff();
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float kg = SECOND && PAIRS ? ref[b] + (float)ey[j] : ref[b];
-          float sum4 = 0.f;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = 4 * j + e;
-            float z = __builtin_fmaf(sc[b][r], k[j], -kg);
-            if (PASS == 0 && some) z = pick((unsigned)((int)(bits << (31 - (8 * j + e))) >> 31), z, -1.0e30f);
-            w[r] = __builtin_amdgcn_exp2f(z);
-            sum4 += w[r];
-            if (PASS == 0) a16 = __builtin_fmaf(w[r], z, a16);
-          }
-          l16 += SECOND && PAIRS ? __builtin_ldexpf(sum4, ey[j]) : sum4;
-        }
-        lsum[b] += l16;
-        if (PASS == 0) asum[b] += a16;
-        if ((t & (SM_CHAIN - 1)) == SM_CHAIN - 1) {        // uniform
-          ltot[b] += lsum[b]; lsum[b] = 0.f;
-          if (PASS == 0) { atot[b] += asum[b]; asum[b] = 0.f; }
-        }
-        if (PASS == 0 && a.first) {
-          if (group_left == 1 || !has_next) {              // uniform
-            if (b == QB - 1) ++group;
-            const int64_t n = b == QB - 1 ? group : group + 1, row = (x * 2 + h) * a.half;     // n: groups finished
-            if constexpr (FEW) {                           // parts begin where it suits the table
-              if (xv[b]) { a.first[row + n - 1] = first_max[b]; a.second[row + n - 1] = second_max[b]; }
-            } else {
-              // four groups of a lane at a time: stores of 4 bytes a row apart cost as much as the products
-              first4[b] = (v4f){first4[b][1], first4[b][2], first4[b][3], first_max[b]};
-              second4[b] = (v4f){second4[b][1], second4[b][2], second4[b][3], second_max[b]};
-              if (xv[b]) {
-                if ((n & 3) == 0) {
-                  *reinterpret_cast<v4f*>(a.first + row + n - 4) = first4[b];
-                  *reinterpret_cast<v4f*>(a.second + row + n - 4) = second4[b];
-                } else if (!has_next) {                    // a part's last groups
-#pragma unroll
-                  for (int j = 1; j < 4; ++j) if (j >= 4 - (int)(n & 3)) { a.first[row + n - 4 + j] = first4[b][j]; a.second[row + n - 4 + j] = second4[b][j]; }
-                }
-              }
-            }
-            first_max[b] = second_max[b] = SM_NO_REF;
-          }
-        }
-        if constexpr (PASS == 1) {
-          // the answer's own row is left out of the product: its weight less one may cancel, and is applied in fp32 at the end
-          const int mine = tgt[b] - y0;
-          if (__any(mine >= 0 && mine < 32)) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) w[r] = mine == 8 * (r >> 2) + 4 * h + (r & 3) ? 0.f : w[r];
-          }
+          const float big = fmaxf(fmaxf(sc[4 * j], sc[4 * j + 1]), fmaxf(sc[4 * j + 2], sc[4 * j + 3])) * k[j];
+          ztop = fmaxf(ztop, SECOND ? big - (float)ey[j] : big);
         }
       } else {
-        // ---- weights p u of the tile's queries (rows) for the lane's table row
-        const int tm = rows_t[buf][m];
-        const bool hit = __any(tm >= x_first && tm < x_first + 32);   // the answer of one of the tile's queries is among the wave's rows
-        const unsigned neg = (unsigned)__builtin_amdgcn_readfirstlane((int)rows_neg[buf]);
-        float ztop = -__builtin_inff();
+        ztop = sc[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) ztop = fmaxf(ztop, sc[r]);
+      }
+      if (PASS == 0) ztop = __uint_as_float(__float_as_uint(ztop) & ~15u);   // the same reference with and without the numbers
+      if (!PAIRS) ztop *= k[0];
+      // the reference moves
+      if (__any(ztop > ref + SM_ABOVE)) {
+        ztop = fmaxf(ztop, __shfl_xor(ztop, 32));        // both halves' weights meet in one product
+        const float to = fmaxf(ref, ztop - SM_BELOW), by = ref - to, fct = __builtin_amdgcn_exp2f(by);
+        if (PASS == 0) {
+          const float l = lsum + ltot;
+          asum = l != 0.f ? fct * __builtin_fmaf(by, l, asum + atot) : 0.f;
+          atot = 0.f;
+        }
+        lsum *= fct; ltot *= fct;
+        if constexpr (SECOND) rescale(fct);
+        ref = to;
+      }
+      float l16 = 0.f, a16 = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float kg = SECOND && PAIRS ? ref + (float)ey[j] : ref;
+        float sum4 = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * j + e;
+          float z = __builtin_fmaf(sc[r], k[j], -kg);
+          if (PASS == 0 && some) z = pick((unsigned)((int)(bits << (31 - (8 * j + e))) >> 31), z, -1.0e30f);
+          w[r] = __builtin_amdgcn_exp2f(z);
+          sum4 += w[r];
+          if (PASS == 0) a16 = __builtin_fmaf(w[r], z, a16);
+        }
+        l16 += SECOND && PAIRS ? __builtin_ldexpf(sum4, ey[j]) : sum4;
+      }
+      lsum += l16;
+      if (PASS == 0) asum += a16;
+      if ((t & (SM_CHAIN - 1)) == SM_CHAIN - 1) {        // uniform
+        ltot += lsum; lsum = 0.f;
+        if (PASS == 0) { atot += asum; asum = 0.f; }
+      }
+      if (PASS == 0 && a.first) {
+        if (group_left == 1 || !has_next) {              // uniform
+          const int64_t n = ++group, row = (x * 2 + h) * a.half;
+          if constexpr (FEW) {                           // parts begin where it suits the table
+            if (xv) { a.first[row + n - 1] = first_max; a.second[row + n - 1] = second_max; }
+          } else {
+            // four groups of a lane at a time: stores of 4 bytes a row apart cost as much as the products
+            first4 = (v4f){first4[1], first4[2], first4[3], first_max};
+            second4 = (v4f){second4[1], second4[2], second4[3], second_max};
+            if (xv) {
+              if ((n & 3) == 0) {
+                *reinterpret_cast<v4f*>(a.first + row + n - 4) = first4;
+                *reinterpret_cast<v4f*>(a.second + row + n - 4) = second4;
+              } else if (!has_next) {                    // a part's last groups
+#pragma unroll
+                for (int j = 1; j < 4; ++j) if (j >= 4 - (int)(n & 3)) { a.first[row + n - 4 + j] = first4[j]; a.second[row + n - 4 + j] = second4[j]; }
+              }
+            }
+          }
+          first_max = second_max = SM_NO_REF;
+        }
+      }
+      if constexpr (PASS == 1) {
+        // the answer's own row is left out of the product: its weight less one may cancel, and is applied in fp32 at the end
+        const int mine = tgt - y0;
+        if (__any(mine >= 0 && mine < 32)) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) w[r] = mine == 8 * (r >> 2) + 4 * h + (r & 3) ? 0.f : w[r];
+        }
+      }
+    } else {
+      // ---- weights p u of the tile's queries (rows) for the lane's table row
+      const int tm = rows_t[buf][m];
+      const bool hit = __any(tm >= x_first && tm < x_first + 32);   // the answer of one of the tile's queries is among the wave's rows
+      const unsigned neg = (unsigned)__builtin_amdgcn_readfirstlane((int)rows_neg[buf]);
+      float ztop = -__builtin_inff();
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float4 f4 = *reinterpret_cast<const float4*>(&rows_f[buf][8 * j + 4 * h]);
+        const float fr[4] = {f4.x, f4.y, f4.z, f4.w};
+        float mr[4] = {0.f, 0.f, 0.f, 0.f};
+        if (PAIRS) {
+          const float4 m4 = *reinterpret_cast<const float4*>(&rows_m[buf][8 * j + 4 * h]);
+          mr[0] = m4.x; mr[1] = m4.y; mr[2] = m4.z; mr[3] = m4.w;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * j + e;
+          w[r] = PAIRS ? __builtin_fmaf(sc[r], k[j], -mr[e]) + (fr[e] - (float)ey[j]) : __builtin_fmaf(sc[r], k[j], fr[e]);
+          if (REFS) ztop = fmaxf(ztop, w[r]);
+        }
+        if (PAIRS) __builtin_amdgcn_sched_barrier(0);    // a block's statistics at a time: registers are full
+      }
+      if constexpr (REFS) {
+        if (__any(ztop > ref + SM_ABOVE)) {
+          ztop = fmaxf(ztop, __shfl_xor(ztop, 32));
+          const float to = fmaxf(ref, ztop - SM_BELOW), fct = __builtin_amdgcn_exp2f(ref - to);
+          rescale(fct);
+          ref = to;
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) w[r] = __builtin_amdgcn_exp2f(REFS ? w[r] - ref : w[r]);
+      if (neg) {                                         // uniform
+        const unsigned bits = neg >> (4 * h);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) w[r] = __uint_as_float(__float_as_uint(w[r]) ^ ((bits << (31 - (8 * (r >> 2) + (r & 3)))) & 0x80000000u));
+      }
+      if (hit) {                                         // an answer's own weight less u, before it is rounded
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float4 f4 = *reinterpret_cast<const float4*>(&rows_f[buf][8 * j + 4 * h]);
-          const float fr[4] = {f4.x, f4.y, f4.z, f4.w};
-          float mr[4] = {0.f, 0.f, 0.f, 0.f};
-          if (PAIRS) {
-            const float4 m4 = *reinterpret_cast<const float4*>(&rows_m[buf][8 * j + 4 * h]);
-            mr[0] = m4.x; mr[1] = m4.y; mr[2] = m4.z; mr[3] = m4.w;
-          }
+          const float4 u4 = *reinterpret_cast<const float4*>(&rows_u[buf][8 * j + 4 * h]);
+          const int4 t4 = *reinterpret_cast<const int4*>(&rows_t[buf][8 * j + 4 * h]);
+          const float u[4] = {u4.x, u4.y, u4.z, u4.w}, f = REFS ? __builtin_amdgcn_exp2f(-(ref + (float)ey[j])) : 1.f;
+          const int id[4] = {t4.x, t4.y, t4.z, t4.w};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = 4 * j + e;
-            w[r] = PAIRS ? __builtin_fmaf(sc[b][r], k[j], -mr[e]) + (fr[e] - (float)ey[j]) : __builtin_fmaf(sc[b][r], k[j], fr[e]);
-            if (REFS) ztop = fmaxf(ztop, w[r]);
-          }
-          if (PAIRS) __builtin_amdgcn_sched_barrier(0);    // a block's statistics at a time: registers are full
-        }
-        if constexpr (REFS) {
-          if (__any(ztop > ref[b] + SM_ABOVE)) {
-            ztop = fmaxf(ztop, __shfl_xor(ztop, 32));
-            const float to = fmaxf(ref[b], ztop - SM_BELOW), fct = __builtin_amdgcn_exp2f(ref[b] - to);
-            rescale(fct);
-            ref[b] = to;
-          }
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) w[r] = __builtin_amdgcn_exp2f(REFS ? w[r] - ref[b] : w[r]);
-        if (neg) {                                         // uniform
-          const unsigned bits = neg >> (4 * h);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) w[r] = __uint_as_float(__float_as_uint(w[r]) ^ ((bits << (31 - (8 * (r >> 2) + (r & 3)))) & 0x80000000u));
-        }
-        if (hit) {                                         // an answer's own weight less u, before it is rounded
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float4 u4 = *reinterpret_cast<const float4*>(&rows_u[buf][8 * j + 4 * h]);
-            const int4 t4 = *reinterpret_cast<const int4*>(&rows_t[buf][8 * j + 4 * h]);
-            const float u[4] = {u4.x, u4.y, u4.z, u4.w}, f = REFS ? __builtin_amdgcn_exp2f(-(ref[b] + (float)ey[j])) : 1.f;
-            const int id[4] = {t4.x, t4.y, t4.z, t4.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[4 * j + e] -= id[e] == (int)x ? u[e] * f : 0.f;
-          }
+          for (int e = 0; e < 4; ++e) w[4 * j + e] -= id[e] == (int)x ? u[e] * f : 0.f;
         }
       }
     }
@@ -632,30 +625,26 @@ k_softmax(SmArgs a) {
   }
 
   // ---- what the part leaves
+  if (PASS != 2) {                                       // the halves of a tile's rows share their reference
+    const float lw = lsum + ltot, aw = asum + atot;
+    const float l = lw + __shfl_xor(lw, 32), s = aw + __shfl_xor(aw, 32);
+    if (h == 0 && xv) a.stats[(size_t)part * a.n_x + x] = make_float4(ref, l, s, 0.f);
+  }
+  if constexpr (SECOND) {
+    float f = 1.f;                                       // twice the square root: the power itself may leave the floats' range
+    if (PASS == 2 && REFS) f = __builtin_amdgcn_exp2f(0.5f * ref);
+    unrolled<NO>([&](auto block) {
+      constexpr int c = block;
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-  for (int b = 0; b < QB; ++b) {
-    const int64_t x = x_first + 32 * b + m;
-    if (PASS != 2) {                                       // the halves of a tile's rows share their reference
-      const float lw = lsum[b] + ltot[b], aw = asum[b] + atot[b];
-      const float l = lw + __shfl_xor(lw, 32), s = aw + __shfl_xor(aw, 32);
-      if (h == 0 && xv[b]) a.stats[(size_t)part * a.n_x + x] = make_float4(ref[b], l, s, 0.f);
-    }
-    if constexpr (SECOND) {
-      float f = 1.f;                                       // twice the square root: the power itself may leave the floats' range
-      if (PASS == 2 && REFS) f = __builtin_amdgcn_exp2f(0.5f * ref[b]);
-      unrolled<NO>([&](auto block) {
-        constexpr int c = block;
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int col = 32 * c + 8 * j + 4 * h;
-          const float v[4] = {oacc[c][4 * j] * f * f, oacc[c][4 * j + 1] * f * f, oacc[c][4 * j + 2] * f * f, oacc[c][4 * j + 3] * f * f};
-          if (!xv[b] || col >= dim) continue;
-          if (PASS == 2 && a.out) store_cols<TYPE, 4>((T*)a.out + x * a.out_stride, col, dim, v);
-          else *reinterpret_cast<float4*>(a.O + ((size_t)part * a.n_x + x) * a.o_pitch + col) = make_float4(v[0], v[1], v[2], v[3]);
-        }
-      });
-    }
+      for (int j = 0; j < 4; ++j) {
+        const int col = 32 * c + 8 * j + 4 * h;
+        const float v[4] = {oacc[c][4 * j] * f * f, oacc[c][4 * j + 1] * f * f, oacc[c][4 * j + 2] * f * f, oacc[c][4 * j + 3] * f * f};
+        if (!xv || col >= dim) continue;
+        if (PASS == 2 && a.out) store_cols<TYPE, 4>((T*)a.out + x * a.out_stride, col, dim, v);
+        else *reinterpret_cast<float4*>(a.O + ((size_t)part * a.n_x + x) * a.o_pitch + col) = make_float4(v[0], v[1], v[2], v[3]);
+      }
+    });
   }
 }
 
@@ -682,7 +671,6 @@ k_softmax_pack(SmPackArgs a) {
       stage.zero = bad != 0u;
     }
   }
-  if (a.own_top && tid < SM_TY && t * SM_TY + tid < a.n) a.own_top[t * SM_TY + tid] = SM_NO_OWN;
   // units that no piece fills: up to the pitch
   for (int u = 2 * NK + (tid & 7); u < G::UNITS; u += 8) {
 #pragma unroll

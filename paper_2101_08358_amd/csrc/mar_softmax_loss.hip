@@ -11,7 +11,6 @@ struct LossArgs {
   const int32_t* targets; const float* weights;
   const float4* stats; const float* O;
   float *row_m, *row_f, *row_u;
-  const int* exps; int32_t* own_top;   // exponents of the queries' image (fp32)
   float *loss, *lse;
   void* grad; int64_t grad_stride;
 };
@@ -52,12 +51,6 @@ k_loss_rows(LossArgs a) {
       a.row_m[q] = u != 0.f ? m : 0.f;
       a.row_u[q] = us;
       const float lu = log2f(fabsf(us));
-      // largest of the row's own queries: the order in which they come does not matter.  A popular row's value is mostly there
-      // already (every query's atomic instead: 10,000 queries, a third of them with one answer, 66 us; none 22)
-      if (us != 0.f) {
-        const int key = own_key(lu - (TYPE == MAR_DTYPE_FP32 ? (float)a.exps[q >> 3] : 0.f));
-        if (__hip_atomic_load(a.own_top + t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < key) atomicMax(a.own_top + t, key);
-      }
       a.row_f[q] = us != 0.f ? lu - log2f(l) : -__builtin_inff();
     }
   }
@@ -114,13 +107,13 @@ template <int TYPE, int PASS>
 static void launch_nk(const SmArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)((a.units + 7) / 8 * 8)), block(256);
   switch (sm_nk(a.dim)) {
-    case 2: hipLaunchKernelGGL((k_softmax<TYPE, 2, PASS, SM_IMAGES, 1>), grid, block, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((k_softmax<TYPE, 4, PASS, SM_IMAGES, 1>), grid, block, 0, st, a); break;
-    case 7: hipLaunchKernelGGL((k_softmax<TYPE, 7, PASS, SM_IMAGES, 1>), grid, block, 0, st, a); break;
-    case 8: hipLaunchKernelGGL((k_softmax<TYPE, 8, PASS, SM_IMAGES, 1>), grid, block, 0, st, a); break;
-    case 12: hipLaunchKernelGGL((k_softmax<TYPE, 12, PASS, SM_IMAGES, 1>), grid, block, 0, st, a); break;
-    case 16: hipLaunchKernelGGL((k_softmax<TYPE, 16, PASS, SM_IMAGES, 1>), grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL((k_softmax<TYPE, 25, PASS, SM_IMAGES, 1>), grid, block, 0, st, a); break;
+    case 2: hipLaunchKernelGGL((k_softmax<TYPE, 2, PASS, SM_IMAGES>), grid, block, 0, st, a); break;
+    case 4: hipLaunchKernelGGL((k_softmax<TYPE, 4, PASS, SM_IMAGES>), grid, block, 0, st, a); break;
+    case 7: hipLaunchKernelGGL((k_softmax<TYPE, 7, PASS, SM_IMAGES>), grid, block, 0, st, a); break;
+    case 8: hipLaunchKernelGGL((k_softmax<TYPE, 8, PASS, SM_IMAGES>), grid, block, 0, st, a); break;
+    case 12: hipLaunchKernelGGL((k_softmax<TYPE, 12, PASS, SM_IMAGES>), grid, block, 0, st, a); break;
+    case 16: hipLaunchKernelGGL((k_softmax<TYPE, 16, PASS, SM_IMAGES>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((k_softmax<TYPE, 25, PASS, SM_IMAGES>), grid, block, 0, st, a); break;
   }
 }
 template <int PASS> static hipError_t launch_pass(int dtype, const SmArgs& a, hipStream_t st) {
@@ -132,12 +125,12 @@ template <int PASS> static hipError_t launch_pass(int dtype, const SmArgs& a, hi
 
 // ------------------------------------------------------------------------------------------ entry points -----
 // Workspace: images of both matrices, statistics, the queries' sums, what pass 2 reads per query, the parts of the table's gradient.
-struct LossLayout { size_t qtiles, qexps, wtiles, wexps, stats, O1, row_m, row_f, row_u, own_top, O2, bytes; SmPlan p1, p2; int32_t o_pitch; };
+struct LossLayout { size_t qtiles, qexps, wtiles, wexps, stats, O1, row_m, row_f, row_u, O2, bytes; SmPlan p1, p2; int32_t o_pitch; };
 
 static LossLayout loss_layout(const mar_softmax* p) {
   LossLayout L;
-  L.p1 = sm_plan(p->dtype, p->dim, 1, SM_IMAGES, 1, p->num_queries, p->num_rows, 1);
-  L.p2 = sm_plan(p->dtype, p->dim, 2, SM_IMAGES, 1, p->num_rows, p->num_queries, 1);
+  L.p1 = sm_plan(p->dtype, p->dim, 1, SM_IMAGES, p->num_queries, p->num_rows, 1);
+  L.p2 = sm_plan(p->dtype, p->dim, 2, SM_IMAGES, p->num_rows, p->num_queries, 1);
   L.o_pitch = (p->dim + 3) / 4 * 4;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
@@ -146,7 +139,7 @@ static LossLayout loss_layout(const mar_softmax* p) {
   L.wtiles = take(sm_image_bytes(p->dtype, p->dim, p->num_rows)); L.wexps = take(sm_exps_bytes(p->num_rows));
   L.stats = take((size_t)L.p1.parts * T * sizeof(float4));
   L.O1 = take((size_t)L.p1.parts * T * L.o_pitch * 4);
-  L.row_m = take(T * 4); L.row_f = take(T * 4); L.row_u = take(T * 4); L.own_top = take((size_t)p->num_rows * 4);
+  L.row_m = take(T * 4); L.row_f = take(T * 4); L.row_u = take(T * 4);
   L.O2 = take(L.p2.parts > 1 ? (size_t)L.p2.parts * p->num_rows * L.o_pitch * 4 : 0);
   L.bytes = at > 256 ? at : 256;
   return L;
@@ -183,9 +176,7 @@ extern "C" int mar_softmax_loss(const mar_softmax* p, const void* queries, const
   SmPackArgs k = {};
   k.dim = p->dim;
   k.src = table; k.stride = p->row_stride; k.n = (int32_t)p->num_rows; k.tiles = ws + L.wtiles; k.exps = (int*)(ws + L.wexps);
-  k.own_top = (int32_t*)(ws + L.own_top);
   hipError_t e = sm_pack(p->dtype, k, st);
-  k.own_top = nullptr;
   if (e == hipSuccess && p->num_queries > 0) {
     k.src = queries; k.stride = p->query_stride; k.n = p->num_queries; k.tiles = ws + L.qtiles; k.exps = (int*)(ws + L.qexps);
     k.ids = targets; k.weights = weights; k.num_ids = p->num_rows;
@@ -204,7 +195,6 @@ extern "C" int mar_softmax_loss(const mar_softmax* p, const void* queries, const
     r.n = p->num_queries; r.dim = p->dim; r.parts = L.p1.parts; r.o_pitch = L.o_pitch; r.rows = p->num_rows;
     r.scale = p->scale; r.unscale = (double)p->scale / (double)c;
     r.targets = targets; r.weights = weights; r.stats = a.stats; r.O = a.O;
-    r.exps = qimg.exps; r.own_top = (int32_t*)(ws + L.own_top);
     if (grad_table) { r.row_m = (float*)(ws + L.row_m); r.row_f = (float*)(ws + L.row_f); r.row_u = (float*)(ws + L.row_u); }
     r.loss = loss; r.lse = lse; r.grad = grad_queries; r.grad_stride = grad_query_stride;
     if (p->dtype == MAR_DTYPE_FP32) launch_rows<0>(r, st); else if (p->dtype == MAR_DTYPE_BF16) launch_rows<1>(r, st); else launch_rows<2>(r, st);
@@ -216,7 +206,6 @@ extern "C" int mar_softmax_loss(const mar_softmax* p, const void* queries, const
   a.yimg = qimg; a.n_y = p->num_queries;
   a.nstripes = L.p2.stripes; a.parts = L.p2.parts; a.tps = L.p2.tps; a.units = a.nstripes * a.parts;
   a.row_m = (const float*)(ws + L.row_m); a.row_f = (const float*)(ws + L.row_f); a.row_u = (const float*)(ws + L.row_u);
-  a.own_top = (const int32_t*)(ws + L.own_top);
   a.O = (float*)(ws + L.O2);
   if (L.p2.parts == 1) { a.out = grad_table; a.out_stride = grad_row_stride; }
   e = launch_pass<2>(p->dtype, a, st);
