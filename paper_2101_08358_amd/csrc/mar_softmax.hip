@@ -129,11 +129,12 @@ __device__ __forceinline__ void add_entries(TopList& top, const uint32_t (&key)[
     collect();
   }
   const int fresh = min(top.num, SM_CAP), all = fresh + old;
+  static_assert(MAR_MAX_TOP + SM_MARGIN + 8 <= 64 && NT >= 64, "a thread for every entry of the list");
   if (tid < old) top.cand[fresh + tid] = top.best[tid];
   if (tid >= old && tid < old + 8) top.cand[fresh + tid] = 0ull;
   __syncthreads();
-  if (tid < (all + 63) / 64 * 64) {                        // whole waves
-    const unsigned long long k = tid < all ? top.cand[tid] : ~0ull;
+  for (int e = tid; e < (all + 63) / 64 * 64; e += NT) {   // whole waves; there may be more entries than threads
+    const unsigned long long k = e < all ? top.cand[e] : ~0ull;
     int rank = 0;
     for (int j0 = 0; j0 < all; j0 += 8) {                  // eight reads in flight; entries from `all` on are 0
       unsigned long long w[8];
@@ -142,7 +143,7 @@ __device__ __forceinline__ void add_entries(TopList& top, const uint32_t (&key)[
 #pragma unroll
       for (int j = 0; j < 8; ++j) rank += w[j] > k ? 1 : 0;
     }
-    if (tid < all && rank < want) top.best[rank] = k;
+    if (e < all && rank < want) top.best[rank] = k;
   }
   if (tid == 0) top.have = min(all, want);
   __syncthreads();

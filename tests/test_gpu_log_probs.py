@@ -16,11 +16,16 @@ SIZES = ((1, 1, 1), (1, 31, 3), (5, 33, 8), (3, 100, 17), (130, 257, 50), (64, 1
          (65, 2000, 193), (300, 1025, 33))
 
 
-def check(q, w, tname, targets, allowed, top, scale, out):
+def check(q, w, tname, targets, allowed, top, scale, out, copies=None):
+    """copies: rows that are the same; the 64-bit product gives those of fp32 rows scores 5e-15 apart, by where they lie."""
     lp, en, ids, tp = out
     T, V = q.shape[0], w.shape[0]
     clean = torch.nan_to_num(w.double(), posinf=0.0, neginf=0.0).to(w.dtype) if allowed is not None else w
-    s = su.scores(q, clean, scale, allowed)
+    s = su.scores(q, clean, scale)
+    if copies is not None:
+        s[:, copies] = s[:, copies[:1]].clone()
+    if allowed is not None:
+        s = s.masked_fill(~allowed, -math.inf)
     empty = torch.isinf(s).all(1) if allowed is not None else torch.zeros(T, dtype=torch.bool, device=DEV)
     lse = torch.logsumexp(s, 1)
     delta, total = su.score_error(q, clean, scale), su.sum_error(V)
@@ -69,6 +74,18 @@ def test_against_64_bits(T, V, d, tname):
 
 
 @pytest.mark.parametrize("tname", ("fp32", "bf16", "fp16"))
+@pytest.mark.parametrize("T", (20, 100, 300))
+@pytest.mark.parametrize("d", (9, 50, 100, 128, 150, 250, 300, 400))
+def test_every_width_however_the_rows_come(d, T, tname):
+    """Few queries (a wave each), some (rows staged), many (images): every width there is a kernel for."""
+    g = su.gen(d + T)
+    dt, V = su.TYPES[tname][0], 4500
+    q, w = su.rows(g, T, d, dt), su.rows(g, V, d, dt, stride=d + 1, offset=1)
+    targets = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    check(q, w, tname, targets, None, 10, 1.0, su.run_log_probs(q, w, tname, targets, top=10))
+
+
+@pytest.mark.parametrize("tname", ("fp32", "bf16", "fp16"))
 @pytest.mark.parametrize("T,V,d,shared", ((1, 1, 4, 0), (9, 65, 20, 0), (140, 1000, 100, 0), (33, 3333, 75, 1), (515, 700, 64, 0), (4, 9000, 400, 0)))
 def test_masks(T, V, d, shared, tname):
     """Rows that do not count hold NaN and infinities; one query has no allowed row, one a single row."""
@@ -90,6 +107,23 @@ def test_masks(T, V, d, shared, tname):
     words = su.pack(allowed)
     out = su.run_log_probs(q, w, tname, targets, words, 0 if shared else words.shape[1], top=12)
     check(q, w, tname, targets, allowed.expand(T, V), 12, 1.0, out)
+
+
+@pytest.mark.parametrize("tname", ("fp32", "bf16", "fp16"))
+@pytest.mark.parametrize("T,V,d,top", ((2050, 3001, 40, 32), (2001, 700, 270, 32), (2300, 9000, 33, 20), (300, 20_000, 20, 32), (256, 70_000, 16, 32), (257, 140_000, 8, 32)))
+def test_many_best_rows_of_many_queries(T, V, d, top, tname):
+    """The most best rows there can be, where a wave, a workgroup of 256 and one of 1,024 look for them; half of the rows masked; half
+    of the rows close to one another, so that many groups reach the threshold."""
+    print("case", T, V, d, top, tname, flush=True)
+    g = su.gen(T + V)
+    dt = su.TYPES[tname][0]
+    q, w = su.rows(g, T, d, dt), su.rows(g, V, d, dt)
+    w[::2] = w[0]
+    copies = torch.arange(0, V, 2, device=DEV)
+    allowed = torch.rand((T, V), generator=g, device=DEV) < 0.5
+    words = su.pack(allowed)
+    check(q, w, tname, None, allowed, top, 1.0, su.run_log_probs(q, w, tname, None, words, words.shape[1], top=top), copies)
+    check(q, w, tname, None, None, top, 1.0, su.run_log_probs(q, w, tname, top=top), copies)
 
 
 def test_mask_rows_with_a_stride_of_their_own():

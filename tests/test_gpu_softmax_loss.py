@@ -11,7 +11,7 @@ DEV = su.DEV
 
 SIZES = ((1, 1, 1), (1, 31, 3), (5, 33, 8), (3, 100, 17), (130, 257, 50), (64, 1000, 75), (129, 2049, 100), (33, 5000, 128), (7, 700, 200),
          (40, 1000, 256), (70, 999, 400), (600, 300, 52), (1, 40_000, 100), (4097, 129, 64), (513, 4097, 96), (2, 3000, 129), (32, 64, 112),
-         (300, 1025, 33), (2000, 31, 400), (65, 2000, 193), (1500, 600, 384))
+         (300, 1025, 33), (2000, 31, 400), (65, 2000, 193), (1500, 600, 384), (400, 900, 150))
 
 
 def make(T, V, d, tname, odd, hot=False):
