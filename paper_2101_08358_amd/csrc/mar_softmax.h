@@ -54,7 +54,7 @@ struct SmPackArgs {
 };
 size_t sm_image_bytes(int dtype, int dim, int64_t rows);   // a multiple of 256
 size_t sm_exps_bytes(int64_t rows);
-hipError_t sm_pack(int dtype, const SmPackArgs& a, hipStream_t st);
+hipError_t sm_pack(int dtype, const SmPackArgs& first, const SmPackArgs& second, hipStream_t st);   // one width
 
 struct SmPlan { int32_t stripes, parts, tps, ntiles; };
 

@@ -422,20 +422,20 @@ template <int TYPE, int MODE> static void launch_nk(const SmArgs& a, hipStream_t
     default: if constexpr (MODE != SM_FEW) hipLaunchKernelGGL((k_softmax<TYPE, 25, 0, MODE>), grid, block, 0, st, a); break;
   }
 }
-template <int TYPE> static void launch_pack(const SmPackArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)(((int64_t)a.n + SM_TY - 1) / SM_TY)), block(256);
+template <int TYPE> static void launch_pack(const SmPackArgs& a, const SmPackArgs& b, hipStream_t st) {
+  const dim3 grid((unsigned)(((int64_t)a.n + SM_TY - 1) / SM_TY + ((int64_t)b.n + SM_TY - 1) / SM_TY)), block(256);
   switch (sm_nk(a.dim)) {
-    case 2: hipLaunchKernelGGL((k_softmax_pack<TYPE, 2>), grid, block, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((k_softmax_pack<TYPE, 4>), grid, block, 0, st, a); break;
-    case 7: hipLaunchKernelGGL((k_softmax_pack<TYPE, 7>), grid, block, 0, st, a); break;
-    case 8: hipLaunchKernelGGL((k_softmax_pack<TYPE, 8>), grid, block, 0, st, a); break;
-    case 12: hipLaunchKernelGGL((k_softmax_pack<TYPE, 12>), grid, block, 0, st, a); break;
-    case 16: hipLaunchKernelGGL((k_softmax_pack<TYPE, 16>), grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL((k_softmax_pack<TYPE, 25>), grid, block, 0, st, a); break;
+    case 2: hipLaunchKernelGGL((k_softmax_pack<TYPE, 2>), grid, block, 0, st, a, b); break;
+    case 4: hipLaunchKernelGGL((k_softmax_pack<TYPE, 4>), grid, block, 0, st, a, b); break;
+    case 7: hipLaunchKernelGGL((k_softmax_pack<TYPE, 7>), grid, block, 0, st, a, b); break;
+    case 8: hipLaunchKernelGGL((k_softmax_pack<TYPE, 8>), grid, block, 0, st, a, b); break;
+    case 12: hipLaunchKernelGGL((k_softmax_pack<TYPE, 12>), grid, block, 0, st, a, b); break;
+    case 16: hipLaunchKernelGGL((k_softmax_pack<TYPE, 16>), grid, block, 0, st, a, b); break;
+    default: hipLaunchKernelGGL((k_softmax_pack<TYPE, 25>), grid, block, 0, st, a, b); break;
   }
 }
-hipError_t sm_pack(int dtype, const SmPackArgs& a, hipStream_t st) {
-  if (dtype == MAR_DTYPE_FP32) launch_pack<0>(a, st); else if (dtype == MAR_DTYPE_BF16) launch_pack<1>(a, st); else launch_pack<2>(a, st);
+hipError_t sm_pack(int dtype, const SmPackArgs& a, const SmPackArgs& b, hipStream_t st) {
+  if (dtype == MAR_DTYPE_FP32) launch_pack<0>(a, b, st); else if (dtype == MAR_DTYPE_BF16) launch_pack<1>(a, b, st); else launch_pack<2>(a, b, st);
   return hipGetLastError();
 }
 size_t sm_image_bytes(int dtype, int dim, int64_t rows) {
@@ -505,12 +505,11 @@ extern "C" int mar_log_probs(const mar_softmax* p, const void* queries, const vo
   a.allowed = allowed; a.allowed_stride = allowed_stride;
   hipError_t e;
   if (L.mode == SM_IMAGES) {
-    SmPackArgs k = {};
-    k.dim = p->dim;
-    k.src = table; k.stride = p->row_stride; k.n = (int32_t)p->num_rows; k.tiles = (char*)workspace + L.wtiles; k.exps = (int*)((char*)workspace + L.wexps);
-    e = sm_pack(p->dtype, k, st);
+    SmPackArgs w = {}, k = {};
+    w.dim = k.dim = p->dim;
+    w.src = table; w.stride = p->row_stride; w.n = (int32_t)p->num_rows; w.tiles = (char*)workspace + L.wtiles; w.exps = (int*)((char*)workspace + L.wexps);
     k.src = queries; k.stride = p->query_stride; k.n = p->num_queries; k.tiles = (char*)workspace + L.qtiles; k.exps = (int*)((char*)workspace + L.qexps);
-    if (e == hipSuccess) e = sm_pack(p->dtype, k, st);
+    e = sm_pack(p->dtype, w, k, st);
     if (e != hipSuccess) { mar_set_error("image kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
     a.ximg = {(char*)workspace + L.qtiles, (const int*)((char*)workspace + L.qexps)};
     a.yimg = {(char*)workspace + L.wtiles, (const int*)((char*)workspace + L.wexps)};

@@ -288,29 +288,41 @@ k_softmax(SmArgs a) {
       if constexpr (PAIRS) xl[s] = *reinterpret_cast<const v8s*>(row + G::PLANE + ((32 * s + 16 * h) ^ swz));
     });
   }
-  if (PAIRS && !IMG) {
-    int big = 0;
-    unrolled<NK>([&](int s) {
-      float v[8];
-      load8<TYPE>(xrow, 16 * s + 8 * h, dim, v);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) big = max(big, finite_bits(v[e]));
-      if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
-    });
-    big = max(big, __shfl_xor(big, 32));
-    ex = sm_exponent(big);
-  }
-  if constexpr (!IMG) unrolled<NK>([&](auto step) {
+  if constexpr (!IMG && !PAIRS) unrolled<NK>([&](auto step) {
     constexpr int s = step;
-    if constexpr (PAIRS) {
-      float v[8];
-      load8<TYPE>(xrow, 16 * s + 8 * h, dim, v);
-      sm_parts8(v, __builtin_ldexpf(1.f, ex), xh[s], xl[s]);
-    } else {
-      xh[s] = __builtin_bit_cast(v8s, load8_bits(xrow, 16 * s + 8 * h, dim));
-    }
+    xh[s] = __builtin_bit_cast(v8s, load8_bits(xrow, 16 * s + 8 * h, dim));
     if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
   });
+  if constexpr (!IMG && PAIRS) {
+    // the row's exponent first, then its parts: from registers up to 128 columns (a second read is a memory latency), else read again
+    constexpr bool HOLD = NK <= 8;
+    float v[HOLD ? NK : 1][8];
+    int big = 0;
+    unrolled<NK>([&](auto step) {
+      constexpr int s = step, at = HOLD ? s : 0;
+      load8<TYPE>(xrow, 16 * s + 8 * h, dim, v[at]);
+      if (!HOLD) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) big = max(big, finite_bits(v[at][e]));
+        if (s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+      }
+    });
+    if constexpr (HOLD) {
+#pragma unroll
+      for (int s = 0; s < NK; ++s) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) big = max(big, finite_bits(v[s][e]));
+      }
+    }
+    big = max(big, __shfl_xor(big, 32));
+    ex = sm_exponent(big);
+    unrolled<NK>([&](auto step) {
+      constexpr int s = step, at = HOLD ? s : 0;
+      if (!HOLD) load8<TYPE>(xrow, 16 * s + 8 * h, dim, v[at]);
+      sm_parts8(v[at], __builtin_ldexpf(1.f, ex), xh[s], xl[s]);
+      if (!HOLD && s % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    });
+  }
 
   v16f oacc[NO];
 #pragma unroll
@@ -648,13 +660,15 @@ k_softmax(SmArgs a) {
   }
 }
 
-// Images: a workgroup a tile.
+// Images of two matrices: a workgroup a tile, the first matrix's first.
 template <int TYPE, int NK>
 __global__ void __launch_bounds__(256)
-k_softmax_pack(SmPackArgs a) {
+k_softmax_pack(SmPackArgs first, SmPackArgs second) {
   typedef SmGeom<TYPE, NK> G;
   typedef typename RowType<TYPE>::T T;
-  const int tid = threadIdx.x, t = blockIdx.x, y = min(t * SM_TY + (tid >> 3), a.n - 1);
+  const int tiles = (int)(((int64_t)first.n + SM_TY - 1) / SM_TY);
+  const SmPackArgs a = (int)blockIdx.x < tiles ? first : second;
+  const int tid = threadIdx.x, t = (int)blockIdx.x < tiles ? blockIdx.x : blockIdx.x - tiles, y = min(t * SM_TY + (tid >> 3), a.n - 1);
   char* const tile = a.tiles + (size_t)t * G::TILE;
   SmStage<TYPE, NK> stage;
   stage.begin((const T*)a.src, a.stride, a.n, t * SM_TY, tid);

@@ -173,15 +173,12 @@ extern "C" int mar_softmax_loss(const mar_softmax* p, const void* queries, const
   SmArgs a = {};
   a.dim = p->dim; a.c = c; a.o_pitch = L.o_pitch; a.targets = targets;
   const SmImage qimg = {ws + L.qtiles, (const int*)(ws + L.qexps)}, wimg = {ws + L.wtiles, (const int*)(ws + L.wexps)};
-  SmPackArgs k = {};
-  k.dim = p->dim;
-  k.src = table; k.stride = p->row_stride; k.n = (int32_t)p->num_rows; k.tiles = ws + L.wtiles; k.exps = (int*)(ws + L.wexps);
-  hipError_t e = sm_pack(p->dtype, k, st);
-  if (e == hipSuccess && p->num_queries > 0) {
-    k.src = queries; k.stride = p->query_stride; k.n = p->num_queries; k.tiles = ws + L.qtiles; k.exps = (int*)(ws + L.qexps);
-    k.ids = targets; k.weights = weights; k.num_ids = p->num_rows;
-    e = sm_pack(p->dtype, k, st);
-  }
+  SmPackArgs w = {}, k = {};
+  w.dim = k.dim = p->dim;
+  w.src = table; w.stride = p->row_stride; w.n = (int32_t)p->num_rows; w.tiles = ws + L.wtiles; w.exps = (int*)(ws + L.wexps);
+  k.src = queries; k.stride = p->query_stride; k.n = p->num_queries; k.tiles = ws + L.qtiles; k.exps = (int*)(ws + L.qexps);
+  k.ids = targets; k.weights = weights; k.num_ids = p->num_rows;
+  hipError_t e = sm_pack(p->dtype, w, k, st);
   if (e != hipSuccess) { mar_set_error("image kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
   if (p->num_queries > 0) {
     a.ximg = qimg; a.n_x = p->num_queries;
