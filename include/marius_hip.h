@@ -204,7 +204,8 @@ int mar_rank_metrics_static(const int32_t* ranks, int64_t n_ranks, const int32_t
 
 /*
  * Operators on whole tables.  They need no context: matrices are plain rows of any of the types below with any stride
- * (in elements, at least the row's width), aligned to their type alone.
+ * (in elements, at least the row's width), aligned to their type alone.  They run on the CURRENT device, to which hip_stream
+ * and all pointers must belong, keep nothing between calls, and may be captured into a HIP graph.
  */
 #define MAR_DTYPE_FP32 0
 #define MAR_DTYPE_BF16 1
@@ -227,8 +228,9 @@ int mar_dropout(const void* x, int64_t x_stride, int64_t rows, int32_t dim, int3
  * Softmax over ALL rows of a table: query i gives row j the score s_ij = scale * (query_i . row_j).  For the bilinear score
  * functions a query is the edge's operand of everything but the replaced endpoint (DistMult: theta_s * theta_r; ComplEx:
  * theta_s theta_r as [re | im] for destinations; Dot: theta_s) and the table is the node embeddings.
- * Products of bf16 and fp16 values are exact and summed in fp32; fp32 values are taken as the sum of two scaled f16
- * numbers (as accurate as fp32).  Scores that are not finite make the results of their query NaN or infinite.
+ * Products of bf16 and fp16 values are exact and summed in fp32; fp32 values are taken as the sum of two f16 numbers scaled
+ * by the largest of eight neighbouring rows (as accurate as fp32 down to rows 2^-17 of that, and of 2^-100).  Scores that are
+ * not finite make the results of their query NaN or infinite.
  */
 #define MAR_SOFTMAX_MAX_ROWS    ((int64_t)0x7fffff00)
 #define MAR_SOFTMAX_MAX_QUERIES 0x7fffff00
@@ -270,8 +272,8 @@ int mar_log_probs(const mar_softmax* problem, const void* queries, const void* t
  * losses:
  *     d queries_i = scale u_i (sum_j p_ij row_j - row_target),   d table_j = scale sum_i u_i (p_ij - [target_i = j]) query_i.
  *   targets  : device, [num_queries]; a query whose id lies outside the table has weight 0: loss and gradient are 0, and its
- *              values, finite or not, touch nothing else
- *   weights  : device, [num_queries] of either sign, or NULL: 1
+ *              values, finite or not, touch nothing else (its lse, where they are not, is that of a zero query)
+ *   weights  : device, [num_queries], finite, of either sign, or NULL: 1.  Below 2^-100 / scale in magnitude: 0
  *   loss, lse: device, out, [num_queries] floats, each may be NULL; lse is the log-sum-exp of every query
  *   grad_queries, grad_table : device, out, rows like the inputs' with their own strides, each may be NULL; overwritten.
  *              They must not overlap the inputs.

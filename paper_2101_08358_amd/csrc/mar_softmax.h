@@ -45,12 +45,15 @@ struct SmArgs {
   void* out; int64_t out_stride;   // pass 2 in one part: the gradient itself
 };
 
-// Lays rows out as images.  skip: where not NULL, a row whose weight (ids outside 0 .. num_ids - 1: 0) is 0 becomes zeros if it
-// holds values that are not finite.
+// A weight times the scale below this counts as 0: its inverse, and the weights' reference below it, stay floats.
+#define SM_LEAST_WEIGHT 0x1p-100f
+// Lays rows out as images.  ids: where not NULL, a row whose id lies outside 0 .. num_ids - 1 or whose weight is below least_weight
+// becomes zeros if it holds values that are not finite.
 struct SmPackArgs {
   const void* src; int64_t stride; int32_t n, dim;
   char* tiles; int* exps;
   const int32_t* ids; const float* weights; int64_t num_ids;
+  float least_weight;
 };
 size_t sm_image_bytes(int dtype, int dim, int64_t rows);   // a multiple of 256
 size_t sm_exps_bytes(int64_t rows);

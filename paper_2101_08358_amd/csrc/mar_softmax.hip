@@ -238,7 +238,7 @@ k_answer(AnswerArgs a) {
   __syncthreads();
   auto element = [&](int grp) { return (int64_t)(grp & 1) * a.half + (grp >> 1); };
   auto row_of = [&](int grp, int tile, int r) { return ((int64_t)(grp >> 1) * G + tile) * SM_TY + 8 * (r >> 2) + 4 * (grp & 1) + (r & 3); };
-  constexpr int NU = (MAR_MAX_DIM + 63) / 64;              // eights of columns that each of a row's eight lanes takes
+  constexpr int UL = TYPE == MAR_DTYPE_FP32 && NT > 256 ? 2 : 4;   // as registers allow
   double wmax = 0.0;                                       // largest squared norm of a row (fp32 squares may leave the floats' range)
   // Scores items [0, n): row(item) or -1, eight lanes an item.  The list is cut back to its best `want` after every BATCH items.
   auto score_items = [&](int n, auto row) {
@@ -250,12 +250,12 @@ k_answer(AnswerArgs a) {
         double dot = 0.0, n2 = 0.0;
         if (rw >= 0) {
           const T* wr = W + rw * a.w_stride;
-          for (int u0 = 0; 64 * u0 < a.dim; u0 += 4) {     // uniform; four loads in flight
-            float v[4][8];
+          for (int u0 = 0; 64 * u0 < a.dim; u0 += UL) {    // uniform; UL loads in flight
+            float v[UL][8];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) load8<TYPE>(wr, 8 * (8 * (u0 + u) + (tid & 7)), a.dim, v[u]);
+            for (int u = 0; u < UL; ++u) load8<TYPE>(wr, 8 * (8 * (u0 + u) + (tid & 7)), a.dim, v[u]);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
+            for (int u = 0; u < UL; ++u) {
               const int c = min(8 * (8 * (u0 + u) + (tid & 7)), QN - 8);     // values from dim on are zeros
               const float4 qa = *reinterpret_cast<const float4*>(qs + c), qb = *reinterpret_cast<const float4*>(qs + c + 4);
               const float qv[8] = {qa.x, qa.y, qa.z, qa.w, qb.x, qb.y, qb.z, qb.w};
@@ -368,7 +368,7 @@ SmPlan sm_plan(int dtype, int dim, int pass, int mode, int64_t n_x, int64_t n_y,
   int64_t best = INT64_MAX;
   r.parts = 1; r.tps = r.ntiles;
   const int most = pass == 0 ? 1024 : MAR_SOFTMAX_MAX_PARTS;
-  for (int k = 1; k <= most && k <= r.ntiles; ++k) {
+  for (int k = 1; k <= most && k <= r.ntiles; k += 1 + k / 32) {           // the host has some microseconds
     int64_t tps = (r.ntiles + k - 1) / k;
     tps = (tps + multiple - 1) / multiple * multiple;
     const int64_t parts = (r.ntiles + tps - 1) / tps;

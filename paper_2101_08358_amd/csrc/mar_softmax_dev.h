@@ -229,7 +229,8 @@ k_softmax(SmArgs a) {
       const bool neg = tid < SM_TY && q_u < 0.f;
       const unsigned long long all = __builtin_amdgcn_ballot_w64(neg);
       if (tid < SM_TY) {
-        rows_m[buf][tid] = q_m; rows_f[buf][tid] = PAIRS ? q_f : q_f - q_m; rows_u[buf][tid] = q_u; rows_t[buf][tid] = q_t;
+        rows_m[buf][tid] = q_m; rows_f[buf][tid] = PAIRS ? q_f : q_f - q_m; rows_u[buf][tid] = q_u;
+        rows_t[buf][tid] = q_u != 0.f ? q_t : -1;          // a row that no query counts for has no reference yet, and 0 times its inverse is no number
         if (tid == 0) rows_neg[buf] = (unsigned)all;
       }
     }
@@ -262,7 +263,7 @@ k_softmax(SmArgs a) {
         if (id[k] < first || id[k] >= first + 128) continue;
         const int64_t y = y0 + 256 * k + tid;
         const float u = a.row_u[y];
-        if (u != 0.f) atomicMax(&own[id[k] - (int)first], own_key(__builtin_amdgcn_logf(fabsf(u)) - (PAIRS ? (float)a.yimg.exps[y >> 3] : 0.f)));
+        if (u != 0.f) atomicMax(&own[id[k] - (int)first], own_key(log2f(fabsf(u)) - (PAIRS ? (float)a.yimg.exps[y >> 3] : 0.f)));
       }
     }
     __syncthreads();
@@ -676,7 +677,7 @@ k_softmax_pack(SmPackArgs first, SmPackArgs second) {
   for (int p = 0; p < G::NP; ++p) stage.load(p, a.dim, tid);
   if (a.ids) {
     const int id = a.ids[y];
-    if (id < 0 || id >= a.num_ids || (a.weights && a.weights[y] == 0.f)) {
+    if (id < 0 || id >= a.num_ids || (a.weights && fabsf(a.weights[y]) < a.least_weight)) {
       bool finite = true;
       for (int c = tid & 7; c < a.dim; c += 8) finite = finite && fabsf((float)stage.row[c]) <= 3.4028234663852886e38f;
       // the row's eight threads are neighbours, all of them here

@@ -36,7 +36,8 @@ k_loss_rows(LossArgs a) {
   if (wave == 0) fac[lane] = f;
   const int t = a.targets[q];
   const bool has = t >= 0 && t < a.rows;
-  const float u = has ? (a.weights ? a.weights[q] : 1.f) : 0.f, us = u * a.scale;
+  const float given = has ? (a.weights ? a.weights[q] : 1.f) : 0.f;
+  const float u = fabsf(given) < SM_LEAST_WEIGHT / a.scale ? 0.f : given, us = u * a.scale;
   const T* qr = (const T*)a.Q + q * a.q_stride;
   const T* wr = (const T*)a.W + (int64_t)(has ? t : 0) * a.w_stride;
   double dot = 0.0;
@@ -177,7 +178,7 @@ extern "C" int mar_softmax_loss(const mar_softmax* p, const void* queries, const
   w.dim = k.dim = p->dim;
   w.src = table; w.stride = p->row_stride; w.n = (int32_t)p->num_rows; w.tiles = ws + L.wtiles; w.exps = (int*)(ws + L.wexps);
   k.src = queries; k.stride = p->query_stride; k.n = p->num_queries; k.tiles = ws + L.qtiles; k.exps = (int*)(ws + L.qexps);
-  k.ids = targets; k.weights = weights; k.num_ids = p->num_rows;
+  k.ids = targets; k.weights = weights; k.num_ids = p->num_rows; k.least_weight = SM_LEAST_WEIGHT / p->scale;
   hipError_t e = sm_pack(p->dtype, w, k, st);
   if (e != hipSuccess) { mar_set_error("image kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
   if (p->num_queries > 0) {

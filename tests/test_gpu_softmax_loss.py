@@ -91,6 +91,38 @@ def test_weights_of_any_size():
         su.check_loss(su.run_loss(q, w, tname, targets, u), q, w, tname, targets, u, 1.0)
 
 
+def test_weights_that_count_as_none():
+    """Below 2^-100, the smallest floats among them: zero, also where the query is not finite."""
+    for tname in ("fp32", "bf16", "fp16"):
+        g, q, w, targets = make(130, 300, 48, tname, 0)
+        u = torch.ones(130, device=DEV)
+        u[::4], u[1::8] = 2.0 ** -149, -(2.0 ** -101)
+        clean = u.clone()
+        clean[u.abs() < 2.0 ** -100] = 0.0
+        q[4] = float("nan")
+        loss, _, gq, gw = su.run_loss(q, w, tname, targets, u)
+        assert not loss[clean == 0].any() and not gq[clean == 0].any()
+        q[4] = 0
+        su.check_loss((loss, None, gq, gw), q, w, tname, targets, clean, 1.0)
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each, enqueued one beside the other: the bits of either alone."""
+    cases = [make(900, 4000, 100, "fp32", 0)[1:], make(1200, 3000, 64, "bf16", 0)[1:]]
+    want = [su.run_loss(q, w, t, targets) for (q, w, targets), t in zip(cases, ("fp32", "bf16"))]
+    probs = [su.run_log_probs(q, w, t, targets, top=7) for (q, w, targets), t in zip(cases, ("fp32", "bf16"))]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        got = []
+        for st, (q, w, targets), t in zip(streams, cases, ("fp32", "bf16")):
+            with torch.cuda.stream(st):
+                got.append((su.run_loss(q, w, t, targets), su.run_log_probs(q, w, t, targets, top=7)))
+        torch.cuda.synchronize()
+        for (a, b), x, y in zip(got, want, probs):
+            assert all(torch.equal(m, n) for m, n in zip(a, x)) and all(torch.equal(m, n) for m, n in zip(b, y))
+
+
 @pytest.mark.parametrize("tname", ("fp32", "bf16", "fp16"))
 def test_large_scores(tname):
     g, q, w, targets = make(150, 2100, 100, tname, 0)
