@@ -448,12 +448,14 @@ template <int MODE> static hipError_t launch_stats(int dtype, const SmArgs& a, h
   return hipGetLastError();
 }
 
-// Threads per query: all that hide a query's own latency where there are few, a wave each where the device is full of them.
-// us a call, 64 / 256 / 1,024 threads: bf16, 120,000 rows of 100 columns, 128 queries 73 / 41 / 38, 512: 103 / 74 / 83, 1,000: 135 /
-// 115 / 142, 4,000: 356 / 351 / 469; 15,000 rows, 1,000 queries 56 / 55 / 82, 2,000: 66 / 80 / 139, 4,000: 125 / 157 / 283.
+// Threads per query: all that hide a query's own latency where there are few, and as many as leave all queries resident at once
+// (twelve waves a CU).  us a call, 64 / 128 / 256 / 1,024 threads: bf16, 120,000 rows of 100 columns, 128 queries 73 / - / 41 / 38,
+// 512: 103 / 80 / 70 / 83, 1,000: 135 / 108 / 111 / 142, 4,000: 356 / - / 351 / 469; 15,000 rows, 700 queries - / 40 / 37 / -, 1,000:
+// 56 / 44 / 54 / 82, 2,000: 66 / 67 / 75 / 139, 4,000: 125 / - / 157 / 283.
 template <int TYPE> static void launch_answer(const AnswerArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)a.n);
-  if (a.n >= 2000) hipLaunchKernelGGL((k_answer<TYPE, 64, 32>), grid, dim3(64), 0, st, a);
+  if (a.n > 1536) hipLaunchKernelGGL((k_answer<TYPE, 64, 32>), grid, dim3(64), 0, st, a);
+  else if (a.n > 768) hipLaunchKernelGGL((k_answer<TYPE, 128, 16>), grid, dim3(128), 0, st, a);
   else if (a.n > 256) hipLaunchKernelGGL((k_answer<TYPE, 256, 16>), grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((k_answer<TYPE, 1024, 16>), grid, dim3(1024), 0, st, a);
 }

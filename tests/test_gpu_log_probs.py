@@ -110,7 +110,7 @@ def test_masks(T, V, d, shared, tname):
 
 
 @pytest.mark.parametrize("tname", ("fp32", "bf16", "fp16"))
-@pytest.mark.parametrize("T,V,d,top", ((2050, 3001, 40, 32), (2001, 700, 270, 32), (2300, 9000, 33, 20), (300, 20_000, 20, 32), (256, 70_000, 16, 32), (257, 140_000, 8, 32)))
+@pytest.mark.parametrize("T,V,d,top", ((2050, 3001, 40, 32), (2001, 700, 270, 32), (2300, 9000, 33, 20), (1000, 2500, 60, 32), (300, 20_000, 20, 32), (256, 70_000, 16, 32), (257, 140_000, 8, 32)))
 def test_many_best_rows_of_many_queries(T, V, d, top, tname):
     """The most best rows there can be, where a wave, a workgroup of 256 and one of 1,024 look for them; half of the rows masked; half
     of the rows close to one another, so that many groups reach the threshold."""

@@ -14,7 +14,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 @pytest.mark.skipif(not (os.path.exists(HIPCC) or shutil.which("hipcc")), reason="hipcc not available")
 @pytest.mark.parametrize("name,kernels", (
     # three types; seven widths from images and from rows, six for few queries
-    ("mar_softmax", {"k_softmax": 3 * 20, "k_softmax_pack": 3 * 7, "k_answer": 3 * 3}),
+    ("mar_softmax", {"k_softmax": 3 * 20, "k_softmax_pack": 3 * 7, "k_answer": 3 * 4}),
     ("mar_softmax_loss", {"k_softmax": 3 * 7 * 2, "k_loss_rows": 3 * 2, "k_loss_table": 3}),
     ("mar_dropout", {"k_dropout": 3})))
 def test_no_scratch_memory(name, kernels, tmp_path):
