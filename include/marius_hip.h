@@ -273,14 +273,14 @@ int mar_log_probs(const mar_softmax* problem, const void* queries, const void* t
  *     d queries_i = scale u_i (sum_j p_ij row_j - row_target),   d table_j = scale sum_i u_i (p_ij - [target_i = j]) query_i.
  *   targets  : device, [num_queries]; a query whose id lies outside the table has weight 0: loss and gradient are 0, and its
  *              values, finite or not, touch nothing else (its lse, where they are not, is that of a zero query)
- *   weights  : device, [num_queries], finite, of either sign, or NULL: 1.  Below 2^-100 / scale in magnitude: 0
+ *   weights  : device, [num_queries], finite, of either sign, or NULL: 1.  Below 2^-100 in magnitude: 0
  *   loss, lse: device, out, [num_queries] floats, each may be NULL; lse is the log-sum-exp of every query
  *   grad_queries, grad_table : device, out, rows like the inputs' with their own strides, each may be NULL; overwritten.
  *              They must not overlap the inputs.
  *   workspace: device, >= mar_softmax_loss_workspace_bytes of the same problem, 256-byte aligned; calls that may overlap in
  *              time need one each
  * Sums are held in fp32 and formed in an order that depends on the problem alone (bit-reproducible); weights enter the
- * gradients' products in the operands' 16 bits (fp32: as pairs), an answer's own weight in fp32.
+ * gradients' products in the operands' 16 bits (fp32: as pairs), an answer's own weight in at least twice as many.
  */
 int mar_softmax_loss_workspace_bytes(const mar_softmax* problem, size_t* out_bytes);
 int mar_softmax_loss(const mar_softmax* problem, const void* queries, const void* table, const int32_t* targets, const float* weights,

