@@ -39,7 +39,7 @@ struct SmArgs {
   int64_t half;                    // groups a half, rounded up to a multiple of 4
   int32_t group_tiles;
   const uint32_t* allowed; int64_t allowed_stride;
-  const int32_t* targets;
+  const int32_t* targets; const float* weights;
   float* O; int32_t o_pitch;       // [parts][n_x][o_pitch]
   const float* row_m; const float* row_f; const float* row_u;   // pass 2: per query, see k_loss_rows
   void* out; int64_t out_stride;   // pass 2 in one part: the gradient itself

@@ -443,7 +443,7 @@ k_softmax(SmArgs a) {
     }
 
     float w[16];
-    unsigned own_bits = 0u;                                // PASS 2, 16-bit types: own weights whose remainder counts too
+    bool remainder = false;                                // PASS 2, 16-bit types: own weights' remainders count too
     // ---- t = sc k[r / 4]: scores in log2 units
     float k[4];
 #pragma unroll
@@ -591,23 +591,26 @@ k_softmax(SmArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) w[r] = __uint_as_float(__float_as_uint(w[r]) ^ ((bits << (31 - (8 * (r >> 2) + (r & 3)))) & 0x80000000u));
       }
-      if (hit) {                                         // an answer's own weight less u, before it is rounded
+      if (hit) {                                           // an answer's own weight less u, before it is rounded
+        float own_p = -1.f, f = 1.f;                       // largest own weight before, -1: none
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float4 u4 = *reinterpret_cast<const float4*>(&rows_u[buf][8 * j + 4 * h]);
           const int4 t4 = *reinterpret_cast<const int4*>(&rows_t[buf][8 * j + 4 * h]);
-          const float u[4] = {u4.x, u4.y, u4.z, u4.w}, f = REFS ? __builtin_amdgcn_exp2f(-(ref + (float)ey[j])) : 1.f;
+          const float u[4] = {u4.x, u4.y, u4.z, u4.w};
           const int id[4] = {t4.x, t4.y, t4.z, t4.w};
+          if (REFS) f = __builtin_amdgcn_exp2f(-(ref + (float)ey[j]));
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int r = 4 * j + e;
-            w[r] -= id[e] == (int)x ? u[e] * f : 0.f;
-            // what it loses to 16 bits makes a row's gradient as inexact as its own rounding does: taken along unless all are
-            // below a quarter of the largest (u = 1 and p of 2^-10, fp16 2^-13, or less).  Without: bf16, u of any size, the
-            // table's gradient off by 2.6e-3 of its norm where its own rounding is 1.7e-3
-            if (!PAIRS) own_bits |= id[e] == (int)x && fabsf(w[r] - sm_rounded<TYPE>(w[r])) > (TYPE == MAR_DTYPE_BF16 ? 0x1p-10f : 0x1p-13f) * fabsf(w[r]) ? 1u << r : 0u;
+            const bool mine = id[e] == (int)x;
+            if (!PAIRS) own_p = fmaxf(own_p, mine ? fabsf(w[r]) : -1.f);
+            w[r] -= mine ? u[e] * f : 0.f;
           }
         }
+        // What own weights lose to 16 bits makes a row's gradient as inexact as its own rounding does (bf16, u of any size: off by 2.6e-3
+        // of its norm where that is 1.7e-3).  A weight of p - 1 with p up to 2^-10 (fp16 2^-13) loses no more than a quarter of that.
+        if (!PAIRS) remainder = __any(a.weights ? own_p >= 0.f : own_p > (TYPE == MAR_DTYPE_BF16 ? 0x1p-10f : 0x1p-13f) * f);
       }
     }
     if (PASS == 0) group_left = group_left == 1 ? a.group_tiles : group_left - 1;
@@ -641,12 +644,22 @@ k_softmax(SmArgs a) {
         __builtin_amdgcn_sched_barrier(0);
       });
       if constexpr (!PAIRS && PASS == 2) {
-        unrolled<2>([&](auto half) {                       // 16 of the tile's queries each
+        if (remainder) unrolled<2>([&](auto half) {        // 16 of the tile's queries each
           constexpr int s = half;
-          if (__any((own_bits >> (8 * s) & 0xffu) != 0u)) {
-            float r8[8];
+          float r8[8];
+          bool some = false;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) r8[e] = own_bits >> (8 * s + e) & 1u ? w[8 * s + e] - sm_rounded<TYPE>(w[8 * s + e]) : 0.f;
+          for (int k = 0; k < 2; ++k) {
+            const int4 t4 = *reinterpret_cast<const int4*>(&rows_t[buf][16 * s + 8 * k + 4 * h]);
+            const int id[4] = {t4.x, t4.y, t4.z, t4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float v = w[8 * s + 4 * k + e];
+              r8[4 * k + e] = id[e] == (int)x ? v - sm_rounded<TYPE>(v) : 0.f;
+              some = some || id[e] == (int)x;
+            }
+          }
+          if (__any(some)) {
             const v8s rest = sm_round8<TYPE>(r8);
             unrolled<NO>([&](auto step) {
               constexpr int c = step;

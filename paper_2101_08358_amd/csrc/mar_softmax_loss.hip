@@ -179,7 +179,7 @@ extern "C" int mar_softmax_loss(const mar_softmax* p, const void* queries, const
   const float c = p->scale * 1.44269504088896341f;
 
   SmArgs a = {};
-  a.dim = p->dim; a.c = c; a.scale = p->scale; a.o_pitch = L.o_pitch; a.targets = targets;
+  a.dim = p->dim; a.c = c; a.scale = p->scale; a.o_pitch = L.o_pitch; a.targets = targets; a.weights = weights;
   const SmImage qimg = {ws + L.qtiles, (const int*)(ws + L.qexps)}, wimg = {ws + L.wtiles, (const int*)(ws + L.wexps)};
   SmPackArgs w = {}, k = {};
   w.dim = k.dim = p->dim;
