@@ -232,8 +232,8 @@ int mar_dropout(const void* x, int64_t x_stride, int64_t rows, int32_t dim, int3
  * by the largest of eight neighbouring rows (as accurate as fp32 down to rows 2^-17 of that, and of 2^-100).  Scores that are
  * not finite make the results of their query NaN or infinite.
  */
-#define MAR_SOFTMAX_MAX_ROWS    ((int64_t)0x7fffff00)
-#define MAR_SOFTMAX_MAX_QUERIES 0x7fffff00
+#define MAR_SOFTMAX_MAX_ROWS    ((int64_t)0x1fffff00)   /* launches hold fewer than 2^32 threads */
+#define MAR_SOFTMAX_MAX_QUERIES 0x3ffff00
 #define MAR_MAX_TOP 32
 typedef struct mar_softmax {
   int64_t num_rows;      /* rows of the table, 1 .. MAR_SOFTMAX_MAX_ROWS            */

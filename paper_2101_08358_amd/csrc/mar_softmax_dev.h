@@ -58,14 +58,12 @@ template <int TYPE, int NK> struct SmGeom {
 };
 
 // A tile on its way from memory to LDS: wave w takes rows 8 w .. 8 w + 7, eight threads to a row, a piece of 8 columns each at a time.
-// fp32: the exponent of a wave's eight rows is known once all pieces are there; the widest rows (SLIM) are loaded twice, for
-// their pieces and the sums of a pass do not fit the registers together.
+// fp32: the exponent of a wave's eight rows is known once all pieces are there.
 template <int TYPE, int NK> struct SmStage {
   typedef SmGeom<TYPE, NK> G;
   typedef typename RowType<TYPE>::T T;
-  static constexpr bool PAIRS = TYPE == MAR_DTYPE_FP32, SLIM = PAIRS && NK > 16;
-  static constexpr int KEEP = SLIM ? 1 : G::NP;
-  row_u4 r[KEEP][G::PLANES];
+  static constexpr bool PAIRS = TYPE == MAR_DTYPE_FP32;
+  row_u4 r[G::NP][G::PLANES];
   int big;
   bool zero;                                               // the row is taken as zeros whatever it holds
   const T* row;
@@ -91,11 +89,7 @@ template <int TYPE, int NK> struct SmStage {
       for (int j = 0; j < 4; ++j) big = max(big, finite_bits(__uint_as_float(v[k][j])));
     }
   }
-  // piece p is asked for; SLIM: the piece before it has arrived and is looked at
-  __device__ __forceinline__ void load(int p, int dim, int tid) {
-    if constexpr (SLIM) { if (p > 0) measure(r[0]); }
-    fetch(p, dim, tid, r[SLIM ? 0 : p]);
-  }
+  __device__ __forceinline__ void load(int p, int dim, int tid) { fetch(p, dim, tid, r[p]); }
   __device__ __forceinline__ void put(int p, char* tile, float scale, int dim, int tid, const row_u4 (&v)[G::PLANES]) const {
     const int u = (tid & 7) + 8 * p, y = tid >> 3;
     char* const to = tile + y * G::PA + ((16 * u) ^ (16 * sp_swizzle(G::UNITS, y)));
@@ -117,11 +111,8 @@ template <int TYPE, int NK> struct SmStage {
   __device__ __forceinline__ void store(char* tile, int* exps, int dim, int tid) {
     float scale = 1.f;
     if constexpr (PAIRS) {
-      if constexpr (SLIM) measure(r[0]);
-      else {
 #pragma unroll
-        for (int p = 0; p < G::NP; ++p) measure(r[p]);
-      }
+      for (int p = 0; p < G::NP; ++p) measure(r[p]);
       if (zero) big = 0;
 #pragma unroll
       for (int o = 32; o >= 1; o >>= 1) big = max(big, __shfl_xor(big, o));
@@ -129,18 +120,8 @@ template <int TYPE, int NK> struct SmStage {
       if ((tid & 63) == 0) exps[tid >> 6] = e;
       scale = __builtin_ldexpf(1.f, e);
     }
-    if constexpr (SLIM) {
 #pragma unroll
-      for (int p = 0; p < G::NP; ++p) {
-        row_u4 v[G::PLANES];
-        fetch(p, dim, tid, v);
-        put(p, tile, scale, dim, tid, v);
-        if (p % 2) __builtin_amdgcn_sched_barrier(0);      // two pieces in flight
-      }
-    } else {
-#pragma unroll
-      for (int p = 0; p < G::NP; ++p) put(p, tile, scale, dim, tid, r[p]);
-    }
+    for (int p = 0; p < G::NP; ++p) put(p, tile, scale, dim, tid, r[p]);
   }
 };
 

@@ -22,7 +22,8 @@ def test_struct_layout_matches_header():
 BAD_PROBLEMS = ((dict(dtype=3), -1), (dict(dtype=-1), -1), (dict(scale=0.0), -1), (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1),
                 (dict(scale=float("inf")), -1), (dict(num_rows=0), -2), (dict(num_rows=1 << 31), -2), (dict(num_queries=-1), -2), (dict(dim=0), -2),
                 (dict(dim=401, row_stride=500, query_stride=500), -2), (dict(row_stride=49), -1), (dict(query_stride=49), -1),
-                (dict(row_stride=1 << 31), -1), (dict(num_queries=0x7fffff01), -2))
+                (dict(row_stride=1 << 31), -1), (dict(num_queries=0x7fffff01), -2),
+                (dict(num_rows=0x1fffff01), -2), (dict(num_queries=0x3ffff01), -2))
 
 
 @pytest.mark.parametrize("bad,code", BAD_PROBLEMS)

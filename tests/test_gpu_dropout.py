@@ -107,3 +107,18 @@ def test_a_training_call_with_all_operators(tname):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((loss, lse, gq, gw, lp, en, ids, tp), want))
+
+
+def test_more_groups_than_a_launch_has_threads():
+    """Two groups a row in 2^31 - 1 rows: a launch's threads take two each, and offsets pass 32 bits."""
+    rows = 2 ** 31 - 1
+    free = torch.cuda.mem_get_info()[0]
+    if free < 60 << 30:
+        pytest.skip("needs 60 GB")
+    x = torch.ones(rows * 9, dtype=torch.bfloat16, device=DEV)
+    mar.mar_dropout(x, 9, rows, 9, mar.DTYPE_BF16, 0.5, 3, 4, x, 9)      # 2^32 - 2 groups, in place
+    torch.cuda.synchronize()
+    for first in (0, 2 ** 30 - 5, 2 ** 31 - 40):
+        got = x[first * 9:(first + 30) * 9].view(30, 9).float().cpu().numpy()
+        keep = keep_mask(30, 9, 0.5, 3, 4, first_row=first)
+        assert np.array_equal(got, keep * np.float32(2.0)), first
