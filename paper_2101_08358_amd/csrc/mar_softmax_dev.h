@@ -33,6 +33,16 @@ __device__ __forceinline__ void sm_parts8(const float (&v)[8], float scale, v8s&
   for (int e = 0; e < 8; ++e) { _Float16 a, b; sp_parts(v[e] * scale, a, b); h[e] = a; l[e] = b; }
   hi = __builtin_bit_cast(v8s, h); lo = __builtin_bit_cast(v8s, l);
 }
+// Largest of a wave's values, none of them negative, in all lanes: by turns within rows of 16 lanes, then over the four rows.
+__device__ __forceinline__ float wave_largest(float v) {
+  auto turned = [&](auto ctrl) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false)); };
+  v = fmaxf(v, turned(std::integral_constant<int, 0x128>{}));
+  v = fmaxf(v, turned(std::integral_constant<int, 0x124>{}));
+  v = fmaxf(v, turned(std::integral_constant<int, 0x122>{}));
+  v = fmaxf(v, turned(std::integral_constant<int, 0x121>{}));
+  auto lane = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
+  return fmaxf(fmaxf(lane(0), lane(16)), fmaxf(lane(32), lane(48)));
+}
 template <int TYPE> __device__ __forceinline__ v8s sm_round8(const float (&v)[8]) {
   if (TYPE == MAR_DTYPE_BF16) { v8b b; 
 #pragma unroll
@@ -64,13 +74,11 @@ template <int TYPE, int NK> struct SmStage {
   typedef typename RowType<TYPE>::T T;
   static constexpr bool PAIRS = TYPE == MAR_DTYPE_FP32;
   row_u4 r[G::NP][G::PLANES];
-  int big;
   bool zero;                                               // the row is taken as zeros whatever it holds
   const T* row;
   __device__ __forceinline__ void begin(const T* __restrict__ Y, int64_t stride, int n_y, int y0, int tid) {
     row = Y + (int64_t)min(y0 + (tid >> 3), n_y - 1) * stride;               // rows beyond the last are the last again
     zero = false;
-    big = 0;
   }
   __device__ __forceinline__ void fetch(int p, int dim, int tid, row_u4 (&v)[G::PLANES]) const {
     const int u = (tid & 7) + 8 * p;
@@ -81,47 +89,67 @@ template <int TYPE, int NK> struct SmStage {
       v[0] = take8_bits(row, 8 * u, dim);
     }
   }
-  // columns that a piece at the row's end holds besides its own belong to the same eight rows: they may be measured too
-  __device__ __forceinline__ void measure(const row_u4 (&v)[G::PLANES]) {
-#pragma unroll
-    for (int k = 0; k < G::PLANES; ++k) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) big = max(big, finite_bits(__uint_as_float(v[k][j])));
-    }
-  }
   __device__ __forceinline__ void load(int p, int dim, int tid) { fetch(p, dim, tid, r[p]); }
-  __device__ __forceinline__ void put(int p, char* tile, float scale, int dim, int tid, const row_u4 (&v)[G::PLANES]) const {
+  // FINITE: no value is infinite (a NaN makes its row's scores NaN either way)
+  template <bool FINITE> __device__ __forceinline__ void put(int p, char* tile, float scale, int dim, int tid) const {
     const int u = (tid & 7) + 8 * p, y = tid >> 3;
     char* const to = tile + y * G::PA + ((16 * u) ^ (16 * sp_swizzle(G::UNITS, y)));
     if (u >= 2 * NK) return;
     if constexpr (PAIRS) {
-      const row_u4 q[2] = {place4_floats(v[0], 8 * u, dim), place4_floats(v[1], 8 * u + 4, dim)};
+      const row_u4 q[2] = {place4_floats(r[p][0], 8 * u, dim), place4_floats(r[p][1], 8 * u + 4, dim)};
       float f[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) f[j] = zero ? 0.f : __uint_as_float(q[j >> 2][j & 3]);
       v8s hi, lo;
-      sm_parts8(f, scale, hi, lo);
+      if (FINITE) {
+        float neg1 = -1.f;
+        asm volatile("" : "+v"(neg1));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] *= scale;
+        split8<true>(f, neg1, hi, lo);
+      } else {
+        sm_parts8(f, scale, hi, lo);
+      }
       *reinterpret_cast<v8s*>(to) = hi;
       *reinterpret_cast<v8s*>(to + G::PLANE) = lo;
     } else {
-      *reinterpret_cast<row_u4*>(to) = zero ? (row_u4)(0u) : place8_bits(v[0], 8 * u, dim);
+      *reinterpret_cast<row_u4*>(to) = zero ? (row_u4)(0u) : place8_bits(r[p][0], 8 * u, dim);
     }
   }
   // exps: the exponents of the tile's four blocks of eight rows (fp32)
   __device__ __forceinline__ void store(char* tile, int* exps, int dim, int tid) {
     float scale = 1.f;
     if constexpr (PAIRS) {
+      // columns that a piece at the row's end holds besides its own belong to the same eight rows: they may be measured too
+      float big = 0.f;
 #pragma unroll
-      for (int p = 0; p < G::NP; ++p) measure(r[p]);
-      if (zero) big = 0;
+      for (int p = 0; p < G::NP; ++p) {
 #pragma unroll
-      for (int o = 32; o >= 1; o >>= 1) big = max(big, __shfl_xor(big, o));
-      const int e = sm_exponent(big);
+        for (int j = 0; j < 8; ++j) big = fmaxf(big, fabsf(__uint_as_float(r[p][j >> 2][j & 3])));
+      }
+      if (zero) big = 0.f;
+      int bits = __float_as_int(wave_largest(big));
+      const bool finite = bits < 0x7f800000;               // uniform
+      if (!finite) {                                       // an infinity: the exponent of what is finite
+        int most = 0;
+#pragma unroll
+        for (int p = 0; p < G::NP; ++p) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) most = max(most, finite_bits(__uint_as_float(r[p][j >> 2][j & 3])));
+        }
+        bits = __float_as_int(wave_largest(__int_as_float(zero ? 0 : most)));
+      }
+      const int e = sm_exponent(bits);
       if ((tid & 63) == 0) exps[tid >> 6] = e;
       scale = __builtin_ldexpf(1.f, e);
+      if (!finite) {
+#pragma unroll
+        for (int p = 0; p < G::NP; ++p) put<false>(p, tile, scale, dim, tid);
+        return;
+      }
     }
 #pragma unroll
-    for (int p = 0; p < G::NP; ++p) put(p, tile, scale, dim, tid, r[p]);
+    for (int p = 0; p < G::NP; ++p) put<true>(p, tile, scale, dim, tid);
   }
 };
 
