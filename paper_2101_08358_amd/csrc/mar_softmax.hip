@@ -7,10 +7,10 @@
 // scored again, 16 each: 4,096 queries, 131,072 rows of 400 columns, 16 best rows 367 us, for 1 GB of rows read at random.)
 #include "mar_softmax_dev.h"
 
-// Queries above which the matrices are laid out as images first, us rows / images: fp32, 120,000 rows of 100 columns, 128 queries 63 /
-// 70, 256: 89 / 83, 400: 137 / 109; 1,000,000 rows 284 / 417, 486 / 487, 845 / 671; bf16, 1,000,000 rows 241 / 257, 260 / 278,
-// 423 / 384; 100,000 rows of 400 columns 57 / 74, 78 / 91, 115 / 117.
-#define MAR_SOFTMAX_ROWS_MAX 256
+// Queries above which the matrices are laid out as images first, us rows / images: fp32, 120,000 rows of 100 columns, 128 queries 56 /
+// 62, 256: 79 / 78, 384: 105 / 92; 1,000,000 rows 256 / 411, 411 / 471, 581 / 585; 100,000 rows of 400 columns 123 / 143, 188 / 179,
+// 231 / 212.  bf16, 256, 384 and 512 queries: 47 / 51, 60 / 61, 67 / 69; 190 / 239, 254 / 297, 342 / 371; 70 / 83, 93 / 102, 111 / 114.
+constexpr int sm_rows_most(int type) { return type == MAR_DTYPE_FP32 ? 256 : 512; }
 #define SM_MARGIN 12              // groups, and rows, kept beyond the number asked for: what fp32 less four bits cannot tell apart
 
 struct AnswerArgs {
@@ -390,7 +390,7 @@ struct ProbsLayout { size_t stats, first, second, qtiles, qexps, wtiles, wexps, 
 static ProbsLayout probs_layout(const mar_softmax* p, int num_top) {
   ProbsLayout L;
   L.group_tiles = num_top ? group_tiles(p, num_top) : 1;
-  L.mode = p->num_queries <= 32 && sm_nk(p->dim) <= 16 ? SM_FEW : (p->num_queries > MAR_SOFTMAX_ROWS_MAX ? SM_IMAGES : SM_ROWS);
+  L.mode = p->num_queries <= 32 && sm_nk(p->dim) <= 16 ? SM_FEW : (p->num_queries > sm_rows_most(p->dtype) ? SM_IMAGES : SM_ROWS);
   // group maxima are stored four groups at a time, but for few queries
   L.p0 = sm_plan(p->dtype, p->dim, 0, L.mode, p->num_queries, p->num_rows, num_top ? (L.mode == SM_FEW ? 1 : 4) * L.group_tiles : 1);
   L.ngroups = num_top ? (L.p0.ntiles + L.group_tiles - 1) / L.group_tiles : 0;

@@ -74,7 +74,7 @@ def test_against_64_bits(T, V, d, tname):
 
 
 @pytest.mark.parametrize("tname", ("fp32", "bf16", "fp16"))
-@pytest.mark.parametrize("T", (20, 100, 300))
+@pytest.mark.parametrize("T", (20, 100, 300, 520))
 @pytest.mark.parametrize("d", (9, 50, 100, 128, 150, 250, 300, 400))
 def test_every_width_however_the_rows_come(d, T, tname):
     """Few queries (a wave each), some (rows staged), many (images): every width there is a kernel for."""
