@@ -230,7 +230,7 @@ int mar_dropout(const void* x, int64_t x_stride, int64_t rows, int32_t dim, int3
  * theta_s theta_r as [re | im] for destinations; Dot: theta_s) and the table is the node embeddings.
  * Products of bf16 and fp16 values are exact and summed in fp32; fp32 values are taken as the sum of two f16 numbers scaled
  * by the largest of eight neighbouring rows (as accurate as fp32 down to rows 2^-17 of that, and of 2^-100).  Scores that are
- * not finite make the results of their query NaN or infinite.
+ * not finite, or of 2^24 and more (whose own rounding is a factor e), make the results of their query NaN or infinite.
  */
 #define MAR_SOFTMAX_MAX_ROWS    ((int64_t)0x1fffff00)   /* launches hold fewer than 2^32 threads */
 #define MAR_SOFTMAX_MAX_QUERIES 0x3ffff00
@@ -272,7 +272,8 @@ int mar_log_probs(const mar_softmax* problem, const void* queries, const void* t
  * losses:
  *     d queries_i = scale u_i (sum_j p_ij row_j - row_target),   d table_j = scale sum_i u_i (p_ij - [target_i = j]) query_i.
  *   targets  : device, [num_queries]; a query whose id lies outside the table has weight 0: loss and gradient are 0, and its
- *              values, finite or not, touch nothing else (its lse, where they are not, is that of a zero query)
+ *              values, finite or not and of any size, touch nothing else.  Its lse is its own (of a zero query, where
+ *              they are not finite)
  *   weights  : device, [num_queries], finite, of either sign, or NULL: 1.  Below 2^-100 in magnitude: 0
  *   loss, lse: device, out, [num_queries] floats, each may be NULL; lse is the log-sum-exp of every query
  *   grad_queries, grad_table : device, out, rows like the inputs' with their own strides, each may be NULL; overwritten.

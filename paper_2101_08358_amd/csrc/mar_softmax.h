@@ -24,8 +24,9 @@ constexpr int sm_nk(int d) { return d <= 32 ? 2 : (d <= 64 ? 4 : (d <= 112 ? 7 :
 #define SM_NO_REF -3.0e38f        // reference of a row that has met no score yet
 
 // Tiles of rows as the passes read them ("images", [tiles][planes][32][pitch], units of a row in the order of sp_swizzle), with the
-// exponents of every eight rows: laid out once, they are copied into LDS as they lie, by every stripe.
-struct SmImage { const char* tiles; const int* exps; };
+// exponents of every eight rows (of those that count) and of every row: laid out once, they are copied into LDS as they lie, by every
+// stripe.
+struct SmImage { char* tiles; int *exps, *row_exps; };       // [tiles][4], [tiles][32]
 
 struct SmArgs {
   const void *X, *Y;               // stationary and streamed rows
@@ -48,15 +49,17 @@ struct SmArgs {
 // A weight below this counts as 0: its inverse, and the weights' reference below it, stay floats.
 #define SM_LEAST_WEIGHT 0x1p-100f
 // Lays rows out as images.  ids: where not NULL, a row whose id lies outside 0 .. num_ids - 1 or whose weight is below least_weight
-// becomes zeros if it holds values that are not finite.
+// does not count: its exponent is its own and no other row's, and it becomes zeros if it holds values that are not finite.
 struct SmPackArgs {
   const void* src; int64_t stride; int32_t n, dim;
-  char* tiles; int* exps;
+  SmImage to;
   const int32_t* ids; const float* weights; int64_t num_ids;
   float least_weight;
 };
+static inline int64_t sm_tiles(int64_t rows) { return (rows + SM_TY - 1) / SM_TY; }
 size_t sm_image_bytes(int dtype, int dim, int64_t rows);   // a multiple of 256
-size_t sm_exps_bytes(int64_t rows);
+static inline size_t sm_exps_bytes(int64_t rows) { return ((size_t)sm_tiles(rows) * (4 + SM_TY) * 4 + 255) / 256 * 256; }
+static inline SmImage sm_image(void* tiles, void* exps, int64_t rows) { return {(char*)tiles, (int*)exps, (int*)exps + 4 * sm_tiles(rows)}; }
 hipError_t sm_pack(int dtype, const SmPackArgs& first, const SmPackArgs& second, hipStream_t st);   // one width
 
 struct SmPlan { int32_t stripes, parts, tps, ntiles; };

@@ -442,7 +442,6 @@ size_t sm_image_bytes(int dtype, int dim, int64_t rows) {
   const int nk = sm_nk(dim);
   return (size_t)((rows + SM_TY - 1) / SM_TY) * SM_TY * sp_pitch(nk) * (dtype == MAR_DTYPE_FP32 ? 2 : 1);
 }
-size_t sm_exps_bytes(int64_t rows) { return ((size_t)((rows + SM_TY - 1) / SM_TY) * 16 + 255) / 256 * 256; }
 template <int MODE> static hipError_t launch_stats(int dtype, const SmArgs& a, hipStream_t st) {
   if (dtype == MAR_DTYPE_FP32) launch_nk<0, MODE>(a, st); else if (dtype == MAR_DTYPE_BF16) launch_nk<1, MODE>(a, st); else launch_nk<2, MODE>(a, st);
   return hipGetLastError();
@@ -507,14 +506,14 @@ extern "C" int mar_log_probs(const mar_softmax* p, const void* queries, const vo
   a.allowed = allowed; a.allowed_stride = allowed_stride;
   hipError_t e;
   if (L.mode == SM_IMAGES) {
+    a.ximg = sm_image((char*)workspace + L.qtiles, (char*)workspace + L.qexps, p->num_queries);
+    a.yimg = sm_image((char*)workspace + L.wtiles, (char*)workspace + L.wexps, p->num_rows);
     SmPackArgs w = {}, k = {};
     w.dim = k.dim = p->dim;
-    w.src = table; w.stride = p->row_stride; w.n = (int32_t)p->num_rows; w.tiles = (char*)workspace + L.wtiles; w.exps = (int*)((char*)workspace + L.wexps);
-    k.src = queries; k.stride = p->query_stride; k.n = p->num_queries; k.tiles = (char*)workspace + L.qtiles; k.exps = (int*)((char*)workspace + L.qexps);
+    w.src = table; w.stride = p->row_stride; w.n = (int32_t)p->num_rows; w.to = a.yimg;
+    k.src = queries; k.stride = p->query_stride; k.n = p->num_queries; k.to = a.ximg;
     e = sm_pack(p->dtype, w, k, st);
     if (e != hipSuccess) { mar_set_error("image kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
-    a.ximg = {(char*)workspace + L.qtiles, (const int*)((char*)workspace + L.qexps)};
-    a.yimg = {(char*)workspace + L.wtiles, (const int*)((char*)workspace + L.wexps)};
     e = launch_stats<SM_IMAGES>(p->dtype, a, st);
   } else {
     e = L.mode == SM_FEW ? launch_stats<SM_FEW>(p->dtype, a, st) : launch_stats<SM_ROWS>(p->dtype, a, st);

@@ -33,13 +33,18 @@ __device__ __forceinline__ void sm_parts8(const float (&v)[8], float scale, v8s&
   for (int e = 0; e < 8; ++e) { _Float16 a, b; sp_parts(v[e] * scale, a, b); h[e] = a; l[e] = b; }
   hi = __builtin_bit_cast(v8s, h); lo = __builtin_bit_cast(v8s, l);
 }
-// Largest of a wave's values, none of them negative, in all lanes: by turns within rows of 16 lanes, then over the four rows.
-__device__ __forceinline__ float wave_largest(float v) {
-  auto turned = [&](auto ctrl) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, false)); };
-  v = fmaxf(v, turned(std::integral_constant<int, 0x128>{}));
-  v = fmaxf(v, turned(std::integral_constant<int, 0x124>{}));
-  v = fmaxf(v, turned(std::integral_constant<int, 0x122>{}));
-  v = fmaxf(v, turned(std::integral_constant<int, 0x121>{}));
+// Largest value of eight neighbouring lanes (a staged row's), none negative, in all of them.
+template <int CTRL> __device__ __forceinline__ float sm_turned(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float row_largest(float v) {
+  v = fmaxf(v, sm_turned<0xB1>(v));                        // lane ^ 1, lane ^ 2 of four, then the eight mirrored
+  v = fmaxf(v, sm_turned<0x4E>(v));
+  return fmaxf(v, sm_turned<0x141>(v));
+}
+// Largest of a wave's eight rows' values, each the same in its eight lanes.
+__device__ __forceinline__ float rows_largest(float v) {
+  v = fmaxf(v, sm_turned<0x128>(v));                       // the other row of 16 lanes
   auto lane = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
   return fmaxf(fmaxf(lane(0), lane(16)), fmaxf(lane(32), lane(48)));
 }
@@ -75,10 +80,11 @@ template <int TYPE, int NK> struct SmStage {
   static constexpr bool PAIRS = TYPE == MAR_DTYPE_FP32;
   row_u4 r[G::NP][G::PLANES];
   bool zero;                                               // the row is taken as zeros whatever it holds
+  bool apart;                                              // it has an exponent of its own, and the eight rows' does without it
   const T* row;
   __device__ __forceinline__ void begin(const T* __restrict__ Y, int64_t stride, int n_y, int y0, int tid) {
     row = Y + (int64_t)min(y0 + (tid >> 3), n_y - 1) * stride;               // rows beyond the last are the last again
-    zero = false;
+    zero = apart = false;
   }
   __device__ __forceinline__ void fetch(int p, int dim, int tid, row_u4 (&v)[G::PLANES]) const {
     const int u = (tid & 7) + 8 * p;
@@ -116,11 +122,11 @@ template <int TYPE, int NK> struct SmStage {
       *reinterpret_cast<row_u4*>(to) = zero ? (row_u4)(0u) : place8_bits(r[p][0], 8 * u, dim);
     }
   }
-  // exps: the exponents of the tile's four blocks of eight rows (fp32)
-  __device__ __forceinline__ void store(char* tile, int* exps, int dim, int tid) {
+  // fp32: exps: the exponents of the tile's four blocks of eight rows; row_exps, where not NULL: of every row
+  __device__ __forceinline__ void store(char* tile, int* exps, int* row_exps, int dim, int tid) {
     float scale = 1.f;
     if constexpr (PAIRS) {
-      // columns that a piece at the row's end holds besides its own belong to the same eight rows: they may be measured too
+      // columns that a piece at the row's end holds besides its own belong to the same row: they may be measured too
       float big = 0.f;
 #pragma unroll
       for (int p = 0; p < G::NP; ++p) {
@@ -128,8 +134,7 @@ template <int TYPE, int NK> struct SmStage {
         for (int j = 0; j < 8; ++j) big = fmaxf(big, fabsf(__uint_as_float(r[p][j >> 2][j & 3])));
       }
       if (zero) big = 0.f;
-      int bits = __float_as_int(wave_largest(big));
-      const bool finite = bits < 0x7f800000;               // uniform
+      const bool finite = !__any(__float_as_int(big) >= 0x7f800000);       // uniform
       if (!finite) {                                       // an infinity: the exponent of what is finite
         int most = 0;
 #pragma unroll
@@ -137,10 +142,13 @@ template <int TYPE, int NK> struct SmStage {
 #pragma unroll
           for (int j = 0; j < 8; ++j) most = max(most, finite_bits(__uint_as_float(r[p][j >> 2][j & 3])));
         }
-        bits = __float_as_int(wave_largest(__int_as_float(zero ? 0 : most)));
+        big = __int_as_float(zero ? 0 : most);
       }
-      const int e = sm_exponent(bits);
-      if ((tid & 63) == 0) exps[tid >> 6] = e;
+      big = row_largest(big);
+      const int block = sm_exponent(__float_as_int(rows_largest(apart ? 0.f : big)));
+      const int e = apart ? sm_exponent(__float_as_int(big)) : block;
+      if ((tid & 63) == 0) exps[tid >> 6] = block;
+      if (row_exps && (tid & 7) == 0) row_exps[tid >> 3] = e;
       scale = __builtin_ldexpf(1.f, e);
       if (!finite) {
 #pragma unroll
@@ -292,7 +300,7 @@ k_softmax(SmArgs a) {
     const int64_t xt = min(x_first / SM_TY, (int64_t)(a.n_x - 1) / SM_TY);         // the wave's rows are a tile
     const char* const row = a.ximg.tiles + xt * G::TILE + m * G::PA;
     const int swz = 16 * sp_swizzle(G::UNITS, m);
-    if (PAIRS) ex = a.ximg.exps[4 * xt + (m >> 3)];
+    if (PAIRS) ex = a.ximg.row_exps[32 * xt + m];
     unrolled<NK>([&](auto step) {
       constexpr int s = step;
       xh[s] = *reinterpret_cast<const v8s*>(row + ((32 * s + 16 * h) ^ swz));
@@ -376,7 +384,7 @@ k_softmax(SmArgs a) {
       store_rows(buf);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     } else {
-      unrolled<NSG>([&](auto k) { constexpr int w = k; stage[w].store(smem + buf * G::TILE, exps[buf], dim, 64 * w + tid); });
+      unrolled<NSG>([&](auto k) { constexpr int w = k; stage[w].store(smem + buf * G::TILE, exps[buf], nullptr, dim, 64 * w + tid); });
     }
   };
   if (!IMG) __syncthreads();                               // the zeros are there
@@ -719,7 +727,7 @@ k_softmax_pack(SmPackArgs first, SmPackArgs second) {
   const int tiles = (int)(((int64_t)first.n + SM_TY - 1) / SM_TY);
   const SmPackArgs a = (int)blockIdx.x < tiles ? first : second;
   const int tid = threadIdx.x, t = (int)blockIdx.x < tiles ? blockIdx.x : blockIdx.x - tiles, y = min(t * SM_TY + (tid >> 3), a.n - 1);
-  char* const tile = a.tiles + (size_t)t * G::TILE;
+  char* const tile = a.to.tiles + (size_t)t * G::TILE;
   SmStage<TYPE, NK> stage;
   stage.begin((const T*)a.src, a.stride, a.n, t * SM_TY, tid);
 #pragma unroll
@@ -733,6 +741,7 @@ k_softmax_pack(SmPackArgs first, SmPackArgs second) {
       unsigned bad = finite ? 0u : 1u;
       bad |= __shfl_xor(bad, 1); bad |= __shfl_xor(bad, 2); bad |= __shfl_xor(bad, 4);
       stage.zero = bad != 0u;
+      stage.apart = true;
     }
   }
   // units that no piece fills: up to the pitch
@@ -741,7 +750,7 @@ k_softmax_pack(SmPackArgs first, SmPackArgs second) {
     for (int k = 0; k < G::PLANES; ++k)
       *reinterpret_cast<row_u4*>(tile + k * G::PLANE + (tid >> 3) * G::PA + ((16 * u) ^ (16 * sp_swizzle(G::UNITS, tid >> 3)))) = (row_u4)(0u);
   }
-  stage.store(tile, a.exps ? a.exps + 4 * (size_t)t : nullptr, a.dim, tid);
+  stage.store(tile, a.to.exps + 4 * (size_t)t, a.to.row_exps + SM_TY * (size_t)t, a.dim, tid);
 }
 
 // Natural logarithm of a sum of weights: the exponent apart from the mantissa, whose logarithm keeps its bits.

@@ -180,11 +180,11 @@ extern "C" int mar_softmax_loss(const mar_softmax* p, const void* queries, const
 
   SmArgs a = {};
   a.dim = p->dim; a.c = c; a.scale = p->scale; a.o_pitch = L.o_pitch; a.targets = targets; a.weights = weights;
-  const SmImage qimg = {ws + L.qtiles, (const int*)(ws + L.qexps)}, wimg = {ws + L.wtiles, (const int*)(ws + L.wexps)};
+  const SmImage qimg = sm_image(ws + L.qtiles, ws + L.qexps, p->num_queries), wimg = sm_image(ws + L.wtiles, ws + L.wexps, p->num_rows);
   SmPackArgs w = {}, k = {};
   w.dim = k.dim = p->dim;
-  w.src = table; w.stride = p->row_stride; w.n = (int32_t)p->num_rows; w.tiles = ws + L.wtiles; w.exps = (int*)(ws + L.wexps);
-  k.src = queries; k.stride = p->query_stride; k.n = p->num_queries; k.tiles = ws + L.qtiles; k.exps = (int*)(ws + L.qexps);
+  w.src = table; w.stride = p->row_stride; w.n = (int32_t)p->num_rows; w.to = wimg;
+  k.src = queries; k.stride = p->query_stride; k.n = p->num_queries; k.to = qimg;
   k.ids = targets; k.weights = weights; k.num_ids = p->num_rows; k.least_weight = SM_LEAST_WEIGHT;
   hipError_t e = sm_pack(p->dtype, w, k, st);
   if (e != hipSuccess) { mar_set_error("image kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }

@@ -1,0 +1,51 @@
+"""GPU parity of mar_softmax_loss with 64 bits where values are out of the ordinary: queries that do not count, of any size, beside
+others."""
+import pytest
+import torch
+
+import softmax_util as su
+
+pytestmark = pytest.mark.gpu
+DEV = su.DEV
+LARGE = {"fp32": (1e5, 1e8, 1e12, 1e30, 3.0e38), "bf16": (1e5, 1e8, 1e30), "fp16": (6e4,)}
+
+
+def make(T, V, d, tname, std=0.3):
+    g = su.gen(T * 11 + V + d)
+    dt = su.TYPES[tname][0]
+    q, w = su.rows(g, T, d, dt, std), su.rows(g, V, d, dt, std)
+    return g, q, w, torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+
+
+def signs(g, n, d):
+    return torch.randint(0, 2, (n, d), generator=g, device=DEV).float() * 2 - 1
+
+
+@pytest.mark.parametrize("tname,value", [(t, v) for t in LARGE for v in LARGE[t]])
+@pytest.mark.parametrize("T,V,d", ((300, 777, 60), (1000, 5000, 20), (140, 900, 300)))
+def test_large_queries_that_do_not_count_touch_no_other(T, V, d, tname, value):
+    """Finite values of any size in queries without an answer and in queries without weight; several in a block of eight."""
+    print("case", T, V, d, tname, value, flush=True)
+    g, q, w, targets = make(T, V, d, tname)
+    weights = torch.rand(T, generator=g, device=DEV) + 0.5
+    targets[::5] = -1
+    targets[3::50] = V
+    weights[4::16] = 0.0
+    weights[6::48] = 2.0 ** -120
+    none = (targets < 0) | (targets >= V) | (weights < 2.0 ** -100)
+    n = int(none.sum())
+    q[none] = (signs(g, n, d) * value * (0.5 + 0.5 * torch.rand((n, d), generator=g, device=DEV))).to(q.dtype)
+    assert torch.isfinite(q).all()
+    out = su.run_loss(q, w, tname, targets, weights)
+    assert (out[0][none] == 0).all() and (out[2][none] == 0).all()
+    clean, kept = q.clone(), ~none
+    clean[none] = 0
+    u = torch.where(none, torch.zeros_like(weights), weights)
+    su.check_loss((out[0], None, out[2], out[3]), clean, w, tname, targets, u, 1.0)
+    ref = torch.logsumexp(su.scores(q[kept], w, 1.0), 1)
+    err = (out[1].double()[kept] - ref).abs()
+    assert (err <= su.score_error(q[kept], w, 1.0) + su.sum_error(V) + ref.abs() * 2.0 ** -23).all(), float(err.max())
+    if value <= 1e5:                                         # their own scores stay below 2^23
+        ref = torch.logsumexp(su.scores(q[none], w, 1.0), 1)
+        err = (out[1].double()[none] - ref).abs()
+        assert (err <= su.score_error(q[none], w, 1.0) + su.sum_error(V) + ref.abs() * 2.0 ** -23).all(), float(err.max())
