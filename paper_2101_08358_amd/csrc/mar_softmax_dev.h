@@ -204,7 +204,8 @@ k_softmax(SmArgs a) {
   // pass 2, per query of a tile: f = log2(|u| / sum of its weights), m its reference (16-bit types: f - m and nothing)
   __shared__ __attribute__((aligned(16))) float rows_m[2][SM_TY], rows_f[2][SM_TY], rows_u[2][SM_TY];
   __shared__ __attribute__((aligned(16))) int rows_t[2][SM_TY];
-  __shared__ unsigned rows_neg[2];                         // queries with a negative u
+  __shared__ unsigned rows_neg[2], rows_none[2];           // queries with a negative u; without weight (or beyond the last)
+  __shared__ __attribute__((aligned(16))) short rows_keep[2][SM_TY];       // 0 for those without, else all ones
   __shared__ int own[PASS == 2 && REFS ? 128 : 1];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -244,12 +245,12 @@ k_softmax(SmArgs a) {
   };
   auto store_rows = [&](int buf) {
     if (PASS == 2 && tid < 64) {
-      const bool neg = tid < SM_TY && q_u < 0.f;
-      const unsigned long long all = __builtin_amdgcn_ballot_w64(neg);
+      const unsigned neg = (unsigned)__builtin_amdgcn_ballot_w64(q_u < 0.f), none = (unsigned)__builtin_amdgcn_ballot_w64(q_u == 0.f);
       if (tid < SM_TY) {
         rows_m[buf][tid] = q_m; rows_f[buf][tid] = PAIRS ? q_f : q_f - q_m; rows_u[buf][tid] = q_u;
         rows_t[buf][tid] = q_u != 0.f ? q_t : -1;          // a row that no query counts for has no reference yet, and 0 times its inverse is no number
-        if (tid == 0) rows_neg[buf] = (unsigned)all;
+        rows_keep[buf][tid] = q_u == 0.f ? 0 : -1;
+        if (tid == 0) { rows_neg[buf] = neg; rows_none[buf] = none; }
       }
     }
   };
@@ -644,6 +645,15 @@ k_softmax(SmArgs a) {
           split8<true>(p8, neg1, ph[s], pl[s]);
         } else {
           ph[s] = sm_round8<TYPE>(p8);
+        }
+      }
+      // no weight is none whatever the score: an infinite one plus log2 0 is no number
+      if (PASS == 2 && __builtin_amdgcn_readfirstlane((int)rows_none[buf])) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const v8s keep = join8(*reinterpret_cast<const v4s*>(&rows_keep[buf][16 * s + 4 * h]), *reinterpret_cast<const v4s*>(&rows_keep[buf][16 * s + 8 + 4 * h]));
+          ph[s] &= keep;
+          if (PAIRS) pl[s] &= keep;
         }
       }
       __builtin_amdgcn_sched_barrier(0);

@@ -1,5 +1,5 @@
 """GPU parity of mar_softmax_loss with 64 bits where values are out of the ordinary: queries that do not count, of any size, beside
-others."""
+others and beside rows that are not finite."""
 import pytest
 import torch
 
@@ -7,7 +7,7 @@ import softmax_util as su
 
 pytestmark = pytest.mark.gpu
 DEV = su.DEV
-LARGE = {"fp32": (1e5, 1e8, 1e12, 1e30, 3.0e38), "bf16": (1e5, 1e8, 1e30), "fp16": (6e4,)}
+LARGE = {"fp32": (1e5, 1e8, 1e12, 1e30, 3.0e38), "bf16": (1e5, 1e8, 1e30, 3.0e38), "fp16": (6e4,)}
 
 
 def make(T, V, d, tname, std=0.3):
@@ -49,3 +49,13 @@ def test_large_queries_that_do_not_count_touch_no_other(T, V, d, tname, value):
         ref = torch.logsumexp(su.scores(q[none], w, 1.0), 1)
         err = (out[1].double()[none] - ref).abs()
         assert (err <= su.score_error(q[none], w, 1.0) + su.sum_error(V) + ref.abs() * 2.0 ** -23).all(), float(err.max())
+
+
+@pytest.mark.parametrize("tname", ("fp32", "bf16", "fp16"))
+def test_queries_that_do_not_count_beside_rows_that_are_not_finite(tname):
+    """Their weight is zero by itself, not zero times their probabilities."""
+    g, q, w, targets = make(200, 300, 40, tname)
+    targets[:] = -1
+    w[17], w[40, 3] = float("inf"), float("nan")
+    loss, _, gq, gw = su.run_loss(q, w, tname, targets)
+    assert not loss.any() and not gq.any() and not gw.any()
