@@ -228,9 +228,11 @@ int mar_dropout(const void* x, int64_t x_stride, int64_t rows, int32_t dim, int3
  * Softmax over ALL rows of a table: query i gives row j the score s_ij = scale * (query_i . row_j).  For the bilinear score
  * functions a query is the edge's operand of everything but the replaced endpoint (DistMult: theta_s * theta_r; ComplEx:
  * theta_s theta_r as [re | im] for destinations; Dot: theta_s) and the table is the node embeddings.
- * Products of bf16 and fp16 values are exact and summed in fp32; fp32 values are taken as the sum of two f16 numbers scaled
- * by the largest of eight neighbouring rows (as accurate as fp32 down to rows 2^-17 of that, and of 2^-100).  Scores that are
- * not finite, or of 2^24 and more (whose own rounding is a factor e), make the results of their query NaN or infinite.
+ * Products of bf16 and fp16 values are exact and summed in fp32; fp32 values are taken as the sum of two f16 numbers (22 bits),
+ * scaled by the row's own largest value in mar_log_probs, and by that of the row's block in mar_softmax_loss: rows 8 k .. 8 k + 7
+ * of the table, or those of them that count among the queries (as accurate as fp32 down to rows 2^-17 of that; and down to
+ * 2^-100).  Scores that are not finite, or of 2^24 and more (whose own rounding is a factor e), may make the results of their
+ * query NaN or infinite.
  */
 #define MAR_SOFTMAX_MAX_ROWS    ((int64_t)0x1fffff00)   /* launches hold fewer than 2^32 threads */
 #define MAR_SOFTMAX_MAX_QUERIES 0x3ffff00

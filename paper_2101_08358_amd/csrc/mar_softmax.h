@@ -8,7 +8,7 @@
 //   PASS 1  stationary queries, streamed table: the same without the entropy, and O = sum of weights times rows
 //   PASS 2  stationary table rows, streamed queries: O = sum of weights times queries, with the finished log-sum-exp
 // bf16 and fp16 values go to the matrix pipe as they are; an fp32 value v is v 2^e = hi + lo, both f16 (mar_split.h), a product
-// three of theirs, with one exponent per stationary row and per eight streamed rows.
+// three of theirs.  Exponents are the rows' own in pass 0; rows that a second product sums over (passes 1 and 2) share one by eights.
 //
 // Lane layouts (lane = 32 h + m = 16 g + i): A lane holds streamed row m, columns 16 s + 8 h .. + 7 of step s; B lane the same
 // columns of stationary row m; D lane holds stationary row m, register r = streamed row 8 (r / 4) + 4 h + r % 4.  Second product
@@ -53,6 +53,7 @@ struct SmArgs {
 struct SmPackArgs {
   const void* src; int64_t stride; int32_t n, dim;
   SmImage to;
+  int32_t apart;                   // every row has an exponent of its own
   const int32_t* ids; const float* weights; int64_t num_ids;
   float least_weight;
 };

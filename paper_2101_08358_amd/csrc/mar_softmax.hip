@@ -20,7 +20,7 @@ struct AnswerArgs {
   float scale; double unscale;
   const int32_t* targets;
   const uint32_t* allowed; int64_t allowed_stride;
-  const float4* stats; const float *first, *second; int32_t pairs;
+  const float4* stats; const float *first, *second;
   float c;                         // scale log2(e)
   float *log_probs, *entropy, *top_log_probs; int32_t* top_ids;
 };
@@ -316,8 +316,8 @@ k_answer(AnswerArgs a) {
   const double kth = full ? exact[a.num_top - 1] * (double)a.c : 0.0;
   const float bar = (float)(kth - (fabs(kth) * 0x1p-16 + sqrt(qn) * sqrt(__longlong_as_double((long long)reach)) * (double)a.c * 0x1p-18));
   if (tid < ngr) {
-    const float two = a.second[q * 2 * a.half + element(groups[tid])] * (a.pairs ? 1.f : a.c);
-    if (two > 0.99f * SM_NO_REF * (a.pairs ? 1.f : a.c) && (!full || two >= bar)) again[atomicAdd(&top.num, 1)] = groups[tid];
+    const float two = a.second[q * 2 * a.half + element(groups[tid])] * a.c;
+    if (two > 0.99f * SM_NO_REF * a.c && (!full || two >= bar)) again[atomicAdd(&top.num, 1)] = groups[tid];
   }
   __syncthreads();
   const int nagain = top.num;
@@ -509,7 +509,7 @@ extern "C" int mar_log_probs(const mar_softmax* p, const void* queries, const vo
     a.ximg = sm_image((char*)workspace + L.qtiles, (char*)workspace + L.qexps, p->num_queries);
     a.yimg = sm_image((char*)workspace + L.wtiles, (char*)workspace + L.wexps, p->num_rows);
     SmPackArgs w = {}, k = {};
-    w.dim = k.dim = p->dim;
+    w.dim = k.dim = p->dim; w.apart = k.apart = 1;
     w.src = table; w.stride = p->row_stride; w.n = (int32_t)p->num_rows; w.to = a.yimg;
     k.src = queries; k.stride = p->query_stride; k.n = p->num_queries; k.to = a.ximg;
     e = sm_pack(p->dtype, w, k, st);
@@ -523,7 +523,7 @@ extern "C" int mar_log_probs(const mar_softmax* p, const void* queries, const vo
   r.Q = queries; r.W = table; r.q_stride = p->query_stride; r.w_stride = p->row_stride; r.rows = p->num_rows;
   r.n = p->num_queries; r.dim = p->dim; r.parts = L.p0.parts; r.num_top = num_top; r.group_tiles = L.group_tiles; r.ngroups = L.ngroups; r.half = L.half;
   r.scale = p->scale; r.unscale = (double)p->scale / (double)a.c;
-  r.targets = targets; r.allowed = allowed; r.allowed_stride = allowed_stride; r.stats = a.stats; r.first = a.first; r.second = a.second; r.pairs = p->dtype == MAR_DTYPE_FP32; r.c = a.c;
+  r.targets = targets; r.allowed = allowed; r.allowed_stride = allowed_stride; r.stats = a.stats; r.first = a.first; r.second = a.second; r.c = a.c;
   r.log_probs = log_probs; r.entropy = entropy; r.top_ids = top_ids; r.top_log_probs = top_log_probs;
   if (p->dtype == MAR_DTYPE_FP32) launch_answer<0>(r, st); else if (p->dtype == MAR_DTYPE_BF16) launch_answer<1>(r, st); else launch_answer<2>(r, st);
   e = hipGetLastError();

@@ -24,7 +24,7 @@ template <int TYPE> __device__ __forceinline__ v16f sm_mfma(v8s a, v8s b, v16f c
 }
 // Largest finite magnitude's bits.
 __device__ __forceinline__ int finite_bits(float v) { const int b = __float_as_int(v) & 0x7fffffff; return b < 0x7f800000 ? b : 0; }
-// Exponent of a row or block whose largest finite magnitude has these bits: 2^e max lies in [2^14, 2^15).  Zeros take 80: the second
+// Exponent of a row or of a block of eight whose largest finite magnitude has these bits: 2^e max lies in [2^14, 2^15).  Zeros take 80: the second
 // product's weights are 2^(t - e), and one far from the others' exponents would leave the floats' range.
 __device__ __forceinline__ int sm_exponent(int max_bits) { return max_bits == 0 ? 80 : min(141 - (max_bits >> 23), 116); }
 __device__ __forceinline__ void sm_parts8(const float (&v)[8], float scale, v8s& hi, v8s& lo) {
@@ -122,8 +122,8 @@ template <int TYPE, int NK> struct SmStage {
       *reinterpret_cast<row_u4*>(to) = zero ? (row_u4)(0u) : place8_bits(r[p][0], 8 * u, dim);
     }
   }
-  // fp32: exps: the exponents of the tile's four blocks of eight rows; row_exps, where not NULL: of every row
-  __device__ __forceinline__ void store(char* tile, int* exps, int* row_exps, int dim, int tid) {
+  // fp32: row_exps: every row's exponent; exps: of the tile's four blocks of eight rows.  OWN: all rows lie apart, exps is not written.
+  template <bool OWN> __device__ __forceinline__ void store(char* tile, int* exps, int* row_exps, int dim, int tid) {
     float scale = 1.f;
     if constexpr (PAIRS) {
       // columns that a piece at the row's end holds besides its own belong to the same row: they may be measured too
@@ -145,10 +145,13 @@ template <int TYPE, int NK> struct SmStage {
         big = __int_as_float(zero ? 0 : most);
       }
       big = row_largest(big);
-      const int block = sm_exponent(__float_as_int(rows_largest(apart ? 0.f : big)));
-      const int e = apart ? sm_exponent(__float_as_int(big)) : block;
-      if ((tid & 63) == 0) exps[tid >> 6] = block;
-      if (row_exps && (tid & 7) == 0) row_exps[tid >> 3] = e;
+      int e = sm_exponent(__float_as_int(big));
+      if (!OWN) {
+        const int block = sm_exponent(__float_as_int(rows_largest(apart ? 0.f : big)));
+        if ((tid & 63) == 0) exps[tid >> 6] = block;
+        e = apart ? e : block;
+      }
+      if ((tid & 7) == 0) row_exps[tid >> 3] = e;
       scale = __builtin_ldexpf(1.f, e);
       if (!finite) {
 #pragma unroll
@@ -200,7 +203,9 @@ k_softmax(SmArgs a) {
   static_assert(IMG || PASS == 0, "passes with a second product take images");
   constexpr int NB = FEW ? 1 : 2;                          // tiles in LDS
   __shared__ __attribute__((aligned(1024))) char smem[NB * G::TILE];
-  __shared__ int exps[2][4];
+  // fp32: exponents of a tile's rows; of its four blocks of eight, which a second product over the rows needs to share
+  constexpr int NE = PASS == 0 ? SM_TY : 4;
+  __shared__ __attribute__((aligned(16))) int exps[2][NE];
   // pass 2, per query of a tile: f = log2(|u| / sum of its weights), m its reference (16-bit types: f - m and nothing)
   __shared__ __attribute__((aligned(16))) float rows_m[2][SM_TY], rows_f[2][SM_TY], rows_u[2][SM_TY];
   __shared__ __attribute__((aligned(16))) int rows_t[2][SM_TY];
@@ -232,8 +237,8 @@ k_softmax(SmArgs a) {
     if (piece < G::TILE / 1024)
       buf_load4_to_lds(buf_words(a.yimg.tiles + (size_t)t * G::TILE, G::TILE), lds_address_b(smem) + buf * G::TILE + piece * 1024, lane * 16, piece * 1024, token);
   };
-  int ye = 0;                                              // exponent of block lane % 4 of the tile on its way
-  auto ask_exps = [&](int t) { if (IMG && PAIRS) ye = a.yimg.exps[4 * (int64_t)t + (lane & 3)]; };
+  int ye = 0;                                              // exponent lane % NE of the tile on its way
+  auto ask_exps = [&](int t) { if (IMG && PAIRS) ye = (PASS == 0 ? a.yimg.row_exps : a.yimg.exps)[NE * (int64_t)t + (lane & (NE - 1))]; };
   float q_m = 0.f, q_f = 0.f, q_u = 0.f;
   int q_t = -1;
   auto load_rows = [&](int y0) {
@@ -355,7 +360,7 @@ k_softmax(SmArgs a) {
   unsigned word_next = PASS == 0 && a.allowed && t_begin < t_end ? words[t_begin] : ~0u;
   int group_left = a.group_tiles;
   int64_t group = PASS == 0 ? t_begin / max(a.group_tiles, 1) : 0;             // finished groups
-  float first_max = SM_NO_REF, second_max = SM_NO_REF;     // of the group so far (scores of 16-bit types before their factor k)
+  float first_max = SM_NO_REF, second_max = SM_NO_REF;     // of the group so far (scores before their factor k)
   v4f first4 = (v4f)(SM_NO_REF), second4 = first4;
   float neg1 = -1.f;
   asm volatile("" : "+v"(neg1));
@@ -381,11 +386,11 @@ k_softmax(SmArgs a) {
   };
   auto land = [&](int buf) {                               // the tile on its way is in LDS, but for the barrier
     if constexpr (IMG) {
-      if (PAIRS && tid < 4) exps[buf][tid] = ye;
+      if (PAIRS && tid < NE) exps[buf][tid] = ye;
       store_rows(buf);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     } else {
-      unrolled<NSG>([&](auto k) { constexpr int w = k; stage[w].store(smem + buf * G::TILE, exps[buf], nullptr, dim, 64 * w + tid); });
+      unrolled<NSG>([&](auto k) { constexpr int w = k; stage[w].template store<true>(smem + buf * G::TILE, nullptr, exps[buf], dim, 64 * w + tid); });
     }
   };
   if (!IMG) __syncthreads();                               // the zeros are there
@@ -440,9 +445,19 @@ k_softmax(SmArgs a) {
       });
     }
     int ey[4] = {0, 0, 0, 0};
-    if (PAIRS) {
+    if (PAIRS && PASS != 0) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) ey[k] = __builtin_amdgcn_readfirstlane(exps[buf][k]);
+    }
+    // pass 0: rows scale their scores themselves, so that none, masked out or not, takes bits from another
+    if constexpr (PAIRS && PASS == 0) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int4 e4 = *reinterpret_cast<const int4*>(&exps[buf][8 * j + 4 * h]);
+        const int e[4] = {e4.x, e4.y, e4.z, e4.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[4 * j + i] = __builtin_ldexpf(sc[4 * j + i], -ex - e[i]);
+      }
     }
     // ---- the first transposed fragments of the second product: step s of 16 rows, block c of 32 columns
     constexpr int NG = 2 * NO, PG = SECOND ? (PAIRS ? 2 : (NG < 4 ? NG : 4)) : 1;
@@ -465,7 +480,7 @@ k_softmax(SmArgs a) {
     // ---- t = sc k[r / 4]: scores in log2 units
     float k[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) k[j] = PAIRS ? fmaxf(__builtin_ldexpf(a.c, max(-200, min(120, -(ex + ey[j])))), 0x1p-126f) : a.c;   // never 0: -inf times it stays
+    for (int j = 0; j < 4; ++j) k[j] = PAIRS && PASS != 0 ? fmaxf(__builtin_ldexpf(a.c, max(-200, min(120, -(ex + ey[j])))), 0x1p-126f) : a.c;   // never 0: -inf times it stays
     if constexpr (PASS != 2) {
       // rows that do not count: beyond the last, or not allowed
       const int left = a.n_y - y0;
@@ -483,7 +498,7 @@ k_softmax(SmArgs a) {
         float v[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          v[r] = __uint_as_float((__float_as_uint(PAIRS ? sc[r] * k[r >> 2] : sc[r]) & ~15u) | r);
+          v[r] = __uint_as_float((__float_as_uint(sc[r]) & ~15u) | r);
           if (some) v[r] = pick((unsigned)((int)(bits << (31 - (8 * (r >> 2) + (r & 3)))) >> 31), v[r], SM_NO_REF);   // -inf would become a NaN
         }
         float one = fmaxf(v[0], v[1]), two = fminf(v[0], v[1]);
@@ -492,12 +507,12 @@ k_softmax(SmArgs a) {
         ztop = one;
         second_max = fmaxf(fmaxf(fminf(first_max, one), second_max), two);
         first_max = fmaxf(first_max, one);
-      } else if constexpr (PAIRS) {
+      } else if constexpr (PAIRS && SECOND) {
         ztop = -__builtin_inff();
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float big = fmaxf(fmaxf(sc[4 * j], sc[4 * j + 1]), fmaxf(sc[4 * j + 2], sc[4 * j + 3])) * k[j];
-          ztop = fmaxf(ztop, SECOND ? big - (float)ey[j] : big);
+          ztop = fmaxf(ztop, big - (float)ey[j]);
         }
       } else {
         ztop = sc[0];
@@ -505,7 +520,7 @@ k_softmax(SmArgs a) {
         for (int r = 1; r < 16; ++r) ztop = fmaxf(ztop, sc[r]);
       }
       if (PASS == 0) ztop = __uint_as_float(__float_as_uint(ztop) & ~15u);   // the same reference with and without the numbers
-      if (!PAIRS) ztop *= k[0];
+      if (!PAIRS || PASS == 0) ztop *= k[0];
       // the reference moves
       if (__any(ztop > ref + SM_ABOVE)) {
         ztop = fmaxf(ztop, __shfl_xor(ztop, 32));        // both halves' weights meet in one product
@@ -742,6 +757,7 @@ k_softmax_pack(SmPackArgs first, SmPackArgs second) {
   stage.begin((const T*)a.src, a.stride, a.n, t * SM_TY, tid);
 #pragma unroll
   for (int p = 0; p < G::NP; ++p) stage.load(p, a.dim, tid);
+  stage.apart = a.apart != 0;
   if (a.ids) {
     const int id = a.ids[y];
     if (id < 0 || id >= a.num_ids || (a.weights && fabsf(a.weights[y]) < a.least_weight)) {
@@ -760,7 +776,7 @@ k_softmax_pack(SmPackArgs first, SmPackArgs second) {
     for (int k = 0; k < G::PLANES; ++k)
       *reinterpret_cast<row_u4*>(tile + k * G::PLANE + (tid >> 3) * G::PA + ((16 * u) ^ (16 * sp_swizzle(G::UNITS, tid >> 3)))) = (row_u4)(0u);
   }
-  stage.store(tile, a.to.exps + 4 * (size_t)t, a.to.row_exps + SM_TY * (size_t)t, a.dim, tid);
+  stage.template store<false>(tile, a.to.exps + 4 * (size_t)t, a.to.row_exps + SM_TY * (size_t)t, a.dim, tid);
 }
 
 // Natural logarithm of a sum of weights: the exponent apart from the mantissa, whose logarithm keeps its bits.
