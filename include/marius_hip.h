@@ -258,7 +258,9 @@ typedef struct mar_softmax {
  *   log_probs      : device, out, [num_queries], or NULL; -infinity where the target is not allowed
  *   entropy        : device, out, [num_queries], or NULL: -sum p log p in natural units
  *   top_ids, top_log_probs : device, out, [num_queries][num_top], by descending probability; scores are compared in
- *                    64 bits, equal ones ordered by id.  Where fewer rows count: id -1, log probability -infinity.
+ *                    64 bits, equal ones ordered by id.  Where fewer rows count: id -1, log probability -infinity.  All rows
+ *                    within 2^-15 |query| |best row| of the last one are scored again (many of them take time); a row 32 times
+ *                    as long as the best ones whose 32-bit score is further off than that may be missed.
  *   workspace      : device, >= mar_log_probs_workspace_bytes of the same problem and num_top, 256-byte aligned; calls
  *                    that may overlap in time need one each
  * A query without an allowed row: log probability -infinity, entropy 0, no top rows.

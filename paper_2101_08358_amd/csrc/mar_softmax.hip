@@ -3,7 +3,8 @@
 // Pass 0 (mar_softmax_dev.h) leaves statistics per query and part of the table, and of every group of 16 group_tiles rows the largest
 // score, with the register it came from, and the second largest.  k_answer joins the parts, a workgroup per query.  The most
 // probable rows lie in the groups with the largest maxima.  The rows behind the maxima are scored in 64 bits; only where a
-// group's second largest score reaches the k-th best of those are its other rows looked at too.  (All rows of the best groups
+// group's second largest score reaches the k-th best of those are its other rows looked at too, and only where the least maximum of
+// the groups taken reaches it are there more groups to look at.  (All rows of the best groups
 // scored again, 16 each: 4,096 queries, 131,072 rows of 400 columns, 16 best rows 367 us, for 1 GB of rows read at random.)
 #include "mar_softmax_dev.h"
 
@@ -11,7 +12,7 @@
 // 62, 256: 79 / 78, 384: 105 / 92; 1,000,000 rows 256 / 411, 411 / 471, 581 / 585; 100,000 rows of 400 columns 123 / 143, 188 / 179,
 // 231 / 212.  bf16, 256, 384 and 512 queries: 47 / 51, 60 / 61, 67 / 69; 190 / 239, 254 / 297, 342 / 371; 70 / 83, 93 / 102, 111 / 114.
 constexpr int sm_rows_most(int type) { return type == MAR_DTYPE_FP32 ? 256 : 512; }
-#define SM_MARGIN 12              // groups, and rows, kept beyond the number asked for: what fp32 less four bits cannot tell apart
+#define SM_MARGIN 12              // groups, and rows, kept beyond the number asked for: few scores that fp32 less four bits cannot tell apart
 
 struct AnswerArgs {
   const void *Q, *W; int64_t q_stride, w_stride, rows;
@@ -159,10 +160,11 @@ k_answer(AnswerArgs a) {
   __shared__ float s_m[NW], s_l[NW], s_a[NW];
   __shared__ __attribute__((aligned(16))) float qs[QN];
   __shared__ TopList top;
-  __shared__ double exact[BATCH + MAXW];
+  __shared__ double exact[BATCH + MAXW], qn, s_lse;        // kept where registers are few
   __shared__ unsigned long long reach;
   __shared__ uint32_t exact_row[BATCH + MAXW];
-  __shared__ int groups[MAXW], again[MAXW], num_exact;
+  constexpr int LIST = NT > MAXW ? NT : MAXW;
+  __shared__ int groups[LIST], again[LIST], num_exact;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t q = blockIdx.x;
   const T* qr = (const T*)a.Q + q * a.q_stride;
@@ -214,6 +216,7 @@ k_answer(AnswerArgs a) {
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) dot += __shfl_xor(dot, o);
     if (lane == 0) {
+      s_lse = lse;
       if (a.log_probs) a.log_probs[q] = !has ? 0.f : (is_allowed(t) ? (float)(dot * (double)a.scale - lse) : -__builtin_inff());
       if (a.entropy) a.entropy[q] = l == 0.f ? 0.f : fmaxf((float)(log_of_sum(l) - 0.69314718055994530942 * ((double)s / (double)l)), 0.f);
     }
@@ -238,9 +241,10 @@ k_answer(AnswerArgs a) {
   __syncthreads();
   auto element = [&](int grp) { return (int64_t)(grp & 1) * a.half + (grp >> 1); };
   auto row_of = [&](int grp, int tile, int r) { return ((int64_t)(grp >> 1) * G + tile) * SM_TY + 8 * (r >> 2) + 4 * (grp & 1) + (r & 3); };
-  constexpr int UL = TYPE == MAR_DTYPE_FP32 && NT > 256 ? 2 : 4;   // as registers allow
-  double wmax = 0.0;                                       // largest squared norm of a row (fp32 squares may leave the floats' range)
-  // Scores items [0, n): row(item) or -1, eight lanes an item.  The list is cut back to its best `want` after every BATCH items.
+  constexpr int UL = NT <= 256 ? 4 : (TYPE == MAR_DTYPE_FP32 ? 2 : 3);   // as registers allow
+  // Scores items [0, n): row(item) or -1, eight lanes an item.  The list is put in order and cut back to its best `want` after every
+  // BATCH items of which some come before its num_top-th.
+  int listed = 0;                                          // entries in order
   auto score_items = [&](int n, auto row) {
     for (int b0 = 0; b0 < n; b0 += BATCH) {
       for (int e0 = b0; e0 < min(n, b0 + BATCH); e0 += NT / 8) {
@@ -266,14 +270,18 @@ k_answer(AnswerArgs a) {
         }
 #pragma unroll
         for (int o = 1; o < 8; o <<= 1) { dot += __shfl_xor(dot, o); n2 += __shfl_xor(n2, o); }
-        wmax = fmax(wmax, n2);
+        const int end = a.num_top - 1;
         if ((tid & 7) == 0 && rw >= 0 && dot == dot) {
-          const int at = atomicAdd(&num_exact, 1);         // below BATCH + MAXW
-          exact[at] = dot; exact_row[at] = (uint32_t)rw;
+          atomicMax(&reach, (unsigned long long)__double_as_longlong(n2));   // the largest squared norm (fp32 squares may leave the floats' range)
+          if (listed <= end || dot > exact[end] || (dot == exact[end] && rw < exact_row[end])) {
+            const int at = atomicAdd(&num_exact, 1);       // below BATCH + MAXW
+            exact[at] = dot; exact_row[at] = (uint32_t)rw;
+          }
         }
       }
       __syncthreads();
       const int have = num_exact;
+      if (have == listed) { __syncthreads(); continue; }   // uniform; all have read the number
       // an entry's rank: SL threads each compare it with a part of the others
       double v[EPT];
       uint32_t rw[EPT];
@@ -294,41 +302,75 @@ k_answer(AnswerArgs a) {
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < EPT; ++i) if (rank[i] < want && tid % SL == 0) { exact[rank[i]] = v[i]; exact_row[rank[i]] = rw[i]; }
-      if (tid == 0) num_exact = min(have, want);
+      listed = __builtin_amdgcn_readfirstlane(min(have, want));
+      if (tid == 0) num_exact = listed;
       __syncthreads();
     }
   };
-  score_items(ngr * G, [&](int e) {
-    const int grp = groups[e / G];
-    return row_of(grp, e % G, (int)(__float_as_uint(gm[element(grp)]) & 15u));
-  });
-  // ---- groups whose second largest score may reach the k-th best: within what the passes' scores are off
+  // What a pass's score is off at most: MFMA chains of up to 75 products in fp32 and pairs of f16, 2^-15 of |q| |row| (2^-20 as measured; so
+  // the rows' lengths need not be known beyond those that are scored), and the four bits that hold the register's number.
+  if (wave == 0) {
+    double n2 = 0.0;
+    for (int c = lane; c < a.dim; c += 64) n2 = __builtin_fma((double)qs[c], (double)qs[c], n2);
 #pragma unroll
-  for (int o = 8; o < 64; o <<= 1) wmax = fmax(wmax, __shfl_xor(wmax, o));
-  if (lane == 0) atomicMax(&reach, (unsigned long long)__double_as_longlong(wmax));                // of numbers that are not negative
-  if (tid == 0) top.num = 0;
-  __syncthreads();
-  double qn = 0.0;
-  for (int c = lane; c < a.dim; c += 64) qn = __builtin_fma((double)qs[c], (double)qs[c], qn);
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) qn += __shfl_xor(qn, o);
-  const bool full = num_exact >= a.num_top;
-  const double kth = full ? exact[a.num_top - 1] * (double)a.c : 0.0;
-  const float bar = (float)(kth - (fabs(kth) * 0x1p-16 + sqrt(qn) * sqrt(__longlong_as_double((long long)reach)) * (double)a.c * 0x1p-18));
-  if (tid < ngr) {
-    const float two = a.second[q * 2 * a.half + element(groups[tid])] * a.c;
-    if (two > 0.99f * SM_NO_REF * a.c && (!full || two >= bar)) again[atomicAdd(&top.num, 1)] = groups[tid];
+    for (int o = 32; o >= 1; o >>= 1) n2 += __shfl_xor(n2, o);
+    if (lane == 0) qn = n2;                                // read behind a barrier of score_items
   }
-  __syncthreads();
-  const int nagain = top.num;
-  score_items(nagain * G * 16, [&](int e) {
-    const int grp = again[e / (G * 16)], r = e & 15, one = (int)(__float_as_uint(gm[element(grp)]) & 15u);
-    return r == one ? (int64_t)-1 : row_of(grp, (e >> 4) % G, r);
-  });
+  // The k-th best score so far less that, in the passes' log2 units; -inf while there are fewer.
+  auto bar = [&]() {
+    if (num_exact < a.num_top) return -__builtin_inff();
+    const double kth = exact[a.num_top - 1] * (double)a.c;
+    return (float)(kth - (fabs(kth) * 0x1p-16 + sqrt(qn) * sqrt(__longlong_as_double((long long)reach)) * (double)a.c * 0x1p-15));
+  };
+  // Groups of the list first, then (rare: many scores that the passes cannot tell apart) all others whose maxima reach the bar, a chunk
+  // of NT groups at a time.
+  const int all = (int)(2 * a.half);
+  int n = ngr, e0 = 0;
+  while (true) {
+    if (n) {                                               // uniform
+      score_items(n * G, [&](int e) {
+        const int grp = groups[e / G];
+        return row_of(grp, e % G, (int)(__float_as_uint(gm[element(grp)]) & 15u));
+      });
+      // ---- groups whose second largest score may reach the k-th best
+      const float least = bar();
+      if (tid == 0) top.num = 0;
+      __syncthreads();
+      if (tid < n) {
+        const float two = a.second[q * 2 * a.half + element(groups[tid])] * a.c;
+        if (two > 0.99f * SM_NO_REF * a.c && two >= least) again[atomicAdd(&top.num, 1)] = groups[tid];
+      }
+      __syncthreads();
+      score_items(top.num * G * 16, [&](int e) {
+        const int grp = again[e / (G * 16)], r = e & 15, one = (int)(__float_as_uint(gm[element(grp)]) & 15u);
+        return r == one ? (int64_t)-1 : row_of(grp, (e >> 4) % G, r);
+      });
+    }
+    if (top.have < want || e0 >= all) break;               // every group was in the list, or has been looked at
+    if (qn == 0.0 || reach == 0ull) break;                 // all scores are zeros, as measured: the list has the lowest ids
+    const float least = bar();
+    const unsigned long long last = top.best[want - 1];    // groups up to this one have been seen, in the order of the list
+    if (e0 == 0) {
+      const uint32_t key = (uint32_t)(last >> 32) | 15u;   // the least maximum in the list
+      if (__uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key) * a.c < least) break;
+    }
+    __syncthreads();
+    if (tid == 0) top.num = 0;
+    __syncthreads();
+    const int e = e0 + tid, half = (int)a.half;
+    if (e < all && (e < half ? e : e - half) < a.ngroups) {
+      const float v = gm[e];
+      const uint32_t key = v > 0.99f * SM_NO_REF ? order_key(v) & ~15u : 0u, id = (uint32_t)(e < half ? 2 * e : 2 * (e - half) + 1);
+      if (key && ((unsigned long long)key << 32 | (uint32_t)~id) < last && v * a.c >= least) groups[atomicAdd(&top.num, 1)] = (int)id;
+    }
+    __syncthreads();
+    n = top.num;
+    e0 += NT;
+  }
   const int have = min(num_exact, a.num_top);
   for (int e = tid; e < a.num_top; e += NT) {
     a.top_ids[q * a.num_top + e] = e < have ? (int32_t)exact_row[e] : -1;
-    a.top_log_probs[q * a.num_top + e] = e < have ? (float)(exact[e] * (double)a.scale - lse) : -__builtin_inff();
+    a.top_log_probs[q * a.num_top + e] = e < have ? (float)(exact[e] * (double)a.scale - s_lse) : -__builtin_inff();
   }
 }
 

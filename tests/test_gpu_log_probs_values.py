@@ -1,5 +1,5 @@
 """GPU parity of mar_log_probs with 64 bits where values are out of the ordinary: rows that a mask takes out, of any size, beside
-others, rows of very different size."""
+others, rows of very different size, scores that 32 bits cannot tell apart."""
 import pytest
 import torch
 
@@ -52,3 +52,36 @@ def test_small_rows_and_queries_beside_large_ones(T):
     out = su.run_log_probs(q, plain, "fp32", targets)
     kept = torch.arange(T, device=DEV) % 8 != 3
     check(q[kept], plain, "fp32", targets[kept], None, 0, 1.0, tuple(x[kept] for x in out))
+
+
+@pytest.mark.parametrize("tname", ("fp32", "bf16", "fp16"))
+@pytest.mark.parametrize("T,V,top,shared", ((5, 70_000, 10, 256.0), (100, 30_000, 32, 128.0), (600, 20_000, 10, 128.0), (1700, 6_000, 5, 240.0), (3, 300_000, 10, 200.0)))
+def test_best_rows_that_32_bits_cannot_tell_apart(T, V, top, shared, tname):
+    """A column that all share makes the scores large, and their differences small beside what a 32-bit score is off."""
+    print("case", T, V, top, shared, tname, flush=True)
+    g = su.gen(V)
+    dt, d = su.TYPES[tname][0], 32
+    q, w = su.rows(g, T, d, dt, std=0.05), su.rows(g, V, d, dt, std=0.05)
+    q[:, 7] = shared
+    w[:, 7] = shared
+    out = su.run_log_probs(q, w, tname, top=top)
+    check(q, w, tname, None, None, top, 1.0, (None, out[1], out[2], out[3]))
+    allowed = torch.rand((T, V), generator=g, device=DEV) < 0.5
+    words = su.pack(allowed)
+    out = su.run_log_probs(q, w, tname, None, words, words.shape[1], top=top)
+    check(q, w, tname, None, allowed, top, 1.0, (None, out[1], out[2], out[3]))
+
+
+@pytest.mark.parametrize("T", (3, 300, 900, 1600))
+def test_best_rows_that_all_score_the_same(T):
+    """Copies of one row, and a query of zeros: every group of rows may hold the best, and the lowest ids are it."""
+    g = su.gen(T)
+    q, w = su.rows(g, T, 30, torch.bfloat16), su.rows(g, 1, 30, torch.bfloat16).expand(9000, 30).contiguous()
+    q[1] = 0
+    ids = su.run_log_probs(q, w, "bf16", top=12)[2]
+    assert torch.equal(ids, torch.arange(12, device=DEV, dtype=torch.int32).expand(T, 12))
+    w[4321] = 2 * q[2]                                       # one that stands out for its query, at the end for those that it repels
+    s = su.scores(q, w, 1.0)
+    s[:, torch.arange(9000, device=DEV) != 4321] = s[:, :1].clone()
+    want = s.sort(dim=1, descending=True, stable=True).indices[:, :12]
+    assert torch.equal(su.run_log_probs(q, w, "bf16", top=12)[2].long(), want)
