@@ -231,8 +231,8 @@ int mar_dropout(const void* x, int64_t x_stride, int64_t rows, int32_t dim, int3
  * Products of bf16 and fp16 values are exact and summed in fp32; fp32 values are taken as the sum of two f16 numbers (22 bits),
  * scaled by the row's own largest value in mar_log_probs, and by that of the row's block in mar_softmax_loss: rows 8 k .. 8 k + 7
  * of the table, or those of them that count among the queries (as accurate as fp32 down to rows 2^-17 of that; and down to
- * 2^-100).  Scores that are not finite, or of 2^24 and more (whose own rounding is a factor e), may make the results of their
- * query NaN or infinite.
+ * 2^-100, in a table whose blocks' largest values are not 2^100 apart).  Scores that are not finite, or of 2^24 and more (whose
+ * own rounding is a factor e), may make the results of their query NaN or infinite.
  */
 #define MAR_SOFTMAX_MAX_ROWS    ((int64_t)0x1fffff00)   /* launches hold fewer than 2^32 threads */
 #define MAR_SOFTMAX_MAX_QUERIES 0x3ffff00

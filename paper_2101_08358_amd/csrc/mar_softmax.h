@@ -35,7 +35,9 @@ struct SmArgs {
   int32_t n_x, n_y, dim, nstripes, units;
   int32_t parts, tps;              // parts of the streamed tiles, tiles each
   float c, scale;                  // c = scale log2(e)
-  float4* stats;                   // [parts][n_x]: reference (log2 units), sum of 2^(t - reference), sum of that times (t - reference)
+  // [parts][n_x]: reference (log2 units); sum of 2^(t - reference), in pass 1 with a reference of its own, the third number; pass 0: sum of
+  // the weights times (t - reference)
+  float4* stats;
   float *first, *second;           // [n_x][2][half]: largest and second largest score of a group: one half's rows of group_tiles tiles
   int64_t half;                    // groups a half, rounded up to a multiple of 4
   int32_t group_tiles;

@@ -173,6 +173,7 @@ __device__ __forceinline__ float own_float(int k) { return __int_as_float(k < 0 
 // References are integers: moving one, and joining parts, multiplies by powers of two only, and a weight of 1 stays exact.
 #define SM_ABOVE 15.f
 #define SM_BELOW 12.f
+#define SM_SUM_ABOVE 60.f
 #define SM_CHAIN 16               // tiles whose weights are summed before their sum is added to the part's: chains of fp32 sums stay short
 
 // How the streamed rows come: SM_IMAGES: both matrices as images.  SM_ROWS: from the rows themselves, a tile staged by the
@@ -353,6 +354,9 @@ k_softmax(SmArgs a) {
 #pragma unroll
   for (int c = 0; c < NO; ++c) oacc[c] = (v16f)(0.f);
   float ref = SM_NO_REF, lsum = 0.f, ltot = 0.f, asum = 0.f, atot = 0.f;
+  // fp32 pairs in pass 1: weights follow t - e, and their sum, which is one of 2^t, would leave the floats' range where all rows are tiny
+  // (e near 116): it has a reference of its own, ref - es, which moves when a score exceeds it by more than SM_SUM_ABOVE.
+  int es = 0;
   if (PASS == 2 && REFS) {                                 // the weights of the row's own queries stay below it
     const int top = own[wave * 32 + m];
     if (top != SM_NO_OWN) ref = __builtin_ceilf(own_float(top)) - SM_BELOW;
@@ -522,7 +526,9 @@ k_softmax(SmArgs a) {
       if (PASS == 0) ztop = __uint_as_float(__float_as_uint(ztop) & ~15u);   // the same reference with and without the numbers
       if (!PAIRS || PASS == 0) ztop *= k[0];
       // the reference moves
-      if (__any(ztop > ref + SM_ABOVE)) {
+      bool moves = ztop > ref + SM_ABOVE;
+      if (PAIRS && SECOND) moves = moves || es + max(max(ey[0], ey[1]), max(ey[2], ey[3])) > (int)(SM_SUM_ABOVE - SM_ABOVE);   // t may exceed it
+      if (__any(moves)) {
         ztop = fmaxf(ztop, __shfl_xor(ztop, 32));        // both halves' weights meet in one product
         const float to = fmaxf(ref, __builtin_ceilf(ztop) - SM_BELOW), by = ref - to, fct = __builtin_amdgcn_exp2f(by);
         if (PASS == 0) {
@@ -530,7 +536,17 @@ k_softmax(SmArgs a) {
           asum = l != 0.f ? fct * __builtin_fmaf(by, l, asum + atot) : 0.f;
           atot = 0.f;
         }
-        lsum *= fct; ltot *= fct;
+        float by_sum = fct;
+        if constexpr (PAIRS && SECOND) {
+          float ttop = -__builtin_inff();
+#pragma unroll
+          for (int j = 0; j < 4; ++j) ttop = fmaxf(ttop, fmaxf(fmaxf(sc[4 * j], sc[4 * j + 1]), fmaxf(sc[4 * j + 2], sc[4 * j + 3])) * k[j]);
+          ttop = fmaxf(ttop, __shfl_xor(ttop, 32));
+          const float from = ref - (float)es, to_sum = ttop > from + SM_SUM_ABOVE ? __builtin_ceilf(ttop) : from;
+          by_sum = __builtin_amdgcn_exp2f(from - to_sum);
+          es = (int)(to - to_sum);
+        }
+        lsum *= by_sum; ltot *= by_sum;
         if constexpr (SECOND) rescale(fct);
         ref = to;
       }
@@ -548,7 +564,7 @@ k_softmax(SmArgs a) {
           sum4 += w[r];
           if (PASS == 0) a16 = __builtin_fmaf(w[r], z, a16);
         }
-        l16 += SECOND && PAIRS ? __builtin_ldexpf(sum4, ey[j]) : sum4;
+        l16 += SECOND && PAIRS ? __builtin_ldexpf(sum4, ey[j] + es) : sum4;
       }
       lsum += l16;
       if (PASS == 0) asum += a16;
@@ -722,7 +738,7 @@ k_softmax(SmArgs a) {
   if (PASS != 2) {                                       // the halves of a tile's rows share their reference
     const float lw = lsum + ltot, aw = asum + atot;
     const float l = lw + __shfl_xor(lw, 32), s = aw + __shfl_xor(aw, 32);
-    if (h == 0 && xv) a.stats[(size_t)part * a.n_x + x] = make_float4(ref, l, s, 0.f);
+    if (h == 0 && xv) a.stats[(size_t)part * a.n_x + x] = make_float4(ref, l, PASS == 0 ? s : ref - (float)es, 0.f);
   }
   if constexpr (SECOND) {
     float f = 1.f;                                       // twice the square root: the power itself may leave the floats' range

@@ -29,12 +29,12 @@ k_loss_rows(LossArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t q = blockIdx.x;
   // every wave for itself: a lane a part
-  const float4 mine = lane < a.parts ? a.stats[(size_t)lane * a.n + q] : make_float4(SM_NO_REF, 0.f, 0.f, 0.f);
-  float m = mine.x;
+  const float4 mine = lane < a.parts ? a.stats[(size_t)lane * a.n + q] : make_float4(SM_NO_REF, 0.f, SM_NO_REF, 0.f);
+  float mo = mine.x, m = mine.z;                           // references of the sums of rows and of weights
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  const float f = __builtin_amdgcn_exp2f(mine.x - m);
-  float l = mine.y * f;
+  for (int o = 32; o >= 1; o >>= 1) { mo = fmaxf(mo, __shfl_xor(mo, o)); m = fmaxf(m, __shfl_xor(m, o)); }
+  const float f = __builtin_amdgcn_exp2f(mine.x - mo);
+  float l = mine.y * __builtin_amdgcn_exp2f(mine.z - m);
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) l += __shfl_xor(l, o);
   if (wave == 0) fac[lane] = f;
@@ -79,11 +79,12 @@ k_loss_rows(LossArgs a) {
   __syncthreads();
   T* out = (T*)a.grad + q * a.grad_stride;
   const float less = expm1f((float)over), inv = 1.f / l, us = u * a.scale;
+  const int up = (int)(mo - m);
   for (int c = threadIdx.x; c < a.dim; c += 64 * WAVES) {
     float sum = 0.f;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) sum += reinterpret_cast<const float*>(sums[w])[c];
-    const float v = us * __builtin_fmaf(less, (float)wr[c], sum * inv);
+    const float v = us * __builtin_fmaf(less, (float)wr[c], __builtin_ldexpf(sum * inv, up));
     out[c] = (T)(u != 0.f ? v : 0.f);
   }
 }

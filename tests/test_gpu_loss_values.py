@@ -1,5 +1,5 @@
 """GPU parity of mar_softmax_loss with 64 bits where values are out of the ordinary: queries that do not count, of any size, beside
-others and beside rows that are not finite."""
+others and beside rows that are not finite, the ends of the floats' range."""
 import pytest
 import torch
 
@@ -59,3 +59,14 @@ def test_queries_that_do_not_count_beside_rows_that_are_not_finite(tname):
     w[17], w[40, 3] = float("inf"), float("nan")
     loss, _, gq, gw = su.run_loss(q, w, tname, targets)
     assert not loss.any() and not gq.any() and not gw.any()
+
+
+@pytest.mark.parametrize("up,down", ((100, -100), (-100, 100), (60, -60), (0, -100), (-100, 0), (88, -88)))
+@pytest.mark.parametrize("T,V,d", ((70, 3000, 100), (300, 700, 40), (20, 15_000, 16)))
+def test_values_towards_the_ends_of_the_range(T, V, d, up, down):
+    """fp32: one matrix 2^up times and the other 2^down times what is usual; weights and their sums stay inside the floats' range."""
+    print("case", T, V, d, up, down, flush=True)
+    g, q, w, targets = make(T, V, d, "fp32", std=1.0)
+    q, w = q * 2.0 ** up, w * 2.0 ** down
+    weights = torch.rand(T, generator=g, device=DEV) + 0.5
+    su.check_loss(su.run_loss(q, w, "fp32", targets, weights), q, w, "fp32", targets, weights, 1.0)
