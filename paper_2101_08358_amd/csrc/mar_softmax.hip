@@ -217,7 +217,7 @@ k_answer(AnswerArgs a) {
     for (int o = 32; o >= 1; o >>= 1) dot += __shfl_xor(dot, o);
     if (lane == 0) {
       s_lse = lse;
-      if (a.log_probs) a.log_probs[q] = !has ? 0.f : (is_allowed(t) ? (float)(dot * (double)a.scale - lse) : -__builtin_inff());
+      if (a.log_probs) a.log_probs[q] = !has ? 0.f : (is_allowed(t) ? (float)at_most_0(dot * (double)a.scale - lse) : -__builtin_inff());
       if (a.entropy) a.entropy[q] = l == 0.f ? 0.f : fmaxf((float)(log_of_sum(l) - 0.69314718055994530942 * ((double)s / (double)l)), 0.f);
     }
   }
@@ -370,7 +370,7 @@ k_answer(AnswerArgs a) {
   const int have = min(num_exact, a.num_top);
   for (int e = tid; e < a.num_top; e += NT) {
     a.top_ids[q * a.num_top + e] = e < have ? (int32_t)exact_row[e] : -1;
-    a.top_log_probs[q * a.num_top + e] = e < have ? (float)(exact[e] * (double)a.scale - s_lse) : -__builtin_inff();
+    a.top_log_probs[q * a.num_top + e] = e < have ? (float)at_most_0(exact[e] * (double)a.scale - s_lse) : -__builtin_inff();
   }
 }
 

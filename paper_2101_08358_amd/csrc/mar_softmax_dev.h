@@ -801,3 +801,5 @@ __device__ __forceinline__ double log_of_sum(float l) {
   const float m = frexpf(l, &e);
   return (double)e * 0.69314718055994530942 + (double)logf(m);
 }
+// A log probability: a score in 64 bits less a log-sum-exp of scores in 32 may come out above 0.
+__device__ __forceinline__ double at_most_0(double v) { return v > 0.0 ? 0.0 : v; }   // NaN stays

@@ -48,7 +48,7 @@ k_loss_rows(LossArgs a) {
   for (int c = lane; c < a.dim; c += 64) dot = __builtin_fma((double)(float)qr[c], (double)(float)wr[c], dot);
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) dot += __shfl_xor(dot, o);
-  const double lse = (double)m * a.unscale + log_of_sum(l), over = dot * (double)a.scale - lse;   // log p of the answer
+  const double lse = (double)m * a.unscale + log_of_sum(l), over = at_most_0(dot * (double)a.scale - lse);   // log p of the answer
   if (threadIdx.x == 0) {
     if (a.lse) a.lse[q] = (float)lse;
     if (a.loss) a.loss[q] = u != 0.f ? (float)(-(double)u * over) : 0.f;

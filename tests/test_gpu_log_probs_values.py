@@ -1,5 +1,5 @@
 """GPU parity of mar_log_probs with 64 bits where values are out of the ordinary: rows that a mask takes out, of any size, beside
-others, rows of very different size, scores that 32 bits cannot tell apart."""
+others, rows of very different size, scores that 32 bits cannot tell apart, distributions with nearly all probability in one row."""
 import pytest
 import torch
 
@@ -85,3 +85,16 @@ def test_best_rows_that_all_score_the_same(T):
     s[:, torch.arange(9000, device=DEV) != 4321] = s[:, :1].clone()
     want = s.sort(dim=1, descending=True, stable=True).indices[:, :12]
     assert torch.equal(su.run_log_probs(q, w, "bf16", top=12)[2].long(), want)
+
+
+@pytest.mark.parametrize("tname", ("fp32", "bf16", "fp16"))
+@pytest.mark.parametrize("T", (30, 200, 2000))
+def test_no_log_probability_is_positive(T, tname):
+    g = su.gen(T)
+    dt, V, d = su.TYPES[tname][0], 500, 64
+    w = su.rows(g, V, d, dt, std=1.0)
+    targets = torch.randint(0, V, (T,), generator=g, device=DEV, dtype=torch.int32)
+    q = (w[targets.long()].float() * (1.0 + torch.rand((T, 1), generator=g, device=DEV))).to(dt)
+    lp, en, ids, tp = su.run_log_probs(q, w, tname, targets, top=3)
+    assert (lp <= 0).all() and (tp <= 0).all() and (en >= 0).all(), (float(lp.max()), float(tp.max()))
+    check(q, w, tname, targets, None, 3, 1.0, (lp, en, ids, tp))

@@ -1,5 +1,5 @@
 """GPU parity of mar_softmax_loss with 64 bits where values are out of the ordinary: queries that do not count, of any size, beside
-others and beside rows that are not finite, the ends of the floats' range."""
+others, the ends of the floats' range, answers with all of the probability."""
 import pytest
 import torch
 
@@ -70,3 +70,13 @@ def test_values_towards_the_ends_of_the_range(T, V, d, up, down):
     q, w = q * 2.0 ** up, w * 2.0 ** down
     weights = torch.rand(T, generator=g, device=DEV) + 0.5
     su.check_loss(su.run_loss(q, w, "fp32", targets, weights), q, w, "fp32", targets, weights, 1.0)
+
+
+@pytest.mark.parametrize("tname", ("fp32", "bf16", "fp16"))
+def test_no_loss_is_negative(tname):
+    """Answers with all of the probability: the log-sum-exp, in 32 bits, may come out below the answer's score in 64."""
+    g, q, w, targets = make(2000, 500, 64, tname, std=1.0)
+    q.copy_((w[targets.long()].float() * (1.0 + torch.rand((2000, 1), generator=g, device=DEV))).to(q.dtype))
+    out = su.run_loss(q, w, tname, targets)
+    assert (out[0] >= 0).all(), float(out[0].min())
+    su.check_loss(out, q, w, tname, targets, None, 1.0)
