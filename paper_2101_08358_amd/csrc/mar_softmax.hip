@@ -150,6 +150,7 @@ __device__ __forceinline__ void add_entries(TopList& top, const uint32_t (&key)[
   __syncthreads();
 }
 
+__device__ __forceinline__ double at_least_0(double v) { return v < 0.0 ? 0.0 : v; }        // NaN stays
 // R: keys of group maxima a thread looks at together.
 template <int TYPE, int NT, int R>
 __global__ void __launch_bounds__(NT)
@@ -218,7 +219,7 @@ k_answer(AnswerArgs a) {
     if (lane == 0) {
       s_lse = lse;
       if (a.log_probs) a.log_probs[q] = !has ? 0.f : (is_allowed(t) ? (float)at_most_0(dot * (double)a.scale - lse) : -__builtin_inff());
-      if (a.entropy) a.entropy[q] = l == 0.f ? 0.f : fmaxf((float)(log_of_sum(l) - 0.69314718055994530942 * ((double)s / (double)l)), 0.f);
+      if (a.entropy) a.entropy[q] = l == 0.f ? 0.f : (float)at_least_0(log_of_sum(l) - 0.69314718055994530942 * ((double)s / (double)l));
     }
   }
   if (a.num_top == 0) return;

@@ -1,5 +1,5 @@
 """GPU parity of mar_log_probs with 64 bits where values are out of the ordinary: rows that a mask takes out, of any size, beside
-others, rows of very different size, scores that 32 bits cannot tell apart, distributions with nearly all probability in one row."""
+others, rows of very different size, scores that 32 bits cannot tell apart, queries that are not finite."""
 import pytest
 import torch
 
@@ -98,3 +98,15 @@ def test_no_log_probability_is_positive(T, tname):
     lp, en, ids, tp = su.run_log_probs(q, w, tname, targets, top=3)
     assert (lp <= 0).all() and (tp <= 0).all() and (en >= 0).all(), (float(lp.max()), float(tp.max()))
     check(q, w, tname, targets, None, 3, 1.0, (lp, en, ids, tp))
+
+
+@pytest.mark.parametrize("T", (5, 70, 400))
+def test_entropy_of_a_query_that_is_not_finite(T):
+    g = su.gen(T)
+    q, w = su.rows(g, T, 40, torch.float32), su.rows(g, 300, 40, torch.float32)
+    q[2, 5], q[4, 0] = float("nan"), float("inf")
+    en = su.run_log_probs(q, w, "fp32", top=3)[1]
+    assert not torch.isfinite(en[2]) and not torch.isfinite(en[4])
+    kept = torch.ones(T, dtype=torch.bool, device=DEV)
+    kept[2] = kept[4] = False
+    assert (en[kept] > 0).all()
