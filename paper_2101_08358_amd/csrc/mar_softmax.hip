@@ -188,23 +188,18 @@ k_answer(AnswerArgs a) {
   if (a.num_top) load_keys(0, key);
 
   // ---- statistics of all parts
-  auto join = [](float& m, float& l, float& s, float m2, float l2, float s2) {
-    const float to = fmaxf(m, m2), d1 = m - to, d2 = m2 - to, f1 = __builtin_amdgcn_exp2f(d1), f2 = __builtin_amdgcn_exp2f(d2);
-    const float sa = l != 0.f ? f1 * __builtin_fmaf(d1, l, s) : 0.f, sb = l2 != 0.f ? f2 * __builtin_fmaf(d2, l2, s2) : 0.f;
-    l = l * f1 + l2 * f2; s = sa + sb; m = to;
-  };
   float m = SM_NO_REF, l = 0.f, s = 0.f;
-  for (int p = tid; p < a.parts; p += NT) { const float4 v = a.stats[(size_t)p * a.n + q]; join(m, l, s, v.x, v.y, v.z); }
+  for (int p = tid; p < a.parts; p += NT) { const float4 v = a.stats[(size_t)p * a.n + q]; sm_join(m, l, s, v.x, v.y, v.z); }
   if (a.parts > 1) {
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) join(m, l, s, __shfl_xor(m, o), __shfl_xor(l, o), __shfl_xor(s, o));
+    for (int o = 32; o >= 1; o >>= 1) sm_join(m, l, s, __shfl_xor(m, o), __shfl_xor(l, o), __shfl_xor(s, o));
   }
   if (lane == 0) { s_m[wave] = m; s_l[wave] = l; s_a[wave] = s; }
   for (int c = tid; c < QN; c += NT) qs[c] = c < a.dim ? (float)qr[c] : 0.f;
   if (tid == 0) top.have = 0;
   __syncthreads();
   m = s_m[0]; l = s_l[0]; s = s_a[0];
-  for (int w = 1; w < NW && w * 64 < a.parts; ++w) join(m, l, s, s_m[w], s_l[w], s_a[w]);
+  for (int w = 1; w < NW && w * 64 < a.parts; ++w) sm_join(m, l, s, s_m[w], s_l[w], s_a[w]);
   const double lse = (double)m * a.unscale + log_of_sum(l);
 
   // ---- the answer's log probability, the entropy

@@ -164,13 +164,21 @@ template <int TYPE, int NK> struct SmStage {
   }
 };
 
+// Joins two parts' statistics: reference, sum of weights, sum of weights times (t - reference).
+__device__ __forceinline__ void sm_join(float& m, float& l, float& s, float m2, float l2, float s2) {
+  const float to = fmaxf(m, m2), d1 = m - to, d2 = m2 - to, f1 = __builtin_amdgcn_exp2f(d1), f2 = __builtin_amdgcn_exp2f(d2);
+  const float sa = l != 0.f ? f1 * __builtin_fmaf(d1, l, s) : 0.f, sb = l2 != 0.f ? f2 * __builtin_fmaf(d2, l2, s2) : 0.f;
+  l = l * f1 + l2 * f2; s = sa + sb; m = to;
+}
 // Floats as integers of the same order.
 #define SM_NO_OWN INT32_MIN
 __device__ __forceinline__ int own_key(float v) { const int b = __float_as_int(v); return b < 0 ? b ^ 0x7fffffff : b; }
 __device__ __forceinline__ float own_float(int k) { return __int_as_float(k < 0 ? k ^ 0x7fffffff : k); }
 // Softmax weights in fp16 (and as pairs of f16) lie between 2^-24 and 2^16: the reference is put 12 below the largest exponent met
 // and moves when one exceeds it by more than 15; what is 2^-36 of the largest weight is lost to the second product (never to the sum).
-// References are integers: moving one, and joining parts, multiplies by powers of two only, and a weight of 1 stays exact.
+// References are integers: moving one, and joining parts, multiplies by powers of two only, and a weight of 1 stays exact.  In pass 0,
+// without a second product, a lane's reference is its largest score: the entropy of a confident query is what the other rows' weights
+// add to log 1, and to 0 (with references 12 below, differences of numbers near 12 log 2: off by 5e-7).
 #define SM_ABOVE 15.f
 #define SM_BELOW 12.f
 #define SM_SUM_ABOVE 60.f
@@ -526,11 +534,11 @@ k_softmax(SmArgs a) {
       if (PASS == 0) ztop = __uint_as_float(__float_as_uint(ztop) & ~15u);   // the same reference with and without the numbers
       if (!PAIRS || PASS == 0) ztop *= k[0];
       // the reference moves
-      bool moves = ztop > ref + SM_ABOVE;
+      bool moves = ztop > (PASS == 0 ? ref : ref + SM_ABOVE);
       if (PAIRS && SECOND) moves = moves || es + max(max(ey[0], ey[1]), max(ey[2], ey[3])) > (int)(SM_SUM_ABOVE - SM_ABOVE);   // t may exceed it
       if (__any(moves)) {
-        ztop = fmaxf(ztop, __shfl_xor(ztop, 32));        // both halves' weights meet in one product
-        const float to = fmaxf(ref, __builtin_ceilf(ztop) - SM_BELOW), by = ref - to, fct = __builtin_amdgcn_exp2f(by);
+        if (SECOND) ztop = fmaxf(ztop, __shfl_xor(ztop, 32));              // both halves' weights meet in one product
+        const float to = fmaxf(ref, SECOND ? __builtin_ceilf(ztop) - SM_BELOW : ztop), by = ref - to, fct = __builtin_amdgcn_exp2f(by);
         if (PASS == 0) {
           const float l = lsum + ltot;
           asum = l != 0.f ? fct * __builtin_fmaf(by, l, asum + atot) : 0.f;
@@ -735,10 +743,14 @@ k_softmax(SmArgs a) {
   }
 
   // ---- what the part leaves
-  if (PASS != 2) {                                       // the halves of a tile's rows share their reference
-    const float lw = lsum + ltot, aw = asum + atot;
-    const float l = lw + __shfl_xor(lw, 32), s = aw + __shfl_xor(aw, 32);
-    if (h == 0 && xv) a.stats[(size_t)part * a.n_x + x] = make_float4(ref, l, PASS == 0 ? s : ref - (float)es, 0.f);
+  if (PASS == 0) {
+    float l = lsum + ltot, s = asum + atot;
+    sm_join(ref, l, s, __shfl_xor(ref, 32), __shfl_xor(l, 32), __shfl_xor(s, 32));
+    if (h == 0 && xv) a.stats[(size_t)part * a.n_x + x] = make_float4(ref, l, s, 0.f);
+  }
+  if (PASS == 1) {                                       // the halves of a tile's rows share their reference
+    const float lw = lsum + ltot, l = lw + __shfl_xor(lw, 32);
+    if (h == 0 && xv) a.stats[(size_t)part * a.n_x + x] = make_float4(ref, l, ref - (float)es, 0.f);
   }
   if constexpr (SECOND) {
     float f = 1.f;                                       // twice the square root: the power itself may leave the floats' range
@@ -795,10 +807,11 @@ k_softmax_pack(SmPackArgs first, SmPackArgs second) {
   stage.template store<false>(tile, a.to.exps + 4 * (size_t)t, a.to.row_exps + SM_TY * (size_t)t, a.dim, tid);
 }
 
-// Natural logarithm of a sum of weights: the exponent apart from the mantissa, whose logarithm keeps its bits.
+// Natural logarithm of a sum of weights: the exponent apart from the mantissa, whose logarithm keeps its bits, also beside 1.
 __device__ __forceinline__ double log_of_sum(float l) {
   int e;
-  const float m = frexpf(l, &e);
+  float m = frexpf(l, &e);
+  if (m < 0.70710678f) { m *= 2.f; --e; }
   return (double)e * 0.69314718055994530942 + (double)logf(m);
 }
 // A log probability: a score in 64 bits less a log-sum-exp of scores in 32 may come out above 0.

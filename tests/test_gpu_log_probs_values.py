@@ -1,5 +1,6 @@
 """GPU parity of mar_log_probs with 64 bits where values are out of the ordinary: rows that a mask takes out, of any size, beside
-others, rows of very different size, scores that 32 bits cannot tell apart, queries that are not finite."""
+others, rows of very different size, scores that 32 bits cannot tell apart, queries that are
+not finite, distributions with nearly all probability in one row."""
 import pytest
 import torch
 
@@ -98,6 +99,28 @@ def test_no_log_probability_is_positive(T, tname):
     lp, en, ids, tp = su.run_log_probs(q, w, tname, targets, top=3)
     assert (lp <= 0).all() and (tp <= 0).all() and (en >= 0).all(), (float(lp.max()), float(tp.max()))
     check(q, w, tname, targets, None, 3, 1.0, (lp, en, ids, tp))
+
+
+@pytest.mark.parametrize("tname", ("fp32", "bf16", "fp16"))
+@pytest.mark.parametrize("T", (32, 250, 1500))
+def test_entropy_of_confident_queries(T, tname):
+    """One row has nearly all of the probability.  A sum of weights 1 + x takes some 16 roundings of 2^-24 (a lane's 16 scores, the
+    joins of halves, waves and parts): together, root mean square, 16^0.5 / 3^0.5 = 2.3 of them; twice that is allowed.  What is
+    left is as exact as the weights of the other rows."""
+    g = su.gen(T)
+    dt, V, d = su.TYPES[tname][0], 60, 64
+    w = su.rows(g, V, d, dt, std=0.25)
+    q = su.rows(g, T, d, dt, std=0.25)
+    at = torch.randint(0, V, (T,), generator=g, device=DEV)
+    q.copy_((q.float() + w[at].float() * (2.5 + 1.5 * torch.rand((T, 1), generator=g, device=DEV))).to(dt))
+    en = su.run_log_probs(q, w, tname)[1].double()
+    logp = torch.log_softmax(su.scores(q, w, 1.0), 1)
+    H = -(logp.exp() * logp).sum(1)
+    confident = H < 1e-2
+    assert int(confident.sum()) > T // 4
+    err = (en - H).abs()[confident]
+    size = H[confident] * (4 * su.score_error(q, w, 1.0) + 2.0 ** -20)
+    assert float((err - size).clamp(min=0).square().mean().sqrt()) <= 4.6 * 2.0 ** -24, float(err.square().mean().sqrt())
 
 
 @pytest.mark.parametrize("T", (5, 70, 400))
