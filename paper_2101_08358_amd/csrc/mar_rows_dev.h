@@ -93,9 +93,10 @@ template <int TYPE, int N> __device__ __forceinline__ void store_cols(typename R
   typename RowType<TYPE>::T o[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) o[e] = (typename RowType<TYPE>::T)v[e];
-  if (c + N <= d) { __builtin_memcpy(row + c, o, sizeof(o)); return; }
+  const int left = d - c;                                  // c + N may pass 2^31
+  if (N <= left) { __builtin_memcpy(row + c, o, sizeof(o)); return; }
 #pragma unroll
-  for (int e = 0; e < N; ++e) if (c + e < d) row[c + e] = o[e];
+  for (int e = 0; e < N; ++e) if (e < left) row[c + e] = o[e];
 }
 template <int TYPE> __device__ __forceinline__ void store8(typename RowType<TYPE>::T* row, int c, int d, const float (&v)[8]) {
   store_cols<TYPE, 8>(row, c, d, v);
