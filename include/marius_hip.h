@@ -234,7 +234,7 @@ int mar_dropout(const void* x, int64_t x_stride, int64_t rows, int32_t dim, int3
  * 2^-100, in a table whose blocks' largest values are not 2^100 apart).  Scores that are not finite, or of 2^24 and more (whose
  * own rounding is a factor e), may make the results of their query NaN or infinite.
  */
-#define MAR_SOFTMAX_MAX_ROWS    ((int64_t)0x1fffff00)   /* launches hold fewer than 2^32 threads */
+#define MAR_SOFTMAX_MAX_ROWS    ((int64_t)0x1fffff00)   /* below 2^29: ids, tiles and units stay clear of 32 bits */
 #define MAR_SOFTMAX_MAX_QUERIES 0x3ffff00
 #define MAR_MAX_TOP 32
 typedef struct mar_softmax {

@@ -65,6 +65,17 @@ static inline size_t sm_exps_bytes(int64_t rows) { return ((size_t)sm_tiles(rows
 static inline SmImage sm_image(void* tiles, void* exps, int64_t rows) { return {(char*)tiles, (int*)exps, (int*)exps + 4 * sm_tiles(rows)}; }
 hipError_t sm_pack(int dtype, const SmPackArgs& first, const SmPackArgs& second, hipStream_t st);   // one width
 
+// Launches hold fewer than 2^32 threads: launch(first workgroup, workgroups) for as many launches as it takes.
+constexpr int64_t sm_most_blocks(int threads) { return 0xffffffffll / threads; }
+template <typename F> static inline void sm_launches(int64_t blocks, int threads, F launch) {
+  for (int64_t b0 = 0; b0 < blocks; b0 += sm_most_blocks(threads)) {
+    const int64_t left = blocks - b0;
+    launch(b0, (unsigned)(left < sm_most_blocks(threads) ? left : sm_most_blocks(threads)));
+  }
+}
+// Waves per query of k_loss_rows: many parts are worth several, while they make one launch.
+static inline int sm_loss_waves(int parts, int64_t n) { return parts > 4 && n <= sm_most_blocks(256) ? 4 : 1; }
+
 struct SmPlan { int32_t stripes, parts, tps, ntiles; };
 
 const char* sm_check(const mar_softmax* p, int* code);

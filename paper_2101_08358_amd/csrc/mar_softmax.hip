@@ -406,7 +406,8 @@ SmPlan sm_plan(int dtype, int dim, int pass, int mode, int64_t n_x, int64_t n_y,
   int64_t best = INT64_MAX;
   r.parts = 1; r.tps = r.ntiles;
   const int most = pass == 0 ? 1024 : MAR_SOFTMAX_MAX_PARTS;
-  for (int k = 1; k <= most && k <= r.ntiles; k += 1 + k / 32) {           // the host has some microseconds
+  const int64_t room = (sm_most_blocks(256) - 7) / (r.stripes > 0 ? r.stripes : 1);    // one launch, its units rounded up to eights
+  for (int k = 1; k <= most && k <= r.ntiles && k <= room; k += 1 + k / 32) {          // the host has some microseconds
     int64_t tps = (r.ntiles + k - 1) / k;
     tps = (tps + multiple - 1) / multiple * multiple;
     const int64_t parts = (r.ntiles + tps - 1) / tps;
@@ -461,16 +462,19 @@ template <int TYPE, int MODE> static void launch_nk(const SmArgs& a, hipStream_t
   }
 }
 template <int TYPE> static void launch_pack(const SmPackArgs& a, const SmPackArgs& b, hipStream_t st) {
-  const dim3 grid((unsigned)(((int64_t)a.n + SM_TY - 1) / SM_TY + ((int64_t)b.n + SM_TY - 1) / SM_TY)), block(256);
-  switch (sm_nk(a.dim)) {
-    case 2: hipLaunchKernelGGL((k_softmax_pack<TYPE, 2>), grid, block, 0, st, a, b); break;
-    case 4: hipLaunchKernelGGL((k_softmax_pack<TYPE, 4>), grid, block, 0, st, a, b); break;
-    case 7: hipLaunchKernelGGL((k_softmax_pack<TYPE, 7>), grid, block, 0, st, a, b); break;
-    case 8: hipLaunchKernelGGL((k_softmax_pack<TYPE, 8>), grid, block, 0, st, a, b); break;
-    case 12: hipLaunchKernelGGL((k_softmax_pack<TYPE, 12>), grid, block, 0, st, a, b); break;
-    case 16: hipLaunchKernelGGL((k_softmax_pack<TYPE, 16>), grid, block, 0, st, a, b); break;
-    default: hipLaunchKernelGGL((k_softmax_pack<TYPE, 25>), grid, block, 0, st, a, b); break;
-  }
+  sm_launches(sm_tiles(a.n) + sm_tiles(b.n), 256, [&](int64_t first, unsigned blocks) {
+    const dim3 grid(blocks), block(256);
+    const int at = (int)first;
+    switch (sm_nk(a.dim)) {
+      case 2: hipLaunchKernelGGL((k_softmax_pack<TYPE, 2>), grid, block, 0, st, a, b, at); break;
+      case 4: hipLaunchKernelGGL((k_softmax_pack<TYPE, 4>), grid, block, 0, st, a, b, at); break;
+      case 7: hipLaunchKernelGGL((k_softmax_pack<TYPE, 7>), grid, block, 0, st, a, b, at); break;
+      case 8: hipLaunchKernelGGL((k_softmax_pack<TYPE, 8>), grid, block, 0, st, a, b, at); break;
+      case 12: hipLaunchKernelGGL((k_softmax_pack<TYPE, 12>), grid, block, 0, st, a, b, at); break;
+      case 16: hipLaunchKernelGGL((k_softmax_pack<TYPE, 16>), grid, block, 0, st, a, b, at); break;
+      default: hipLaunchKernelGGL((k_softmax_pack<TYPE, 25>), grid, block, 0, st, a, b, at); break;
+    }
+  });
 }
 hipError_t sm_pack(int dtype, const SmPackArgs& a, const SmPackArgs& b, hipStream_t st) {
   if (dtype == MAR_DTYPE_FP32) launch_pack<0>(a, b, st); else if (dtype == MAR_DTYPE_BF16) launch_pack<1>(a, b, st); else launch_pack<2>(a, b, st);

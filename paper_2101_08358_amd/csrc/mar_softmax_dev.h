@@ -771,15 +771,16 @@ k_softmax(SmArgs a) {
   }
 }
 
-// Images of two matrices: a workgroup a tile, the first matrix's first.
+// Images of two matrices: a workgroup a tile, the first matrix's first, from tile `begin` on.
 template <int TYPE, int NK>
 __global__ void __launch_bounds__(256)
-k_softmax_pack(SmPackArgs first, SmPackArgs second) {
+k_softmax_pack(SmPackArgs first, SmPackArgs second, int begin) {
   typedef SmGeom<TYPE, NK> G;
   typedef typename RowType<TYPE>::T T;
   const int tiles = (int)(((int64_t)first.n + SM_TY - 1) / SM_TY);
-  const SmPackArgs a = (int)blockIdx.x < tiles ? first : second;
-  const int tid = threadIdx.x, t = (int)blockIdx.x < tiles ? blockIdx.x : blockIdx.x - tiles, y = min(t * SM_TY + (tid >> 3), a.n - 1);
+  const int at = begin + (int)blockIdx.x;
+  const SmPackArgs a = at < tiles ? first : second;
+  const int tid = threadIdx.x, t = at < tiles ? at : at - tiles, y = min(t * SM_TY + (tid >> 3), a.n - 1);
   char* const tile = a.to.tiles + (size_t)t * G::TILE;
   SmStage<TYPE, NK> stage;
   stage.begin((const T*)a.src, a.stride, a.n, t * SM_TY, tid);

@@ -89,16 +89,16 @@ k_loss_rows(LossArgs a) {
   }
 }
 template <int TYPE> static void launch_rows(const LossArgs& a, hipStream_t st) {
-  if (a.parts > 4) hipLaunchKernelGGL((k_loss_rows<TYPE, 4>), dim3((unsigned)a.n), dim3(256), 0, st, a);
+  if (sm_loss_waves(a.parts, a.n) == 4) hipLaunchKernelGGL((k_loss_rows<TYPE, 4>), dim3((unsigned)a.n), dim3(256), 0, st, a);
   else hipLaunchKernelGGL((k_loss_rows<TYPE, 1>), dim3((unsigned)a.n), dim3(64), 0, st, a);
 }
 
-// Adds the parts of pass 2: a thread per four columns.
+// Adds the parts of pass 2: a thread per four columns, from workgroup `begin` on.
 template <int TYPE>
 __global__ void __launch_bounds__(256)
-k_loss_table(const float* __restrict__ O, int parts, int64_t rows, int dim, int o_pitch, void* grad, int64_t stride) {
+k_loss_table(const float* __restrict__ O, int parts, int64_t rows, int dim, int o_pitch, void* grad, int64_t stride, int64_t begin) {
   typedef typename RowType<TYPE>::T T;
-  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t at = (begin + blockIdx.x) * 256 + threadIdx.x;
   const int quads = o_pitch / 4;
   const int64_t row = at / quads;
   if (row >= rows) return;
@@ -216,11 +216,12 @@ extern "C" int mar_softmax_loss(const mar_softmax* p, const void* queries, const
   if (L.p2.parts == 1) { a.out = grad_table; a.out_stride = grad_row_stride; }
   e = launch_pass<2>(p->dtype, a, st);
   if (e == hipSuccess && L.p2.parts > 1) {
-    const int64_t threads = p->num_rows * (L.o_pitch / 4);
-    const dim3 grid((unsigned)((threads + 255) / 256)), block(256);
-    if (p->dtype == MAR_DTYPE_FP32) hipLaunchKernelGGL(k_loss_table<0>, grid, block, 0, st, a.O, L.p2.parts, p->num_rows, p->dim, L.o_pitch, grad_table, grad_row_stride);
-    else if (p->dtype == MAR_DTYPE_BF16) hipLaunchKernelGGL(k_loss_table<1>, grid, block, 0, st, a.O, L.p2.parts, p->num_rows, p->dim, L.o_pitch, grad_table, grad_row_stride);
-    else hipLaunchKernelGGL(k_loss_table<2>, grid, block, 0, st, a.O, L.p2.parts, p->num_rows, p->dim, L.o_pitch, grad_table, grad_row_stride);
+    sm_launches((p->num_rows * (L.o_pitch / 4) + 255) / 256, 256, [&](int64_t first, unsigned blocks) {
+      const dim3 grid(blocks), block(256);
+      if (p->dtype == MAR_DTYPE_FP32) hipLaunchKernelGGL(k_loss_table<0>, grid, block, 0, st, a.O, L.p2.parts, p->num_rows, p->dim, L.o_pitch, grad_table, grad_row_stride, first);
+      else if (p->dtype == MAR_DTYPE_BF16) hipLaunchKernelGGL(k_loss_table<1>, grid, block, 0, st, a.O, L.p2.parts, p->num_rows, p->dim, L.o_pitch, grad_table, grad_row_stride, first);
+      else hipLaunchKernelGGL(k_loss_table<2>, grid, block, 0, st, a.O, L.p2.parts, p->num_rows, p->dim, L.o_pitch, grad_table, grad_row_stride, first);
+    });
     e = hipGetLastError();
   }
   if (e != hipSuccess) { mar_set_error("table gradient kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }

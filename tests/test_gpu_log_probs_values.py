@@ -1,6 +1,8 @@
 """GPU parity of mar_log_probs with 64 bits where values are out of the ordinary: rows that a mask takes out, of any size, beside
 others, rows of very different size, scores that 32 bits cannot tell apart, queries that are
 not finite, distributions with nearly all probability in one row."""
+import math
+
 import pytest
 import torch
 
@@ -133,3 +135,22 @@ def test_entropy_of_a_query_that_is_not_finite(T):
     kept = torch.ones(T, dtype=torch.bool, device=DEV)
     kept[2] = kept[4] = False
     assert (en[kept] > 0).all()
+
+
+def test_the_largest_table_and_many_queries():
+    """Both matrices' layout takes more than one launch: all rows are zeros but one for every query, with nearly all probability (the
+    zeros' part, 2^29 of e^40, and what their sum is off lie below 2^-24)."""
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("needs 80 GB")
+    V, T, d = 0x1fffff00, 600, 8
+    g = su.gen(1)
+    q = su.rows(g, T, d, torch.bfloat16, std=1.0)
+    w = torch.zeros((V, d), dtype=torch.bfloat16, device=DEV)
+    targets = torch.linspace(0, V - 1, T, dtype=torch.float64, device=DEV).long()
+    planted = (q.float() * (45.0 / q.float().square().sum(1, keepdim=True))).to(torch.bfloat16)
+    w[targets] = planted
+    lp = su.run_log_probs(q, w, "bf16", targets.to(torch.int32))[0].double()
+    s = su.scores(q, planted, 1.0)
+    ref = s.diagonal() - torch.logsumexp(torch.cat([s, torch.full((T, 1), math.log(V - T), dtype=torch.float64, device=DEV)], 1), 1)
+    err = (lp - ref).abs()
+    assert (err <= 2 * su.score_error(q, planted, 1.0) + 256 * 2.0 ** -24 + ref.abs() * 2.0 ** -23).all(), float(err.max())
