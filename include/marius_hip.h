@@ -231,8 +231,8 @@ int mar_dropout(const void* x, int64_t x_stride, int64_t rows, int32_t dim, int3
  * Products of bf16 and fp16 values are exact and summed in fp32; fp32 values are taken as the sum of two f16 numbers (22 bits),
  * scaled by the row's own largest value in mar_log_probs, and by that of the row's block in mar_softmax_loss: rows 8 k .. 8 k + 7
  * of the table, or those of them that count among the queries (as accurate as fp32 down to rows 2^-17 of that; and down to
- * 2^-100, in a table whose blocks' largest values are not 2^100 apart).  Scores that are not finite, or of 2^24 and more (whose
- * own rounding is a factor e), may make the results of their query NaN or infinite.
+ * 2^-100, in a table whose blocks' largest values are not 2^100 apart).  Scores that are not finite, or of 2^23 and more (whose
+ * own rounding is a half), may make the results of their query NaN or infinite.
  */
 #define MAR_SOFTMAX_MAX_ROWS    ((int64_t)0x1fffff00)   /* below 2^29: ids, tiles and units stay clear of 32 bits */
 #define MAR_SOFTMAX_MAX_QUERIES 0x3ffff00
@@ -262,7 +262,8 @@ typedef struct mar_softmax {
  *                    within 2^-15 |query| |best row| of the last one are scored again (many of them take time); a row 32 times
  *                    as long as the best ones whose 32-bit score is further off than that may be missed.
  *   workspace      : device, >= mar_log_probs_workspace_bytes of the same problem and num_top, 256-byte aligned; calls
- *                    that may overlap in time need one each
+ *                    that may overlap in time need one each.  With num_top it grows with num_queries num_rows (half a byte
+ *                    each and less): cut large batches against large tables
  * A query without an allowed row: log probability -infinity, entropy 0, no top rows.
  */
 int mar_log_probs_workspace_bytes(const mar_softmax* problem, int32_t num_top, size_t* out_bytes);
@@ -285,7 +286,9 @@ int mar_log_probs(const mar_softmax* problem, const void* queries, const void* t
  *   workspace: device, >= mar_softmax_loss_workspace_bytes of the same problem, 256-byte aligned; calls that may overlap in
  *              time need one each
  * Sums are held in fp32 and formed in an order that depends on the problem alone (bit-reproducible); weights enter the
- * gradients' products in the operands' 16 bits (fp32: as pairs), an answer's own weight in at least twice as many.
+ * gradients' products in the operands' 16 bits (fp32: as pairs), an answer's own weight in at least twice as many.  fp16 and
+ * fp32: weights below 2^-36 of the largest that meets them in a sum may be lost to it (never to lse); bf16 and fp16: those of a
+ * query in the table's gradient share an error of half an ulp of its lse.
  */
 int mar_softmax_loss_workspace_bytes(const mar_softmax* problem, size_t* out_bytes);
 int mar_softmax_loss(const mar_softmax* problem, const void* queries, const void* table, const int32_t* targets, const float* weights,

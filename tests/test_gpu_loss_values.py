@@ -80,3 +80,34 @@ def test_no_loss_is_negative(tname):
     out = su.run_loss(q, w, tname, targets)
     assert (out[0] >= 0).all(), float(out[0].min())
     su.check_loss(out, q, w, tname, targets, None, 1.0)
+
+
+@pytest.mark.parametrize("T,V,d", ((300, 1200, 100), (40, 3000, 300)))
+def test_rows_2_17_times_as_large_as_their_neighbours(T, V, d):
+    """fp32 rows share an exponent by eights: beside rows 2^16 times as large, of which the queries see a zero column, scores are as
+    exact as the others' own size allows."""
+    g, q, w, targets = make(T, V, d, "fp32")
+    large = torch.arange(V, device=DEV) % 8 == 5
+    q[:, 0] = 0
+    w[large] = 0
+    plain = w.clone()
+    w[large, 0] = 2.0 ** 15
+    loss, lse, _, gw = su.run_loss(q, w, "fp32", targets)
+    su.check_loss((loss, lse, None, gw), q, plain, "fp32", targets, None, 1.0)
+
+
+@pytest.mark.parametrize("tname", ("fp32", "bf16", "fp16"))
+def test_scores_towards_2_23(tname):
+    """As large as they may be: results stay finite, and log-sum-exps as exact as the scores."""
+    g, q, w, targets = make(150, 900, 64, tname, std=1.0)
+    size = (2.0 ** 22.9 / float(su.scores(q, w, 1.0).abs().max())) ** 0.5
+    q, w = (q.float() * size * 0.99).to(q.dtype), (w.float() * size * 0.99).to(w.dtype)
+    loss, lse, gq, gw = su.run_loss(q, w, tname, targets)
+    lp, en, ids, tp = su.run_log_probs(q, w, tname, targets, top=5)
+    assert all(torch.isfinite(x).all() for x in (loss, lse, gq, gw, lp, en, tp))
+    s = su.scores(q, w, 1.0)
+    ref, bound = torch.logsumexp(s, 1), su.score_error(q, w, 1.0) + su.sum_error(900)
+    at = s[torch.arange(150, device=DEV), targets.long()]
+    assert ((lse.double() - ref).abs() <= bound + ref.abs() * 2.0 ** -23).all()
+    assert ((lp.double() - (at - ref)).abs() <= bound + (at - ref).abs() * 2.0 ** -23).all()
+    assert torch.equal(ids.long(), s.sort(dim=1, descending=True, stable=True).indices[:, :5])
