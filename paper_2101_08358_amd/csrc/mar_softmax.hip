@@ -4,13 +4,13 @@
 // score, with the register it came from, and the second largest.  k_answer joins the parts, a workgroup per query.  The most
 // probable rows lie in the groups with the largest maxima.  The rows behind the maxima are scored in 64 bits; only where a
 // group's second largest score reaches the k-th best of those are its other rows looked at too, and only where the least maximum of
-// the groups taken reaches it are there more groups to look at.  (All rows of the best groups
-// scored again, 16 each: 4,096 queries, 131,072 rows of 400 columns, 16 best rows 367 us, for 1 GB of rows read at random.)
+// the groups taken reaches it are there more groups to look at.  (All rows of the best groups scored again, 16 each: 4,096 queries,
+// 131,072 rows of 400 columns, 16 best rows 367 us, for 1 GB of rows read at random.)
 #include "mar_softmax_dev.h"
 
-// Queries above which the matrices are laid out as images first, us rows / images: fp32, 120,000 rows of 100 columns, 128 queries 56 /
-// 62, 256: 79 / 78, 384: 105 / 92; 1,000,000 rows 256 / 411, 411 / 471, 581 / 585; 100,000 rows of 400 columns 123 / 143, 188 / 179,
-// 231 / 212.  bf16, 256, 384 and 512 queries: 47 / 51, 60 / 61, 67 / 69; 190 / 239, 254 / 297, 342 / 371; 70 / 83, 93 / 102, 111 / 114.
+// Queries above which the matrices are laid out as images first, us rows / images: fp32, 120,000 rows of 100 columns, 128 queries 54 /
+// 62, 256: 74 / 77, 384: 98 / 92; 1,000,000 rows 244 / 416, 400 / 473, 574 / 592; 100,000 rows of 400 columns 125 / 143, 190 / 179,
+// 229 / 209.  bf16, 256, 384 and 512 queries: 46 / 51, 60 / 62, 69 / 70; 191 / 246, 255 / 301, 341 / 368; 71 / 83, 96 / 102, 113 / 115.
 constexpr int sm_rows_most(int type) { return type == MAR_DTYPE_FP32 ? 256 : 512; }
 #define SM_MARGIN 12              // groups, and rows, kept beyond the number asked for: few scores that fp32 less four bits cannot tell apart
 
@@ -490,9 +490,9 @@ template <int MODE> static hipError_t launch_stats(int dtype, const SmArgs& a, h
 }
 
 // Threads per query: all that hide a query's own latency where there are few, and as many as leave all queries resident at once
-// (twelve waves a CU).  us a call, 64 / 128 / 256 / 1,024 threads: bf16, 120,000 rows of 100 columns, 128 queries 73 / - / 41 / 38,
-// 512: 103 / 80 / 70 / 83, 1,000: 135 / 108 / 111 / 142, 4,000: 356 / - / 351 / 469; 15,000 rows, 700 queries - / 40 / 37 / -, 1,000:
-// 56 / 44 / 54 / 82, 2,000: 66 / 67 / 75 / 139, 4,000: 125 / - / 157 / 283.
+// (twelve waves a CU).  us a call, 64 / 128 / 256 / 1,024 threads: bf16, 120,000 rows of 100 columns, 128 queries 74 / 54 / 42 / 38,
+// 512: 99 / 81 / 71 / 79, 1,000: 130 / 111 / 116 / 134, 4,000: 330 / 324 / 346 / 454; 15,000 rows, 700 queries 48 / 41 / 38 / 60, 1,000:
+// 53 / 44 / 54 / 79, 2,000: 62 / 68 / 76 / 137, 4,000: 109 / 111 / 140 / 265.
 template <int TYPE> static void launch_answer(const AnswerArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)a.n);
   if (a.n > 1536) hipLaunchKernelGGL((k_answer<TYPE, 64, 32>), grid, dim3(64), 0, st, a);

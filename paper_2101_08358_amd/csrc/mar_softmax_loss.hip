@@ -2,9 +2,9 @@
 // weighted sum of rows for every query), k_loss_rows (joins the parts: log-sum-exp, loss, the queries' gradient), pass 2 (the
 // table's gradient, scores computed again), k_loss_table (adds its parts).
 //
-// 10,000 queries, 14,951 rows of 100 floats, us: layout 7, pass 1 210 (1,050 TFLOP/s of 16-bit products counting padded columns), k_loss_rows
-// 22, pass 2 240, k_loss_table 6; 8,192 queries, 65,536 bf16 rows of 400 columns: 20, 900 to 960, 17, 1,060 to 1,110.  A large
-// library product reaches 1,170 TFLOP/s on the card, whose clock gives way to its power limit.
+// 10,000 queries, 14,951 rows of 100 floats, us: layout 7, pass 1 208 (1,050 TFLOP/s of 16-bit products counting padded columns), k_loss_rows
+// 23, pass 2 244, k_loss_table 6; 8,192 queries, 65,536 bf16 rows of 400 columns: 20, 900 to 970, 18, 1,050 to 1,100.  A large
+// library product reaches 1,170 TFLOP/s on the card (1,190 to 1,240 on others), whose clock gives way to its power limit.
 #include "mar_softmax_dev.h"
 
 struct LossArgs {
