@@ -232,7 +232,7 @@ int mar_dropout(const void* x, int64_t x_stride, int64_t rows, int32_t dim, int3
  * scaled by the row's own largest value in mar_log_probs, and by that of the row's block in mar_softmax_loss: rows 8 k .. 8 k + 7
  * of the table, or those of them that count among the queries (as accurate as fp32 down to rows 2^-17 of that; and down to
  * 2^-100, in a table whose blocks' largest values are not 2^100 apart).  Scores that are not finite, or of 2^23 and more (whose
- * own rounding is a half), may make the results of their query NaN or infinite.
+ * own rounding is a half), may make the results of their query, and the table's gradient where it counts, NaN or infinite.
  */
 #define MAR_SOFTMAX_MAX_ROWS    ((int64_t)0x1fffff00)   /* below 2^29: ids, tiles and units stay clear of 32 bits */
 #define MAR_SOFTMAX_MAX_QUERIES 0x3ffff00

@@ -24,8 +24,8 @@ template <int TYPE> __device__ __forceinline__ v16f sm_mfma(v8s a, v8s b, v16f c
 }
 // Largest finite magnitude's bits.
 __device__ __forceinline__ int finite_bits(float v) { const int b = __float_as_int(v) & 0x7fffffff; return b < 0x7f800000 ? b : 0; }
-// Exponent of a row or of a block of eight whose largest finite magnitude has these bits: 2^e max lies in [2^14, 2^15).  Zeros take 80: the second
-// product's weights are 2^(t - e), and one far from the others' exponents would leave the floats' range.
+// Exponent of a row or of a block of eight whose largest finite magnitude has these bits: 2^e max lies in [2^14, 2^15).  Zeros take 80:
+// the second product's weights are 2^(t - e), and one far from the others' exponents would leave the floats' range.
 __device__ __forceinline__ int sm_exponent(int max_bits) { return max_bits == 0 ? 80 : min(141 - (max_bits >> 23), 116); }
 __device__ __forceinline__ void sm_parts8(const float (&v)[8], float scale, v8s& hi, v8s& lo) {
   v8h h, l;
@@ -181,7 +181,7 @@ __device__ __forceinline__ float own_float(int k) { return __int_as_float(k < 0 
 // add to log 1, and to 0 (with references 12 below, differences of numbers near 12 log 2: off by 5e-7).
 #define SM_ABOVE 15.f
 #define SM_BELOW 12.f
-#define SM_SUM_ABOVE 60.f
+#define SM_SUM_ABOVE 90.f         // 2^29 rows' sum stays a float; a block of zeros (exponent 80) beside rows of up to 2^20 moves nothing
 #define SM_CHAIN 16               // tiles whose weights are summed before their sum is added to the part's: chains of fp32 sums stay short
 
 // How the streamed rows come: SM_IMAGES: both matrices as images.  SM_ROWS: from the rows themselves, a tile staged by the
