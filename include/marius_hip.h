@@ -296,6 +296,94 @@ int mar_softmax_loss(const mar_softmax* problem, const void* queries, const void
                      void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * Tables held in microscaled 4-bit floats: an eighth of fp32's memory and traffic where a model only answers.  32 columns of a row (a
+ * block; the last one of a row is filled up with zeros) share a scale 2^e, e = floor(log2 of the block's largest magnitude) - 2, held as
+ * the byte e + 127 (0 .. 254; 0 for a block of zeros).  A column is a code: bits 0 - 2 the level 0, 0.5, 1, 1.5, 2, 3, 4, 6 nearest to its magnitude
+ * times 2^-e, ties to the even code, at most 6 (so that magnitudes between 6 and 8 times the scale end at 6); bit 3 its sign.  The
+ * even column of a byte lies in its low four bits.  A block that holds a value that is not finite: scale byte 255, codes 0; its columns
+ * read back as NaN.
+ *   codes        : device, rows of 16 ceil(dim / 32) bytes, 16-byte aligned; codes_stride bytes from row to row, a multiple of 16
+ *   scales       : device, rows of ceil(dim / 32) bytes; scales_stride bytes from row to row
+ * mar_mxfp_quantise writes both from x, whole blocks of every row.
+ * mar_mxfp_rows writes the values of n given rows (ids: device, [n], or NULL: rows 0 .. n - 1; the same id may come twice) as fp32 or
+ * bf16 (exact) or fp16 (rounded to the nearest), infinite above the type's range; an id outside 0 .. num_rows - 1 gives a row of zeros.
+ *   x, out : device, rows of dim values, any stride of at least dim.  rows, num_rows, n < 2^31, 1 <= dim <= MAR_MXFP_MAX_COLUMNS.
+ * Outputs must not overlap inputs.
+ */
+#define MAR_DTYPE_MXFP4 3                                   /* queries of mar_mxfp_scores alone */
+#define MAR_MXFP_MAX_COLUMNS (1 << 24)
+int mar_mxfp_quantise(const void* x, int64_t x_stride, int64_t rows, int32_t dim, int32_t dtype, uint8_t* codes, int64_t codes_stride,
+                      uint8_t* scales, int64_t scales_stride, void* hip_stream);
+int mar_mxfp_rows(const uint8_t* codes, int64_t codes_stride, const uint8_t* scales, int64_t scales_stride, int64_t num_rows, int32_t dim,
+                  const int32_t* ids, int64_t n, int32_t dtype, void* out, int64_t out_stride, void* hip_stream);
+
+/*
+ * Scores of queries against every row of such a table: scores[i][j] = scale * (query_i . row_j), rounded to score_dtype.
+ * The table's values are exact, products too, sums are held in fp32.  Queries: fp32 values are taken to 24 bits, bf16 and fp16 ones
+ * to 19 bits, counted down from the largest magnitude of their block of 32 columns (fewer where that is below 2^-100),
+ * MAR_DTYPE_MXFP4 ones (codes as above with query_scales) as they are.  A query with a value that is not finite
+ * has scores NaN, and so has a row.
+ *   queries, codes, scales, scores : device; query_scales: device, for MAR_DTYPE_MXFP4
+ *   workspace : device, >= mar_mxfp_scores_workspace_bytes of the same problem, 256-byte aligned; calls that may overlap in time need
+ *               one each
+ */
+typedef struct mar_mxfp {
+  int64_t num_rows;             /* rows of the table, 1 .. MAR_SOFTMAX_MAX_ROWS                        */
+  int64_t codes_stride, scales_stride;                              /* of the table, in bytes           */
+  int64_t query_stride;         /* elements (MAR_DTYPE_MXFP4: bytes) from one query to the next         */
+  int64_t query_scales_stride;  /* bytes; MAR_DTYPE_MXFP4 alone                                         */
+  int64_t score_stride;         /* elements from one query's scores to the next's, at least num_rows    */
+  int32_t num_queries;          /* 0 .. MAR_SOFTMAX_MAX_QUERIES                                         */
+  int32_t dim;                  /* 1 .. MAR_MAX_DIM                                                     */
+  int32_t dtype;                /* of the queries: MAR_DTYPE_*                                          */
+  int32_t score_dtype;          /* MAR_DTYPE_FP32, _BF16 or _FP16                                       */
+  float   scale;                /* multiplies every score: 1e-6 .. 1e6                                  */
+  int32_t reserved;             /* must be 0                                                            */
+} mar_mxfp;
+int mar_mxfp_scores_workspace_bytes(const mar_mxfp* problem, size_t* out_bytes);
+int mar_mxfp_scores(const mar_mxfp* problem, const void* queries, const uint8_t* query_scales, const uint8_t* codes, const uint8_t* scales,
+                    void* scores, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Rows drawn by their scores, as answers or as hard negatives.  For query i the rows that count (allowed, and their score neither NaN
+ * nor -infinity; +infinity counts as the largest float) are ranked by descending score, equal ones by id; row j weighs
+ * w_j = exp((s_ij - s_i,best) / temperature).  Kept are the rows of rank below top_k whose predecessors' weights sum to less than
+ * top_p times the sum of the first top_k ones, and that weigh at least min_p.  Draw n of query i is the first kept row, by id, at
+ * which the kept rows' running sum of weights exceeds uniforms[i][n] times their whole sum.
+ * Weights are integers of 60 to 61 bits for their whole sum, from exponentials in 64 bits: sums are exact, whatever their order, and
+ * results depend on the arguments alone.
+ *   scores      : device, [num_queries] rows of num_rows values
+ *   allowed     : device, or NULL (all rows): bits as in mar_log_probs
+ *   temperatures, top_ks, top_ps, min_ps : device, [num_queries], each may be NULL: then the problem's value serves all queries.
+ *                 temperature 0 (or, in the array, below, or NaN): the best row; top_k 0 (or below): all rows; top_p of 1 and more or
+ *                 NaN: all, of 0 and less: the best row; min_p of 0 and less or NaN: all, of 1 and more: rows that score like the best
+ *   uniforms    : device, [num_queries][num_draws] in [0, 1) (below or NaN: 0; 1 and more: the last kept row)
+ *   ids         : device, out, [num_queries][num_draws]; -1 where no row counts
+ *   log_probs   : device, out, [num_queries][num_draws], or NULL: log probability of each draw among the kept rows; -infinity where
+ *                 no row counts
+ *   num_kept    : device, out, [num_queries], or NULL: kept rows
+ *   workspace   : device, >= mar_sample_rows_workspace_bytes of the same problem, 256-byte aligned; calls that may overlap in time
+ *                 need one each
+ */
+typedef struct mar_sampling {
+  int64_t num_rows;      /* scores of a query, 1 .. MAR_SOFTMAX_MAX_ROWS                                */
+  int64_t score_stride;  /* elements from one query's scores to the next's, num_rows .. 2^40            */
+  int32_t num_queries;   /* 0 .. MAR_SOFTMAX_MAX_QUERIES                                                */
+  int32_t num_draws;     /* of every query, 1 .. MAR_MAX_DRAWS                                          */
+  int32_t dtype;         /* of the scores: MAR_DTYPE_FP32, _BF16 or _FP16                               */
+  int32_t top_k;         /* >= 0                                                                        */
+  float   temperature;   /* >= 0                                                                        */
+  float   top_p;         /* 0 .. 1                                                                      */
+  float   min_p;         /* 0 .. 1                                                                      */
+  int32_t reserved;      /* must be 0                                                                   */
+} mar_sampling;
+#define MAR_MAX_DRAWS 65536
+int mar_sample_rows_workspace_bytes(const mar_sampling* problem, size_t* out_bytes);
+int mar_sample_rows(const mar_sampling* problem, const void* scores, const uint32_t* allowed, int64_t allowed_stride,
+                    const float* temperatures, const int32_t* top_ks, const float* top_ps, const float* min_ps, const float* uniforms,
+                    int32_t* ids, float* log_probs, int32_t* num_kept, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Edge-bucket ordering for out-of-memory training (Sec. 4.1).  Host-only: all pointers are HOST memory.
  *   mar_beta_buffer_sequence  : Alg. 3.  Writes the sequence of partition buffers, row r = the c partition
  *                               ids in the buffer at step r; successive rows differ by one swapped

@@ -13,8 +13,10 @@ _lib = None
 
 MODEL_DISTMULT, MODEL_COMPLEX, MODEL_TRANSE, MODEL_DOT = 0, 1, 2, 3
 PRECISION_FP32, PRECISION_SPLIT_BF16 = 0, 1
-DTYPE_FP32, DTYPE_BF16, DTYPE_FP16 = 0, 1, 2
+DTYPE_FP32, DTYPE_BF16, DTYPE_FP16, DTYPE_MXFP4 = 0, 1, 2, 3
 MAX_TOP = 32
+MAX_DRAWS = 65536
+MXFP_MAX_COLUMNS = 1 << 24
 NUM_PHASES = 6
 PHASE_NAMES = ("index", "gather", "score_softmax_gq", "neg_grad", "chain_rule", "reduce_adagrad")
 
@@ -44,10 +46,23 @@ class MarSoftmax(ctypes.Structure):
                 ("num_queries", ctypes.c_int32), ("dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
+class MarMxfp(ctypes.Structure):
+    _fields_ = [("num_rows", ctypes.c_int64), ("codes_stride", ctypes.c_int64), ("scales_stride", ctypes.c_int64), ("query_stride", ctypes.c_int64),
+                ("query_scales_stride", ctypes.c_int64), ("score_stride", ctypes.c_int64), ("num_queries", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("score_dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class MarSampling(ctypes.Structure):
+    _fields_ = [("num_rows", ctypes.c_int64), ("score_stride", ctypes.c_int64), ("num_queries", ctypes.c_int32), ("num_draws", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("top_k", ctypes.c_int32), ("temperature", ctypes.c_float), ("top_p", ctypes.c_float),
+                ("min_p", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
 EXPORTS = ("mar_workspace_bytes", "mar_init_tables", "mar_sample_negatives", "mar_train_batch", "mar_eval_scores",
            "mar_eval_filter", "mar_rank_metrics", "mar_rank_metrics_static", "mar_beta_buffer_sequence", "mar_beta_edge_bucket_order", "mar_buffer_simulate",
            "mar_swap_lower_bound", "mar_beta_swap_count", "mar_dropout", "mar_log_probs_workspace_bytes", "mar_log_probs",
-           "mar_softmax_loss_workspace_bytes", "mar_softmax_loss",
+           "mar_softmax_loss_workspace_bytes", "mar_softmax_loss", "mar_mxfp_quantise", "mar_mxfp_rows", "mar_mxfp_scores_workspace_bytes",
+           "mar_mxfp_scores", "mar_sample_rows_workspace_bytes", "mar_sample_rows",
            "mar_pipe_workspace_bytes", "mar_pipe_create", "mar_pipe_submit", "mar_pipe_drain", "mar_pipe_destroy",
            "mar_profile_enable", "mar_profile_read", "mar_destroy", "mar_last_error")
 
@@ -80,6 +95,12 @@ def load_library():
     lib.mar_log_probs.argtypes = [ctypes.POINTER(MarSoftmax), vp, vp, vp, vp, i64, i32, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.mar_softmax_loss_workspace_bytes.argtypes = [ctypes.POINTER(MarSoftmax), ctypes.POINTER(ctypes.c_size_t)]
     lib.mar_softmax_loss.argtypes = [ctypes.POINTER(MarSoftmax), vp, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp, ctypes.c_size_t, vp]
+    lib.mar_mxfp_quantise.argtypes = [vp, i64, i64, i32, i32, vp, i64, vp, i64, vp]
+    lib.mar_mxfp_rows.argtypes = [vp, i64, vp, i64, i64, i32, vp, i64, i32, vp, i64, vp]
+    lib.mar_mxfp_scores_workspace_bytes.argtypes = [ctypes.POINTER(MarMxfp), ctypes.POINTER(ctypes.c_size_t)]
+    lib.mar_mxfp_scores.argtypes = [ctypes.POINTER(MarMxfp), vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.mar_sample_rows_workspace_bytes.argtypes = [ctypes.POINTER(MarSampling), ctypes.POINTER(ctypes.c_size_t)]
+    lib.mar_sample_rows.argtypes = [ctypes.POINTER(MarSampling), vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.mar_beta_buffer_sequence.argtypes = [i32, i32, vp, i64, ctypes.POINTER(i64)]
     lib.mar_beta_edge_bucket_order.argtypes = [i32, i32, i32, u64, vp]
     lib.mar_buffer_simulate.argtypes = [i32, i32, vp, i64, ctypes.POINTER(i64)]
@@ -206,6 +227,40 @@ def mar_softmax_loss(problem, queries, table, targets, weights, loss, lse, grad_
     _check(load_library().mar_softmax_loss(ctypes.byref(problem), _ptr(queries), _ptr(table), _ptr(targets), _ptr(weights),
                                            _ptr(loss), _ptr(lse), _ptr(grad_queries), int(grad_query_stride), _ptr(grad_table),
                                            int(grad_row_stride), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def mar_mxfp_quantise(x, x_stride, rows, dim, dtype, codes, codes_stride, scales, scales_stride, stream=None):
+    _check(load_library().mar_mxfp_quantise(_ptr(x), int(x_stride), int(rows), int(dim), int(dtype), _ptr(codes), int(codes_stride), _ptr(scales),
+                                            int(scales_stride), _stream(stream)))
+
+
+def mar_mxfp_rows(codes, codes_stride, scales, scales_stride, num_rows, dim, ids, n, dtype, out, out_stride, stream=None):
+    _check(load_library().mar_mxfp_rows(_ptr(codes), int(codes_stride), _ptr(scales), int(scales_stride), int(num_rows), int(dim), _ptr(ids),
+                                        int(n), int(dtype), _ptr(out), int(out_stride), _stream(stream)))
+
+
+def mar_mxfp_scores_workspace_bytes(problem):
+    out = ctypes.c_size_t(0)
+    _check(load_library().mar_mxfp_scores_workspace_bytes(ctypes.byref(problem), ctypes.byref(out)))
+    return out.value
+
+
+def mar_mxfp_scores(problem, queries, query_scales, codes, scales, scores, workspace, workspace_bytes, stream=None):
+    _check(load_library().mar_mxfp_scores(ctypes.byref(problem), _ptr(queries), _ptr(query_scales), _ptr(codes), _ptr(scales), _ptr(scores),
+                                          _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def mar_sample_rows_workspace_bytes(problem):
+    out = ctypes.c_size_t(0)
+    _check(load_library().mar_sample_rows_workspace_bytes(ctypes.byref(problem), ctypes.byref(out)))
+    return out.value
+
+
+def mar_sample_rows(problem, scores, allowed, allowed_stride, temperatures, top_ks, top_ps, min_ps, uniforms, ids, log_probs, num_kept,
+                    workspace, workspace_bytes, stream=None):
+    _check(load_library().mar_sample_rows(ctypes.byref(problem), _ptr(scores), _ptr(allowed), int(allowed_stride), _ptr(temperatures),
+                                          _ptr(top_ks), _ptr(top_ps), _ptr(min_ps), _ptr(uniforms), _ptr(ids), _ptr(log_probs),
+                                          _ptr(num_kept), _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 def mar_swap_lower_bound(p, c):
