@@ -11,6 +11,7 @@
 // Lane layouts (lane = 32 h + m): A lane holds query m, block 2 k + h of step k; B lane the same block of table row m; D lane holds
 // row m, register r = query 8 (r / 4) + 4 h + r % 4.
 #include "mar_common.h"
+#include "mar_flash.h"
 #include "mar_mxfp.h"
 #include "mar_rows_dev.h"
 #include "mar_softmax.h"
@@ -21,9 +22,10 @@ typedef float mx_f16 __attribute__((ext_vector_type(16)));
 // Images of 32 queries each: [slice][step]: 16 bytes of every lane, then (6-bit slices) 8 more; then the scales of every slice, a byte a step.
 template <int NK, int NS> struct MxImage {
   static constexpr int FRAG = NS == 1 ? 1024 : 1536, NW = (NK + 3) / 4;
-  static constexpr int SCALES = NS * NK * FRAG, BYTES = SCALES + NS * NW * 256;
+  static constexpr int SCALES = NS * NK * FRAG, BYTES = (SCALES + NS * NW * 256 + 1023) / 1024 * 1024;
 };
-static int mx_image_bytes(int nk, int ns) { return ns * nk * (ns == 1 ? 1024 : 1536) + ns * ((nk + 3) / 4) * 256; }
+static int mx_image_bytes(int nk, int ns) { return (ns * nk * (ns == 1 ? 1024 : 1536) + ns * ((nk + 3) / 4) * 256 + 1023) / 1024 * 1024; }
+constexpr int mx_slices_of(int type) { return type == MAR_DTYPE_MXFP4 ? 1 : (type == MAR_DTYPE_FP32 ? 5 : 4); }
 
 struct MxArgs {
   const void* queries; const uint8_t* query_scales;
@@ -35,182 +37,277 @@ struct MxArgs {
   float scale;
 };
 
-// A thread per lane of a step's operand.
-template <int TYPE, int NK, int NS>
-__global__ void __launch_bounds__(256)
-k_mxfp_pack(MxArgs a) {
+// One of the 256 NK pieces of an image: eight columns of a block of one query (four neighbouring threads a block).
+template <int TYPE, int NK>
+__device__ __forceinline__ void mx_pack(const MxArgs& a, int64_t tile, int piece, char* image) {
+  constexpr int NS = mx_slices_of(TYPE);
   typedef MxImage<NK, NS> I;
-  const int lane = threadIdx.x & 63, unit = (int)blockIdx.x * 4 + (threadIdx.x >> 6), tile = unit / NK, k = unit - tile * NK;
-  const int64_t q = (int64_t)tile * 32 + (lane & 31);
-  if ((int64_t)tile * 32 >= a.n) return;
-  const int b = 2 * k + (lane >> 5);
+  const int part = piece & 3, lane = piece >> 2 & 63, k = piece >> 8, b = 2 * k + (lane >> 5);
+  const int64_t q = tile * 32 + (lane & 31);
   const bool in = q < a.n && b < a.row_blocks;
-  char* image = a.images + (size_t)tile * I::BYTES;
   uint8_t* scales = (uint8_t*)image + I::SCALES + ((k / 4) * 64 + lane) * 4 + k % 4;
-  if constexpr (TYPE == 3) {
-    row_u4 c = {0u, 0u, 0u, 0u};
-    if (in) c = *reinterpret_cast<const row_u4*>((const uint8_t*)a.queries + q * a.query_stride + 16 * b);
-    *reinterpret_cast<row_u4*>(image + k * 1024 + lane * 16) = c;
-    *scales = in ? a.query_scales[q * a.query_scales_stride + b] : (uint8_t)127;
+  if constexpr (TYPE == MAR_DTYPE_MXFP4) {
+    unsigned c = 0;
+    if (in) c = *reinterpret_cast<const unsigned*>((const uint8_t*)a.queries + q * a.query_stride + 16 * b + 4 * part);
+    *reinterpret_cast<unsigned*>(image + k * 1024 + lane * 16 + 4 * part) = c;
+    if (part == 0) *scales = in ? a.query_scales[q * a.query_scales_stride + b] : (uint8_t)127;
   } else {
     typedef typename RowType<TYPE>::T T;
-    float v[32];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float part[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (in) load8<TYPE>((const T*)a.queries + q * a.query_stride, 32 * b + 8 * j, a.dim, part);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[8 * j + e] = part[e];
-    }
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (in) load8<TYPE>((const T*)a.queries + q * a.query_stride, 32 * b + 8 * part, a.dim, v);
     unsigned largest = 0;
 #pragma unroll
-    for (int e = 0; e < 32; ++e) largest = max(largest, __float_as_uint(v[e]) & 0x7fffffffu);
+    for (int e = 0; e < 8; ++e) largest = max(largest, __float_as_uint(v[e]) & 0x7fffffffu);
+    largest = max(largest, (unsigned)__shfl_xor((int)largest, 1));
+    largest = max(largest, (unsigned)__shfl_xor((int)largest, 2));
     const bool finite = largest < 0x7f800000u;
     const int field = max((int)(largest >> 23), 1);        // e + 127
 #pragma unroll
-    for (int e = 0; e < 32; ++e) v[e] = finite ? __builtin_ldexpf(v[e], 130 - field) : 0.f;   // largest in [8, 16)
+    for (int e = 0; e < 8; ++e) v[e] = finite ? __builtin_ldexpf(v[e], 130 - field) : 0.f;   // the block's largest in [8, 16)
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-      unsigned w[6] = {0u, 0u, 0u, 0u, 0u, 0u};
-      const bool held = field - 5 * s >= 0;                // scales end at 2^-127
+      unsigned long long w = 0;
 #pragma unroll
-      for (int e = 0; e < 32; ++e) {
+      for (int e = 0; e < 8; ++e) {
         const float d = rintf(v[e]);
         v[e] = (v[e] - d) * 32.f;
-        const unsigned c = (unsigned)fabsf(d) | (__float_as_uint(d) >> 31) << 5;
-        const int at = 6 * e;
-        w[at / 32] |= c << (at % 32);
-        if (at % 32 > 26) w[at / 32 + 1] |= c >> (32 - at % 32);
+        w |= (unsigned long long)((unsigned)fabsf(d) | (__float_as_uint(d) >> 31) << 5) << (6 * e);
       }
+      if (field - 5 * s < 0) w = 0;                        // scales end at 2^-127
       char* frag = image + (s * NK + k) * I::FRAG;
-      row_u4 lo = {w[0], w[1], w[2], w[3]};
-      uint2 hi = make_uint2(w[4], w[5]);
-      if (!held) { lo = (row_u4)(0u); hi = make_uint2(0u, 0u); }
-      *reinterpret_cast<row_u4*>(frag + lane * 16) = lo;
-      *reinterpret_cast<uint2*>(frag + 1024 + lane * 8) = hi;
-      scales[s * I::NW * 256] = (uint8_t)(finite ? max(field - 5 * s, 0) : 255);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const int byte = 6 * part + 2 * i;
+        *reinterpret_cast<unsigned short*>(frag + (byte < 16 ? lane * 16 + byte : 1024 + lane * 8 + byte - 16)) = (unsigned short)(w >> (16 * i));
+      }
+      if (part == 0) scales[s * I::NW * 256] = (uint8_t)(finite ? max(field - 5 * s, 0) : 255);
     }
   }
 }
+// A workgroup a tile and step.
+template <int TYPE, int NK>
+__global__ void __launch_bounds__(256)
+k_mxfp_pack(MxArgs a) {
+  const int64_t tile = blockIdx.x / NK;
+  mx_pack<TYPE, NK>(a, tile, (int)(blockIdx.x - tile * NK) * 256 + threadIdx.x, a.images + (size_t)tile * MxImage<NK, mx_slices_of(TYPE)>::BYTES);
+}
 
-// One slice's products with RT x 32 rows: step K's scales are byte K % 4 of their words.
-template <int K, int NK, int NS, int RT>
-__device__ __forceinline__ void mx_steps(const char* frags, int lane, const int* qs, const row_u4 (&w)[RT][NK], const int (&ws)[RT][(NK + 3) / 4], mx_f16 (&acc)[RT]) {
-  if constexpr (K < NK) {
-    typedef MxImage<NK, NS> I;
-    mx_v8 q = {0, 0, 0, 0, 0, 0, 0, 0};
-    const row_u4 lo = *reinterpret_cast<const row_u4*>(frags + K * I::FRAG + lane * 16);
+// Step J of an image's products with RT x 32 rows: slice NS - 1 - J / NK, so that the smallest comes first, block pair J % NK, whose scales
+// are byte J % NK % 4 of their words.  The next step's operand is read ahead of its products.
+template <int NK, int NS>
+__device__ __forceinline__ mx_v8 mx_operand(const char* image, int lane, int j) {
+  typedef MxImage<NK, NS> I;
+  const char* frag = image + ((NS - 1 - j / NK) * NK + j % NK) * I::FRAG;
+  mx_v8 q = {0, 0, 0, 0, 0, 0, 0, 0};
+  const row_u4 lo = *reinterpret_cast<const row_u4*>(frag + lane * 16);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) q[i] = (int)lo[i];
-    if constexpr (NS > 1) {
-      const uint2 hi = *reinterpret_cast<const uint2*>(frags + K * I::FRAG + 1024 + lane * 8);
-      q[4] = (int)hi.x; q[5] = (int)hi.y;
-    }
+  for (int i = 0; i < 4; ++i) q[i] = (int)lo[i];
+  if constexpr (NS > 1) {
+    const uint2 hi = *reinterpret_cast<const uint2*>(frag + 1024 + lane * 8);
+    q[4] = (int)hi.x; q[5] = (int)hi.y;
+  }
+  return q;
+}
+template <int J, int NK, int NS, int RT>
+__device__ __forceinline__ void mx_steps(const char* image, int lane, const mx_v8& q, const int (&qs)[NS][(NK + 3) / 4], const row_u4 (&w)[RT][NK],
+                                         const int (&ws)[RT][(NK + 3) / 4], mx_f16 (&acc)[RT]) {
+  if constexpr (J < NS * NK) {
+    constexpr int S = NS - 1 - J / NK, K = J % NK;
+    mx_v8 next = q;
+    if constexpr (J + 1 < NS * NK) next = mx_operand<NK, NS>(image, lane, J + 1);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       const mx_v8 r = {(int)w[t][K][0], (int)w[t][K][1], (int)w[t][K][2], (int)w[t][K][3], 0, 0, 0, 0};
       // operand types: 2 = 6 bits (2 exponent, 3 mantissa), 4 = 4 bits
-      acc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(q, r, acc[t], NS > 1 ? 2 : 4, 4, K % 4, qs[K / 4], K % 4, ws[t][K / 4]);
+      acc[t] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(q, r, acc[t], NS > 1 ? 2 : 4, 4, K % 4, qs[S][K / 4], K % 4, ws[t][K / 4]);
     }
-    mx_steps<K + 1, NK, NS, RT>(frags, lane, qs, w, ws, acc);
+    __builtin_amdgcn_sched_barrier(0);
+    mx_steps<J + 1, NK, NS, RT>(image, lane, next, qs, w, ws, acc);
   }
 }
 
-// A wave holds 32 RT rows of the table in registers, lane m's RT rows neighbours, and takes the queries' images one by one out of LDS.
-template <int NK, int NS, int RT>
-__global__ void __launch_bounds__(256)
-k_mxfp_scores(MxArgs a) {
-  typedef MxImage<NK, NS> I;
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 31, h = lane >> 5;
-  const int part = (int)blockIdx.x / a.stripes, stripe = (int)blockIdx.x - part * a.stripes;
-  const int row0 = (stripe * 4 + wave) * 32 * RT + m * RT;
-  const int tiles = (a.n + 31) / 32, t0 = part * a.tiles_part, t1 = min(tiles, t0 + a.tiles_part);
-
-  row_u4 w[RT][NK];
-  int ws[RT][I::NW];
+// A wave's 32 RT rows of the table, lane m's RT neighbours from row0 on, block 2 k + h.  Rows beyond the last are taken for it and not written.
+template <int NK, int RT>
+__device__ __forceinline__ void mx_load_rows(const MxArgs& a, int row0, int h, row_u4 (&w)[RT][NK], int (&ws)[RT][(NK + 3) / 4]) {
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
-    const int64_t row = min(row0 + t, a.num_rows - 1);     // rows beyond the last are taken and not written
+    const int64_t row = min(row0 + t, a.num_rows - 1);
     const uint8_t* codes = a.codes + row * a.codes_stride;
     const uint8_t* scales = a.scales + row * a.scales_stride;
 #pragma unroll
-    for (int k = 0; k < I::NW; ++k) ws[t][k] = 0;
+    for (int k = 0; k < (NK + 3) / 4; ++k) ws[t][k] = 0;
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
       const int b = 2 * k + h;
-      w[t][k] = (row_u4)(0u);
       unsigned s = 0;
+      w[t][k] = (row_u4)(0u);
       if (b < a.row_blocks) { w[t][k] = *reinterpret_cast<const row_u4*>(codes + 16 * b); s = scales[b]; }
-      ws[t][k / 4] |= s << (8 * (k % 4));
+      ws[t][k / 4] |= (int)(s << (8 * (k % 4)));
     }
   }
-  for (int tile = t0; tile < t1; ++tile) {
-    __syncthreads();
-    const char* image = a.images + (size_t)tile * I::BYTES;
-    for (int at = tid * 16; at < I::BYTES; at += 256 * 16) *reinterpret_cast<row_u4*>(smem + at) = *reinterpret_cast<const row_u4*>(image + at);
-    __syncthreads();
-    mx_f16 acc[RT];
+}
+
+// All slices of an image, the smallest first.
+template <int NK, int NS, int RT>
+__device__ __forceinline__ void mx_tile(const char* image, int lane, const row_u4 (&w)[RT][NK], const int (&ws)[RT][(NK + 3) / 4], mx_f16 (&acc)[RT]) {
+  typedef MxImage<NK, NS> I;
+  int qs[NS][I::NW];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) acc[t] = (mx_f16)(0.f);
+  for (int s = 0; s < NS; ++s) {
 #pragma unroll
-    for (int s = NS - 1; s >= 0; --s) {
-      int qs[I::NW];
+    for (int k = 0; k < I::NW; ++k) qs[s][k] = *reinterpret_cast<const int*>(image + I::SCALES + ((s * I::NW + k) * 64 + lane) * 4);
+  }
 #pragma unroll
-      for (int k = 0; k < I::NW; ++k) qs[k] = *reinterpret_cast<const int*>(smem + I::SCALES + ((s * I::NW + k) * 64 + lane) * 4);
-      mx_steps<0, NK, NS, RT>(smem + s * NK * I::FRAG, lane, qs, w, ws, acc);
+  for (int t = 0; t < RT; ++t) acc[t] = (mx_f16)(0.f);
+  mx_steps<0, NK, NS, RT>(image, lane, mx_operand<NK, NS>(image, lane, 0), qs, w, ws, acc);
+}
+
+// Scores of 32 queries from `q0` on and a lane's RT neighbouring rows: a wave instruction writes two queries' 32 RT scores.
+template <int TYPE, int RT>
+__device__ __forceinline__ void mx_store(const MxArgs& a, int64_t q0, int row0, int h, bool whole, const mx_f16 (&acc)[RT]) {
+  typedef typename RowType<TYPE>::T T;
+  T* base = (T*)a.out + (q0 + 4 * h) * a.out_stride + row0;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int i = 8 * (r / 4) + r % 4;
+    T* to = base + i * a.out_stride;
+    T v[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) v[t] = (T)(acc[t][r] * a.scale);
+    if (whole) { __builtin_memcpy(to, v, sizeof(v)); continue; }
+    if (q0 + i >= a.n) break;                              // uniform: half 0's queries come first
+    if (q0 + i + 4 * h < a.n) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) if (row0 + t < a.num_rows) to[t] = v[t];
     }
+  }
+}
+template <int RT>
+__device__ __forceinline__ void mx_store_any(const MxArgs& a, int64_t q0, int row0, int h, bool whole, const mx_f16 (&acc)[RT]) {
+  if (a.out_type == MAR_DTYPE_FP32) { if (whole) mx_store<0, RT>(a, q0, row0, h, true, acc); else mx_store<0, RT>(a, q0, row0, h, false, acc); }
+  else if (a.out_type == MAR_DTYPE_BF16) { if (whole) mx_store<1, RT>(a, q0, row0, h, true, acc); else mx_store<1, RT>(a, q0, row0, h, false, acc); }
+  else { if (whole) mx_store<2, RT>(a, q0, row0, h, true, acc); else mx_store<2, RT>(a, q0, row0, h, false, acc); }
+}
+
+// Many queries: eight waves hold 32 RT rows each and take the images out of LDS, G at a time; the next G are copied there meanwhile.
+template <int NK, int NS> constexpr int mx_group() { return MxImage<NK, NS>::BYTES > 16 * 1024 ? 1 : 32 * 1024 / MxImage<NK, NS>::BYTES; }
+template <int NK, int NS, int RT>
+__global__ void __launch_bounds__(512)
+k_mxfp_scores(MxArgs a) {
+  typedef MxImage<NK, NS> I;
+  constexpr int G = mx_group<NK, NS>(), STAGE = G * I::BYTES;
+  __shared__ __attribute__((aligned(16))) char smem[2 * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+  const int part = (int)blockIdx.x / a.stripes, stripe = (int)blockIdx.x - part * a.stripes;
+  const int first = (stripe * 8 + wave) * 32 * RT, row0 = first + (lane & 31) * RT;
+  const int tiles = (a.n + 31) / 32, t0 = part * a.tiles_part, t1 = min(tiles, t0 + a.tiles_part);
+  // images t .. t + G - 1, those that there are, by loads that write LDS, 1 KB a wave instruction.  In asm: the compiler would have
+  // every read of LDS wait for them, of the other half too
+  int token = 0;
+  auto copy = [&](int t, int buf) {
+    const int bytes = min(G, t1 - t) * I::BYTES;
+    const v4i words = buf_words(a.images + (size_t)t * I::BYTES, (uint32_t)bytes);
+    const unsigned to = (unsigned)(unsigned long long)(__attribute__((address_space(3))) const char*)smem + buf * STAGE;
+    for (int at = wave * 1024; at < bytes; at += 8 * 1024) buf_load4_to_lds(words, to + at, lane * 16, at, token);
+  };
+  copy(t0, 0);
+  row_u4 w[RT][NK];
+  int ws[RT][I::NW];
+  mx_load_rows<NK, RT>(a, row0, h, w, ws);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  for (int t = t0, buf = 0; t < t1; t += G, buf ^= 1) {
+    if (t + G < t1) copy(t + G, buf ^ 1);
+    const int here = min(G, t1 - t);
+    for (int g = 0; g < here; ++g) {
+      mx_f16 acc[RT];
+      mx_tile<NK, NS, RT>(smem + buf * STAGE + g * I::BYTES, lane, w, ws, acc);
+      // the copies have landed; the last tile's scores need not have: nothing waits for them at the barrier
+      if (g == here - 1) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      const int64_t q0 = (int64_t)(t + g) * 32;
+      mx_store_any<RT>(a, q0, row0, h, first + 32 * RT <= a.num_rows && q0 + 32 <= a.n, acc);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  }
+}
+
+// Up to 32 queries: every workgroup lays out their image for itself and its waves go through the table, the next rows on their way.
+template <int TYPE, int NK, int RT>
+__global__ void __launch_bounds__(256)
+k_mxfp_few(MxArgs a) {
+  constexpr int NS = mx_slices_of(TYPE);
+  typedef MxImage<NK, NS> I;
+  __shared__ __attribute__((aligned(16))) char image[I::BYTES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, at = (lane & 31) * RT;
+  row_u4 w[RT][NK], next[RT][NK];
+  int ws[RT][I::NW], next_s[RT][I::NW];
+  int stripe = (int)blockIdx.x * 4 + wave;
+  mx_load_rows<NK, RT>(a, min(stripe, a.stripes - 1) * 32 * RT + at, h, w, ws);
+  for (int piece = tid; piece < 256 * NK; piece += 256) mx_pack<TYPE, NK>(a, 0, piece, image);
+  __syncthreads();
+  for (; stripe < a.stripes; stripe += (int)gridDim.x * 4) {
+    const int following = stripe + (int)gridDim.x * 4;
+    if (following < a.stripes) mx_load_rows<NK, RT>(a, following * 32 * RT + at, h, next, next_s);
+    mx_f16 acc[RT];
+    mx_tile<NK, NS, RT>(image, lane, w, ws, acc);
+    mx_store_any<RT>(a, 0, stripe * 32 * RT + at, h, stripe * 32 * RT + 32 * RT <= a.num_rows && a.n == 32, acc);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int64_t q = (int64_t)tile * 32 + 8 * (r / 4) + 4 * h + r % 4;
-      float v[RT];
+    for (int t = 0; t < RT; ++t) {
 #pragma unroll
-      for (int t = 0; t < RT; ++t) v[t] = acc[t][r] * a.scale;
-      if (q < a.n) {
-        if (a.out_type == 0) store_cols<0, RT>((float*)a.out + q * a.out_stride, row0, a.num_rows, v);
-        else if (a.out_type == 1) store_cols<1, RT>((__bf16*)a.out + q * a.out_stride, row0, a.num_rows, v);
-        else store_cols<2, RT>((_Float16*)a.out + q * a.out_stride, row0, a.num_rows, v);
-      }
+      for (int k = 0; k < NK; ++k) w[t][k] = next[t][k];
+#pragma unroll
+      for (int k = 0; k < I::NW; ++k) ws[t][k] = next_s[t][k];
     }
   }
 }
 
 // ------------------------------------------------------------------------------------------ launches -----
-static int mx_slices(int dtype) { return dtype == MAR_DTYPE_MXFP4 ? 1 : (dtype == MAR_DTYPE_FP32 ? 5 : 4); }
 static int64_t mx_tiles(int64_t queries) { return (queries + 31) / 32; }
 
-struct MxPlan { int rt, stripes, parts, tiles_part; };
+struct MxPlan { bool few; int rt, stripes, parts, tiles_part, grid; };
+// Few queries: workgroups that stay, two a CU.  Else a workgroup a stripe of rows and part of the queries' tiles: one a CU at a time,
+// estimated by the rounds of workgroups and their tiles, a workgroup's rows and first images costing some two tiles.
 static MxPlan mx_plan(const mar_mxfp* p) {
-  MxPlan r;
+  MxPlan r = {};
   const int64_t tiles = mx_tiles(p->num_queries);
-  r.rt = p->num_rows * tiles >= 4 * 32 * 1024 ? 4 : 1;
-  r.stripes = (int)((p->num_rows + 128 * r.rt - 1) / (128 * r.rt));
-  int64_t parts = (1024 + r.stripes - 1) / r.stripes;
-  if (parts > tiles) parts = tiles;
-  r.tiles_part = (int)((tiles + parts - 1) / parts);
-  r.parts = (int)((tiles + r.tiles_part - 1) / r.tiles_part);
+  const int nk = (p->dim + 63) / 64;
+  r.few = tiles <= 1;
+  if (r.few) {
+    r.rt = p->num_rows <= 64 * 1024 ? 1 : (nk <= 3 ? 4 : 2);
+    r.stripes = (int)((p->num_rows + 32 * r.rt - 1) / (32 * r.rt));
+    r.grid = (r.stripes + 3) / 4 < 512 ? (r.stripes + 3) / 4 : 512;
+    return r;
+  }
+  r.rt = p->num_rows * tiles >= 2048 * 1024 ? 4 : 1;
+  r.stripes = (int)((p->num_rows + 256 * r.rt - 1) / (256 * r.rt));
+  const int64_t slots = 256;
+  int64_t best = INT64_MAX;
+  for (int64_t k = 1; k <= tiles && k <= 1024 && k * r.stripes <= 1 << 22; k += 1 + k / 32) {
+    const int64_t each = (tiles + k - 1) / k, parts = (tiles + each - 1) / each, cost = (r.stripes * parts + slots - 1) / slots * (each + 2);
+    if (cost < best) { best = cost; r.parts = (int)parts; r.tiles_part = (int)each; }
+  }
+  r.grid = r.stripes * r.parts;
   return r;
 }
 
-template <int TYPE, int NK> static void launch_pack(const MxArgs& a, hipStream_t st) {
-  constexpr int NS = TYPE == 3 ? 1 : (TYPE == 0 ? 5 : 4);
-  const int64_t units = mx_tiles(a.n) * NK;
-  hipLaunchKernelGGL((k_mxfp_pack<TYPE, NK, NS>), dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st, a);
-}
-template <int NK> static void launch_nk(int dtype, int rt, const MxArgs& a, hipStream_t st) {
-  if (dtype == MAR_DTYPE_FP32) launch_pack<0, NK>(a, st); else if (dtype == MAR_DTYPE_BF16) launch_pack<1, NK>(a, st);
-  else if (dtype == MAR_DTYPE_FP16) launch_pack<2, NK>(a, st); else launch_pack<3, NK>(a, st);
-  const dim3 grid((unsigned)(a.stripes * a.parts)), block(256);
-  const int ns = mx_slices(dtype);
-  if (rt == 4) {
-    if (ns == 5) hipLaunchKernelGGL((k_mxfp_scores<NK, 5, 4>), grid, block, (MxImage<NK, 5>::BYTES), st, a);
-    else if (ns == 4) hipLaunchKernelGGL((k_mxfp_scores<NK, 4, 4>), grid, block, (MxImage<NK, 4>::BYTES), st, a);
-    else hipLaunchKernelGGL((k_mxfp_scores<NK, 1, 4>), grid, block, (MxImage<NK, 1>::BYTES), st, a);
-  } else {
-    if (ns == 5) hipLaunchKernelGGL((k_mxfp_scores<NK, 5, 1>), grid, block, (MxImage<NK, 5>::BYTES), st, a);
-    else if (ns == 4) hipLaunchKernelGGL((k_mxfp_scores<NK, 4, 1>), grid, block, (MxImage<NK, 4>::BYTES), st, a);
-    else hipLaunchKernelGGL((k_mxfp_scores<NK, 1, 1>), grid, block, (MxImage<NK, 1>::BYTES), st, a);
+template <int TYPE, int NK> static void launch_type(const MxPlan& plan, const MxArgs& a, hipStream_t st) {
+  constexpr int NS = mx_slices_of(TYPE);
+  const dim3 grid((unsigned)plan.grid);
+  if (plan.few) {
+    if (plan.rt == 1) hipLaunchKernelGGL((k_mxfp_few<TYPE, NK, 1>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_mxfp_few<TYPE, NK, (NK <= 3 ? 4 : 2)>), grid, dim3(256), 0, st, a);
+    return;
   }
+  hipLaunchKernelGGL((k_mxfp_pack<TYPE, NK>), dim3((unsigned)(mx_tiles(a.n) * NK)), dim3(256), 0, st, a);
+  if (plan.rt == 4) hipLaunchKernelGGL((k_mxfp_scores<NK, NS, 4>), grid, dim3(512), 0, st, a);
+  else hipLaunchKernelGGL((k_mxfp_scores<NK, NS, 1>), grid, dim3(512), 0, st, a);
+}
+template <int NK> static void launch_nk(int dtype, const MxPlan& plan, const MxArgs& a, hipStream_t st) {
+  if (dtype == MAR_DTYPE_FP32) launch_type<0, NK>(plan, a, st);
+  else if (dtype == MAR_DTYPE_BF16) launch_type<1, NK>(plan, a, st);
+  else if (dtype == MAR_DTYPE_FP16) launch_type<2, NK>(plan, a, st);
+  else launch_type<3, NK>(plan, a, st);
 }
 
 // ------------------------------------------------------------------------------------------ entry points -----
@@ -238,7 +335,7 @@ extern "C" int mar_mxfp_scores_workspace_bytes(const mar_mxfp* p, size_t* out_by
   int code;
   if (const char* why = mx_check(p, &code)) { mar_set_error("%s", why); return code; }
   if (!out_bytes) { mar_set_error("out_bytes is NULL"); return MAR_EINVAL; }
-  const size_t bytes = (size_t)mx_tiles(p->num_queries) * mx_image_bytes((p->dim + 63) / 64, mx_slices(p->dtype));
+  const size_t bytes = (size_t)mx_tiles(p->num_queries) * mx_image_bytes((p->dim + 63) / 64, mx_slices_of(p->dtype));
   *out_bytes = bytes > 256 ? bytes : 256;
   return MAR_OK;
 }
@@ -266,13 +363,13 @@ extern "C" int mar_mxfp_scores(const mar_mxfp* p, const void* queries, const uin
   a.out_type = p->score_dtype; a.stripes = plan.stripes; a.parts = plan.parts; a.tiles_part = plan.tiles_part; a.scale = p->scale;
   const hipStream_t st = (hipStream_t)hip_stream;
   switch ((p->dim + 63) / 64) {
-    case 1: launch_nk<1>(p->dtype, plan.rt, a, st); break;
-    case 2: launch_nk<2>(p->dtype, plan.rt, a, st); break;
-    case 3: launch_nk<3>(p->dtype, plan.rt, a, st); break;
-    case 4: launch_nk<4>(p->dtype, plan.rt, a, st); break;
-    case 5: launch_nk<5>(p->dtype, plan.rt, a, st); break;
-    case 6: launch_nk<6>(p->dtype, plan.rt, a, st); break;
-    default: launch_nk<7>(p->dtype, plan.rt, a, st); break;
+    case 1: launch_nk<1>(p->dtype, plan, a, st); break;
+    case 2: launch_nk<2>(p->dtype, plan, a, st); break;
+    case 3: launch_nk<3>(p->dtype, plan, a, st); break;
+    case 4: launch_nk<4>(p->dtype, plan, a, st); break;
+    case 5: launch_nk<5>(p->dtype, plan, a, st); break;
+    case 6: launch_nk<6>(p->dtype, plan, a, st); break;
+    default: launch_nk<7>(p->dtype, plan, a, st); break;
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) { mar_set_error("score kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
