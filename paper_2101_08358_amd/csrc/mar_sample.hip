@@ -1,232 +1,565 @@
 // Rows drawn from scores with temperature, top-k, top-p and min-p (gfx950).
 //
-// Ranks are by (score descending, id ascending), so that every filter is a threshold: a key tau above which all rows are kept and a number
-// of rows at tau, the first by id.  Weights are integers W = round(2^bits exp((s - max) / temperature)), bits such that their sum lies below
-// 2^61: sums are exact in any order, and a border (top-p's, a draw's) falls where the integers say, for every kernel here alike.
+// A row's place in the order (score descending, id ascending) is one number, so that every filter is a cut: rows whose place is not below it
+// are kept.  Weights are integers W = round(2^bits exp((s - max) / temperature)), bits such that their sum lies below 2^61: sums are exact
+// in any order, and a border (top-p's, a draw's) falls where the integers say, whatever way found it.
+//
+// Up to 16,384 rows (k_draw_small): a workgroup a query holds them in registers.  More:
+//   k_draw_scan    a workgroup a chunk: greatest key, rows that count, sum of weights in fp32; maxima of groups of rows
+//   k_draw_few     queries with top-k: the k-th largest of the groups' maxima bounds the k-th best row from below; rows that reach it are
+//                  picked from the groups whose maximum does, and everything else concerns those rows alone
+//   k_draw_hist    other queries with top-p: weights in fp32 by their binary order of magnitude, 1/32 apart; k_draw_range: the bins that
+//                  the border lies in, whatever the sums' rounding
+//   k_draw_weigh   every row's integer weight: the sum of all, the sums of segments of 512 rows above the range, the range's rows by themselves
+//   k_draw_rows    the border among those rows, then the draws: the segment by the sums before it, the row by a wave that weighs it again
+// What does not fit (borders among more rows than a list holds, top-k above 1,024 with a table too large for registers) goes through
+// all rows by digits, one workgroup a query, in the last kernel.
 #include "mar_sample_dev.h"
 
-#define DRAW_SEGMENT 512                                    // columns of a segment: a wave's eight a lane
-
-// Sums and maxima over a workgroup of 16 waves; everyone gets the result.
-template <typename T, typename F> __device__ __forceinline__ T draw_reduce(T v, T* slots, F join) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = join(v, __shfl_xor(v, o));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = slots[0];
-  for (int w = 1; w < (int)(blockDim.x >> 6); ++w) v = join(v, slots[w]);
-  return v;
+// ------------------------------------------------------------------------------------------ pieces -----
+template <int TYPE> __device__ __forceinline__ void draw_nothing(const DrawArgs& a, int64_t q) {
+  for (int d = threadIdx.x; d < a.draws; d += blockDim.x) {
+    a.ids[q * a.draws + d] = -1;
+    if (a.log_probs) a.log_probs[q * a.draws + d] = -__builtin_inff();
+  }
+  if (threadIdx.x == 0 && a.num_kept) a.num_kept[q] = 0;
 }
-// Exclusive prefix sums over a workgroup; the whole sum in `total`.
-template <typename T> __device__ __forceinline__ T draw_prefix(T v, T* slots, T& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  T run = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) { const T up = __shfl_up(run, o); if (lane >= o) run += up; }
-  __syncthreads();
-  if (lane == 63) slots[wave] = run;
-  __syncthreads();
-  T before = 0, all = 0;
-  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) { if (w < wave) before += slots[w]; all += slots[w]; }
-  total = all;
-  return before + run - v;
+__device__ __forceinline__ draw_u64 draw_target(float u, draw_u64 total) { return !(u > 0.f) ? 0 : (u >= 1.f ? total - 1 : draw_share_down(u, total)); }
+
+// What the chunks of a query say together (all threads; up to 256 chunks).
+struct DrawWhole { unsigned best, count; float sum; };
+__device__ __forceinline__ DrawWhole draw_whole(const DrawArgs& a, int64_t q, float c, draw_u64* slots) {
+  DrawWhole r = {0u, 0u, 0.f};
+  DrawChunk mine = {0u, 0u, 0.f};
+  if ((int)threadIdx.x < a.chunks) mine = a.stats[q * a.chunks + threadIdx.x];
+  r.best = draw_reduce(mine.best, (unsigned*)slots, [](unsigned x, unsigned y) { return x > y ? x : y; });
+  r.count = draw_sum(mine.count, (unsigned*)slots);
+  const float part = mine.best ? mine.sum * __builtin_amdgcn_exp2f(-draw_depth(draw_score(r.best), draw_score(mine.best), c)) : 0.f;
+  r.sum = draw_sum(part, (float*)slots);
+  return r;
 }
 
-// One workgroup a query.
+// The draws of a query: rows with place >= cut and weight >= least; mass: the segments' sums (LDS or memory), replaced by those before them.
 template <int TYPE>
-__global__ void __launch_bounds__(1024)
-k_sample(DrawArgs a, int64_t first) {
-  typedef typename RowType<TYPE>::T T;
-  __shared__ draw_u64 bins[2048], slots[16];
-  __shared__ unsigned found[2];
-  __shared__ draw_u64 found_sum;
-  const int64_t q = first + blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, threads = blockDim.x;
-  const T* scores = (const T*)a.scores + q * a.score_stride;
-  const uint32_t* allowed = a.allowed ? a.allowed + q * a.allowed_stride : nullptr;
-  const DrawParams par = draw_params(a, q);
-  auto max_of = [](unsigned x, unsigned y) { return x > y ? x : y; };
-  auto sum_of = [](auto x, auto y) { return x + y; };
-
-  // keys of columns c .. c + 7
-  auto load = [&](int c, unsigned (&key)[8]) {
-    float v[8];
-    load8<TYPE>(scores, c, a.rows, v);
-    const unsigned bits = allowed ? allowed[c >> 5] >> (c & 31) : 0xffu;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) key[e] = c + e < a.rows && (bits >> e & 1u) ? draw_key(v[e]) : 0u;
-  };
-  auto each = [&](auto f) {
-    for (int64_t c = 8 * tid; c < a.rows; c += 8 * threads) {
-      unsigned key[8];
-      load((int)c, key);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f(key[e]);
-    }
-  };
-
-  unsigned best = 0, count = 0;
-  each([&](unsigned k) { best = max(best, k); count += k != 0; });
-  best = draw_reduce(best, (unsigned*)slots, max_of);
-  count = draw_reduce(count, (unsigned*)slots, sum_of);
-  if (count == 0) {                                        // uniform
-    for (int d = tid; d < a.draws; d += threads) {
-      a.ids[q * a.draws + d] = -1;
-      if (a.log_probs) a.log_probs[q * a.draws + d] = -__builtin_inff();
-    }
-    if (tid == 0 && a.num_kept) a.num_kept[q] = 0;
-    return;
-  }
-  const double top = (double)draw_score(best);
-  auto distance = [&](unsigned k) { return ((double)draw_score(k) - top) * par.inv_temperature; };
-  float approx = 0.f;
-  each([&](unsigned k) { if (k) approx += __builtin_amdgcn_exp2f((float)(distance(k) * 1.4426950408889634)); });
-  approx = draw_reduce(approx, (float*)slots, sum_of);
-  const int bits = 60 - ilogbf(fmaxf(approx, 1.f));
-  auto weight = [&](unsigned k) { return draw_weight(distance(k), bits); };
-
-  // rows with a key above tau, and the first `at_tau` rows that have it
-  unsigned tau = 0, at_tau = 0;
-  // The largest key at which `of` summed over the keys from it upwards reaches `want`, by digits of 11, 11 and 10 bits; `above`: the
-  // sum over greater keys.
-  auto select = [&](draw_u64 want, unsigned least, auto of, draw_u64& above) {
-    unsigned prefix = 0;
-    draw_u64 over = 0;
-    for (int level = 0; level < 3; ++level) {
-      const int shift = level == 0 ? 21 : (level == 1 ? 10 : 0), width = level == 2 ? 10 : 11;
-      for (int i = tid; i < 2048; i += threads) bins[i] = 0;
-      __syncthreads();
-      each([&](unsigned k) {
-        if (k != 0 && k >= least && (level == 0 || k >> (shift + width) == prefix)) {
-          const draw_u64 w = of(k);
-          if (w) atomicAdd(&bins[k >> shift & ((1u << width) - 1)], w);
-        }
-      });
-      __syncthreads();
-      // thread i takes the i-th pair of bins from the top
-      for (int i0 = 0; i0 < 1024; i0 += threads) {
-        const int i = i0 + tid, hi = 2047 - 2 * i;
-        const draw_u64 x = bins[hi], y = bins[hi - 1];
-        draw_u64 all;
-        const draw_u64 before = over + draw_prefix(x + y, slots, all);
-        if (before < want && before + x + y >= want) {
-          const bool one = before + x >= want;
-          found[0] = (unsigned)(one ? hi : hi - 1);
-          found_sum = before + (one ? 0 : x);
-        }
-        over += all;
-      }
-      __syncthreads();
-      over = found_sum;
-      prefix = prefix << width | found[0];
-      __syncthreads();
-    }
-    above = over;
-    return prefix;
-  };
-  if (par.top_k > 0 && (unsigned)par.top_k < count) {
-    draw_u64 above;
-    tau = select((draw_u64)par.top_k, 0, [](unsigned) { return (draw_u64)1; }, above);
-    at_tau = (unsigned)(par.top_k - (int)above);
-  }
-  if (par.top_p < 2.f) {
-    draw_u64 all = 0;
-    each([&](unsigned k) { if (k > tau) all += weight(k); });
-    all = draw_reduce(all, slots, sum_of) + (tau ? at_tau * weight(tau) : 0);
-    draw_u64 want = draw_share_up(par.top_p, all);
-    if (want == 0) want = 1;
-    // rows at the border of top-k count fully here: the sum is reached at that key at the latest, and its rows are counted below
-    draw_u64 above;
-    const unsigned border = select(want, tau, [&](unsigned k) { return weight(k); }, above);
-    const draw_u64 w = weight(border);
-    tau = border; at_tau = (unsigned)((want - above + w - 1) / w);
-  }
-  const draw_u64 least = par.min_p > 0.f ? (draw_u64)__builtin_ceil(__builtin_ldexp((double)par.min_p, bits)) : 0;
-  const draw_u64 w_tau = tau ? weight(tau) : 0;
-
-  // mass above tau and rows at tau, segment by segment
-  draw_u64* mass = a.mass + q * a.segments;
-  uint32_t* ties = a.ties + q * a.segments;
-  unsigned kept = 0;
-  for (int seg = wave; seg < a.segments; seg += threads >> 6) {
-    const int64_t c = (int64_t)seg * DRAW_SEGMENT + 8 * lane;
-    draw_u64 sum = 0;
-    unsigned same = 0;
-    if (c < a.rows) {
-      unsigned key[8];
-      load((int)c, key);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (key[e] > tau) { const draw_u64 w = weight(key[e]); if (w >= least) { sum += w; ++kept; } }
-        same += tau != 0 && key[e] == tau;
-      }
-    }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) { sum += __shfl_xor(sum, o); same += __shfl_xor(same, o); }
-    if (lane == 0) { mass[seg] = sum; ties[seg] = same; }
-  }
-  kept = draw_reduce(kept, (unsigned*)slots, sum_of);
-  if (tid == 0 && a.num_kept) a.num_kept[q] = (int)(kept + (tau && w_tau >= least ? at_tau : 0));
-  if (w_tau < least) at_tau = 0;
-  __syncthreads();
-  // prefixes: rows at tau before the segment, mass before it
+__device__ __forceinline__ void draw_rows(const DrawArgs& a, int64_t q, const DrawRow<TYPE>& row, const DrawWeights& w, draw_u64 cut, draw_u64 least, draw_u64* mass,
+                                          draw_u64* slots) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, threads = blockDim.x;
   draw_u64 total = 0;
-  unsigned before_ties = 0;
   for (int s0 = 0; s0 < a.segments; s0 += threads) {
-    const int seg = s0 + tid;
-    const unsigned mine = seg < a.segments ? ties[seg] : 0;
-    unsigned all_ties;
-    const unsigned before = before_ties + draw_prefix(mine, (unsigned*)slots, all_ties);
-    before_ties += all_ties;
-    const unsigned taken = before >= at_tau ? 0 : min(mine, at_tau - before);
+    const int s = s0 + threadIdx.x;
     draw_u64 all;
-    const draw_u64 m = (seg < a.segments ? mass[seg] : 0) + taken * w_tau;
-    const draw_u64 start = total + draw_prefix(m, slots, all);
+    const draw_u64 m = s < a.segments ? mass[s] : 0, before = total + draw_prefix(m, slots, all);
     total += all;
-    if (seg < a.segments) { mass[seg] = start; ties[seg] = before; }
+    if (s < a.segments) mass[s] = before;
   }
   __syncthreads();
-  // a wave a draw
-  const double log_total = log(__builtin_ldexp((double)total, -bits));
-  for (int d = wave; d < a.draws; d += threads >> 6) {
-    const float u = a.uniforms[q * a.draws + d];
-    draw_u64 target = !(u > 0.f) ? 0 : (u >= 1.f ? total - 1 : draw_share_down(u, total));
-    int lo = 0, hi = a.segments;                           // the last segment that begins at or below the target
-    while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (mass[mid] <= target) lo = mid; else hi = mid; }
-    target -= mass[lo];
-    const int64_t c = (int64_t)lo * DRAW_SEGMENT + 8 * lane;
+  const double log_total = log(__builtin_ldexp((double)total, -w.bits));
+  for (int d = wave; d < a.draws; d += threads >> 6) {     // a wave a draw
+    draw_u64 target = draw_target(a.uniforms[q * a.draws + d], total);
+    // the last segment that begins at or below the target, 64 at a time
+    int from = 0, step = 1;
+    while ((int64_t)step * 64 < a.segments) step *= 64;
+    for (; step >= 1; step /= 64) {
+      const int64_t s = from + (int64_t)lane * step;
+      const bool below = s < a.segments && mass[s] <= target;
+      from += (__popcll(__ballot(below)) - 1) * step;      // lane 0 is
+    }
+    target -= mass[from];
+    const int64_t c = (int64_t)from * DRAW_SEGMENT + 8 * lane;
     unsigned key[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
-    if (c < a.rows) load((int)c, key);
-    unsigned same = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) same += tau != 0 && key[e] == tau;
-    unsigned rank = same;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const unsigned up = __shfl_up(rank, o); if (lane >= o) rank += up; }
-    rank += ties[lo] - same;
-    draw_u64 w[8], sum = 0;
+    if (c < a.rows) row.keys((int)c, key);
+    draw_u64 each[8], sum = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      w[e] = 0;
-      if (key[e] > tau) { w[e] = weight(key[e]); if (w[e] < least) w[e] = 0; }
-      else if (tau != 0 && key[e] == tau) { if (rank < at_tau) w[e] = w_tau; ++rank; }
-      sum += w[e];
+      each[e] = key[e] != 0 && draw_place(key[e], (unsigned)c + e) >= cut ? w.of(key[e]) : 0;
+      if (each[e] < least) each[e] = 0;
+      sum += each[e];
     }
-    draw_u64 run = sum;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const draw_u64 up = __shfl_up(run, o); if (lane >= o) run += up; }
-    draw_u64 start = run - sum;
+    const draw_u64 run = draw_wave_prefix(sum), start = run - sum;
     if (start <= target && target < run) {                 // one lane
-      int e = 0;
+      int at = 0;
       unsigned k = key[0];
-      draw_u64 at = start + w[0];
+      draw_u64 upto = start + each[0];
 #pragma unroll
-      for (int j = 1; j < 8; ++j) if (at <= target) { at += w[j]; e = j; k = key[j]; }
-      a.ids[q * a.draws + d] = (int)c + e;
-      if (a.log_probs) a.log_probs[q * a.draws + d] = (float)(distance(k) - log_total);
+      for (int j = 1; j < 8; ++j) if (upto <= target) { upto += each[j]; at = j; k = key[j]; }
+      a.ids[q * a.draws + d] = (int)c + at;
+      if (a.log_probs) a.log_probs[q * a.draws + d] = (float)(w.distance(k) - log_total);
     }
   }
+}
+
+// Everything by digits over all rows of a query.
+template <int TYPE>
+__device__ void draw_slowly(const DrawArgs& a, int64_t q, const DrawRow<TYPE>& row, const DrawParams& par, const DrawWhole& whole, draw_u64* mass, DrawShared& lds) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const DrawWeights w = draw_weights(whole.best, par, whole.sum);
+  auto each = [&](auto f) {
+    for (int64_t c = 8 * tid; c < a.rows; c += 8 * 1024) {
+      unsigned key[8];
+      row.keys((int)c, key);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f(draw_place(key[e], (unsigned)c + e));
+    }
+  };
+  auto ones = [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); };
+  draw_u64 cut = 1;
+  if (par.top_k > 0 && (unsigned)par.top_k < whole.count) cut = draw_border(lds, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
+  if (par.top_p < 2.f) {
+    draw_u64 all = 0;
+    each([&](draw_u64 place) { if (place >= cut) all += w.of((unsigned)(place >> 32)); });
+    all = draw_sum(all, lds.slots);
+    const draw_u64 want = draw_share_up(par.top_p, all), top_k = cut;
+    // rows below top-k's cut have no say: they come after the border
+    cut = draw_border(lds, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { if (place >= top_k) f(place, [&] { return w.of((unsigned)(place >> 32)); }); }); },
+                      [&](unsigned k) { return w.of(k); });
+  }
+  const draw_u64 least = w.least(par.min_p);
+  unsigned kept = 0;
+  for (int s = wave; s < a.segments; s += 16) {
+    const int64_t c = (int64_t)s * DRAW_SEGMENT + 8 * lane;
+    draw_u64 sum = 0;
+    if (c < a.rows) {
+      unsigned key[8];
+      row.keys((int)c, key);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (key[e] && draw_place(key[e], (unsigned)c + e) >= cut) { const draw_u64 x = w.of(key[e]); if (x >= least) { sum += x; ++kept; } }
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) mass[s] = sum;
+  }
+  kept = draw_sum(kept, (unsigned*)lds.slots);
+  if (tid == 0 && a.num_kept) a.num_kept[q] = (int)kept;
+  __syncthreads();
+  draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.slots);
+}
+
+// ------------------------------------------------------------------------------------------ up to 16,384 rows -----
+template <int TYPE>
+__global__ void __launch_bounds__(1024)
+k_draw_small(DrawArgs a, int64_t first) {
+  __shared__ DrawShared lds;
+  __shared__ draw_u64 starts[33];
+  const int64_t q = first + blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const DrawRow<TYPE> row(a, q);
+  const DrawParams par = draw_params(a, q);
+  unsigned key[2][8];                                       // columns 8 tid .. and 8,192 + 8 tid ..: a wave holds segments `wave` and 16 + wave
+  unsigned best = 0, count = 0;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) key[b][e] = 0u;
+    if (8192 * b + 8 * tid < a.rows) row.keys(8192 * b + 8 * tid, key[b]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { best = max(best, key[b][e]); count += key[b][e] != 0; }
+  }
+  best = draw_reduce(best, (unsigned*)lds.slots, [](unsigned x, unsigned y) { return x > y ? x : y; });
+  count = draw_sum(count, (unsigned*)lds.slots);
+  if (count == 0) { draw_nothing<TYPE>(a, q); return; }    // uniform
+  const float c = draw_depth_scale(par), top = draw_score(best);
+  float approx = 0.f;
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) if (key[b][e]) approx += __builtin_amdgcn_exp2f(-draw_depth(top, draw_score(key[b][e]), c));
+  approx = draw_sum(approx, (float*)lds.slots);
+  const DrawWeights w = draw_weights(best, par, approx);
+  draw_u64 cut = 1;
+  if (par.top_k > 0 && (unsigned)par.top_k < count) {
+    auto ones = [&](auto f) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f(draw_place(key[b][e], (unsigned)(8192 * b + 8 * tid + e)), draw_one);
+    };
+    cut = draw_border(lds, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
+  }
+  draw_u64 weight[2][8], sum[2] = {0, 0};
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      weight[b][e] = key[b][e] && draw_place(key[b][e], (unsigned)(8192 * b + 8 * tid + e)) >= cut ? w.of(key[b][e]) : 0;
+      sum[b] += weight[b][e];
+    }
+  if (par.top_p < 2.f) {
+    const draw_u64 want = draw_share_up(par.top_p, draw_sum(sum[0] + sum[1], lds.slots));
+    auto each = [&](auto f) {                              // what top-k leaves out weighs nothing
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f(draw_place(key[b][e], (unsigned)(8192 * b + 8 * tid + e)), [&] { return weight[b][e]; });
+    };
+    cut = max(cut, draw_border(lds, want ? want : 1, 0, each, [&](unsigned k) { return w.of(k); }));
+  }
+  const draw_u64 least = w.least(par.min_p);
+  unsigned kept = 0;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    sum[b] = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const bool in = key[b][e] && draw_place(key[b][e], (unsigned)(8192 * b + 8 * tid + e)) >= cut && weight[b][e] >= least;
+      kept += in;
+      if (!in) weight[b][e] = 0;
+      sum[b] += weight[b][e];
+    }
+  }
+  if (a.num_kept) {                                        // uniform
+    kept = draw_sum(kept, (unsigned*)lds.slots);
+    if (tid == 0) a.num_kept[q] = (int)kept;
+  }
+  draw_u64 run[2];
+  __syncthreads();
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    run[b] = draw_wave_prefix(sum[b]);
+    if (lane == 63) starts[16 * b + wave] = run[b];
+  }
+  __syncthreads();
+  if (wave == 0) {
+    const draw_u64 m = lane < 32 ? starts[lane] : 0, upto = draw_wave_prefix(m);
+    if (lane < 32) starts[lane] = upto - m;
+    if (lane == 31) starts[32] = upto;
+  }
+  __syncthreads();
+  const draw_u64 total = starts[32];
+  const double log_total = log(__builtin_ldexp((double)total, -w.bits));
+  // every wave goes through all draws and takes those that fall into its segments
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const draw_u64 begin = starts[16 * b + wave], end = starts[16 * b + wave + 1], before = begin + run[b] - sum[b];
+    if (begin == end) continue;
+    for (int d0 = 0; d0 < a.draws; d0 += 64) {
+      const int d = d0 + lane;
+      const draw_u64 t = d < a.draws ? draw_target(a.uniforms[q * a.draws + d], total) : ~(draw_u64)0;
+      draw_u64 mine = __ballot(t >= begin && t < end);
+      while (mine) {                                       // uniform
+        const int i = __ffsll((long long)mine) - 1;
+        mine &= mine - 1;
+        const draw_u64 target = __shfl(t, i);
+        if (before <= target && target < before + sum[b]) {        // one lane
+          int at = 0;
+          unsigned k = key[b][0];
+          draw_u64 upto = before + weight[b][0];
+#pragma unroll
+          for (int j = 1; j < 8; ++j) if (upto <= target) { upto += weight[b][j]; at = j; k = key[b][j]; }
+          a.ids[q * a.draws + d0 + i] = 8192 * b + 8 * tid + at;
+          if (a.log_probs) a.log_probs[q * a.draws + d0 + i] = (float)(w.distance(k) - log_total);
+        }
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------ more rows -----
+// A workgroup a chunk of a query.  Group (chunk, block b, thread): the thread's columns of the iterations of block b.
+template <int TYPE>
+__global__ void __launch_bounds__(256)
+k_draw_scan(DrawArgs a, int64_t first) {
+  __shared__ draw_u64 slots[16];
+  const int64_t unit = first + blockIdx.x, q = unit / a.chunks;
+  const int chunk = (int)(unit - q * a.chunks), tid = threadIdx.x;
+  const DrawRow<TYPE> row(a, q);
+  const DrawParams par = draw_params(a, q);
+  const bool few = draw_few(a, par);
+  const float c = draw_depth_scale(par);
+  const int begin = chunk * a.chunk_rows, end = (int)min((int64_t)a.rows, (int64_t)begin + a.chunk_rows);
+  const int turns = a.chunk_rows / 2048, turns_block = (turns + a.blocks - 1) / a.blocks;
+  unsigned best = 0, count = 0, group = 0;
+  float sum = 0.f, top = 0.f;
+  unsigned* maxima = a.maxima + q * a.groups + (int64_t)chunk * a.blocks * 256 + tid;
+  int block = 0, left = turns_block;
+  for (int i = 0; i < turns; ++i) {
+    const int64_t at = (int64_t)begin + i * 2048 + 8 * tid;
+    if (at < end) {
+      unsigned key[8], here = 0;
+      row.keys((int)at, key);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) { here = max(here, key[e]); count += key[e] != 0; }
+      group = max(group, here);
+      if (here > best) {
+        const float now = draw_score(here);
+        sum = best ? sum * __builtin_amdgcn_exp2f(-draw_depth(now, top, c)) : 0.f;
+        best = here; top = now;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += key[e] ? __builtin_amdgcn_exp2f(-draw_depth(top, draw_score(key[e]), c)) : 0.f;
+    }
+    if (--left == 0 || i + 1 == turns) {
+      if (few) maxima[256 * block] = group;
+      group = 0; ++block; left = turns_block;
+    }
+  }
+  if (few) for (; block < a.blocks; ++block) maxima[256 * block] = 0;
+  const unsigned all = draw_reduce(best, (unsigned*)slots, [](unsigned x, unsigned y) { return x > y ? x : y; });
+  count = draw_sum(count, (unsigned*)slots);
+  sum = best ? sum * __builtin_amdgcn_exp2f(-draw_depth(draw_score(all), top, c)) : 0.f;
+  sum = draw_sum(sum, (float*)slots);
+  if (tid == 0) {
+    a.stats[q * a.chunks + chunk] = {all, count, sum};
+    if (chunk == 0) a.listed[q] = 0;
+  }
+}
+
+// Queries with top-k: a workgroup a query.
+template <int TYPE>
+__global__ void __launch_bounds__(1024)
+k_draw_few(DrawArgs a, int64_t first) {
+  __shared__ DrawShared lds;
+  __shared__ draw_u64 list[4 * DRAW_FEW];
+  __shared__ draw_u64 near_mass[2048];
+  __shared__ unsigned listed;
+  const int64_t q = first + blockIdx.x;
+  const DrawParams par = draw_params(a, q);
+  if (!draw_few(a, par)) return;                           // uniform
+  const int tid = threadIdx.x;
+  const DrawRow<TYPE> row(a, q);
+  const DrawWhole whole = draw_whole(a, q, draw_depth_scale(par), lds.slots);
+  if (whole.count == 0) { draw_nothing<TYPE>(a, q); return; }
+  const unsigned* maxima = a.maxima + q * a.groups;
+  // the k-th largest maximum: k rows at least reach it
+  const draw_u64 bound = draw_border(lds, (draw_u64)par.top_k, 0, [&](auto f) { for (int g = tid; g < a.groups; g += 1024) f((draw_u64)(maxima[g] ? maxima[g] : 1u) << 32, draw_one); },
+                                     [](unsigned) { return draw_one(); }) >> 32;
+  if (tid == 0) listed = 0;
+  __syncthreads();
+  const int turns = a.chunk_rows / 2048, turns_block = (turns + a.blocks - 1) / a.blocks, per_chunk = a.blocks * 256;
+  for (int g = tid; g < a.groups; g += 1024) {
+    if (maxima[g] < bound || maxima[g] == 0) continue;
+    const int chunk = g / per_chunk, block = (g - chunk * per_chunk) / 256, thread = g & 255;
+    const int end = (int)min((int64_t)a.rows, (int64_t)(chunk + 1) * a.chunk_rows);
+    for (int i = block * turns_block; i < min(turns, (block + 1) * turns_block); ++i) {
+      const int64_t c = (int64_t)chunk * a.chunk_rows + i * 2048 + 8 * thread;
+      if (c >= end) break;
+      unsigned key[8];
+      row.keys((int)c, key);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (key[e] >= bound && key[e]) {
+        const unsigned at = atomicAdd(&listed, 1u);
+        if (at < 4 * DRAW_FEW) list[at] = draw_place(key[e], (unsigned)c + e);
+      }
+    }
+  }
+  __syncthreads();
+  const unsigned n = listed;
+  draw_u64* mass = a.segments <= 2048 ? near_mass : a.mass + q * a.segments;
+  if (n > 4 * DRAW_FEW) { draw_slowly<TYPE>(a, q, row, par, whole, mass, lds); return; }     // uniform: many equal scores
+  const DrawWeights w = draw_weights(whole.best, par, whole.sum);
+  auto each = [&](auto f) { for (unsigned i = tid; i < n; i += 1024) f(list[i]); };
+  draw_u64 cut = bound << 32;                              // the listed rows and no others
+  if ((unsigned)par.top_k < n) cut = draw_border(lds, (draw_u64)par.top_k, 0, [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); }, [](unsigned) { return draw_one(); });
+  if (par.top_p < 2.f) {
+    draw_u64 all = 0;
+    each([&](draw_u64 place) { if (place >= cut) all += w.of((unsigned)(place >> 32)); });
+    const draw_u64 want = draw_share_up(par.top_p, draw_sum(all, lds.slots)), top_k = cut;
+    cut = draw_border(lds, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { if (place >= top_k) f(place, [&] { return w.of((unsigned)(place >> 32)); }); }); },
+                      [&](unsigned k) { return w.of(k); });
+  }
+  const draw_u64 least = w.least(par.min_p);
+  for (int s = tid; s < a.segments; s += 1024) mass[s] = 0;
+  __syncthreads();
+  unsigned kept = 0;
+  each([&](draw_u64 place) {
+    if (place < cut) return;
+    const draw_u64 x = w.of((unsigned)(place >> 32));
+    if (x < least) return;
+    ++kept;
+    if (x) atomicAdd(&mass[~(unsigned)place / DRAW_SEGMENT], x);
+  });
+  kept = draw_sum(kept, (unsigned*)lds.slots);
+  if (tid == 0 && a.num_kept) a.num_kept[q] = (int)kept;
+  __syncthreads();
+  draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.slots);
+}
+
+// Other queries with top-p: a chunk's weights by their bins.
+template <int TYPE>
+__global__ void __launch_bounds__(256)
+k_draw_hist(DrawArgs a, int64_t first) {
+  __shared__ unsigned bins[DRAW_BINS];
+  __shared__ draw_u64 slots[16];
+  const int64_t unit = first + blockIdx.x, q = unit / a.chunks;
+  const int chunk = (int)(unit - q * a.chunks), tid = threadIdx.x;
+  const DrawParams par = draw_params(a, q);
+  if (draw_few(a, par) || !draw_all(a, par) || par.top_p >= 2.f) return;
+  const DrawRow<TYPE> row(a, q);
+  const float c = draw_depth_scale(par);
+  for (int i = tid; i < DRAW_BINS; i += 256) bins[i] = 0;
+  const DrawWhole whole = draw_whole(a, q, c, slots);
+  const float top = draw_score(whole.best), unit_weight = (float)(1 << a.hist_bits);
+  auto bin_top = [](int bin) { return bin * (1.f / 32.f); };
+  const int begin = chunk * a.chunk_rows, end = (int)min((int64_t)a.rows, (int64_t)begin + a.chunk_rows);
+  for (int64_t at = (int64_t)begin + 8 * tid; at < end; at += 2048) {
+    unsigned key[8];
+    row.keys((int)at, key);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) if (key[e]) {
+      // 2^-x, x the depth below the bin's top, at most 1/32 but in the last bin: 1 - x ln 2 + (x ln 2)^2 / 2 is off by 2^-19 at most
+      const float depth = draw_depth(top, draw_score(key[e]), c), x = fminf(depth - bin_top(draw_bin(depth)), 1.f / 32.f);
+      atomicAdd(&bins[draw_bin(depth)], (unsigned)__builtin_fmaf(unit_weight, __builtin_fmaf(x, __builtin_fmaf(x, 0.24022651f, -0.69314718f), 1.f), 0.5f));
+    }
+  }
+  __syncthreads();
+  unsigned* out = a.hist + unit * DRAW_BINS;
+  for (int i = tid; i < DRAW_BINS; i += 256) out[i] = bins[i];
+}
+
+// The bins in which the border of top-p lies.  A weight in the histogram is off by 2^-17 of itself at most by its depth (up to 64, in fp32)
+// and polynomial and by half a unit, 2^-hist_bits at most of any but those below 2^-64: so are sums.
+__global__ void __launch_bounds__(1024)
+k_draw_range(DrawArgs a, int64_t first) {
+  __shared__ draw_u64 slots[16];
+  __shared__ int low, high;
+  const int64_t q = first + blockIdx.x;
+  const DrawParams par = draw_params(a, q);
+  const int tid = threadIdx.x;
+  if (draw_few(a, par) || !draw_all(a, par)) return;
+  if (par.top_p >= 2.f) { if (tid == 0) a.range[q] = {DRAW_BINS, DRAW_BINS}; return; }     // everything lies above
+  if (tid == 0) { low = DRAW_BINS - 1; high = DRAW_BINS - 1; }
+  draw_u64 nx = 0, ny = 0;                                 // bins 2 tid and 2 tid + 1
+  for (int k = 0; k < a.chunks; ++k) {
+    const uint2 v = *reinterpret_cast<const uint2*>(a.hist + (q * a.chunks + k) * DRAW_BINS + 2 * tid);
+    nx += v.x; ny += v.y;
+  }
+  const double x = (double)nx * exp2(-tid / 16.0), y = (double)ny * exp2(-tid / 16.0 - 1 / 32.0);
+  double all;
+  const double before = draw_prefix(x + y, (double*)slots, all), off = __builtin_ldexp(1.0, -a.hist_bits) + 0x1p-16, want = (double)par.top_p * all;
+  // the first bin at whose end the border may have been reached, and the first at whose end it must have been
+  const double may = want * (1.0 - off), must = want * (1.0 + off);
+  if (before < may && before + x + y >= may) low = before + x >= may ? 2 * tid : 2 * tid + 1;
+  if (before < must && before + x + y >= must) high = before + x >= must ? 2 * tid : 2 * tid + 1;
+  __syncthreads();
+  if (tid == 0) a.range[q] = {want <= 0.0 ? 0 : low, want <= 0.0 ? 0 : high};
+}
+
+// Integer weights of a chunk.
+template <int TYPE>
+__global__ void __launch_bounds__(256)
+k_draw_weigh(DrawArgs a, int64_t first) {
+  __shared__ draw_u64 slots[16], list[DRAW_LIST_CHUNK];
+  __shared__ unsigned listed, list_at;
+  const int64_t unit = first + blockIdx.x, q = unit / a.chunks;
+  const int chunk = (int)(unit - q * a.chunks), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (threadIdx.x == 0) listed = 0;
+  const DrawParams par = draw_params(a, q);
+  if (draw_few(a, par) || !draw_all(a, par)) return;
+  const DrawRow<TYPE> row(a, q);
+  const float c = draw_depth_scale(par);
+  const DrawWhole whole = draw_whole(a, q, c, slots);
+  if (whole.count == 0) return;
+  const DrawWeights w = draw_weights(whole.best, par, whole.sum);
+  const DrawRange range = a.range[q];
+  const draw_u64 least = w.least(par.min_p);
+  const float top = draw_score(whole.best);
+  const int begin = chunk * a.chunk_rows, end = (int)min((int64_t)a.rows, (int64_t)begin + a.chunk_rows);
+  draw_u64 all = 0, above = 0;
+  unsigned kept = 0;
+  for (int64_t s = (int64_t)begin + wave * DRAW_SEGMENT; s < end; s += 4 * DRAW_SEGMENT) {
+    const int64_t at = s + 8 * lane;
+    draw_u64 sum = 0;
+    if (at < end) {
+      unsigned key[8];
+      row.keys((int)at, key);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (key[e]) {
+        const draw_u64 x = w.of(key[e]);
+        all += x;
+        const int bin = range.low < DRAW_BINS ? draw_bin(draw_depth(top, draw_score(key[e]), c)) : 0;
+        if (bin < range.low) {
+          above += x;                                      // before min-p: top-p goes by it
+          if (x >= least) { sum += x; ++kept; }
+        } else if (bin <= range.high) {
+          const unsigned n = atomicAdd(&listed, 1u);
+          if (n < DRAW_LIST_CHUNK) list[n] = draw_place(key[e], (unsigned)at + e);
+        }
+      }
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) a.mass[q * a.segments + s / DRAW_SEGMENT] = sum;
+  }
+  all = draw_sum(all, slots);
+  above = draw_sum(above, slots);
+  kept = draw_sum(kept, (unsigned*)slots);
+  const unsigned n = listed;                               // the reductions' barriers lie behind the last one
+  if (threadIdx.x == 0) {
+    a.totals[2 * unit] = all; a.totals[2 * unit + 1] = above;
+    a.kept[unit] = kept;
+    // a chunk whose rows its list does not hold: more than the query's list holds, whatever the others add (256 chunks at most)
+    list_at = n ? atomicAdd(&a.listed[q], n > DRAW_LIST_CHUNK ? 1u << 22 : n) : 0;
+  }
+  if (n == 0 || n > DRAW_LIST_CHUNK) return;               // uniform
+  __syncthreads();
+  for (unsigned i = threadIdx.x; i < n; i += 256) if (list_at + i < (unsigned)a.list) a.lists[q * a.list + list_at + i] = list[i];
+}
+
+// The border among the range's rows, and the draws.
+template <int TYPE>
+__global__ void __launch_bounds__(1024)
+k_draw_rows(DrawArgs a, int64_t first) {
+  __shared__ DrawShared lds;
+  const int64_t q = first + blockIdx.x;
+  const DrawParams par = draw_params(a, q);
+  if (draw_few(a, par)) return;                            // uniform
+  const int tid = threadIdx.x;
+  const DrawRow<TYPE> row(a, q);
+  const DrawWhole whole = draw_whole(a, q, draw_depth_scale(par), lds.slots);
+  if (whole.count == 0) { draw_nothing<TYPE>(a, q); return; }
+  draw_u64* mass = a.mass + q * a.segments;
+  const unsigned n = a.listed[q];
+  if (!draw_all(a, par) || n > (unsigned)a.list) { draw_slowly<TYPE>(a, q, row, par, whole, mass, lds); return; }
+  const DrawWeights w = draw_weights(whole.best, par, whole.sum);
+  const draw_u64 least = w.least(par.min_p);
+  const bool in = tid < a.chunks;
+  unsigned kept = draw_sum(in ? a.kept[q * a.chunks + tid] : 0u, (unsigned*)lds.slots);
+  draw_u64 cut = 1;
+  if (par.top_p < 2.f) {
+    const draw_u64 all = draw_sum(in ? a.totals[2 * (q * a.chunks + tid)] : 0, lds.slots), above = draw_sum(in ? a.totals[2 * (q * a.chunks + tid) + 1] : 0, lds.slots);
+    const draw_u64 want = draw_share_up(par.top_p, all);
+    const draw_u64* list = a.lists + q * a.list;
+    auto each = [&](auto f) { for (unsigned i = tid; i < n; i += 1024) f(list[i]); };
+    draw_u64 listed = 0;
+    each([&](draw_u64 place) { listed += w.of((unsigned)(place >> 32)); });
+    listed = draw_sum(listed, lds.slots);
+    // temperatures whose inverse 32 bits do not hold: the histogram was of something else
+    if (above >= (want ? want : 1) || above + listed < want) { draw_slowly<TYPE>(a, q, row, par, whole, mass, lds); return; }     // uniform
+    cut = draw_border(lds, want ? want : 1, above, [&](auto f) { each([&](draw_u64 place) { f(place, [&] { return w.of((unsigned)(place >> 32)); }); }); },
+                      [&](unsigned k) { return w.of(k); });
+    unsigned more = 0;
+    each([&](draw_u64 place) {
+      if (place < cut) return;
+      const draw_u64 x = w.of((unsigned)(place >> 32));
+      if (x < least) return;
+      ++more;
+      if (x) atomicAdd(&mass[~(unsigned)place / DRAW_SEGMENT], x);
+    });
+    kept += draw_sum(more, (unsigned*)lds.slots);
+    __threadfence();                                       // the atomics passed this workgroup's cache by
+  }
+  if (tid == 0 && a.num_kept) a.num_kept[q] = (int)kept;
+  __syncthreads();
+  draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.slots);
+}
+
+// ------------------------------------------------------------------------------------------ launches -----
+// Kernels that no query of the call can need, as far as the host knows, are left out.
+template <int TYPE> static void launch_draws(const DrawArgs& a, int64_t queries, hipStream_t st) {
+  if (a.rows <= DRAW_SMALL) {
+    sm_launches(queries, 1024, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_small<TYPE>, dim3(n), dim3(1024), 0, st, a, first); });
+    return;
+  }
+  const bool greedy = !a.temperatures && a.temperature == 0.f;
+  const bool few = a.temperatures || a.top_ks || greedy || (a.top_k > 0 && a.top_k <= DRAW_FEW);
+  const bool all = a.top_ks || (!greedy && (a.top_k == 0 || a.top_k >= a.rows)), cuts = a.top_ps || a.top_p < 1.f;
+  sm_launches(queries * a.chunks, 256, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_scan<TYPE>, dim3(n), dim3(256), 0, st, a, first); });
+  if (few) sm_launches(queries, 1024, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_few<TYPE>, dim3(n), dim3(1024), 0, st, a, first); });
+  if (all) {
+    if (cuts) sm_launches(queries * a.chunks, 256, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_hist<TYPE>, dim3(n), dim3(256), 0, st, a, first); });
+    sm_launches(queries, 1024, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_range, dim3(n), dim3(1024), 0, st, a, first); });
+    sm_launches(queries * a.chunks, 256, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_weigh<TYPE>, dim3(n), dim3(256), 0, st, a, first); });
+  }
+  sm_launches(queries, 1024, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_rows<TYPE>, dim3(n), dim3(1024), 0, st, a, first); });
 }
 
 // ------------------------------------------------------------------------------------------ entry points -----
@@ -247,15 +580,37 @@ static const char* draw_check(const mar_sampling* p, int* code) {
   if (p->score_stride < p->num_rows || p->score_stride > (int64_t)1 << 40) return "score_stride is below num_rows or above 2^40";
   return nullptr;
 }
-struct DrawLayout { size_t mass, ties, bytes; int segments; };
+// Chunks: as many as fill the device some eight times, of 2,048 to 2^21 rows.  Blocks: groups enough for top-k's bound.
+struct DrawLayout { size_t stats, maxima, hist, range, totals, kept, listed, lists, mass, bytes; int segments, chunks, chunk_rows, blocks, groups, list, hist_bits; };
 static DrawLayout draw_layout(const mar_sampling* p) {
-  DrawLayout L;
+  DrawLayout L = {};
+  if (p->num_rows <= DRAW_SMALL || p->num_queries == 0) { L.bytes = 256; return L; }
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
+  const size_t Q = (size_t)p->num_queries;
   L.segments = (int)((p->num_rows + DRAW_SEGMENT - 1) / DRAW_SEGMENT);
-  L.mass = take((size_t)p->num_queries * L.segments * 8);
-  L.ties = take((size_t)p->num_queries * L.segments * 4);
-  L.bytes = at > 256 ? at : 256;
+  int64_t chunks = 2048 / p->num_queries;
+  if (chunks < (p->num_rows + (1 << 21) - 1) >> 21) chunks = (p->num_rows + (1 << 21) - 1) >> 21;
+  chunks = chunks < 1 ? 1 : (chunks > 256 ? 256 : chunks);
+  int64_t turns = (p->num_rows + 2048 * chunks - 1) / (2048 * chunks);
+  L.chunk_rows = (int)(2048 * turns);
+  L.chunks = (int)((p->num_rows + L.chunk_rows - 1) / L.chunk_rows);
+  int64_t blocks = 4096 / (256 * L.chunks);
+  L.blocks = (int)(blocks < 1 ? 1 : (blocks > turns ? turns : blocks));
+  L.groups = L.chunks * L.blocks * 256;
+  L.list = (int)(p->num_rows / 16 < DRAW_LIST ? p->num_rows / 16 : DRAW_LIST);
+  L.stats = take(Q * L.chunks * sizeof(DrawChunk));
+  L.maxima = take(Q * L.groups * 4);
+  L.hist = take(Q * L.chunks * DRAW_BINS * 4);
+  L.hist_bits = 16;                                        // a bin's sum of a chunk stays below 2^32
+  while ((int64_t)L.chunk_rows << L.hist_bits >= 1ll << 32) --L.hist_bits;
+  L.range = take(Q * sizeof(DrawRange));
+  L.totals = take(Q * L.chunks * 16);
+  L.kept = take(Q * L.chunks * 4);
+  L.listed = take(Q * 4);
+  L.lists = take(Q * L.list * 8);
+  L.mass = take(Q * L.segments * 8);
+  L.bytes = at;
   return L;
 }
 
@@ -286,13 +641,15 @@ extern "C" int mar_sample_rows(const mar_sampling* p, const void* scores, const 
   a.ids = ids; a.log_probs = log_probs; a.num_kept = num_kept; a.score_stride = p->score_stride; a.allowed_stride = allowed_stride;
   a.rows = (int32_t)p->num_rows; a.draws = p->num_draws; a.segments = L.segments;
   a.top_k = p->top_k; a.temperature = p->temperature; a.top_p = p->top_p; a.min_p = p->min_p;
-  a.mass = (draw_u64*)((char*)workspace + L.mass); a.ties = (uint32_t*)((char*)workspace + L.ties);
+  a.chunks = L.chunks; a.chunk_rows = L.chunk_rows; a.blocks = L.blocks; a.groups = L.groups; a.list = L.list;
+  char* const ws = (char*)workspace;
+  a.stats = (DrawChunk*)(ws + L.stats); a.maxima = (unsigned*)(ws + L.maxima); a.hist = (unsigned*)(ws + L.hist); a.hist_bits = L.hist_bits; a.range = (DrawRange*)(ws + L.range);
+  a.totals = (draw_u64*)(ws + L.totals); a.kept = (unsigned*)(ws + L.kept); a.listed = (unsigned*)(ws + L.listed); a.lists = (draw_u64*)(ws + L.lists);
+  a.mass = (draw_u64*)(ws + L.mass);
   const hipStream_t st = (hipStream_t)hip_stream;
-  sm_launches(p->num_queries, 1024, [&](int64_t first, unsigned blocks) {
-    if (p->dtype == MAR_DTYPE_FP32) hipLaunchKernelGGL(k_sample<0>, dim3(blocks), dim3(1024), 0, st, a, first);
-    else if (p->dtype == MAR_DTYPE_BF16) hipLaunchKernelGGL(k_sample<1>, dim3(blocks), dim3(1024), 0, st, a, first);
-    else hipLaunchKernelGGL(k_sample<2>, dim3(blocks), dim3(1024), 0, st, a, first);
-  });
+  if (p->dtype == MAR_DTYPE_FP32) launch_draws<0>(a, p->num_queries, st);
+  else if (p->dtype == MAR_DTYPE_BF16) launch_draws<1>(a, p->num_queries, st);
+  else launch_draws<2>(a, p->num_queries, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) { mar_set_error("sampling kernel: %s", hipGetErrorString(e)); return MAR_EHIP; }
   return MAR_OK;
