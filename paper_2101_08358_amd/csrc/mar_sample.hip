@@ -1,7 +1,7 @@
 // Rows drawn from scores with temperature, top-k, top-p and min-p (gfx950).
 //
 // A row's place in the order (score descending, id ascending) is one number, so that every filter is a cut: rows whose place is not below it
-// are kept.  Weights are integers W = round(2^bits exp((s - max) / temperature)), bits such that their sum lies below 2^61: sums are exact
+// are kept.  Weights are integers W = round(2^n exp((s - max) / temperature)), n such that their sum lies below 2^61: sums are exact
 // in any order, and a border (top-p's, a draw's) falls where the integers say, whatever way found it.
 //
 // Up to 16,384 rows (k_draw_small): a workgroup a query holds them in registers.  More:
@@ -27,13 +27,12 @@ template <int TYPE> __device__ __forceinline__ void draw_nothing(const DrawArgs&
 __device__ __forceinline__ draw_u64 draw_target(float u, draw_u64 total) { return !(u > 0.f) ? 0 : (u >= 1.f ? total - 1 : draw_share_down(u, total)); }
 
 // What the chunks of a query say together (all threads; up to 256 chunks).
-struct DrawWhole { unsigned best, count; float sum; };
+struct DrawWhole { unsigned best; float sum; };
 __device__ __forceinline__ DrawWhole draw_whole(const DrawArgs& a, int64_t q, float c, draw_u64* slots) {
-  DrawWhole r = {0u, 0u, 0.f};
-  DrawChunk mine = {0u, 0u, 0.f};
+  DrawWhole r = {0u, 0.f};
+  DrawChunk mine = {0u, 0.f};
   if ((int)threadIdx.x < a.chunks) mine = a.stats[q * a.chunks + threadIdx.x];
-  r.best = draw_reduce(mine.best, (unsigned*)slots, [](unsigned x, unsigned y) { return x > y ? x : y; });
-  r.count = draw_sum(mine.count, (unsigned*)slots);
+  r.best = draw_reduce(mine.best, (unsigned*)slots, DrawMax());
   const float part = mine.best ? mine.sum * __builtin_amdgcn_exp2f(-draw_depth(draw_score(r.best), draw_score(mine.best), c)) : 0.f;
   r.sum = draw_sum(part, (float*)slots);
   return r;
@@ -53,7 +52,7 @@ __device__ __forceinline__ void draw_rows(const DrawArgs& a, int64_t q, const Dr
     if (s < a.segments) mass[s] = before;
   }
   __syncthreads();
-  const double log_total = log(__builtin_ldexp((double)total, -w.bits));
+  const double log_total = w.log_sum(total);
   for (int d = wave; d < a.draws; d += threads >> 6) {     // a wave a draw
     draw_u64 target = draw_target(a.uniforms[q * a.draws + d], total);
     // the last segment that begins at or below the target, 64 at a time
@@ -103,14 +102,16 @@ __device__ void draw_slowly(const DrawArgs& a, int64_t q, const DrawRow<TYPE>& r
   };
   auto ones = [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); };
   draw_u64 cut = 1;
-  if (par.top_k > 0 && (unsigned)par.top_k < whole.count) cut = draw_border(lds, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
+  unsigned count = 0;
+  if (par.top_k > 0) { each([&](draw_u64 place) { count += place != 0; }); count = draw_sum(count, (unsigned*)lds.slots); }
+  if (par.top_k > 0 && (unsigned)par.top_k < count) cut = draw_border<false>(lds, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
   if (par.top_p < 2.f) {
     draw_u64 all = 0;
     each([&](draw_u64 place) { if (place >= cut) all += w.of((unsigned)(place >> 32)); });
     all = draw_sum(all, lds.slots);
     const draw_u64 want = draw_share_up(par.top_p, all), top_k = cut;
     // rows below top-k's cut have no say: they come after the border
-    cut = draw_border(lds, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { if (place >= top_k) f(place, [&] { return w.of((unsigned)(place >> 32)); }); }); },
+    cut = draw_border<false>(lds, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { if (place >= top_k) f(place, [&] { return w.of((unsigned)(place >> 32)); }); }); },
                       [&](unsigned k) { return w.of(k); });
   }
   const draw_u64 least = w.least(par.min_p);
@@ -124,8 +125,7 @@ __device__ void draw_slowly(const DrawArgs& a, int64_t q, const DrawRow<TYPE>& r
 #pragma unroll
       for (int e = 0; e < 8; ++e) if (key[e] && draw_place(key[e], (unsigned)c + e) >= cut) { const draw_u64 x = w.of(key[e]); if (x >= least) { sum += x; ++kept; } }
     }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
+    sum = draw_wave_sum(sum);
     if (lane == 0) mass[s] = sum;
   }
   kept = draw_sum(kept, (unsigned*)lds.slots);
@@ -154,7 +154,7 @@ k_draw_small(DrawArgs a, int64_t first) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) { best = max(best, key[b][e]); count += key[b][e] != 0; }
   }
-  best = draw_reduce(best, (unsigned*)lds.slots, [](unsigned x, unsigned y) { return x > y ? x : y; });
+  best = draw_reduce(best, (unsigned*)lds.slots, DrawMax());
   count = draw_sum(count, (unsigned*)lds.slots);
   if (count == 0) { draw_nothing<TYPE>(a, q); return; }    // uniform
   const float c = draw_depth_scale(par), top = draw_score(best);
@@ -173,7 +173,7 @@ k_draw_small(DrawArgs a, int64_t first) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) f(draw_place(key[b][e], (unsigned)(8192 * b + 8 * tid + e)), draw_one);
     };
-    cut = draw_border(lds, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
+    cut = draw_border<false>(lds, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
   }
   draw_u64 weight[2][8], sum[2] = {0, 0};
 #pragma unroll
@@ -189,9 +189,9 @@ k_draw_small(DrawArgs a, int64_t first) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f(draw_place(key[b][e], (unsigned)(8192 * b + 8 * tid + e)), [&] { return weight[b][e]; });
+        for (int e = 0; e < 8; ++e) f(weight[b][e] ? draw_place(key[b][e], (unsigned)(8192 * b + 8 * tid + e)) : 0, [&] { return weight[b][e]; });
     };
-    cut = max(cut, draw_border(lds, want ? want : 1, 0, each, [&](unsigned k) { return w.of(k); }));
+    cut = max(cut, draw_border<false>(lds, want ? want : 1, 0, each, [&](unsigned k) { return w.of(k); }));
   }
   const draw_u64 least = w.least(par.min_p);
   unsigned kept = 0;
@@ -225,7 +225,7 @@ k_draw_small(DrawArgs a, int64_t first) {
   }
   __syncthreads();
   const draw_u64 total = starts[32];
-  const double log_total = log(__builtin_ldexp((double)total, -w.bits));
+  const double log_total = w.log_sum(total);
   // every wave goes through all draws and takes those that fall into its segments
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
@@ -267,38 +267,35 @@ k_draw_scan(DrawArgs a, int64_t first) {
   const float c = draw_depth_scale(par);
   const int begin = chunk * a.chunk_rows, end = (int)min((int64_t)a.rows, (int64_t)begin + a.chunk_rows);
   const int turns = a.chunk_rows / 2048, turns_block = (turns + a.blocks - 1) / a.blocks;
-  unsigned best = 0, count = 0, group = 0;
-  float sum = 0.f, top = 0.f;
+  // scores as floats, -infinity where a row does not count
+  float best = -__builtin_inff(), sum = 0.f, group = best;
   unsigned* maxima = a.maxima + q * a.groups + (int64_t)chunk * a.blocks * 256 + tid;
   int block = 0, left = turns_block;
   for (int i = 0; i < turns; ++i) {
     const int64_t at = (int64_t)begin + i * 2048 + 8 * tid;
     if (at < end) {
-      unsigned key[8], here = 0;
-      row.keys((int)at, key);
+      float v[8], here = -__builtin_inff();
+      row.scores_of((int)at, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) { here = max(here, key[e]); count += key[e] != 0; }
-      group = max(group, here);
-      if (here > best) {
-        const float now = draw_score(here);
-        sum = best ? sum * __builtin_amdgcn_exp2f(-draw_depth(now, top, c)) : 0.f;
-        best = here; top = now;
+      for (int e = 0; e < 8; ++e) here = fmaxf(here, v[e]);
+      group = fmaxf(group, here);
+      if (here > best) { sum = sum > 0.f ? sum * __builtin_amdgcn_exp2f(-draw_depth(here, best, c)) : 0.f; best = here; }
+      if (best > -__builtin_inff()) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += __builtin_amdgcn_exp2f(-draw_depth(best, v[e], c));
       }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum += key[e] ? __builtin_amdgcn_exp2f(-draw_depth(top, draw_score(key[e]), c)) : 0.f;
     }
     if (--left == 0 || i + 1 == turns) {
-      if (few) maxima[256 * block] = group;
-      group = 0; ++block; left = turns_block;
+      if (few) maxima[256 * block] = draw_key(group);
+      group = -__builtin_inff(); ++block; left = turns_block;
     }
   }
   if (few) for (; block < a.blocks; ++block) maxima[256 * block] = 0;
-  const unsigned all = draw_reduce(best, (unsigned*)slots, [](unsigned x, unsigned y) { return x > y ? x : y; });
-  count = draw_sum(count, (unsigned*)slots);
-  sum = best ? sum * __builtin_amdgcn_exp2f(-draw_depth(draw_score(all), top, c)) : 0.f;
+  const unsigned mine = draw_key(best), all = draw_reduce(mine, (unsigned*)slots, DrawMax());
+  sum = mine ? sum * __builtin_amdgcn_exp2f(-draw_depth(draw_score(all), best, c)) : 0.f;
   sum = draw_sum(sum, (float*)slots);
   if (tid == 0) {
-    a.stats[q * a.chunks + chunk] = {all, count, sum};
+    a.stats[q * a.chunks + chunk] = {all, sum};
     if (chunk == 0) a.listed[q] = 0;
   }
 }
@@ -317,10 +314,10 @@ k_draw_few(DrawArgs a, int64_t first) {
   const int tid = threadIdx.x;
   const DrawRow<TYPE> row(a, q);
   const DrawWhole whole = draw_whole(a, q, draw_depth_scale(par), lds.slots);
-  if (whole.count == 0) { draw_nothing<TYPE>(a, q); return; }
+  if (whole.best == 0) { draw_nothing<TYPE>(a, q); return; }
   const unsigned* maxima = a.maxima + q * a.groups;
   // the k-th largest maximum: k rows at least reach it
-  const draw_u64 bound = draw_border(lds, (draw_u64)par.top_k, 0, [&](auto f) { for (int g = tid; g < a.groups; g += 1024) f((draw_u64)(maxima[g] ? maxima[g] : 1u) << 32, draw_one); },
+  const draw_u64 bound = draw_border<true>(lds, (draw_u64)par.top_k, 0, [&](auto f) { for (int g = tid; g < a.groups; g += 1024) f((draw_u64)(maxima[g] ? maxima[g] : 1u) << 32, draw_one); },
                                      [](unsigned) { return draw_one(); }) >> 32;
   if (tid == 0) listed = 0;
   __syncthreads();
@@ -348,12 +345,12 @@ k_draw_few(DrawArgs a, int64_t first) {
   const DrawWeights w = draw_weights(whole.best, par, whole.sum);
   auto each = [&](auto f) { for (unsigned i = tid; i < n; i += 1024) f(list[i]); };
   draw_u64 cut = bound << 32;                              // the listed rows and no others
-  if ((unsigned)par.top_k < n) cut = draw_border(lds, (draw_u64)par.top_k, 0, [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); }, [](unsigned) { return draw_one(); });
+  if ((unsigned)par.top_k < n) cut = draw_border<false>(lds, (draw_u64)par.top_k, 0, [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); }, [](unsigned) { return draw_one(); });
   if (par.top_p < 2.f) {
     draw_u64 all = 0;
     each([&](draw_u64 place) { if (place >= cut) all += w.of((unsigned)(place >> 32)); });
     const draw_u64 want = draw_share_up(par.top_p, draw_sum(all, lds.slots)), top_k = cut;
-    cut = draw_border(lds, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { if (place >= top_k) f(place, [&] { return w.of((unsigned)(place >> 32)); }); }); },
+    cut = draw_border<false>(lds, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { if (place >= top_k) f(place, [&] { return w.of((unsigned)(place >> 32)); }); }); },
                       [&](unsigned k) { return w.of(k); });
   }
   const draw_u64 least = w.least(par.min_p);
@@ -388,16 +385,18 @@ k_draw_hist(DrawArgs a, int64_t first) {
   for (int i = tid; i < DRAW_BINS; i += 256) bins[i] = 0;
   const DrawWhole whole = draw_whole(a, q, c, slots);
   const float top = draw_score(whole.best), unit_weight = (float)(1 << a.hist_bits);
-  auto bin_top = [](int bin) { return bin * (1.f / 32.f); };
   const int begin = chunk * a.chunk_rows, end = (int)min((int64_t)a.rows, (int64_t)begin + a.chunk_rows);
   for (int64_t at = (int64_t)begin + 8 * tid; at < end; at += 2048) {
-    unsigned key[8];
-    row.keys((int)at, key);
+    float v[8];
+    row.scores_of((int)at, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) if (key[e]) {
+    for (int e = 0; e < 8; ++e) {
       // 2^-x, x the depth below the bin's top, at most 1/32 but in the last bin: 1 - x ln 2 + (x ln 2)^2 / 2 is off by 2^-19 at most
-      const float depth = draw_depth(top, draw_score(key[e]), c), x = fminf(depth - bin_top(draw_bin(depth)), 1.f / 32.f);
-      atomicAdd(&bins[draw_bin(depth)], (unsigned)__builtin_fmaf(unit_weight, __builtin_fmaf(x, __builtin_fmaf(x, 0.24022651f, -0.69314718f), 1.f), 0.5f));
+      const float depth = draw_depth(top, v[e], c);
+      const int bin = draw_bin(depth);
+      const float x = fminf(__builtin_fmaf(bin, -1.f / 32.f, depth), 1.f / 32.f);
+      const unsigned w = (unsigned)__builtin_fmaf(unit_weight, __builtin_fmaf(x, __builtin_fmaf(x, 0.24022651f, -0.69314718f), 1.f), 0.5f);
+      if (v[e] > -__builtin_inff()) atomicAdd(&bins[bin], w);
     }
   }
   __syncthreads();
@@ -447,11 +446,12 @@ k_draw_weigh(DrawArgs a, int64_t first) {
   const DrawRow<TYPE> row(a, q);
   const float c = draw_depth_scale(par);
   const DrawWhole whole = draw_whole(a, q, c, slots);
-  if (whole.count == 0) return;
+  if (whole.best == 0) return;
   const DrawWeights w = draw_weights(whole.best, par, whole.sum);
   const DrawRange range = a.range[q];
   const draw_u64 least = w.least(par.min_p);
-  const float top = draw_score(whole.best);
+  // bins by their depth, 32 to a binary order of magnitude, as the histogram counts them; all lies above where there is none
+  const float top = draw_score(whole.best), low = par.top_p < 2.f ? (float)range.low : __builtin_inff(), high = range.high < DRAW_BINS - 1 ? range.high + 1.f : __builtin_inff();
   const int begin = chunk * a.chunk_rows, end = (int)min((int64_t)a.rows, (int64_t)begin + a.chunk_rows);
   draw_u64 all = 0, above = 0;
   unsigned kept = 0;
@@ -459,24 +459,29 @@ k_draw_weigh(DrawArgs a, int64_t first) {
     const int64_t at = s + 8 * lane;
     draw_u64 sum = 0;
     if (at < end) {
-      unsigned key[8];
-      row.keys((int)at, key);
+      float v[8];
+      row.scores_of((int)at, v);
+      unsigned near = 0;                                   // rows of the range
 #pragma unroll
-      for (int e = 0; e < 8; ++e) if (key[e]) {
-        const draw_u64 x = w.of(key[e]);
+      for (int e = 0; e < 8; ++e) {
+        const draw_u64 x = w.of_score(v[e]);
+        const float bin = draw_depth(top, v[e], c) * 32.f;
         all += x;
-        const int bin = range.low < DRAW_BINS ? draw_bin(draw_depth(top, draw_score(key[e]), c)) : 0;
-        if (bin < range.low) {
-          above += x;                                      // before min-p: top-p goes by it
-          if (x >= least) { sum += x; ++kept; }
-        } else if (bin <= range.high) {
+        const bool over = bin < low, in = over && x >= least && v[e] > -__builtin_inff();
+        above += over ? x : 0;                             // before min-p: top-p goes by it
+        sum += in ? x : 0;
+        kept += in;
+        near |= (!over && bin < high && x ? 1u : 0u) << e;
+      }
+      if (near) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (near >> e & 1u) {
           const unsigned n = atomicAdd(&listed, 1u);
-          if (n < DRAW_LIST_CHUNK) list[n] = draw_place(key[e], (unsigned)at + e);
+          if (n < DRAW_LIST_CHUNK) list[n] = draw_place(draw_key(v[e]), (unsigned)at + e);
         }
       }
     }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
+    sum = draw_wave_sum(sum);
     if (lane == 0) a.mass[q * a.segments + s / DRAW_SEGMENT] = sum;
   }
   all = draw_sum(all, slots);
@@ -505,27 +510,34 @@ k_draw_rows(DrawArgs a, int64_t first) {
   const int tid = threadIdx.x;
   const DrawRow<TYPE> row(a, q);
   const DrawWhole whole = draw_whole(a, q, draw_depth_scale(par), lds.slots);
-  if (whole.count == 0) { draw_nothing<TYPE>(a, q); return; }
+  if (whole.best == 0) { draw_nothing<TYPE>(a, q); return; }
   draw_u64* mass = a.mass + q * a.segments;
   const unsigned n = a.listed[q];
-  if (!draw_all(a, par) || n > (unsigned)a.list) { draw_slowly<TYPE>(a, q, row, par, whole, mass, lds); return; }
   const DrawWeights w = draw_weights(whole.best, par, whole.sum);
-  const draw_u64 least = w.least(par.min_p);
   const bool in = tid < a.chunks;
+  const draw_u64* list = a.lists + q * a.list;
+  auto each = [&](auto f) { for (unsigned i = tid; i < n; i += 1024) f(list[i]); };
+  bool slowly = !draw_all(a, par) || n > (unsigned)a.list;
+  draw_u64 want = 1, above = 0;
+  if (!slowly && par.top_p < 2.f) {                        // uniform
+    draw_u64 all = 0, listed = 0;
+    if (in) { all = a.totals[2 * (q * a.chunks + tid)]; above = a.totals[2 * (q * a.chunks + tid) + 1]; }
+    each([&](draw_u64 place) { listed += w.of((unsigned)(place >> 32)); });
+    all = draw_sum(all, lds.slots);
+    above = draw_sum(above, lds.slots);
+    listed = draw_sum(listed, lds.slots);
+    want = draw_share_up(par.top_p, all);
+    if (want == 0) want = 1;
+    // temperatures whose inverse 32 bits do not hold: the histogram was of something else
+    slowly = above >= want || above + listed < want;
+  }
+  if (slowly) { draw_slowly<TYPE>(a, q, row, par, whole, mass, lds); return; }
+  const draw_u64 least = w.least(par.min_p);
   unsigned kept = draw_sum(in ? a.kept[q * a.chunks + tid] : 0u, (unsigned*)lds.slots);
   draw_u64 cut = 1;
   if (par.top_p < 2.f) {
-    const draw_u64 all = draw_sum(in ? a.totals[2 * (q * a.chunks + tid)] : 0, lds.slots), above = draw_sum(in ? a.totals[2 * (q * a.chunks + tid) + 1] : 0, lds.slots);
-    const draw_u64 want = draw_share_up(par.top_p, all);
-    const draw_u64* list = a.lists + q * a.list;
-    auto each = [&](auto f) { for (unsigned i = tid; i < n; i += 1024) f(list[i]); };
-    draw_u64 listed = 0;
-    each([&](draw_u64 place) { listed += w.of((unsigned)(place >> 32)); });
-    listed = draw_sum(listed, lds.slots);
-    // temperatures whose inverse 32 bits do not hold: the histogram was of something else
-    if (above >= (want ? want : 1) || above + listed < want) { draw_slowly<TYPE>(a, q, row, par, whole, mass, lds); return; }     // uniform
-    cut = draw_border(lds, want ? want : 1, above, [&](auto f) { each([&](draw_u64 place) { f(place, [&] { return w.of((unsigned)(place >> 32)); }); }); },
-                      [&](unsigned k) { return w.of(k); });
+    cut = draw_border<false>(lds, want, above, [&](auto f) { each([&](draw_u64 place) { f(place, [&] { return w.of((unsigned)(place >> 32)); }); }); },
+                             [&](unsigned k) { return w.of(k); });
     unsigned more = 0;
     each([&](draw_u64 place) {
       if (place < cut) return;

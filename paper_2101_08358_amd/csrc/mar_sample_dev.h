@@ -6,34 +6,29 @@
 
 typedef unsigned long long draw_u64;
 
-// Scores as unsigned integers in their order; 0: the row does not count (NaN, -infinity).  -0 and 0 are one, +infinity is the largest float.
+// Scores as unsigned integers in their order; 0: the row does not count (-infinity).  -0 and 0 are one.
 __device__ __forceinline__ unsigned draw_key(float s) {
   if (!(s > -__builtin_inff())) return 0u;
-  const unsigned b = __float_as_uint(fminf(s, 3.402823466e38f) + 0.f);
+  const unsigned b = __float_as_uint(s + 0.f);
   return b ^ ((unsigned)((int)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float draw_score(unsigned key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 
-// round(2^(bits + x log2 e)), x <= 0, to 2^-50 of itself: 2^f by its Taylor series, |f| <= 1/2, (f ln 2)^13 / 13! < 2^-52.
-__device__ __forceinline__ draw_u64 draw_weight(double x, int bits) {
-  const double n = __builtin_rint(x * 1.4426950408889634);
-  if (!(n > -70.0)) return 0;                              // bits <= 61
-  // log2 e in two parts: x log2 e - n without the rounding of its product
-  const double f = __builtin_fma(x, 2.0355273740931033e-17, __builtin_fma(x, 1.4426950408889634, -n));
-  double p = 2.5678435993488206e-11;                       // ln2^k / k!, k = 12 .. 0
-  p = __builtin_fma(p, f, 4.4455382718708116e-10);
-  p = __builtin_fma(p, f, 7.0549116208011233e-09);
-  p = __builtin_fma(p, f, 1.0178086009239699e-07);
-  p = __builtin_fma(p, f, 1.3215486790144309e-06);
-  p = __builtin_fma(p, f, 1.5252733804059841e-05);
-  p = __builtin_fma(p, f, 1.5403530393381609e-04);
-  p = __builtin_fma(p, f, 1.3333558146428443e-03);
-  p = __builtin_fma(p, f, 9.6181291076284772e-03);
-  p = __builtin_fma(p, f, 5.5504108664821580e-02);
-  p = __builtin_fma(p, f, 2.4022650695910072e-01);
-  p = __builtin_fma(p, f, 6.9314718055994531e-01);
-  p = __builtin_fma(p, f, 1.0);
-  return (draw_u64)__builtin_rint(__builtin_ldexp(p, bits + (int)n));
+// round(2^(62 - shift - depth)), depth >= 0 (not a number, or 64 and more: 0), to 2^-51 of itself: 1 + 2^-(1/2 + g), |g| <= 1/2, by the
+// polynomial of degree 10 through its Chebyshev series (off by 2^-52.5), whose bits less those of 1 are the power in units of 2^-52.
+// The coefficients come from memory: out of scalar registers they are an operand of the products, constants would be copied for each.
+static __constant__ double draw_power[11] = {1.7071067811865475, -0.4901290717342769, 0.1698657920915381, -0.039247331620345965, 0.006801044314302664,
+                                             -0.0009428249441899351, 0.0001089194084511562, -1.0785257377670457e-05, 9.344721961284408e-07,
+                                             -7.21863451712333e-08, 5.002210946656729e-09};
+__device__ __forceinline__ draw_u64 draw_weight(double depth, int shift) {
+  depth = fmin(depth, 64.0);
+  const int down = (int)depth + shift;                     // shift >= 2
+  const double g = __builtin_amdgcn_fract(depth) - 0.5;
+  double p = draw_power[10];
+#pragma unroll
+  for (int i = 9; i >= 0; --i) p = __builtin_fma(p, g, draw_power[i]);
+  const draw_u64 m = ((draw_u64)__double_as_longlong(p) - 0x3ff0000000000000ull) << 10;      // up to 2^62
+  return ((m >> min(down - 1, 63)) + 1) >> 1;
 }
 
 // ceil(part * whole), part in [0, 1), whole < 2^62.
@@ -55,7 +50,7 @@ __device__ __forceinline__ draw_u64 draw_place(unsigned key, unsigned id) { retu
 #define DRAW_LIST 8192              // most rows a border is looked for among
 #define DRAW_LIST_CHUNK 2048        // of one chunk
 
-struct DrawChunk { unsigned best, count; float sum; };      // of a chunk: greatest key, rows that count, sum of weights relative to `best`
+struct DrawChunk { unsigned best; float sum; };     // of a chunk: greatest key (0: no row counts), sum of weights relative to it
 // Of a query, after the histogram: bins below `low` lie above top-p's border, bins above `high` below it.
 struct DrawRange { int low, high; };
 
@@ -103,26 +98,43 @@ template <int TYPE> struct DrawRow {
   const T* scores; const uint32_t* allowed; int rows;
   __device__ __forceinline__ DrawRow(const DrawArgs& a, int64_t q)
       : scores((const T*)a.scores + q * a.score_stride), allowed(a.allowed ? a.allowed + q * a.allowed_stride : nullptr), rows(a.rows) {}
-  __device__ __forceinline__ void keys(int c, unsigned (&key)[8]) const {           // c < rows
-    float v[8];
+  // c < rows.  -infinity: the row does not count; +infinity is the largest float
+  __device__ __forceinline__ void scores_of(int c, float (&v)[8]) const {
     load8<TYPE>(scores, c, rows, v);
-    const unsigned bits = allowed ? allowed[c >> 5] >> (c & 31) : 0xffu;
+    unsigned bits = allowed ? allowed[c >> 5] >> (c & 31) : 0xffu;
+    if (c + 8 > rows) bits &= 0xffu >> (c + 8 - rows);
+    const float none = -__builtin_inff();
 #pragma unroll
-    for (int e = 0; e < 8; ++e) key[e] = c + e < rows && (bits >> e & 1u) ? draw_key(v[e]) : 0u;
+    for (int e = 0; e < 8; ++e) v[e] = fminf(fmaxf(v[e], none), 3.402823466e38f);          // NaN gives way
+    if ((bits & 0xffu) != 0xffu) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (!(bits >> e & 1u)) v[e] = none;
+    }
+  }
+  __device__ __forceinline__ void keys(int c, unsigned (&key)[8]) const {
+    float v[8];
+    scores_of(c, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) key[e] = draw_key(v[e]);
   }
 };
 
-// Weights of a query's rows: the best score, the inverse temperature, the integers' scale.
+// Weights of a query's rows: the best score, the inverse temperature and the same in binary orders of magnitude, the integers' scale 2^(62 - shift).
 struct DrawWeights {
-  double top, inv_temperature; int bits;
+  double top, inv_temperature, slope; int shift;
   __device__ __forceinline__ double distance(unsigned key) const { return ((double)draw_score(key) - top) * inv_temperature; }
-  __device__ __forceinline__ draw_u64 of(unsigned key) const { return draw_weight(distance(key), bits); }
+  __device__ __forceinline__ draw_u64 of_score(float score) const { return draw_weight((top - (double)score) * slope, shift); }
+  __device__ __forceinline__ draw_u64 of(unsigned key) const { return of_score(draw_score(key)); }
+  __device__ __forceinline__ double log_sum(draw_u64 sum) const { return log(__builtin_ldexp((double)sum, shift - 62)); }
   // min-p's weight
-  __device__ __forceinline__ draw_u64 least(float min_p) const { return min_p > 0.f ? (draw_u64)__builtin_ceil(__builtin_ldexp((double)min_p, bits)) : 0; }
+  __device__ __forceinline__ draw_u64 least(float min_p) const {
+    const draw_u64 best = draw_weight(0.0, shift);
+    return min_p >= 1.f ? best : (min_p > 0.f ? draw_share_up(min_p, best) : 0);
+  }
 };
 // approx: sum of weights relative to the best one, in fp32: the integers' sum lies below 2^61 and a little more.
 __device__ __forceinline__ DrawWeights draw_weights(unsigned best, const DrawParams& p, float approx) {
-  return {(double)draw_score(best), p.inv_temperature, 60 - ilogbf(fmaxf(approx, 1.f))};
+  return {(double)draw_score(best), p.inv_temperature, p.inv_temperature * 1.4426950408889634, 2 + ilogbf(fmaxf(approx, 1.f))};
 }
 // The same in fp32 and binary orders of magnitude below the best, for sums that only choose a scale or a range of bins.
 __device__ __forceinline__ float draw_depth(float top, float s, float c) { return fminf(top - s, 3.402823466e38f) * c; }
@@ -130,76 +142,135 @@ __device__ __forceinline__ float draw_depth_scale(const DrawParams& p) { return 
 __device__ __forceinline__ int draw_bin(float depth) { return (int)fminf(depth * 32.f, DRAW_BINS - 1.f); }
 __device__ __forceinline__ draw_u64 draw_one() { return 1; }
 
-// Sums and maxima over a workgroup; everyone gets the result.  slots: one a wave.
-template <typename T, typename F> __device__ __forceinline__ T draw_reduce(T v, T* slots, F join) {
+// Sums and maxima by lane exchanges within a wave, zeros beyond its ends.
+template <int CTRL, int ROWS, typename T> __device__ __forceinline__ T draw_moved(T v) {
+  unsigned w[(sizeof(T) + 3) / 4];
+  __builtin_memcpy(w, &v, sizeof(T));
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = join(v, __shfl_xor(v, o));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = slots[0];
-  for (int w = 1; w < (int)(blockDim.x >> 6); ++w) v = join(v, slots[w]);
+  for (unsigned i = 0; i < sizeof(T) / 4; ++i) w[i] = (unsigned)__builtin_amdgcn_update_dpp(0, (int)w[i], CTRL, ROWS, 0xf, false);
+  __builtin_memcpy(&v, w, sizeof(T));
   return v;
 }
-template <typename T> __device__ __forceinline__ T draw_sum(T v, T* slots) { return draw_reduce(v, slots, [](T x, T y) { return x + y; }); }
-template <typename T> __device__ __forceinline__ T draw_wave_prefix(T v) {                // inclusive
-  const int lane = threadIdx.x & 63;
+template <typename T> __device__ __forceinline__ T draw_lane(T v, int lane) {             // lane: uniform
+  unsigned w[(sizeof(T) + 3) / 4];
+  __builtin_memcpy(w, &v, sizeof(T));
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) { const T up = __shfl_up(v, o); if (lane >= o) v += up; }
+  for (unsigned i = 0; i < sizeof(T) / 4; ++i) w[i] = (unsigned)__builtin_amdgcn_readlane((int)w[i], lane);
+  __builtin_memcpy(&v, w, sizeof(T));
   return v;
 }
+struct DrawAdd { template <typename T> __device__ __forceinline__ T operator()(T x, T y) const { return x + y; } };
+struct DrawMax { template <typename T> __device__ __forceinline__ T operator()(T x, T y) const { return x > y ? x : y; } };
+template <typename J, typename T> __device__ __forceinline__ T draw_row_prefix(T v, J join) {         // inclusive, within 16 lanes
+  v = join(v, draw_moved<0x111, 0xf>(v));
+  v = join(v, draw_moved<0x112, 0xf>(v));
+  v = join(v, draw_moved<0x114, 0xf>(v));
+  return join(v, draw_moved<0x118, 0xf>(v));
+}
+template <typename J, typename T> __device__ __forceinline__ T draw_wave_prefix(T v, J join) {        // inclusive; zero is the joining's own
+  v = draw_row_prefix(v, join);
+  v = join(v, draw_moved<0x142, 0xa>(v));                  // lane 15 of rows 0 and 2 to rows 1 and 3
+  return join(v, draw_moved<0x143, 0xc>(v));               // lane 31 to rows 2 and 3
+}
+template <typename T> __device__ __forceinline__ T draw_wave_prefix(T v) { return draw_wave_prefix(v, DrawAdd()); }
+template <typename T> __device__ __forceinline__ T draw_wave_sum(T v) { return draw_lane(draw_wave_prefix(v, DrawAdd()), 63); }
+// Over a workgroup of up to 16 waves; everyone gets the result.  slots: one a wave.
+template <typename J, typename T> __device__ __forceinline__ T draw_reduce(T v, T* slots, J join) {
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  v = draw_wave_prefix(v, join);
+  __syncthreads();
+  if (lane == 63) slots[threadIdx.x >> 6] = v;
+  __syncthreads();
+  T each = 0;
+  if ((lane & 15) < waves) each = slots[lane & 15];
+  return draw_lane(draw_row_prefix(each, join), 15);
+}
+template <typename T> __device__ __forceinline__ T draw_sum(T v, T* slots) { return draw_reduce(v, slots, DrawAdd()); }
 // Exclusive prefix sums over a workgroup; the whole sum in `total`.
 template <typename T> __device__ __forceinline__ T draw_prefix(T v, T* slots, T& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const T run = draw_wave_prefix(v);
   __syncthreads();
   if (lane == 63) slots[wave] = run;
   __syncthreads();
-  T before = 0, all = 0;
-  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) { if (w < wave) before += slots[w]; all += slots[w]; }
-  total = all;
+  T each = 0;
+  if ((lane & 15) < waves) each = slots[lane & 15];
+  each = draw_row_prefix(each, DrawAdd());
+  total = draw_lane(each, 15);
+  const T before = wave ? draw_lane(each, wave - 1) : T(0);
   return before + run - v;
 }
 
 // LDS of a workgroup of 1,024 threads that looks for a border.
 struct DrawShared {
   draw_u64 bins[2048], slots[16], found_sum, found_all;
-  unsigned found;
+  unsigned found, ends[2][16];
 };
+// One digit: bins[..] have been summed up; the bin, from the top, in which the sum reaches `want`.  over: the sum above it, all: its own.
+__device__ __forceinline__ unsigned draw_digit(DrawShared& lds, draw_u64 want, draw_u64& over, draw_u64& all) {
+  const int hi = 2047 - 2 * (int)threadIdx.x;              // a pair of bins a thread, from the top
+  const draw_u64 x = lds.bins[hi], y = lds.bins[hi - 1];
+  draw_u64 whole;
+  const draw_u64 before = over + draw_prefix(x + y, lds.slots, whole);
+  if (before < want && before + x + y >= want) {
+    const bool one = before + x >= want;
+    lds.found = (unsigned)(one ? hi : hi - 1);
+    lds.found_sum = before + (one ? 0 : x);
+    lds.found_all = one ? x : y;
+  }
+  __syncthreads();
+  over = lds.found_sum; all = lds.found_all;
+  return lds.found;                                        // written again behind the next digit's barriers
+}
 // The place of the first row, in the order of places, at which the sum of the rows' weights up to it reaches `want`; `over`: what lies
-// above all rows that `each` goes through.  By digits of 11, 11 and 10 bits of the keys and, where several rows share the border's key, of
-// the ids.  All 1,024 threads call it; each(f) calls f(place, weight) for every row of the thread, weight() its weight, of(key) that of a key.
-template <typename E, typename W>
+// above all rows that `each` goes through.  By digits of up to 11 bits of the keys' distance from the least one, so that the first digit
+// spreads whatever the range (scores share their first bits: by those, most rows would meet at few addresses, one after the other),
+// then, where several rows share the border's key, of the ids.  All 1,024 threads call it; each(f) calls f(place, weight) for every row
+// of the thread, weight() its weight, of(key) that of a key.  COARSE: one digit, and the least key of its bin alone.
+template <bool COARSE, typename E, typename W>
 __device__ __forceinline__ draw_u64 draw_border(DrawShared& lds, draw_u64 want, draw_u64 over, E each, W of) {
-  draw_u64 prefix = 0;
-  for (int level = 0; level < 6; ++level) {
-    const int width = level % 3 == 2 ? 10 : 11, shift = (level < 3 ? 32 : 0) + (level % 3 == 0 ? 21 : (level % 3 == 1 ? 10 : 0));
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  unsigned hi = 0, lo = 0;                                 // lo: of the keys' complements
+  each([&](draw_u64 place, auto) { if (place) { hi = max(hi, (unsigned)(place >> 32)); lo = max(lo, ~(unsigned)(place >> 32)); } });
+  hi = draw_wave_prefix(hi, DrawMax());
+  lo = draw_wave_prefix(lo, DrawMax());
+  __syncthreads();
+  if (lane == 63) { lds.ends[0][wave] = hi; lds.ends[1][wave] = lo; }
+  __syncthreads();
+  hi = draw_lane(draw_row_prefix(lds.ends[0][lane & 15], DrawMax()), 15);
+  unsigned base = ~draw_lane(draw_row_prefix(lds.ends[1][lane & 15], DrawMax()), 15);
+  int left = hi > base ? 32 - __builtin_clz(hi - base) : 1;
+  draw_u64 ties = 0;
+  while (left > 0) {
+    const int width = min(left, 11), shift = left - width;
     for (int i = threadIdx.x; i < 2048; i += 1024) lds.bins[i] = 0;
     __syncthreads();
     each([&](draw_u64 place, auto weight) {
-      if (place != 0 && (level == 0 || place >> (shift + width) == prefix)) {
+      const unsigned k = (unsigned)(place >> 32);
+      if (place != 0 && k >= base && (draw_u64)(k - base) >> left == 0) {
         const draw_u64 w = weight();
-        if (w) atomicAdd(&lds.bins[place >> shift & ((1u << width) - 1)], w);
+        if (w) atomicAdd(&lds.bins[(k - base) >> shift], w);
       }
     });
     __syncthreads();
-    const int hi = 2047 - 2 * (int)threadIdx.x;            // a pair of bins a thread, from the top
-    const draw_u64 x = lds.bins[hi], y = lds.bins[hi - 1];
-    draw_u64 all;
-    const draw_u64 before = over + draw_prefix(x + y, lds.slots, all);
-    if (before < want && before + x + y >= want) {
-      const bool one = before + x >= want;
-      lds.found = (unsigned)(one ? hi : hi - 1);
-      lds.found_sum = before + (one ? 0 : x);
-      lds.found_all = one ? x : y;
-    }
-    __syncthreads();
-    over = lds.found_sum;
-    prefix = prefix << width | lds.found;
-    const draw_u64 ties = lds.found_all;
-    __syncthreads();
-    // all rows at the key are needed: no id decides
-    if (level == 2 && want - over > ties - of((unsigned)prefix)) return prefix << 32;
+    base += draw_digit(lds, want, over, ties) << shift;
+    left = shift;
+    if (COARSE) return (draw_u64)base << 32;
   }
-  return prefix;
+  // all rows at the key are needed: no id decides
+  if (want - over > ties - of(base)) return (draw_u64)base << 32;
+  unsigned prefix = 0;
+  for (int level = 0; level < 3; ++level) {
+    const int width = level == 2 ? 10 : 11, shift = level == 0 ? 21 : (level == 1 ? 10 : 0);
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2048; i += 1024) lds.bins[i] = 0;
+    __syncthreads();
+    each([&](draw_u64 place, auto weight) {
+      const unsigned id = (unsigned)place;
+      if (place != 0 && (unsigned)(place >> 32) == base && (level == 0 || id >> (shift + width) == prefix)) atomicAdd(&lds.bins[id >> shift & ((1u << width) - 1)], weight());
+    });
+    __syncthreads();
+    prefix = prefix << width | draw_digit(lds, want, over, ties);
+  }
+  return (draw_u64)base << 32 | prefix;
 }
