@@ -14,6 +14,7 @@
 //   k_draw_rows    the border among those rows, then the draws: the segment by the sums before it, the row by a wave that weighs it again
 // What does not fit (borders among more rows than a list holds, top-k above 1,024 with a table too large for registers) goes through
 // all rows by digits, one workgroup a query, in the last kernel.
+#include <type_traits>
 #include "mar_sample_dev.h"
 
 // ------------------------------------------------------------------------------------------ pieces -----
@@ -111,7 +112,7 @@ __device__ void draw_slowly(const DrawArgs& a, int64_t q, const DrawRow<TYPE>& r
     all = draw_sum(all, lds.slots);
     const draw_u64 want = draw_share_up(par.top_p, all), top_k = cut;
     // rows below top-k's cut have no say: they come after the border
-    cut = draw_border<false>(lds, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { if (place >= top_k) f(place, [&] { return w.of((unsigned)(place >> 32)); }); }); },
+    cut = draw_border<false>(lds, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
                       [&](unsigned k) { return w.of(k); });
   }
   const draw_u64 least = w.least(par.min_p);
@@ -134,89 +135,152 @@ __device__ void draw_slowly(const DrawArgs& a, int64_t q, const DrawRow<TYPE>& r
   draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.slots);
 }
 
+// Up to 256 rows, with all that top-k leaves among them: a thread a row compares it with all others.  Called by all threads of the workgroup.
+struct DrawShort { draw_u64 place[256], weight[256], slots[16]; };
+__device__ __forceinline__ void draw_short(const DrawArgs& a, int64_t q, DrawShort& lds, unsigned n, const DrawParams& par, const DrawWeights& w) {
+  const unsigned tid = threadIdx.x;
+  const draw_u64 mine = tid < n ? lds.place[tid] : 0;
+  const draw_u64 weight = tid < n ? w.of((unsigned)(mine >> 32)) : 0;
+  if (tid < n) lds.weight[tid] = weight;
+  __syncthreads();
+  unsigned rank = 0;
+  draw_u64 before = 0;
+  if (tid < n) for (unsigned i = 0; i < n; ++i) {
+    const bool better = lds.place[i] > mine;
+    rank += better;
+    before += better ? lds.weight[i] : 0;
+  }
+  bool in = tid < n && (par.top_k == 0 || rank < (unsigned)par.top_k);
+  if (par.top_p < 2.f) {                                   // uniform
+    const draw_u64 want = draw_share_up(par.top_p, draw_sum(in ? weight : 0, lds.slots));
+    in = in && before < (want ? want : 1);
+  }
+  in = in && weight >= w.least(par.min_p);
+  if (a.num_kept) {
+    const unsigned kept = draw_sum(in ? 1u : 0u, (unsigned*)lds.slots);
+    if (tid == 0) a.num_kept[q] = (int)kept;
+  }
+  __syncthreads();
+  if (tid < n) lds.weight[tid] = in ? weight : 0;
+  const draw_u64 total = draw_sum(in ? weight : 0, lds.slots);      // its barriers order the list
+  if (!in) return;
+  const unsigned id = (unsigned)mine;                      // complements: greater ones come first
+  draw_u64 start = 0;
+  for (unsigned i = 0; i < n; ++i) start += (unsigned)lds.place[i] > id ? lds.weight[i] : 0;
+  const float log_prob = (float)(w.distance((unsigned)(mine >> 32)) - w.log_sum(total));
+  for (int d = 0; d < a.draws; ++d) {
+    const draw_u64 target = draw_target(a.uniforms[q * a.draws + d], total);
+    if (start <= target && target < start + weight) {
+      a.ids[q * a.draws + d] = (int)~id;
+      if (a.log_probs) a.log_probs[q * a.draws + d] = log_prob;
+    }
+  }
+}
+
 // ------------------------------------------------------------------------------------------ up to 16,384 rows -----
 template <int TYPE>
 __global__ void __launch_bounds__(1024)
 k_draw_small(DrawArgs a, int64_t first) {
-  __shared__ DrawShared lds;
+  __shared__ union { DrawShared border; DrawShort list; } lds;
   __shared__ draw_u64 starts[33];
+  __shared__ unsigned listed;
   const int64_t q = first + blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const DrawRow<TYPE> row(a, q);
   const DrawParams par = draw_params(a, q);
-  unsigned key[2][8];                                       // columns 8 tid .. and 8,192 + 8 tid ..: a wave holds segments `wave` and 16 + wave
-  unsigned best = 0, count = 0;
+  if (tid == 0) listed = 0;
+  float v[2][8], mine = -__builtin_inff();                  // columns 8 tid .. and 8,192 + 8 tid ..: a wave holds segments `wave` and 16 + wave
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) key[b][e] = 0u;
-    if (8192 * b + 8 * tid < a.rows) row.keys(8192 * b + 8 * tid, key[b]);
+    for (int e = 0; e < 8; ++e) v[b][e] = -__builtin_inff();
+    if (8192 * b + 8 * tid < a.rows) row.scores_of(8192 * b + 8 * tid, v[b]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) { best = max(best, key[b][e]); count += key[b][e] != 0; }
+    for (int e = 0; e < 8; ++e) mine = fmaxf(mine, v[b][e]);
   }
-  best = draw_reduce(best, (unsigned*)lds.slots, DrawMax());
-  count = draw_sum(count, (unsigned*)lds.slots);
-  if (count == 0) { draw_nothing<TYPE>(a, q); return; }    // uniform
+  const unsigned best = draw_reduce(draw_key(mine), (unsigned*)lds.border.slots, DrawMax());
+  if (best == 0) { draw_nothing<TYPE>(a, q); return; }     // uniform
   const float c = draw_depth_scale(par), top = draw_score(best);
   float approx = 0.f;
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) if (key[b][e]) approx += __builtin_amdgcn_exp2f(-draw_depth(top, draw_score(key[b][e]), c));
-  approx = draw_sum(approx, (float*)lds.slots);
+    for (int e = 0; e < 8; ++e) approx += __builtin_amdgcn_exp2f(-draw_depth(top, v[b][e], c));
+  approx = draw_sum(approx, (float*)lds.border.slots);
   const DrawWeights w = draw_weights(best, par, approx);
+  auto place = [&](int b, int e) { return draw_place(draw_key(v[b][e]), (unsigned)(8192 * b + 8 * tid + e)); };
   draw_u64 cut = 1;
-  if (par.top_k > 0 && (unsigned)par.top_k < count) {
-    auto ones = [&](auto f) {
+  if (par.top_k > 0 && par.top_k < a.rows) {               // uniform
+    if (par.top_k <= 128) {
+      // the k-th largest of the threads' maxima bounds the k-th best row from below: few rows reach it
+      const unsigned bound = (unsigned)(draw_border<true>(lds.border, (draw_u64)par.top_k, 0, [&](auto f) { f((draw_u64)max(draw_key(mine), 1u) << 32, draw_one); },
+                                                         [](unsigned) { return draw_one(); }) >> 32);
+      __syncthreads();
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f(draw_place(key[b][e], (unsigned)(8192 * b + 8 * tid + e)), draw_one);
-    };
-    cut = draw_border<false>(lds, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
-  }
-  draw_u64 weight[2][8], sum[2] = {0, 0};
-#pragma unroll
-  for (int b = 0; b < 2; ++b)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      weight[b][e] = key[b][e] && draw_place(key[b][e], (unsigned)(8192 * b + 8 * tid + e)) >= cut ? w.of(key[b][e]) : 0;
-      sum[b] += weight[b][e];
+        for (int e = 0; e < 8; ++e) if (draw_key(v[b][e]) >= max(bound, 1u)) {
+          const unsigned n = atomicAdd(&listed, 1u);
+          if (n < 256) lds.list.place[n] = place(b, e);
+        }
+      __syncthreads();
+      if (listed <= 256) { draw_short(a, q, lds.list, listed, par, w); return; }
     }
+    unsigned count = 0;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) count += v[b][e] > -__builtin_inff();
+    count = draw_sum(count, (unsigned*)lds.border.slots);
+    if ((unsigned)par.top_k < count) {
+      auto ones = [&](auto f) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f(place(b, e), draw_one);
+      };
+      cut = draw_border<false>(lds.border, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
+    }
+  }
   if (par.top_p < 2.f) {
-    const draw_u64 want = draw_share_up(par.top_p, draw_sum(sum[0] + sum[1], lds.slots));
-    auto each = [&](auto f) {                              // what top-k leaves out weighs nothing
+    draw_u64 all = 0;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) all += place(b, e) >= cut ? w.of_score(v[b][e]) : 0;
+    const draw_u64 want = draw_share_up(par.top_p, draw_sum(all, lds.border.slots)), top_k = cut;
+    auto each = [&](auto f) {
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f(weight[b][e] ? draw_place(key[b][e], (unsigned)(8192 * b + 8 * tid + e)) : 0, [&] { return weight[b][e]; });
+        for (int e = 0; e < 8; ++e) { const draw_u64 here = place(b, e); f(here >= top_k ? here : 0, [&] { return w.of_score(v[b][e]); }); }
     };
-    cut = max(cut, draw_border<false>(lds, want ? want : 1, 0, each, [&](unsigned k) { return w.of(k); }));
+    cut = draw_border<false>(lds.border, want ? want : 1, 0, each, [&](unsigned k) { return w.of(k); });
   }
   const draw_u64 least = w.least(par.min_p);
+  auto weight = [&](int b, int e) {
+    const draw_u64 x = w.of_score(v[b][e]);
+    return place(b, e) >= cut && x >= least ? x : 0;
+  };
   unsigned kept = 0;
+  draw_u64 sum[2] = {0, 0}, run[2];
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
-    sum[b] = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const bool in = key[b][e] && draw_place(key[b][e], (unsigned)(8192 * b + 8 * tid + e)) >= cut && weight[b][e] >= least;
+      const draw_u64 x = w.of_score(v[b][e]);
+      const bool in = place(b, e) >= cut && x >= least;
       kept += in;
-      if (!in) weight[b][e] = 0;
-      sum[b] += weight[b][e];
+      sum[b] += in ? x : 0;
     }
+    run[b] = draw_wave_prefix(sum[b]);
   }
   if (a.num_kept) {                                        // uniform
-    kept = draw_sum(kept, (unsigned*)lds.slots);
+    kept = draw_sum(kept, (unsigned*)lds.border.slots);
     if (tid == 0) a.num_kept[q] = (int)kept;
   }
-  draw_u64 run[2];
-  __syncthreads();
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    run[b] = draw_wave_prefix(sum[b]);
-    if (lane == 63) starts[16 * b + wave] = run[b];
-  }
+  for (int b = 0; b < 2; ++b) if (lane == 63) starts[16 * b + wave] = run[b];
   __syncthreads();
   if (wave == 0) {
     const draw_u64 m = lane < 32 ? starts[lane] : 0, upto = draw_wave_prefix(m);
@@ -238,15 +302,15 @@ k_draw_small(DrawArgs a, int64_t first) {
       while (mine) {                                       // uniform
         const int i = __ffsll((long long)mine) - 1;
         mine &= mine - 1;
-        const draw_u64 target = __shfl(t, i);
+        const draw_u64 target = draw_lane(t, i);
         if (before <= target && target < before + sum[b]) {        // one lane
           int at = 0;
-          unsigned k = key[b][0];
-          draw_u64 upto = before + weight[b][0];
+          float score = v[b][0];
+          draw_u64 upto = before + weight(b, 0);
 #pragma unroll
-          for (int j = 1; j < 8; ++j) if (upto <= target) { upto += weight[b][j]; at = j; k = key[b][j]; }
+          for (int j = 1; j < 8; ++j) if (upto <= target) { upto += weight(b, j); at = j; score = v[b][j]; }
           a.ids[q * a.draws + d0 + i] = 8192 * b + 8 * tid + at;
-          if (a.log_probs) a.log_probs[q * a.draws + d0 + i] = (float)(w.distance(k) - log_total);
+          if (a.log_probs) a.log_probs[q * a.draws + d0 + i] = (float)(w.distance(draw_key(score)) - log_total);
         }
       }
     }
@@ -304,35 +368,50 @@ k_draw_scan(DrawArgs a, int64_t first) {
 template <int TYPE>
 __global__ void __launch_bounds__(1024)
 k_draw_few(DrawArgs a, int64_t first) {
-  __shared__ DrawShared lds;
+  __shared__ union { DrawShared border; DrawShort list; } lds;
   __shared__ draw_u64 list[4 * DRAW_FEW];
-  __shared__ draw_u64 near_mass[2048];
-  __shared__ unsigned listed;
+  __shared__ union { unsigned groups[4 * DRAW_FEW]; draw_u64 mass[2048]; } near;
+  __shared__ unsigned listed, grouped;
   const int64_t q = first + blockIdx.x;
   const DrawParams par = draw_params(a, q);
   if (!draw_few(a, par)) return;                           // uniform
   const int tid = threadIdx.x;
+  if (tid == 0) { listed = 0; grouped = 0; }
   const DrawRow<TYPE> row(a, q);
-  const DrawWhole whole = draw_whole(a, q, draw_depth_scale(par), lds.slots);
+  const DrawWhole whole = draw_whole(a, q, draw_depth_scale(par), lds.border.slots);
   if (whole.best == 0) { draw_nothing<TYPE>(a, q); return; }
   const unsigned* maxima = a.maxima + q * a.groups;
-  // the k-th largest maximum: k rows at least reach it
-  const draw_u64 bound = draw_border<true>(lds, (draw_u64)par.top_k, 0, [&](auto f) { for (int g = tid; g < a.groups; g += 1024) f((draw_u64)(maxima[g] ? maxima[g] : 1u) << 32, draw_one); },
-                                     [](unsigned) { return draw_one(); }) >> 32;
-  if (tid == 0) listed = 0;
+  unsigned some[8];                                        // the first 8,192 maxima stay in registers
+#pragma unroll
+  for (int i = 0; i < 8; ++i) some[i] = tid + 1024 * i < a.groups ? maxima[tid + 1024 * i] : 0;
+  auto groups = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (tid + 1024 * i < a.groups) f(some[i], tid + 1024 * i);
+    for (int g = tid + 8192; g < a.groups; g += 1024) f(maxima[g], g);
+  };
+  // the k-th largest maximum, or somewhat less: k rows at least reach it
+  const unsigned bound = max(1u, (unsigned)(draw_border<true>(lds.border, (draw_u64)par.top_k, 0, [&](auto f) { groups([&](unsigned m, int) { f((draw_u64)max(m, 1u) << 32, draw_one); }); },
+                                                              [](unsigned) { return draw_one(); }) >> 32));
+  groups([&](unsigned m, int g) {
+    if (m < bound) return;
+    const unsigned at = atomicAdd(&grouped, 1u);
+    if (at < 4 * DRAW_FEW) near.groups[at] = (unsigned)g;
+  });
   __syncthreads();
-  const int turns = a.chunk_rows / 2048, turns_block = (turns + a.blocks - 1) / a.blocks, per_chunk = a.blocks * 256;
-  for (int g = tid; g < a.groups; g += 1024) {
-    if (maxima[g] < bound || maxima[g] == 0) continue;
-    const int chunk = g / per_chunk, block = (g - chunk * per_chunk) / 256, thread = g & 255;
-    const int end = (int)min((int64_t)a.rows, (int64_t)(chunk + 1) * a.chunk_rows);
-    for (int i = block * turns_block; i < min(turns, (block + 1) * turns_block); ++i) {
-      const int64_t c = (int64_t)chunk * a.chunk_rows + i * 2048 + 8 * thread;
-      if (c >= end) break;
+  const unsigned found = grouped;
+  draw_u64* mass = a.segments <= 2048 ? near.mass : a.mass + q * a.segments;
+  bool fits = found <= 4 * DRAW_FEW;
+  if (fits) {
+    // a group's turns are work for a thread each
+    const int turns = a.chunk_rows / 2048, turns_block = (turns + a.blocks - 1) / a.blocks, per_chunk = a.blocks * 256;
+    for (unsigned i = tid; i < found * turns_block; i += 1024) {
+      const int g = (int)near.groups[i / turns_block], chunk = g / per_chunk, block = (g - chunk * per_chunk) / 256, turn = block * turns_block + (int)(i % turns_block);
+      const int64_t c = (int64_t)chunk * a.chunk_rows + turn * 2048 + 8 * (g & 255);
+      if (turn >= turns || c >= min((int64_t)a.rows, (int64_t)(chunk + 1) * a.chunk_rows)) continue;
       unsigned key[8];
       row.keys((int)c, key);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) if (key[e] >= bound && key[e]) {
+      for (int e = 0; e < 8; ++e) if (key[e] >= bound) {
         const unsigned at = atomicAdd(&listed, 1u);
         if (at < 4 * DRAW_FEW) list[at] = draw_place(key[e], (unsigned)c + e);
       }
@@ -340,18 +419,23 @@ k_draw_few(DrawArgs a, int64_t first) {
   }
   __syncthreads();
   const unsigned n = listed;
-  draw_u64* mass = a.segments <= 2048 ? near_mass : a.mass + q * a.segments;
-  if (n > 4 * DRAW_FEW) { draw_slowly<TYPE>(a, q, row, par, whole, mass, lds); return; }     // uniform: many equal scores
+  if (!fits || n > 4 * DRAW_FEW) { draw_slowly<TYPE>(a, q, row, par, whole, mass, lds.border); return; }     // uniform: many equal scores
   const DrawWeights w = draw_weights(whole.best, par, whole.sum);
+  if (n <= 256) {
+    if (tid < (int)n) lds.list.place[tid] = list[tid];
+    __syncthreads();
+    draw_short(a, q, lds.list, n, par, w);
+    return;
+  }
   auto each = [&](auto f) { for (unsigned i = tid; i < n; i += 1024) f(list[i]); };
-  draw_u64 cut = bound << 32;                              // the listed rows and no others
-  if ((unsigned)par.top_k < n) cut = draw_border<false>(lds, (draw_u64)par.top_k, 0, [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); }, [](unsigned) { return draw_one(); });
+  draw_u64 cut = (draw_u64)bound << 32;                    // the listed rows and no others
+  if ((unsigned)par.top_k < n) cut = draw_border<false>(lds.border, (draw_u64)par.top_k, 0, [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); }, [](unsigned) { return draw_one(); });
   if (par.top_p < 2.f) {
     draw_u64 all = 0;
     each([&](draw_u64 place) { if (place >= cut) all += w.of((unsigned)(place >> 32)); });
-    const draw_u64 want = draw_share_up(par.top_p, draw_sum(all, lds.slots)), top_k = cut;
-    cut = draw_border<false>(lds, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { if (place >= top_k) f(place, [&] { return w.of((unsigned)(place >> 32)); }); }); },
-                      [&](unsigned k) { return w.of(k); });
+    const draw_u64 want = draw_share_up(par.top_p, draw_sum(all, lds.border.slots)), top_k = cut;
+    cut = draw_border<false>(lds.border, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
+                             [&](unsigned k) { return w.of(k); });
   }
   const draw_u64 least = w.least(par.min_p);
   for (int s = tid; s < a.segments; s += 1024) mass[s] = 0;
@@ -364,10 +448,11 @@ k_draw_few(DrawArgs a, int64_t first) {
     ++kept;
     if (x) atomicAdd(&mass[~(unsigned)place / DRAW_SEGMENT], x);
   });
-  kept = draw_sum(kept, (unsigned*)lds.slots);
+  kept = draw_sum(kept, (unsigned*)lds.border.slots);
   if (tid == 0 && a.num_kept) a.num_kept[q] = (int)kept;
+  __threadfence();                                         // atomics in memory passed this workgroup's cache by
   __syncthreads();
-  draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.slots);
+  draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.border.slots);
 }
 
 // Other queries with top-p: a chunk's weights by their bins.
@@ -384,19 +469,18 @@ k_draw_hist(DrawArgs a, int64_t first) {
   const float c = draw_depth_scale(par);
   for (int i = tid; i < DRAW_BINS; i += 256) bins[i] = 0;
   const DrawWhole whole = draw_whole(a, q, c, slots);
-  const float top = draw_score(whole.best), unit_weight = (float)(1 << a.hist_bits);
+  const float top = draw_score(whole.best), unit_weight = (float)(1 << a.hist_bits), c32 = c * 32.f, l = 0.69314718f / 32.f, w1 = -l * unit_weight, w2 = 0.5f * l * l * unit_weight;
   const int begin = chunk * a.chunk_rows, end = (int)min((int64_t)a.rows, (int64_t)begin + a.chunk_rows);
   for (int64_t at = (int64_t)begin + 8 * tid; at < end; at += 2048) {
     float v[8];
     row.scores_of((int)at, v);
+    // 2^-(x / 32), x what the depth has below its bin's top: 1 - x l + (x l)^2 / 2, l = ln 2 / 32, is off by 2^-19 at most.  Rows that do not
+    // count, and those below 2^-64, end in the last bin: up to 2^-64 too much each
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      // 2^-x, x the depth below the bin's top, at most 1/32 but in the last bin: 1 - x ln 2 + (x ln 2)^2 / 2 is off by 2^-19 at most
-      const float depth = draw_depth(top, v[e], c);
-      const int bin = draw_bin(depth);
-      const float x = fminf(__builtin_fmaf(bin, -1.f / 32.f, depth), 1.f / 32.f);
-      const unsigned w = (unsigned)__builtin_fmaf(unit_weight, __builtin_fmaf(x, __builtin_fmaf(x, 0.24022651f, -0.69314718f), 1.f), 0.5f);
-      if (v[e] > -__builtin_inff()) atomicAdd(&bins[bin], w);
+      const float depth = (top - v[e]) * c32, x = __builtin_amdgcn_fractf(depth);
+      const unsigned w = (unsigned)__builtin_fmaf(x, __builtin_fmaf(x, w2, w1), unit_weight);
+      atomicAdd(&bins[min((int)depth, DRAW_BINS - 1)], w);
     }
   }
   __syncthreads();
@@ -405,7 +489,7 @@ k_draw_hist(DrawArgs a, int64_t first) {
 }
 
 // The bins in which the border of top-p lies.  A weight in the histogram is off by 2^-17 of itself at most by its depth (up to 64, in fp32)
-// and polynomial and by half a unit, 2^-hist_bits at most of any but those below 2^-64: so are sums.
+// and polynomial and by a unit, 2^-hist_bits at most of any but those below 2^-64: so are sums.
 __global__ void __launch_bounds__(1024)
 k_draw_range(DrawArgs a, int64_t first) {
   __shared__ draw_u64 slots[16];
@@ -423,7 +507,7 @@ k_draw_range(DrawArgs a, int64_t first) {
   }
   const double x = (double)nx * exp2(-tid / 16.0), y = (double)ny * exp2(-tid / 16.0 - 1 / 32.0);
   double all;
-  const double before = draw_prefix(x + y, (double*)slots, all), off = __builtin_ldexp(1.0, -a.hist_bits) + 0x1p-16, want = (double)par.top_p * all;
+  const double before = draw_prefix(x + y, (double*)slots, all), off = __builtin_ldexp(2.0, -a.hist_bits) + 0x1p-16, want = (double)par.top_p * all;
   // the first bin at whose end the border may have been reached, and the first at whose end it must have been
   const double may = want * (1.0 - off), must = want * (1.0 + off);
   if (before < may && before + x + y >= may) low = before + x >= may ? 2 * tid : 2 * tid + 1;
@@ -450,40 +534,52 @@ k_draw_weigh(DrawArgs a, int64_t first) {
   const DrawWeights w = draw_weights(whole.best, par, whole.sum);
   const DrawRange range = a.range[q];
   const draw_u64 least = w.least(par.min_p);
-  // bins by their depth, 32 to a binary order of magnitude, as the histogram counts them; all lies above where there is none
-  const float top = draw_score(whole.best), low = par.top_p < 2.f ? (float)range.low : __builtin_inff(), high = range.high < DRAW_BINS - 1 ? range.high + 1.f : __builtin_inff();
+  // bins by their depth, 32 to a binary order of magnitude, as the histogram counts them
+  const float top = draw_score(whole.best), c32 = c * 32.f, low = (float)range.low, high = range.high < DRAW_BINS - 1 ? range.high + 1.f : __builtin_inff();
   const int begin = chunk * a.chunk_rows, end = (int)min((int64_t)a.rows, (int64_t)begin + a.chunk_rows);
   draw_u64 all = 0, above = 0;
   unsigned kept = 0;
-  for (int64_t s = (int64_t)begin + wave * DRAW_SEGMENT; s < end; s += 4 * DRAW_SEGMENT) {
-    const int64_t at = s + 8 * lane;
-    draw_u64 sum = 0;
-    if (at < end) {
-      float v[8];
-      row.scores_of((int)at, v);
-      unsigned near = 0;                                   // rows of the range
+  auto segments = [&](auto cuts, auto floor) {             // with top-p; with min-p
+    constexpr bool CUTS = decltype(cuts)::value, FLOOR = decltype(floor)::value;
+    for (int64_t s = (int64_t)begin + wave * DRAW_SEGMENT; s < end; s += 4 * DRAW_SEGMENT) {
+      const int64_t at = s + 8 * lane;
+      draw_u64 sum = 0;
+      if (at < end) {
+        float v[8];
+        row.scores_of((int)at, v);
+        draw_u64 near[8];                                  // lanes whose row lies in the range
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const draw_u64 x = w.of_score(v[e]);
-        const float bin = draw_depth(top, v[e], c) * 32.f;
-        all += x;
-        const bool over = bin < low, in = over && x >= least && v[e] > -__builtin_inff();
-        above += over ? x : 0;                             // before min-p: top-p goes by it
-        sum += in ? x : 0;
-        kept += in;
-        near |= (!over && bin < high && x ? 1u : 0u) << e;
-      }
-      if (near) {
+        for (int e = 0; e < 8; ++e) {
+          const draw_u64 x = w.of_score(v[e]);
+          bool in = CUTS || v[e] > -__builtin_inff();      // a row that does not count lies below every range
+          if (CUTS) {
+            const float bin = (top - v[e]) * c32;
+            in = bin < low;
+            all += x;
+            near[e] = __ballot(bin >= low && bin < high);
+            if (FLOOR) above += in ? x : 0;                // before min-p: top-p goes by it
+          }
+          if (FLOOR) in = in && x >= least;
+          sum += in ? x : 0;
+          kept += in;
+        }
+        if (CUTS) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) if (near >> e & 1u) {
-          const unsigned n = atomicAdd(&listed, 1u);
-          if (n < DRAW_LIST_CHUNK) list[n] = draw_place(draw_key(v[e]), (unsigned)at + e);
+          for (int e = 0; e < 8; ++e) if (near[e] && (near[e] >> lane & 1)) {
+            if (w.of_score(v[e]) == 0) continue;
+            const unsigned n = atomicAdd(&listed, 1u);
+            if (n < DRAW_LIST_CHUNK) list[n] = draw_place(draw_key(v[e]), (unsigned)at + e);
+          }
+          if (!FLOOR) above += sum;
         }
       }
+      sum = draw_wave_sum(sum);
+      if (lane == 0) a.mass[q * a.segments + s / DRAW_SEGMENT] = sum;
     }
-    sum = draw_wave_sum(sum);
-    if (lane == 0) a.mass[q * a.segments + s / DRAW_SEGMENT] = sum;
-  }
+  };
+  const std::true_type yes; const std::false_type no;
+  if (par.top_p < 2.f) { if (least) segments(yes, yes); else segments(yes, no); }
+  else { if (least) segments(no, yes); else segments(no, no); }
   all = draw_sum(all, slots);
   above = draw_sum(above, slots);
   kept = draw_sum(kept, (unsigned*)slots);

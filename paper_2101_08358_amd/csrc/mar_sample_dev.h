@@ -22,13 +22,12 @@ static __constant__ double draw_power[11] = {1.7071067811865475, -0.490129071734
                                              -7.21863451712333e-08, 5.002210946656729e-09};
 __device__ __forceinline__ draw_u64 draw_weight(double depth, int shift) {
   depth = fmin(depth, 64.0);
-  const int down = (int)depth + shift;                     // shift >= 2
   const double g = __builtin_amdgcn_fract(depth) - 0.5;
   double p = draw_power[10];
 #pragma unroll
   for (int i = 9; i >= 0; --i) p = __builtin_fma(p, g, draw_power[i]);
   const draw_u64 m = ((draw_u64)__double_as_longlong(p) - 0x3ff0000000000000ull) << 10;      // up to 2^62
-  return ((m >> min(down - 1, 63)) + 1) >> 1;
+  return ((m >> min((int)depth + (shift - 1), 63)) + 1) >> 1;          // shift >= 2
 }
 
 // ceil(part * whole), part in [0, 1), whole < 2^62.
