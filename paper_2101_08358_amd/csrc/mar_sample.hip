@@ -6,14 +6,15 @@
 //
 // Up to 16,384 rows (k_draw_small): a workgroup a query holds them in registers.  More:
 //   k_draw_scan    a workgroup a chunk: greatest key, rows that count, sum of weights in fp32; maxima of groups of rows
-//   k_draw_few     queries with top-k: the k-th largest of the groups' maxima bounds the k-th best row from below; rows that reach it are
-//                  picked from the groups whose maximum does, and everything else concerns those rows alone
-//   k_draw_hist    other queries with top-p: weights in fp32 by their binary order of magnitude, 1/32 apart; k_draw_range: the bins that
-//                  the border lies in, whatever the sums' rounding
-//   k_draw_weigh   every row's integer weight: the sum of all, the sums of segments of 512 rows above the range, the range's rows by themselves
-//   k_draw_rows    the border among those rows, then the draws: the segment by the sums before it, the row by a wave that weighs it again
+//   k_draw_hist    queries without top-k, with top-p: weights by their binary order of magnitude, 1/32 apart; k_draw_range: the bins that the
+//                  border lies in, whatever the rounding
+//   k_draw_weigh   queries without top-k: every row's integer weight: the sum of all, the sums of segments of 512 rows above the range, the
+//                  range's rows by themselves
+//   k_draw_rows    a workgroup a query.  Top-k: the k-th largest of the groups' maxima bounds the k-th best row from below; rows that reach it
+//                  are picked from the groups whose maximum does, and everything else concerns those rows alone.  Others: the border among
+//                  the range's rows, then the draws: the segment by the sums before it, the row by a wave that weighs it again
 // What does not fit (borders among more rows than a list holds, top-k above 1,024 with a table too large for registers) goes through
-// all rows by digits, one workgroup a query, in the last kernel.
+// all rows by digits in the last kernel.
 #include <type_traits>
 #include "mar_sample_dev.h"
 
@@ -90,13 +91,14 @@ __device__ __forceinline__ void draw_rows(const DrawArgs& a, int64_t q, const Dr
 
 // Everything by digits over all rows of a query.
 template <int TYPE>
-__device__ void draw_slowly(const DrawArgs& a, int64_t q, const DrawRow<TYPE>& row, const DrawParams& par, const DrawWhole& whole, draw_u64* mass, DrawShared& lds) {
+__device__ __attribute__((noinline)) void draw_slowly(const DrawArgs& a, int64_t q, const DrawRow<TYPE> row, const DrawParams par, const DrawWhole whole, draw_u64* mass, DrawShared& lds) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const DrawWeights w = draw_weights(whole.best, par, whole.sum);
   auto each = [&](auto f) {
-    for (int64_t c = 8 * tid; c < a.rows; c += 8 * 1024) {
-      unsigned key[8];
-      row.keys((int)c, key);
+    for (int64_t c0 = 0; c0 < a.rows; c0 += 8 * 1024) {
+      const int64_t c = c0 + 8 * tid;
+      unsigned key[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+      if (c < a.rows) row.keys((int)c, key);
 #pragma unroll
       for (int e = 0; e < 8; ++e) f(draw_place(key[e], (unsigned)c + e));
     }
@@ -135,53 +137,85 @@ __device__ void draw_slowly(const DrawArgs& a, int64_t q, const DrawRow<TYPE>& r
   draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.slots);
 }
 
-// Up to 256 rows, with all that top-k leaves among them: a thread a row compares it with all others.  Called by all threads of the workgroup.
-struct DrawShort { draw_u64 place[256], weight[256], slots[16]; };
+// Up to 256 rows, with all that top-k leaves among them: four threads a row compare it with all others.  Called by 1,024 threads.
+#define DRAW_SHORT 256
+struct DrawShort {
+  struct { draw_u64 place, weight; } row[DRAW_SHORT];
+  draw_u64 start[DRAW_SHORT], slots[16];
+  unsigned id[DRAW_SHORT];
+  float log_prob[DRAW_SHORT];
+};
 __device__ __forceinline__ void draw_short(const DrawArgs& a, int64_t q, DrawShort& lds, unsigned n, const DrawParams& par, const DrawWeights& w) {
-  const unsigned tid = threadIdx.x;
-  const draw_u64 mine = tid < n ? lds.place[tid] : 0;
-  const draw_u64 weight = tid < n ? w.of((unsigned)(mine >> 32)) : 0;
-  if (tid < n) lds.weight[tid] = weight;
+  const unsigned tid = threadIdx.x, r = tid >> 2, part = tid & 3, padded = (n + 15) & ~15u;
+  draw_u64 mine = 0;
+  if (tid >= n && tid < padded) lds.row[tid] = {0, 0};     // comes after all others
+  if (tid < n) lds.row[tid].weight = w.of((unsigned)(lds.row[tid].place >> 32));
   __syncthreads();
+  const bool has = r < n;
+  draw_u64 weight = 0;
+  if (has) { mine = lds.row[r].place; weight = lds.row[r].weight; }
+  // sums over the four threads of a row
+  auto joined = [](auto v) { v += draw_moved<0xB1, 0xf>(v); return v + draw_moved<0x4E, 0xf>(v); };       // lanes 1 0 3 2, then 2 3 0 1
   unsigned rank = 0;
   draw_u64 before = 0;
-  if (tid < n) for (unsigned i = 0; i < n; ++i) {
-    const bool better = lds.place[i] > mine;
+#pragma unroll 4
+  for (unsigned i = part; i < padded; i += 4) {
+    const auto other = lds.row[i];
+    const bool better = other.place > mine;
     rank += better;
-    before += better ? lds.weight[i] : 0;
+    before += better ? other.weight : 0;
   }
-  bool in = tid < n && (par.top_k == 0 || rank < (unsigned)par.top_k);
+  rank = joined(rank);
+  before = joined(before);
+  bool in = has && (par.top_k == 0 || rank < (unsigned)par.top_k);
   if (par.top_p < 2.f) {                                   // uniform
-    const draw_u64 want = draw_share_up(par.top_p, draw_sum(in ? weight : 0, lds.slots));
+    const draw_u64 want = draw_share_up(par.top_p, draw_sum(in && part == 0 ? weight : 0, lds.slots));
     in = in && before < (want ? want : 1);
   }
   in = in && weight >= w.least(par.min_p);
   if (a.num_kept) {
-    const unsigned kept = draw_sum(in ? 1u : 0u, (unsigned*)lds.slots);
+    const unsigned kept = draw_sum(in && part == 0 ? 1u : 0u, (unsigned*)lds.slots);
     if (tid == 0) a.num_kept[q] = (int)kept;
   }
   __syncthreads();
-  if (tid < n) lds.weight[tid] = in ? weight : 0;
-  const draw_u64 total = draw_sum(in ? weight : 0, lds.slots);      // its barriers order the list
-  if (!in) return;
-  const unsigned id = (unsigned)mine;                      // complements: greater ones come first
+  if (has && part == 0 && !in) lds.row[r] = {0, 0};
+  const draw_u64 total = draw_sum(in && part == 0 ? weight : 0, lds.slots);       // its barriers order the list
+  // by id: places of lesser ids have greater lower halves
+  const unsigned id = ~(unsigned)mine;
   draw_u64 start = 0;
-  for (unsigned i = 0; i < n; ++i) start += (unsigned)lds.place[i] > id ? lds.weight[i] : 0;
-  const float log_prob = (float)(w.distance((unsigned)(mine >> 32)) - w.log_sum(total));
-  for (int d = 0; d < a.draws; ++d) {
+  unsigned at = 0;
+#pragma unroll 4
+  for (unsigned i = part; i < padded; i += 4) {
+    const auto other = lds.row[i];
+    const bool ahead = other.weight != 0 && ~(unsigned)other.place < id;
+    at += ahead;
+    start += ahead ? other.weight : 0;
+  }
+  at = joined(at);
+  start = joined(start);
+  const unsigned count = draw_sum(in && weight && part == 0 ? 1u : 0u, (unsigned*)lds.slots);
+  if (in && weight && part == 0) {
+    lds.start[at] = start; lds.id[at] = id;
+    lds.log_prob[at] = (float)(w.distance((unsigned)(mine >> 32)) - w.log_sum(total));
+  }
+  __syncthreads();
+  for (int d = tid; d < a.draws; d += 1024) {
     const draw_u64 target = draw_target(a.uniforms[q * a.draws + d], total);
-    if (start <= target && target < start + weight) {
-      a.ids[q * a.draws + d] = (int)~id;
-      if (a.log_probs) a.log_probs[q * a.draws + d] = log_prob;
-    }
+    unsigned from = 0;                                     // the last row that begins at or below the target
+#pragma unroll
+    for (unsigned step = DRAW_SHORT / 2; step >= 1; step /= 2) if (from + step < count && lds.start[from + step] <= target) from += step;
+    a.ids[q * a.draws + d] = (int)lds.id[from];
+    if (a.log_probs) a.log_probs[q * a.draws + d] = lds.log_prob[from];
   }
 }
 
 // ------------------------------------------------------------------------------------------ up to 16,384 rows -----
-template <int TYPE>
+// CUTS: some query may have top-k or top-p; without the code for them two workgroups fit a CU.
+template <int TYPE, bool CUTS>
 __global__ void __launch_bounds__(1024)
 k_draw_small(DrawArgs a, int64_t first) {
-  __shared__ union { DrawShared border; DrawShort list; } lds;
+  __shared__ union { DrawShared border; DrawShort list; } cuts[1];
+  __shared__ draw_u64 slots[16];
   __shared__ draw_u64 starts[33];
   __shared__ unsigned listed;
   const int64_t q = first + blockIdx.x;
@@ -198,69 +232,71 @@ k_draw_small(DrawArgs a, int64_t first) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) mine = fmaxf(mine, v[b][e]);
   }
-  const unsigned best = draw_reduce(draw_key(mine), (unsigned*)lds.border.slots, DrawMax());
+  const unsigned best = draw_reduce(draw_key(mine), (unsigned*)slots, DrawMax());
   if (best == 0) { draw_nothing<TYPE>(a, q); return; }     // uniform
+  auto place = [&](int b, int e) { return draw_place(draw_key(v[b][e]), (unsigned)(8192 * b + 8 * tid + e)); };
+  draw_u64 cut = 1;
+  if constexpr (CUTS) if (par.top_k > 0 && par.top_k <= 128 && par.top_k < a.rows) {       // uniform
+    // the k-th largest of the threads' maxima bounds the k-th best row from below: few rows reach it
+    const unsigned bound = max(1u, (unsigned)(draw_border<true>(cuts[0].border, (draw_u64)par.top_k, 0, [&](auto f) { f((draw_u64)max(draw_key(mine), 1u) << 32, draw_one); },
+                                                                [](unsigned) { return draw_one(); }) >> 32));
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (draw_key(v[b][e]) >= bound) {
+        const unsigned n = atomicAdd(&listed, 1u);
+        if (n < DRAW_SHORT) cuts[0].list.row[n].place = place(b, e);
+      }
+    __syncthreads();
+    if (listed <= DRAW_SHORT) { draw_short(a, q, cuts[0].list, listed, par, draw_weights(best, par, 256.f)); return; }
+  }
   const float c = draw_depth_scale(par), top = draw_score(best);
   float approx = 0.f;
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
     for (int e = 0; e < 8; ++e) approx += __builtin_amdgcn_exp2f(-draw_depth(top, v[b][e], c));
-  approx = draw_sum(approx, (float*)lds.border.slots);
+  approx = draw_sum(approx, (float*)slots);
   const DrawWeights w = draw_weights(best, par, approx);
-  auto place = [&](int b, int e) { return draw_place(draw_key(v[b][e]), (unsigned)(8192 * b + 8 * tid + e)); };
-  draw_u64 cut = 1;
-  if (par.top_k > 0 && par.top_k < a.rows) {               // uniform
-    if (par.top_k <= 128) {
-      // the k-th largest of the threads' maxima bounds the k-th best row from below: few rows reach it
-      const unsigned bound = (unsigned)(draw_border<true>(lds.border, (draw_u64)par.top_k, 0, [&](auto f) { f((draw_u64)max(draw_key(mine), 1u) << 32, draw_one); },
-                                                         [](unsigned) { return draw_one(); }) >> 32);
-      __syncthreads();
+  if constexpr (CUTS) {
+    if (par.top_k > 0 && par.top_k < a.rows) {             // uniform
+      unsigned count = 0;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) if (draw_key(v[b][e]) >= max(bound, 1u)) {
-          const unsigned n = atomicAdd(&listed, 1u);
-          if (n < 256) lds.list.place[n] = place(b, e);
-        }
-      __syncthreads();
-      if (listed <= 256) { draw_short(a, q, lds.list, listed, par, w); return; }
+        for (int e = 0; e < 8; ++e) count += v[b][e] > -__builtin_inff();
+      count = draw_sum(count, (unsigned*)slots);
+      if ((unsigned)par.top_k < count) {
+        auto ones = [&](auto f) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f(place(b, e), draw_one);
+        };
+        cut = draw_border<false>(cuts[0].border, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
+      }
     }
-    unsigned count = 0;
+    if (par.top_p < 2.f) {
+      draw_u64 all = 0;
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) count += v[b][e] > -__builtin_inff();
-    count = draw_sum(count, (unsigned*)lds.border.slots);
-    if ((unsigned)par.top_k < count) {
-      auto ones = [&](auto f) {
+        for (int e = 0; e < 8; ++e) all += place(b, e) >= cut ? w.of_score(v[b][e]) : 0;
+      const draw_u64 want = draw_share_up(par.top_p, draw_sum(all, slots)), top_k = cut;
+      auto each = [&](auto f) {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f(place(b, e), draw_one);
+          for (int e = 0; e < 8; ++e) { const draw_u64 here = place(b, e); f(here >= top_k ? here : 0, [&] { return w.of_score(v[b][e]); }); }
       };
-      cut = draw_border<false>(lds.border, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
+      cut = draw_border<false>(cuts[0].border, want ? want : 1, 0, each, [&](unsigned k) { return w.of(k); });
     }
-  }
-  if (par.top_p < 2.f) {
-    draw_u64 all = 0;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) all += place(b, e) >= cut ? w.of_score(v[b][e]) : 0;
-    const draw_u64 want = draw_share_up(par.top_p, draw_sum(all, lds.border.slots)), top_k = cut;
-    auto each = [&](auto f) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { const draw_u64 here = place(b, e); f(here >= top_k ? here : 0, [&] { return w.of_score(v[b][e]); }); }
-    };
-    cut = draw_border<false>(lds.border, want ? want : 1, 0, each, [&](unsigned k) { return w.of(k); });
   }
   const draw_u64 least = w.least(par.min_p);
   auto weight = [&](int b, int e) {
     const draw_u64 x = w.of_score(v[b][e]);
-    return place(b, e) >= cut && x >= least ? x : 0;
+    return (CUTS ? place(b, e) >= cut : v[b][e] > -__builtin_inff()) && x >= least ? x : 0;
   };
   unsigned kept = 0;
   draw_u64 sum[2] = {0, 0}, run[2];
@@ -269,14 +305,14 @@ k_draw_small(DrawArgs a, int64_t first) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const draw_u64 x = w.of_score(v[b][e]);
-      const bool in = place(b, e) >= cut && x >= least;
+      const bool in = (CUTS ? place(b, e) >= cut : v[b][e] > -__builtin_inff()) && x >= least;
       kept += in;
       sum[b] += in ? x : 0;
     }
     run[b] = draw_wave_prefix(sum[b]);
   }
   if (a.num_kept) {                                        // uniform
-    kept = draw_sum(kept, (unsigned*)lds.border.slots);
+    kept = draw_sum(kept, (unsigned*)slots);
     if (tid == 0) a.num_kept[q] = (int)kept;
   }
 #pragma unroll
@@ -364,97 +400,6 @@ k_draw_scan(DrawArgs a, int64_t first) {
   }
 }
 
-// Queries with top-k: a workgroup a query.
-template <int TYPE>
-__global__ void __launch_bounds__(1024)
-k_draw_few(DrawArgs a, int64_t first) {
-  __shared__ union { DrawShared border; DrawShort list; } lds;
-  __shared__ draw_u64 list[4 * DRAW_FEW];
-  __shared__ union { unsigned groups[4 * DRAW_FEW]; draw_u64 mass[2048]; } near;
-  __shared__ unsigned listed, grouped;
-  const int64_t q = first + blockIdx.x;
-  const DrawParams par = draw_params(a, q);
-  if (!draw_few(a, par)) return;                           // uniform
-  const int tid = threadIdx.x;
-  if (tid == 0) { listed = 0; grouped = 0; }
-  const DrawRow<TYPE> row(a, q);
-  const DrawWhole whole = draw_whole(a, q, draw_depth_scale(par), lds.border.slots);
-  if (whole.best == 0) { draw_nothing<TYPE>(a, q); return; }
-  const unsigned* maxima = a.maxima + q * a.groups;
-  unsigned some[8];                                        // the first 8,192 maxima stay in registers
-#pragma unroll
-  for (int i = 0; i < 8; ++i) some[i] = tid + 1024 * i < a.groups ? maxima[tid + 1024 * i] : 0;
-  auto groups = [&](auto f) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) if (tid + 1024 * i < a.groups) f(some[i], tid + 1024 * i);
-    for (int g = tid + 8192; g < a.groups; g += 1024) f(maxima[g], g);
-  };
-  // the k-th largest maximum, or somewhat less: k rows at least reach it
-  const unsigned bound = max(1u, (unsigned)(draw_border<true>(lds.border, (draw_u64)par.top_k, 0, [&](auto f) { groups([&](unsigned m, int) { f((draw_u64)max(m, 1u) << 32, draw_one); }); },
-                                                              [](unsigned) { return draw_one(); }) >> 32));
-  groups([&](unsigned m, int g) {
-    if (m < bound) return;
-    const unsigned at = atomicAdd(&grouped, 1u);
-    if (at < 4 * DRAW_FEW) near.groups[at] = (unsigned)g;
-  });
-  __syncthreads();
-  const unsigned found = grouped;
-  draw_u64* mass = a.segments <= 2048 ? near.mass : a.mass + q * a.segments;
-  bool fits = found <= 4 * DRAW_FEW;
-  if (fits) {
-    // a group's turns are work for a thread each
-    const int turns = a.chunk_rows / 2048, turns_block = (turns + a.blocks - 1) / a.blocks, per_chunk = a.blocks * 256;
-    for (unsigned i = tid; i < found * turns_block; i += 1024) {
-      const int g = (int)near.groups[i / turns_block], chunk = g / per_chunk, block = (g - chunk * per_chunk) / 256, turn = block * turns_block + (int)(i % turns_block);
-      const int64_t c = (int64_t)chunk * a.chunk_rows + turn * 2048 + 8 * (g & 255);
-      if (turn >= turns || c >= min((int64_t)a.rows, (int64_t)(chunk + 1) * a.chunk_rows)) continue;
-      unsigned key[8];
-      row.keys((int)c, key);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) if (key[e] >= bound) {
-        const unsigned at = atomicAdd(&listed, 1u);
-        if (at < 4 * DRAW_FEW) list[at] = draw_place(key[e], (unsigned)c + e);
-      }
-    }
-  }
-  __syncthreads();
-  const unsigned n = listed;
-  if (!fits || n > 4 * DRAW_FEW) { draw_slowly<TYPE>(a, q, row, par, whole, mass, lds.border); return; }     // uniform: many equal scores
-  const DrawWeights w = draw_weights(whole.best, par, whole.sum);
-  if (n <= 256) {
-    if (tid < (int)n) lds.list.place[tid] = list[tid];
-    __syncthreads();
-    draw_short(a, q, lds.list, n, par, w);
-    return;
-  }
-  auto each = [&](auto f) { for (unsigned i = tid; i < n; i += 1024) f(list[i]); };
-  draw_u64 cut = (draw_u64)bound << 32;                    // the listed rows and no others
-  if ((unsigned)par.top_k < n) cut = draw_border<false>(lds.border, (draw_u64)par.top_k, 0, [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); }, [](unsigned) { return draw_one(); });
-  if (par.top_p < 2.f) {
-    draw_u64 all = 0;
-    each([&](draw_u64 place) { if (place >= cut) all += w.of((unsigned)(place >> 32)); });
-    const draw_u64 want = draw_share_up(par.top_p, draw_sum(all, lds.border.slots)), top_k = cut;
-    cut = draw_border<false>(lds.border, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
-                             [&](unsigned k) { return w.of(k); });
-  }
-  const draw_u64 least = w.least(par.min_p);
-  for (int s = tid; s < a.segments; s += 1024) mass[s] = 0;
-  __syncthreads();
-  unsigned kept = 0;
-  each([&](draw_u64 place) {
-    if (place < cut) return;
-    const draw_u64 x = w.of((unsigned)(place >> 32));
-    if (x < least) return;
-    ++kept;
-    if (x) atomicAdd(&mass[~(unsigned)place / DRAW_SEGMENT], x);
-  });
-  kept = draw_sum(kept, (unsigned*)lds.border.slots);
-  if (tid == 0 && a.num_kept) a.num_kept[q] = (int)kept;
-  __threadfence();                                         // atomics in memory passed this workgroup's cache by
-  __syncthreads();
-  draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.border.slots);
-}
-
 // Other queries with top-p: a chunk's weights by their bins.
 template <int TYPE>
 __global__ void __launch_bounds__(256)
@@ -501,6 +446,7 @@ k_draw_range(DrawArgs a, int64_t first) {
   if (par.top_p >= 2.f) { if (tid == 0) a.range[q] = {DRAW_BINS, DRAW_BINS}; return; }     // everything lies above
   if (tid == 0) { low = DRAW_BINS - 1; high = DRAW_BINS - 1; }
   draw_u64 nx = 0, ny = 0;                                 // bins 2 tid and 2 tid + 1
+#pragma unroll 8
   for (int k = 0; k < a.chunks; ++k) {
     const uint2 v = *reinterpret_cast<const uint2*>(a.hist + (q * a.chunks + k) * DRAW_BINS + 2 * tid);
     nx += v.x; ny += v.y;
@@ -556,7 +502,7 @@ k_draw_weigh(DrawArgs a, int64_t first) {
             const float bin = (top - v[e]) * c32;
             in = bin < low;
             all += x;
-            near[e] = __ballot(bin >= low && bin < high);
+            near[e] = __builtin_amdgcn_ballot_w64(bin >= low) & __builtin_amdgcn_ballot_w64(bin < high);
             if (FLOOR) above += in ? x : 0;                // before min-p: top-p goes by it
           }
           if (FLOOR) in = in && x >= least;
@@ -565,8 +511,9 @@ k_draw_weigh(DrawArgs a, int64_t first) {
         }
         if (CUTS) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) if (near[e] && (near[e] >> lane & 1)) {
-            if (w.of_score(v[e]) == 0) continue;
+          for (int e = 0; e < 8; ++e) if (near[e]) {       // uniform
+            const float bin = (top - v[e]) * c32;
+            if (!(bin >= low && bin < high)) continue;
             const unsigned n = atomicAdd(&listed, 1u);
             if (n < DRAW_LIST_CHUNK) list[n] = draw_place(draw_key(v[e]), (unsigned)at + e);
           }
@@ -574,7 +521,7 @@ k_draw_weigh(DrawArgs a, int64_t first) {
         }
       }
       sum = draw_wave_sum(sum);
-      if (lane == 0) a.mass[q * a.segments + s / DRAW_SEGMENT] = sum;
+      if (lane == 0) a.mass[q * a.mass_pitch + s / DRAW_SEGMENT] = sum;
     }
   };
   const std::true_type yes; const std::false_type no;
@@ -595,73 +542,145 @@ k_draw_weigh(DrawArgs a, int64_t first) {
   for (unsigned i = threadIdx.x; i < n; i += 256) if (list_at + i < (unsigned)a.list) a.lists[q * a.list + list_at + i] = list[i];
 }
 
-// The border among the range's rows, and the draws.
+// A workgroup a query.
 template <int TYPE>
 __global__ void __launch_bounds__(1024)
 k_draw_rows(DrawArgs a, int64_t first) {
-  __shared__ DrawShared lds;
+  __shared__ union { DrawShared border; DrawShort few; } lds;
+  __shared__ draw_u64 list[DRAW_LIST];
+  __shared__ union { unsigned groups[4 * DRAW_FEW]; draw_u64 mass[2048]; } near;
+  __shared__ unsigned listed, grouped;
   const int64_t q = first + blockIdx.x;
   const DrawParams par = draw_params(a, q);
-  if (draw_few(a, par)) return;                            // uniform
   const int tid = threadIdx.x;
+  if (tid == 0) { listed = 0; grouped = 0; }
   const DrawRow<TYPE> row(a, q);
-  const DrawWhole whole = draw_whole(a, q, draw_depth_scale(par), lds.slots);
-  if (whole.best == 0) { draw_nothing<TYPE>(a, q); return; }
-  draw_u64* mass = a.mass + q * a.segments;
-  const unsigned n = a.listed[q];
+  const DrawWhole whole = draw_whole(a, q, draw_depth_scale(par), lds.border.slots);
+  if (whole.best == 0) { draw_nothing<TYPE>(a, q); return; }         // uniform, like all conditions that end in a return or a barrier
+  const bool few = draw_few(a, par), cuts = par.top_p < 2.f;
   const DrawWeights w = draw_weights(whole.best, par, whole.sum);
-  const bool in = tid < a.chunks;
-  const draw_u64* list = a.lists + q * a.list;
-  auto each = [&](auto f) { for (unsigned i = tid; i < n; i += 1024) f(list[i]); };
-  bool slowly = !draw_all(a, par) || n > (unsigned)a.list;
-  draw_u64 want = 1, above = 0;
-  if (!slowly && par.top_p < 2.f) {                        // uniform
-    draw_u64 all = 0, listed = 0;
-    if (in) { all = a.totals[2 * (q * a.chunks + tid)]; above = a.totals[2 * (q * a.chunks + tid) + 1]; }
-    each([&](draw_u64 place) { listed += w.of((unsigned)(place >> 32)); });
-    all = draw_sum(all, lds.slots);
-    above = draw_sum(above, lds.slots);
-    listed = draw_sum(listed, lds.slots);
-    want = draw_share_up(par.top_p, all);
-    if (want == 0) want = 1;
-    // temperatures whose inverse 32 bits do not hold: the histogram was of something else
-    slowly = above >= want || above + listed < want;
-  }
-  if (slowly) { draw_slowly<TYPE>(a, q, row, par, whole, mass, lds); return; }
-  const draw_u64 least = w.least(par.min_p);
-  unsigned kept = draw_sum(in ? a.kept[q * a.chunks + tid] : 0u, (unsigned*)lds.slots);
-  draw_u64 cut = 1;
-  if (par.top_p < 2.f) {
-    cut = draw_border<false>(lds, want, above, [&](auto f) { each([&](draw_u64 place) { f(place, [&] { return w.of((unsigned)(place >> 32)); }); }); },
-                             [&](unsigned k) { return w.of(k); });
-    unsigned more = 0;
-    each([&](draw_u64 place) {
-      if (place < cut) return;
-      const draw_u64 x = w.of((unsigned)(place >> 32));
-      if (x < least) return;
-      ++more;
-      if (x) atomicAdd(&mass[~(unsigned)place / DRAW_SEGMENT], x);
+  const bool held = a.segments <= 2048;                    // the segments' sums fit LDS
+  draw_u64* mass = held ? near.mass : a.mass + q * a.mass_pitch;
+  draw_u64 cut = 1, all = 0, above = 0;                    // of the listed rows; sums of weights: of all rows for top-p, of those above the list
+  unsigned n, kept = 0;
+  bool slowly;
+  if (few) {
+    const unsigned* maxima = a.maxima + q * a.groups;
+    unsigned some[8];                                      // the first 8,192 maxima stay in registers
+#pragma unroll
+    for (int i = 0; i < 8; ++i) some[i] = tid + 1024 * i < a.groups ? maxima[tid + 1024 * i] : 0;
+    auto groups = [&](auto f) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) if (1024 * i < a.groups) f(some[i], tid + 1024 * i);
+      for (int g = tid + 8192; g - tid < a.groups; g += 1024) f(g < a.groups ? maxima[g] : 0, g);
+    };
+    // the k-th largest maximum, or somewhat less: k rows at least reach it
+    const unsigned bound = max(1u, (unsigned)(draw_border<true>(lds.border, (draw_u64)par.top_k, 0, [&](auto f) { groups([&](unsigned m, int g) { f(g < a.groups ? (draw_u64)max(m, 1u) << 32 : 0, draw_one); }); },
+                                                                [](unsigned) { return draw_one(); }) >> 32));
+    groups([&](unsigned m, int g) {
+      if (m < bound) return;
+      const unsigned at = atomicAdd(&grouped, 1u);
+      if (at < 4 * DRAW_FEW) near.groups[at] = (unsigned)g;
     });
-    kept += draw_sum(more, (unsigned*)lds.slots);
-    __threadfence();                                       // the atomics passed this workgroup's cache by
+    __syncthreads();
+    const unsigned found = grouped;
+    if (found <= 4 * DRAW_FEW) {
+      // a group's turns are work for a thread each
+      const int turns = a.chunk_rows / 2048, turns_block = (turns + a.blocks - 1) / a.blocks, per_chunk = a.blocks * 256;
+      for (unsigned i = tid; i < found * turns_block; i += 1024) {
+        const int g = (int)near.groups[i / turns_block], chunk = g / per_chunk, block = (g - chunk * per_chunk) / 256, turn = block * turns_block + (int)(i % turns_block);
+        const int64_t c = (int64_t)chunk * a.chunk_rows + turn * 2048 + 8 * (g & 255);
+        if (turn >= turns || c >= min((int64_t)a.rows, (int64_t)(chunk + 1) * a.chunk_rows)) continue;
+        unsigned key[8];
+        row.keys((int)c, key);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (key[e] >= bound) {
+          const unsigned at = atomicAdd(&listed, 1u);
+          if (at < DRAW_LIST) list[at] = draw_place(key[e], (unsigned)c + e);
+        }
+      }
+    }
+    __syncthreads();
+    n = listed;
+    slowly = found > 4 * DRAW_FEW || n > DRAW_LIST;        // many equal rows
+    cut = (draw_u64)bound << 32;
+    if (!slowly && n <= DRAW_SHORT) {
+      if (tid < (int)n) lds.few.row[tid].place = list[tid];
+      __syncthreads();
+      draw_short(a, q, lds.few, n, par, w);
+      return;
+    }
+    if (!slowly) for (int s = tid; s < a.segments; s += 1024) mass[s] = 0;
+  } else {
+    n = cuts ? a.listed[q] : 0;
+    slowly = !draw_all(a, par) || n > (unsigned)a.list;
+    if (!slowly) {
+      for (unsigned i = tid; i < n; i += 1024) list[i] = a.lists[q * a.list + i];
+      if (held) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) if (tid + 1024 * i < a.segments) near.mass[tid + 1024 * i] = a.mass[q * a.mass_pitch + tid + 1024 * i];
+      }
+      if (tid < a.chunks) {
+        all = a.totals[2 * (q * a.chunks + tid)]; above = a.totals[2 * (q * a.chunks + tid) + 1];
+        kept = a.kept[q * a.chunks + tid];
+      }
+      all = draw_sum(all, lds.border.slots);
+      above = draw_sum(above, lds.border.slots);
+    }
   }
-  if (tid == 0 && a.num_kept) a.num_kept[q] = (int)kept;
-  __syncthreads();
-  draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.slots);
+  if (!slowly) {
+    __syncthreads();
+    auto each = [&](auto f) { for (unsigned i = tid; i - tid < n; i += 1024) f(i < n ? list[i] : 0); };
+    // top-k by counts, then top-p by weights
+    for (int kind = few && (unsigned)par.top_k < n ? 0 : 1; kind < (cuts ? 2 : 1) && !slowly; ++kind) {
+      draw_u64 want = (draw_u64)par.top_k;
+      const draw_u64 last = cut;
+      if (kind == 1) {
+        draw_u64 sum = 0;
+        each([&](draw_u64 place) { sum += place >= last ? w.of((unsigned)(place >> 32)) : 0; });
+        sum = draw_sum(sum, lds.border.slots);
+        want = draw_share_up(par.top_p, few ? sum : all);
+        if (want == 0) want = 1;
+        // temperatures whose inverse 32 bits do not hold: the histogram was of something else
+        slowly = above >= want || above + sum < want;
+      }
+      if (!slowly) cut = draw_border<false>(lds.border, want, kind == 1 ? above : 0, [&](auto f) {
+        each([&](draw_u64 place) { f(place >= last ? place : 0, [&] { return kind == 1 ? w.of((unsigned)(place >> 32)) : draw_one(); }); });
+      }, [&](unsigned k) { return kind == 1 ? w.of(k) : draw_one(); });
+    }
+    if (!slowly) {
+      const draw_u64 least = w.least(par.min_p);
+      each([&](draw_u64 place) {
+        if (place < cut) return;
+        const draw_u64 x = w.of((unsigned)(place >> 32));
+        if (x < least) return;
+        ++kept;
+        if (x) atomicAdd(&mass[~(unsigned)place / DRAW_SEGMENT], x);
+      });
+      kept = draw_sum(kept, (unsigned*)lds.border.slots);
+      if (tid == 0 && a.num_kept) a.num_kept[q] = (int)kept;
+      // additions in memory pass the CU's cache by, which holds none of their lines: a query's sums have lines of their own
+      __syncthreads();
+      draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.border.slots);
+    }
+  }
+  if (slowly) draw_slowly<TYPE>(a, q, row, par, whole, a.mass + q * a.mass_pitch, lds.border);
 }
 
 // ------------------------------------------------------------------------------------------ launches -----
 // Kernels that no query of the call can need, as far as the host knows, are left out.
 template <int TYPE> static void launch_draws(const DrawArgs& a, int64_t queries, hipStream_t st) {
   if (a.rows <= DRAW_SMALL) {
-    sm_launches(queries, 1024, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_small<TYPE>, dim3(n), dim3(1024), 0, st, a, first); });
+    const bool cuts = a.temperatures || a.temperature == 0.f || a.top_ks || a.top_k > 0 || a.top_ps || a.top_p < 1.f;
+    sm_launches(queries, 1024, [&](int64_t first, unsigned n) {
+      if (cuts) hipLaunchKernelGGL((k_draw_small<TYPE, true>), dim3(n), dim3(1024), 0, st, a, first);
+      else hipLaunchKernelGGL((k_draw_small<TYPE, false>), dim3(n), dim3(1024), 0, st, a, first);
+    });
     return;
   }
   const bool greedy = !a.temperatures && a.temperature == 0.f;
-  const bool few = a.temperatures || a.top_ks || greedy || (a.top_k > 0 && a.top_k <= DRAW_FEW);
   const bool all = a.top_ks || (!greedy && (a.top_k == 0 || a.top_k >= a.rows)), cuts = a.top_ps || a.top_p < 1.f;
   sm_launches(queries * a.chunks, 256, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_scan<TYPE>, dim3(n), dim3(256), 0, st, a, first); });
-  if (few) sm_launches(queries, 1024, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_few<TYPE>, dim3(n), dim3(1024), 0, st, a, first); });
   if (all) {
     if (cuts) sm_launches(queries * a.chunks, 256, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_hist<TYPE>, dim3(n), dim3(256), 0, st, a, first); });
     sm_launches(queries, 1024, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_range, dim3(n), dim3(1024), 0, st, a, first); });
@@ -689,7 +708,7 @@ static const char* draw_check(const mar_sampling* p, int* code) {
   return nullptr;
 }
 // Chunks: as many as fill the device some eight times, of 2,048 to 2^21 rows.  Blocks: groups enough for top-k's bound.
-struct DrawLayout { size_t stats, maxima, hist, range, totals, kept, listed, lists, mass, bytes; int segments, chunks, chunk_rows, blocks, groups, list, hist_bits; };
+struct DrawLayout { size_t stats, maxima, hist, range, totals, kept, listed, lists, mass, bytes; int segments, chunks, chunk_rows, blocks, groups, list, hist_bits, mass_pitch; };
 static DrawLayout draw_layout(const mar_sampling* p) {
   DrawLayout L = {};
   if (p->num_rows <= DRAW_SMALL || p->num_queries == 0) { L.bytes = 256; return L; }
@@ -717,7 +736,8 @@ static DrawLayout draw_layout(const mar_sampling* p) {
   L.kept = take(Q * L.chunks * 4);
   L.listed = take(Q * 4);
   L.lists = take(Q * L.list * 8);
-  L.mass = take(Q * L.segments * 8);
+  L.mass_pitch = (L.segments + 15) / 16 * 16;              // lines of 128 bytes
+  L.mass = take(Q * L.mass_pitch * 8);
   L.bytes = at;
   return L;
 }
@@ -753,7 +773,7 @@ extern "C" int mar_sample_rows(const mar_sampling* p, const void* scores, const 
   char* const ws = (char*)workspace;
   a.stats = (DrawChunk*)(ws + L.stats); a.maxima = (unsigned*)(ws + L.maxima); a.hist = (unsigned*)(ws + L.hist); a.hist_bits = L.hist_bits; a.range = (DrawRange*)(ws + L.range);
   a.totals = (draw_u64*)(ws + L.totals); a.kept = (unsigned*)(ws + L.kept); a.listed = (unsigned*)(ws + L.listed); a.lists = (draw_u64*)(ws + L.lists);
-  a.mass = (draw_u64*)(ws + L.mass);
+  a.mass = (draw_u64*)(ws + L.mass); a.mass_pitch = L.mass_pitch;
   const hipStream_t st = (hipStream_t)hip_stream;
   if (p->dtype == MAR_DTYPE_FP32) launch_draws<0>(a, p->num_queries, st);
   else if (p->dtype == MAR_DTYPE_BF16) launch_draws<1>(a, p->num_queries, st);

@@ -72,7 +72,8 @@ struct DrawArgs {
   unsigned* kept;                   // [queries][chunks]: rows kept above the range
   unsigned* listed;                 // [queries]: rows in the list (more than there are places: it does not serve)
   draw_u64* lists;                  // [queries][list]
-  draw_u64* mass;                   // [queries][segments]
+  draw_u64* mass;                   // [queries][mass_pitch]: sums of weights kept in segments
+  int32_t mass_pitch;
 };
 // A query's parameters with the special values resolved.
 struct DrawParams { double inv_temperature; int top_k; float top_p, min_p; };   // top_k 0, top_p 2, min_p 0: off
@@ -205,6 +206,21 @@ struct DrawShared {
   draw_u64 bins[2048], slots[16], found_sum, found_all;
   unsigned found, ends[2][16];
 };
+// Adds a wave's weights to their bins.  Lanes that share a bin add up first, as long as many do: additions to one address go one by one.
+__device__ __forceinline__ void draw_add(DrawShared& lds, bool has, unsigned bin, draw_u64 w) {
+  draw_u64 left = __builtin_amdgcn_ballot_w64(has);
+  for (int turn = 0; turn < 4 && left; ++turn) {           // uniform
+    const unsigned one = (unsigned)__builtin_amdgcn_readlane((int)bin, __ffsll((long long)left) - 1);
+    const bool same = has && bin == one;
+    const draw_u64 lanes = __builtin_amdgcn_ballot_w64(same);
+    if (__popcll(lanes) < 6) break;
+    const draw_u64 sum = draw_wave_sum(same ? w : 0);
+    if ((int)(threadIdx.x & 63) == __ffsll((long long)lanes) - 1) atomicAdd(&lds.bins[one], sum);
+    has = has && !same;
+    left &= ~lanes;
+  }
+  if (has) atomicAdd(&lds.bins[bin], w);
+}
 // One digit: bins[..] have been summed up; the bin, from the top, in which the sum reaches `want`.  over: the sum above it, all: its own.
 __device__ __forceinline__ unsigned draw_digit(DrawShared& lds, draw_u64 want, draw_u64& over, draw_u64& all) {
   const int hi = 2047 - 2 * (int)threadIdx.x;              // a pair of bins a thread, from the top
@@ -225,7 +241,7 @@ __device__ __forceinline__ unsigned draw_digit(DrawShared& lds, draw_u64 want, d
 // above all rows that `each` goes through.  By digits of up to 11 bits of the keys' distance from the least one, so that the first digit
 // spreads whatever the range (scores share their first bits: by those, most rows would meet at few addresses, one after the other),
 // then, where several rows share the border's key, of the ids.  All 1,024 threads call it; each(f) calls f(place, weight) for every row
-// of the thread, weight() its weight, of(key) that of a key.  COARSE: one digit, and the least key of its bin alone.
+// of the thread, weight() its weight, as often in all lanes of a wave (place 0: no row); of(key): a key's weight.  COARSE: one digit, and the least key of its bin alone.
 template <bool COARSE, typename E, typename W>
 __device__ __forceinline__ draw_u64 draw_border(DrawShared& lds, draw_u64 want, draw_u64 over, E each, W of) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -246,10 +262,8 @@ __device__ __forceinline__ draw_u64 draw_border(DrawShared& lds, draw_u64 want, 
     __syncthreads();
     each([&](draw_u64 place, auto weight) {
       const unsigned k = (unsigned)(place >> 32);
-      if (place != 0 && k >= base && (draw_u64)(k - base) >> left == 0) {
-        const draw_u64 w = weight();
-        if (w) atomicAdd(&lds.bins[(k - base) >> shift], w);
-      }
+      const bool has = place != 0 && k >= base && (draw_u64)(k - base) >> left == 0;
+      draw_add(lds, has, (k - base) >> shift, has ? weight() : 0);
     });
     __syncthreads();
     base += draw_digit(lds, want, over, ties) << shift;
@@ -266,7 +280,8 @@ __device__ __forceinline__ draw_u64 draw_border(DrawShared& lds, draw_u64 want, 
     __syncthreads();
     each([&](draw_u64 place, auto weight) {
       const unsigned id = (unsigned)place;
-      if (place != 0 && (unsigned)(place >> 32) == base && (level == 0 || id >> (shift + width) == prefix)) atomicAdd(&lds.bins[id >> shift & ((1u << width) - 1)], weight());
+      const bool has = place != 0 && (unsigned)(place >> 32) == base && (level == 0 || id >> (shift + width) == prefix);
+      draw_add(lds, has, id >> shift & ((1u << width) - 1), has ? weight() : 0);
     });
     __syncthreads();
     prefix = prefix << width | draw_digit(lds, want, over, ties);
