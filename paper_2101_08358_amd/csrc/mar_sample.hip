@@ -212,11 +212,11 @@ __device__ __forceinline__ void draw_short(const DrawArgs& a, int64_t q, DrawSho
 // ------------------------------------------------------------------------------------------ up to 16,384 rows -----
 // CUTS: some query may have top-k or top-p; without the code for them two workgroups fit a CU.
 template <int TYPE, bool CUTS>
-__global__ void __launch_bounds__(1024)
+__global__ void __launch_bounds__(1024, CUTS ? 4 : 8)
 k_draw_small(DrawArgs a, int64_t first) {
-  __shared__ union { DrawShared border; DrawShort list; } cuts[1];
+  __shared__ union { DrawShared border; DrawShort list; draw_u64 before[2048]; } lds;
   __shared__ draw_u64 slots[16];
-  __shared__ draw_u64 starts[33];
+  __shared__ draw_u64 starts[32];
   __shared__ unsigned listed;
   const int64_t q = first + blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -238,7 +238,7 @@ k_draw_small(DrawArgs a, int64_t first) {
   draw_u64 cut = 1;
   if constexpr (CUTS) if (par.top_k > 0 && par.top_k <= 128 && par.top_k < a.rows) {       // uniform
     // the k-th largest of the threads' maxima bounds the k-th best row from below: few rows reach it
-    const unsigned bound = max(1u, (unsigned)(draw_border<true>(cuts[0].border, (draw_u64)par.top_k, 0, [&](auto f) { f((draw_u64)max(draw_key(mine), 1u) << 32, draw_one); },
+    const unsigned bound = max(1u, (unsigned)(draw_border<true>(lds.border, (draw_u64)par.top_k, 0, [&](auto f) { f((draw_u64)max(draw_key(mine), 1u) << 32, draw_one); },
                                                                 [](unsigned) { return draw_one(); }) >> 32));
     __syncthreads();
 #pragma unroll
@@ -246,10 +246,10 @@ k_draw_small(DrawArgs a, int64_t first) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) if (draw_key(v[b][e]) >= bound) {
         const unsigned n = atomicAdd(&listed, 1u);
-        if (n < DRAW_SHORT) cuts[0].list.row[n].place = place(b, e);
+        if (n < DRAW_SHORT) lds.list.row[n].place = place(b, e);
       }
     __syncthreads();
-    if (listed <= DRAW_SHORT) { draw_short(a, q, cuts[0].list, listed, par, draw_weights(best, par, 256.f)); return; }
+    if (listed <= DRAW_SHORT) { draw_short(a, q, lds.list, listed, par, draw_weights(best, par, 256.f)); return; }
   }
   const float c = draw_depth_scale(par), top = draw_score(best);
   float approx = 0.f;
@@ -274,7 +274,7 @@ k_draw_small(DrawArgs a, int64_t first) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) f(place(b, e), draw_one);
         };
-        cut = draw_border<false>(cuts[0].border, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
+        cut = draw_border<false>(lds.border, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
       }
     }
     if (par.top_p < 2.f) {
@@ -290,14 +290,10 @@ k_draw_small(DrawArgs a, int64_t first) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) { const draw_u64 here = place(b, e); f(here >= top_k ? here : 0, [&] { return w.of_score(v[b][e]); }); }
       };
-      cut = draw_border<false>(cuts[0].border, want ? want : 1, 0, each, [&](unsigned k) { return w.of(k); });
+      cut = draw_border<false>(lds.border, want ? want : 1, 0, each, [&](unsigned k) { return w.of(k); });
     }
   }
   const draw_u64 least = w.least(par.min_p);
-  auto weight = [&](int b, int e) {
-    const draw_u64 x = w.of_score(v[b][e]);
-    return (CUTS ? place(b, e) >= cut : v[b][e] > -__builtin_inff()) && x >= least ? x : 0;
-  };
   unsigned kept = 0;
   draw_u64 sum[2] = {0, 0}, run[2];
 #pragma unroll
@@ -315,41 +311,34 @@ k_draw_small(DrawArgs a, int64_t first) {
     kept = draw_sum(kept, (unsigned*)slots);
     if (tid == 0) a.num_kept[q] = (int)kept;
   }
+  __syncthreads();                                         // `before` takes the place of the borders' LDS
 #pragma unroll
   for (int b = 0; b < 2; ++b) if (lane == 63) starts[16 * b + wave] = run[b];
   __syncthreads();
-  if (wave == 0) {
-    const draw_u64 m = lane < 32 ? starts[lane] : 0, upto = draw_wave_prefix(m);
-    if (lane < 32) starts[lane] = upto - m;
-    if (lane == 31) starts[32] = upto;
-  }
+  const draw_u64 m = lane < 32 ? starts[lane] : 0, upto = draw_wave_prefix(m), total = draw_lane(upto, 31);      // every wave for itself
+#pragma unroll
+  for (int b = 0; b < 2; ++b) lds.before[1024 * b + tid] = draw_lane(upto - m, 16 * b + wave) + run[b] - sum[b];
   __syncthreads();
-  const draw_u64 total = starts[32];
+  // a thread a draw: the eight columns by the sums before them, the row by weighing those again
   const double log_total = w.log_sum(total);
-  // every wave goes through all draws and takes those that fall into its segments
+  for (int d = tid; d < a.draws; d += 1024) {
+    const draw_u64 target = draw_target(a.uniforms[q * a.draws + d], total);
+    int at = 0;                                            // the last that begin at or below the target
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const draw_u64 begin = starts[16 * b + wave], end = starts[16 * b + wave + 1], before = begin + run[b] - sum[b];
-    if (begin == end) continue;
-    for (int d0 = 0; d0 < a.draws; d0 += 64) {
-      const int d = d0 + lane;
-      const draw_u64 t = d < a.draws ? draw_target(a.uniforms[q * a.draws + d], total) : ~(draw_u64)0;
-      draw_u64 mine = __ballot(t >= begin && t < end);
-      while (mine) {                                       // uniform
-        const int i = __ffsll((long long)mine) - 1;
-        mine &= mine - 1;
-        const draw_u64 target = draw_lane(t, i);
-        if (before <= target && target < before + sum[b]) {        // one lane
-          int at = 0;
-          float score = v[b][0];
-          draw_u64 upto = before + weight(b, 0);
+    for (int step = 1024; step >= 1; step /= 2) if (lds.before[at + step] <= target) at += step;        // at + step < 2,048
+    float score[8], found = 0.f;
+    row.scores_of(8 * at, score);
+    draw_u64 sum = lds.before[at];
+    int column = -1;
 #pragma unroll
-          for (int j = 1; j < 8; ++j) if (upto <= target) { upto += weight(b, j); at = j; score = v[b][j]; }
-          a.ids[q * a.draws + d0 + i] = 8192 * b + 8 * tid + at;
-          if (a.log_probs) a.log_probs[q * a.draws + d0 + i] = (float)(w.distance(draw_key(score)) - log_total);
-        }
-      }
+    for (int e = 0; e < 8; ++e) {
+      const draw_u64 x = w.of_score(score[e]);
+      const bool in = (CUTS ? draw_place(draw_key(score[e]), (unsigned)(8 * at + e)) >= cut : score[e] > -__builtin_inff()) && x >= least;
+      sum += in ? x : 0;
+      if (column < 0 && sum > target) { column = e; found = score[e]; }
     }
+    a.ids[q * a.draws + d] = 8 * at + column;
+    if (a.log_probs) a.log_probs[q * a.draws + d] = (float)(w.distance(draw_key(found)) - log_total);
   }
 }
 
