@@ -91,9 +91,8 @@ __device__ __forceinline__ void draw_rows(const DrawArgs& a, int64_t q, const Dr
 
 // Everything by digits over all rows of a query.
 template <int TYPE>
-__device__ __attribute__((noinline)) void draw_slowly(const DrawArgs& a, int64_t q, const DrawRow<TYPE> row, const DrawParams par, const DrawWhole whole, draw_u64* mass, DrawShared& lds) {
+__device__ __attribute__((noinline)) void draw_slowly(const DrawArgs& a, int64_t q, const DrawRow<TYPE> row, const DrawParams par, unsigned best, draw_u64* mass, DrawShared& lds) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const DrawWeights w = draw_weights(whole.best, par, whole.sum);
   auto each = [&](auto f) {
     for (int64_t c0 = 0; c0 < a.rows; c0 += 8 * 1024) {
       const int64_t c = c0 + 8 * tid;
@@ -104,6 +103,10 @@ __device__ __attribute__((noinline)) void draw_slowly(const DrawArgs& a, int64_t
     }
   };
   auto ones = [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); };
+  const float top = draw_score(best), c = draw_depth_scale(par);
+  float approx = 0.f;
+  each([&](draw_u64 place) { if (place) approx += __builtin_amdgcn_exp2f(-draw_depth(top, draw_score((unsigned)(place >> 32)), c)); });
+  const DrawWeights w = draw_weights(best, par, draw_sum(approx, (float*)lds.slots));
   draw_u64 cut = 1;
   unsigned count = 0;
   if (par.top_k > 0) { each([&](draw_u64 place) { count += place != 0; }); count = draw_sum(count, (unsigned*)lds.slots); }
@@ -356,7 +359,7 @@ k_draw_scan(DrawArgs a, int64_t first) {
   const float c = draw_depth_scale(par);
   const int begin = chunk * a.chunk_rows, end = (int)min((int64_t)a.rows, (int64_t)begin + a.chunk_rows);
   const int turns = a.chunk_rows / 2048, turns_block = (turns + a.blocks - 1) / a.blocks;
-  // scores as floats, -infinity where a row does not count
+  const bool sums = !few && draw_all(a, par) && par.top_p >= 2.f;
   float best = -__builtin_inff(), sum = 0.f, group = best;
   unsigned* maxima = a.maxima + q * a.groups + (int64_t)chunk * a.blocks * 256 + tid;
   int block = 0, left = turns_block;
@@ -364,15 +367,20 @@ k_draw_scan(DrawArgs a, int64_t first) {
     const int64_t at = (int64_t)begin + i * 2048 + 8 * tid;
     if (at < end) {
       float v[8], here = -__builtin_inff();
-      row.scores_of((int)at, v);
+      row.raw((int)at, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) here = fmaxf(here, v[e]);
+      for (int e = 0; e < 8; ++e) here = fmaxf(here, v[e]);          // NaN gives way
+      here = fminf(here, DRAW_TOP);
       group = fmaxf(group, here);
-      if (here > best) { sum = sum > 0.f ? sum * __builtin_amdgcn_exp2f(-draw_depth(here, best, c)) : 0.f; best = here; }
-      if (best > -__builtin_inff()) {
+      if (sums) {
+        if (here > best) sum = sum > 0.f ? sum * __builtin_amdgcn_exp2f(-draw_depth(here, best, c)) : 0.f;
+        const float top = fmaxf(best, here);
+        if (top > -__builtin_inff()) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum += __builtin_amdgcn_exp2f(-draw_depth(best, v[e], c));
+          for (int e = 0; e < 8; ++e) sum += __builtin_amdgcn_exp2f(-draw_depth(top, fmaxf(v[e], -DRAW_TOP), c));
+        }
       }
+      best = fmaxf(best, here);
     }
     if (--left == 0 || i + 1 == turns) {
       if (few) maxima[256 * block] = draw_key(group);
@@ -403,11 +411,12 @@ k_draw_hist(DrawArgs a, int64_t first) {
   const float c = draw_depth_scale(par);
   for (int i = tid; i < DRAW_BINS; i += 256) bins[i] = 0;
   const DrawWhole whole = draw_whole(a, q, c, slots);
+  if (draw_infinite(whole.best)) return;
   const float top = draw_score(whole.best), unit_weight = (float)(1 << a.hist_bits), c32 = c * 32.f, l = 0.69314718f / 32.f, w1 = -l * unit_weight, w2 = 0.5f * l * l * unit_weight;
   const int begin = chunk * a.chunk_rows, end = (int)min((int64_t)a.rows, (int64_t)begin + a.chunk_rows);
   for (int64_t at = (int64_t)begin + 8 * tid; at < end; at += 2048) {
     float v[8];
-    row.scores_of((int)at, v);
+    row.raw((int)at, v);
     // 2^-(x / 32), x what the depth has below its bin's top: 1 - x l + (x l)^2 / 2, l = ln 2 / 32, is off by 2^-19 at most.  Rows that do not
     // count, and those below 2^-64, end in the last bin: up to 2^-64 too much each
 #pragma unroll
@@ -432,7 +441,7 @@ k_draw_range(DrawArgs a, int64_t first) {
   const DrawParams par = draw_params(a, q);
   const int tid = threadIdx.x;
   if (draw_few(a, par) || !draw_all(a, par)) return;
-  if (par.top_p >= 2.f) { if (tid == 0) a.range[q] = {DRAW_BINS, DRAW_BINS}; return; }     // everything lies above
+  if (par.top_p >= 2.f) return;
   if (tid == 0) { low = DRAW_BINS - 1; high = DRAW_BINS - 1; }
   draw_u64 nx = 0, ny = 0;                                 // bins 2 tid and 2 tid + 1
 #pragma unroll 8
@@ -448,7 +457,7 @@ k_draw_range(DrawArgs a, int64_t first) {
   if (before < may && before + x + y >= may) low = before + x >= may ? 2 * tid : 2 * tid + 1;
   if (before < must && before + x + y >= must) high = before + x >= must ? 2 * tid : 2 * tid + 1;
   __syncthreads();
-  if (tid == 0) a.range[q] = {want <= 0.0 ? 0 : low, want <= 0.0 ? 0 : high};
+  if (tid == 0) a.range[q] = {want <= 0.0 ? 0 : low, want <= 0.0 ? 0 : high, (float)__builtin_ldexp(all, -a.hist_bits)};
 }
 
 // Integer weights of a chunk.
@@ -465,9 +474,9 @@ k_draw_weigh(DrawArgs a, int64_t first) {
   const DrawRow<TYPE> row(a, q);
   const float c = draw_depth_scale(par);
   const DrawWhole whole = draw_whole(a, q, c, slots);
-  if (whole.best == 0) return;
-  const DrawWeights w = draw_weights(whole.best, par, whole.sum);
-  const DrawRange range = a.range[q];
+  if (whole.best == 0 || draw_infinite(whole.best)) return;
+  const DrawRange range = par.top_p < 2.f ? a.range[q] : DrawRange{0, 0, 0.f};
+  const DrawWeights w = draw_weights(whole.best, par, par.top_p < 2.f ? range.sum : whole.sum);
   const draw_u64 least = w.least(par.min_p);
   // bins by their depth, 32 to a binary order of magnitude, as the histogram counts them
   const float top = draw_score(whole.best), c32 = c * 32.f, low = (float)range.low, high = range.high < DRAW_BINS - 1 ? range.high + 1.f : __builtin_inff();
@@ -481,7 +490,7 @@ k_draw_weigh(DrawArgs a, int64_t first) {
       draw_u64 sum = 0;
       if (at < end) {
         float v[8];
-        row.scores_of((int)at, v);
+        row.raw((int)at, v);
         draw_u64 near[8];                                  // lanes whose row lies in the range
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -547,7 +556,7 @@ k_draw_rows(DrawArgs a, int64_t first) {
   const DrawWhole whole = draw_whole(a, q, draw_depth_scale(par), lds.border.slots);
   if (whole.best == 0) { draw_nothing<TYPE>(a, q); return; }         // uniform, like all conditions that end in a return or a barrier
   const bool few = draw_few(a, par), cuts = par.top_p < 2.f;
-  const DrawWeights w = draw_weights(whole.best, par, whole.sum);
+  const DrawWeights w = draw_weights(whole.best, par, few ? (float)DRAW_LIST : (draw_all(a, par) && cuts ? a.range[q].sum : whole.sum));
   const bool held = a.segments <= 2048;                    // the segments' sums fit LDS
   draw_u64* mass = held ? near.mass : a.mass + q * a.mass_pitch;
   draw_u64 cut = 1, all = 0, above = 0;                    // of the listed rows; sums of weights: of all rows for top-p, of those above the list
@@ -602,7 +611,7 @@ k_draw_rows(DrawArgs a, int64_t first) {
     if (!slowly) for (int s = tid; s < a.segments; s += 1024) mass[s] = 0;
   } else {
     n = cuts ? a.listed[q] : 0;
-    slowly = !draw_all(a, par) || n > (unsigned)a.list;
+    slowly = !draw_all(a, par) || draw_infinite(whole.best) || n > (unsigned)a.list;
     if (!slowly) {
       for (unsigned i = tid; i < n; i += 1024) list[i] = a.lists[q * a.list + i];
       if (held) {
@@ -653,7 +662,7 @@ k_draw_rows(DrawArgs a, int64_t first) {
       draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.border.slots);
     }
   }
-  if (slowly) draw_slowly<TYPE>(a, q, row, par, whole, a.mass + q * a.mass_pitch, lds.border);
+  if (slowly) draw_slowly<TYPE>(a, q, row, par, whole.best, a.mass + q * a.mass_pitch, lds.border);
 }
 
 // ------------------------------------------------------------------------------------------ launches -----

@@ -42,6 +42,7 @@ __device__ __forceinline__ draw_u64 draw_share_down(float part, draw_u64 whole) 
 // A row's place in the order (score descending, id ascending) as one number: greater comes first.  0: the row does not count.
 __device__ __forceinline__ draw_u64 draw_place(unsigned key, unsigned id) { return (draw_u64)key << 32 | (key ? ~id : 0u); }
 
+#define DRAW_TOP 3.402823466e38f    // the largest float
 #define DRAW_SEGMENT 512            // columns of a segment: a wave's eight a lane
 #define DRAW_SMALL (16 * 1024)      // rows that a workgroup holds in registers
 #define DRAW_BINS 2048              // of weights: 1/32 of a binary order of magnitude each; the last one holds all below 2^-64 too
@@ -49,9 +50,9 @@ __device__ __forceinline__ draw_u64 draw_place(unsigned key, unsigned id) { retu
 #define DRAW_LIST 8192              // most rows a border is looked for among
 #define DRAW_LIST_CHUNK 2048        // of one chunk
 
-struct DrawChunk { unsigned best; float sum; };     // of a chunk: greatest key (0: no row counts), sum of weights relative to it
-// Of a query, after the histogram: bins below `low` lie above top-p's border, bins above `high` below it.
-struct DrawRange { int low, high; };
+struct DrawChunk { unsigned best; float sum; };     // of a chunk: greatest key (0: no row counts), sum of weights relative to it (where no histogram gives it)
+// Of a query, after the histogram: bins below `low` lie above top-p's border, bins above `high` below it; the sum of weights.
+struct DrawRange { int low, high; float sum; };
 
 struct DrawArgs {
   const void* scores; const uint32_t* allowed;
@@ -91,6 +92,8 @@ __device__ __forceinline__ DrawParams draw_params(const DrawArgs& a, int64_t q) 
 // Ways of a query: rows picked from groups' maxima, or all rows weighed, with a histogram where top-p's border is looked for.
 __device__ __forceinline__ bool draw_few(const DrawArgs& a, const DrawParams& p) { return p.top_k > 0 && p.top_k <= DRAW_FEW && 2 * p.top_k <= a.groups; }
 __device__ __forceinline__ bool draw_all(const DrawArgs& a, const DrawParams& p) { return p.top_k == 0 || p.top_k >= a.rows; }
+// Whose best score is infinite (or the largest float) goes by digits: the passes over all rows take their values as they are.
+__device__ __forceinline__ bool draw_infinite(unsigned best) { return best >= 0xff7fffffu; }
 
 // Keys of a query's columns, eight at a time.
 template <int TYPE> struct DrawRow {
@@ -98,18 +101,21 @@ template <int TYPE> struct DrawRow {
   const T* scores; const uint32_t* allowed; int rows;
   __device__ __forceinline__ DrawRow(const DrawArgs& a, int64_t q)
       : scores((const T*)a.scores + q * a.score_stride), allowed(a.allowed ? a.allowed + q * a.allowed_stride : nullptr), rows(a.rows) {}
-  // c < rows.  -infinity: the row does not count; +infinity is the largest float
-  __device__ __forceinline__ void scores_of(int c, float (&v)[8]) const {
+  // c < rows.  -infinity: the row does not count, as where NaN is left
+  __device__ __forceinline__ void raw(int c, float (&v)[8]) const {
     load8<TYPE>(scores, c, rows, v);
     unsigned bits = allowed ? allowed[c >> 5] >> (c & 31) : 0xffu;
     if (c + 8 > rows) bits &= 0xffu >> (c + 8 - rows);
-    const float none = -__builtin_inff();
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = fminf(fmaxf(v[e], none), 3.402823466e38f);          // NaN gives way
     if ((bits & 0xffu) != 0xffu) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) if (!(bits >> e & 1u)) v[e] = none;
+      for (int e = 0; e < 8; ++e) if (!(bits >> e & 1u)) v[e] = -__builtin_inff();
     }
+  }
+  // Without NaN, and +infinity as the largest float.
+  __device__ __forceinline__ void scores_of(int c, float (&v)[8]) const {
+    raw(c, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = fminf(fmaxf(v[e], -__builtin_inff()), DRAW_TOP);    // NaN gives way
   }
   __device__ __forceinline__ void keys(int c, unsigned (&key)[8]) const {
     float v[8];
@@ -137,7 +143,7 @@ __device__ __forceinline__ DrawWeights draw_weights(unsigned best, const DrawPar
   return {(double)draw_score(best), p.inv_temperature, p.inv_temperature * 1.4426950408889634, 2 + ilogbf(fmaxf(approx, 1.f))};
 }
 // The same in fp32 and binary orders of magnitude below the best, for sums that only choose a scale or a range of bins.
-__device__ __forceinline__ float draw_depth(float top, float s, float c) { return fminf(top - s, 3.402823466e38f) * c; }
+__device__ __forceinline__ float draw_depth(float top, float s, float c) { return fminf(top - s, DRAW_TOP) * c; }
 __device__ __forceinline__ float draw_depth_scale(const DrawParams& p) { return (float)fmin(p.inv_temperature * 1.4426950408889634, 3e38); }
 __device__ __forceinline__ int draw_bin(float depth) { return (int)fminf(depth * 32.f, DRAW_BINS - 1.f); }
 __device__ __forceinline__ draw_u64 draw_one() { return 1; }
