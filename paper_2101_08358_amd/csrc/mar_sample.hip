@@ -13,8 +13,7 @@
 //   k_draw_rows    a workgroup a query.  Top-k: the k-th largest of the groups' maxima bounds the k-th best row from below; rows that reach it
 //                  are picked from the groups whose maximum does, and everything else concerns those rows alone.  Others: the border among
 //                  the range's rows, then the draws: the segment by the sums before it, the row by a wave that weighs it again
-// What does not fit (borders among more rows than a list holds, top-k above 1,024 with a table too large for registers) goes through
-// all rows by digits in the last kernel.
+//   k_draw_slowly  what does not fit (borders among more rows than a list holds, top-k above 2,048) by digits over all rows
 #include <type_traits>
 #include "mar_sample_dev.h"
 
@@ -87,57 +86,6 @@ __device__ __forceinline__ void draw_rows(const DrawArgs& a, int64_t q, const Dr
       if (a.log_probs) a.log_probs[q * a.draws + d] = (float)(w.distance(k) - log_total);
     }
   }
-}
-
-// Everything by digits over all rows of a query.
-template <int TYPE>
-__device__ __attribute__((noinline)) void draw_slowly(const DrawArgs& a, int64_t q, const DrawRow<TYPE> row, const DrawParams par, unsigned best, draw_u64* mass, DrawShared& lds) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  auto each = [&](auto f) {
-    for (int64_t c0 = 0; c0 < a.rows; c0 += 8 * 1024) {
-      const int64_t c = c0 + 8 * tid;
-      unsigned key[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
-      if (c < a.rows) row.keys((int)c, key);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) f(draw_place(key[e], (unsigned)c + e));
-    }
-  };
-  auto ones = [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); };
-  const float top = draw_score(best), c = draw_depth_scale(par);
-  float approx = 0.f;
-  each([&](draw_u64 place) { if (place) approx += __builtin_amdgcn_exp2f(-draw_depth(top, draw_score((unsigned)(place >> 32)), c)); });
-  const DrawWeights w = draw_weights(best, par, draw_sum(approx, (float*)lds.slots));
-  draw_u64 cut = 1;
-  unsigned count = 0;
-  if (par.top_k > 0) { each([&](draw_u64 place) { count += place != 0; }); count = draw_sum(count, (unsigned*)lds.slots); }
-  if (par.top_k > 0 && (unsigned)par.top_k < count) cut = draw_border<false>(lds, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
-  if (par.top_p < 2.f) {
-    draw_u64 all = 0;
-    each([&](draw_u64 place) { if (place >= cut) all += w.of((unsigned)(place >> 32)); });
-    all = draw_sum(all, lds.slots);
-    const draw_u64 want = draw_share_up(par.top_p, all), top_k = cut;
-    // rows below top-k's cut have no say: they come after the border
-    cut = draw_border<false>(lds, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
-                      [&](unsigned k) { return w.of(k); });
-  }
-  const draw_u64 least = w.least(par.min_p);
-  unsigned kept = 0;
-  for (int s = wave; s < a.segments; s += 16) {
-    const int64_t c = (int64_t)s * DRAW_SEGMENT + 8 * lane;
-    draw_u64 sum = 0;
-    if (c < a.rows) {
-      unsigned key[8];
-      row.keys((int)c, key);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) if (key[e] && draw_place(key[e], (unsigned)c + e) >= cut) { const draw_u64 x = w.of(key[e]); if (x >= least) { sum += x; ++kept; } }
-    }
-    sum = draw_wave_sum(sum);
-    if (lane == 0) mass[s] = sum;
-  }
-  kept = draw_sum(kept, (unsigned*)lds.slots);
-  if (tid == 0 && a.num_kept) a.num_kept[q] = (int)kept;
-  __syncthreads();
-  draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.slots);
 }
 
 // Up to 256 rows, with all that top-k leaves among them: four threads a row compare it with all others.  Called by 1,024 threads.
@@ -546,7 +494,7 @@ __global__ void __launch_bounds__(1024)
 k_draw_rows(DrawArgs a, int64_t first) {
   __shared__ union { DrawShared border; DrawShort few; } lds;
   __shared__ draw_u64 list[DRAW_LIST];
-  __shared__ union { unsigned groups[4 * DRAW_FEW]; draw_u64 mass[2048]; } near;
+  __shared__ union { unsigned groups[2 * DRAW_FEW]; draw_u64 mass[2048]; } near;
   __shared__ unsigned listed, grouped;
   const int64_t q = first + blockIdx.x;
   const DrawParams par = draw_params(a, q);
@@ -554,6 +502,7 @@ k_draw_rows(DrawArgs a, int64_t first) {
   if (tid == 0) { listed = 0; grouped = 0; }
   const DrawRow<TYPE> row(a, q);
   const DrawWhole whole = draw_whole(a, q, draw_depth_scale(par), lds.border.slots);
+  if (tid == 0) a.undone[q] = 0;
   if (whole.best == 0) { draw_nothing<TYPE>(a, q); return; }         // uniform, like all conditions that end in a return or a barrier
   const bool few = draw_few(a, par), cuts = par.top_p < 2.f;
   const DrawWeights w = draw_weights(whole.best, par, few ? (float)DRAW_LIST : (draw_all(a, par) && cuts ? a.range[q].sum : whole.sum));
@@ -578,11 +527,11 @@ k_draw_rows(DrawArgs a, int64_t first) {
     groups([&](unsigned m, int g) {
       if (m < bound) return;
       const unsigned at = atomicAdd(&grouped, 1u);
-      if (at < 4 * DRAW_FEW) near.groups[at] = (unsigned)g;
+      if (at < 2 * DRAW_FEW) near.groups[at] = (unsigned)g;
     });
     __syncthreads();
     const unsigned found = grouped;
-    if (found <= 4 * DRAW_FEW) {
+    if (found <= 2 * DRAW_FEW) {
       // a group's turns are work for a thread each
       const int turns = a.chunk_rows / 2048, turns_block = (turns + a.blocks - 1) / a.blocks, per_chunk = a.blocks * 256;
       for (unsigned i = tid; i < found * turns_block; i += 1024) {
@@ -600,7 +549,7 @@ k_draw_rows(DrawArgs a, int64_t first) {
     }
     __syncthreads();
     n = listed;
-    slowly = found > 4 * DRAW_FEW || n > DRAW_LIST;        // many equal rows
+    slowly = found > 2 * DRAW_FEW || n > DRAW_LIST;        // many equal rows
     cut = (draw_u64)bound << 32;
     if (!slowly && n <= DRAW_SHORT) {
       if (tid < (int)n) lds.few.row[tid].place = list[tid];
@@ -662,7 +611,67 @@ k_draw_rows(DrawArgs a, int64_t first) {
       draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.border.slots);
     }
   }
-  if (slowly) draw_slowly<TYPE>(a, q, row, par, whole.best, a.mass + q * a.mass_pitch, lds.border);
+  if (tid == 0) a.undone[q] = slowly;
+}
+
+// Queries that the kernel before could not do: everything by digits over all rows.  A kernel of its own: with this code in the other one,
+// that took 10 to 15 us longer for all queries.
+template <int TYPE>
+__global__ void __launch_bounds__(1024)
+k_draw_slowly(DrawArgs a, int64_t first) {
+  __shared__ DrawShared lds;
+  const int64_t q = first + blockIdx.x;
+  if (!a.undone[q]) return;                                // uniform
+  const DrawRow<TYPE> row(a, q);
+  const DrawParams par = draw_params(a, q);
+  const unsigned best = draw_whole(a, q, 0.f, lds.slots).best;
+  draw_u64* mass = a.mass + q * a.mass_pitch;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto each = [&](auto f) {
+    for (int64_t c0 = 0; c0 < a.rows; c0 += 8 * 1024) {
+      const int64_t c = c0 + 8 * tid;
+      unsigned key[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+      if (c < a.rows) row.keys((int)c, key);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f(draw_place(key[e], (unsigned)c + e));
+    }
+  };
+  auto ones = [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); };
+  const float top = draw_score(best), c = draw_depth_scale(par);
+  float approx = 0.f;
+  each([&](draw_u64 place) { if (place) approx += __builtin_amdgcn_exp2f(-draw_depth(top, draw_score((unsigned)(place >> 32)), c)); });
+  const DrawWeights w = draw_weights(best, par, draw_sum(approx, (float*)lds.slots));
+  draw_u64 cut = 1;
+  unsigned count = 0;
+  if (par.top_k > 0) { each([&](draw_u64 place) { count += place != 0; }); count = draw_sum(count, (unsigned*)lds.slots); }
+  if (par.top_k > 0 && (unsigned)par.top_k < count) cut = draw_border<false>(lds, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
+  if (par.top_p < 2.f) {
+    draw_u64 all = 0;
+    each([&](draw_u64 place) { if (place >= cut) all += w.of((unsigned)(place >> 32)); });
+    all = draw_sum(all, lds.slots);
+    const draw_u64 want = draw_share_up(par.top_p, all), top_k = cut;
+    // rows below top-k's cut have no say: they come after the border
+    cut = draw_border<false>(lds, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
+                      [&](unsigned k) { return w.of(k); });
+  }
+  const draw_u64 least = w.least(par.min_p);
+  unsigned kept = 0;
+  for (int s = wave; s < a.segments; s += 16) {
+    const int64_t c = (int64_t)s * DRAW_SEGMENT + 8 * lane;
+    draw_u64 sum = 0;
+    if (c < a.rows) {
+      unsigned key[8];
+      row.keys((int)c, key);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) if (key[e] && draw_place(key[e], (unsigned)c + e) >= cut) { const draw_u64 x = w.of(key[e]); if (x >= least) { sum += x; ++kept; } }
+    }
+    sum = draw_wave_sum(sum);
+    if (lane == 0) mass[s] = sum;
+  }
+  kept = draw_sum(kept, (unsigned*)lds.slots);
+  if (tid == 0 && a.num_kept) a.num_kept[q] = (int)kept;
+  __syncthreads();
+  draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.slots);
 }
 
 // ------------------------------------------------------------------------------------------ launches -----
@@ -685,6 +694,7 @@ template <int TYPE> static void launch_draws(const DrawArgs& a, int64_t queries,
     sm_launches(queries * a.chunks, 256, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_weigh<TYPE>, dim3(n), dim3(256), 0, st, a, first); });
   }
   sm_launches(queries, 1024, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_rows<TYPE>, dim3(n), dim3(1024), 0, st, a, first); });
+  sm_launches(queries, 1024, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_slowly<TYPE>, dim3(n), dim3(1024), 0, st, a, first); });
 }
 
 // ------------------------------------------------------------------------------------------ entry points -----
@@ -706,7 +716,7 @@ static const char* draw_check(const mar_sampling* p, int* code) {
   return nullptr;
 }
 // Chunks: as many as fill the device some eight times, of 2,048 to 2^21 rows.  Blocks: groups enough for top-k's bound.
-struct DrawLayout { size_t stats, maxima, hist, range, totals, kept, listed, lists, mass, bytes; int segments, chunks, chunk_rows, blocks, groups, list, hist_bits, mass_pitch; };
+struct DrawLayout { size_t stats, maxima, hist, range, totals, kept, listed, undone, lists, mass, bytes; int segments, chunks, chunk_rows, blocks, groups, list, hist_bits, mass_pitch; };
 static DrawLayout draw_layout(const mar_sampling* p) {
   DrawLayout L = {};
   if (p->num_rows <= DRAW_SMALL || p->num_queries == 0) { L.bytes = 256; return L; }
@@ -733,6 +743,7 @@ static DrawLayout draw_layout(const mar_sampling* p) {
   L.totals = take(Q * L.chunks * 16);
   L.kept = take(Q * L.chunks * 4);
   L.listed = take(Q * 4);
+  L.undone = take(Q * 4);
   L.lists = take(Q * L.list * 8);
   L.mass_pitch = (L.segments + 15) / 16 * 16;              // lines of 128 bytes
   L.mass = take(Q * L.mass_pitch * 8);
@@ -770,7 +781,7 @@ extern "C" int mar_sample_rows(const mar_sampling* p, const void* scores, const 
   a.chunks = L.chunks; a.chunk_rows = L.chunk_rows; a.blocks = L.blocks; a.groups = L.groups; a.list = L.list;
   char* const ws = (char*)workspace;
   a.stats = (DrawChunk*)(ws + L.stats); a.maxima = (unsigned*)(ws + L.maxima); a.hist = (unsigned*)(ws + L.hist); a.hist_bits = L.hist_bits; a.range = (DrawRange*)(ws + L.range);
-  a.totals = (draw_u64*)(ws + L.totals); a.kept = (unsigned*)(ws + L.kept); a.listed = (unsigned*)(ws + L.listed); a.lists = (draw_u64*)(ws + L.lists);
+  a.totals = (draw_u64*)(ws + L.totals); a.kept = (unsigned*)(ws + L.kept); a.listed = (unsigned*)(ws + L.listed); a.undone = (unsigned*)(ws + L.undone); a.lists = (draw_u64*)(ws + L.lists);
   a.mass = (draw_u64*)(ws + L.mass); a.mass_pitch = L.mass_pitch;
   const hipStream_t st = (hipStream_t)hip_stream;
   if (p->dtype == MAR_DTYPE_FP32) launch_draws<0>(a, p->num_queries, st);

@@ -46,7 +46,7 @@ __device__ __forceinline__ draw_u64 draw_place(unsigned key, unsigned id) { retu
 #define DRAW_SEGMENT 512            // columns of a segment: a wave's eight a lane
 #define DRAW_SMALL (16 * 1024)      // rows that a workgroup holds in registers
 #define DRAW_BINS 2048              // of weights: 1/32 of a binary order of magnitude each; the last one holds all below 2^-64 too
-#define DRAW_FEW 1024               // largest top-k whose rows are picked from groups' maxima
+#define DRAW_FEW 2048               // largest top-k whose rows are picked from groups' maxima
 #define DRAW_LIST 8192              // most rows a border is looked for among
 #define DRAW_LIST_CHUNK 2048        // of one chunk
 
@@ -72,6 +72,7 @@ struct DrawArgs {
   draw_u64* totals;                 // [queries][chunks][2]: sum of all weights, of those kept above the range
   unsigned* kept;                   // [queries][chunks]: rows kept above the range
   unsigned* listed;                 // [queries]: rows in the list (more than there are places: it does not serve)
+  unsigned* undone;                 // [queries]: left to the last kernel
   draw_u64* lists;                  // [queries][list]
   draw_u64* mass;                   // [queries][mass_pitch]: sums of weights kept in segments
   int32_t mass_pitch;
@@ -145,7 +146,6 @@ __device__ __forceinline__ DrawWeights draw_weights(unsigned best, const DrawPar
 // The same in fp32 and binary orders of magnitude below the best, for sums that only choose a scale or a range of bins.
 __device__ __forceinline__ float draw_depth(float top, float s, float c) { return fminf(top - s, DRAW_TOP) * c; }
 __device__ __forceinline__ float draw_depth_scale(const DrawParams& p) { return (float)fmin(p.inv_temperature * 1.4426950408889634, 3e38); }
-__device__ __forceinline__ int draw_bin(float depth) { return (int)fminf(depth * 32.f, DRAW_BINS - 1.f); }
 __device__ __forceinline__ draw_u64 draw_one() { return 1; }
 
 // Sums and maxima by lane exchanges within a wave, zeros beyond its ends.
