@@ -127,6 +127,28 @@ __device__ __forceinline__ void mx_steps(const char* image, int lane, const mx_v
   }
 }
 
+// A row's scale bytes, block 2 k + h in byte k % 4 of word k / 4: taken as whole words, the last from the row's last four bytes; zeros beyond it.
+template <int NK>
+__device__ __forceinline__ void mx_load_scales(const uint8_t* scales, int row_blocks, int h, int (&ws)[(NK + 3) / 4]) {
+  constexpr int ND = (NK + 1) / 2;                         // words of four blocks
+  unsigned d[ND + 1];
+#pragma unroll
+  for (int j = 0; j < ND; ++j) {
+    d[j] = 0u;
+    if (row_blocks < 4) {                                  // uniform
+#pragma unroll
+      for (int e = 0; e < 3; ++e) if (e < row_blocks) d[j] |= (unsigned)scales[e] << (8 * e);
+    } else {
+      const int over = max(4 * j + 4 - row_blocks, 0);     // below 4: there are more than 4 j blocks; uniform
+      __builtin_memcpy(&d[j], scales + 4 * j - over, 4);
+      d[j] >>= 8 * over;
+    }
+  }
+  d[ND] = 0u;
+  const unsigned pick = h ? 0x07050301u : 0x06040200u;
+#pragma unroll
+  for (int k = 0; k < (NK + 3) / 4; ++k) ws[k] = (int)__builtin_amdgcn_perm(d[2 * k + 1], d[2 * k], pick);
+}
 // A wave's 32 RT rows of the table, lane m's RT neighbours from row0 on, block 2 k + h.  Rows beyond the last are taken for it and not written.
 template <int NK, int RT>
 __device__ __forceinline__ void mx_load_rows(const MxArgs& a, int row0, int h, row_u4 (&w)[RT][NK], int (&ws)[RT][(NK + 3) / 4]) {
@@ -134,18 +156,47 @@ __device__ __forceinline__ void mx_load_rows(const MxArgs& a, int row0, int h, r
   for (int t = 0; t < RT; ++t) {
     const int64_t row = min(row0 + t, a.num_rows - 1);
     const uint8_t* codes = a.codes + row * a.codes_stride;
-    const uint8_t* scales = a.scales + row * a.scales_stride;
-#pragma unroll
-    for (int k = 0; k < (NK + 3) / 4; ++k) ws[t][k] = 0;
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
       const int b = 2 * k + h;
-      unsigned s = 0;
       w[t][k] = (row_u4)(0u);
-      if (b < a.row_blocks) { w[t][k] = *reinterpret_cast<const row_u4*>(codes + 16 * b); s = scales[b]; }
-      ws[t][k / 4] |= (int)(s << (8 * (k % 4)));
+      if (b < a.row_blocks) w[t][k] = *reinterpret_cast<const row_u4*>(codes + 16 * b);
     }
+    mx_load_scales<NK>(a.scales + row * a.scales_stride, a.row_blocks, h, ws[t]);
   }
+}
+// The same of 32 RT rows from `first` on, 32 t + m, with loads of 64 bytes of a row where two steps remain: sixteen lanes take block 0 (of
+// four) of rows 0 .. 15, the next block 2, then 1 and 3; another load the same of rows 16 .. 31.  mx_settle exchanges lanes 16 .. 31 and
+// 48 .. 63 of the first with lanes 0 .. 15 and 32 .. 47 of the second, which leaves a step in each.
+template <int NK, int RT>
+__device__ __forceinline__ void mx_fetch_rows(const MxArgs& a, int first, int lane, row_u4 (&w)[RT][NK], int (&ws)[RT][(NK + 3) / 4]) {
+  const int m = lane & 31, h = lane >> 5, i = lane & 15, block = (lane >> 5) | (lane >> 4 & 1) << 1;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int64_t last = a.num_rows - 1, row = min((int64_t)first + 32 * t + m, last);
+    const uint8_t* low = a.codes + min((int64_t)first + 32 * t + i, last) * a.codes_stride;
+    const uint8_t* high = a.codes + min((int64_t)first + 32 * t + 16 + i, last) * a.codes_stride;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+      w[t][k] = (row_u4)(0u);
+      if (k + 1 < NK || k % 2) {
+        const int b = 4 * (k / 2) + block;
+        if (b < a.row_blocks) w[t][k] = *reinterpret_cast<const row_u4*>((k % 2 ? high : low) + 16 * b);
+      } else if (2 * k + h < a.row_blocks) w[t][k] = *reinterpret_cast<const row_u4*>(a.codes + row * a.codes_stride + 16 * (2 * k + h));
+    }
+    mx_load_scales<NK>(a.scales + row * a.scales_stride, a.row_blocks, h, ws[t]);
+  }
+}
+template <int NK, int RT> __device__ __forceinline__ void mx_settle(row_u4 (&w)[RT][NK]) {
+#pragma unroll
+  for (int t = 0; t < RT; ++t)
+#pragma unroll
+    for (int k = 0; k + 1 < NK; k += 2)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const auto r = __builtin_amdgcn_permlane16_swap(w[t][k][d], w[t][k + 1][d], false, false);
+        w[t][k][d] = r[0]; w[t][k + 1][d] = r[1];
+      }
 }
 
 // All slices of an image, the smallest first.
@@ -239,19 +290,22 @@ k_mxfp_few(MxArgs a) {
   constexpr int NS = mx_slices_of(TYPE);
   typedef MxImage<NK, NS> I;
   __shared__ __attribute__((aligned(16))) char image[I::BYTES];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, at = (lane & 31) * RT;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, m = lane & 31;
   row_u4 w[RT][NK], next[RT][NK];
   int ws[RT][I::NW], next_s[RT][I::NW];
   int stripe = (int)blockIdx.x * 4 + wave;
-  mx_load_rows<NK, RT>(a, min(stripe, a.stripes - 1) * 32 * RT + at, h, w, ws);
+  mx_fetch_rows<NK, RT>(a, min(stripe, a.stripes - 1) * 32 * RT, lane, w, ws);
   for (int piece = tid; piece < 256 * NK; piece += 256) mx_pack<TYPE, NK>(a, 0, piece, image);
   __syncthreads();
-  for (; stripe < a.stripes; stripe += (int)gridDim.x * 4) {
-    const int following = stripe + (int)gridDim.x * 4;
-    if (following < a.stripes) mx_load_rows<NK, RT>(a, following * 32 * RT + at, h, next, next_s);
+  while (stripe < a.stripes) {
+    const int first = stripe * 32 * RT;
+    stripe += (int)gridDim.x * 4;
+    if (stripe < a.stripes) mx_fetch_rows<NK, RT>(a, stripe * 32 * RT, lane, next, next_s);
+    mx_settle<NK, RT>(w);
     mx_f16 acc[RT];
     mx_tile<NK, NS, RT>(image, lane, w, ws, acc);
-    mx_store_any<RT>(a, 0, stripe * 32 * RT + at, h, stripe * 32 * RT + 32 * RT <= a.num_rows && a.n == 32, acc);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) mx_store_any<1>(a, 0, first + 32 * t + m, h, false, reinterpret_cast<const mx_f16 (&)[1]>(acc[t]));
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
 #pragma unroll
