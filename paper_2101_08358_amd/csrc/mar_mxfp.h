@@ -11,17 +11,19 @@ static inline const char* mx_check_strides(int dim, int64_t codes_stride, int64_
   return nullptr;
 }
 
-// The code of v times 2^-e, |v| < 8 (a block's own largest magnitude lies in [4, 8)): nearest level, ties to the even code.
-__device__ __forceinline__ unsigned mx_code(float v) {
-  const float a = fabsf(v);
-  const unsigned c = (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.f);
-  return c | (__float_as_uint(v) >> 31) << 3;
+// The codes of eight values times 2^-e, |v| < 8 (a block's own largest magnitude lies in [4, 8)): nearest level, ties to the even code.
+__device__ __forceinline__ unsigned mx_codes(const float (&v)[8]) {
+  unsigned c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], 1.f, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], 1.f, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], 1.f, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], 1.f, 3);
 }
-// The level of a code with its sign.  Codes 2 .. 7 are 1 + 1 bits of a float: exponent 1 .. 3, mantissa.
-__device__ __forceinline__ float mx_value(unsigned c) {
-  const unsigned m = c & 7u;
-  const unsigned bits = m < 2 ? m * 0x3f000000u : 0x3f000000u + (m << 22);
-  return __uint_as_float(bits | (c & 8u) << 28);
+// The levels of eight codes with their signs.
+__device__ __forceinline__ void mx_values(unsigned c, float (&v)[8]) {
+  const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.f, 1);
+  const auto d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.f, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.f, 3);
+  v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1]; v[4] = d[0]; v[5] = d[1]; v[6] = e[0]; v[7] = e[1];
 }
 // 2^(byte - 127); 255: NaN.
 __device__ __forceinline__ float mx_scale(unsigned byte) {

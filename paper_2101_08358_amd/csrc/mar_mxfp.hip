@@ -45,10 +45,9 @@ k_quantise(QuantiseArgs a) {
   const bool finite = m < 0x7f800000u;
   const int scale = max((int)(m >> 23) - 2, 0);
   const float up = __uint_as_float((unsigned)(254 - scale) << 23);
-  unsigned codes = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) codes |= mx_code(v[e] * up) << (4 * e);
-  if (!finite) codes = 0;
+  for (int e = 0; e < 8; ++e) v[e] *= up;
+  const unsigned codes = finite ? mx_codes(v) : 0u;
   *reinterpret_cast<unsigned*>(a.codes + at.row * a.codes_stride + 16 * at.b + 4 * at.part) = codes;
   if (at.part == 0) a.scales[at.row * a.scales_stride + at.b] = (uint8_t)(finite ? scale : 255);
 }
@@ -72,8 +71,9 @@ k_mxfp_rows(RowsArgs a) {
     scale = mx_scale(a.scales[id * a.scales_stride + at.b]);
   }
   float v[8];
+  mx_values(codes, v);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = mx_value(codes >> (4 * e) & 15u) * scale;
+  for (int e = 0; e < 8; ++e) v[e] *= scale;
   const int c = 32 * at.b + 8 * at.part;
   if (c < a.dim) store8<TYPE>((T*)a.out + at.row * a.out_stride, c, a.dim, v);
 }
