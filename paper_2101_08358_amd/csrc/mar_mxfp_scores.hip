@@ -317,34 +317,6 @@ k_mxfp_few(MxArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------ launches -----
-static int64_t mx_tiles(int64_t queries) { return (queries + 31) / 32; }
-
-struct MxPlan { bool few; int rt, stripes, parts, tiles_part, grid; };
-// Few queries: workgroups that stay, two a CU.  Else a workgroup a stripe of rows and part of the queries' tiles: one a CU at a time,
-// estimated by the rounds of workgroups and their tiles, a workgroup's rows and first images costing some two tiles.
-static MxPlan mx_plan(const mar_mxfp* p) {
-  MxPlan r = {};
-  const int64_t tiles = mx_tiles(p->num_queries);
-  const int nk = (p->dim + 63) / 64;
-  r.few = tiles <= 1;
-  if (r.few) {
-    r.rt = p->num_rows <= 64 * 1024 ? 1 : (nk <= 3 ? 4 : 2);
-    r.stripes = (int)((p->num_rows + 32 * r.rt - 1) / (32 * r.rt));
-    r.grid = (r.stripes + 3) / 4 < 512 ? (r.stripes + 3) / 4 : 512;
-    return r;
-  }
-  r.rt = p->num_rows * tiles >= 2048 * 1024 ? 4 : 1;
-  r.stripes = (int)((p->num_rows + 256 * r.rt - 1) / (256 * r.rt));
-  const int64_t slots = 256;
-  int64_t best = INT64_MAX;
-  for (int64_t k = 1; k <= tiles && k <= 1024 && k * r.stripes <= 1 << 22; k += 1 + k / 32) {
-    const int64_t each = (tiles + k - 1) / k, parts = (tiles + each - 1) / each, cost = (r.stripes * parts + slots - 1) / slots * (each + 2);
-    if (cost < best) { best = cost; r.parts = (int)parts; r.tiles_part = (int)each; }
-  }
-  r.grid = r.stripes * r.parts;
-  return r;
-}
-
 template <int TYPE, int NK> static void launch_type(const MxPlan& plan, const MxArgs& a, hipStream_t st) {
   constexpr int NS = mx_slices_of(TYPE);
   const dim3 grid((unsigned)plan.grid);

@@ -83,7 +83,7 @@ __device__ __forceinline__ void draw_rows(const DrawArgs& a, int64_t q, const Dr
 #pragma unroll
       for (int j = 1; j < 8; ++j) if (upto <= target) { upto += each[j]; at = j; k = key[j]; }
       a.ids[q * a.draws + d] = (int)c + at;
-      if (a.log_probs) a.log_probs[q * a.draws + d] = (float)(w.distance(k) - log_total);
+      if (a.log_probs) a.log_probs[q * a.draws + d] = w.log_prob(k, log_total);
     }
   }
 }
@@ -147,7 +147,7 @@ __device__ __forceinline__ void draw_short(const DrawArgs& a, int64_t q, DrawSho
   const unsigned count = draw_sum(in && weight && part == 0 ? 1u : 0u, (unsigned*)lds.slots);
   if (in && weight && part == 0) {
     lds.start[at] = start; lds.id[at] = id;
-    lds.log_prob[at] = (float)(w.distance((unsigned)(mine >> 32)) - w.log_sum(total));
+    lds.log_prob[at] = w.log_prob((unsigned)(mine >> 32), w.log_sum(total));
   }
   __syncthreads();
   for (int d = tid; d < a.draws; d += 1024) {
@@ -289,7 +289,7 @@ k_draw_small(DrawArgs a, int64_t first) {
       if (column < 0 && sum > target) { column = e; found = score[e]; }
     }
     a.ids[q * a.draws + d] = 8 * at + column;
-    if (a.log_probs) a.log_probs[q * a.draws + d] = (float)(w.distance(draw_key(found)) - log_total);
+    if (a.log_probs) a.log_probs[q * a.draws + d] = w.log_prob(draw_key(found), log_total);
   }
 }
 
@@ -715,42 +715,6 @@ static const char* draw_check(const mar_sampling* p, int* code) {
   if (p->score_stride < p->num_rows || p->score_stride > (int64_t)1 << 40) return "score_stride is below num_rows or above 2^40";
   return nullptr;
 }
-// Chunks: as many as fill the device some eight times, of 2,048 to 2^21 rows.  Blocks: groups enough for top-k's bound.
-struct DrawLayout { size_t stats, maxima, hist, range, totals, kept, listed, undone, lists, mass, bytes; int segments, chunks, chunk_rows, blocks, groups, list, hist_bits, mass_pitch; };
-static DrawLayout draw_layout(const mar_sampling* p) {
-  DrawLayout L = {};
-  if (p->num_rows <= DRAW_SMALL || p->num_queries == 0) { L.bytes = 256; return L; }
-  size_t at = 0;
-  auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
-  const size_t Q = (size_t)p->num_queries;
-  L.segments = (int)((p->num_rows + DRAW_SEGMENT - 1) / DRAW_SEGMENT);
-  int64_t chunks = 2048 / p->num_queries;
-  if (chunks < (p->num_rows + (1 << 21) - 1) >> 21) chunks = (p->num_rows + (1 << 21) - 1) >> 21;
-  chunks = chunks < 1 ? 1 : (chunks > 256 ? 256 : chunks);
-  int64_t turns = (p->num_rows + 2048 * chunks - 1) / (2048 * chunks);
-  L.chunk_rows = (int)(2048 * turns);
-  L.chunks = (int)((p->num_rows + L.chunk_rows - 1) / L.chunk_rows);
-  int64_t blocks = 4096 / (256 * L.chunks);
-  L.blocks = (int)(blocks < 1 ? 1 : (blocks > turns ? turns : blocks));
-  L.groups = L.chunks * L.blocks * 256;
-  L.list = (int)(p->num_rows / 16 < DRAW_LIST ? p->num_rows / 16 : DRAW_LIST);
-  L.stats = take(Q * L.chunks * sizeof(DrawChunk));
-  L.maxima = take(Q * L.groups * 4);
-  L.hist = take(Q * L.chunks * DRAW_BINS * 4);
-  L.hist_bits = 16;                                        // a bin's sum of a chunk stays below 2^32
-  while ((int64_t)L.chunk_rows << L.hist_bits >= 1ll << 32) --L.hist_bits;
-  L.range = take(Q * sizeof(DrawRange));
-  L.totals = take(Q * L.chunks * 16);
-  L.kept = take(Q * L.chunks * 4);
-  L.listed = take(Q * 4);
-  L.undone = take(Q * 4);
-  L.lists = take(Q * L.list * 8);
-  L.mass_pitch = (L.segments + 15) / 16 * 16;              // lines of 128 bytes
-  L.mass = take(Q * L.mass_pitch * 8);
-  L.bytes = at;
-  return L;
-}
-
 extern "C" int mar_sample_rows_workspace_bytes(const mar_sampling* p, size_t* out_bytes) {
   int code;
   if (const char* why = draw_check(p, &code)) { mar_set_error("%s", why); return code; }

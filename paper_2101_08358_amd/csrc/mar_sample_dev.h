@@ -129,10 +129,13 @@ template <int TYPE> struct DrawRow {
 // Weights of a query's rows: the best score, the inverse temperature and the same in binary orders of magnitude, the integers' scale 2^(62 - shift).
 struct DrawWeights {
   double top, inv_temperature, slope; int shift;
-  __device__ __forceinline__ double distance(unsigned key) const { return ((double)draw_score(key) - top) * inv_temperature; }
   __device__ __forceinline__ draw_u64 of_score(float score) const { return draw_weight((top - (double)score) * slope, shift); }
   __device__ __forceinline__ draw_u64 of(unsigned key) const { return of_score(draw_score(key)); }
   __device__ __forceinline__ double log_sum(draw_u64 sum) const { return log(__builtin_ldexp((double)sum, shift - 62)); }
+  // The best row's weight is a power of two less its rounding: a row that is certain keeps log 1.
+  __device__ __forceinline__ float log_prob(unsigned key, double log_sum) const {
+    return (float)fmin(((double)draw_score(key) - top) * inv_temperature - log_sum, 0.0);
+  }
   // min-p's weight
   __device__ __forceinline__ draw_u64 least(float min_p) const {
     const draw_u64 best = draw_weight(0.0, shift);
@@ -293,4 +296,40 @@ __device__ __forceinline__ draw_u64 draw_border(DrawShared& lds, draw_u64 want, 
     prefix = prefix << width | draw_digit(lds, want, over, ties);
   }
   return (draw_u64)base << 32 | prefix;
+}
+
+// Chunks: as many as fill the device some eight times, of 2,048 to 2^21 rows.  Blocks: groups enough for top-k's bound.
+struct DrawLayout { size_t stats, maxima, hist, range, totals, kept, listed, undone, lists, mass, bytes; int segments, chunks, chunk_rows, blocks, groups, list, hist_bits, mass_pitch; };
+static inline DrawLayout draw_layout(const mar_sampling* p) {
+  DrawLayout L = {};
+  if (p->num_rows <= DRAW_SMALL || p->num_queries == 0) { L.bytes = 256; return L; }
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
+  const size_t Q = (size_t)p->num_queries;
+  L.segments = (int)((p->num_rows + DRAW_SEGMENT - 1) / DRAW_SEGMENT);
+  int64_t chunks = 2048 / p->num_queries;
+  if (chunks < (p->num_rows + (1 << 21) - 1) >> 21) chunks = (p->num_rows + (1 << 21) - 1) >> 21;
+  chunks = chunks < 1 ? 1 : (chunks > 256 ? 256 : chunks);
+  int64_t turns = (p->num_rows + 2048 * chunks - 1) / (2048 * chunks);
+  L.chunk_rows = (int)(2048 * turns);
+  L.chunks = (int)((p->num_rows + L.chunk_rows - 1) / L.chunk_rows);
+  int64_t blocks = 4096 / (256 * L.chunks);
+  L.blocks = (int)(blocks < 1 ? 1 : (blocks > turns ? turns : blocks));
+  L.groups = L.chunks * L.blocks * 256;
+  L.list = (int)(p->num_rows / 16 < DRAW_LIST ? p->num_rows / 16 : DRAW_LIST);
+  L.stats = take(Q * L.chunks * sizeof(DrawChunk));
+  L.maxima = take(Q * L.groups * 4);
+  L.hist = take(Q * L.chunks * DRAW_BINS * 4);
+  L.hist_bits = 16;                                        // a bin's sum of a chunk stays below 2^32
+  while ((int64_t)L.chunk_rows << L.hist_bits >= 1ll << 32) --L.hist_bits;
+  L.range = take(Q * sizeof(DrawRange));
+  L.totals = take(Q * L.chunks * 16);
+  L.kept = take(Q * L.chunks * 4);
+  L.listed = take(Q * 4);
+  L.undone = take(Q * 4);
+  L.lists = take(Q * L.list * 8);
+  L.mass_pitch = (L.segments + 15) / 16 * 16;              // lines of 128 bytes
+  L.mass = take(Q * L.mass_pitch * 8);
+  L.bytes = at;
+  return L;
 }
