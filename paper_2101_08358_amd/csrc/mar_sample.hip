@@ -166,6 +166,7 @@ template <int TYPE, bool CUTS>
 __global__ void __launch_bounds__(1024, CUTS ? 4 : 8)
 k_draw_small(DrawArgs a, int64_t first) {
   __shared__ union { DrawShared border; DrawShort list; draw_u64 before[2048]; } lds;
+  __shared__ __attribute__((aligned(16))) float held[CUTS ? DRAW_SMALL : 4];
   __shared__ draw_u64 slots[16];
   __shared__ draw_u64 starts[32];
   __shared__ unsigned listed;
@@ -189,7 +190,7 @@ k_draw_small(DrawArgs a, int64_t first) {
   draw_u64 cut = 1;
   if constexpr (CUTS) if (par.top_k > 0 && par.top_k <= 128 && par.top_k < a.rows) {       // uniform
     // the k-th largest of the threads' maxima bounds the k-th best row from below: few rows reach it
-    const unsigned bound = max(1u, (unsigned)(draw_border<true>(lds.border, (draw_u64)par.top_k, 0, [&](auto f) { f((draw_u64)max(draw_key(mine), 1u) << 32, draw_one); },
+    const unsigned bound = max(1u, (unsigned)(draw_border<true>(lds.border, a.rows, (draw_u64)par.top_k, 0, [&](auto f) { f((draw_u64)max(draw_key(mine), 1u) << 32, draw_one); },
                                                                 [](unsigned) { return draw_one(); }) >> 32));
     __syncthreads();
 #pragma unroll
@@ -210,38 +211,36 @@ k_draw_small(DrawArgs a, int64_t first) {
     for (int e = 0; e < 8; ++e) approx += __builtin_amdgcn_exp2f(-draw_depth(top, v[b][e], c));
   approx = draw_sum(approx, (float*)slots);
   const DrawWeights w = draw_weights(best, par, approx);
-  if constexpr (CUTS) {
-    if (par.top_k > 0 && par.top_k < a.rows) {             // uniform
+  if constexpr (CUTS) if ((par.top_k > 0 && par.top_k < a.rows) || par.top_p < 2.f) {       // uniform
+    // through LDS: loops over the rows take a sixteenth of the code, and no registers beside the weights'
+    struct Eight { float v[8]; };
+#pragma unroll
+    for (int b = 0; b < 2; ++b) *reinterpret_cast<Eight*>(held + 8192 * b + 8 * tid) = __builtin_bit_cast(Eight, v[b]);
+    __syncthreads();
+    auto each = [&](auto f) {
+#pragma unroll 2
+      for (int i = tid; i < DRAW_SMALL; i += 1024) f(draw_place(draw_key(held[i]), (unsigned)i));
+    };
+    if (par.top_k > 0 && par.top_k < a.rows) {
       unsigned count = 0;
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) count += v[b][e] > -__builtin_inff();
+      each([&](draw_u64 place) { count += place != 0; });
       count = draw_sum(count, (unsigned*)slots);
-      if ((unsigned)par.top_k < count) {
-        auto ones = [&](auto f) {
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f(place(b, e), draw_one);
-        };
-        cut = draw_border<false>(lds.border, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
-      }
+      if ((unsigned)par.top_k < count) cut = draw_border<false>(lds.border, a.rows, (draw_u64)par.top_k, 0, [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); },
+                                                               [](unsigned) { return draw_one(); });
     }
     if (par.top_p < 2.f) {
       draw_u64 all = 0;
+      const draw_u64 top_k = cut;
+      each([&](draw_u64 place) { all += place >= top_k ? w.of((unsigned)(place >> 32)) : 0; });
+      const draw_u64 want = draw_share_up(par.top_p, draw_sum(all, slots));
+      cut = draw_border<false>(lds.border, a.rows, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
+                               [&](unsigned k) { return w.of(k); });
+    }
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < 2; ++b) {
+      const Eight back = *reinterpret_cast<const Eight*>(held + 8192 * b + 8 * tid);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) all += place(b, e) >= cut ? w.of_score(v[b][e]) : 0;
-      const draw_u64 want = draw_share_up(par.top_p, draw_sum(all, slots)), top_k = cut;
-      auto each = [&](auto f) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) { const draw_u64 here = place(b, e); f(here >= top_k ? here : 0, [&] { return w.of_score(v[b][e]); }); }
-      };
-      cut = draw_border<false>(lds.border, want ? want : 1, 0, each, [&](unsigned k) { return w.of(k); });
+      for (int e = 0; e < 8; ++e) v[b][e] = back.v[e];
     }
   }
   const draw_u64 least = w.least(par.min_p);
@@ -522,7 +521,7 @@ k_draw_rows(DrawArgs a, int64_t first) {
       for (int g = tid + 8192; g - tid < a.groups; g += 1024) f(g < a.groups ? maxima[g] : 0, g);
     };
     // the k-th largest maximum, or somewhat less: k rows at least reach it
-    const unsigned bound = max(1u, (unsigned)(draw_border<true>(lds.border, (draw_u64)par.top_k, 0, [&](auto f) { groups([&](unsigned m, int g) { f(g < a.groups ? (draw_u64)max(m, 1u) << 32 : 0, draw_one); }); },
+    const unsigned bound = max(1u, (unsigned)(draw_border<true>(lds.border, a.rows, (draw_u64)par.top_k, 0, [&](auto f) { groups([&](unsigned m, int g) { f(g < a.groups ? (draw_u64)max(m, 1u) << 32 : 0, draw_one); }); },
                                                                 [](unsigned) { return draw_one(); }) >> 32));
     groups([&](unsigned m, int g) {
       if (m < bound) return;
@@ -534,16 +533,34 @@ k_draw_rows(DrawArgs a, int64_t first) {
     if (found <= 2 * DRAW_FEW) {
       // a group's turns are work for a thread each
       const int turns = a.chunk_rows / 2048, turns_block = (turns + a.blocks - 1) / a.blocks, per_chunk = a.blocks * 256;
-      for (unsigned i = tid; i < found * turns_block; i += 1024) {
-        const int g = (int)near.groups[i / turns_block], chunk = g / per_chunk, block = (g - chunk * per_chunk) / 256, turn = block * turns_block + (int)(i % turns_block);
-        const int64_t c = (int64_t)chunk * a.chunk_rows + turn * 2048 + 8 * (g & 255);
-        if (turn >= turns || c >= min((int64_t)a.rows, (int64_t)(chunk + 1) * a.chunk_rows)) continue;
-        unsigned key[8];
-        row.keys((int)c, key);
+      const unsigned items = found * turns_block;
+      for (unsigned i0 = 0; i0 < items; i0 += 4 * 1024) {  // four a thread on their way
+        unsigned key[4][8];
+        int column[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) if (key[e] >= bound) {
-          const unsigned at = atomicAdd(&listed, 1u);
-          if (at < DRAW_LIST) list[at] = draw_place(key[e], (unsigned)c + e);
+        for (int j = 0; j < 4; ++j) {
+          const unsigned i = i0 + 1024 * j + tid;
+          column[j] = -1;
+          if (i < items) {
+            const int g = (int)near.groups[i / turns_block], chunk = g / per_chunk, block = (g - chunk * per_chunk) / 256, turn = block * turns_block + (int)(i % turns_block);
+            const int64_t c = (int64_t)chunk * a.chunk_rows + turn * 2048 + 8 * (g & 255);
+            if (turn < turns && c < min((int64_t)a.rows, (int64_t)(chunk + 1) * a.chunk_rows)) { column[j] = (int)c; row.keys((int)c, key[j]); }
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (i0 + 1024 * j >= items) break;               // uniform
+          unsigned here = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) here += column[j] >= 0 && key[j][e] >= bound;
+          const unsigned upto = draw_wave_prefix(here);
+          unsigned at = 0;
+          if ((tid & 63) == 63 && upto) at = atomicAdd(&listed, upto);
+          at = draw_lane(at, 63) + upto - here;
+          if (here) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) if (key[j][e] >= bound) { if (at < DRAW_LIST) list[at] = draw_place(key[j][e], (unsigned)column[j] + e); ++at; }
+          }
         }
       }
     }
@@ -591,7 +608,7 @@ k_draw_rows(DrawArgs a, int64_t first) {
         // temperatures whose inverse 32 bits do not hold: the histogram was of something else
         slowly = above >= want || above + sum < want;
       }
-      if (!slowly) cut = draw_border<false>(lds.border, want, kind == 1 ? above : 0, [&](auto f) {
+      if (!slowly) cut = draw_border<false>(lds.border, a.rows, want, kind == 1 ? above : 0, [&](auto f) {
         each([&](draw_u64 place) { f(place >= last ? place : 0, [&] { return kind == 1 ? w.of((unsigned)(place >> 32)) : draw_one(); }); });
       }, [&](unsigned k) { return kind == 1 ? w.of(k) : draw_one(); });
     }
@@ -644,14 +661,14 @@ k_draw_slowly(DrawArgs a, int64_t first) {
   draw_u64 cut = 1;
   unsigned count = 0;
   if (par.top_k > 0) { each([&](draw_u64 place) { count += place != 0; }); count = draw_sum(count, (unsigned*)lds.slots); }
-  if (par.top_k > 0 && (unsigned)par.top_k < count) cut = draw_border<false>(lds, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
+  if (par.top_k > 0 && (unsigned)par.top_k < count) cut = draw_border<false>(lds, a.rows, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
   if (par.top_p < 2.f) {
     draw_u64 all = 0;
     each([&](draw_u64 place) { if (place >= cut) all += w.of((unsigned)(place >> 32)); });
     all = draw_sum(all, lds.slots);
     const draw_u64 want = draw_share_up(par.top_p, all), top_k = cut;
     // rows below top-k's cut have no say: they come after the border
-    cut = draw_border<false>(lds, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
+    cut = draw_border<false>(lds, a.rows, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
                       [&](unsigned k) { return w.of(k); });
   }
   const draw_u64 least = w.least(par.min_p);

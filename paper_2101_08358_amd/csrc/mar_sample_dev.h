@@ -210,10 +210,11 @@ template <typename T> __device__ __forceinline__ T draw_prefix(T v, T* slots, T&
   return before + run - v;
 }
 
+#define DRAW_DIGIT 12               // bits of a border's digit: 24 bits of range take two
 // LDS of a workgroup of 1,024 threads that looks for a border.
 struct DrawShared {
-  draw_u64 bins[2048], slots[16], found_sum, found_all;
-  unsigned found, ends[2][16];
+  draw_u64 bins[1 << DRAW_DIGIT], slots[16], found_sum, found_all;
+  unsigned found, ends[4][16];
 };
 // Adds a wave's weights to their bins.  Lanes that share a bin add up first, as long as many do: additions to one address go one by one.
 __device__ __forceinline__ void draw_add(DrawShared& lds, bool has, unsigned bin, draw_u64 w) {
@@ -230,72 +231,79 @@ __device__ __forceinline__ void draw_add(DrawShared& lds, bool has, unsigned bin
   }
   if (has) atomicAdd(&lds.bins[bin], w);
 }
-// One digit: bins[..] have been summed up; the bin, from the top, in which the sum reaches `want`.  over: the sum above it, all: its own.
+// One digit: the bin, from the top, in which the sum reaches `want`.  over: the sum above it, all: its own.
 __device__ __forceinline__ unsigned draw_digit(DrawShared& lds, draw_u64 want, draw_u64& over, draw_u64& all) {
-  const int hi = 2047 - 2 * (int)threadIdx.x;              // a pair of bins a thread, from the top
-  const draw_u64 x = lds.bins[hi], y = lds.bins[hi - 1];
-  draw_u64 whole;
-  const draw_u64 before = over + draw_prefix(x + y, lds.slots, whole);
-  if (before < want && before + x + y >= want) {
-    const bool one = before + x >= want;
-    lds.found = (unsigned)(one ? hi : hi - 1);
-    lds.found_sum = before + (one ? 0 : x);
-    lds.found_all = one ? x : y;
+  constexpr int N = (1 << DRAW_DIGIT) / 1024;              // neighbouring bins a thread, from the top
+  const int low = (1023 - (int)threadIdx.x) * N;
+  draw_u64 bin[N], sum = 0, whole;
+#pragma unroll
+  for (int i = 0; i < N; ++i) { bin[i] = lds.bins[low + i]; sum += bin[i]; }
+  draw_u64 before = over + draw_prefix(sum, lds.slots, whole);
+  if (before < want && before + sum >= want) {
+#pragma unroll
+    for (int i = N - 1; i >= 0; --i) {
+      if (before < want && before + bin[i] >= want) { lds.found = (unsigned)(low + i); lds.found_sum = before; lds.found_all = bin[i]; }
+      before += bin[i];
+    }
   }
   __syncthreads();
   over = lds.found_sum; all = lds.found_all;
   return lds.found;                                        // written again behind the next digit's barriers
 }
 // The place of the first row, in the order of places, at which the sum of the rows' weights up to it reaches `want`; `over`: what lies
-// above all rows that `each` goes through.  By digits of up to 11 bits of the keys' distance from the least one, so that the first digit
+// above all rows that `each` goes through.  By digits of up to 12 bits of the keys' distance from the least one, so that the first digit
 // spreads whatever the range (scores share their first bits: by those, most rows would meet at few addresses, one after the other),
-// then, where several rows share the border's key, of the ids.  All 1,024 threads call it; each(f) calls f(place, weight) for every row
-// of the thread, weight() its weight, as often in all lanes of a wave (place 0: no row); of(key): a key's weight.  COARSE: one digit, and the least key of its bin alone.
+// without the last bits that all keys share (16 of bf16's); then, where several rows share the border's key, of the ids.  All 1,024 threads
+// call it; each(f) calls f(place, weight) for every row of the thread, weight() its weight, as often in all lanes of a wave (place 0: no
+// row); of(key): a key's weight.  COARSE: one digit, and the least key of its bin alone.
 template <bool COARSE, typename E, typename W>
-__device__ __forceinline__ draw_u64 draw_border(DrawShared& lds, draw_u64 want, draw_u64 over, E each, W of) {
+__device__ __forceinline__ draw_u64 draw_border(DrawShared& lds, int rows, draw_u64 want, draw_u64 over, E each, W of) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  unsigned hi = 0, lo = 0;                                 // lo: of the keys' complements
-  each([&](draw_u64 place, auto) { if (place) { hi = max(hi, (unsigned)(place >> 32)); lo = max(lo, ~(unsigned)(place >> 32)); } });
-  hi = draw_wave_prefix(hi, DrawMax());
-  lo = draw_wave_prefix(lo, DrawMax());
+  unsigned end[4] = {0, 0, 0, 0};                          // greatest key, greatest complement; all bits set somewhere, all clear somewhere
+  each([&](draw_u64 place, auto) {
+    const unsigned k = (unsigned)(place >> 32);
+    if (place) { end[0] = max(end[0], k); end[1] = max(end[1], ~k); end[2] |= k; end[3] |= ~k; }
+  });
+  struct Or { __device__ __forceinline__ unsigned operator()(unsigned x, unsigned y) const { return x | y; } };
+  end[0] = draw_wave_prefix(end[0], DrawMax()); end[1] = draw_wave_prefix(end[1], DrawMax());
+  end[2] = draw_wave_prefix(end[2], Or()); end[3] = draw_wave_prefix(end[3], Or());
   __syncthreads();
-  if (lane == 63) { lds.ends[0][wave] = hi; lds.ends[1][wave] = lo; }
+  if (lane == 63) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) lds.ends[i][wave] = end[i];
+  }
   __syncthreads();
-  hi = draw_lane(draw_row_prefix(lds.ends[0][lane & 15], DrawMax()), 15);
+  const unsigned hi = draw_lane(draw_row_prefix(lds.ends[0][lane & 15], DrawMax()), 15);
   unsigned base = ~draw_lane(draw_row_prefix(lds.ends[1][lane & 15], DrawMax()), 15);
-  int left = hi > base ? 32 - __builtin_clz(hi - base) : 1;
+  const unsigned differ = draw_lane(draw_row_prefix(lds.ends[2][lane & 15], Or()) & draw_row_prefix(lds.ends[3][lane & 15], Or()), 15);
+  const int same = differ ? __builtin_ctz(differ) : 0;     // last bits that all share
+  int left = hi > base ? 32 - __builtin_clz(hi - base) : same + 1;
   draw_u64 ties = 0;
-  while (left > 0) {
-    const int width = min(left, 11), shift = left - width;
-    for (int i = threadIdx.x; i < 2048; i += 1024) lds.bins[i] = 0;
+  unsigned key = 0, upper = 0;
+  // keys, then (upper != 0) the ids of the rows that have the key found: greater lower halves of places first
+  while (true) {
+    const int end_at = upper ? 0 : same, width = min(left - end_at, DRAW_DIGIT), shift = left - width;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 1 << DRAW_DIGIT; i += 1024) lds.bins[i] = 0;
     __syncthreads();
     each([&](draw_u64 place, auto weight) {
-      const unsigned k = (unsigned)(place >> 32);
-      const bool has = place != 0 && k >= base && (draw_u64)(k - base) >> left == 0;
+      const unsigned k = upper ? (unsigned)place : (unsigned)(place >> 32);
+      const bool has = place != 0 && (upper == 0 || (unsigned)(place >> 32) == upper) && k >= base && (draw_u64)(k - base) >> left == 0;
       draw_add(lds, has, (k - base) >> shift, has ? weight() : 0);
     });
     __syncthreads();
     base += draw_digit(lds, want, over, ties) << shift;
     left = shift;
     if (COARSE) return (draw_u64)base << 32;
+    if (left > end_at) continue;
+    if (upper) return (draw_u64)upper << 32 | base;
+    key = base;
+    // all rows at the key are needed: no id decides
+    if (want - over > ties - of(key)) return (draw_u64)key << 32;
+    upper = key;
+    base = ~(unsigned)(rows - 1);
+    left = rows > 1 ? 32 - __builtin_clz((unsigned)(rows - 1)) : 1;
   }
-  // all rows at the key are needed: no id decides
-  if (want - over > ties - of(base)) return (draw_u64)base << 32;
-  unsigned prefix = 0;
-  for (int level = 0; level < 3; ++level) {
-    const int width = level == 2 ? 10 : 11, shift = level == 0 ? 21 : (level == 1 ? 10 : 0);
-    __syncthreads();
-    for (int i = threadIdx.x; i < 2048; i += 1024) lds.bins[i] = 0;
-    __syncthreads();
-    each([&](draw_u64 place, auto weight) {
-      const unsigned id = (unsigned)place;
-      const bool has = place != 0 && (unsigned)(place >> 32) == base && (level == 0 || id >> (shift + width) == prefix);
-      draw_add(lds, has, id >> shift & ((1u << width) - 1), has ? weight() : 0);
-    });
-    __syncthreads();
-    prefix = prefix << width | draw_digit(lds, want, over, ties);
-  }
-  return (draw_u64)base << 32 | prefix;
 }
 
 // Chunks: as many as fill the device some eight times, of 2,048 to 2^21 rows.  Blocks: groups enough for top-k's bound.
