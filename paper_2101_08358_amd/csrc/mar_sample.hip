@@ -5,7 +5,7 @@
 // in any order, and a border (top-p's, a draw's) falls where the integers say, whatever way found it.
 //
 // Up to 16,384 rows (k_draw_small): a workgroup a query holds them in registers.  More:
-//   k_draw_scan    a workgroup a chunk: greatest key, rows that count, sum of weights in fp32; maxima of groups of rows
+//   k_draw_scan    a workgroup a chunk: greatest score; sum of weights in fp32 where no histogram follows; maxima of groups of rows
 //   k_draw_hist    queries without top-k, with top-p: weights by their binary order of magnitude, 1/32 apart; k_draw_range: the bins that the
 //                  border lies in, whatever the rounding
 //   k_draw_weigh   queries without top-k: every row's integer weight: the sum of all, the sums of segments of 512 rows above the range, the
@@ -48,7 +48,8 @@ __device__ __forceinline__ void draw_rows(const DrawArgs& a, int64_t q, const Dr
   for (int s0 = 0; s0 < a.segments; s0 += threads) {
     const int s = s0 + threadIdx.x;
     draw_u64 all;
-    const draw_u64 m = s < a.segments ? mass[s] : 0, before = total + draw_prefix(m, slots, all);
+    // past the CU's cache: sums in memory have been added to
+    const draw_u64 m = s < a.segments ? __hip_atomic_load(&mass[s], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0, before = total + draw_prefix(m, slots, all);
     total += all;
     if (s < a.segments) mass[s] = before;
   }
@@ -324,7 +325,7 @@ k_draw_scan(DrawArgs a, int64_t first) {
         const float top = fmaxf(best, here);
         if (top > -__builtin_inff()) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sum += __builtin_amdgcn_exp2f(-draw_depth(top, fmaxf(v[e], -DRAW_TOP), c));
+          for (int e = 0; e < 8; ++e) sum += __builtin_amdgcn_exp2f(-draw_depth(top, fminf(fmaxf(v[e], -DRAW_TOP), top), c));
         }
       }
       best = fmaxf(best, here);
@@ -368,9 +369,9 @@ k_draw_hist(DrawArgs a, int64_t first) {
     // count, and those below 2^-64, end in the last bin: up to 2^-64 too much each
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float depth = (top - v[e]) * c32, x = __builtin_amdgcn_fractf(depth);
+      const float depth = __builtin_amdgcn_fmed3f((top - fmaxf(v[e], -__builtin_inff())) * c32, 0.f, DRAW_BINS - 0.01f), x = __builtin_amdgcn_fractf(depth);
       const unsigned w = (unsigned)__builtin_fmaf(x, __builtin_fmaf(x, w2, w1), unit_weight);
-      atomicAdd(&bins[min((int)depth, DRAW_BINS - 1)], w);
+      atomicAdd(&bins[(int)depth], w);
     }
   }
   __syncthreads();
@@ -623,7 +624,6 @@ k_draw_rows(DrawArgs a, int64_t first) {
       });
       kept = draw_sum(kept, (unsigned*)lds.border.slots);
       if (tid == 0 && a.num_kept) a.num_kept[q] = (int)kept;
-      // additions in memory pass the CU's cache by, which holds none of their lines: a query's sums have lines of their own
       __syncthreads();
       draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.border.slots);
     }

@@ -93,3 +93,9 @@ def test_results_do_not_depend_on_the_call():
         assert all(torch.equal(x, y) for x, y in zip(sample(wide, u, **f), want))
         one = sample(s[7:8], u[7:8].contiguous(), **f)
         assert torch.equal(one[0], want[0][7:8]) and torch.equal(one[2], want[2][7:8])
+
+
+@pytest.mark.parametrize("f", (dict(top_k=50), dict(top_k=600, top_p=0.9), dict(top_k=1900), dict(top_p=0.8, min_p=0.001), dict(min_p=0.01), dict(top_k=3000)), ids=str)
+def test_more_segments_than_fit_beside_the_borders(f):
+    for dt in (torch.float32, torch.bfloat16):
+        check(scores_of(21, 2, 2_000_003, dt), uniforms_of(21, 2, 40), **f)
