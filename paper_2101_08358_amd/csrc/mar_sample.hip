@@ -191,8 +191,7 @@ k_draw_small(DrawArgs a, int64_t first) {
   draw_u64 cut = 1;
   if constexpr (CUTS) if (par.top_k > 0 && par.top_k <= 128 && par.top_k < a.rows) {       // uniform
     // the k-th largest of the threads' maxima bounds the k-th best row from below: few rows reach it
-    const unsigned bound = max(1u, (unsigned)(draw_border<true>(lds.border, a.rows, (draw_u64)par.top_k, 0, [&](auto f) { f((draw_u64)max(draw_key(mine), 1u) << 32, draw_one); },
-                                                                [](unsigned) { return draw_one(); }) >> 32));
+    const unsigned bound = draw_bound(lds.border, (unsigned)par.top_k, [&](auto f) { f(max(draw_key(mine), 1u)); });
     __syncthreads();
 #pragma unroll
     for (int b = 0; b < 2; ++b)
@@ -226,7 +225,7 @@ k_draw_small(DrawArgs a, int64_t first) {
       unsigned count = 0;
       each([&](draw_u64 place) { count += place != 0; });
       count = draw_sum(count, (unsigned*)slots);
-      if ((unsigned)par.top_k < count) cut = draw_border<false>(lds.border, a.rows, (draw_u64)par.top_k, 0, [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); },
+      if ((unsigned)par.top_k < count) cut = draw_border(lds.border, a.rows, (draw_u64)par.top_k, 0, [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); },
                                                                [](unsigned) { return draw_one(); });
     }
     if (par.top_p < 2.f) {
@@ -234,7 +233,7 @@ k_draw_small(DrawArgs a, int64_t first) {
       const draw_u64 top_k = cut;
       each([&](draw_u64 place) { all += place >= top_k ? w.of((unsigned)(place >> 32)) : 0; });
       const draw_u64 want = draw_share_up(par.top_p, draw_sum(all, slots));
-      cut = draw_border<false>(lds.border, a.rows, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
+      cut = draw_border(lds.border, a.rows, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
                                [&](unsigned k) { return w.of(k); });
     }
 #pragma unroll
@@ -522,8 +521,7 @@ k_draw_rows(DrawArgs a, int64_t first) {
       for (int g = tid + 8192; g - tid < a.groups; g += 1024) f(g < a.groups ? maxima[g] : 0, g);
     };
     // the k-th largest maximum, or somewhat less: k rows at least reach it
-    const unsigned bound = max(1u, (unsigned)(draw_border<true>(lds.border, a.rows, (draw_u64)par.top_k, 0, [&](auto f) { groups([&](unsigned m, int g) { f(g < a.groups ? (draw_u64)max(m, 1u) << 32 : 0, draw_one); }); },
-                                                                [](unsigned) { return draw_one(); }) >> 32));
+    const unsigned bound = draw_bound(lds.border, (unsigned)par.top_k, [&](auto f) { groups([&](unsigned m, int g) { f(g < a.groups ? max(m, 1u) : 0u); }); });
     groups([&](unsigned m, int g) {
       if (m < bound) return;
       const unsigned at = atomicAdd(&grouped, 1u);
@@ -609,7 +607,7 @@ k_draw_rows(DrawArgs a, int64_t first) {
         // temperatures whose inverse 32 bits do not hold: the histogram was of something else
         slowly = above >= want || above + sum < want;
       }
-      if (!slowly) cut = draw_border<false>(lds.border, a.rows, want, kind == 1 ? above : 0, [&](auto f) {
+      if (!slowly) cut = draw_border(lds.border, a.rows, want, kind == 1 ? above : 0, [&](auto f) {
         each([&](draw_u64 place) { f(place >= last ? place : 0, [&] { return kind == 1 ? w.of((unsigned)(place >> 32)) : draw_one(); }); });
       }, [&](unsigned k) { return kind == 1 ? w.of(k) : draw_one(); });
     }
@@ -661,14 +659,14 @@ k_draw_slowly(DrawArgs a, int64_t first) {
   draw_u64 cut = 1;
   unsigned count = 0;
   if (par.top_k > 0) { each([&](draw_u64 place) { count += place != 0; }); count = draw_sum(count, (unsigned*)lds.slots); }
-  if (par.top_k > 0 && (unsigned)par.top_k < count) cut = draw_border<false>(lds, a.rows, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
+  if (par.top_k > 0 && (unsigned)par.top_k < count) cut = draw_border(lds, a.rows, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
   if (par.top_p < 2.f) {
     draw_u64 all = 0;
     each([&](draw_u64 place) { if (place >= cut) all += w.of((unsigned)(place >> 32)); });
     all = draw_sum(all, lds.slots);
     const draw_u64 want = draw_share_up(par.top_p, all), top_k = cut;
     // rows below top-k's cut have no say: they come after the border
-    cut = draw_border<false>(lds, a.rows, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
+    cut = draw_border(lds, a.rows, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
                       [&](unsigned k) { return w.of(k); });
   }
   const draw_u64 least = w.least(par.min_p);

@@ -255,8 +255,8 @@ __device__ __forceinline__ unsigned draw_digit(DrawShared& lds, draw_u64 want, d
 // spreads whatever the range (scores share their first bits: by those, most rows would meet at few addresses, one after the other),
 // without the last bits that all keys share (16 of bf16's); then, where several rows share the border's key, of the ids.  All 1,024 threads
 // call it; each(f) calls f(place, weight) for every row of the thread, weight() its weight, as often in all lanes of a wave (place 0: no
-// row); of(key): a key's weight.  COARSE: one digit, and the least key of its bin alone.
-template <bool COARSE, typename E, typename W>
+// row); of(key): a key's weight.
+template <typename E, typename W>
 __device__ __forceinline__ draw_u64 draw_border(DrawShared& lds, int rows, draw_u64 want, draw_u64 over, E each, W of) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   unsigned end[4] = {0, 0, 0, 0};                          // greatest key, greatest complement; all bits set somewhere, all clear somewhere
@@ -294,7 +294,6 @@ __device__ __forceinline__ draw_u64 draw_border(DrawShared& lds, int rows, draw_
     __syncthreads();
     base += draw_digit(lds, want, over, ties) << shift;
     left = shift;
-    if (COARSE) return (draw_u64)base << 32;
     if (left > end_at) continue;
     if (upper) return (draw_u64)upper << 32 | base;
     key = base;
@@ -303,6 +302,39 @@ __device__ __forceinline__ draw_u64 draw_border(DrawShared& lds, int rows, draw_
     upper = key;
     base = ~(unsigned)(rows - 1);
     left = rows > 1 ? 32 - __builtin_clz((unsigned)(rows - 1)) : 1;
+  }
+}
+
+// A key that the k greatest of the keys reach, and few others: the least of its bin among 1,024 from the least key to the greatest, again within
+// the bin while that leaves a quarter too many.  All 1,024 threads call it; each(f) calls f(key) for every key of the thread (0: none), of
+// which there are k at least.
+template <typename E> __device__ __forceinline__ unsigned draw_bound(DrawShared& lds, unsigned k, E each) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  unsigned* bins = reinterpret_cast<unsigned*>(lds.bins);
+  unsigned hi = 0, lo = 0, over = 0;                       // lo: of the keys' complements
+  each([&](unsigned key) { if (key) { hi = max(hi, key); lo = max(lo, ~key); } });
+  hi = draw_wave_prefix(hi, DrawMax());
+  lo = draw_wave_prefix(lo, DrawMax());
+  if (lane == 63) { lds.ends[0][wave] = hi; lds.ends[1][wave] = lo; }
+  bins[threadIdx.x] = 0;
+  __syncthreads();
+  hi = draw_lane(draw_row_prefix(lds.ends[0][lane & 15], DrawMax()), 15);
+  unsigned base = ~draw_lane(draw_row_prefix(lds.ends[1][lane & 15], DrawMax()), 15);
+  int left = hi > base ? 32 - __builtin_clz(hi - base) : 1;
+  while (true) {
+    const int shift = max(left - 10, 0);
+    each([&](unsigned key) { if (key >= base && (draw_u64)(key - base) >> left == 0) atomicAdd(&bins[(key - base) >> shift], 1u); });
+    __syncthreads();
+    const unsigned mine = bins[1023 - threadIdx.x];        // from the top
+    unsigned all;
+    const unsigned before = over + draw_prefix(mine, (unsigned*)lds.slots, all);
+    bins[1023 - threadIdx.x] = 0;
+    if (before < k && before + mine >= k) { lds.found = 1023 - threadIdx.x; lds.found_sum = before; lds.found_all = mine; }
+    __syncthreads();
+    base += lds.found << shift;
+    over = (unsigned)lds.found_sum;
+    left = shift;
+    if (left == 0 || over + (unsigned)lds.found_all <= k + k / 4 + 8) return base;         // uniform
   }
 }
 
