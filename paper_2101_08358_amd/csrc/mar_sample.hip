@@ -161,16 +161,73 @@ __device__ __forceinline__ void draw_short(const DrawArgs& a, int64_t q, DrawSho
   }
 }
 
+// Adds a row's weight to its bin, in units of 2^-bits of the bin's largest: 2^-(x / 32), x what the depth has below its bin's top;
+// 1 - x l + (x l)^2 / 2, l = ln 2 / 32, is off by 2^-19 at most.  Rows that do not count, and those below 2^-63.9, go to 64 words
+// behind the bins: additions to one address go one by one, and those would all meet at one (100 x 1,000,003 in 16 bits,
+// a tenth of them counting: 509 us for the call at one, 251 at 64; all counting: 280 and 286).
+struct DrawBins {
+  float top, c32, w0, w1, w2;
+  __device__ __forceinline__ DrawBins(float top, float c, int bits) : top(top), c32(c * 32.f), w0((float)(1 << bits)) {
+    const float l = 0.69314718f / 32.f;
+    w1 = -l * w0; w2 = 0.5f * l * l * w0;
+  }
+  __device__ __forceinline__ void operator()(unsigned* bins, float v) const {
+    const float depth = __builtin_amdgcn_fmed3f((top - v) * c32, 0.f, DRAW_BINS - 1.f), x = __builtin_amdgcn_fractf(depth);
+    atomicAdd(&bins[depth < DRAW_BINS - 1.f ? (int)depth : DRAW_BINS + (int)(threadIdx.x & 63)], (unsigned)__builtin_fmaf(x, __builtin_fmaf(x, w2, w1), w0));
+  }
+};
+// The bins in which the border of top-p lies: thread t of 1,024 has the sums of bins 2 t and 2 t + 1.  A weight in the histogram is off by
+// 2^-17 of itself at most by its depth (up to 64, in fp32) and polynomial and by a unit, 2^-bits at most of any; those left out are 2^-63.9
+// of the best one each: so are sums.
+__device__ __forceinline__ DrawRange draw_range(draw_u64 nx, draw_u64 ny, int bits, float top_p, draw_u64* slots, int* ends) {
+  const int tid = threadIdx.x;
+  if (tid == 0) { ends[0] = DRAW_BINS - 1; ends[1] = DRAW_BINS - 1; }
+  const double x = (double)nx * exp2(-tid / 16.0), y = (double)ny * exp2(-tid / 16.0 - 1 / 32.0);
+  double all;
+  const double before = draw_prefix(x + y, (double*)slots, all), off = __builtin_ldexp(2.0, -bits) + 0x1p-16, want = (double)top_p * all;
+  // the first bin at whose end the border may have been reached, and the first at whose end it must have been
+  const double may = want * (1.0 - off), must = want * (1.0 + off);
+  if (before < may && before + x + y >= may) ends[0] = before + x >= may ? 2 * tid : 2 * tid + 1;
+  if (before < must && before + x + y >= must) ends[1] = before + x >= must ? 2 * tid : 2 * tid + 1;
+  __syncthreads();
+  return {want <= 0.0 ? 0 : ends[0], want <= 0.0 ? 0 : ends[1], (float)__builtin_ldexp(all, -bits)};
+}
+
+// The row of up to 256 at which the sum of weights reaches `want`, `over` above them: less than half of the time of the digits, which take a
+// dozen barriers each.  place(i): of row i.  Called by 1,024 threads.
+template <typename P>
+__device__ __forceinline__ draw_u64 draw_border_short(DrawShort& lds, unsigned n, draw_u64 want, draw_u64 over, P place, const DrawWeights& w) {
+  const unsigned tid = threadIdx.x, r = tid >> 2, part = tid & 3, padded = (n + 15) & ~15u;
+  if (tid < padded) {
+    const draw_u64 p = tid < n ? place(tid) : 0;
+    lds.row[tid] = {p, p ? w.of((unsigned)(p >> 32)) : 0};
+  }
+  __syncthreads();
+  const draw_u64 mine = r < n ? lds.row[r].place : 0, weight = r < n ? lds.row[r].weight : 0;
+  draw_u64 before = 0;
+#pragma unroll 4
+  for (unsigned i = part; i < padded; i += 4) {
+    const auto other = lds.row[i];
+    before += other.place > mine ? other.weight : 0;
+  }
+  before += draw_moved<0xB1, 0xf>(before);                 // over the four threads of a row
+  before += draw_moved<0x4E, 0xf>(before) + over;
+  if (part == 0 && before < want && before + weight >= want) lds.slots[0] = mine;      // one row
+  __syncthreads();
+  return lds.slots[0];
+}
+
 // ------------------------------------------------------------------------------------------ up to 16,384 rows -----
 // CUTS: some query may have top-k or top-p; without the code for them two workgroups fit a CU.
 template <int TYPE, bool CUTS>
 __global__ void __launch_bounds__(1024, CUTS ? 4 : 8)
 k_draw_small(DrawArgs a, int64_t first) {
   __shared__ union { DrawShared border; DrawShort list; draw_u64 before[2048]; } lds;
-  __shared__ __attribute__((aligned(16))) float held[CUTS ? DRAW_SMALL : 4];
+  __shared__ __attribute__((aligned(16))) union { float score[CUTS ? DRAW_SMALL : 4]; draw_u64 list[CUTS ? DRAW_LIST : 2]; } held;
   __shared__ draw_u64 slots[16];
   __shared__ draw_u64 starts[32];
   __shared__ unsigned listed;
+  __shared__ int ends[2];
   const int64_t q = first + blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const DrawRow<TYPE> row(a, q);
@@ -204,22 +261,67 @@ k_draw_small(DrawArgs a, int64_t first) {
     if (listed <= DRAW_SHORT) { draw_short(a, q, lds.list, listed, par, draw_weights(best, par, 256.f)); return; }
   }
   const float c = draw_depth_scale(par), top = draw_score(best);
-  float approx = 0.f;
+  DrawWeights w = {};
+  bool found_cut = false;
+  if constexpr (CUTS) if (par.top_p < 2.f && draw_all(a, par) && !draw_infinite(best)) {    // uniform
+    // top-p alone: the border's range of bins by a histogram, then the border among the range's rows.  4,000 and 16,000 rows: 19 and 21 us a
+    // query, 76 and 87 us 1,000 of them; by digits over all rows, as below, 35 and 47, 144 and 191
+    unsigned* const bins = reinterpret_cast<unsigned*>(lds.border.bins);
+    for (int i = tid; i < DRAW_BINS; i += 1024) bins[i] = 0;
+    __syncthreads();
+    const DrawBins add(top, c, 17);                        // 2^14 rows in 32 bits
 #pragma unroll
-  for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) approx += __builtin_amdgcn_exp2f(-draw_depth(top, v[b][e], c));
-  approx = draw_sum(approx, (float*)slots);
-  const DrawWeights w = draw_weights(best, par, approx);
-  if constexpr (CUTS) if ((par.top_k > 0 && par.top_k < a.rows) || par.top_p < 2.f) {       // uniform
+      for (int e = 0; e < 8; ++e) add(bins, v[b][e]);
+    __syncthreads();
+    const DrawRange range = draw_range(bins[2 * tid], bins[2 * tid + 1], 17, par.top_p, slots, ends);
+    w = draw_weights(best, par, range.sum);
+    const float c32 = c * 32.f, low = (float)range.low, high = range.high < DRAW_BINS - 1 ? range.high + 1.f : __builtin_inff();
+    draw_u64* const list = held.list;
+    draw_u64 all = 0, above = 0, sum = 0;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const draw_u64 x = w.of_score(v[b][e]);
+        const float bin = (top - v[b][e]) * c32;
+        all += x;
+        above += bin < low ? x : 0;
+        if (bin >= low && bin < high) {
+          sum += x;
+          const unsigned n = atomicAdd(&listed, 1u);
+          if (n < DRAW_LIST) list[n] = place(b, e);
+        }
+      }
+    all = draw_sum(all, slots); above = draw_sum(above, slots); sum = draw_sum(sum, slots);           // their barriers order the list
+    draw_u64 want = draw_share_up(par.top_p, all);
+    if (want == 0) want = 1;
+    const unsigned n = listed;
+    // else many equal rows, or temperatures whose inverse 32 bits do not hold
+    found_cut = n <= DRAW_LIST && above < want && above + sum >= want;
+    if (found_cut && n <= DRAW_SHORT) cut = draw_border_short(lds.list, n, want, above, [&](unsigned i) { return list[i]; }, w);
+    else if (found_cut) cut = draw_border(lds.border, a.rows, want, above, [&](auto f) {
+      for (unsigned i = tid; i - tid < n; i += 1024) { const draw_u64 p = i < n ? list[i] : 0; f(p, [&] { return w.of((unsigned)(p >> 32)); }); }
+    }, [&](unsigned k) { return w.of(k); });
+  }
+  if (!found_cut) {
+    float approx = 0.f;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) approx += __builtin_amdgcn_exp2f(-draw_depth(top, v[b][e], c));
+    w = draw_weights(best, par, draw_sum(approx, (float*)slots));
+  }
+  if constexpr (CUTS) if (!found_cut && ((par.top_k > 0 && par.top_k < a.rows) || par.top_p < 2.f)) {       // uniform
     // through LDS: loops over the rows take a sixteenth of the code, and no registers beside the weights'
     struct Eight { float v[8]; };
 #pragma unroll
-    for (int b = 0; b < 2; ++b) *reinterpret_cast<Eight*>(held + 8192 * b + 8 * tid) = __builtin_bit_cast(Eight, v[b]);
+    for (int b = 0; b < 2; ++b) *reinterpret_cast<Eight*>(held.score + 8192 * b + 8 * tid) = __builtin_bit_cast(Eight, v[b]);
     __syncthreads();
     auto each = [&](auto f) {
 #pragma unroll 2
-      for (int i = tid; i < DRAW_SMALL; i += 1024) f(draw_place(draw_key(held[i]), (unsigned)i));
+      for (int i = tid; i < DRAW_SMALL; i += 1024) f(draw_place(draw_key(held.score[i]), (unsigned)i));
     };
     if (par.top_k > 0 && par.top_k < a.rows) {
       unsigned count = 0;
@@ -238,7 +340,7 @@ k_draw_small(DrawArgs a, int64_t first) {
     }
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const Eight back = *reinterpret_cast<const Eight*>(held + 8192 * b + 8 * tid);
+      const Eight back = *reinterpret_cast<const Eight*>(held.score + 8192 * b + 8 * tid);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[b][e] = back.v[e];
     }
@@ -348,7 +450,7 @@ k_draw_scan(DrawArgs a, int64_t first) {
 template <int TYPE>
 __global__ void __launch_bounds__(256)
 k_draw_hist(DrawArgs a, int64_t first) {
-  __shared__ unsigned bins[DRAW_BINS];
+  __shared__ unsigned bins[DRAW_BINS + 64];
   __shared__ draw_u64 slots[16];
   const int64_t unit = first + blockIdx.x, q = unit / a.chunks;
   const int chunk = (int)(unit - q * a.chunks), tid = threadIdx.x;
@@ -359,52 +461,36 @@ k_draw_hist(DrawArgs a, int64_t first) {
   for (int i = tid; i < DRAW_BINS; i += 256) bins[i] = 0;
   const DrawWhole whole = draw_whole(a, q, c, slots);
   if (draw_infinite(whole.best)) return;
-  const float top = draw_score(whole.best), unit_weight = (float)(1 << a.hist_bits), c32 = c * 32.f, l = 0.69314718f / 32.f, w1 = -l * unit_weight, w2 = 0.5f * l * l * unit_weight;
+  const DrawBins add(draw_score(whole.best), c, a.hist_bits);
   const int begin = chunk * a.chunk_rows, end = (int)min((int64_t)a.rows, (int64_t)begin + a.chunk_rows);
   for (int64_t at = (int64_t)begin + 8 * tid; at < end; at += 2048) {
     float v[8];
     row.raw((int)at, v);
-    // 2^-(x / 32), x what the depth has below its bin's top: 1 - x l + (x l)^2 / 2, l = ln 2 / 32, is off by 2^-19 at most.  Rows that do not
-    // count, and those below 2^-64, end in the last bin: up to 2^-64 too much each
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float depth = __builtin_amdgcn_fmed3f((top - fmaxf(v[e], -__builtin_inff())) * c32, 0.f, DRAW_BINS - 0.01f), x = __builtin_amdgcn_fractf(depth);
-      const unsigned w = (unsigned)__builtin_fmaf(x, __builtin_fmaf(x, w2, w1), unit_weight);
-      atomicAdd(&bins[(int)depth], w);
-    }
+    for (int e = 0; e < 8; ++e) add(bins, fmaxf(v[e], -__builtin_inff()));         // NaN gives way
   }
   __syncthreads();
   unsigned* out = a.hist + unit * DRAW_BINS;
   for (int i = tid; i < DRAW_BINS; i += 256) out[i] = bins[i];
 }
 
-// The bins in which the border of top-p lies.  A weight in the histogram is off by 2^-17 of itself at most by its depth (up to 64, in fp32)
-// and polynomial and by a unit, 2^-hist_bits at most of any but those below 2^-64: so are sums.
 __global__ void __launch_bounds__(1024)
 k_draw_range(DrawArgs a, int64_t first) {
   __shared__ draw_u64 slots[16];
-  __shared__ int low, high;
+  __shared__ int ends[2];
   const int64_t q = first + blockIdx.x;
   const DrawParams par = draw_params(a, q);
   const int tid = threadIdx.x;
   if (draw_few(a, par) || !draw_all(a, par)) return;
   if (par.top_p >= 2.f) return;
-  if (tid == 0) { low = DRAW_BINS - 1; high = DRAW_BINS - 1; }
   draw_u64 nx = 0, ny = 0;                                 // bins 2 tid and 2 tid + 1
 #pragma unroll 8
   for (int k = 0; k < a.chunks; ++k) {
     const uint2 v = *reinterpret_cast<const uint2*>(a.hist + (q * a.chunks + k) * DRAW_BINS + 2 * tid);
     nx += v.x; ny += v.y;
   }
-  const double x = (double)nx * exp2(-tid / 16.0), y = (double)ny * exp2(-tid / 16.0 - 1 / 32.0);
-  double all;
-  const double before = draw_prefix(x + y, (double*)slots, all), off = __builtin_ldexp(2.0, -a.hist_bits) + 0x1p-16, want = (double)par.top_p * all;
-  // the first bin at whose end the border may have been reached, and the first at whose end it must have been
-  const double may = want * (1.0 - off), must = want * (1.0 + off);
-  if (before < may && before + x + y >= may) low = before + x >= may ? 2 * tid : 2 * tid + 1;
-  if (before < must && before + x + y >= must) high = before + x >= must ? 2 * tid : 2 * tid + 1;
-  __syncthreads();
-  if (tid == 0) a.range[q] = {want <= 0.0 ? 0 : low, want <= 0.0 ? 0 : high, (float)__builtin_ldexp(all, -a.hist_bits)};
+  const DrawRange range = draw_range(nx, ny, a.hist_bits, par.top_p, slots, ends);
+  if (tid == 0) a.range[q] = range;
 }
 
 // Integer weights of a chunk.
@@ -595,7 +681,7 @@ k_draw_rows(DrawArgs a, int64_t first) {
     __syncthreads();
     auto each = [&](auto f) { for (unsigned i = tid; i - tid < n; i += 1024) f(i < n ? list[i] : 0); };
     // top-k by counts, then top-p by weights
-    for (int kind = few && (unsigned)par.top_k < n ? 0 : 1; kind < (cuts ? 2 : 1) && !slowly; ++kind) {
+    for (int kind = few && (unsigned)par.top_k < n ? 0 : 1; kind < (cuts ? 2 : 1); ++kind) {
       draw_u64 want = (draw_u64)par.top_k;
       const draw_u64 last = cut;
       if (kind == 1) {
@@ -607,7 +693,11 @@ k_draw_rows(DrawArgs a, int64_t first) {
         // temperatures whose inverse 32 bits do not hold: the histogram was of something else
         slowly = above >= want || above + sum < want;
       }
-      if (!slowly) cut = draw_border(lds.border, a.rows, want, kind == 1 ? above : 0, [&](auto f) {
+      if (slowly) break;
+      if (n <= DRAW_SHORT) {                               // of top-p: top-k's few rows went another way
+        __syncthreads();                                   // all have their sums
+        cut = draw_border_short(lds.few, n, want, above, [&](unsigned i) { return list[i]; }, w);
+      } else cut = draw_border(lds.border, a.rows, want, kind == 1 ? above : 0, [&](auto f) {
         each([&](draw_u64 place) { f(place >= last ? place : 0, [&] { return kind == 1 ? w.of((unsigned)(place >> 32)) : draw_one(); }); });
       }, [&](unsigned k) { return kind == 1 ? w.of(k) : draw_one(); });
     }

@@ -99,3 +99,19 @@ def test_results_do_not_depend_on_the_call():
 def test_more_segments_than_fit_beside_the_borders(f):
     for dt in (torch.float32, torch.bfloat16):
         check(scores_of(21, 2, 2_000_003, dt), uniforms_of(21, 2, 40), **f)
+
+
+@pytest.mark.parametrize("V", (9_000, 16_384, 140_000))
+@pytest.mark.parametrize("equal", (1, 2, 255, 256, 257, 2048, 2049, 8192, 8193))
+def test_equal_rows_at_the_border_of_top_p(V, equal):
+    """The border among so many equal rows: it goes by id whichever way has room for them."""
+    g = np.random.default_rng(equal)
+    s = np.full((3, V), -25.0, dtype=np.float32)
+    for q in range(3):                                        # a row above them, the equal ones, and too little below to matter
+        at = g.permutation(V)[:equal + 1]
+        s[q, at] = 1.0
+        s[q, at[0]] = 1.0 + np.log(equal)
+    s = torch.from_numpy(s).to(DEV)
+    for top_p in (0.4999, 0.75, 0.999):
+        check(s, uniforms_of(equal, 3, 8), top_p=top_p)
+    check(s, uniforms_of(equal, 3, 8), top_p=0.75, temperature=0.9, min_p=0.5 / equal)
