@@ -35,8 +35,17 @@ __device__ __forceinline__ float mx_scale(unsigned byte) {
 static inline int64_t mx_tiles(int64_t queries) { return (queries + 31) / 32; }
 
 struct MxPlan { bool few; int rt, stripes, parts, tiles_part, grid; };
-// Few queries: workgroups that stay, two a CU.  Else a workgroup a stripe of rows and part of the queries' tiles: one a CU at a time,
-// estimated by the rounds of workgroups and their tiles, a workgroup's rows and first images costing some two tiles.
+// Up to 32 queries: workgroups that stay, two a CU, of waves with their own stripes of 32 rt rows.  More: a workgroup a stripe of 256 rt rows
+// and part of the queries' tiles: one a CU at a time, estimated by the rounds of workgroups and their tiles, a workgroup's rows and first
+// images costing some two tiles.  (32 queries of 4,000,000 x 100: 164 us by the first way, 183 by the second; 1 of them: 57 and 118.)
+//
+// rt, 32 rows a lane each, chosen by times of fp32 scores.  Up to 32 queries: 1 where the table is too short for more to fill the device
+// (32,000 x 100: 5.6 us with 1, 7.0 with 4; 64,000 x 400: 17 with 1, 13 with 2; 256,000 x 100: 9.3 and 8.7), 4 up to 192 columns, 2 beyond:
+// the rows ahead are held in registers.  More: 4 reads a quarter of the images and of their matrix operands for the same products, 1 has
+// workgroups enough for small calls and more of them loading rows where these are most of the bytes:
+//   999 x 120,007 x 400, fp32 queries    209 us with 1, 158 with 4      256 x 200,000 x 400   102 and 70       1,000 x 30,000 x 100   33 and 28
+//   256 x 100,000 x 100                   24 and 28                     64 x 60,000 x 100      11 and 14       64 x 2,000,000 x 128  131 and 145
+//   1,000 x 30,000 x 400, 4-bit queries   32 and 34                     4,096 x 12,000 x 400   44 and 48       256 x 500,000 x 400   155 and 139
 static inline MxPlan mx_plan(const mar_mxfp* p) {
   MxPlan r = {};
   const int64_t tiles = mx_tiles(p->num_queries);
@@ -48,7 +57,8 @@ static inline MxPlan mx_plan(const mar_mxfp* p) {
     r.grid = (r.stripes + 3) / 4 < 512 ? (r.stripes + 3) / 4 : 512;
     return r;
   }
-  r.rt = p->num_rows * tiles >= 2048 * 1024 ? 4 : 1;
+  const bool rows_first = tiles < 8 && nk <= 4, products_first = p->dtype != MAR_DTYPE_MXFP4 && (tiles >= 16 || nk > 4);
+  r.rt = !rows_first && p->num_rows * tiles >= (products_first ? 512 * 1024 : 2048 * 1024) ? 4 : 1;
   r.stripes = (int)((p->num_rows + 256 * r.rt - 1) / (256 * r.rt));
   const int64_t slots = 256;
   int64_t best = INT64_MAX;

@@ -26,8 +26,10 @@ def test_scores(tmp_path):
     out = _run(tmp_path, "mar_mxfp.h", """
   long taken = 0, bad = 0;
   for (int64_t rows : {(int64_t)1, (int64_t)31, (int64_t)1000, (int64_t)65536, (int64_t)65537, (int64_t)1048576, (int64_t)40000000, MAR_SOFTMAX_MAX_ROWS - 1, MAR_SOFTMAX_MAX_ROWS})
-    for (int queries : {1, 31, 32, 33, 64, 1000, 4096, 100000, 10000000, MAR_SOFTMAX_MAX_QUERIES}) for (int dim : {1, 64, 65, 192, 193, 400}) {
+    for (int queries : {1, 31, 32, 33, 64, 224, 225, 1000, 4096, 100000, 10000000, MAR_SOFTMAX_MAX_QUERIES}) for (int dim : {1, 64, 65, 192, 193, 256, 257, 400})
+    for (int dtype : {MAR_DTYPE_FP32, MAR_DTYPE_FP16, MAR_DTYPE_MXFP4}) {
       mar_mxfp p = {};
+      p.dtype = dtype;
       p.num_rows = rows; p.num_queries = queries; p.dim = dim;
       const MxPlan r = mx_plan(&p);
       const int64_t tiles = mx_tiles(queries), threads = (int64_t)r.grid * (r.few ? 256 : 512);
@@ -39,7 +41,7 @@ def test_scores(tmp_path):
       if ((int64_t)r.stripes * 256 * r.rt > INT32_MAX || tiles * ((dim + 63) / 64) * 256 >= 1ll << 32) ++bad;
     }
   printf("%ld %ld", taken, bad);""")
-    assert int(out[0]) == 9 * 10 * 6 and out[1] == "0", out
+    assert int(out[0]) == 9 * 12 * 8 * 3 and out[1] == "0", out
 
 
 def test_draws(tmp_path):
