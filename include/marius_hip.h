@@ -326,6 +326,7 @@ int mar_mxfp_rows(const uint8_t* codes, int64_t codes_stride, const uint8_t* sca
  *   queries, codes, scales, scores : device; query_scales: device, for MAR_DTYPE_MXFP4
  *   workspace : device, >= mar_mxfp_scores_workspace_bytes of the same problem, 256-byte aligned; calls that may overlap in time need
  *               one each
+ * scores and workspace must not overlap the inputs.
  */
 typedef struct mar_mxfp {
   int64_t num_rows;             /* rows of the table, 1 .. MAR_SOFTMAX_MAX_ROWS                        */
@@ -364,6 +365,7 @@ int mar_mxfp_scores(const mar_mxfp* problem, const void* queries, const uint8_t*
  *   num_kept    : device, out, [num_queries], or NULL: kept rows
  *   workspace   : device, >= mar_sample_rows_workspace_bytes of the same problem, 256-byte aligned; calls that may overlap in time
  *                 need one each
+ * Outputs and workspace must not overlap the inputs.
  */
 typedef struct mar_sampling {
   int64_t num_rows;      /* scores of a query, 1 .. MAR_SOFTMAX_MAX_ROWS                                */
