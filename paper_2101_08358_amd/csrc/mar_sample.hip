@@ -90,13 +90,6 @@ __device__ __forceinline__ void draw_rows(const DrawArgs& a, int64_t q, const Dr
 }
 
 // Up to 256 rows, with all that top-k leaves among them: four threads a row compare it with all others.  Called by 1,024 threads.
-#define DRAW_SHORT 256
-struct DrawShort {
-  struct { draw_u64 place, weight; } row[DRAW_SHORT];
-  draw_u64 start[DRAW_SHORT], slots[16];
-  unsigned id[DRAW_SHORT];
-  float log_prob[DRAW_SHORT];
-};
 __device__ __forceinline__ void draw_short(const DrawArgs& a, int64_t q, DrawShort& lds, unsigned n, const DrawParams& par, const DrawWeights& w) {
   const unsigned tid = threadIdx.x, r = tid >> 2, part = tid & 3, padded = (n + 15) & ~15u;
   draw_u64 mine = 0;
@@ -193,30 +186,6 @@ __device__ __forceinline__ DrawRange draw_range(draw_u64 nx, draw_u64 ny, int bi
   return {want <= 0.0 ? 0 : ends[0], want <= 0.0 ? 0 : ends[1], (float)__builtin_ldexp(all, -bits)};
 }
 
-// The row of up to 256 at which the sum of weights reaches `want`, `over` above them: less than half of the time of the digits, which take a
-// dozen barriers each.  place(i): of row i.  Called by 1,024 threads.
-template <typename P>
-__device__ __forceinline__ draw_u64 draw_border_short(DrawShort& lds, unsigned n, draw_u64 want, draw_u64 over, P place, const DrawWeights& w) {
-  const unsigned tid = threadIdx.x, r = tid >> 2, part = tid & 3, padded = (n + 15) & ~15u;
-  if (tid < padded) {
-    const draw_u64 p = tid < n ? place(tid) : 0;
-    lds.row[tid] = {p, p ? w.of((unsigned)(p >> 32)) : 0};
-  }
-  __syncthreads();
-  const draw_u64 mine = r < n ? lds.row[r].place : 0, weight = r < n ? lds.row[r].weight : 0;
-  draw_u64 before = 0;
-#pragma unroll 4
-  for (unsigned i = part; i < padded; i += 4) {
-    const auto other = lds.row[i];
-    before += other.place > mine ? other.weight : 0;
-  }
-  before += draw_moved<0xB1, 0xf>(before);                 // over the four threads of a row
-  before += draw_moved<0x4E, 0xf>(before) + over;
-  if (part == 0 && before < want && before + weight >= want) lds.slots[0] = mine;      // one row
-  __syncthreads();
-  return lds.slots[0];
-}
-
 // ------------------------------------------------------------------------------------------ up to 16,384 rows -----
 // CUTS: some query may have top-k or top-p; without the code for them two workgroups fit a CU.
 template <int TYPE, bool CUTS>
@@ -300,8 +269,8 @@ k_draw_small(DrawArgs a, int64_t first) {
     const unsigned n = listed;
     // else many equal rows, or temperatures whose inverse 32 bits do not hold
     found_cut = n <= DRAW_LIST && above < want && above + sum >= want;
-    if (found_cut && n <= DRAW_SHORT) cut = draw_border_short(lds.list, n, want, above, [&](unsigned i) { return list[i]; }, w);
-    else if (found_cut) cut = draw_border(lds.border, a.rows, want, above, [&](auto f) {
+    if (found_cut && n <= DRAW_SHORT) cut = draw_border_short(lds.list, n, want, above, [&](unsigned i) { return list[i]; }, [&](unsigned k) { return w.of(k); });
+    else if (found_cut) cut = draw_border<true>(lds.border, a.rows, want, above, [&](auto f) {
       for (unsigned i = tid; i - tid < n; i += 1024) { const draw_u64 p = i < n ? list[i] : 0; f(p, [&] { return w.of((unsigned)(p >> 32)); }); }
     }, [&](unsigned k) { return w.of(k); });
   }
@@ -327,7 +296,7 @@ k_draw_small(DrawArgs a, int64_t first) {
       unsigned count = 0;
       each([&](draw_u64 place) { count += place != 0; });
       count = draw_sum(count, (unsigned*)slots);
-      if ((unsigned)par.top_k < count) cut = draw_border(lds.border, a.rows, (draw_u64)par.top_k, 0, [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); },
+      if ((unsigned)par.top_k < count) cut = draw_border<true>(lds.border, a.rows, (draw_u64)par.top_k, 0, [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); },
                                                                [](unsigned) { return draw_one(); });
     }
     if (par.top_p < 2.f) {
@@ -335,7 +304,7 @@ k_draw_small(DrawArgs a, int64_t first) {
       const draw_u64 top_k = cut;
       each([&](draw_u64 place) { all += place >= top_k ? w.of((unsigned)(place >> 32)) : 0; });
       const draw_u64 want = draw_share_up(par.top_p, draw_sum(all, slots));
-      cut = draw_border(lds.border, a.rows, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
+      cut = draw_border<true>(lds.border, a.rows, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
                                [&](unsigned k) { return w.of(k); });
     }
 #pragma unroll
@@ -696,8 +665,8 @@ k_draw_rows(DrawArgs a, int64_t first) {
       if (slowly) break;
       if (n <= DRAW_SHORT) {                               // of top-p: top-k's few rows went another way
         __syncthreads();                                   // all have their sums
-        cut = draw_border_short(lds.few, n, want, above, [&](unsigned i) { return list[i]; }, w);
-      } else cut = draw_border(lds.border, a.rows, want, kind == 1 ? above : 0, [&](auto f) {
+        cut = draw_border_short(lds.few, n, want, above, [&](unsigned i) { return list[i]; }, [&](unsigned k) { return w.of(k); });
+      } else cut = draw_border<true>(lds.border, a.rows, want, kind == 1 ? above : 0, [&](auto f) {
         each([&](draw_u64 place) { f(place >= last ? place : 0, [&] { return kind == 1 ? w.of((unsigned)(place >> 32)) : draw_one(); }); });
       }, [&](unsigned k) { return kind == 1 ? w.of(k) : draw_one(); });
     }
@@ -749,14 +718,14 @@ k_draw_slowly(DrawArgs a, int64_t first) {
   draw_u64 cut = 1;
   unsigned count = 0;
   if (par.top_k > 0) { each([&](draw_u64 place) { count += place != 0; }); count = draw_sum(count, (unsigned*)lds.slots); }
-  if (par.top_k > 0 && (unsigned)par.top_k < count) cut = draw_border(lds, a.rows, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
+  if (par.top_k > 0 && (unsigned)par.top_k < count) cut = draw_border<false>(lds, a.rows, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
   if (par.top_p < 2.f) {
     draw_u64 all = 0;
     each([&](draw_u64 place) { if (place >= cut) all += w.of((unsigned)(place >> 32)); });
     all = draw_sum(all, lds.slots);
     const draw_u64 want = draw_share_up(par.top_p, all), top_k = cut;
     // rows below top-k's cut have no say: they come after the border
-    cut = draw_border(lds, a.rows, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
+    cut = draw_border<false>(lds, a.rows, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
                       [&](unsigned k) { return w.of(k); });
   }
   const draw_u64 least = w.least(par.min_p);
@@ -794,8 +763,10 @@ template <int TYPE> static void launch_draws(const DrawArgs& a, int64_t queries,
   const bool all = a.top_ks || (!greedy && (a.top_k == 0 || a.top_k >= a.rows)), cuts = a.top_ps || a.top_p < 1.f;
   sm_launches(queries * a.chunks, 256, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_scan<TYPE>, dim3(n), dim3(256), 0, st, a, first); });
   if (all) {
-    if (cuts) sm_launches(queries * a.chunks, 256, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_hist<TYPE>, dim3(n), dim3(256), 0, st, a, first); });
-    sm_launches(queries, 1024, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_range, dim3(n), dim3(1024), 0, st, a, first); });
+    if (cuts) {
+      sm_launches(queries * a.chunks, 256, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_hist<TYPE>, dim3(n), dim3(256), 0, st, a, first); });
+      sm_launches(queries, 1024, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_range, dim3(n), dim3(1024), 0, st, a, first); });
+    }
     sm_launches(queries * a.chunks, 256, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_weigh<TYPE>, dim3(n), dim3(256), 0, st, a, first); });
   }
   sm_launches(queries, 1024, [&](int64_t first, unsigned n) { hipLaunchKernelGGL(k_draw_rows<TYPE>, dim3(n), dim3(1024), 0, st, a, first); });

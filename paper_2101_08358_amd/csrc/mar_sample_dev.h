@@ -210,12 +210,44 @@ template <typename T> __device__ __forceinline__ T draw_prefix(T v, T* slots, T&
   return before + run - v;
 }
 
+// LDS of up to 256 rows, each compared with all others by four of 1,024 threads.
+#define DRAW_SHORT 256
+struct DrawShort {
+  struct { draw_u64 place, weight; } row[DRAW_SHORT];
+  draw_u64 start[DRAW_SHORT], slots[16];
+  unsigned id[DRAW_SHORT];
+  float log_prob[DRAW_SHORT];
+};
+// The row of up to 256 at which the sum of weights reaches `want`, `over` above them.  place(i): of row i; of(key): a key's weight.
+template <typename P, typename W>
+__device__ __forceinline__ draw_u64 draw_border_short(DrawShort& lds, unsigned n, draw_u64 want, draw_u64 over, P place, W of) {
+  const unsigned tid = threadIdx.x, r = tid >> 2, part = tid & 3, padded = (n + 15) & ~15u;
+  if (tid < padded) {
+    const draw_u64 p = tid < n ? place(tid) : 0;
+    lds.row[tid] = {p, p ? of((unsigned)(p >> 32)) : 0};
+  }
+  __syncthreads();
+  const draw_u64 mine = r < n ? lds.row[r].place : 0, weight = r < n ? lds.row[r].weight : 0;
+  draw_u64 before = 0;
+#pragma unroll 4
+  for (unsigned i = part; i < padded; i += 4) {
+    const auto other = lds.row[i];
+    before += other.place > mine ? other.weight : 0;
+  }
+  before += draw_moved<0xB1, 0xf>(before);                 // over the four threads of a row: lanes 1 0 3 2, then 2 3 0 1
+  before += draw_moved<0x4E, 0xf>(before) + over;
+  if (part == 0 && before < want && before + weight >= want) lds.slots[0] = mine;      // one row
+  __syncthreads();
+  return lds.slots[0];
+}
+
 #define DRAW_DIGIT 12               // bits of a border's digit: 24 bits of range take two
 // LDS of a workgroup of 1,024 threads that looks for a border.
 struct DrawShared {
   draw_u64 bins[1 << DRAW_DIGIT], slots[16], found_sum, found_all;
-  unsigned found, ends[4][16];
+  unsigned found, listed, ends[4][16];
 };
+static_assert(sizeof(DrawShort) + DRAW_SHORT * sizeof(draw_u64) <= sizeof(draw_u64) << DRAW_DIGIT, "the border's rows and their list in the digits' place");
 // Adds a wave's weights to their bins.  Lanes that share a bin add up first, as long as many do: additions to one address go one by one.
 __device__ __forceinline__ void draw_add(DrawShared& lds, bool has, unsigned bin, draw_u64 w) {
   draw_u64 left = __builtin_amdgcn_ballot_w64(has);
@@ -255,8 +287,8 @@ __device__ __forceinline__ unsigned draw_digit(DrawShared& lds, draw_u64 want, d
 // spreads whatever the range (scores share their first bits: by those, most rows would meet at few addresses, one after the other),
 // without the last bits that all keys share (16 of bf16's); then, where several rows share the border's key, of the ids.  All 1,024 threads
 // call it; each(f) calls f(place, weight) for every row of the thread, weight() its weight, as often in all lanes of a wave (place 0: no
-// row); of(key): a key's weight.
-template <typename E, typename W>
+// row); of(key): a key's weight.  LISTS: a pass costs little (rows in LDS): the rows of a digit's bin, where they are few, go to the end at once.
+template <bool LISTS, typename E, typename W>
 __device__ __forceinline__ draw_u64 draw_border(DrawShared& lds, int rows, draw_u64 want, draw_u64 over, E each, W of) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   unsigned end[4] = {0, 0, 0, 0};                          // greatest key, greatest complement; all bits set somewhere, all clear somewhere
@@ -285,6 +317,7 @@ __device__ __forceinline__ draw_u64 draw_border(DrawShared& lds, int rows, draw_
     const int end_at = upper ? 0 : same, width = min(left - end_at, DRAW_DIGIT), shift = left - width;
     __syncthreads();
     for (int i = threadIdx.x; i < 1 << DRAW_DIGIT; i += 1024) lds.bins[i] = 0;
+    if (threadIdx.x == 0) lds.listed = 0;
     __syncthreads();
     each([&](draw_u64 place, auto weight) {
       const unsigned k = upper ? (unsigned)place : (unsigned)(place >> 32);
@@ -294,6 +327,18 @@ __device__ __forceinline__ draw_u64 draw_border(DrawShared& lds, int rows, draw_
     __syncthreads();
     base += draw_digit(lds, want, over, ties) << shift;
     left = shift;
+    if (LISTS && !upper) {
+      DrawShort& few = *reinterpret_cast<DrawShort*>(lds.bins);
+      draw_u64* const list = lds.bins + (sizeof(DrawShort) + 7) / 8;
+      each([&](draw_u64 place, auto) {
+        const unsigned k = (unsigned)(place >> 32);
+        if (place == 0 || k < base || (draw_u64)(k - base) >> left != 0) return;
+        const unsigned n = atomicAdd(&lds.listed, 1u);
+        if (n < DRAW_SHORT) list[n] = place;
+      });
+      __syncthreads();
+      if (lds.listed <= DRAW_SHORT) return draw_border_short(few, lds.listed, want, over, [&](unsigned i) { return list[i]; }, of);          // uniform
+    }
     if (left > end_at) continue;
     if (upper) return (draw_u64)upper << 32 | base;
     key = base;
