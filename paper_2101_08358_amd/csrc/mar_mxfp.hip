@@ -4,7 +4,9 @@
 // is a sign and the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times the scale, ties to the even code, at most 6: code 0 .. 7, sign in bit 3.
 // v 2^-e is exact in fp32 (a subnormal that it leaves is below every threshold), so that the one rounding is the code's.
 //
-// Both kernels are bound by memory: a thread takes eight columns, four neighbouring threads a block.
+// Both kernels are bound by memory: a thread takes eight columns (32 bytes of fp32 in, 4 bytes of codes out), four neighbouring threads a
+// block, whose maximum they exchange among their lanes.  No row has a workgroup of its own: rows are of any number of blocks, and a
+// division a workgroup finds where its 64 blocks lie.
 #include "mar_common.h"
 #include "mar_mxfp.h"
 #include "mar_rows_dev.h"
@@ -29,6 +31,7 @@ __device__ __forceinline__ BlockOf block_of(int64_t first, int64_t blocks, int r
   return r;
 }
 
+// 1,000,003 x 400 fp32: 362 to 390 us, 1.82 GB at 4.7 to 5.0 TB/s, a large copy's rate; 10,000 x 50: 2.6 to 3 us, a launch.
 template <int TYPE>
 __global__ void __launch_bounds__(256)
 k_quantise(QuantiseArgs a) {
@@ -57,6 +60,8 @@ struct RowsArgs {
   int64_t codes_stride, scales_stride, out_stride, num_rows, blocks, first;
   int32_t dim, row_blocks;
 };
+// value = level (a conversion instruction's, exact) times 2^e.  1,000,003 x 400 to bf16: 227 to 250 us, 1.02 GB at 4.1 to 4.5 TB/s; 100,000
+// rows by id out of 2,000,000: 19 us, 5.3 TB/s; 1,000 of 50 columns: 2.6 to 3 us, a launch.
 template <int TYPE>
 __global__ void __launch_bounds__(256)
 k_mxfp_rows(RowsArgs a) {
