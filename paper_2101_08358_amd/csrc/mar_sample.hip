@@ -32,12 +32,24 @@ __device__ __forceinline__ draw_u64 draw_target(float u, draw_u64 total) { retur
 struct DrawWhole { unsigned best; float sum; };
 __device__ __forceinline__ DrawWhole draw_whole(const DrawArgs& a, int64_t q, float c, draw_u64* slots) {
   DrawWhole r = {0u, 0.f};
-  DrawChunk mine = {0u, 0.f};
+  DrawChunk mine = {0u, 0u, 0.f};
   if ((int)threadIdx.x < a.chunks) mine = a.stats[q * a.chunks + threadIdx.x];
   r.best = draw_reduce(mine.best, (unsigned*)slots, DrawMax());
   const float part = mine.best ? mine.sum * __builtin_amdgcn_exp2f(-draw_depth(draw_score(r.best), draw_score(mine.best), c)) : 0.f;
   r.sum = draw_sum(part, (float*)slots);
   return r;
+}
+
+// Bins to a binary order of magnitude: 32, doubled as long as all rows that count fit, so that flat scores spread over the bins as well (100 x
+// 1,000,003 in 16 bits, scores over the temperature of deviation 0.2: 3.4 ms for the call with 32, all of whose bins' rows no
+// list holds, and 0.28).
+__device__ __forceinline__ float draw_fine(const DrawArgs& a, int64_t q, float c, unsigned best, draw_u64* slots) {
+  unsigned low = (int)threadIdx.x < a.chunks ? a.stats[q * a.chunks + threadIdx.x].low : 0;
+  low = draw_reduce(low, (unsigned*)slots, DrawMax());
+  const float depth = draw_depth(draw_score(best), draw_score(~low), c);
+  float span = 63.f / 2, fine = 32.f;
+  if (low) while (fine < 32768.f && depth <= span) { span /= 2; fine *= 2; }       // uniform
+  return fine;
 }
 
 // The draws of a query: rows with place >= cut and weight >= least; mass: the segments' sums (LDS or memory), replaced by those before them.
@@ -155,28 +167,28 @@ __device__ __forceinline__ void draw_short(const DrawArgs& a, int64_t q, DrawSho
   }
 }
 
-// Adds a row's weight to its bin, in units of 2^-bits of the bin's largest: 2^-(x / 32), x what the depth has below its bin's top;
-// 1 - x l + (x l)^2 / 2, l = ln 2 / 32, is off by 2^-19 at most.  Rows that do not count, and those below 2^-63.9, go to 64 words
+// Adds a row's weight to its bin, in units of 2^-bits of the bin's largest: 2^-(x / fine), x what the depth has below its bin's top;
+// 1 - x l + (x l)^2 / 2, l = ln 2 / fine, is off by 2^-19 at most.  Rows that do not count, and those below 2^-63.9, go to 64 words
 // behind the bins: additions to one address go one by one, and those would all meet at one (100 x 1,000,003 in 16 bits,
 // a tenth of them counting: 509 us for the call at one, 251 at 64; all counting: 280 and 286).
 struct DrawBins {
-  float top, c32, w0, w1, w2;
-  __device__ __forceinline__ DrawBins(float top, float c, int bits) : top(top), c32(c * 32.f), w0((float)(1 << bits)) {
-    const float l = 0.69314718f / 32.f;
+  float top, scale, w0, w1, w2;
+  __device__ __forceinline__ DrawBins(float top, float c, float fine, int bits) : top(top), scale(c * fine), w0((float)(1 << bits)) {
+    const float l = 0.69314718f / fine;
     w1 = -l * w0; w2 = 0.5f * l * l * w0;
   }
   __device__ __forceinline__ void operator()(unsigned* bins, float v) const {
-    const float depth = __builtin_amdgcn_fmed3f((top - v) * c32, 0.f, DRAW_BINS - 1.f), x = __builtin_amdgcn_fractf(depth);
+    const float depth = __builtin_amdgcn_fmed3f((top - v) * scale, 0.f, DRAW_BINS - 1.f), x = __builtin_amdgcn_fractf(depth);
     atomicAdd(&bins[depth < DRAW_BINS - 1.f ? (int)depth : DRAW_BINS + (int)(threadIdx.x & 63)], (unsigned)__builtin_fmaf(x, __builtin_fmaf(x, w2, w1), w0));
   }
 };
 // The bins in which the border of top-p lies: thread t of 1,024 has the sums of bins 2 t and 2 t + 1.  A weight in the histogram is off by
 // 2^-17 of itself at most by its depth (up to 64, in fp32) and polynomial and by a unit, 2^-bits at most of any; those left out are 2^-63.9
 // of the best one each: so are sums.
-__device__ __forceinline__ DrawRange draw_range(draw_u64 nx, draw_u64 ny, int bits, float top_p, draw_u64* slots, int* ends) {
+__device__ __forceinline__ DrawRange draw_range(draw_u64 nx, draw_u64 ny, int bits, float fine, float top_p, draw_u64* slots, int* ends) {
   const int tid = threadIdx.x;
   if (tid == 0) { ends[0] = DRAW_BINS - 1; ends[1] = DRAW_BINS - 1; }
-  const double x = (double)nx * exp2(-tid / 16.0), y = (double)ny * exp2(-tid / 16.0 - 1 / 32.0);
+  const double x = (double)nx * exp2(-2 * tid / (double)fine), y = (double)ny * exp2(-(2 * tid + 1) / (double)fine);
   double all;
   const double before = draw_prefix(x + y, (double*)slots, all), off = __builtin_ldexp(2.0, -bits) + 0x1p-16, want = (double)top_p * all;
   // the first bin at whose end the border may have been reached, and the first at whose end it must have been
@@ -198,13 +210,13 @@ k_draw_small(DrawArgs a, int64_t first) {
   __shared__ __attribute__((aligned(16))) union { float score[CUTS ? DRAW_SMALL : 4]; draw_u64 list[CUTS ? DRAW_LIST : 2]; } held;
   __shared__ draw_u64 slots[16];
   __shared__ draw_u64 starts[32];
-  __shared__ unsigned listed;
+  __shared__ unsigned listed, reached;
   __shared__ int ends[2];
   const int64_t q = first + blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const DrawRow<TYPE> row(a, q);
   const DrawParams par = draw_params(a, q);
-  if (tid == 0) listed = 0;
+  if (tid == 0) { listed = 0; reached = 0; }
   float v[2][8], mine = -__builtin_inff();                  // columns 8 tid .. and 8,192 + 8 tid ..: a wave holds segments `wave` and 16 + wave
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
@@ -241,13 +253,13 @@ k_draw_small(DrawArgs a, int64_t first) {
     unsigned* const bins = reinterpret_cast<unsigned*>(lds.border.bins);
     for (int i = tid; i < DRAW_BINS; i += 1024) bins[i] = 0;
     __syncthreads();
-    const DrawBins add(top, c, 17);                        // 2^14 rows in 32 bits
+    const DrawBins add(top, c, 32.f, 17);                        // 2^14 rows in 32 bits
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int e = 0; e < 8; ++e) add(bins, v[b][e]);
     __syncthreads();
-    const DrawRange range = draw_range(bins[2 * tid], bins[2 * tid + 1], 17, par.top_p, slots, ends);
+    const DrawRange range = draw_range(bins[2 * tid], bins[2 * tid + 1], 17, 32.f, par.top_p, slots, ends);
     w = draw_weights(best, par, range.sum);
     const float c32 = c * 32.f, low = (float)range.low, high = range.high < DRAW_BINS - 1 ? range.high + 1.f : __builtin_inff();
     draw_u64* const list = held.list;
@@ -284,6 +296,58 @@ k_draw_small(DrawArgs a, int64_t first) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) approx += __builtin_amdgcn_exp2f(-draw_depth(top, v[b][e], c));
     w = draw_weights(best, par, draw_sum(approx, (float*)slots));
+  }
+  if constexpr (CUTS) if (par.top_k > 0 && par.top_k < a.rows) {       // uniform
+    // larger top-k: a bound among all rows, and everything else concerns the rows that reach it (16,000 rows, top-k 1,000, top-p 0.9: 28 us; by
+    // digits over all rows, as below, 53; 1,000 queries: 114 and 218)
+    const unsigned k = (unsigned)par.top_k;
+    unsigned count = 0;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) count += v[b][e] > -__builtin_inff();
+    count = draw_sum(count, (unsigned*)slots);
+    if (k < count) {
+      const unsigned bound = draw_bound(lds.border, k, [&](auto f) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f(draw_key(v[b][e]));
+      });
+      unsigned here = 0;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) here += draw_key(v[b][e]) >= bound;
+      const unsigned upto = draw_wave_prefix(here);
+      unsigned at = 0;
+      if (lane == 63 && upto) at = atomicAdd(&reached, upto);
+      at = draw_lane(at, 63) + upto - here;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (draw_key(v[b][e]) >= bound) { if (at < DRAW_LIST) held.list[at] = place(b, e); ++at; }
+      __syncthreads();
+      const unsigned n = reached;
+      found_cut = n <= DRAW_LIST;                          // else many equal rows
+      if (found_cut) {
+        auto each = [&](auto f) { for (unsigned i = tid; i - tid < n; i += 1024) f(i < n ? held.list[i] : 0); };
+        cut = (draw_u64)bound << 32;
+        for (int kind = k < n ? 0 : 1; kind < (par.top_p < 2.f ? 2 : 1); ++kind) {         // by counts, then by weights
+          draw_u64 want = k;
+          const draw_u64 last = cut;
+          if (kind == 1) {
+            draw_u64 sum = 0;
+            each([&](draw_u64 p) { sum += p >= last ? w.of((unsigned)(p >> 32)) : 0; });
+            want = draw_share_up(par.top_p, draw_sum(sum, slots));
+            if (want == 0) want = 1;
+          }
+          cut = draw_border<true>(lds.border, a.rows, want, 0, [&](auto f) {
+            each([&](draw_u64 p) { f(p >= last ? p : 0, [&] { return kind == 1 ? w.of((unsigned)(p >> 32)) : draw_one(); }); });
+          }, [&](unsigned key) { return kind == 1 ? w.of(key) : draw_one(); });
+        }
+      }
+    }
   }
   if constexpr (CUTS) if (!found_cut && ((par.top_k > 0 && par.top_k < a.rows) || par.top_p < 2.f)) {       // uniform
     // through LDS: loops over the rows take a sixteenth of the code, and no registers beside the weights'
@@ -367,8 +431,8 @@ k_draw_small(DrawArgs a, int64_t first) {
 }
 
 // ------------------------------------------------------------------------------------------ more rows -----
-// A workgroup a chunk of a query.  Group (chunk, block b, thread): the thread's columns of the iterations of block b.  Bound by memory: 100 x
-// 1,000,003 bf16: 33 us, 6.1 TB/s (part of the scores comes out of the last-level cache); 64 x 131,072 fp32: 7 to 8 us.
+// A workgroup a chunk of a query.  Group (chunk, block b, i): the columns of threads merge i .. merge i + merge - 1 in the iterations of block b.  Bound by memory: 100 x
+// 1,000,003 bf16: 36 us, 5.5 TB/s (part of the scores comes out of the last-level cache); 64 x 131,072 fp32: 7 to 10 us.
 template <int TYPE>
 __global__ void __launch_bounds__(256)
 k_draw_scan(DrawArgs a, int64_t first) {
@@ -382,8 +446,11 @@ k_draw_scan(DrawArgs a, int64_t first) {
   const int begin = chunk * a.chunk_rows, end = (int)min((int64_t)a.rows, (int64_t)begin + a.chunk_rows);
   const int turns = a.chunk_rows / 2048, turns_block = (turns + a.blocks - 1) / a.blocks;
   const bool sums = !few && draw_all(a, par) && par.top_p >= 2.f;
-  float best = -__builtin_inff(), sum = 0.f, group = best;
-  unsigned* maxima = a.maxima + q * a.groups + (int64_t)chunk * a.blocks * 256 + tid;
+  const bool lows = !few && draw_all(a, par) && par.top_p < 2.f;
+  float best = -__builtin_inff(), low = __builtin_inff(), sum = 0.f, group = best;
+  const int width = 256 / a.merge;
+  unsigned* maxima = a.maxima + q * a.groups + (int64_t)chunk * a.blocks * width + tid / a.merge;
+  const bool first_of = tid % a.merge == 0;
   int block = 0, left = turns_block;
   for (int i = 0; i < turns; ++i) {
     const int64_t at = (int64_t)begin + i * 2048 + 8 * tid;
@@ -394,6 +461,17 @@ k_draw_scan(DrawArgs a, int64_t first) {
       for (int e = 0; e < 8; ++e) here = fmaxf(here, v[e]);          // NaN gives way
       here = fminf(here, DRAW_TOP);
       group = fmaxf(group, here);
+      if (lows) {                                          // uniform
+        float least = DRAW_TOP;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) least = fminf(least, v[e]);
+        if (!(least > -__builtin_inff())) {                // some do not count
+          least = DRAW_TOP;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) least = fminf(least, v[e] > -__builtin_inff() ? v[e] : DRAW_TOP);
+        }
+        low = fminf(low, least);
+      }
       if (sums) {
         if (here > best) sum = sum > 0.f ? sum * __builtin_amdgcn_exp2f(-draw_depth(here, best, c)) : 0.f;
         const float top = fmaxf(best, here);
@@ -405,16 +483,20 @@ k_draw_scan(DrawArgs a, int64_t first) {
       best = fmaxf(best, here);
     }
     if (--left == 0 || i + 1 == turns) {
-      if (few) maxima[256 * block] = draw_key(group);
+      if (few) {                                           // uniform
+        for (int i = 1; i < a.merge; i *= 2) group = fmaxf(group, __shfl_xor(group, i));
+        if (first_of) maxima[width * block] = draw_key(group);
+      }
       group = -__builtin_inff(); ++block; left = turns_block;
     }
   }
-  if (few) for (; block < a.blocks; ++block) maxima[256 * block] = 0;
+  if (few && first_of) for (; block < a.blocks; ++block) maxima[width * block] = 0;
   const unsigned mine = draw_key(best), all = draw_reduce(mine, (unsigned*)slots, DrawMax());
   sum = mine ? sum * __builtin_amdgcn_exp2f(-draw_depth(draw_score(all), best, c)) : 0.f;
   sum = draw_sum(sum, (float*)slots);
+  const unsigned least = draw_reduce(lows && mine ? ~draw_key(low) : 0u, (unsigned*)slots, DrawMax());
   if (tid == 0) {
-    a.stats[q * a.chunks + chunk] = {all, sum};
+    a.stats[q * a.chunks + chunk] = {all, least, sum};
     if (chunk == 0) a.listed[q] = 0;
   }
 }
@@ -435,7 +517,7 @@ k_draw_hist(DrawArgs a, int64_t first) {
   for (int i = tid; i < DRAW_BINS; i += 256) bins[i] = 0;
   const DrawWhole whole = draw_whole(a, q, c, slots);
   if (draw_infinite(whole.best)) return;
-  const DrawBins add(draw_score(whole.best), c, a.hist_bits);
+  const DrawBins add(draw_score(whole.best), c, draw_fine(a, q, c, whole.best, slots), a.hist_bits);
   const int begin = chunk * a.chunk_rows, end = (int)min((int64_t)a.rows, (int64_t)begin + a.chunk_rows);
   for (int64_t at = (int64_t)begin + 8 * tid; at < end; at += 2048) {
     float v[8];
@@ -448,7 +530,7 @@ k_draw_hist(DrawArgs a, int64_t first) {
   for (int i = tid; i < DRAW_BINS; i += 256) out[i] = bins[i];
 }
 
-// A workgroup a query: 256 chunks' bins are 2 MB, read by one CU: 6 to 7 us.
+// A workgroup a query: 20 to 256 chunks' bins of 8 KB each, read by one CU: 7 to 8 us.
 __global__ void __launch_bounds__(1024)
 k_draw_range(DrawArgs a, int64_t first) {
   __shared__ draw_u64 slots[16];
@@ -464,7 +546,8 @@ k_draw_range(DrawArgs a, int64_t first) {
     const uint2 v = *reinterpret_cast<const uint2*>(a.hist + (q * a.chunks + k) * DRAW_BINS + 2 * tid);
     nx += v.x; ny += v.y;
   }
-  const DrawRange range = draw_range(nx, ny, a.hist_bits, par.top_p, slots, ends);
+  const float c = draw_depth_scale(par), fine = draw_fine(a, q, c, draw_whole(a, q, c, slots).best, slots);
+  const DrawRange range = draw_range(nx, ny, a.hist_bits, fine, par.top_p, slots, ends);
   if (tid == 0) a.range[q] = range;
 }
 
@@ -486,8 +569,8 @@ k_draw_weigh(DrawArgs a, int64_t first) {
   const DrawRange range = par.top_p < 2.f ? a.range[q] : DrawRange{0, 0, 0.f};
   const DrawWeights w = draw_weights(whole.best, par, par.top_p < 2.f ? range.sum : whole.sum);
   const draw_u64 least = w.least(par.min_p);
-  // bins by their depth, 32 to a binary order of magnitude, as the histogram counts them
-  const float top = draw_score(whole.best), c32 = c * 32.f, low = (float)range.low, high = range.high < DRAW_BINS - 1 ? range.high + 1.f : __builtin_inff();
+  // bins by their depth, as the histogram counts them
+  const float top = draw_score(whole.best), scale = par.top_p < 2.f ? c * draw_fine(a, q, c, whole.best, slots) : 0.f, low = (float)range.low, high = range.high < DRAW_BINS - 1 ? range.high + 1.f : __builtin_inff();
   const int begin = chunk * a.chunk_rows, end = (int)min((int64_t)a.rows, (int64_t)begin + a.chunk_rows);
   draw_u64 all = 0, above = 0;
   unsigned kept = 0;
@@ -505,7 +588,7 @@ k_draw_weigh(DrawArgs a, int64_t first) {
           const draw_u64 x = w.of_score(v[e]);
           bool in = CUTS || v[e] > -__builtin_inff();      // a row that does not count lies below every range
           if (CUTS) {
-            const float bin = (top - v[e]) * c32;
+            const float bin = (top - v[e]) * scale;
             in = bin < low;
             all += x;
             near[e] = __builtin_amdgcn_ballot_w64(bin >= low) & __builtin_amdgcn_ballot_w64(bin < high);
@@ -518,10 +601,12 @@ k_draw_weigh(DrawArgs a, int64_t first) {
         if (CUTS) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) if (near[e]) {       // uniform
-            const float bin = (top - v[e]) * c32;
+            const float bin = (top - v[e]) * scale;
             if (!(bin >= low && bin < high)) continue;
             const unsigned n = atomicAdd(&listed, 1u);
-            if (n < DRAW_LIST_CHUNK) list[n] = draw_place(draw_key(v[e]), (unsigned)at + e);
+            const draw_u64 place = draw_place(draw_key(v[e]), (unsigned)at + e);
+            if (n < DRAW_LIST_CHUNK) list[n] = place;
+            else if (const unsigned m = atomicAdd(&a.listed[q], 1u); m < (unsigned)a.list) a.lists[q * a.list + m] = place;
           }
           if (!FLOOR) above += sum;
         }
@@ -536,14 +621,13 @@ k_draw_weigh(DrawArgs a, int64_t first) {
   all = draw_sum(all, slots);
   above = draw_sum(above, slots);
   kept = draw_sum(kept, (unsigned*)slots);
-  const unsigned n = listed;                               // the reductions' barriers lie behind the last one
+  const unsigned n = min(listed, (unsigned)DRAW_LIST_CHUNK);          // the reductions' barriers lie behind the last one
   if (threadIdx.x == 0) {
     a.totals[2 * unit] = all; a.totals[2 * unit + 1] = above;
     a.kept[unit] = kept;
-    // a chunk whose rows its list does not hold: more than the query's list holds, whatever the others add (256 chunks at most)
-    list_at = n ? atomicAdd(&a.listed[q], n > DRAW_LIST_CHUNK ? 1u << 22 : n) : 0;
+    list_at = n ? atomicAdd(&a.listed[q], n) : 0;
   }
-  if (n == 0 || n > DRAW_LIST_CHUNK) return;               // uniform
+  if (n == 0) return;                                      // uniform
   __syncthreads();
   for (unsigned i = threadIdx.x; i < n; i += 256) if (list_at + i < (unsigned)a.list) a.lists[q * a.list + list_at + i] = list[i];
 }
@@ -592,9 +676,9 @@ k_draw_rows(DrawArgs a, int64_t first) {
     __syncthreads();
     const unsigned found = grouped;
     if (found <= 2 * DRAW_FEW) {
-      // a group's turns are work for a thread each
-      const int turns = a.chunk_rows / 2048, turns_block = (turns + a.blocks - 1) / a.blocks, per_chunk = a.blocks * 256;
-      const unsigned items = found * turns_block;
+      // a group's turns and threads are work for a thread each
+      const int turns = a.chunk_rows / 2048, turns_block = (turns + a.blocks - 1) / a.blocks, width = 256 / a.merge, per_chunk = a.blocks * width;
+      const unsigned each = (unsigned)(turns_block * a.merge), items = found * each;
       for (unsigned i0 = 0; i0 < items; i0 += 4 * 1024) {  // four a thread on their way
         unsigned key[4][8];
         int column[4];
@@ -603,8 +687,9 @@ k_draw_rows(DrawArgs a, int64_t first) {
           const unsigned i = i0 + 1024 * j + tid;
           column[j] = -1;
           if (i < items) {
-            const int g = (int)near.groups[i / turns_block], chunk = g / per_chunk, block = (g - chunk * per_chunk) / 256, turn = block * turns_block + (int)(i % turns_block);
-            const int64_t c = (int64_t)chunk * a.chunk_rows + turn * 2048 + 8 * (g & 255);
+            const int g = (int)near.groups[i / each], chunk = g / per_chunk, block = (g - chunk * per_chunk) / width, part = (int)(i % each);
+            const int turn = block * turns_block + part / a.merge;
+            const int64_t c = (int64_t)chunk * a.chunk_rows + turn * 2048 + 8 * (g % width * a.merge + part % a.merge);
             if (turn < turns && c < min((int64_t)a.rows, (int64_t)(chunk + 1) * a.chunk_rows)) { column[j] = (int)c; row.keys((int)c, key[j]); }
           }
         }
@@ -640,7 +725,7 @@ k_draw_rows(DrawArgs a, int64_t first) {
     n = cuts ? a.listed[q] : 0;
     slowly = !draw_all(a, par) || draw_infinite(whole.best) || n > (unsigned)a.list;
     if (!slowly) {
-      for (unsigned i = tid; i < n; i += 1024) list[i] = a.lists[q * a.list + i];
+      if (n <= DRAW_LIST) for (unsigned i = tid; i < n; i += 1024) list[i] = a.lists[q * a.list + i];
       if (held) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) if (tid + 1024 * i < a.segments) near.mass[tid + 1024 * i] = a.mass[q * a.mass_pitch + tid + 1024 * i];
@@ -655,7 +740,8 @@ k_draw_rows(DrawArgs a, int64_t first) {
   }
   if (!slowly) {
     __syncthreads();
-    auto each = [&](auto f) { for (unsigned i = tid; i - tid < n; i += 1024) f(i < n ? list[i] : 0); };
+    const draw_u64* const far = a.lists + q * a.list;         // where the workgroup does not hold them
+    auto each = [&](auto f) { for (unsigned i = tid; i - tid < n; i += 1024) f(i < n ? (n <= DRAW_LIST ? list[i] : far[i]) : 0); };
     // top-k by counts, then top-p by weights
     for (int kind = few && (unsigned)par.top_k < n ? 0 : 1; kind < (cuts ? 2 : 1); ++kind) {
       draw_u64 want = (draw_u64)par.top_k;
@@ -825,7 +911,7 @@ extern "C" int mar_sample_rows(const mar_sampling* p, const void* scores, const 
   a.ids = ids; a.log_probs = log_probs; a.num_kept = num_kept; a.score_stride = p->score_stride; a.allowed_stride = allowed_stride;
   a.rows = (int32_t)p->num_rows; a.draws = p->num_draws; a.segments = L.segments;
   a.top_k = p->top_k; a.temperature = p->temperature; a.top_p = p->top_p; a.min_p = p->min_p;
-  a.chunks = L.chunks; a.chunk_rows = L.chunk_rows; a.blocks = L.blocks; a.groups = L.groups; a.list = L.list;
+  a.chunks = L.chunks; a.chunk_rows = L.chunk_rows; a.blocks = L.blocks; a.merge = L.merge; a.groups = L.groups; a.list = L.list;
   char* const ws = (char*)workspace;
   a.stats = (DrawChunk*)(ws + L.stats); a.maxima = (unsigned*)(ws + L.maxima); a.hist = (unsigned*)(ws + L.hist); a.hist_bits = L.hist_bits; a.range = (DrawRange*)(ws + L.range);
   a.totals = (draw_u64*)(ws + L.totals); a.kept = (unsigned*)(ws + L.kept); a.listed = (unsigned*)(ws + L.listed); a.undone = (unsigned*)(ws + L.undone); a.lists = (draw_u64*)(ws + L.lists);

@@ -45,12 +45,14 @@ __device__ __forceinline__ draw_u64 draw_place(unsigned key, unsigned id) { retu
 #define DRAW_TOP 3.402823466e38f    // the largest float
 #define DRAW_SEGMENT 512            // columns of a segment: a wave's eight a lane
 #define DRAW_SMALL (16 * 1024)      // rows that a workgroup holds in registers
-#define DRAW_BINS 2048              // of weights: 1/32 of a binary order of magnitude each; the last one holds all below 2^-64 too
+#define DRAW_BINS 2048              // of weights: 1/32 of a binary order of magnitude each, or less (draw_fine)
 #define DRAW_FEW 2048               // largest top-k whose rows are picked from groups' maxima
-#define DRAW_LIST 8192              // most rows a border is looked for among
+#define DRAW_LIST 8192              // rows of a border that a workgroup holds
 #define DRAW_LIST_CHUNK 2048        // of one chunk
 
-struct DrawChunk { unsigned best; float sum; };     // of a chunk: greatest key (0: no row counts), sum of weights relative to it (where no histogram gives it)
+// Of a chunk: greatest key (0: no row counts), complement of the least one (0: not looked for), sum of weights relative to the best (where no histogram
+// gives it).
+struct DrawChunk { unsigned best, low; float sum; };
 // Of a query, after the histogram: bins below `low` lie above top-p's border, bins above `high` below it; the sum of weights.
 struct DrawRange { int low, high; float sum; };
 
@@ -62,7 +64,7 @@ struct DrawArgs {
   int32_t rows, draws, segments;
   int32_t top_k; float temperature, top_p, min_p;
   int32_t chunks, chunk_rows;       // of a query; a multiple of 2,048 rows
-  int32_t blocks, groups;           // groups of rows a thread of the scan takes in a chunk, of a query in all
+  int32_t blocks, merge, groups;    // groups of rows a thread of the scan takes in a chunk, threads that share one, of a query in all
   int32_t list;                     // places in a query's list
   DrawChunk* stats;                 // [queries][chunks]
   unsigned* maxima;                 // [queries][groups]
@@ -383,8 +385,8 @@ template <typename E> __device__ __forceinline__ unsigned draw_bound(DrawShared&
   }
 }
 
-// Chunks: as many as fill the device some eight times, of 2,048 to 2^21 rows.  Blocks: groups enough for top-k's bound.
-struct DrawLayout { size_t stats, maxima, hist, range, totals, kept, listed, undone, lists, mass, bytes; int segments, chunks, chunk_rows, blocks, groups, list, hist_bits, mass_pitch; };
+// Chunks: as many as fill the device some eight times, of 2,048 to 2^21 rows.
+struct DrawLayout { size_t stats, maxima, hist, range, totals, kept, listed, undone, lists, mass, bytes; int segments, chunks, chunk_rows, blocks, merge, groups, list, hist_bits, mass_pitch; };
 static inline DrawLayout draw_layout(const mar_sampling* p) {
   DrawLayout L = {};
   if (p->num_rows <= DRAW_SMALL || p->num_queries == 0) { L.bytes = 256; return L; }
@@ -398,10 +400,24 @@ static inline DrawLayout draw_layout(const mar_sampling* p) {
   int64_t turns = (p->num_rows + 2048 * chunks - 1) / (2048 * chunks);
   L.chunk_rows = (int)(2048 * turns);
   L.chunks = (int)((p->num_rows + L.chunk_rows - 1) / L.chunk_rows);
+  // Groups: some 4,096 to 8,192, which stay in registers where they are looked through, and enough for a top-k of up to 2,048; a chunk's turns by
+  // blocks where there are too few, neighbouring threads merged where there are too many (5 x 1,000,003, top-k 50: 80 us with 62,720, 26 with
+  // 7,840), up to 256 rows (1 x 20,000,000, top-k 1,000: 210 us with 312 rows, 273 with 2,496).  A large top-k has the groups that reach its bound looked through again, and wants them smaller: at most eight turns (100 x 1,000,003,
+  // top-k 2,000: 248 -> 173 us).
   int64_t blocks = 4096 / (256 * L.chunks);
+  if (p->top_k > 512) {
+    const int64_t more = 16384 / (256 * L.chunks);
+    blocks = blocks > more ? blocks : (more < turns / 8 ? more : turns / 8);
+  }
   L.blocks = (int)(blocks < 1 ? 1 : (blocks > turns ? turns : blocks));
-  L.groups = L.chunks * L.blocks * 256;
-  L.list = (int)(p->num_rows / 16 < DRAW_LIST ? p->num_rows / 16 : DRAW_LIST);
+  L.merge = 1;
+  const int64_t group_rows = 8 * ((turns + L.blocks - 1) / L.blocks);
+  while (L.merge < 16 && 2 * L.merge * group_rows <= 256 && L.chunks * L.blocks * (256 / (2 * L.merge)) >= (p->top_k > 512 ? 16384 : 4096)) L.merge *= 2;
+  L.groups = L.chunks * L.blocks * (256 / L.merge);
+  // Of normal scores the border's range, a bin or two, holds up to 1 in 120 rows with bins as fine as they allow, more with 32 a binary order of
+  // magnitude (rows far below all others): 1 / 58 over the deviation.  A workgroup holds 8,192 of them, the rest stays in memory (100 x 1,000,003,
+  // deviation 0.67: 3.5 ms where all had to fit a workgroup, 0.29).
+  L.list = (int)(p->num_rows / 16 < DRAW_LIST ? p->num_rows / 16 : (p->num_rows / 32 < DRAW_LIST ? DRAW_LIST : p->num_rows / 32));
   L.stats = take(Q * L.chunks * sizeof(DrawChunk));
   L.maxima = take(Q * L.groups * 4);
   L.hist = take(Q * L.chunks * DRAW_BINS * 4);

@@ -115,3 +115,21 @@ def test_equal_rows_at_the_border_of_top_p(V, equal):
     for top_p in (0.4999, 0.75, 0.999):
         check(s, uniforms_of(equal, 3, 8), top_p=top_p)
     check(s, uniforms_of(equal, 3, 8), top_p=0.75, temperature=0.9, min_p=0.5 / equal)
+
+
+@pytest.mark.parametrize("equal", (2048, 2049, 5000, 8193, 60_000, 124_999, 125_001))
+def test_more_equal_rows_than_a_workgroup_holds(equal):
+    """Neighbours, so that one chunk alone has more than its list; from 125,000 on, more than the query's list in memory."""
+    V = 4_000_000
+    s = torch.full((1, V), -30.0, device=DEV)
+    s[0, 1_000_001:1_000_001 + equal] = 0.5
+    s[0, 3_999_999] = 0.5 + float(np.log(equal))
+    for top_p in (0.4999, 0.75):
+        check(s, uniforms_of(equal, 1, 5), top_p=top_p)
+    check(s, uniforms_of(equal, 1, 5), top_p=0.75, min_p=0.5 / equal)
+
+
+@pytest.mark.parametrize("spread", (0.1, 0.3, 1.0))
+def test_flat_scores_over_many_rows(spread):
+    for dt in (torch.float32, torch.bfloat16):
+        check(scores_of(13, 1, 3_000_000, dt, spread=spread), uniforms_of(13, 1, 5), top_p=0.6)

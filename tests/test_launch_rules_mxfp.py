@@ -48,15 +48,16 @@ def test_draws(tmp_path):
     out = _run(tmp_path, "mar_sample_dev.h", """
   long taken = 0, bad = 0;
   for (int64_t rows : {(int64_t)DRAW_SMALL + 1, (int64_t)20000, (int64_t)131072, (int64_t)1000003, (int64_t)50000000, MAR_SOFTMAX_MAX_ROWS - 2047, MAR_SOFTMAX_MAX_ROWS})
-    for (int queries : {1, 2, 7, 64, 100, 1000, 2047, 2048, 2049, 100000, MAR_SOFTMAX_MAX_QUERIES}) {
+    for (int queries : {1, 2, 7, 64, 100, 1000, 2047, 2048, 2049, 100000, MAR_SOFTMAX_MAX_QUERIES}) for (int top_k : {0, 512, 513, 2000000}) {
       mar_sampling p = {};
-      p.num_rows = rows; p.num_queries = queries;
+      p.num_rows = rows; p.num_queries = queries; p.top_k = top_k;
       const DrawLayout L = draw_layout(&p);
       ++taken;
       if (L.chunks < 1 || L.chunks > 256 || (int64_t)L.chunks * L.chunk_rows < rows || (int64_t)(L.chunks - 1) * L.chunk_rows >= rows) ++bad;
       if (L.chunk_rows % 2048 || L.chunk_rows > 1 << 21 || L.hist_bits < 10 || (int64_t)L.chunk_rows << L.hist_bits >= 1ll << 32) ++bad;
-      if (L.blocks < 1 || L.blocks > L.chunk_rows / 2048 || L.groups != L.chunks * L.blocks * 256) ++bad;
-      if (L.list < 1000 || L.list > DRAW_LIST || (int64_t)L.segments * DRAW_SEGMENT < rows || L.mass_pitch % 16 || L.mass_pitch < L.segments) ++bad;
+      if (L.blocks < 1 || L.blocks > L.chunk_rows / 2048 || L.groups != L.chunks * L.blocks * (256 / L.merge)) ++bad;
+      if (L.merge < 1 || L.merge & (L.merge - 1) || L.merge > 16 || (L.groups < 4096 && L.merge > 1)) ++bad;
+      if (L.list < 1000 || (L.list > DRAW_LIST && L.list > rows / 32) || (int64_t)L.segments * DRAW_SEGMENT < rows || L.mass_pitch % 16 || L.mass_pitch < L.segments) ++bad;
       if (L.bytes % 256 || L.mass + (size_t)queries * L.mass_pitch * 8 > L.bytes) ++bad;
       int64_t at = 0;
       sm_launches((int64_t)queries * L.chunks, 256, [&](int64_t first, unsigned n) { if (first != at || (int64_t)n * 256 >= 1ll << 32) ++bad; at = first + n; });
@@ -64,4 +65,4 @@ def test_draws(tmp_path):
     }
   for (int64_t rows : {(int64_t)1, (int64_t)DRAW_SMALL}) { mar_sampling p = {}; p.num_rows = rows; p.num_queries = 9; if (draw_layout(&p).bytes != 256) ++bad; }
   printf("%ld %ld", taken, bad);""")
-    assert int(out[0]) == 77 and out[1] == "0", out
+    assert int(out[0]) == 77 * 4 and out[1] == "0", out
