@@ -333,7 +333,8 @@ typedef struct mar_mxfp {
   int64_t codes_stride, scales_stride;                              /* of the table, in bytes           */
   int64_t query_stride;         /* elements (MAR_DTYPE_MXFP4: bytes) from one query to the next         */
   int64_t query_scales_stride;  /* bytes; MAR_DTYPE_MXFP4 alone                                         */
-  int64_t score_stride;         /* elements from one query's scores to the next's, at least num_rows    */
+  int64_t score_stride;         /* elements from one query's scores to the next's, at least num_rows;
+                                   large results are written fastest where it is a multiple of 128 bytes */
   int32_t num_queries;          /* 0 .. MAR_SOFTMAX_MAX_QUERIES                                         */
   int32_t dim;                  /* 1 .. MAR_MAX_DIM                                                     */
   int32_t dtype;                /* of the queries: MAR_DTYPE_*                                          */

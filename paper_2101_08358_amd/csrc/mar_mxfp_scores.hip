@@ -215,7 +215,9 @@ __device__ __forceinline__ void mx_tile(const char* image, int lane, const row_u
   mx_steps<0, NK, NS, RT>(image, lane, mx_operand<NK, NS>(image, lane, 0), qs, w, ws, acc);
 }
 
-// Scores of 32 queries from `q0` on and a lane's RT neighbouring rows: a wave instruction writes two queries' 32 RT scores.
+// Scores of 32 queries from `q0` on and a lane's RT neighbouring rows: a wave instruction writes two queries' 32 RT scores.  Where these do not begin
+// with lines of 128 bytes a large result takes up to 1.4 times as long (325 x 679,723 x 27 in fp32: 183 us, rows at multiples of 64 bytes 212, at
+// odd places 261; neighbouring stripes on one die do not change that): a lane holds one row for all queries, whose rows lie differently.
 template <int TYPE, int RT>
 __device__ __forceinline__ void mx_store(const MxArgs& a, int64_t q0, int row0, int h, bool whole, const mx_f16 (&acc)[RT]) {
   typedef typename RowType<TYPE>::T T;
