@@ -133,3 +133,25 @@ def test_more_equal_rows_than_a_workgroup_holds(equal):
 def test_flat_scores_over_many_rows(spread):
     for dt in (torch.float32, torch.bfloat16):
         check(scores_of(13, 1, 3_000_000, dt, spread=spread), uniforms_of(13, 1, 5), top_p=0.6)
+
+
+@pytest.mark.parametrize("top_k,top_p", ((600, 1.0), (1500, 0.9), (2048, 0.5), (40, 0.9)))
+def test_many_queries_go_other_ways_to_the_same_rows(top_k, top_p):
+    """Chunks and groups of rows follow the number of queries, what is drawn does not."""
+    s, u = scores_of(17, 300, 200_003, torch.float32, spread=2.0), uniforms_of(17, 300, 3)
+    got = sample(s, u, top_k=top_k, top_p=top_p)
+    for first in (0, 151, 297):
+        want = check(s[first:first + 3], u[first:first + 3], top_k=top_k, top_p=top_p)
+        assert torch.equal(got[0][first:first + 3].cpu(), torch.as_tensor(want[0]).cpu())
+        assert torch.equal(got[2][first:first + 3].cpu(), torch.as_tensor(want[2]).cpu())
+
+
+@pytest.mark.parametrize("tname", TYPES)
+def test_equal_scores_of_a_workgroup(tname):
+    """More equal rows than the list of those that reach top-k's bound; rows that do not count among them."""
+    V = 16_384
+    g = np.random.default_rng(8)
+    s = torch.from_numpy(np.stack((np.full(V, 0.25), np.where(g.random(V) < 0.3, -np.inf, 0.25), np.where(g.random(V) < 0.02, 2.0, 0.25), g.integers(0, 40, V) * 0.125))).to(TYPES[tname][0]).to(DEV)
+    u = uniforms_of(21, 4, 6)
+    for f in (dict(top_k=129), dict(top_k=300, top_p=0.9), dict(top_k=2000), dict(top_k=16_383, top_p=0.5), dict(top_k=12_000, min_p=0.5), dict(top_p=0.7), dict(top_p=0.3, min_p=0.9)):
+        check(s, u, **f)
