@@ -175,3 +175,28 @@ def test_offsets_beyond_32_bits():
     ws = torch.empty(mar.mar_mxfp_scores_workspace_bytes(p), dtype=torch.uint8, device=DEV)
     mar.mar_mxfp_scores(p, x, None, c, s, out, ws, ws.numel())
     check(torch.as_strided(out, (T, V), (far, 1)), q.double().cpu().numpy(), mu.values(codes, scales, dim), "bf16", "bf16", 1.0)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dim", (27, 64, 100, 190, 256, 300, 383, 400))
+@pytest.mark.parametrize("few", (False, True))
+def test_scores_of_large_tables(few, dim, kind):
+    """Sizes from which a lane holds several rows, checked at both ends of the table and at rows between."""
+    if few: T, V = 19, 70_001
+    elif kind != "mxfp4": T, V = 515, 31_003
+    else: T, V = (250, 263_001) if dim <= 256 else (70, 700_003)
+    g = np.random.default_rng(T + dim)
+    codes, scales = table(g, V, dim)
+    c, s = torch.from_numpy(codes).to(DEV), torch.from_numpy(scales).to(DEV)
+    out = ("fp32", "bf16", "fp16")[dim % 3]
+    at = np.unique(np.concatenate((np.arange(300), g.integers(0, V, 1500), np.arange(V - 700, V))))
+    w = mu.values(codes[at], scales[at], dim)
+    if kind == "mxfp4":
+        qc, qs = table(g, T, dim)
+        got = scores(torch.from_numpy(qc).to(DEV), c, s, dim, kind, out, 0.5, dim % 2, dim % 2, torch.from_numpy(qs).to(DEV))
+        q = mu.values(qc, qs, dim)
+    else:
+        x = torch.from_numpy(g.standard_normal((T, dim)) * np.exp2(g.integers(-6, 3, (T, 1)))).to(TYPES[kind][0])
+        got = scores(x.to(DEV), c, s, dim, kind, out, 0.5, dim % 2, dim % 2)
+        q = x.double().numpy()
+    check(got[:, torch.from_numpy(at).to(DEV)], q, w, kind, out, 0.5)
