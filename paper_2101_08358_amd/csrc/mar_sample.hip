@@ -1,8 +1,8 @@
 // Rows drawn from scores with temperature, top-k, top-p and min-p (gfx950).
 //
 // A row's place in the order (score descending, id ascending) is one number, so that every filter is a cut: rows whose place is not below it
-// are kept.  Weights are integers W = round(2^n exp((s - max) / temperature)), n such that their sum lies below 2^61: sums are exact
-// in any order, and a border (top-p's, a draw's) falls where the integers say, whatever way found it.
+// are kept.  Weights are integers W = round(2^n exp((s - max) / temperature)), n such that the sum of those that top-k leaves lies below
+// 2^61 (their own sum in fp32 says which, whatever way a query goes): sums are exact in any order, and a border (top-p's, a draw's) falls where the integers say, whatever way found it.
 //
 // Up to 16,384 rows (k_draw_small): a workgroup a query holds them in registers (one query of 4,000 to 16,000 rows, no filter: 10 us; by the kernels
 // below 18 to 20; 1,000 queries of 16,000 rows: 35 and 72).  More:
@@ -102,48 +102,49 @@ __device__ __forceinline__ void draw_rows(const DrawArgs& a, int64_t q, const Dr
   }
 }
 
-// Up to 256 rows, with all that top-k leaves among them: four threads a row compare it with all others.  Called by 1,024 threads.
-__device__ __forceinline__ void draw_short(const DrawArgs& a, int64_t q, DrawShort& lds, unsigned n, const DrawParams& par, const DrawWeights& w) {
+// Up to 256 rows, with all that top-k (at least 1) leaves among them: four threads a row compare it with all others, once for the rank, which
+// puts top-k's rows in order for their weights and sums, once for the place by id among those kept.  Called by 1,024 threads.
+__device__ __forceinline__ void draw_short(const DrawArgs& a, int64_t q, DrawShort& lds, unsigned n, const DrawParams& par, unsigned best) {
   const unsigned tid = threadIdx.x, r = tid >> 2, part = tid & 3, padded = (n + 15) & ~15u;
-  draw_u64 mine = 0;
-  if (tid >= n && tid < padded) lds.row[tid] = {0, 0};     // comes after all others
-  if (tid < n) lds.row[tid].weight = w.of((unsigned)(lds.row[tid].place >> 32));
+  if (tid >= n && tid < padded) lds.row[tid].place = 0;    // comes after all others
   __syncthreads();
-  const bool has = r < n;
-  draw_u64 weight = 0;
-  if (has) { mine = lds.row[r].place; weight = lds.row[r].weight; }
+  draw_u64 mine = r < n ? lds.row[r].place : 0;
   // sums over the four threads of a row
   auto joined = [](auto v) { v += draw_moved<0xB1, 0xf>(v); return v + draw_moved<0x4E, 0xf>(v); };       // lanes 1 0 3 2, then 2 3 0 1
   unsigned rank = 0;
-  draw_u64 before = 0;
 #pragma unroll 4
-  for (unsigned i = part; i < padded; i += 4) {
-    const auto other = lds.row[i];
-    const bool better = other.place > mine;
-    rank += better;
-    before += better ? other.weight : 0;
-  }
+  for (unsigned i = part; i < padded; i += 4) rank += lds.row[i].place > mine;
   rank = joined(rank);
-  before = joined(before);
-  bool in = has && (par.top_k == 0 || rank < (unsigned)par.top_k);
+  const bool top = part == 0 && r < n && rank < (unsigned)par.top_k;
+  const float weighs = top ? __builtin_amdgcn_exp2f(-draw_depth(draw_score(best), draw_score((unsigned)(mine >> 32)), draw_depth_scale(par))) : 0.f;
+  const DrawWeights w = draw_weights(best, par, draw_sum(weighs, (float*)lds.slots));  // behind its barriers the rows have been read
+  if (top) lds.row[rank].place = mine;
+  __syncthreads();
+  const unsigned m = min(n, (unsigned)par.top_k), padded_m = (m + 15) & ~15u;
+  bool in = tid < m;                                       // a thread a row, by rank
+  const draw_u64 place = in ? lds.row[tid].place : 0, weight = in ? w.of((unsigned)(place >> 32)) : 0;
   if (par.top_p < 2.f) {                                   // uniform
-    const draw_u64 want = draw_share_up(par.top_p, draw_sum(in && part == 0 ? weight : 0, lds.slots));
+    draw_u64 sum;
+    const draw_u64 before = draw_prefix(weight, lds.slots, sum), want = draw_share_up(par.top_p, sum);
     in = in && before < (want ? want : 1);
   }
   in = in && weight >= w.least(par.min_p);
   if (a.num_kept) {
-    const unsigned kept = draw_sum(in && part == 0 ? 1u : 0u, (unsigned*)lds.slots);
+    const unsigned kept = draw_sum(in ? 1u : 0u, (unsigned*)lds.slots);
     if (tid == 0) a.num_kept[q] = (int)kept;
   }
+  const draw_u64 total = draw_sum(in ? weight : 0, lds.slots);
+  const unsigned count = draw_sum(in && weight ? 1u : 0u, (unsigned*)lds.slots);
+  if (tid < padded_m) lds.row[tid] = {in ? place : 0, in ? weight : 0};
   __syncthreads();
-  if (has && part == 0 && !in) lds.row[r] = {0, 0};
-  const draw_u64 total = draw_sum(in && part == 0 ? weight : 0, lds.slots);       // its barriers order the list
   // by id: places of lesser ids have greater lower halves
+  mine = r < m ? lds.row[r].place : 0;
+  const draw_u64 own = r < m ? lds.row[r].weight : 0;
   const unsigned id = ~(unsigned)mine;
   draw_u64 start = 0;
   unsigned at = 0;
 #pragma unroll 4
-  for (unsigned i = part; i < padded; i += 4) {
+  for (unsigned i = part; i < padded_m; i += 4) {
     const auto other = lds.row[i];
     const bool ahead = other.weight != 0 && ~(unsigned)other.place < id;
     at += ahead;
@@ -151,8 +152,7 @@ __device__ __forceinline__ void draw_short(const DrawArgs& a, int64_t q, DrawSho
   }
   at = joined(at);
   start = joined(start);
-  const unsigned count = draw_sum(in && weight && part == 0 ? 1u : 0u, (unsigned*)lds.slots);
-  if (in && weight && part == 0) {
+  if (own && part == 0) {
     lds.start[at] = start; lds.id[at] = id;
     lds.log_prob[at] = w.log_prob((unsigned)(mine >> 32), w.log_sum(total));
   }
@@ -242,7 +242,7 @@ k_draw_small(DrawArgs a, int64_t first) {
         if (n < DRAW_SHORT) lds.list.row[n].place = place(b, e);
       }
     __syncthreads();
-    if (listed <= DRAW_SHORT) { draw_short(a, q, lds.list, listed, par, draw_weights(best, par, 256.f)); return; }
+    if (listed <= DRAW_SHORT) { draw_short(a, q, lds.list, listed, par, best); return; }
   }
   const float c = draw_depth_scale(par), top = draw_score(best);
   DrawWeights w = {};
@@ -289,25 +289,18 @@ k_draw_small(DrawArgs a, int64_t first) {
       for (unsigned i = tid; i - tid < n; i += 1024) { const draw_u64 p = i < n ? list[i] : 0; f(p, [&] { return w.of((unsigned)(p >> 32)); }); }
     }, [&](unsigned k) { return w.of(k); });
   }
-  if (!found_cut) {
-    float approx = 0.f;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) approx += __builtin_amdgcn_exp2f(-draw_depth(top, v[b][e], c));
-    w = draw_weights(best, par, draw_sum(approx, (float*)slots));
-  }
+  bool ranks = false;                                      // top-k leaves rows out
   if constexpr (CUTS) if (par.top_k > 0 && par.top_k < a.rows) {       // uniform
-    // larger top-k: a bound among all rows, and everything else concerns the rows that reach it (16,000 rows, top-k 1,000, top-p 0.9: 28 us; by
-    // digits over all rows, as below, 53; 1,000 queries: 114 and 218)
-    const unsigned k = (unsigned)par.top_k;
     unsigned count = 0;
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int e = 0; e < 8; ++e) count += v[b][e] > -__builtin_inff();
-    count = draw_sum(count, (unsigned*)slots);
-    if (k < count) {
+    ranks = (unsigned)par.top_k < draw_sum(count, (unsigned*)slots);
+    // larger top-k: a bound among all rows, and everything else concerns the rows that reach it (16,000 rows, top-k 1,000, top-p 0.9: 28 us; by
+    // digits over all rows, as below, 53; 1,000 queries: 114 and 218)
+    if (ranks) {
+      const unsigned k = (unsigned)par.top_k;
       const unsigned bound = draw_bound(lds.border, k, [&](auto f) {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -333,10 +326,14 @@ k_draw_small(DrawArgs a, int64_t first) {
       if (found_cut) {
         auto each = [&](auto f) { for (unsigned i = tid; i - tid < n; i += 1024) f(i < n ? held.list[i] : 0); };
         cut = (draw_u64)bound << 32;
-        for (int kind = k < n ? 0 : 1; kind < (par.top_p < 2.f ? 2 : 1); ++kind) {         // by counts, then by weights
+        for (int kind = k < n ? 0 : 1; kind < 2; ++kind) { // by counts, then by weights
           draw_u64 want = k;
           const draw_u64 last = cut;
           if (kind == 1) {
+            float approx = 0.f;
+            each([&](draw_u64 p) { approx += p >= last ? __builtin_amdgcn_exp2f(-draw_depth(top, draw_score((unsigned)(p >> 32)), c)) : 0.f; });
+            w = draw_weights(best, par, draw_sum(approx, (float*)slots));
+            if (par.top_p >= 2.f) break;
             draw_u64 sum = 0;
             each([&](draw_u64 p) { sum += p >= last ? w.of((unsigned)(p >> 32)) : 0; });
             want = draw_share_up(par.top_p, draw_sum(sum, slots));
@@ -349,7 +346,15 @@ k_draw_small(DrawArgs a, int64_t first) {
       }
     }
   }
-  if constexpr (CUTS) if (!found_cut && ((par.top_k > 0 && par.top_k < a.rows) || par.top_p < 2.f)) {       // uniform
+  if (!found_cut && !ranks) {
+    float approx = 0.f;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) approx += __builtin_amdgcn_exp2f(-draw_depth(top, v[b][e], c));
+    w = draw_weights(best, par, draw_sum(approx, (float*)slots));
+  }
+  if constexpr (CUTS) if (!found_cut && (ranks || par.top_p < 2.f)) {       // uniform
     // through LDS: loops over the rows take a sixteenth of the code, and no registers beside the weights'
     struct Eight { float v[8]; };
 #pragma unroll
@@ -359,12 +364,12 @@ k_draw_small(DrawArgs a, int64_t first) {
 #pragma unroll 2
       for (int i = tid; i < DRAW_SMALL; i += 1024) f(draw_place(draw_key(held.score[i]), (unsigned)i));
     };
-    if (par.top_k > 0 && par.top_k < a.rows) {
-      unsigned count = 0;
-      each([&](draw_u64 place) { count += place != 0; });
-      count = draw_sum(count, (unsigned*)slots);
-      if ((unsigned)par.top_k < count) cut = draw_border<true>(lds.border, a.rows, (draw_u64)par.top_k, 0, [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); },
-                                                               [](unsigned) { return draw_one(); });
+    if (ranks) {
+      cut = draw_border<true>(lds.border, a.rows, (draw_u64)par.top_k, 0, [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); },
+                              [](unsigned) { return draw_one(); });
+      float approx = 0.f;
+      each([&](draw_u64 place) { approx += place >= cut ? __builtin_amdgcn_exp2f(-draw_depth(top, draw_score((unsigned)(place >> 32)), c)) : 0.f; });
+      w = draw_weights(best, par, draw_sum(approx, (float*)slots));
     }
     if (par.top_p < 2.f) {
       draw_u64 all = 0;
@@ -650,7 +655,7 @@ k_draw_rows(DrawArgs a, int64_t first) {
   if (tid == 0) a.undone[q] = 0;
   if (whole.best == 0) { draw_nothing<TYPE>(a, q); return; }         // uniform, like all conditions that end in a return or a barrier
   const bool few = draw_few(a, par), cuts = par.top_p < 2.f;
-  const DrawWeights w = draw_weights(whole.best, par, few ? (float)DRAW_LIST : (draw_all(a, par) && cuts ? a.range[q].sum : whole.sum));
+  DrawWeights w = draw_weights(whole.best, par, draw_all(a, par) && cuts ? a.range[q].sum : whole.sum);       // few: anew
   const bool held = a.segments <= 2048;                    // the segments' sums fit LDS
   draw_u64* mass = held ? near.mass : a.mass + q * a.mass_pitch;
   draw_u64 cut = 1, all = 0, above = 0;                    // of the listed rows; sums of weights: of all rows for top-p, of those above the list
@@ -717,7 +722,7 @@ k_draw_rows(DrawArgs a, int64_t first) {
     if (!slowly && n <= DRAW_SHORT) {
       if (tid < (int)n) lds.few.row[tid].place = list[tid];
       __syncthreads();
-      draw_short(a, q, lds.few, n, par, w);
+      draw_short(a, q, lds.few, n, par, whole.best);
       return;
     }
     if (!slowly) for (int s = tid; s < a.segments; s += 1024) mass[s] = 0;
@@ -743,10 +748,17 @@ k_draw_rows(DrawArgs a, int64_t first) {
     const draw_u64* const far = a.lists + q * a.list;         // where the workgroup does not hold them
     auto each = [&](auto f) { for (unsigned i = tid; i - tid < n; i += 1024) f(i < n ? (n <= DRAW_LIST ? list[i] : far[i]) : 0); };
     // top-k by counts, then top-p by weights
-    for (int kind = few && (unsigned)par.top_k < n ? 0 : 1; kind < (cuts ? 2 : 1); ++kind) {
+    for (int kind = few && (unsigned)par.top_k < n ? 0 : 1; kind < 2; ++kind) {
       draw_u64 want = (draw_u64)par.top_k;
       const draw_u64 last = cut;
       if (kind == 1) {
+        if (few) {
+          const float top = draw_score(whole.best), c = draw_depth_scale(par);
+          float approx = 0.f;
+          each([&](draw_u64 place) { approx += place >= last && place ? __builtin_amdgcn_exp2f(-draw_depth(top, draw_score((unsigned)(place >> 32)), c)) : 0.f; });
+          w = draw_weights(whole.best, par, draw_sum(approx, (float*)lds.border.slots));
+        }
+        if (!cuts) break;
         draw_u64 sum = 0;
         each([&](draw_u64 place) { sum += place >= last ? w.of((unsigned)(place >> 32)) : 0; });
         sum = draw_sum(sum, lds.border.slots);
@@ -805,13 +817,13 @@ k_draw_slowly(DrawArgs a, int64_t first) {
   };
   auto ones = [&](auto f) { each([&](draw_u64 place) { f(place, draw_one); }); };
   const float top = draw_score(best), c = draw_depth_scale(par);
-  float approx = 0.f;
-  each([&](draw_u64 place) { if (place) approx += __builtin_amdgcn_exp2f(-draw_depth(top, draw_score((unsigned)(place >> 32)), c)); });
-  const DrawWeights w = draw_weights(best, par, draw_sum(approx, (float*)lds.slots));
   draw_u64 cut = 1;
   unsigned count = 0;
   if (par.top_k > 0) { each([&](draw_u64 place) { count += place != 0; }); count = draw_sum(count, (unsigned*)lds.slots); }
   if (par.top_k > 0 && (unsigned)par.top_k < count) cut = draw_border<false>(lds, a.rows, (draw_u64)par.top_k, 0, ones, [](unsigned) { return draw_one(); });
+  float approx = 0.f;
+  each([&](draw_u64 place) { if (place >= cut) approx += __builtin_amdgcn_exp2f(-draw_depth(top, draw_score((unsigned)(place >> 32)), c)); });
+  const DrawWeights w = draw_weights(best, par, draw_sum(approx, (float*)lds.slots));
   if (par.top_p < 2.f) {
     draw_u64 all = 0;
     each([&](draw_u64 place) { if (place >= cut) all += w.of((unsigned)(place >> 32)); });

@@ -144,7 +144,8 @@ struct DrawWeights {
     return min_p >= 1.f ? best : (min_p > 0.f ? draw_share_up(min_p, best) : 0);
   }
 };
-// approx: sum of weights relative to the best one, in fp32: the integers' sum lies below 2^61 and a little more.
+// approx: sum of weights relative to the best one, in fp32: the integers' sum
+// lies between 2^60 and 2^61, or a little more.
 __device__ __forceinline__ DrawWeights draw_weights(unsigned best, const DrawParams& p, float approx) {
   return {(double)draw_score(best), p.inv_temperature, p.inv_temperature * 1.4426950408889634, 2 + ilogbf(fmaxf(approx, 1.f))};
 }
