@@ -52,9 +52,9 @@ __device__ __forceinline__ float draw_fine(const DrawArgs& a, int64_t q, float c
   return fine;
 }
 
-// The draws of a query: rows with place >= cut and weight >= least; mass: the segments' sums (LDS or memory), replaced by those before them.
+// The draws of a query: rows with place >= cut that score min-p's floor or more; mass: the segments' sums (LDS or memory), replaced by those before them.
 template <int TYPE>
-__device__ __forceinline__ void draw_rows(const DrawArgs& a, int64_t q, const DrawRow<TYPE>& row, const DrawWeights& w, draw_u64 cut, draw_u64 least, draw_u64* mass,
+__device__ __forceinline__ void draw_rows(const DrawArgs& a, int64_t q, const DrawRow<TYPE>& row, const DrawWeights& w, draw_u64 cut, float floor, draw_u64* mass,
                                           draw_u64* slots) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, threads = blockDim.x;
   draw_u64 total = 0;
@@ -85,8 +85,7 @@ __device__ __forceinline__ void draw_rows(const DrawArgs& a, int64_t q, const Dr
     draw_u64 each[8], sum = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      each[e] = key[e] != 0 && draw_place(key[e], (unsigned)c + e) >= cut ? w.of(key[e]) : 0;
-      if (each[e] < least) each[e] = 0;
+      each[e] = key[e] != 0 && draw_place(key[e], (unsigned)c + e) >= cut && draw_score(key[e]) >= floor ? w.of(key[e]) : 0;
       sum += each[e];
     }
     const draw_u64 run = draw_wave_prefix(sum), start = run - sum;
@@ -104,7 +103,7 @@ __device__ __forceinline__ void draw_rows(const DrawArgs& a, int64_t q, const Dr
 
 // Up to 256 rows, with all that top-k (at least 1) leaves among them: four threads a row compare it with all others, once for the rank, which
 // puts top-k's rows in order for their weights and sums, once for the place by id among those kept.  Called by 1,024 threads.
-__device__ __forceinline__ void draw_short(const DrawArgs& a, int64_t q, DrawShort& lds, unsigned n, const DrawParams& par, unsigned best) {
+__device__ __forceinline__ void draw_short(const DrawArgs& a, int64_t q, DrawShort& lds, unsigned n, const DrawParams& par, unsigned best, double drop) {
   const unsigned tid = threadIdx.x, r = tid >> 2, part = tid & 3, padded = (n + 15) & ~15u;
   if (tid >= n && tid < padded) lds.row[tid].place = 0;    // comes after all others
   __syncthreads();
@@ -128,7 +127,7 @@ __device__ __forceinline__ void draw_short(const DrawArgs& a, int64_t q, DrawSho
     const draw_u64 before = draw_prefix(weight, lds.slots, sum), want = draw_share_up(par.top_p, sum);
     in = in && before < (want ? want : 1);
   }
-  in = in && weight >= w.least(par.min_p);
+  in = in && draw_score((unsigned)(place >> 32)) >= w.floor(drop);
   if (a.num_kept) {
     const unsigned kept = draw_sum(in ? 1u : 0u, (unsigned*)lds.slots);
     if (tid == 0) a.num_kept[q] = (int)kept;
@@ -211,6 +210,7 @@ k_draw_small(DrawArgs a, int64_t first) {
   __shared__ draw_u64 slots[16];
   __shared__ draw_u64 starts[32];
   __shared__ unsigned listed, reached;
+  __shared__ double drop;
   __shared__ int ends[2];
   const int64_t q = first + blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -223,9 +223,12 @@ k_draw_small(DrawArgs a, int64_t first) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[b][e] = -__builtin_inff();
     if (8192 * b + 8 * tid < a.rows) row.scores_of(8192 * b + 8 * tid, v[b]);
+  }
+  if (wave == 0) drop = draw_drop(par);
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
 #pragma unroll
     for (int e = 0; e < 8; ++e) mine = fmaxf(mine, v[b][e]);
-  }
   const unsigned best = draw_reduce(draw_key(mine), (unsigned*)slots, DrawMax());
   if (best == 0) { draw_nothing<TYPE>(a, q); return; }     // uniform
   auto place = [&](int b, int e) { return draw_place(draw_key(v[b][e]), (unsigned)(8192 * b + 8 * tid + e)); };
@@ -242,7 +245,7 @@ k_draw_small(DrawArgs a, int64_t first) {
         if (n < DRAW_SHORT) lds.list.row[n].place = place(b, e);
       }
     __syncthreads();
-    if (listed <= DRAW_SHORT) { draw_short(a, q, lds.list, listed, par, best); return; }
+    if (listed <= DRAW_SHORT) { draw_short(a, q, lds.list, listed, par, best, drop); return; }
   }
   const float c = draw_depth_scale(par), top = draw_score(best);
   DrawWeights w = {};
@@ -386,7 +389,7 @@ k_draw_small(DrawArgs a, int64_t first) {
       for (int e = 0; e < 8; ++e) v[b][e] = back.v[e];
     }
   }
-  const draw_u64 least = w.least(par.min_p);
+  const float floor = w.floor(drop);
   unsigned kept = 0;
   draw_u64 sum[2] = {0, 0}, run[2];
 #pragma unroll
@@ -394,7 +397,7 @@ k_draw_small(DrawArgs a, int64_t first) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const draw_u64 x = w.of_score(v[b][e]);
-      const bool in = (CUTS ? place(b, e) >= cut : v[b][e] > -__builtin_inff()) && x >= least;
+      const bool in = (CUTS ? place(b, e) >= cut : v[b][e] > -__builtin_inff()) && v[b][e] >= floor;
       kept += in;
       sum[b] += in ? x : 0;
     }
@@ -426,7 +429,7 @@ k_draw_small(DrawArgs a, int64_t first) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const draw_u64 x = w.of_score(score[e]);
-      const bool in = (CUTS ? draw_place(draw_key(score[e]), (unsigned)(8 * at + e)) >= cut : score[e] > -__builtin_inff()) && x >= least;
+      const bool in = (CUTS ? draw_place(draw_key(score[e]), (unsigned)(8 * at + e)) >= cut : score[e] > -__builtin_inff()) && score[e] >= floor;
       sum += in ? x : 0;
       if (column < 0 && sum > target) { column = e; found = score[e]; }
     }
@@ -562,25 +565,27 @@ __global__ void __launch_bounds__(256)
 k_draw_weigh(DrawArgs a, int64_t first) {
   __shared__ draw_u64 slots[16], list[DRAW_LIST_CHUNK];
   __shared__ unsigned listed, list_at;
+  __shared__ double drop;
   const int64_t unit = first + blockIdx.x, q = unit / a.chunks;
   const int chunk = (int)(unit - q * a.chunks), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (threadIdx.x == 0) listed = 0;
   const DrawParams par = draw_params(a, q);
   if (draw_few(a, par) || !draw_all(a, par)) return;
+  if (wave == 0) drop = draw_drop(par);
   const DrawRow<TYPE> row(a, q);
   const float c = draw_depth_scale(par);
   const DrawWhole whole = draw_whole(a, q, c, slots);
   if (whole.best == 0 || draw_infinite(whole.best)) return;
   const DrawRange range = par.top_p < 2.f ? a.range[q] : DrawRange{0, 0, 0.f};
   const DrawWeights w = draw_weights(whole.best, par, par.top_p < 2.f ? range.sum : whole.sum);
-  const draw_u64 least = w.least(par.min_p);
+  const float floor = w.floor(drop);
   // bins by their depth, as the histogram counts them
   const float top = draw_score(whole.best), scale = par.top_p < 2.f ? c * draw_fine(a, q, c, whole.best, slots) : 0.f, low = (float)range.low, high = range.high < DRAW_BINS - 1 ? range.high + 1.f : __builtin_inff();
   const int begin = chunk * a.chunk_rows, end = (int)min((int64_t)a.rows, (int64_t)begin + a.chunk_rows);
   draw_u64 all = 0, above = 0;
   unsigned kept = 0;
-  auto segments = [&](auto cuts, auto floor) {             // with top-p; with min-p
-    constexpr bool CUTS = decltype(cuts)::value, FLOOR = decltype(floor)::value;
+  auto segments = [&](auto cuts, auto floors) {            // with top-p; with min-p
+    constexpr bool CUTS = decltype(cuts)::value, FLOOR = decltype(floors)::value;
     for (int64_t s = (int64_t)begin + wave * DRAW_SEGMENT; s < end; s += 4 * DRAW_SEGMENT) {
       const int64_t at = s + 8 * lane;
       draw_u64 sum = 0;
@@ -599,7 +604,7 @@ k_draw_weigh(DrawArgs a, int64_t first) {
             near[e] = __builtin_amdgcn_ballot_w64(bin >= low) & __builtin_amdgcn_ballot_w64(bin < high);
             if (FLOOR) above += in ? x : 0;                // before min-p: top-p goes by it
           }
-          if (FLOOR) in = in && x >= least;
+          if (FLOOR) in = in && v[e] >= floor;
           sum += in ? x : 0;
           kept += in;
         }
@@ -621,8 +626,8 @@ k_draw_weigh(DrawArgs a, int64_t first) {
     }
   };
   const std::true_type yes; const std::false_type no;
-  if (par.top_p < 2.f) { if (least) segments(yes, yes); else segments(yes, no); }
-  else { if (least) segments(no, yes); else segments(no, no); }
+  if (par.top_p < 2.f) { if (par.min_p > 0.f) segments(yes, yes); else segments(yes, no); }
+  else { if (par.min_p > 0.f) segments(no, yes); else segments(no, no); }
   all = draw_sum(all, slots);
   above = draw_sum(above, slots);
   kept = draw_sum(kept, (unsigned*)slots);
@@ -646,10 +651,12 @@ k_draw_rows(DrawArgs a, int64_t first) {
   __shared__ draw_u64 list[DRAW_LIST];
   __shared__ union { unsigned groups[2 * DRAW_FEW]; draw_u64 mass[2048]; } near;
   __shared__ unsigned listed, grouped;
+  __shared__ double drop;
   const int64_t q = first + blockIdx.x;
   const DrawParams par = draw_params(a, q);
   const int tid = threadIdx.x;
   if (tid == 0) { listed = 0; grouped = 0; }
+  if (tid < 64) drop = draw_drop(par);
   const DrawRow<TYPE> row(a, q);
   const DrawWhole whole = draw_whole(a, q, draw_depth_scale(par), lds.border.slots);
   if (tid == 0) a.undone[q] = 0;
@@ -722,7 +729,7 @@ k_draw_rows(DrawArgs a, int64_t first) {
     if (!slowly && n <= DRAW_SHORT) {
       if (tid < (int)n) lds.few.row[tid].place = list[tid];
       __syncthreads();
-      draw_short(a, q, lds.few, n, par, whole.best);
+      draw_short(a, q, lds.few, n, par, whole.best, drop);
       return;
     }
     if (!slowly) for (int s = tid; s < a.segments; s += 1024) mass[s] = 0;
@@ -776,18 +783,18 @@ k_draw_rows(DrawArgs a, int64_t first) {
       }, [&](unsigned k) { return kind == 1 ? w.of(k) : draw_one(); });
     }
     if (!slowly) {
-      const draw_u64 least = w.least(par.min_p);
+      const float floor = w.floor(drop);
       each([&](draw_u64 place) {
         if (place < cut) return;
+        if (draw_score((unsigned)(place >> 32)) < floor) return;
         const draw_u64 x = w.of((unsigned)(place >> 32));
-        if (x < least) return;
         ++kept;
         if (x) atomicAdd(&mass[~(unsigned)place / DRAW_SEGMENT], x);
       });
       kept = draw_sum(kept, (unsigned*)lds.border.slots);
       if (tid == 0 && a.num_kept) a.num_kept[q] = (int)kept;
       __syncthreads();
-      draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.border.slots);
+      draw_rows<TYPE>(a, q, row, w, cut, floor, mass, lds.border.slots);
     }
   }
   if (tid == 0) a.undone[q] = slowly;
@@ -833,7 +840,7 @@ k_draw_slowly(DrawArgs a, int64_t first) {
     cut = draw_border<false>(lds, a.rows, want ? want : 1, 0, [&](auto f) { each([&](draw_u64 place) { f(place >= top_k ? place : 0, [&] { return w.of((unsigned)(place >> 32)); }); }); },
                       [&](unsigned k) { return w.of(k); });
   }
-  const draw_u64 least = w.least(par.min_p);
+  const float floor = w.floor(draw_drop(par));
   unsigned kept = 0;
   for (int s = wave; s < a.segments; s += 16) {
     const int64_t c = (int64_t)s * DRAW_SEGMENT + 8 * lane;
@@ -842,7 +849,7 @@ k_draw_slowly(DrawArgs a, int64_t first) {
       unsigned key[8];
       row.keys((int)c, key);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) if (key[e] && draw_place(key[e], (unsigned)c + e) >= cut) { const draw_u64 x = w.of(key[e]); if (x >= least) { sum += x; ++kept; } }
+      for (int e = 0; e < 8; ++e) if (key[e] && draw_place(key[e], (unsigned)c + e) >= cut && draw_score(key[e]) >= floor) { sum += w.of(key[e]); ++kept; }
     }
     sum = draw_wave_sum(sum);
     if (lane == 0) mass[s] = sum;
@@ -850,7 +857,7 @@ k_draw_slowly(DrawArgs a, int64_t first) {
   kept = draw_sum(kept, (unsigned*)lds.slots);
   if (tid == 0 && a.num_kept) a.num_kept[q] = (int)kept;
   __syncthreads();
-  draw_rows<TYPE>(a, q, row, w, cut, least, mass, lds.slots);
+  draw_rows<TYPE>(a, q, row, w, cut, floor, mass, lds.slots);
 }
 
 // ------------------------------------------------------------------------------------------ launches -----

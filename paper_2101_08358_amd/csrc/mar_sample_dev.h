@@ -92,6 +92,13 @@ __device__ __forceinline__ DrawParams draw_params(const DrawArgs& a, int64_t q) 
   r.min_p = m > 0.f ? fminf(m, 1.f) : 0.f;
   return r;
 }
+// What a row may score below the best one for min-p to keep it; infinite: off, or an infinite temperature.  One wave finds it for all, before the first barrier: logarithm and
+// division in every wave took 1,000 x 16,000 with min-p from 36.4 to 38.0 us.
+__device__ __forceinline__ double draw_drop(const DrawParams& p) {
+  if (!(p.min_p > 0.f)) return __builtin_inf();
+  const double drop = -log((double)p.min_p) / p.inv_temperature;
+  return drop >= 0.0 ? drop : __builtin_inf();
+}
 // Ways of a query: rows picked from groups' maxima, or all rows weighed, with a histogram where top-p's border is looked for.
 __device__ __forceinline__ bool draw_few(const DrawArgs& a, const DrawParams& p) { return p.top_k > 0 && p.top_k <= DRAW_FEW && 2 * p.top_k <= a.groups; }
 __device__ __forceinline__ bool draw_all(const DrawArgs& a, const DrawParams& p) { return p.top_k == 0 || p.top_k >= a.rows; }
@@ -138,10 +145,11 @@ struct DrawWeights {
   __device__ __forceinline__ float log_prob(unsigned key, double log_sum) const {
     return (float)fmin(((double)draw_score(key) - top) * inv_temperature - log_sum, 0.0);
   }
-  // min-p's weight
-  __device__ __forceinline__ draw_u64 least(float min_p) const {
-    const draw_u64 best = draw_weight(0.0, shift);
-    return min_p >= 1.f ? best : (min_p > 0.f ? draw_share_up(min_p, best) : 0);
+  // The least score that min-p keeps, rounded up: it tells rows apart whose integers are 0 too.
+  __device__ __forceinline__ float floor(double drop) const {
+    const double least = fmax(top - drop, -(double)DRAW_TOP);
+    const float s = (float)least;
+    return (double)s < least ? draw_score(draw_key(s) + 1) : s;
   }
 };
 // approx: sum of weights relative to the best one, in fp32: the integers' sum

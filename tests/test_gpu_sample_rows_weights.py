@@ -34,3 +34,14 @@ def test_kept_rows_of_next_to_no_weight_can_be_drawn(V, top_k, tname):
     check(s, u, top_k=top_k)
     check(s, u, top_k=top_k, min_p=2.0 ** -60)
     check(s, u, top_k=top_k, top_p=0.5)
+
+
+@pytest.mark.parametrize("tname", TYPES)
+@pytest.mark.parametrize("V,top_k", WAYS + ((3000, 0), (16_384, 0), (16_385, 0), (40_001, 0)))
+def test_min_p_goes_by_the_weights_themselves(V, top_k, tname):
+    """Rows at e^-64 .. e^-60 weigh nothing as integers; min_p between them and those far below, and among them."""
+    s = steep(3, V, top_k or 70, 64.0, TYPES[tname][0])
+    u = torch.tensor([[0.5, 0.25]] * 3, device=DEV)
+    for min_p in (1e-30, 1e-37, 2e-27, 5e-27, 2.0 ** -149):
+        for f in (dict(), dict(top_p=0.9)):
+            check(s, u, top_k=top_k, min_p=min_p, **f)
