@@ -319,10 +319,13 @@ int mar_mxfp_rows(const uint8_t* codes, int64_t codes_stride, const uint8_t* sca
 
 /*
  * Scores of queries against every row of such a table: scores[i][j] = scale * (query_i . row_j), rounded to score_dtype.
- * The table's values are exact, products too, sums are held in fp32.  Queries: fp32 values are taken to 24 bits, bf16 and fp16 ones
- * to 19 bits, counted down from the largest magnitude of their block of 32 columns (fewer where that is below 2^-100),
- * MAR_DTYPE_MXFP4 ones (codes as above with query_scales) as they are.  A query with a value that is not finite
- * has scores NaN, and so has a row.
+ * The table's values are exact, products too, sums are held in fp32.  Queries: values are taken to 24 bits, counted down from the
+ * largest magnitude of their block of 32 columns: all of a bf16 value within 2^-16 of it, all of an fp16 value within 2^-13.  Where a
+ * block's magnitudes lie far apart (a value below 2^-22 of the largest, or half of them, eight at least, below 2^-6, or half of them
+ * below 2^-12) what that leaves over is taken to 24 bits again, up to three times, counted from its own largest: an outlier does not
+ * take its neighbours' bits.  Fewer bits where that largest is below 2^-100.  MAR_DTYPE_MXFP4 queries (codes as above with
+ * query_scales) enter as they are.  A query with a value that is not finite has scores NaN, and so has a row; a score whose sums leave
+ * fp32's range is infinite or NaN.
  *   queries, codes, scales, scores : device; query_scales: device, for MAR_DTYPE_MXFP4
  *   workspace : device, >= mar_mxfp_scores_workspace_bytes of the same problem, 256-byte aligned; calls that may overlap in time need
  *               one each

@@ -37,15 +37,18 @@ static inline int64_t mx_tiles(int64_t queries) { return (queries + 31) / 32; }
 struct MxPlan { bool few; int rt, stripes, parts, tiles_part, grid; };
 // Up to 32 queries: workgroups that stay, two a CU, of waves with their own stripes of 32 rt rows.  More: a workgroup a stripe of 256 rt rows
 // and part of the queries' tiles: one a CU at a time, estimated by the rounds of workgroups and their tiles, a workgroup's rows and first
-// images costing some two tiles.  (32 queries of 4,000,000 x 100: 164 us by the first way, 183 by the second; 1 of them: 57 and 118.)
+// images costing some two tiles.  (1 query of 2,000,000 x 400: 98 us by the first way, 148 by the second; 32 of them: 156 and 190; 32 queries of few or
+// narrow rows are as fast by the second: 2,000,000 x 100: 88 and 78.)
 //
 // rt, 32 rows a lane each, chosen by times of fp32 scores.  Up to 32 queries: 1 where the table is too short for more to fill the device
-// (32,000 x 100: 5.6 us with 1, 7.0 with 4; 64,000 x 400: 17 with 1, 13 with 2; 256,000 x 100: 9.3 and 8.7), 4 up to 192 columns, 2 beyond:
-// the rows ahead are held in registers.  More: 4 reads a quarter of the images and of their matrix operands for the same products, 1 has
-// workgroups enough for small calls and more of them loading rows where these are most of the bytes:
-//   999 x 120,007 x 400, fp32 queries    209 us with 1, 158 with 4      256 x 200,000 x 400   102 and 70       1,000 x 30,000 x 100   33 and 28
-//   256 x 100,000 x 100                   24 and 28                     64 x 60,000 x 100      11 and 14       64 x 2,000,000 x 128  131 and 145
-//   1,000 x 30,000 x 400, 4-bit queries   32 and 34                     4,096 x 12,000 x 400   44 and 48       256 x 500,000 x 400   155 and 139
+// (32,000 x 100: 5.0 us with 1, 7.1 with 4; 64,000 x 400: 6.4 with 1, 7.6 with 2), 4 up to 192 columns (1 query, 4,000,000 x 100: 77 with 1, 51 with
+// 4; 256,000 x 100: 7.6 and 7.9), 2 beyond, where the rows ahead take most registers and both are alike (32 queries, 40,000 x 400: 18 with 1,
+// 15 with 2; 4,000,000 x 400: 173 and 190).  More: 4 reads a quarter of the images
+// and of their matrix operands for the same products, 1 has workgroups enough for small calls and more of them loading rows where these are
+// most of the bytes, 2 is between them where many queries meet few rows (us with 1, 2 and 4; fp32 queries where nothing is said):
+//   999 x 120,007 x 400   192 162 160     256 x 200,000 x 400   102 - 70         256 x 100,000 x 100   24 26 27     64 x 2,000,000 x 64   129 116 121
+//   1,000 x 15,000 x 100  20.9 19.4 21.5  1,000 x 20,000 x 400  40.2 36.3 36.8   2,000 x 12,000 x 400  48 44 45     1,000 x 30,000 x 200  42 38 35
+//   4-bit queries: 4,096 x 15,000 x 400   49 39 43    2,000 x 30,000 x 200   38 37 31    1,000 x 30,000 x 400   30 30 32    256 x 500,000 x 400   150 133 132
 static inline MxPlan mx_plan(const mar_mxfp* p) {
   MxPlan r = {};
   const int64_t tiles = mx_tiles(p->num_queries);
@@ -58,7 +61,10 @@ static inline MxPlan mx_plan(const mar_mxfp* p) {
     return r;
   }
   const bool rows_first = tiles < 8 && nk <= 4, products_first = p->dtype != MAR_DTYPE_MXFP4 && (tiles >= 16 || nk > 4);
-  r.rt = !rows_first && p->num_rows * tiles >= (products_first ? 512 * 1024 : 2048 * 1024) ? 4 : 1;
+  const int64_t units = p->num_rows * tiles / 1024;
+  if (rows_first) r.rt = 1;
+  else if (products_first) r.rt = tiles >= 16 && units >= 384 && units < 896 ? 2 : (units >= 512 ? 4 : 1);
+  else r.rt = units >= (tiles >= 48 ? 1792 : 2048) ? 4 : (tiles >= 48 && units >= 1024 ? 2 : 1);
   r.stripes = (int)((p->num_rows + 256 * r.rt - 1) / (256 * r.rt));
   const int64_t slots = 256;
   int64_t best = INT64_MAX;
