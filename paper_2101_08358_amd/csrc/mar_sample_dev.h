@@ -412,11 +412,13 @@ static inline DrawLayout draw_layout(const mar_sampling* p) {
   // Groups: some 4,096 to 8,192, which stay in registers where they are looked through, and enough for a top-k of up to 2,048; a chunk's turns by
   // blocks where there are too few, neighbouring threads merged where there are too many (5 x 1,000,003, top-k 50: 80 us with 62,720, 26 with
   // 7,840), up to 256 rows (1 x 20,000,000, top-k 1,000: 210 us with 312 rows, 273 with 2,496).  A large top-k has the groups that reach its bound looked through again, and wants them smaller: at most eight turns (100 x 1,000,003,
-  // top-k 2,000: 248 -> 173 us).
+  // top-k 2,000: 248 -> 173 us), and twice as many as its rows, where there are so many turns.
   int64_t blocks = 4096 / (256 * L.chunks);
   if (p->top_k > 512) {
-    const int64_t more = 16384 / (256 * L.chunks);
-    blocks = blocks > more ? blocks : (more < turns / 8 ? more : turns / 8);
+    const int64_t more = 16384 / (256 * L.chunks), eighth = more < turns / 8 ? more : turns / 8;
+    const int64_t least = (2 * (p->top_k < DRAW_FEW ? p->top_k : DRAW_FEW) + 256 * L.chunks - 1) / (256 * L.chunks);
+    blocks = blocks > eighth ? blocks : eighth;
+    blocks = blocks > least ? blocks : least;
   }
   L.blocks = (int)(blocks < 1 ? 1 : (blocks > turns ? turns : blocks));
   L.merge = 1;
