@@ -100,7 +100,9 @@ __device__ __forceinline__ double draw_drop(const DrawParams& p) {
   return drop >= 0.0 ? drop : __builtin_inf();
 }
 // Ways of a query: rows picked from groups' maxima, or all rows weighed, with a histogram where top-p's border is looked for.
-__device__ __forceinline__ bool draw_few(const DrawArgs& a, const DrawParams& p) { return p.top_k > 0 && p.top_k <= DRAW_FEW && 2 * p.top_k <= a.groups; }
+// Picked: as many groups as top-k are enough for a bound; some G ln(1 / (1 - top_k / G)) rows reach it.
+__host__ __device__ inline bool draw_picks(int top_k, int groups) { return top_k > 0 && top_k <= DRAW_FEW && top_k <= groups; }
+__device__ __forceinline__ bool draw_few(const DrawArgs& a, const DrawParams& p) { return draw_picks(p.top_k, a.groups); }
 __device__ __forceinline__ bool draw_all(const DrawArgs& a, const DrawParams& p) { return p.top_k == 0 || p.top_k >= a.rows; }
 // Whose best score is infinite (or the largest float) goes by digits: the passes over all rows take their values as they are.
 __device__ __forceinline__ bool draw_infinite(unsigned best) { return best >= 0xff7fffffu; }

@@ -22,3 +22,28 @@ def test_large_top_k_of_batches(Q, V, top_ks):
     for k in top_ks:
         check_some(s, u, (0, Q // 2, Q - 1), top_k=k)
         check_some(s, u, (1, Q - 2), top_k=k, top_p=0.9)
+
+
+@pytest.mark.parametrize("V,top_ks", ((16_385, (1024, 1025, 1500, 2047, 2048)), (17_000, (1152, 1153, 2048)), (20_001, (1281, 2000)), (30_000, (1920, 1921, 2048))))
+def test_large_top_k_of_few_rows(V, top_ks):
+    """As few groups as eight rows each make."""
+    for dt in (torch.float32, torch.bfloat16):
+        s = scores_of(V, 3, V, dt)
+        for k in top_ks:
+            check(s, uniforms_of(V, 3, 5), top_k=k)
+            check(s, uniforms_of(V, 3, 5), top_k=k, top_p=0.95, min_p=0.001)
+
+
+def test_large_top_k_where_few_rows_count():
+    """Fewer groups with a row that counts than top-k; and as many rows as top-k."""
+    V = 20_000
+    g = np.random.default_rng(1)
+    allowed = np.zeros((4, V), dtype=bool)
+    allowed[0, :900] = True
+    allowed[1, g.permutation(V)[:1500]] = True
+    allowed[2, g.permutation(V)[:2100]] = True
+    allowed[3, 12_000:14_000] = True
+    s = scores_of(5, 4, V, torch.float32)
+    for k in (1000, 1500, 2000, 2048):
+        check(s, uniforms_of(5, 4, 6), allowed, top_k=k)
+        check(s, uniforms_of(5, 4, 6), allowed, top_k=k, top_p=0.8)
