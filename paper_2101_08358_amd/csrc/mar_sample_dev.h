@@ -430,7 +430,7 @@ static inline DrawLayout draw_layout(const mar_sampling* p) {
   // Of normal scores the border's range, a bin or two, holds up to 1 in 120 rows with bins as fine as they allow, more with 32 a binary order of
   // magnitude (rows far below all others): 1 / 58 over the deviation.  A workgroup holds 8,192 of them, the rest stays in memory (100 x 1,000,003,
   // deviation 0.67: 3.5 ms where all had to fit a workgroup, 0.29).
-  L.list = (int)(p->num_rows / 16 < DRAW_LIST ? p->num_rows / 16 : (p->num_rows / 32 < DRAW_LIST ? DRAW_LIST : p->num_rows / 32));
+  L.list = (int)(p->num_rows / 32 < DRAW_LIST ? DRAW_LIST : p->num_rows / 32);
   L.stats = take(Q * L.chunks * sizeof(DrawChunk));
   L.maxima = take(Q * L.groups * 4);
   L.hist = take(Q * L.chunks * DRAW_BINS * 4);

@@ -47,3 +47,19 @@ def test_large_top_k_where_few_rows_count():
     for k in (1000, 1500, 2000, 2048):
         check(s, uniforms_of(5, 4, 6), allowed, top_k=k)
         check(s, uniforms_of(5, 4, 6), allowed, top_k=k, top_p=0.8)
+
+
+@pytest.mark.parametrize("V", (16_385, 17_000, 40_000))
+@pytest.mark.parametrize("equal", (1023, 1024, 1100, 2500, 2501, 8192, 8193))
+def test_equal_rows_at_the_border_of_top_p_of_few_rows(V, equal):
+    """More of them than a sixteenth of the rows, up to more than a workgroup's list holds."""
+    g = np.random.default_rng(equal + V)
+    s = np.full((3, V), -25.0, dtype=np.float32)
+    for q in range(3):
+        at = g.permutation(V)[:equal + 1]
+        s[q, at] = 1.0
+        s[q, at[0]] = 1.0 + np.log(equal)
+    s = torch.from_numpy(s).to(DEV)
+    for top_p in (0.4999, 0.75, 0.999):
+        check(s, uniforms_of(equal, 3, 8), top_p=top_p)
+    check(s, uniforms_of(equal, 3, 8), top_p=0.75, temperature=0.9, min_p=0.5 / equal)
