@@ -40,11 +40,17 @@ __device__ __forceinline__ DrawWhole draw_whole(const DrawArgs& a, int64_t q, fl
   return r;
 }
 
-// Bins to a binary order of magnitude: 32, doubled as long as all rows that count fit, so that flat scores spread over the bins as well (100 x
-// 1,000,003 in 16 bits, scores over the temperature of deviation 0.2: 3.4 ms for the call with 32, all of whose bins' rows no
-// list holds, and 0.28).
+// Bins to a binary order of magnitude: 32, doubled as long as all rows that weigh something beside the best fit, so that flat scores spread over the bins
+// as well (100 x 1,000,003 in 16 bits, scores over the temperature of deviation 0.2: 3.4 ms for the call with 32, all of whose bins' rows no
+// list holds, and 0.28).  Rows 63 binary orders below have no say, one or many (deviation 0.05 and one row at -1e9, which had 32 bins taken: 6.6
+// ms and 0.29).
 __device__ __forceinline__ float draw_fine(const DrawArgs& a, int64_t q, float c, unsigned best, draw_u64* slots) {
-  unsigned low = (int)threadIdx.x < a.chunks ? a.stats[q * a.chunks + threadIdx.x].low : 0;
+  unsigned low = 0;
+  if ((int)threadIdx.x < a.chunks) {
+    const DrawChunk s = a.stats[q * a.chunks + threadIdx.x];
+    const float from = draw_score(best) - draw_window(c);
+    if (s.low && draw_score(s.best) >= from) low = ~draw_key(fmaxf(draw_score(~s.low), from));
+  }
   low = draw_reduce(low, (unsigned*)slots, DrawMax());
   const float depth = draw_depth(draw_score(best), draw_score(~low), c);
   float span = 63.f / 2, fine = 32.f;
@@ -456,6 +462,7 @@ k_draw_scan(DrawArgs a, int64_t first) {
   const bool sums = !few && draw_all(a, par) && par.top_p >= 2.f;
   const bool lows = !few && draw_all(a, par) && par.top_p < 2.f;
   float best = -__builtin_inff(), low = __builtin_inff(), sum = 0.f, group = best;
+  const float window = draw_window(c);
   const int width = 256 / a.merge;
   unsigned* maxima = a.maxima + q * a.groups + (int64_t)chunk * a.blocks * width + tid / a.merge;
   const bool first_of = tid % a.merge == 0;
@@ -470,15 +477,17 @@ k_draw_scan(DrawArgs a, int64_t first) {
       here = fminf(here, DRAW_TOP);
       group = fmaxf(group, here);
       if (lows) {                                          // uniform
+        // of rows within the window of the best so far; where that leaves it behind what came before is forgotten, or ends at its edge
+        const float from = fmaxf(best, here) - window;
         float least = DRAW_TOP;
 #pragma unroll
         for (int e = 0; e < 8; ++e) least = fminf(least, v[e]);
-        if (!(least > -__builtin_inff())) {                // some do not count
-          least = DRAW_TOP;
+        if (!(least > -__builtin_inff() && least >= from)) {       // some do not count, or weigh nothing
+          least = __builtin_inff();
 #pragma unroll
-          for (int e = 0; e < 8; ++e) least = fminf(least, v[e] > -__builtin_inff() ? v[e] : DRAW_TOP);
+          for (int e = 0; e < 8; ++e) least = fminf(least, v[e] > -__builtin_inff() && v[e] >= from ? v[e] : __builtin_inff());
         }
-        low = fminf(low, least);
+        low = fminf(best >= from ? fmaxf(low, from) : __builtin_inff(), least);
       }
       if (sums) {
         if (here > best) sum = sum > 0.f ? sum * __builtin_amdgcn_exp2f(-draw_depth(here, best, c)) : 0.f;
@@ -502,7 +511,11 @@ k_draw_scan(DrawArgs a, int64_t first) {
   const unsigned mine = draw_key(best), all = draw_reduce(mine, (unsigned*)slots, DrawMax());
   sum = mine ? sum * __builtin_amdgcn_exp2f(-draw_depth(draw_score(all), best, c)) : 0.f;
   sum = draw_sum(sum, (float*)slots);
-  const unsigned least = draw_reduce(lows && mine ? ~draw_key(low) : 0u, (unsigned*)slots, DrawMax());
+  unsigned least = 0;
+  if (lows && all) {                                       // uniform
+    const float from = draw_score(all) - window;
+    least = draw_reduce(mine && best >= from ? ~draw_key(fmaxf(low, from)) : 0u, (unsigned*)slots, DrawMax());
+  }
   if (tid == 0) {
     a.stats[q * a.chunks + chunk] = {all, least, sum};
     if (chunk == 0) a.listed[q] = 0;

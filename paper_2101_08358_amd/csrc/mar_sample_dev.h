@@ -50,8 +50,8 @@ __device__ __forceinline__ draw_u64 draw_place(unsigned key, unsigned id) { retu
 #define DRAW_LIST 8192              // rows of a border that a workgroup holds
 #define DRAW_LIST_CHUNK 2048        // of one chunk
 
-// Of a chunk: greatest key (0: no row counts), complement of the least one (0: not looked for), sum of weights relative to the best (where no histogram
-// gives it).
+// Of a chunk: greatest key (0: no row counts), complement of the least one that weighs something beside it (0: not looked for), sum of weights
+// relative to the best (where no histogram gives it).
 struct DrawChunk { unsigned best, low; float sum; };
 // Of a query, after the histogram: bins below `low` lie above top-p's border, bins above `high` below it; the sum of weights.
 struct DrawRange { int low, high; float sum; };
@@ -161,6 +161,8 @@ __device__ __forceinline__ DrawWeights draw_weights(unsigned best, const DrawPar
 }
 // The same in fp32 and binary orders of magnitude below the best, for sums that only choose a scale or a range of bins.
 __device__ __forceinline__ float draw_depth(float top, float s, float c) { return fminf(top - s, DRAW_TOP) * c; }
+// What scores further below the best weigh less than 2^-63 of it.
+__device__ __forceinline__ float draw_window(float c) { return 63.f / c; }
 __device__ __forceinline__ float draw_depth_scale(const DrawParams& p) { return (float)fmin(p.inv_temperature * 1.4426950408889634, 3e38); }
 __device__ __forceinline__ draw_u64 draw_one() { return 1; }
 

@@ -63,3 +63,19 @@ def test_equal_rows_at_the_border_of_top_p_of_few_rows(V, equal):
     for top_p in (0.4999, 0.75, 0.999):
         check(s, uniforms_of(equal, 3, 8), top_p=top_p)
     check(s, uniforms_of(equal, 3, 8), top_p=0.75, temperature=0.9, min_p=0.5 / equal)
+
+
+@pytest.mark.parametrize("spread", (0.05, 0.3))
+@pytest.mark.parametrize("far", (-30.0, -1e4, -60_000.0))
+@pytest.mark.parametrize("how", ("one", "few", "half", "first", "nearly all"))
+def test_flat_scores_with_others_far_below(how, far, spread):
+    """Soft masks: finite scores far below, alone, spread, in one piece, nearly everywhere; beside rows that do not count."""
+    V = 200_003
+    g = np.random.default_rng(4)
+    soft = {"one": np.arange(V) == V // 3, "few": g.random(V) < 0.0005, "half": g.random(V) < 0.5, "first": np.arange(V) < 120_000, "nearly all": g.random(V) < 0.97}[how]
+    s = scores_of(3, 3, V, torch.float32, spread=spread)
+    s[:, torch.from_numpy(soft).to(DEV)] = far
+    s[2, ::7] = -float("inf")
+    for f in (dict(top_p=0.9), dict(top_p=0.4, min_p=0.5), dict(top_p=0.9, temperature=0.02), dict(top_p=0.9, temperature=50.0)):
+        check(s, uniforms_of(9, 3, 4), **f)
+        check(s.half(), uniforms_of(9, 3, 4), **f)
