@@ -435,7 +435,8 @@ static inline DrawLayout draw_layout(const mar_sampling* p) {
   L.list = (int)(p->num_rows / 32 < DRAW_LIST ? DRAW_LIST : p->num_rows / 32);
   L.stats = take(Q * L.chunks * sizeof(DrawChunk));
   L.maxima = take(Q * L.groups * 4);
-  L.hist = take(Q * L.chunks * DRAW_BINS * 4);
+  const size_t hists = Q * L.chunks * DRAW_BINS * 4, lists = Q * L.list * 8;
+  L.hist = L.lists = take(hists > lists ? hists : lists);  // lists are written when the histograms have been read, by an earlier kernel
   L.hist_bits = 16;                                        // a bin's sum of a chunk stays below 2^32
   while ((int64_t)L.chunk_rows << L.hist_bits >= 1ll << 32) --L.hist_bits;
   L.range = take(Q * sizeof(DrawRange));
@@ -443,7 +444,6 @@ static inline DrawLayout draw_layout(const mar_sampling* p) {
   L.kept = take(Q * L.chunks * 4);
   L.listed = take(Q * 4);
   L.undone = take(Q * 4);
-  L.lists = take(Q * L.list * 8);
   L.mass_pitch = (L.segments + 15) / 16 * 16;              // lines of 128 bytes
   L.mass = take(Q * L.mass_pitch * 8);
   L.bytes = at;

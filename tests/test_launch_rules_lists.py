@@ -15,3 +15,20 @@ def test_list_of_a_border(tmp_path):
     }
   printf("%ld", bad);""")
     assert out[0] == "0", out
+
+
+def test_workspace_of_a_batch(tmp_path):
+    """Histograms and lists take turns in the same memory: no more than the larger of them beside sums, maxima and a few words a query."""
+    out = _run(tmp_path, "mar_sample_dev.h", """
+  long bad = 0;
+  for (int64_t rows : {(int64_t)16385, (int64_t)100000, (int64_t)1000003, (int64_t)50000000})
+    for (int64_t queries : {1, 100, 1000}) {
+      mar_sampling p = {};
+      p.num_rows = rows; p.num_queries = (int)queries;
+      const DrawLayout L = draw_layout(&p);
+      const size_t hists = queries * L.chunks * DRAW_BINS * 4, lists = queries * L.list * 8;
+      const size_t others = queries * (L.chunks * (sizeof(DrawChunk) + 20) + L.groups * 4 + sizeof(DrawRange) + 8 + L.mass_pitch * 8) + 10 * 256;
+      if (L.bytes > (hists > lists ? hists : lists) + others) ++bad;
+    }
+  printf("%ld", bad);""")
+    assert out[0] == "0", out
