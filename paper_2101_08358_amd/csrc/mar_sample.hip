@@ -121,8 +121,8 @@ __device__ __forceinline__ void draw_short(const DrawArgs& a, int64_t q, DrawSho
   for (unsigned i = part; i < padded; i += 4) rank += lds.row[i].place > mine;
   rank = joined(rank);
   const bool top = part == 0 && r < n && rank < (unsigned)par.top_k;
-  const float weighs = top ? __builtin_amdgcn_exp2f(-draw_depth(draw_score(best), draw_score((unsigned)(mine >> 32)), draw_depth_scale(par))) : 0.f;
-  const DrawWeights w = draw_weights(best, par, draw_sum(weighs, (float*)lds.slots));  // behind its barriers the rows have been read
+  const unsigned weighs = top ? draw_part(draw_score(best), (unsigned)(mine >> 32), draw_depth_scale(par)) : 0;
+  const DrawWeights w = draw_weights(best, par, draw_parts(draw_sum(weighs, (unsigned*)lds.slots)));         // behind its barriers the rows have been read
   if (top) lds.row[rank].place = mine;
   __syncthreads();
   const unsigned m = min(n, (unsigned)par.top_k), padded_m = (m + 15) & ~15u;
@@ -339,9 +339,9 @@ k_draw_small(DrawArgs a, int64_t first) {
           draw_u64 want = k;
           const draw_u64 last = cut;
           if (kind == 1) {
-            float approx = 0.f;
-            each([&](draw_u64 p) { approx += p >= last ? __builtin_amdgcn_exp2f(-draw_depth(top, draw_score((unsigned)(p >> 32)), c)) : 0.f; });
-            w = draw_weights(best, par, draw_sum(approx, (float*)slots));
+            unsigned parts = 0;
+            each([&](draw_u64 p) { parts += p >= last ? draw_part(top, (unsigned)(p >> 32), c) : 0; });
+            w = draw_weights(best, par, draw_parts(draw_sum(parts, (unsigned*)slots)));
             if (par.top_p >= 2.f) break;
             draw_u64 sum = 0;
             each([&](draw_u64 p) { sum += p >= last ? w.of((unsigned)(p >> 32)) : 0; });
@@ -446,7 +446,7 @@ k_draw_small(DrawArgs a, int64_t first) {
 
 // ------------------------------------------------------------------------------------------ more rows -----
 // A workgroup a chunk of a query.  Group (chunk, block b, i): the columns of threads merge i .. merge i + merge - 1 in the iterations of block b.  Bound by memory: 100 x
-// 1,000,003 bf16: 36 us, 5.5 TB/s (part of the scores comes out of the last-level cache); 64 x 131,072 fp32: 7 to 10 us.
+// 1,000,003 bf16: 38 us, 5.3 TB/s (part of the scores comes out of the last-level cache); 64 x 131,072 fp32: 7 to 10 us.
 template <int TYPE>
 __global__ void __launch_bounds__(256)
 k_draw_scan(DrawArgs a, int64_t first) {
@@ -522,7 +522,7 @@ k_draw_scan(DrawArgs a, int64_t first) {
   }
 }
 
-// Other queries with top-p: a chunk's weights by their bins.  18 instructions and an addition in LDS an element: 100 x 1,000,003: 58 us, bound
+// Other queries with top-p: a chunk's weights by their bins.  20 instructions and an addition in LDS an element: 100 x 1,000,003: 58 us, bound
 // by those.
 template <int TYPE>
 __global__ void __launch_bounds__(256)
@@ -572,7 +572,7 @@ k_draw_range(DrawArgs a, int64_t first) {
   if (tid == 0) a.range[q] = range;
 }
 
-// Integer weights of a chunk.  Bound by the issue of vector instructions: 49 a weight, of which 10 are the polynomial's; 100 x 1,000,003: 156 us.
+// Integer weights of a chunk.  Bound by the issue of vector instructions: 50 a weight, of which 10 are the polynomial's; 100 x 1,000,003: 159 us.
 template <int TYPE>
 __global__ void __launch_bounds__(256)
 k_draw_weigh(DrawArgs a, int64_t first) {
@@ -656,7 +656,7 @@ k_draw_weigh(DrawArgs a, int64_t first) {
 }
 
 // A workgroup a query.  A chain of short steps with barriers between them, bound by their latency: 64 queries of 131,072 rows: without filters
-// 9 us, top-k 50: 14, top-k 300: 20, top-k 1,000 and top-p 0.9: 31, top-p alone: 15; 100 of 1,000,003, top-p alone: 27.
+// 9 us, top-k 50: 14, top-k 300: 20, top-k 1,000 and top-p 0.9: 32, top-p alone: 15; 100 of 1,000,003, top-p alone: 27.
 template <int TYPE>
 __global__ void __launch_bounds__(1024)
 k_draw_rows(DrawArgs a, int64_t first) {
@@ -774,9 +774,9 @@ k_draw_rows(DrawArgs a, int64_t first) {
       if (kind == 1) {
         if (few) {
           const float top = draw_score(whole.best), c = draw_depth_scale(par);
-          float approx = 0.f;
-          each([&](draw_u64 place) { approx += place >= last && place ? __builtin_amdgcn_exp2f(-draw_depth(top, draw_score((unsigned)(place >> 32)), c)) : 0.f; });
-          w = draw_weights(whole.best, par, draw_sum(approx, (float*)lds.border.slots));
+          unsigned parts = 0;
+          each([&](draw_u64 place) { parts += place >= last && place ? draw_part(top, (unsigned)(place >> 32), c) : 0; });
+          w = draw_weights(whole.best, par, draw_parts(draw_sum(parts, (unsigned*)lds.border.slots)));
         }
         if (!cuts) break;
         draw_u64 sum = 0;

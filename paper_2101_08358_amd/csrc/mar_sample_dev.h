@@ -164,6 +164,9 @@ __device__ __forceinline__ float draw_depth(float top, float s, float c) { retur
 // What scores further below the best weigh less than 2^-63 of it.
 __device__ __forceinline__ float draw_window(float c) { return 63.f / c; }
 __device__ __forceinline__ float draw_depth_scale(const DrawParams& p) { return (float)fmin(p.inv_temperature * 1.4426950408889634, 3e38); }
+// A weight relative to the best in units of 2^-18, and the sum of up to 8,192 of them: the same whatever order a list's rows have got.
+__device__ __forceinline__ unsigned draw_part(float top, unsigned key, float c) { return (unsigned)(__builtin_amdgcn_exp2f(-draw_depth(top, draw_score(key), c)) * 0x1p18f); }
+__device__ __forceinline__ float draw_parts(unsigned sum) { return (float)sum * 0x1p-18f; }
 __device__ __forceinline__ draw_u64 draw_one() { return 1; }
 
 // Sums and maxima by lane exchanges within a wave, zeros beyond its ends.

@@ -79,3 +79,21 @@ def test_flat_scores_with_others_far_below(how, far, spread):
     for f in (dict(top_p=0.9), dict(top_p=0.4, min_p=0.5), dict(top_p=0.9, temperature=0.02), dict(top_p=0.9, temperature=50.0)):
         check(s, uniforms_of(9, 3, 4), **f)
         check(s.half(), uniforms_of(9, 3, 4), **f)
+
+
+@pytest.mark.parametrize("V,top_k", ((5000, 100), (16_000, 2023), (40_000, 240), (40_000, 2023), (200_000, 3000)))
+def test_the_same_bits_again(V, top_k):
+    """Rows whose weights sum to a power of two, but for roundings: the integers' scale does not follow the order in which rows are listed."""
+    g = np.random.default_rng(V)
+    s = np.full((4, V), -40.0, dtype=np.float32) - g.random((4, V)).astype(np.float32)
+    ones = 1023 if top_k > 1000 else 63
+    for q in range(4):
+        at = g.permutation(V)[:top_k]
+        s[q, at[:ones]] = 3.0
+        s[q, at[ones:]] = 3.0 - np.log(top_k - ones) + (q - 1.5) * 2.0 ** -20
+    s = torch.from_numpy(s).to(DEV)
+    u = uniforms_of(V, 4, 200)
+    for f in (dict(top_k=top_k), dict(top_k=top_k, top_p=0.9995)):
+        want = check(s, u, **f)
+        for _ in range(20):
+            assert all(torch.equal(a, b) for a, b in zip(sample(s, u, **f), want))
