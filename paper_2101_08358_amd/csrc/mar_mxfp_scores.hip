@@ -49,7 +49,6 @@ template <typename J> __device__ __forceinline__ int mx_joined(int v, J join) {
 }
 struct MxMax { __device__ __forceinline__ int operator()(int x, int y) const { return max(x, y); } };
 struct MxAdd { __device__ __forceinline__ int operator()(int x, int y) const { return x + y; } };
-struct MxOr { __device__ __forceinline__ int operator()(int x, int y) const { return x | y; } };
 // What remains of values o 2^unit after the slices of an image, and so on `level` times: v, the largest of the block in [8, 16) 2^20 again (or all 0), the
 // new unit, and a bit for each value of which something remains.  What slices hold is o 2^grid rounded to an integer, grid that of the last
 // slice, whatever the images before.
@@ -98,8 +97,8 @@ __device__ __forceinline__ MxPiece<TYPE> mx_take(const MxArgs& a, int64_t q, int
 // Writes the slices of what `level` images left over of a piece.
 // Returns whether the block is wide and leaves something over: a value is below 2^-22 of the largest, or half of them, eight at least, below
 // 2^-6 of it, or half of them below 2^-12.  So most values of a block that is not wide keep 12 to 18 bits of their own, and none vanishes;
-// 16-bit values do not leave anything over within 2^-16 (bf16) and 2^-13 (fp16).  Products of normal variables (two embeddings), whose
-// magnitudes crowd at 0, have a wide step of 64 columns and 32 queries in some 2 of 100, normal ones in 1 of 1,000.
+// 16-bit values do not leave anything over within 2^-16 (bf16) and 2^-13 (fp16).  Of steps of 64 columns and 32 queries, products of
+// normal variables (two embeddings), whose magnitudes crowd at 0, have one that is wide in 100, normal variables fewer than one in 1,000.
 template <int TYPE, int NK>
 __device__ __forceinline__ bool mx_pack(const MxPiece<TYPE>& taken, int level, int piece, char* image) {
   constexpr int NS = mx_slices_of(TYPE);

@@ -115,3 +115,50 @@ def test_values_that_are_not_finite_beside_outliers(kind):
         bad[[1, 3, T - 1]] = True
         assert torch.equal(torch.isnan(got).all(1).cpu(), bad) and torch.equal(torch.isnan(got).any(1).cpu(), bad)
         check(np.where(bad.numpy()[:, None], 0.0, x), codes, scales, kind)
+
+
+@pytest.mark.parametrize("kind", ("fp32", "bf16", "fp16"))
+@pytest.mark.parametrize("T", (1, 9, 32, 40, 100))
+def test_captured_with_other_queries_later(T, kind):
+    """A graph captured with ordinary queries serves others that have outliers, and ordinary ones again; its workspace holds anything."""
+    g = np.random.default_rng(T)
+    V, dim = 900, 200
+    codes, scales_ = rows_without(g, V, dim, (3, 70))
+    c, s = torch.from_numpy(codes).to(DEV), torch.from_numpy(scales_).to(DEV)
+    q = torch.zeros((T, dim), dtype=TYPES[kind][0], device=DEV)
+    out = torch.zeros((T, V), device=DEV)
+    p = mar.MarMxfp(V, codes.shape[1], scales_.shape[1], dim, 0, V, T, dim, TYPES[kind][1], mar.DTYPE_FP32, 1.0, 0)
+    ws = torch.zeros(mar.mar_mxfp_scores_workspace_bytes(p) + 256, dtype=torch.uint8, device=DEV)
+
+    def call():
+        mar.mar_mxfp_scores(p, q, None, c, s, out, ws, ws.numel() - 256)
+
+    def queries(turn):
+        x = torch.randn((T, dim), generator=torch.Generator().manual_seed(turn))
+        if turn % 2:
+            x[::2, 3] *= 2.0 ** 12
+            x[::3, 70] *= 2.0 ** 12
+        return x.to(q.dtype)
+
+    q.copy_(queries(0))
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for turn in range(1, 6):
+        q.copy_(queries(turn))
+        call()
+        torch.cuda.synchronize()
+        want = out.clone()
+        out.zero_()
+        ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and (ws[-256:] == 0xFF).all()
+        x = q.double().cpu().numpy()
+        w = mu.values(codes, scales_, dim)
+        # sums as in check.  Half of the values of a block that is not wide are 2^-6 of its largest or more, and hardly one half of 32 normal values
+        # is above 2: such a block's largest is below 2^7, and 2^-24 of that is cut off a value at most; a wide one's remainder is less
+        bound = np.abs(x) @ np.abs(w).T * (2 * 4 * 4 + 4) * 2.0 ** -23 * (32 / 31) + 2.0 ** -17 * np.abs(w).sum(1)
+        assert (np.abs(want.double().cpu().numpy() - x @ w.T) <= bound).all()
