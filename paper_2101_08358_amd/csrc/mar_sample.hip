@@ -1,8 +1,9 @@
 // Rows drawn from scores with temperature, top-k, top-p and min-p (gfx950).
 //
 // A row's place in the order (score descending, id ascending) is one number, so that every filter is a cut: rows whose place is not below it
-// are kept.  Weights are integers W = round(2^n exp((s - max) / temperature)), n such that the sum of those that top-k leaves lies below
-// 2^61 (their own sum in fp32 says which, whatever way a query goes): sums are exact in any order, and a border (top-p's, a draw's) falls where the integers say, whatever way found it.
+// are kept.  Weights are integers W = round(2^n exp((s - max) / temperature)), n such that the sum of those that top-k leaves lies between
+// 2^60 and 2^61 (which their sum in 32 bits says, whatever way a query goes): sums are exact in any order, and a border (top-p's, a draw's) falls
+// where the integers say, whatever way found it.
 //
 // Up to 16,384 rows (k_draw_small): a workgroup a query holds them in registers (one query of 4,000 to 16,000 rows, no filter: 10 us; by the kernels
 // below 18 to 20; 1,000 queries of 16,000 rows: 35 and 72).  More:

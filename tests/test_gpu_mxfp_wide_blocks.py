@@ -57,13 +57,10 @@ def test_a_large_value_beside_ones(kind):
     assert (got.double() == 31 * small).all()
 
 
-@pytest.mark.parametrize("kind", ("fp32", "bf16", "fp16"))
 @pytest.mark.parametrize("dim", (32, 50, 75, 128, 200, 400))
-@pytest.mark.parametrize("power", (7, 10, 13, 20, 40, 100, 200))
-def test_outliers_do_not_take_their_neighbours_bits(dim, power, kind):
+@pytest.mark.parametrize("kind,power", [(k, p) for k in ("fp32", "bf16", "fp16") for p in (7, 10, 13, 20, 40, 100, 200) if k != "fp16" or p <= 13])
+def test_outliers_do_not_take_their_neighbours_bits(dim, kind, power):
     """A value or two 2^power times the others, in some blocks of some queries."""
-    if kind == "fp16" and power > 13:
-        pytest.skip("beyond fp16's range")
     g = np.random.default_rng(dim + power)
     V = 700
     columns = [c for c in (3, 17, 40, 130, 131, 350) if c < dim]
