@@ -355,8 +355,8 @@ int mar_mxfp_scores(const mar_mxfp* problem, const void* queries, const uint8_t*
  * w_j = exp((s_ij - s_i,best) / temperature).  Kept are the rows of rank below top_k whose predecessors' weights sum to less than
  * top_p times the sum of the first top_k ones, and that weigh at least min_p.  Draw n of query i is the first kept row, by id, at
  * which the kept rows' running sum of weights exceeds uniforms[i][n] times their whole sum.
- * Weights are integers, from exponentials in 64 bits, whose sum over the first top_k rows has 60 to 61 bits (fewer at an infinite
- * temperature, where all weigh alike): sums are exact, whatever their order, and results depend on the arguments alone.
+ * Weights are integers, from exponentials in 64 bits, whose sum over the first top_k rows has 60 to 61 bits: sums are exact, whatever
+ * their order, and results depend on the arguments alone.
  *   scores      : device, [num_queries] rows of num_rows values
  *   allowed     : device, or NULL (all rows): bits as in mar_log_probs
  *   temperatures, top_ks, top_ps, min_ps : device, [num_queries], each may be NULL: then the problem's value serves all queries.
